@@ -16,6 +16,15 @@
  *   fc_chunk_cache_apply  chunks that were not recomputed are served from the
  *                         activation cache (Sec. 3.2)
  *
+ * Four more calls, not in the paper, make the queries and keys that the store holds
+ * and keep its clean region in 4 bits:
+ *
+ *   fc_qk_norm_rope         norms of queries and keys per head and the rotation over
+ *                           (time, height, width), in one pass
+ *   fc_kv4_pack             rows into a 4-bit store, gathered through a kept list
+ *   fc_kv4_unpack           rows of a 4-bit store as plain rows (what fc_kv_score reads)
+ *   fc_chunk_attention_kv4  fc_chunk_attention over [4-bit clean region | window]
+ *
  * Conventions
  *   - Plain C types only.  Every pointer argument says whether it is a HOST or a
  *     DEVICE pointer.  The caller owns every buffer, including the workspace,
@@ -71,7 +80,8 @@ typedef enum { FC_POLICY_CHUNKWISE = 0, FC_POLICY_UNIFORM = 1 } fc_policy;
 enum {
   FC_DEV_TIMEOUT = 1u,   /* a bounded in-kernel wait expired; the affected outputs are invalid */
   FC_DEV_NAN_SCORE = 2u, /* a NaN score was ranked as -inf by the selection */
-  FC_DEV_BAD_INDEX = 4u  /* an index read from device memory was out of range and was skipped */
+  FC_DEV_BAD_INDEX = 4u, /* an index read from device memory was out of range and was skipped */
+  FC_DEV_NONFINITE = 8u  /* an infinity or a NaN was packed into a 4-bit store (its group of elements reads as NaN) */
 };
 
 enum { FC_MAX_CHUNKS = 64, FC_MAX_SEGMENTS = 64 };
@@ -337,6 +347,131 @@ int fc_kv_select_compact_ex(fc_ctx* ctx, void* stream, const float* score, int n
                             const fc_select_opts* opts, const void* K_src, const void* V_src, void* K_dst,
                             void* V_dst, int dtype, int d, const fc_compact_strides* strides, int32_t* kept_idx,
                             int32_t* n_kept, uint32_t* status, void* ws, size_t ws_bytes);
+
+/* ------------------------------------------------------------------------------------------
+ * fc_qk_norm_rope — RMS norms of queries and keys for each head and the position rotation over
+ * several axes, in one pass.
+ *
+ * Not in the paper, whose method starts from given Q and K; the models it runs on make them this way.
+ * For every token n and head, with x the head's d elements (fp32 throughout, one rounding to `dtype`):
+ *     y = x * w / sqrt(mean(x^2) + eps)                      norm = FC_NORM_RMS; w = 1 where the weight is NULL
+ *     y = x                                                  norm = FC_NORM_NONE
+ * The first axis_dim[0] elements turn with the token's position on axis 0 (time), the next axis_dim[1]
+ * with axis 1 (height), the next axis_dim[2] with axis 2 (width); elements behind them pass through.
+ * Pair i of a section of n elements is (2i, 2i+1) (FC_ROPE_PAIRS) or (i, i + n/2) (FC_ROPE_HALVES):
+ *     (y0, y1) <- (y0 cos a - y1 sin a, y0 sin a + y1 cos a),   a = position * theta^(-2i/n)
+ * The angle is reduced in 64-bit fixed point, so that it is as exact at position 2^31 as at 1.  Negative
+ * positions turn back: the rotation by -p undoes the rotation by p, and the rotation of an already
+ * rotated key by (new - old) position moves it there.
+ *
+ *   Q, Q_out         DEVICE [H_q, T, d], K, K_out DEVICE [H_kv, T, d]; `dtype` elements with the strides of the
+ *                    descriptor (any order of heads and tokens, e.g. slices of a fused projection).  H_q or
+ *                    H_kv may be 0 (its pointers are then ignored), T too.  An output may be its own input (same pointer
+ *                    and strides); other overlap is not allowed.
+ *   q_weight, k_weight  DEVICE [d] fp32 or NULL; ignored for FC_NORM_NONE.
+ *   pos              DEVICE [T, 3] int32, contiguous, or NULL: token n then stands at
+ *                    (grid_t0 + n / (grid_h grid_w), n / grid_w % grid_h, n % grid_w).
+ *   inv_freq         HOST [sum of axis_dim / 2] double or NULL: the pairs' radians per position in place of theta^(-2i/n),
+ *                    section by section.
+ * Needs no workspace. */
+typedef enum { FC_NORM_NONE = 0, FC_NORM_RMS = 1 } fc_norm;
+typedef enum { FC_ROPE_PAIRS = 0, FC_ROPE_HALVES = 1 } fc_rope_pairing;
+
+typedef struct {
+  int32_t H_q, H_kv, d, T;                       /* d in {64, 128} */
+  int64_t q_hs, q_rs, k_hs, k_rs;                /* element strides of the inputs: head, token */
+  int64_t qo_hs, qo_rs, ko_hs, ko_rs;            /* and of the outputs */
+  int32_t axis_dim[3];                           /* even, >= 0, sum <= d */
+  int32_t pairing;                               /* fc_rope_pairing */
+  int32_t norm;                                  /* fc_norm */
+  float eps;                                     /* >= 0 */
+  double theta;                                  /* > 0; ignored where inv_freq is given */
+  int32_t grid_t0, grid_h, grid_w;               /* ignored where pos is given, or nothing turns */
+} fc_rope_desc;
+
+int fc_qk_norm_rope(fc_ctx* ctx, void* stream, const fc_rope_desc* desc, const void* Q, const void* K, int dtype,
+                    const float* q_weight, const float* k_weight, const int32_t* pos, const double* inv_freq,
+                    void* Q_out, void* K_out);
+
+/* ------------------------------------------------------------------------------------------
+ * The 4-bit store.
+ *
+ * A row of d elements is d/2 bytes of codes and d/32 bf16 scales: 4.5 bits an element, so that a budget
+ * of B tokens takes 0.28 of its bf16 bytes.  Each group of 32 consecutive elements shares a scale s:
+ *     s = the least number with five significant bits that is >= max|x| / 7 (divided in fp32), clamped to
+ *         [2^-126, 2^122]; 0 if all are 0; NaN if one is not finite (FC_DEV_NONFINITE)
+ *     code = 8 + min(max(round_half_even(x / s), -7), 7),   value = (code - 8) * s
+ * A value has at most eight significant bits: it is exactly a bf16 number, so attention over the store is
+ * attention over these values without another rounding.  In each little-endian 32-bit word of eight
+ * elements, element 2i is at bits 4i of the low half and element 2i+1 at bits 4i of the high half (i = 0..3).
+ * The pointers are DEVICE pointers inside a HOST struct; K and V share strides.  Code bases and strides are
+ * multiples of 16 bytes, scale bases of 16 bytes, scale strides of d/32 elements. */
+typedef struct {
+  void *k_codes, *k_scales, *v_codes, *v_scales;
+  int64_t code_hs, code_rs;   /* bytes: head, row (row >= d/2) */
+  int64_t scale_hs, scale_rs; /* bf16 elements: head, row (row >= d/32) */
+  int64_t rows;               /* rows per head that the buffers hold */
+} fc_kv4_cache;
+
+/* fc_kv4_pack — writes rows dst_row .. dst_row + n_out - 1 of the store `dst` (all heads, K and V).
+ *
+ * Output row r of head h is logical row i = kept_idx[h * kept_hs + r], or i = r without a kept list:
+ *     i <  n_old   row i of the store `old`, codes and scales byte for byte (no second rounding)
+ *     i >= n_old   row i - n_old of K_src / V_src, quantised
+ * With the kept list of fc_kv_select_compact over [clean region | finished chunk] this is the compaction of a
+ * 4-bit clean region; with n_old = 0 and no list it appends n_out rows.
+ *
+ *   K_src, V_src     DEVICE [H, n_new, d], `dtype` (may be NULL if n_new is 0).
+ *   old              HOST struct or NULL (n_old 0); its rows >= n_old.  Must not overlap `dst`.
+ *   kept_idx         DEVICE [H, >= n_out] int32 or NULL (n_out <= n_old + n_new then).  An index outside
+ *                    [0, n_old + n_new) sets FC_DEV_BAD_INDEX; its output row is left as it was.
+ * Rows outside the written range are not touched.  Needs no workspace. */
+typedef struct {
+  int32_t H, d;                    /* d in {64, 128} */
+  int32_t n_old, n_new, n_out;     /* rows per head; n_out may be 0 */
+  int64_t dst_row;
+  int64_t k_hs, k_rs, v_hs, v_rs;  /* element strides of K_src, V_src */
+} fc_kv4_pack_desc;
+
+int fc_kv4_pack(fc_ctx* ctx, void* stream, const fc_kv4_pack_desc* desc, const void* K_src, const void* V_src, int dtype,
+                const fc_kv4_cache* old, const int32_t* kept_idx, int64_t kept_hs, const fc_kv4_cache* dst,
+                uint32_t* status);
+
+/* fc_kv4_unpack — the values of rows src_row .. src_row + n - 1 of every head as plain rows.
+ *   K_dst, V_dst     DEVICE [H, n, d], `dtype` (exact in both types); either may be NULL (the score needs the keys
+ *                    only).  Needs no workspace. */
+typedef struct {
+  int32_t H, d;
+  int32_t n;                       /* may be 0 */
+  int64_t src_row;
+  int64_t k_hs, k_rs, v_hs, v_rs;  /* element strides of K_dst, V_dst */
+} fc_kv4_unpack_desc;
+
+int fc_kv4_unpack(fc_ctx* ctx, void* stream, const fc_kv4_unpack_desc* desc, const fc_kv4_cache* src, void* K_dst,
+                  void* V_dst, int dtype);
+
+/* fc_chunk_attention_kv4 — fc_chunk_attention over a 4-bit clean region and a plain window.
+ *
+ * Logical token j < n_cache is row j of the 4-bit store; j >= n_cache is token j - n_cache of the window, found in
+ * K / V through the segment table, whose logical offsets count from the window's start.  kv_visible_len counts both.
+ * Everything else is as in fc_chunk_attention: chunks, active list, grouped heads, rows of inactive chunks left as they are; rows that see no
+ * token get zeros (lse -inf).  There is no token map: a 4-bit store is compacted by fc_kv4_pack.
+ *
+ *   desc             as above; k_* and v_* strides and kv_rows describe the window.  impl: 0 auto; 1 force the
+ *                    CUDA-core kernel (the path of fp32).
+ *   active_ids       as above; an id outside [0, W) sets FC_DEV_BAD_INDEX and is ignored.
+ *   cache            HOST struct, rows >= n_cache; may be NULL if n_cache is 0.
+ *   K, V             DEVICE [H_kv, kv_rows, d], the window; may be NULL if n_seg is 0 (no window).
+ *   n_seg            <= FC_MAX_SEGMENTS - 1.
+ * Deterministic.  Workspace: fc_chunk_attention_kv4_workspace_bytes() of the same arguments (0 for arguments
+ * that the call refuses). */
+size_t fc_chunk_attention_kv4_workspace_bytes(const fc_ctx* ctx, const fc_attn_desc* desc, int dtype,
+                                              const int32_t* q_chunk_row_off, const int32_t* kv_visible_len, int n_cache);
+int fc_chunk_attention_kv4(fc_ctx* ctx, void* stream, const fc_attn_desc* desc, const void* Q, const fc_kv4_cache* cache,
+                           int n_cache, const void* K, const void* V, int dtype, const int32_t* q_chunk_row_off,
+                           const int32_t* kv_visible_len, const int32_t* seg_logical_off, const int32_t* seg_phys_off,
+                           int n_seg, const int32_t* active_ids, const int32_t* n_active, void* O, float* lse,
+                           int64_t lse_hs, uint32_t* status, void* ws, size_t ws_bytes);
 
 #ifdef __cplusplus
 }

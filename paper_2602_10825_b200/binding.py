@@ -17,7 +17,10 @@ _HEADER = os.path.join(_ROOT, "include", "fc.h")
 BF16, F32 = 0, 1
 POLICY_CHUNKWISE, POLICY_UNIFORM = 0, 1
 RED_MEANKEY, RED_TILED, RED_TILED_MAX = 0, 1, 2
-STATUS_BITS = {"timeout": 1, "nan_score": 2, "bad_index": 4}
+NORM_NONE, NORM_RMS = 0, 1
+ROPE_PAIRS, ROPE_HALVES = 0, 1
+KV4_GROUP = 32  # elements of a packed row that share a scale
+STATUS_BITS = {"timeout": 1, "nan_score": 2, "bad_index": 4, "nonfinite": 8}
 
 
 class FcError(RuntimeError):
@@ -40,6 +43,30 @@ class _ScoreDesc(C.Structure):
 
 class _SelectOpts(C.Structure):
     _fields_ = [("unit", C.c_int32), ("n_protect", C.c_int32)]
+
+
+class _RopeDesc(C.Structure):
+    _fields_ = [("H_q", C.c_int32), ("H_kv", C.c_int32), ("d", C.c_int32), ("T", C.c_int32),
+                ("q_hs", C.c_int64), ("q_rs", C.c_int64), ("k_hs", C.c_int64), ("k_rs", C.c_int64),
+                ("qo_hs", C.c_int64), ("qo_rs", C.c_int64), ("ko_hs", C.c_int64), ("ko_rs", C.c_int64),
+                ("axis_dim", C.c_int32 * 3), ("pairing", C.c_int32), ("norm", C.c_int32), ("eps", C.c_float),
+                ("theta", C.c_double), ("grid_t0", C.c_int32), ("grid_h", C.c_int32), ("grid_w", C.c_int32)]
+
+
+class _Kv4Cache(C.Structure):
+    _fields_ = [("k_codes", C.c_void_p), ("k_scales", C.c_void_p), ("v_codes", C.c_void_p), ("v_scales", C.c_void_p),
+                ("code_hs", C.c_int64), ("code_rs", C.c_int64), ("scale_hs", C.c_int64), ("scale_rs", C.c_int64),
+                ("rows", C.c_int64)]
+
+
+class _Kv4PackDesc(C.Structure):
+    _fields_ = [("H", C.c_int32), ("d", C.c_int32), ("n_old", C.c_int32), ("n_new", C.c_int32), ("n_out", C.c_int32),
+                ("dst_row", C.c_int64), ("k_hs", C.c_int64), ("k_rs", C.c_int64), ("v_hs", C.c_int64), ("v_rs", C.c_int64)]
+
+
+class _Kv4UnpackDesc(C.Structure):
+    _fields_ = [("H", C.c_int32), ("d", C.c_int32), ("n", C.c_int32), ("src_row", C.c_int64), ("k_hs", C.c_int64),
+                ("k_rs", C.c_int64), ("v_hs", C.c_int64), ("v_rs", C.c_int64)]
 
 
 class _CompactStrides(C.Structure):
@@ -65,9 +92,15 @@ def lib():
         L.fc_last_cuda_error.restype = C.c_char_p
         for name in ("fc_chunk_decide_static_max_bytes", "fc_chunk_decide_workspace_bytes", "fc_chunk_attention_workspace_bytes",
                      "fc_kv_score_workspace_bytes", "fc_kv_select_compact_workspace_bytes",
-                     "fc_kv_select_compact_ex_workspace_bytes"):
+                     "fc_kv_select_compact_ex_workspace_bytes", "fc_chunk_attention_kv4_workspace_bytes"):
             getattr(L, name).restype = C.c_size_t
         L.fc_chunk_decide_workspace_bytes.argtypes = [C.c_int64, C.c_int]
+        p, i32, i64 = C.c_void_p, C.c_int, C.c_int64
+        L.fc_qk_norm_rope.argtypes = [p, p, p, p, p, i32, p, p, p, p, p, p]
+        L.fc_kv4_pack.argtypes = [p, p, p, p, p, i32, p, p, i64, p, p]
+        L.fc_kv4_unpack.argtypes = [p, p, p, p, p, p, i32]
+        L.fc_chunk_attention_kv4_workspace_bytes.argtypes = [p, p, i32, p, p, i32]
+        L.fc_chunk_attention_kv4.argtypes = [p, p, p, p, p, i32, p, p, i32, p, p, p, p, i32, p, p, p, p, i64, p, p, C.c_size_t]
         _lib = L
     return _lib
 
@@ -113,6 +146,38 @@ def _hsr(t, name):
 def _host_i32(x):
     a = np.ascontiguousarray(np.asarray(x, dtype=np.int32))
     return a, a.ctypes.data_as(C.c_void_p)
+
+
+class Kv4Cache:
+    """A 4-bit store of K and V rows (fc_kv4_cache): codes uint8 [H, rows, d/2] and scales bf16 [H, rows, d/32].
+
+    Strided views (a slice of a larger store) are fine as long as K and V share strides and the last dimensions are
+    contiguous; the format is described in include/fc.h."""
+
+    def __init__(self, k_codes, k_scales, v_codes, v_scales):
+        self.k_codes, self.k_scales, self.v_codes, self.v_scales = k_codes, k_scales, v_codes, v_scales
+        H, rows, half = k_codes.shape
+        for name, t, dtype, shape, like in (("k_codes", k_codes, torch.uint8, (H, rows, half), k_codes),
+                                            ("v_codes", v_codes, torch.uint8, (H, rows, half), k_codes),
+                                            ("k_scales", k_scales, torch.bfloat16, (H, rows, half // 16), k_scales),
+                                            ("v_scales", v_scales, torch.bfloat16, (H, rows, half // 16), k_scales)):
+            if t.dtype != dtype or tuple(t.shape) != shape or t.device != k_codes.device:
+                raise FcError(f"{name} must be {dtype} {list(shape)} on {k_codes.device}")
+            if t.stride() != like.stride() or t.stride(2) != 1:
+                raise FcError(f"{name}: K and V must share strides, with a contiguous last dimension")
+        self.H, self.rows, self.d, self.device = H, rows, 2 * half, k_codes.device
+        ch, cr, _ = k_codes.stride()
+        sh, sr, _ = k_scales.stride()
+        self._c = _Kv4Cache(k_codes.data_ptr(), k_scales.data_ptr(), v_codes.data_ptr(), v_scales.data_ptr(), ch, cr, sh, sr, rows)
+
+    @staticmethod
+    def empty(H, rows, d, device="cuda"):
+        """An uninitialised store of H heads x rows rows of d elements."""
+        if d % KV4_GROUP:
+            raise FcError(f"d must be a multiple of {KV4_GROUP}")
+        codes = [torch.empty((H, rows, d // 2), dtype=torch.uint8, device=device) for _ in range(2)]
+        scales = [torch.empty((H, rows, d // KV4_GROUP), dtype=torch.bfloat16, device=device) for _ in range(2)]
+        return Kv4Cache(codes[0], scales[0], codes[1], scales[1])
 
 
 class Context:
@@ -328,3 +393,177 @@ class Context:
             C.c_size_t(ws.numel()))
         self._check(rc, "fc_kv_select_compact")
         return dict(kept_idx=kept_idx, n_kept=n_kept, K_dst=K_dst, V_dst=V_dst)
+
+    # ------------------------------------------------------------------ the calls around the 4-bit store
+    def _ptr(self, t, name, dtype=None):
+        """Device pointer of a tensor on this context's device (None for None)."""
+        if t is None:
+            return None
+        if not t.is_cuda or t.device.index != self.device:
+            raise FcError(f"{name} must be on cuda:{self.device}, got {t.device}")
+        if dtype is not None and t.dtype != dtype:
+            raise FcError(f"{name} must have dtype {dtype}, got {t.dtype}")
+        return t.data_ptr()
+
+    def _raw_stream(self):
+        return torch.cuda.current_stream(self.device).cuda_stream
+
+    def _scratch(self, key, n_bytes, stream):
+        """Workspace of a call on `stream`: one buffer per stream, since calls on different streams may overlap; during a
+        capture the graph gets its own, which lives in the graph's memory pool."""
+        with torch.cuda.device(self.device):
+            if torch.cuda.is_current_stream_capturing():
+                return torch.empty(n_bytes, dtype=torch.uint8, device=f"cuda:{self.device}")
+        return self.workspace((key, stream), n_bytes)
+
+    # ------------------------------------------------------------------ fc_qk_norm_rope
+    def qk_norm_rope(self, Q, K, *, axes, norm=True, q_weight=None, k_weight=None, eps=1e-6, theta=10000.0, grid=None,
+                     pos=None, pairing=ROPE_PAIRS, inv_freq=None, Q_out=None, K_out=None):
+        """RMS norm per head and rotation over (time, height, width) of Q [H_q, T, d] and K [H_kv, T, d]; either may be None.
+
+        axes: elements of a head that turn with each axis.  grid = (t0, height, width) places the tokens of a chunk in
+        order; pos [T, 3] int32 gives each its own place.  Q_out / K_out may be the inputs themselves."""
+        like = K if Q is None else Q
+        if like is None:
+            raise FcError("Q and K are both None")
+        if Q is not None and K is not None and (Q.dtype != K.dtype or Q.shape[1:] != K.shape[1:]):
+            raise FcError("Q and K must share dtype, tokens and head size")
+        T, d = int(like.shape[1]), int(like.shape[2])
+        side = []
+        for name, x, out, w in (("Q", Q, Q_out, q_weight), ("K", K, K_out, k_weight)):
+            if x is None:
+                side.append((0, (0, 0), (0, 0), None, None, None, None))
+                continue
+            if out is None:
+                out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+            if out.shape != x.shape or out.dtype != x.dtype:
+                raise FcError(f"{name}_out must have {name}'s shape and dtype")
+            if w is not None and (w.shape != (d,) or w.stride(0) != 1):
+                raise FcError(f"the weight of {name} must be contiguous [{d}]")
+            side.append((x.shape[0], _hsr(x, name), _hsr(out, f"{name}_out"), self._ptr(x, name), self._ptr(out, f"{name}_out"),
+                         self._ptr(w, f"the weight of {name}", torch.float32), out))
+        (hq, qs, qos, qp, qop, qw, Q_out), (hk, ks, kos, kp, kop, kw, K_out) = side
+        if pos is not None and (pos.shape != (T, 3) or not pos.is_contiguous()):
+            raise FcError(f"pos must be contiguous [{T}, 3]")
+        if grid is None and pos is None and any(axes):
+            raise FcError("give the tokens' places: grid or pos")
+        freq = None
+        if inv_freq is not None:
+            freq = np.ascontiguousarray(np.asarray(inv_freq, dtype=np.float64))
+            if freq.shape != (sum(axes) // 2,):
+                raise FcError(f"inv_freq must have {sum(axes) // 2} entries")
+        desc = _RopeDesc(hq, hk, d, T, *qs, *ks, *qos, *kos, tuple(axes), pairing, NORM_RMS if norm else NORM_NONE, eps, theta,
+                         *(grid or (0, 0, 0)))
+        rc = self._L.fc_qk_norm_rope(self._h, self._raw_stream(), C.byref(desc), qp, kp, _dt(like), qw, kw,
+                                     self._ptr(pos, "pos", torch.int32), None if freq is None else freq.ctypes.data, qop, kop)
+        if rc:
+            self._check(rc, "fc_qk_norm_rope")
+        return Q_out, K_out
+
+    # ------------------------------------------------------------------ fc_kv4_pack / fc_kv4_unpack
+    def kv4_pack(self, K, V, dst, *, old=None, n_old=None, kept_idx=None, dst_row=0, status=None):
+        """Quantises rows of K, V [H, n_new, d] into the store `dst`, from row dst_row on; returns dst.
+
+        With kept_idx [H, n_out] the rows are picked from [the first n_old rows of the store `old` | the new rows], the
+        old ones copied as they are.  K and V may be None if only old rows are picked."""
+        if (K is None) != (V is None) or (K is not None and (K.dtype != V.dtype or K.shape != V.shape)):
+            raise FcError("K and V must share shape and dtype")
+        n_old = 0 if old is None else old.rows if n_old is None else int(n_old)
+        n_new, ks, vs, dt = 0, (0, 0), (0, 0), BF16
+        if K is not None:
+            if K.shape[0] != dst.H or K.shape[2] != dst.d:
+                raise FcError(f"K and V must be [{dst.H}, rows, {dst.d}]")
+            n_new, ks, vs, dt = K.shape[1], _hsr(K, "K"), _hsr(V, "V"), _dt(K)
+        if old is not None and (old.H != dst.H or old.d != dst.d):
+            raise FcError("old and dst must share heads and head size")
+        n_out, kept_hs = n_old + n_new, 0
+        if kept_idx is not None:
+            if kept_idx.dim() != 2 or kept_idx.shape[0] != dst.H or kept_idx.stride(1) != 1:
+                raise FcError(f"kept_idx must be [{dst.H}, rows] with contiguous rows")
+            n_out, kept_hs = kept_idx.shape[1], max(kept_idx.stride(0), kept_idx.shape[1])
+        for s, name in ((old, "old"), (dst, "dst")):
+            if s is not None:
+                self._ptr(s.k_codes, name)
+        desc = _Kv4PackDesc(dst.H, dst.d, n_old, n_new, n_out, dst_row, *ks, *vs)
+        rc = self._L.fc_kv4_pack(self._h, self._raw_stream(), C.byref(desc), self._ptr(K, "K"), self._ptr(V, "V"), dt,
+                                 None if old is None else C.byref(old._c), self._ptr(kept_idx, "kept_idx", torch.int32), kept_hs,
+                                 C.byref(dst._c), self._ptr(status, "status", torch.int32))
+        if rc:
+            self._check(rc, "fc_kv4_pack")
+        return dst
+
+    def kv4_unpack(self, src, *, row=0, n=None, K_dst=None, V_dst=None, dtype=torch.bfloat16, keys_only=False):
+        """Values of rows row .. row + n - 1 of a store as plain [H, n, d] tensors (K, V); V is None with keys_only."""
+        n = (K_dst.shape[1] if K_dst is not None else src.rows - row) if n is None else int(n)
+        shape = (src.H, n, src.d)
+        if K_dst is None and (V_dst is None or not keys_only):
+            K_dst = torch.empty(shape, dtype=dtype if V_dst is None else V_dst.dtype, device=src.device)
+        if V_dst is None and not keys_only:
+            V_dst = torch.empty(shape, dtype=K_dst.dtype, device=src.device)
+        for name, t in (("K_dst", K_dst), ("V_dst", V_dst)):
+            if t is not None and (tuple(t.shape) != shape or t.dtype != (K_dst if K_dst is not None else V_dst).dtype):
+                raise FcError(f"{name} must be {list(shape)}, K_dst and V_dst of one dtype")
+        self._ptr(src.k_codes, "src")
+        ks = (0, 0) if K_dst is None else _hsr(K_dst, "K_dst")
+        vs = (0, 0) if V_dst is None else _hsr(V_dst, "V_dst")
+        desc = _Kv4UnpackDesc(src.H, src.d, n, row, *ks, *vs)
+        rc = self._L.fc_kv4_unpack(self._h, self._raw_stream(), C.byref(desc), C.byref(src._c), self._ptr(K_dst, "K_dst"),
+                                   self._ptr(V_dst, "V_dst"), _dt(K_dst if K_dst is not None else V_dst))
+        if rc:
+            self._check(rc, "fc_kv4_unpack")
+        return K_dst, V_dst
+
+    # ------------------------------------------------------------------ fc_chunk_attention_kv4
+    def chunk_attention_kv4(self, Q, cache, K, V, q_chunk_row_off, kv_visible_len, active_ids, n_active, O, *,
+                            seg_logical_off=None, seg_phys_off=None, n_cache=None, lse=None, scale=0.0, impl=0, status=None,
+                            ws=None):
+        """fc_chunk_attention over [the first n_cache rows of the 4-bit store | the window K, V].
+
+        cache may be None (no clean region), K and V too (no window).  Without a segment table the window is the rows of
+        K and V in order; with one, its logical offsets count from the window's start."""
+        if (K is None) != (V is None):
+            raise FcError("K and V: give both or neither")
+        if cache is None and K is None:
+            raise FcError("give a store, a window, or both")
+        H_kv = cache.H if cache is not None else K.shape[0]
+        if O.dtype != Q.dtype or (K is not None and (K.dtype != Q.dtype or V.dtype != Q.dtype)):
+            raise FcError("Q, K, V, O must share one dtype")
+        if O.shape != Q.shape or (cache is not None and cache.d != Q.shape[2]):
+            raise FcError("Q, O and the store must share the head size, Q and O their shape")
+        if K is not None and (K.shape[0] != H_kv or K.shape[2] != Q.shape[2] or V.shape != K.shape):
+            raise FcError(f"K and V must be [{H_kv}, rows, {Q.shape[2]}]")
+        n_cache = (0 if cache is None else cache.rows) if n_cache is None else int(n_cache)
+        W = len(kv_visible_len)
+        if len(q_chunk_row_off) != W + 1 or q_chunk_row_off[W] > Q.shape[1] or active_ids.numel() > W:
+            raise FcError("q_chunk_row_off must have one entry more than kv_visible_len and stay inside Q; active_ids at most as many")
+        ks, vs, rows, n_seg, sl, sp = (0, 0), (0, 0), 0, 0, None, None
+        if K is not None:
+            ks, vs, rows = _hsr(K, "K"), _hsr(V, "V"), K.shape[1]
+            if seg_phys_off is None:
+                n_seg, sl, sp = (1, (C.c_int32 * 2)(0, rows), (C.c_int32 * 1)(0)) if rows else (0, None, None)
+            else:
+                n_seg = len(seg_phys_off)
+                if len(seg_logical_off) != n_seg + 1:
+                    raise FcError("seg_logical_off must have one entry more than seg_phys_off")
+                sl, sp = (C.c_int32 * (n_seg + 1))(*seg_logical_off), (C.c_int32 * n_seg)(*seg_phys_off)
+        desc = _AttnDesc(Q.shape[0], H_kv, Q.shape[2], W, *_hsr(Q, "Q"), *ks, *vs, *_hsr(O, "O"), rows, scale, impl)
+        off, vis = (C.c_int32 * (W + 1))(*q_chunk_row_off), (C.c_int32 * W)(*kv_visible_len)
+        dt, stream, dp = _dt(Q), self._raw_stream(), C.byref(desc)
+        if cache is not None:
+            self._ptr(cache.k_codes, "cache")
+        lse_hs = 0
+        if lse is not None:
+            if lse.dim() != 2 or lse.shape[0] != Q.shape[0] or lse.shape[1] < q_chunk_row_off[W] or lse.stride(1) != 1:
+                raise FcError("lse must be [H_q, rows] with contiguous rows")
+            lse_hs = max(lse.stride(0), 1)
+        if ws is None:
+            need = self._L.fc_chunk_attention_kv4_workspace_bytes(self._h, dp, dt, off, vis, n_cache)
+            ws = self._scratch("attention_kv4", need, stream) if need else None
+        rc = self._L.fc_chunk_attention_kv4(
+            self._h, stream, dp, self._ptr(Q, "Q"), None if cache is None else C.byref(cache._c), n_cache, self._ptr(K, "K"),
+            self._ptr(V, "V"), dt, off, vis, sl, sp, n_seg, self._ptr(active_ids, "active_ids", torch.int32),
+            self._ptr(n_active, "n_active", torch.int32), self._ptr(O, "O"), self._ptr(lse, "lse", torch.float32), lse_hs,
+            self._ptr(status, "status", torch.int32), self._ptr(ws, "ws"), 0 if ws is None else ws.numel())
+        if rc:
+            self._check(rc, "fc_chunk_attention_kv4")
+        return O

@@ -1,0 +1,105 @@
+// fc_chunk_attention_kv4: argument validation and the choice of the kernel.
+#include <algorithm>
+#include <climits>
+#include <cmath>
+
+#include "fc_attention_kv4.cuh"
+
+namespace {
+
+// The part of the arguments that the workspace depends on.
+int check_geometry(const fc_attn_desc* desc, int dtype, const int32_t* q_chunk_row_off, const int32_t* kv_visible_len,
+                   int n_cache, fc::Kv4AttnGeom& g) {
+  if (!desc || !q_chunk_row_off || !kv_visible_len) return FC_ERR_INVALID_ARG;
+  if (dtype != FC_BF16 && dtype != FC_F32) return FC_ERR_UNSUPPORTED;
+  if (desc->d != 64 && desc->d != 128) return FC_ERR_UNSUPPORTED;
+  if (desc->H_q <= 0 || desc->H_kv <= 0 || desc->H_q % desc->H_kv || desc->W <= 0 || n_cache < 0) return FC_ERR_INVALID_ARG;
+  if (desc->W > FC_MAX_CHUNKS || desc->H_kv > 65535) return FC_ERR_UNSUPPORTED;
+  if (desc->impl < 0 || desc->impl > 1) return FC_ERR_INVALID_ARG;
+  if (!(desc->scale >= 0.f)) return FC_ERR_INVALID_ARG;
+  fc::AttnGeom& a = g.a;
+  a.H_q = desc->H_q; a.H_kv = desc->H_kv; a.d = desc->d; a.W = desc->W;
+  a.group = desc->H_q / desc->H_kv;
+  a.scale = desc->scale != 0.f ? desc->scale : 1.f / sqrtf((float)desc->d);
+  for (int c = 0; c <= a.W; ++c) {
+    if (q_chunk_row_off[c] < 0 || (c > 0 && q_chunk_row_off[c] < q_chunk_row_off[c - 1])) return FC_ERR_INVALID_ARG;
+    a.q_row_off[c] = q_chunk_row_off[c];
+  }
+  for (int c = 0; c < a.W; ++c) {
+    if (kv_visible_len[c] < 0) return FC_ERR_INVALID_ARG;
+    a.vis[c] = kv_visible_len[c];
+  }
+  g.n_cache = n_cache;
+  g.n_vrows = (int64_t)(a.q_row_off[a.W] - a.q_row_off[0]) * a.group;
+  if (g.n_vrows > INT32_MAX) return FC_ERR_UNSUPPORTED;
+  return FC_OK;
+}
+
+}  // namespace
+
+extern "C" size_t fc_chunk_attention_kv4_workspace_bytes(const fc_ctx* ctx, const fc_attn_desc* desc, int dtype,
+                                                         const int32_t* q_chunk_row_off, const int32_t* kv_visible_len,
+                                                         int n_cache) {
+  fc::Kv4AttnGeom g = {};
+  if (!ctx || check_geometry(desc, dtype, q_chunk_row_off, kv_visible_len, n_cache, g) != FC_OK) return 0;
+  return fc::kv4_simt_workspace(ctx, g);
+}
+
+extern "C" int fc_chunk_attention_kv4(fc_ctx* ctx, void* stream, const fc_attn_desc* desc, const void* Q,
+                                      const fc_kv4_cache* cache, int n_cache, const void* K, const void* V, int dtype,
+                                      const int32_t* q_chunk_row_off, const int32_t* kv_visible_len,
+                                      const int32_t* seg_logical_off, const int32_t* seg_phys_off, int n_seg,
+                                      const int32_t* active_ids, const int32_t* n_active, void* O, float* lse, int64_t lse_hs,
+                                      uint32_t* status, void* ws, size_t ws_bytes) {
+  if (!ctx || !desc || n_seg < 0) return FC_ERR_INVALID_ARG;
+  fc::Kv4AttnGeom g = {};
+  int rc = check_geometry(desc, dtype, q_chunk_row_off, kv_visible_len, n_cache, g);
+  if (rc != FC_OK) return rc;
+  if (g.n_vrows == 0) return FC_OK;
+  if (!Q || !O || !active_ids || !n_active) return FC_ERR_INVALID_ARG;
+  fc::AttnGeom& a = g.a;
+  const int es = fc::elem_size(dtype);
+  const int64_t strides[8] = {desc->q_hs, desc->q_rs, desc->o_hs, desc->o_rs, desc->k_hs, desc->k_rs, desc->v_hs, desc->v_rs};
+  for (int i = 0; i < (n_seg > 0 ? 8 : 4); ++i) {
+    if (strides[i] < 0 || (strides[i] * es) % 16) return FC_ERR_MISALIGNED;
+    if (i % 2 && strides[i] < desc->d) return FC_ERR_INVALID_ARG;
+  }
+  if (!fc::aligned16(Q) || !fc::aligned16(O)) return FC_ERR_MISALIGNED;
+  if (n_cache > 0 && (rc = fc::kv4_check(cache, desc->d, n_cache)) != FC_OK) return rc;
+  if (n_seg > FC_MAX_SEGMENTS - 1) return FC_ERR_UNSUPPORTED;
+  int64_t window = 0;
+  if (n_seg > 0) {
+    if (!K || !V || !seg_logical_off || !seg_phys_off || desc->kv_rows <= 0) return FC_ERR_INVALID_ARG;
+    if (!fc::aligned16(K) || !fc::aligned16(V)) return FC_ERR_MISALIGNED;
+    for (int s = 0; s <= n_seg; ++s) {
+      if (s == 0 ? seg_logical_off[0] != 0 : seg_logical_off[s] < seg_logical_off[s - 1]) return FC_ERR_INVALID_ARG;
+      a.seg_log[s] = seg_logical_off[s];
+    }
+    for (int s = 0; s < n_seg; ++s) {
+      const int64_t len = seg_logical_off[s + 1] - seg_logical_off[s];
+      if (seg_phys_off[s] < 0 || seg_phys_off[s] + len > desc->kv_rows) return FC_ERR_INVALID_ARG;
+      a.seg_phys[s] = seg_phys_off[s];
+    }
+    window = seg_logical_off[n_seg];
+  }
+  for (int c = 0; c < a.W; ++c)
+    if (a.vis[c] > n_cache + window) return FC_ERR_INVALID_ARG;
+  if (lse && lse_hs <= 0) return FC_ERR_INVALID_ARG;
+  a.n_seg = n_seg;
+  a.q_hs = desc->q_hs; a.q_rs = desc->q_rs; a.k_hs = desc->k_hs; a.k_rs = desc->k_rs;
+  a.v_hs = desc->v_hs; a.v_rs = desc->v_rs; a.o_hs = desc->o_hs; a.o_rs = desc->o_rs;
+  a.kv_rows = desc->kv_rows; a.lse_hs = lse_hs;
+  a.active_ids = active_ids; a.n_active = n_active; a.lse = lse; a.status = status;
+  if (n_cache > 0) g.cache = fc::kv4_view(*cache);
+
+  const size_t need = fc::kv4_simt_workspace(ctx, g);
+  if (need > 0) {
+    if (!ws || ws_bytes < need) return FC_ERR_WORKSPACE;
+    if (!fc::aligned16(ws)) return FC_ERR_MISALIGNED;
+    const int64_t parts = a.H_kv * g.n_vrows * g.n_splits;
+    g.part_o = (float*)ws;
+    g.part_ml = (float2*)((char*)ws + fc::align_up(parts * a.d * sizeof(float), 256));
+  }
+  FC_DEVICE_GUARD(ctx);
+  return fc::kv4_simt((cudaStream_t)stream, g, Q, K, V, dtype, O);
+}

@@ -41,6 +41,23 @@ inline int elem_size(int dtype) { return dtype == FC_F32 ? 4 : 2; }
     }                                               \
   } while (0)
 
+// Makes the context's device current for the length of a call (a stream belongs to its device), and the caller's again after it.
+struct DeviceGuard {
+  int before = -1;
+  cudaError_t err;
+  explicit DeviceGuard(int device) {
+    int now = device;
+    err = cudaGetDevice(&now);
+    if (err == cudaSuccess && now != device && (err = cudaSetDevice(device)) == cudaSuccess) before = now;
+  }
+  ~DeviceGuard() {
+    if (before >= 0) cudaSetDevice(before);
+  }
+};
+#define FC_DEVICE_GUARD(ctx)                 \
+  fc::DeviceGuard device_guard__((ctx)->device); \
+  FC_CUDA_CHECK(device_guard__.err)
+
 // Bounds-checking build (-DFC_DEBUG_BOUNDS, libfc_debug.so): every store whose address is computed from data read on
 // the device, or from a tile / slice walk, is guarded; a violated guard sets FC_DEV_BAD_INDEX in the status word and
 // skips the store (nothing traps).  In the normal build the guard is the constant `true`.
