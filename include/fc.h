@@ -462,6 +462,7 @@ int fc_kv4_unpack(fc_ctx* ctx, void* stream, const fc_kv4_unpack_desc* desc, con
  *   active_ids       as above; an id outside [0, W) sets FC_DEV_BAD_INDEX and is ignored.
  *   cache            HOST struct, rows >= n_cache; may be NULL if n_cache is 0.
  *   K, V             DEVICE [H_kv, kv_rows, d], the window; may be NULL if n_seg is 0 (no window).
+ *   kv_visible_len   as above, at most 2^31 - 4097.
  *   n_seg            <= FC_MAX_SEGMENTS - 1.
  * Deterministic.  Workspace: fc_chunk_attention_kv4_workspace_bytes() of the same arguments (0 for arguments
  * that the call refuses). */

@@ -15,7 +15,7 @@ int check_geometry(const fc_attn_desc* desc, int dtype, const int32_t* q_chunk_r
   if (desc->d != 64 && desc->d != 128) return FC_ERR_UNSUPPORTED;
   if (desc->H_q <= 0 || desc->H_kv <= 0 || desc->H_q % desc->H_kv || desc->W <= 0 || n_cache < 0) return FC_ERR_INVALID_ARG;
   if (desc->W > FC_MAX_CHUNKS || desc->H_kv > 65535) return FC_ERR_UNSUPPORTED;
-  if (desc->impl < 0 || desc->impl > 1) return FC_ERR_INVALID_ARG;
+  if (desc->impl < 0 || desc->impl > 3) return FC_ERR_INVALID_ARG;
   if (!(desc->scale >= 0.f)) return FC_ERR_INVALID_ARG;
   fc::AttnGeom& a = g.a;
   a.H_q = desc->H_q; a.H_kv = desc->H_kv; a.d = desc->d; a.W = desc->W;
@@ -27,12 +27,24 @@ int check_geometry(const fc_attn_desc* desc, int dtype, const int32_t* q_chunk_r
   }
   for (int c = 0; c < a.W; ++c) {
     if (kv_visible_len[c] < 0) return FC_ERR_INVALID_ARG;
+    if (kv_visible_len[c] > INT32_MAX - 4096) return FC_ERR_UNSUPPORTED;  // key counters may run past the end by a step
     a.vis[c] = kv_visible_len[c];
   }
   g.n_cache = n_cache;
   g.n_vrows = (int64_t)(a.q_row_off[a.W] - a.q_row_off[0]) * a.group;
   if (g.n_vrows > INT32_MAX) return FC_ERR_UNSUPPORTED;
   return FC_OK;
+}
+
+enum Path { kSimt, kRowsPath };
+
+Path choose(const fc_attn_desc* desc, int dtype, const fc::Kv4AttnGeom& g) {
+  if (dtype == FC_F32 || desc->impl == 1) return kSimt;
+  return kRowsPath;
+}
+
+size_t plan(const fc_ctx* ctx, Path path, fc::Kv4AttnGeom& g) {
+  return path == kSimt ? fc::kv4_simt_workspace(ctx, g) : fc::kv4_rows_workspace(ctx, g);
 }
 
 }  // namespace
@@ -42,7 +54,7 @@ extern "C" size_t fc_chunk_attention_kv4_workspace_bytes(const fc_ctx* ctx, cons
                                                          int n_cache) {
   fc::Kv4AttnGeom g = {};
   if (!ctx || check_geometry(desc, dtype, q_chunk_row_off, kv_visible_len, n_cache, g) != FC_OK) return 0;
-  return fc::kv4_simt_workspace(ctx, g);
+  return plan(ctx, choose(desc, dtype, g), g);
 }
 
 extern "C" int fc_chunk_attention_kv4(fc_ctx* ctx, void* stream, const fc_attn_desc* desc, const void* Q,
@@ -92,7 +104,8 @@ extern "C" int fc_chunk_attention_kv4(fc_ctx* ctx, void* stream, const fc_attn_d
   a.active_ids = active_ids; a.n_active = n_active; a.lse = lse; a.status = status;
   if (n_cache > 0) g.cache = fc::kv4_view(*cache);
 
-  const size_t need = fc::kv4_simt_workspace(ctx, g);
+  const Path path = choose(desc, dtype, g);
+  const size_t need = plan(ctx, path, g);
   if (need > 0) {
     if (!ws || ws_bytes < need) return FC_ERR_WORKSPACE;
     if (!fc::aligned16(ws)) return FC_ERR_MISALIGNED;
@@ -101,5 +114,6 @@ extern "C" int fc_chunk_attention_kv4(fc_ctx* ctx, void* stream, const fc_attn_d
     g.part_ml = (float2*)((char*)ws + fc::align_up(parts * a.d * sizeof(float), 256));
   }
   FC_DEVICE_GUARD(ctx);
-  return fc::kv4_simt((cudaStream_t)stream, g, Q, K, V, dtype, O);
+  cudaStream_t st = (cudaStream_t)stream;
+  return path == kSimt ? fc::kv4_simt(st, g, Q, K, V, dtype, O) : fc::kv4_rows(st, g, Q, K, V, O);
 }
