@@ -9,11 +9,13 @@ namespace fc {
 // Query rows are taken per key head: the `group` query heads that share it are rows of the same tile, so that a key is
 // fetched and unpacked once for all of them.  Virtual row v of chunk c and key head hk is query head hk * group + v % group,
 // row q_row_off[c] + v / group.
+constexpr int kKv4MaxSplits = 512;
+
 struct Kv4AttnGeom {
   AttnGeom a;        // segments and store fields describe the window; vis counts cache and window together
   Kv4View cache;
   int32_t n_cache;
-  int32_t n_splits;  // parts the keys are cut into
+  int32_t n_splits;  // parts the keys are cut into, at most kKv4MaxSplits
   int32_t part_keys; // keys per part
   int32_t cache_parts, window_part_keys;  // few-row kernel: parts of the clean region come first, then parts of the window
   int64_t n_vrows;   // virtual rows per key head, all chunks

@@ -26,6 +26,13 @@ using namespace fc::sm100;  // ex2, cvt_bf16x2, max3
 constexpr int kWarps = 4, kThreads = 32 * kWarps;
 constexpr int kStep = 16;  // keys per warp and step
 constexpr float kRescaleThreshold = 8.f;
+#ifndef BP1
+#define BP1 3
+#endif
+#ifndef BP2
+#define BP2 2
+#endif
+constexpr int blocks_per_sm(int nt) { return nt == 1 ? BP1 : BP2; }  // resident, by the registers the kernel is given
 
 __device__ __forceinline__ void mma(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
   asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
@@ -39,44 +46,55 @@ __device__ __forceinline__ uint32_t transpose8x8(uint32_t x) {
 }
 __device__ __forceinline__ uint32_t prmt(uint32_t a, uint32_t b, uint32_t sel) { return __byte_perm(a, b, sel); }
 
-// The operands of one step as they lie in memory.
-template <int D> struct Raw {
-  static constexpr int WK = D / 32, WV = D / 64;  // words of codes per lane and key
-  uint32_t k[2][WK], ks[2], v[4][WV], vs[4];
+// A warp's ring of 16-key steps in shared memory, filled by cp.async: the codes of K and V, then their scales.
+template <int D> struct Ring {
+  static constexpr int kCodes = kStep * D / 2, kScales = kStep * D / 16;  // bytes of one tensor's step
+  static constexpr int kBytes = 2 * (kCodes + kScales);
+  static constexpr int kStages = 4;
 };
 
-template <int N> __device__ __forceinline__ void load_words(const uint8_t* p, uint32_t (&w)[N]) {
+template <int N> __device__ __forceinline__ void cp_async(uint32_t dst, const void* src) {
+  if constexpr (N == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+  else asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(dst), "l"(src), "n"(N) : "memory");
+}
+__device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N> __device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
+// N words of shared memory in one access
+template <int N> __device__ __forceinline__ void lds_words(const uint8_t* p, uint32_t (&w)[N]) {
   if constexpr (N == 4) {
-    const uint4 x = __ldg(reinterpret_cast<const uint4*>(p));
+    const uint4 x = *reinterpret_cast<const uint4*>(p);
     w[0] = x.x; w[1] = x.y; w[2] = x.z; w[3] = x.w;
   } else if constexpr (N == 2) {
-    const uint2 x = __ldg(reinterpret_cast<const uint2*>(p));
+    const uint2 x = *reinterpret_cast<const uint2*>(p);
     w[0] = x.x; w[1] = x.y;
   } else {
-    w[0] = __ldg(reinterpret_cast<const uint32_t*>(p));
+    w[0] = *reinterpret_cast<const uint32_t*>(p);
   }
 }
 
-// What a warp carries along its keys: O^T, the maxima (log2 units) and this lane's share of the sums.
+// What a warp carries along its keys: O^T, this lane's share of the sums, and per row the reference of its exponents (log2
+// units) with the logit (as the product gives it) above which the reference moves.  A row that has met no finite logit yet has
+// move_at = -inf and the reference 0: weights of -inf are 0 then, and a NaN stays one.
 template <int D, int NT> struct State {
   float o[NT][D / 16][4];
-  float m[NT][2], l[NT][2];
+  float l[NT][2], ref[NT][2], move_at[NT][2];
 };
 
-// S^T (log2 units, masked) -> P^T operands; moves the maxima where they have to move.
-template <int D, int NT>
+// S^T -> P^T operands.  n_valid: keys of the step that exist (kTail only).
+template <int D, int NT, bool kTail>
 __device__ __forceinline__ void softmax_step(State<D, NT>& st, float (&s)[NT][4], float scale_log2, int lane, int n_valid,
                                              uint32_t (&p0)[NT], uint32_t (&p1)[NT]) {
   bool move = false;
 #pragma unroll
   for (int t = 0; t < NT; ++t) {
+    if (kTail) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      s[t][i] *= scale_log2;
-      if (n_valid < kStep && (lane >> 2) + (i >= 2 ? 8 : 0) >= n_valid) s[t][i] = -INFINITY;
+      for (int i = 0; i < 4; ++i)
+        if ((lane >> 2) + (i >= 2 ? 8 : 0) >= n_valid) s[t][i] = -INFINITY;
     }
-    move |= fmaxf(s[t][0], s[t][2]) > st.m[t][0] + kRescaleThreshold;
-    move |= fmaxf(s[t][1], s[t][3]) > st.m[t][1] + kRescaleThreshold;
+    move |= fmaxf(s[t][0], s[t][2]) > st.move_at[t][0];
+    move |= fmaxf(s[t][1], s[t][3]) > st.move_at[t][1];
   }
   if (__any_sync(0xffffffffu, move)) {
 #pragma unroll
@@ -87,9 +105,11 @@ __device__ __forceinline__ void softmax_step(State<D, NT>& st, float (&s)[NT][4]
         x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 4));
         x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 8));
         x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 16));
-        if (x > st.m[t][r] + kRescaleThreshold) {
-          const float alpha = ex2(st.m[t][r] - x);  // 0 the first time
-          st.m[t][r] = x;
+        if (x > st.move_at[t][r]) {
+          const float ref = x * scale_log2;
+          const float alpha = st.move_at[t][r] == -INFINITY ? 0.f : ex2(st.ref[t][r] - ref);
+          st.ref[t][r] = ref;
+          st.move_at[t][r] = x + kRescaleThreshold / scale_log2;
           st.l[t][r] *= alpha;
 #pragma unroll
           for (int j = 0; j < D / 16; ++j) {
@@ -101,9 +121,8 @@ __device__ __forceinline__ void softmax_step(State<D, NT>& st, float (&s)[NT][4]
   }
 #pragma unroll
   for (int t = 0; t < NT; ++t) {
-    // a row all of whose logits so far are -inf has no maximum yet: its weights are 0 (or NaN, where a logit is)
-    const float m0 = st.m[t][0] == -INFINITY ? 0.f : st.m[t][0], m1 = st.m[t][1] == -INFINITY ? 0.f : st.m[t][1];
-    const float e0 = ex2(s[t][0] - m0), e1 = ex2(s[t][1] - m1), e2 = ex2(s[t][2] - m0), e3 = ex2(s[t][3] - m1);
+    const float e0 = ex2(fmaf(s[t][0], scale_log2, -st.ref[t][0])), e1 = ex2(fmaf(s[t][1], scale_log2, -st.ref[t][1]));
+    const float e2 = ex2(fmaf(s[t][2], scale_log2, -st.ref[t][0])), e3 = ex2(fmaf(s[t][3], scale_log2, -st.ref[t][1]));
     st.l[t][0] += e0 + e2;
     st.l[t][1] += e1 + e3;
     p0[t] = transpose8x8(cvt_bf16x2(e0, e1));
@@ -111,21 +130,72 @@ __device__ __forceinline__ void softmax_step(State<D, NT>& st, float (&s)[NT][4]
   }
 }
 
+// One step over 16 packed keys, which lie at `buf`.
+template <int D, int NT, bool kTail>
+__device__ __forceinline__ void packed_step(State<D, NT>& st, const uint8_t* buf, const uint32_t (&qb)[NT][D / 8], float scale_log2,
+                                            int lane, int n_valid) {
+  using R = Ring<D>;
+  const int n = lane >> 2, q = lane & 3;
+  const uint8_t* kc = buf + n * (D / 2) + q * (D / 8);
+  const uint8_t* vc = buf + R::kCodes + 2 * q * (D / 2) + n * (D / 16);
+  const uint16_t* ks = reinterpret_cast<const uint16_t*>(buf + 2 * R::kCodes) + n * (D / 32) + q * D / 128;
+  const uint16_t* vs = reinterpret_cast<const uint16_t*>(buf + 2 * R::kCodes + R::kScales) + 2 * q * (D / 32) + n * D / 256;
+  float s[NT][4] = {};
+  {
+    uint32_t k0[D / 32], k1[D / 32];
+    lds_words(kc, k0);
+    lds_words(kc + 8 * (D / 2), k1);
+    const uint32_t s0 = fc::kv4_scale2(ks[0]), s1 = fc::kv4_scale2(ks[8 * (D / 32)]);
+    const uint32_t b0 = fc::kv4_bias2(s0), b1 = fc::kv4_bias2(s1);
+#pragma unroll
+    for (int w = 0; w < D / 32; ++w) {
+      uint32_t x[4], y[4];
+      fc::kv4_word(k0[w], s0, b0, x);
+      fc::kv4_word(k1[w], s1, b1, y);
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+        mma(s[t], x[0], y[0], x[1], y[1], qb[t][4 * w], qb[t][4 * w + 1]);
+        mma(s[t], x[2], y[2], x[3], y[3], qb[t][4 * w + 2], qb[t][4 * w + 3]);
+      }
+    }
+  }
+  uint32_t v[4][D / 64], p0[NT], p1[NT];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) lds_words(vc + ((i & 1) + 8 * (i >> 1)) * (D / 2), v[i]);
+  const uint32_t sl = vs[0] | ((uint32_t)vs[D / 32] << 16), sh = vs[8 * (D / 32)] | ((uint32_t)vs[9 * (D / 32)] << 16);
+  const uint32_t bl = fc::kv4_bias2(sl), bh = fc::kv4_bias2(sh);
+  softmax_step<D, NT, kTail>(st, s, scale_log2, lane, n_valid, p0, p1);
+#pragma unroll
+  for (int w = 0; w < D / 64; ++w) {
+    uint32_t el[4], ol[4], eh[4], oh[4];  // even and odd elements, low and high keys
+    fc::kv4_word(prmt(v[0][w], v[1][w], 0x5410), sl, bl, el);
+    fc::kv4_word(prmt(v[0][w], v[1][w], 0x7632), sl, bl, ol);
+    fc::kv4_word(prmt(v[2][w], v[3][w], 0x5410), sh, bh, eh);
+    fc::kv4_word(prmt(v[2][w], v[3][w], 0x7632), sh, bh, oh);
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int t = 0; t < NT; ++t) mma(st.o[t][4 * w + i], el[i], ol[i], eh[i], oh[i], p0[t], p1[t]);
+  }
+}
+
 template <int D, int NT>
-__global__ void __launch_bounds__(kThreads, NT == 1 ? 4 : 3)
+__global__ void __launch_bounds__(kThreads, blocks_per_sm(NT))
 attention_kv4_rows_kernel(const __nv_bfloat16* __restrict__ Q, const __nv_bfloat16* __restrict__ K,
                           const __nv_bfloat16* __restrict__ V, __nv_bfloat16* __restrict__ O,
                           const __grid_constant__ fc::Kv4AttnGeom g) {
   constexpr int kRows = 8 * NT, kLaneDims = D / 4, kLaneCols = D / 8;
-  __shared__ float o_s[kWarps][kRows][D + 4];
+  using R = Ring<D>;
+  // the rings, and after the last step, in their place, what the warps join
+  __shared__ __align__(16) uint8_t smem[kWarps * (R::kStages * R::kBytes > kRows * (D + 4) * 4 ? R::kStages * R::kBytes : kRows * (D + 4) * 4)];
   __shared__ float2 ml_s[kWarps][kRows];
+  fc::pdl_launch_dependents();  // the joining kernel may take its place; it waits for this grid to end
   const fc::AttnGeom& a = g.a;
   const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32, n = lane >> 2, q = lane & 3;
   const int part = blockIdx.x, hk = blockIdx.y;
   int v0 = 0;
   const int c = fc::tile_chunk<kRows>(a, blockIdx.z, v0);
-  if (part == 0 && hk == 0 && blockIdx.z == 0 && tid == 0) fc::report_bad_ids(a);
-  if (c < 0 || !fc::chunk_active(a, c)) return;
+  if (c < 0) return;
   const int rows_here = min(kRows, (a.q_row_off[c + 1] - a.q_row_off[c]) * a.group - v0);
 
   // keys of this part: of the clean region, or of the window
@@ -137,6 +207,37 @@ attention_kv4_rows_kernel(const __nv_bfloat16* __restrict__ Q, const __nv_bfloat
   } else {
     k0 = (part - g.cache_parts) * g.window_part_keys;
     k1 = (int)min((int64_t)k0 + g.window_part_keys, (int64_t)a.vis[c] - g.n_cache);
+  }
+
+  // A step's copies: lane L brings 16 bytes of rows L/4 and L/4 + 8 of the codes, and the scales of a row of K or V.
+  constexpr int kLanesPerRow = D / 32, kRowsPerCopy = 32 / kLanesPerRow;
+  const uint32_t ring = smem_u32(smem) + warp * R::kStages * R::kBytes;
+  auto copy = [&](int stage, int kb) {
+    const uint32_t dst = ring + stage * R::kBytes;
+    if (kb < k1) {
+#pragma unroll
+      for (int i = 0; i < kStep / kRowsPerCopy; ++i) {
+        const int r = i * kRowsPerCopy + lane / kLanesPerRow;
+        const int64_t off = hk * g.cache.code_hs + (int64_t)min(kb + r, k1 - 1) * g.cache.code_rs + lane % kLanesPerRow * 16;
+        const uint32_t at = dst + r * (D / 2) + lane % kLanesPerRow * 16;
+        cp_async<16>(at, g.cache.k_codes + off);
+        cp_async<16>(at + R::kCodes, g.cache.v_codes + off);
+      }
+      const int64_t off = hk * g.cache.scale_hs + (int64_t)min(kb + lane % 16, k1 - 1) * g.cache.scale_rs;
+      cp_async<D / 16>(dst + 2 * R::kCodes + lane * (D / 16), (lane < 16 ? g.cache.k_scales : g.cache.v_scales) + off);
+    }
+    cp_async_commit();
+  };
+  const int kb0 = k0 + kStep * warp;
+  if (!window) {
+#pragma unroll
+    for (int i = 0; i < R::kStages - 1; ++i) copy(i, kb0 + i * kStep * kWarps);
+  }
+  // everything up to here reads only what the host knows; the list is on the device
+  if (part == 0 && hk == 0 && blockIdx.z == 0 && tid == 0) fc::report_bad_ids(a);
+  if (!fc::chunk_active(a, c)) {
+    cp_async_wait<0>();
+    return;
   }
 
   uint32_t qb[NT][kLaneDims / 2];
@@ -159,70 +260,24 @@ attention_kv4_rows_kernel(const __nv_bfloat16* __restrict__ Q, const __nv_bfloat
   for (int t = 0; t < NT; ++t) {
 #pragma unroll
     for (int j = 0; j < D / 16; ++j) st.o[t][j][0] = st.o[t][j][1] = st.o[t][j][2] = st.o[t][j][3] = 0.f;
-    st.m[t][0] = st.m[t][1] = -INFINITY;
-    st.l[t][0] = st.l[t][1] = 0.f;
+    st.l[t][0] = st.l[t][1] = st.ref[t][0] = st.ref[t][1] = 0.f;
+    st.move_at[t][0] = st.move_at[t][1] = -INFINITY;
   }
   const float scale_log2 = a.scale * 1.4426950408889634f;
 
   if (!window) {
-    const uint8_t* kc = g.cache.k_codes + hk * g.cache.code_hs + q * (kLaneDims / 2);
-    const uint8_t* vc = g.cache.v_codes + hk * g.cache.code_hs + n * (kLaneCols / 2);
-    const uint16_t* ks = g.cache.k_scales + hk * g.cache.scale_hs + q * kLaneDims / 32;
-    const uint16_t* vs = g.cache.v_scales + hk * g.cache.scale_hs + n * kLaneCols / 32;
-    // positions behind the last key repeat it: their weights are zero
-    auto load = [&](int kb, Raw<D>& r) {
-#pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        const int64_t j = min(kb + 8 * t + n, k1 - 1);
-        load_words(kc + j * g.cache.code_rs, r.k[t]);
-        r.ks[t] = __ldg(ks + j * g.cache.scale_rs);
-      }
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int64_t j = min(kb + 2 * q + (i & 1) + 8 * (i >> 1), k1 - 1);
-        load_words(vc + j * g.cache.code_rs, r.v[i]);
-        r.vs[i] = __ldg(vs + j * g.cache.scale_rs);
-      }
-    };
-    Raw<D> next;
-    int kb = k0 + kStep * warp;
-    if (kb < k1) load(kb, next);
-    for (; kb < k1; kb += kStep * kWarps) {
-      const Raw<D> r = next;
-      if (kb + kStep * kWarps < k1) load(kb + kStep * kWarps, next);
-      float s[NT][4] = {};
-      {
-        const uint32_t s0 = fc::kv4_scale2(r.ks[0]), s1 = fc::kv4_scale2(r.ks[1]);
-        const uint32_t b0 = fc::kv4_bias2(s0), b1 = fc::kv4_bias2(s1);
-#pragma unroll
-        for (int w = 0; w < Raw<D>::WK; ++w) {
-          uint32_t x[4], y[4];
-          fc::kv4_word(r.k[0][w], s0, b0, x);
-          fc::kv4_word(r.k[1][w], s1, b1, y);
-#pragma unroll
-          for (int t = 0; t < NT; ++t) {
-            mma(s[t], x[0], y[0], x[1], y[1], qb[t][4 * w], qb[t][4 * w + 1]);
-            mma(s[t], x[2], y[2], x[3], y[3], qb[t][4 * w + 2], qb[t][4 * w + 3]);
-          }
-        }
-      }
-      uint32_t p0[NT], p1[NT];
-      softmax_step<D, NT>(st, s, scale_log2, lane, k1 - kb, p0, p1);
-      const uint32_t sl = r.vs[0] | (r.vs[1] << 16), sh = r.vs[2] | (r.vs[3] << 16);
-      const uint32_t bl = fc::kv4_bias2(sl), bh = fc::kv4_bias2(sh);
-#pragma unroll
-      for (int w = 0; w < Raw<D>::WV; ++w) {
-        uint32_t el[4], ol[4], eh[4], oh[4];  // even and odd elements, low and high keys
-        fc::kv4_word(prmt(r.v[0][w], r.v[1][w], 0x5410), sl, bl, el);
-        fc::kv4_word(prmt(r.v[0][w], r.v[1][w], 0x7632), sl, bl, ol);
-        fc::kv4_word(prmt(r.v[2][w], r.v[3][w], 0x5410), sh, bh, eh);
-        fc::kv4_word(prmt(r.v[2][w], r.v[3][w], 0x7632), sh, bh, oh);
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-#pragma unroll
-          for (int t = 0; t < NT; ++t) mma(st.o[t][4 * w + i], el[i], ol[i], eh[i], oh[i], p0[t], p1[t]);
-      }
+    int stage = 0;
+    for (int kb = kb0; kb < k1; kb += kStep * kWarps) {
+      copy(stage == 0 ? R::kStages - 1 : stage - 1, kb + (R::kStages - 1) * kStep * kWarps);
+      cp_async_wait<R::kStages - 1>();
+      __syncwarp();
+      const uint8_t* buf = smem + (warp * R::kStages + stage) * R::kBytes;
+      if (kb + kStep <= k1) packed_step<D, NT, false>(st, buf, qb, scale_log2, lane, kStep);
+      else packed_step<D, NT, true>(st, buf, qb, scale_log2, lane, k1 - kb);
+      __syncwarp();  // the stage has been read by every lane before it is filled again
+      stage = stage == R::kStages - 1 ? 0 : stage + 1;
     }
+    cp_async_wait<0>();
   } else {
     const __nv_bfloat16* kp = K + hk * a.k_hs + q * kLaneDims;
     const __nv_bfloat16* vp = V + hk * a.v_hs + n * kLaneCols;
@@ -242,7 +297,7 @@ attention_kv4_rows_kernel(const __nv_bfloat16* __restrict__ Q, const __nv_bfloat
         }
       }
       uint32_t p0[NT], p1[NT];
-      softmax_step<D, NT>(st, s, scale_log2, lane, k1 - kb, p0, p1);
+      softmax_step<D, NT, true>(st, s, scale_log2, lane, k1 - kb, p0, p1);
       const __nv_bfloat16* r[4];
 #pragma unroll
       for (int i = 0; i < 4; ++i) r[i] = vp + fc::window_row(a, min(kb + 2 * q + (i & 1) + 8 * (i >> 1), k1 - 1)) * a.v_rs;
@@ -263,6 +318,8 @@ attention_kv4_rows_kernel(const __nv_bfloat16* __restrict__ Q, const __nv_bfloat
   }
 
   // join the four warps
+  auto o_s = reinterpret_cast<float(*)[kRows][D + 4]>(smem);
+  __syncthreads();
 #pragma unroll
   for (int t = 0; t < NT; ++t)
 #pragma unroll
@@ -272,7 +329,7 @@ attention_kv4_rows_kernel(const __nv_bfloat16* __restrict__ Q, const __nv_bfloat
       l += __shfl_xor_sync(0xffffffffu, l, 8);
       l += __shfl_xor_sync(0xffffffffu, l, 16);
       const int row = 8 * t + 2 * q + r;
-      if (n == 0) ml_s[warp][row] = make_float2(st.m[t][r], l);
+      if (n == 0) ml_s[warp][row] = make_float2(st.move_at[t][r] == -INFINITY ? -INFINITY : st.ref[t][r], l);
 #pragma unroll
       for (int j = 0; j < D / 16; ++j) {
         o_s[warp][row][n * kLaneCols + 2 * j] = st.o[t][j][r];
@@ -330,18 +387,20 @@ size_t kv4_rows_workspace(const fc_ctx* ctx, Kv4AttnGeom& g) {
   const int nt = tiles_of(g);
   const int64_t tiles = tile_count(g.a, 8 * nt) * g.a.H_kv;
   const int64_t cache = std::min(vis, g.n_cache), window = std::max(vis - g.n_cache, 0);
-  // One set of resident blocks, shared out by what a key costs: a window key has 3.6 times the bytes of a packed one.  At least
-  // two steps of every warp in a part.
-  constexpr int64_t kWindowCost = 3, kLeast = 2 * kStep * kWarps;
-  const int64_t work = cache + kWindowCost * window;
-  const int64_t slots = std::max<int64_t>(1, (int64_t)ctx->sm_count * (nt == 1 ? 4 : 3) / std::max<int64_t>(1, tiles));
-  int64_t per = std::max(kLeast, (work + slots - 1) / slots);
-  per = (per + kStep * kWarps - 1) / (kStep * kWarps) * (kStep * kWarps);
-  const int64_t wper = std::max<int64_t>(kStep * kWarps, per / kWindowCost / (kStep * kWarps) * (kStep * kWarps));
+  // At most one set of resident blocks where that leaves two steps for every warp, shared out by what a key costs: a
+  // window key has 3.6 times the bytes of a packed one.
+  constexpr int64_t kWindowCost = 3, kAll = kStep * kWarps, kLeast = 2 * kAll;
+  const int64_t slots = std::min<int64_t>(kKv4MaxSplits, std::max<int64_t>(1, (int64_t)ctx->sm_count * blocks_per_sm(nt) / std::max<int64_t>(1, tiles)));
+  auto parts_of = [&](int64_t per, int64_t wper) { return (cache + per - 1) / per + (window + wper - 1) / wper; };
+  int64_t per = std::max(kLeast, (cache + kWindowCost * window) / slots / kAll * kAll), wper;
+  for (;; per += kAll) {
+    wper = std::max<int64_t>(kAll, per / kWindowCost / kAll * kAll);
+    if (parts_of(per, wper) <= std::max<int64_t>(slots, (cache > 0) + (window > 0))) break;
+  }
   g.part_keys = (int32_t)std::min<int64_t>(per, INT32_MAX / 2);
   g.window_part_keys = (int32_t)std::min<int64_t>(wper, INT32_MAX / 2);
   g.cache_parts = (int32_t)((cache + g.part_keys - 1) / g.part_keys);
-  g.n_splits = (int32_t)std::max<int64_t>(1, g.cache_parts + (window + g.window_part_keys - 1) / g.window_part_keys);
+  g.n_splits = (int32_t)std::max<int64_t>(1, parts_of(g.part_keys, g.window_part_keys));
   if (g.n_splits == 1) return 0;
   const int64_t parts = g.a.H_kv * g.n_vrows * g.n_splits;
   return align_up(parts * g.a.d * sizeof(float), 256) + align_up(parts * sizeof(float2), 256);

@@ -14,6 +14,7 @@ namespace {
 
 constexpr int kRows = 32, kKeys = 32, kThreads = 128;
 constexpr int kMinPart = 128, kMaxSplits = 64;
+constexpr int kCombineThreads = 256;
 
 template <typename T> __device__ __forceinline__ float4 load4(const T* p);
 template <> __device__ __forceinline__ float4 load4<float>(const float* p) { return *reinterpret_cast<const float4*>(p); }
@@ -160,40 +161,84 @@ attention_kv4_simt_kernel(const T* __restrict__ Q, const T* __restrict__ K, cons
   if (a.lse && t == 0) a.lse[(int64_t)h * a.lse_hs + row] = l > 0.f ? m + logf(l) : (l == l ? -INFINITY : l);
 }
 
-// One warp joins the parts of one virtual row: O = sum_p e^(m_p - m) o_p / sum_p e^(m_p - m) l_p.
+// One block joins the parts of one virtual row: O = sum_p e^(m_p - m) o_p / sum_p e^(m_p - m) l_p.  The weights first, one part per
+// thread; then groups of D/4 threads add up every so-many-th part, four elements a thread, and join through shared memory.
+// A lone token has hundreds of parts at most and a few rows: what counts is that no load waits for another.
 template <typename T, int D, bool kLog2>
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(kCombineThreads)
 kv4_combine_kernel(T* __restrict__ O, const __grid_constant__ fc::Kv4AttnGeom g) {
+  constexpr int kLanes = D / 4, kGroups = kCombineThreads / kLanes, kWarps = kCombineThreads / 32;
+  __shared__ float w_s[fc::kKv4MaxSplits];
+  __shared__ float4 o_s[kGroups][kLanes];
+  __shared__ float m_s[kWarps], l_s[kWarps];
   const fc::AttnGeom& a = g.a;
-  const int lane = threadIdx.x % 32, hk = blockIdx.y;
-  const int64_t vr = (int64_t)blockIdx.x * (kThreads / 32) + threadIdx.x / 32;
-  if (vr >= g.n_vrows) return;
+  const int tid = threadIdx.x, lane = tid % 32, warp = tid / 32, hk = blockIdx.y;
+  const int64_t vr = blockIdx.x;
   const int row = a.q_row_off[0] + (int)(vr / a.group), h = hk * a.group + (int)(vr % a.group);
   int c = 0;
   while (c + 1 < a.W && row >= a.q_row_off[c + 1]) ++c;
-  if (!fc::chunk_active(a, c)) return;
+  const bool on = fc::chunk_active(a, c);
+  fc::pdl_wait();  // the list was there before the kernel that wrote the parts began; the parts are there now
+  if (!on) return;
   const int64_t at = (hk * g.n_vrows + vr) * g.n_splits;
   auto power = [](float x) { return kLog2 ? exp2f(x) : expf(x); };
+
   float m = -INFINITY;
-  for (int p = lane; p < g.n_splits; p += 32) m = fmaxf(m, g.part_ml[at + p].x);
+  float2 mine[(fc::kKv4MaxSplits + kCombineThreads - 1) / kCombineThreads];
+#pragma unroll
+  for (int i = 0; i < (int)(sizeof(mine) / sizeof(mine[0])); ++i) {
+    const int p = tid + i * kCombineThreads;
+    mine[i] = p < g.n_splits ? g.part_ml[at + p] : make_float2(-INFINITY, 0.f);
+    m = fmaxf(m, mine[i].x);
+  }
 #pragma unroll
   for (int k = 16; k; k >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, k));
-  float l = 0.f, o[D / 32] = {};
-  for (int p = 0; p < g.n_splits; ++p) {
-    const float2 ml = g.part_ml[at + p];
-    if (!(ml.y != 0.f)) continue;  // an empty part: its maximum is -inf
-    const float w = power(ml.x - m);
-    l += w * ml.y;
+  if (lane == 0) m_s[warp] = m;
+  __syncthreads();
 #pragma unroll
-    for (int i = 0; i < D / 32; ++i) o[i] = fmaf(w, g.part_o[(at + p) * D + i * 32 + lane], o[i]);
+  for (int w = 0; w < kWarps; ++w) m = fmaxf(m, m_s[w]);
+  float l = 0.f;
+#pragma unroll
+  for (int i = 0; i < (int)(sizeof(mine) / sizeof(mine[0])); ++i) {
+    const int p = tid + i * kCombineThreads;
+    const float w = mine[i].y != 0.f ? power(mine[i].x - m) : 0.f;  // an empty part: its maximum is -inf
+    if (p < g.n_splits) w_s[p] = w;
+    l += w == 0.f ? (mine[i].y == mine[i].y ? 0.f : mine[i].y) : w * mine[i].y;
   }
-  const float inv = l > 0.f ? 1.f / l : (l == l ? 0.f : l);
-  T* out = O + (int64_t)h * a.o_hs + (int64_t)row * a.o_rs;
 #pragma unroll
-  for (int i = 0; i < D / 32; ++i) store1(out + i * 32 + lane, o[i] * inv);
-  if (a.lse && lane == 0)
-    a.lse[(int64_t)h * a.lse_hs + row] =
-        l > 0.f ? (kLog2 ? (m + log2f(l)) * 0.6931471805599453f : m + logf(l)) : (l == l ? -INFINITY : l);
+  for (int k = 16; k; k >>= 1) l += __shfl_xor_sync(0xffffffffu, l, k);
+  if (lane == 0) l_s[warp] = l;
+  __syncthreads();
+  l = 0.f;
+#pragma unroll
+  for (int w = 0; w < kWarps; ++w) l += l_s[w];
+
+  const int grp = tid / kLanes, d4 = tid % kLanes;
+  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+  for (int p = grp; p < g.n_splits; p += kGroups) {
+    const float4 x = *reinterpret_cast<const float4*>(g.part_o + (at + p) * D + 4 * d4);
+    const float w = w_s[p];
+    o.x = fmaf(w, x.x, o.x); o.y = fmaf(w, x.y, o.y); o.z = fmaf(w, x.z, o.z); o.w = fmaf(w, x.w, o.w);
+  }
+  o_s[grp][d4] = o;
+  __syncthreads();
+  if (tid < kLanes) {
+#pragma unroll
+    for (int k = 1; k < kGroups; ++k) {
+      const float4 x = o_s[k][tid];
+      o.x += x.x; o.y += x.y; o.z += x.z; o.w += x.w;
+    }
+    const float inv = l > 0.f ? 1.f / l : (l == l ? 0.f : l);
+    T* out = O + (int64_t)h * a.o_hs + (int64_t)row * a.o_rs + 4 * tid;
+    store1(out, o.x * inv);
+    store1(out + 1, o.y * inv);
+    store1(out + 2, o.z * inv);
+    store1(out + 3, o.w * inv);
+    if (a.lse && tid == 0)
+      a.lse[(int64_t)h * a.lse_hs + row] =
+          l > 0.f ? (kLog2 ? (m + log2f(l)) * 0.6931471805599453f : m + logf(l)) : (l == l ? -INFINITY : l);
+  }
 }
 
 }  // namespace
@@ -215,12 +260,11 @@ size_t kv4_simt_workspace(const fc_ctx* ctx, Kv4AttnGeom& g) {
 }
 
 int kv4_combine(cudaStream_t st, const Kv4AttnGeom& g, int dtype, void* O, bool log2_units) {
-  const int64_t blocks = (g.n_vrows + kThreads / 32 - 1) / (kThreads / 32);
-  const dim3 grid((unsigned)blocks, (unsigned)g.a.H_kv);
+  const dim3 grid((unsigned)g.n_vrows, (unsigned)g.a.H_kv);
 #define FC_COMBINE(T, D)                                                                    \
   do {                                                                                      \
-    if (log2_units) kv4_combine_kernel<T, D, true><<<grid, kThreads, 0, st>>>((T*)O, g);    \
-    else kv4_combine_kernel<T, D, false><<<grid, kThreads, 0, st>>>((T*)O, g);              \
+    auto kernel = log2_units ? kv4_combine_kernel<T, D, true> : kv4_combine_kernel<T, D, false>; \
+    FC_CUDA_CHECK(launch_pdl(kernel, grid, dim3(kCombineThreads), 0, st, (T*)O, g));               \
   } while (0)
   if (dtype == FC_F32) { if (g.a.d == 128) FC_COMBINE(float, 128); else FC_COMBINE(float, 64); }
   else { if (g.a.d == 128) FC_COMBINE(__nv_bfloat16, 128); else FC_COMBINE(__nv_bfloat16, 64); }
