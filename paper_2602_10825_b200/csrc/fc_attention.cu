@@ -54,6 +54,7 @@ extern "C" int fc_chunk_attention(fc_ctx* ctx, void* stream, const fc_attn_desc*
   }
   int64_t logical_len = kv_token_index ? kv_index_hs : 0;
   g.n_seg = kv_token_index ? 0 : n_seg;
+  g.n_seg0 = 0;
   if (!kv_token_index) {
     for (int s = 0; s <= n_seg; ++s) {
       g.seg_log[s] = seg_logical_off[s];

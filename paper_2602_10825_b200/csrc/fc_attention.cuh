@@ -9,6 +9,7 @@ namespace fc {
 
 struct AttnGeom {
   int32_t H_q, H_kv, d, W, group, n_seg;
+  int32_t n_seg0;  // leading segments that lie in a second store (attention_tc_two), else 0
   int64_t q_hs, q_rs, k_hs, k_rs, v_hs, v_rs, o_hs, o_rs, kv_rows, lse_hs, tok_hs;
   float scale;
   int32_t q_row_off[FC_MAX_CHUNKS + 1];
@@ -28,9 +29,15 @@ int attention_simt(cudaStream_t st, const AttnGeom& g, const void* Q, const void
 int attention_tc(fc_ctx* ctx, cudaStream_t st, const AttnGeom& g, const void* Q, const void* K,
                  const void* V, void* O, void* ws, size_t ws_bytes);
 size_t attention_tc_workspace_bytes();
-// warp-specialised kernel; tensor maps as built by attention_tc, `counter` = 4 bytes of workspace
+// The same over two stores: logical tokens [0, n0) are the rows of K0 / V0 (dense [H_kv, n0, d]), the others are found
+// in K / V through the segment table, whose offsets count from n0.
+int attention_tc_two(fc_ctx* ctx, cudaStream_t st, const AttnGeom& g, const void* Q, const void* K0, const void* V0, int n0,
+                     const void* K, const void* V, void* O, void* ws, size_t ws_bytes);
+// warp-specialised kernel; tensor maps as built by attention_tc (tk0, tv0: those of the second store, or NULL),
+// `counter` = 4 bytes of workspace
 int attention_ws_launch(fc_ctx* ctx, cudaStream_t st, const AttnGeom& g, const CUtensorMap& tq,
-                        const CUtensorMap& tk, const CUtensorMap& tv, void* O, uint32_t* counter);
+                        const CUtensorMap& tk, const CUtensorMap& tv, const CUtensorMap* tk0, const CUtensorMap* tv0,
+                        void* O, uint32_t* counter);
 bool attention_tc_supported(const AttnGeom& g, int dtype);
 // Tensor map of a [heads, rows, d] bf16 tensor: box = 64 elements (128 bytes) x `box_rows` rows x 1 head, 128-byte
 // swizzle; rows past `rows` read as zero.

@@ -17,6 +17,7 @@ int check_geometry(const fc_attn_desc* desc, int dtype, const int32_t* q_chunk_r
   if (desc->W > FC_MAX_CHUNKS || desc->H_kv > 65535) return FC_ERR_UNSUPPORTED;
   if (desc->impl < 0 || desc->impl > 3) return FC_ERR_INVALID_ARG;
   if (!(desc->scale >= 0.f)) return FC_ERR_INVALID_ARG;
+  if (desc->impl >= 2 && dtype != FC_BF16) return FC_ERR_UNSUPPORTED;
   fc::AttnGeom& a = g.a;
   a.H_q = desc->H_q; a.H_kv = desc->H_kv; a.d = desc->d; a.W = desc->W;
   a.group = desc->H_q / desc->H_kv;
@@ -36,15 +37,26 @@ int check_geometry(const fc_attn_desc* desc, int dtype, const int32_t* q_chunk_r
   return FC_OK;
 }
 
-enum Path { kSimt, kRowsPath };
+enum Path { kSimt, kRows, kUnpacked };
 
 Path choose(const fc_attn_desc* desc, int dtype, const fc::Kv4AttnGeom& g) {
   if (dtype == FC_F32 || desc->impl == 1) return kSimt;
-  return kRowsPath;
+  if (desc->impl == 2) return kUnpacked;
+  if (desc->impl == 3) return kRows;
+  return g.n_vrows > 256 ? kUnpacked : kRows;
+}
+
+// Rows of the clean region that some chunk sees.
+int cache_rows(const fc::Kv4AttnGeom& g) {
+  int n = 0;
+  for (int c = 0; c < g.a.W; ++c) n = std::max(n, g.a.vis[c]);
+  return std::min(n, g.n_cache);
 }
 
 size_t plan(const fc_ctx* ctx, Path path, fc::Kv4AttnGeom& g) {
-  return path == kSimt ? fc::kv4_simt_workspace(ctx, g) : fc::kv4_rows_workspace(ctx, g);
+  if (path == kSimt) return fc::kv4_simt_workspace(ctx, g);
+  if (path == kRows) return fc::kv4_rows_workspace(ctx, g);
+  return fc::attention_tc_workspace_bytes() + 2 * (size_t)g.a.H_kv * cache_rows(g) * g.a.d * 2;
 }
 
 }  // namespace
@@ -109,11 +121,20 @@ extern "C" int fc_chunk_attention_kv4(fc_ctx* ctx, void* stream, const fc_attn_d
   if (need > 0) {
     if (!ws || ws_bytes < need) return FC_ERR_WORKSPACE;
     if (!fc::aligned16(ws)) return FC_ERR_MISALIGNED;
-    const int64_t parts = a.H_kv * g.n_vrows * g.n_splits;
-    g.part_o = (float*)ws;
-    g.part_ml = (float2*)((char*)ws + fc::align_up(parts * a.d * sizeof(float), 256));
+    if (path != kUnpacked) {
+      const int64_t parts = a.H_kv * g.n_vrows * g.n_splits;
+      g.part_o = (float*)ws;
+      g.part_ml = (float2*)((char*)ws + fc::align_up(parts * a.d * sizeof(float), 256));
+    }
   }
   FC_DEVICE_GUARD(ctx);
   cudaStream_t st = (cudaStream_t)stream;
-  return path == kSimt ? fc::kv4_simt(st, g, Q, K, V, dtype, O) : fc::kv4_rows(st, g, Q, K, V, O);
+  if (path == kSimt) return fc::kv4_simt(st, g, Q, K, V, dtype, O);
+  if (path == kRows) return fc::kv4_rows(st, g, Q, K, V, O);
+  const int n0 = cache_rows(g);
+  char* K0 = (char*)ws + fc::attention_tc_workspace_bytes();
+  char* V0 = K0 + (size_t)a.H_kv * n0 * a.d * 2;
+  const int64_t hs = (int64_t)n0 * a.d;
+  if (n0 > 0 && (rc = fc::kv4_unpack_launch(ctx, st, g.cache, a.H_kv, a.d, 0, n0, K0, V0, FC_BF16, hs, a.d, hs, a.d)) != FC_OK) return rc;
+  return fc::attention_tc_two(ctx, st, a, Q, K0, V0, n0, K, V, O, ws, ws_bytes);
 }

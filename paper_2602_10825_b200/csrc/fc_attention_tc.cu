@@ -69,6 +69,25 @@ bool attention_tc_supported(const AttnGeom& g, int dtype) {
   return true;
 }
 
+// Writes the segments of `in` to `out`, behind n segments that are there already and with logical offsets moved by `shift`;
+// logically adjacent segments that are also physically adjacent become one: fewer ragged tails.  Returns the new number.
+static int merge_segments(const AttnGeom& in, AttnGeom& out, int n, int32_t shift) {
+  const int n_first = n;
+  for (int s = 0; s < in.n_seg; ++s) {
+    const int len = in.seg_log[s + 1] - in.seg_log[s];
+    if (len == 0) continue;
+    if (n > n_first && out.seg_phys[n - 1] + (out.seg_log[n] - out.seg_log[n - 1]) == in.seg_phys[s]) {
+      out.seg_log[n] = shift + in.seg_log[s + 1];
+    } else {
+      out.seg_phys[n] = in.seg_phys[s];
+      out.seg_log[n] = shift + in.seg_log[s];
+      out.seg_log[n + 1] = shift + in.seg_log[s + 1];
+      ++n;
+    }
+  }
+  return n;
+}
+
 int attention_tc(fc_ctx* ctx, cudaStream_t st, const AttnGeom& g_in, const void* Q, const void* K, const void* V,
                  void* O, void* ws, size_t ws_bytes) {
   if (!ws || ws_bytes < attention_tc_workspace_bytes()) return FC_ERR_WORKSPACE;
@@ -80,21 +99,7 @@ int attention_tc(fc_ctx* ctx, cudaStream_t st, const AttnGeom& g_in, const void*
     g.seg_log[1] = (int32_t)std::min<int64_t>(g.tok_hs, INT32_MAX);
     g.seg_phys[0] = 0;
   }
-  // merge logically adjacent segments that are also physically adjacent: fewer ragged tails
-  int n = 0;
-  for (int s = 0; s < (g.tok_index ? 0 : g_in.n_seg); ++s) {
-    const int len = g_in.seg_log[s + 1] - g_in.seg_log[s];
-    if (len == 0) continue;
-    if (n > 0 && g.seg_phys[n - 1] + (g.seg_log[n] - g.seg_log[n - 1]) == g_in.seg_phys[s]) {
-      g.seg_log[n] = g_in.seg_log[s + 1];
-    } else {
-      g.seg_phys[n] = g_in.seg_phys[s];
-      g.seg_log[n] = g_in.seg_log[s];
-      g.seg_log[n + 1] = g_in.seg_log[s + 1];
-      ++n;
-    }
-  }
-  if (!g.tok_index) g.n_seg = n;
+  if (!g.tok_index) g.n_seg = merge_segments(g_in, g, 0, 0);
   int64_t q_rows = g.q_row_off[g.W];
   int max_tiles = 0;
   for (int c = 0; c < g.W; ++c) max_tiles += (g.q_row_off[c + 1] - g.q_row_off[c] + kBM - 1) / kBM;
@@ -109,7 +114,35 @@ int attention_tc(fc_ctx* ctx, cudaStream_t st, const AttnGeom& g_in, const void*
     if ((rc = make_tmap(ctx, &tk, K, g.d, g.kv_rows, g.H_kv, g.k_rs, g.H_kv > 1 ? g.k_hs : g.k_rs * g.kv_rows)) != FC_OK) return rc;
     if ((rc = make_tmap(ctx, &tv, V, g.d, g.kv_rows, g.H_kv, g.v_rs, g.H_kv > 1 ? g.v_hs : g.v_rs * g.kv_rows)) != FC_OK) return rc;
   }
-  return attention_ws_launch(ctx, st, g, tq, tk, tv, O, (uint32_t*)ws);
+  return attention_ws_launch(ctx, st, g, tq, tk, tv, nullptr, nullptr, O, (uint32_t*)ws);
+}
+
+int attention_tc_two(fc_ctx* ctx, cudaStream_t st, const AttnGeom& g_in, const void* Q, const void* K0, const void* V0, int n0,
+                     const void* K, const void* V, void* O, void* ws, size_t ws_bytes) {
+  if (!ws || ws_bytes < attention_tc_workspace_bytes()) return FC_ERR_WORKSPACE;
+  if (!aligned16(ws)) return FC_ERR_MISALIGNED;
+  if (n0 == 0 && g_in.n_seg > 0) return attention_tc(ctx, st, g_in, Q, K, V, O, ws, ws_bytes);
+  AttnGeom g = g_in;
+  g.n_seg = g.n_seg0 = 0;
+  if (n0 > 0) {
+    g.seg_log[0] = 0;
+    g.seg_log[1] = n0;
+    g.seg_phys[0] = 0;
+    g.n_seg = g.n_seg0 = 1;
+  }
+  g.n_seg = merge_segments(g_in, g, g.n_seg, n0);
+  const int64_t q_rows = g.q_row_off[g.W];
+  if (q_rows == 0) return FC_OK;
+  CUtensorMap tq, tk0, tv0, tk, tv;
+  int rc;
+  if ((rc = make_tmap(ctx, &tq, Q, g.d, q_rows, g.H_q, g.q_rs, g.H_q > 1 ? g.q_hs : g.q_rs * q_rows)) != FC_OK) return rc;
+  if (n0 == 0) return attention_ws_launch(ctx, st, g, tq, tq, tq, nullptr, nullptr, O, (uint32_t*)ws);  // no token at all
+  if ((rc = make_tmap(ctx, &tk0, K0, g.d, n0, g.H_kv, g.d, (int64_t)n0 * g.d)) != FC_OK) return rc;
+  if ((rc = make_tmap(ctx, &tv0, V0, g.d, n0, g.H_kv, g.d, (int64_t)n0 * g.d)) != FC_OK) return rc;
+  if (g.n_seg == 1) return attention_ws_launch(ctx, st, g, tq, tk0, tv0, nullptr, nullptr, O, (uint32_t*)ws);
+  if ((rc = make_tmap(ctx, &tk, K, g.d, g.kv_rows, g.H_kv, g.k_rs, g.H_kv > 1 ? g.k_hs : g.k_rs * g.kv_rows)) != FC_OK) return rc;
+  if ((rc = make_tmap(ctx, &tv, V, g.d, g.kv_rows, g.H_kv, g.v_rs, g.H_kv > 1 ? g.v_hs : g.v_rs * g.kv_rows)) != FC_OK) return rc;
+  return attention_ws_launch(ctx, st, g, tq, tk, tv, &tk0, &tv0, O, (uint32_t*)ws);
 }
 
 }  // namespace fc

@@ -137,13 +137,20 @@ __device__ __forceinline__ void warp_wait(uint32_t bar, uint32_t parity, volatil
   mbar_wait_bounded(bar, parity, abort);
 }
 
-// kGather: the logical key/value tokens are reached through the per-head token map g.tok_index (tmap_k / tmap_v are
-// then 2-D maps over all rows of all heads, box one row high) instead of the segment table.
-template <int D, bool kGather>
+// How logical key / value tokens are reached.
+//   kSegments   the segment table, one store
+//   kGatherMap  the per-head token map g.tok_index (tmap_k / tmap_v are then 2-D maps over all rows of all heads, box one
+//               row high)
+//   kTwoStores  the segment table; the first g.n_seg0 segments lie in a store of their own (tmap_k0 / tmap_v0)
+enum Source { kSegments, kGatherMap, kTwoStores };
+
+template <int D, Source kSource>
 __global__ void __launch_bounds__(kThreads, 1)
 attention_ws_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant__ CUtensorMap tmap_k,
-                    const __grid_constant__ CUtensorMap tmap_v, const __grid_constant__ fc::AttnGeom g,
+                    const __grid_constant__ CUtensorMap tmap_v, const __grid_constant__ CUtensorMap tmap_k0,
+                    const __grid_constant__ CUtensorMap tmap_v0, const __grid_constant__ fc::AttnGeom g,
                     __nv_bfloat16* __restrict__ O, uint32_t* __restrict__ counter) {
+  constexpr bool kGather = kSource == kGatherMap;
   constexpr uint32_t kTileBytes = kBM * D * 2;
   constexpr int kAtoms = D / 64;
   constexpr uint32_t kAtomBytes = kBM * 128;
@@ -182,6 +189,10 @@ attention_ws_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
     tma_prefetch_desc(&tmap_q);
     tma_prefetch_desc(&tmap_k);
     tma_prefetch_desc(&tmap_v);
+    if (kSource == kTwoStores) {
+      tma_prefetch_desc(&tmap_k0);
+      tma_prefetch_desc(&tmap_v0);
+    }
     // active chunks sorted by visible length, longest first (insertion sort, at most 64 entries)
     const int n_in = min(max(*g.n_active, 0), g.W);
     int n = 0;
@@ -314,20 +325,22 @@ attention_ws_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
       for (int s = 0; s < g.n_seg; ++s) {
         const int seg_vis = min(g.seg_log[s + 1], it.n_vis) - g.seg_log[s];
         if (seg_vis <= 0) break;
+        const CUtensorMap* map_k = kSource == kTwoStores && s < g.n_seg0 ? &tmap_k0 : &tmap_k;
+        const CUtensorMap* map_v = kSource == kTwoStores && s < g.n_seg0 ? &tmap_v0 : &tmap_v;
         for (int j0 = 0; j0 < seg_vis; j0 += kBN, ++kv) {
           const int st = kv % kStages, ph = (kv / kStages) & 1, prow = g.seg_phys[s] + j0;
           warp_wait(smem_u32(&sh->k_empty[st]), ph ^ 1, abort);
           if (lane == 0) {
             mbar_expect_tx(smem_u32(&sh->k_full[st]), kTileBytes);
             for (int x = 0; x < kAtoms; ++x)
-              tma_load_3d(k_s + st * kTileBytes + x * kAtomBytes, &tmap_k, smem_u32(&sh->k_full[st]), x * 64, prow,
+              tma_load_3d(k_s + st * kTileBytes + x * kAtomBytes, map_k, smem_u32(&sh->k_full[st]), x * 64, prow,
                           it.hk);
           }
           warp_wait(smem_u32(&sh->v_empty[st]), ph ^ 1, abort);
           if (lane == 0) {
             mbar_expect_tx(smem_u32(&sh->v_full[st]), kTileBytes);
             for (int x = 0; x < kAtoms; ++x)
-              tma_load_3d(v_s + st * kTileBytes + x * kAtomBytes, &tmap_v, smem_u32(&sh->v_full[st]), x * 64, prow,
+              tma_load_3d(v_s + st * kTileBytes + x * kAtomBytes, map_v, smem_u32(&sh->v_full[st]), x * 64, prow,
                           it.hk);
           }
           __syncwarp();
@@ -660,7 +673,8 @@ attention_ws_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
 namespace fc {
 
 int attention_ws_launch(fc_ctx* ctx, cudaStream_t st, const AttnGeom& g, const CUtensorMap& tq,
-                        const CUtensorMap& tk, const CUtensorMap& tv, void* O, uint32_t* counter) {
+                        const CUtensorMap& tk, const CUtensorMap& tv, const CUtensorMap* tk0, const CUtensorMap* tv0,
+                        void* O, uint32_t* counter) {
   int max_items = 0;
   for (int c = 0; c < g.W; ++c) max_items += (g.q_row_off[c + 1] - g.q_row_off[c] + 2 * kBM - 1) / (2 * kBM);
   const int64_t items = (int64_t)max_items * g.H_q;
@@ -672,12 +686,13 @@ int attention_ws_launch(fc_ctx* ctx, cudaStream_t st, const AttnGeom& g, const C
   const size_t smem = std::max<size_t>(need, 120 * 1024);
   auto launch = [&](auto kernel) -> int {
     FC_CUDA_CHECK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
-    kernel<<<grid, kThreads, smem, st>>>(tq, tk, tv, g, (__nv_bfloat16*)O, counter);
+    kernel<<<grid, kThreads, smem, st>>>(tq, tk, tv, tk0 ? *tk0 : tk, tv0 ? *tv0 : tv, g, (__nv_bfloat16*)O, counter);
     return FC_OK;
   };
   int rc;
-  if (g.tok_index) rc = g.d == 128 ? launch(attention_ws_kernel<128, true>) : launch(attention_ws_kernel<64, true>);
-  else rc = g.d == 128 ? launch(attention_ws_kernel<128, false>) : launch(attention_ws_kernel<64, false>);
+  if (g.tok_index) rc = g.d == 128 ? launch(attention_ws_kernel<128, kGatherMap>) : launch(attention_ws_kernel<64, kGatherMap>);
+  else if (tk0) rc = g.d == 128 ? launch(attention_ws_kernel<128, kTwoStores>) : launch(attention_ws_kernel<64, kTwoStores>);
+  else rc = g.d == 128 ? launch(attention_ws_kernel<128, kSegments>) : launch(attention_ws_kernel<64, kSegments>);
   if (rc != FC_OK) return rc;
   FC_LAUNCH_CHECK("attention_ws_kernel");
   return FC_OK;
