@@ -23,6 +23,14 @@ struct AttnGeom {
   uint32_t* status;
 };
 
+// Parts of the keys whose results another kernel joins (attention_tc_two only; n_splits 1: no parts).
+struct AttnSplit {
+  int32_t n_splits = 1, part_keys = 0;  // part p: logical keys [p part_keys, (p + 1) part_keys), the last one to the end
+  int64_t n_vrows = 0;
+  float* o = nullptr;   // [H_kv, n_vrows, n_splits, d]: sums not divided by their weights
+  float2* ml = nullptr; // [H_kv, n_vrows, n_splits]: reference (log2 units) and sum of the weights
+};
+
 int attention_simt(cudaStream_t st, const AttnGeom& g, const void* Q, const void* K, const void* V,
                    int dtype, void* O);
 // bf16 only: builds the tensor maps and launches the warp-specialised tcgen05 kernel.
@@ -32,12 +40,12 @@ size_t attention_tc_workspace_bytes();
 // The same over two stores: logical tokens [0, n0) are the rows of K0 / V0 (dense [H_kv, n0, d]), the others are found
 // in K / V through the segment table, whose offsets count from n0.
 int attention_tc_two(fc_ctx* ctx, cudaStream_t st, const AttnGeom& g, const void* Q, const void* K0, const void* V0, int n0,
-                     const void* K, const void* V, void* O, void* ws, size_t ws_bytes);
+                     const void* K, const void* V, const AttnSplit& split, void* O, void* ws, size_t ws_bytes);
 // warp-specialised kernel; tensor maps as built by attention_tc (tk0, tv0: those of the second store, or NULL),
 // `counter` = 4 bytes of workspace
 int attention_ws_launch(fc_ctx* ctx, cudaStream_t st, const AttnGeom& g, const CUtensorMap& tq,
                         const CUtensorMap& tk, const CUtensorMap& tv, const CUtensorMap* tk0, const CUtensorMap* tv0,
-                        void* O, uint32_t* counter);
+                        const AttnSplit& split, void* O, uint32_t* counter);
 bool attention_tc_supported(const AttnGeom& g, int dtype);
 // Tensor map of a [heads, rows, d] bf16 tensor: box = 64 elements (128 bytes) x `box_rows` rows x 1 head, 128-byte
 // swizzle; rows past `rows` read as zero.

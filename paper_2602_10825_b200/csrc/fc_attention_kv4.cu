@@ -53,10 +53,46 @@ int cache_rows(const fc::Kv4AttnGeom& g) {
   return std::min(n, g.n_cache);
 }
 
+// Workspace of the unpacked path: the tcgen05 kernel's own, K, V, and the parts where there are any.
+struct UnpackedPlan {
+  fc::AttnSplit split;
+  size_t k, v, o, ml, bytes;  // offsets
+};
+
+UnpackedPlan plan_unpacked(const fc_ctx* ctx, const fc::Kv4AttnGeom& g) {
+  const fc::AttnGeom& a = g.a;
+  UnpackedPlan p;
+  int64_t pairs = 0;
+  int vis = 0;
+  for (int c = 0; c < a.W; ++c) {
+    pairs += (a.q_row_off[c + 1] - a.q_row_off[c] + 255) / 256;  // query rows of a work item
+    vis = std::max(vis, a.vis[c]);
+  }
+  // Work items are handed out one at a time to one block per SM.  With fewer items than two rounds the keys are cut, as
+  // long as a part keeps eight key tiles.
+  const int64_t items = std::max<int64_t>(1, pairs * a.H_q);
+  const int64_t tiles = (vis + 127) / 128;
+  int64_t n = 1;
+  if (items < 2 * ctx->sm_count) n = std::min<int64_t>({(2ll * ctx->sm_count) / items, tiles / 8, 64});
+  if (n > 1) {
+    p.split.part_keys = (int32_t)((tiles + n - 1) / n * 128);
+    p.split.n_splits = (int32_t)((vis + p.split.part_keys - 1) / p.split.part_keys);
+    p.split.n_vrows = g.n_vrows;
+  }
+  const size_t rows = (size_t)a.H_kv * cache_rows(g) * a.d * 2;
+  const size_t parts = p.split.n_splits > 1 ? (size_t)a.H_kv * g.n_vrows * p.split.n_splits : 0;
+  p.k = fc::attention_tc_workspace_bytes();
+  p.v = p.k + fc::align_up(rows, 256);
+  p.o = p.v + fc::align_up(rows, 256);
+  p.ml = p.o + fc::align_up(parts * a.d * sizeof(float), 256);
+  p.bytes = p.ml + parts * sizeof(float2);
+  return p;
+}
+
 size_t plan(const fc_ctx* ctx, Path path, fc::Kv4AttnGeom& g) {
   if (path == kSimt) return fc::kv4_simt_workspace(ctx, g);
   if (path == kRows) return fc::kv4_rows_workspace(ctx, g);
-  return fc::attention_tc_workspace_bytes() + 2 * (size_t)g.a.H_kv * cache_rows(g) * g.a.d * 2;
+  return plan_unpacked(ctx, g).bytes;
 }
 
 }  // namespace
@@ -131,10 +167,15 @@ extern "C" int fc_chunk_attention_kv4(fc_ctx* ctx, void* stream, const fc_attn_d
   cudaStream_t st = (cudaStream_t)stream;
   if (path == kSimt) return fc::kv4_simt(st, g, Q, K, V, dtype, O);
   if (path == kRows) return fc::kv4_rows(st, g, Q, K, V, O);
+  UnpackedPlan p = plan_unpacked(ctx, g);
   const int n0 = cache_rows(g);
-  char* K0 = (char*)ws + fc::attention_tc_workspace_bytes();
-  char* V0 = K0 + (size_t)a.H_kv * n0 * a.d * 2;
+  char* base = (char*)ws;
   const int64_t hs = (int64_t)n0 * a.d;
-  if (n0 > 0 && (rc = fc::kv4_unpack_launch(ctx, st, g.cache, a.H_kv, a.d, 0, n0, K0, V0, FC_BF16, hs, a.d, hs, a.d)) != FC_OK) return rc;
-  return fc::attention_tc_two(ctx, st, a, Q, K0, V0, n0, K, V, O, ws, ws_bytes);
+  if (n0 > 0 && (rc = fc::kv4_unpack_launch(ctx, st, g.cache, a.H_kv, a.d, 0, n0, base + p.k, base + p.v, FC_BF16, hs, a.d, hs, a.d)) != FC_OK)
+    return rc;
+  p.split.o = g.part_o = (float*)(base + p.o);
+  p.split.ml = g.part_ml = (float2*)(base + p.ml);
+  g.n_splits = p.split.n_splits;
+  if ((rc = fc::attention_tc_two(ctx, st, a, Q, base + p.k, base + p.v, n0, K, V, p.split, O, ws, ws_bytes)) != FC_OK) return rc;
+  return p.split.n_splits > 1 ? fc::kv4_combine(st, g, dtype, O, true) : FC_OK;
 }

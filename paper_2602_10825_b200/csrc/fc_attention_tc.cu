@@ -114,14 +114,13 @@ int attention_tc(fc_ctx* ctx, cudaStream_t st, const AttnGeom& g_in, const void*
     if ((rc = make_tmap(ctx, &tk, K, g.d, g.kv_rows, g.H_kv, g.k_rs, g.H_kv > 1 ? g.k_hs : g.k_rs * g.kv_rows)) != FC_OK) return rc;
     if ((rc = make_tmap(ctx, &tv, V, g.d, g.kv_rows, g.H_kv, g.v_rs, g.H_kv > 1 ? g.v_hs : g.v_rs * g.kv_rows)) != FC_OK) return rc;
   }
-  return attention_ws_launch(ctx, st, g, tq, tk, tv, nullptr, nullptr, O, (uint32_t*)ws);
+  return attention_ws_launch(ctx, st, g, tq, tk, tv, nullptr, nullptr, AttnSplit(), O, (uint32_t*)ws);
 }
 
 int attention_tc_two(fc_ctx* ctx, cudaStream_t st, const AttnGeom& g_in, const void* Q, const void* K0, const void* V0, int n0,
-                     const void* K, const void* V, void* O, void* ws, size_t ws_bytes) {
+                     const void* K, const void* V, const AttnSplit& split, void* O, void* ws, size_t ws_bytes) {
   if (!ws || ws_bytes < attention_tc_workspace_bytes()) return FC_ERR_WORKSPACE;
   if (!aligned16(ws)) return FC_ERR_MISALIGNED;
-  if (n0 == 0 && g_in.n_seg > 0) return attention_tc(ctx, st, g_in, Q, K, V, O, ws, ws_bytes);
   AttnGeom g = g_in;
   g.n_seg = g.n_seg0 = 0;
   if (n0 > 0) {
@@ -136,13 +135,19 @@ int attention_tc_two(fc_ctx* ctx, cudaStream_t st, const AttnGeom& g_in, const v
   CUtensorMap tq, tk0, tv0, tk, tv;
   int rc;
   if ((rc = make_tmap(ctx, &tq, Q, g.d, q_rows, g.H_q, g.q_rs, g.H_q > 1 ? g.q_hs : g.q_rs * q_rows)) != FC_OK) return rc;
-  if (n0 == 0) return attention_ws_launch(ctx, st, g, tq, tq, tq, nullptr, nullptr, O, (uint32_t*)ws);  // no token at all
-  if ((rc = make_tmap(ctx, &tk0, K0, g.d, n0, g.H_kv, g.d, (int64_t)n0 * g.d)) != FC_OK) return rc;
-  if ((rc = make_tmap(ctx, &tv0, V0, g.d, n0, g.H_kv, g.d, (int64_t)n0 * g.d)) != FC_OK) return rc;
-  if (g.n_seg == 1) return attention_ws_launch(ctx, st, g, tq, tk0, tv0, nullptr, nullptr, O, (uint32_t*)ws);
-  if ((rc = make_tmap(ctx, &tk, K, g.d, g.kv_rows, g.H_kv, g.k_rs, g.H_kv > 1 ? g.k_hs : g.k_rs * g.kv_rows)) != FC_OK) return rc;
-  if ((rc = make_tmap(ctx, &tv, V, g.d, g.kv_rows, g.H_kv, g.v_rs, g.H_kv > 1 ? g.v_hs : g.v_rs * g.kv_rows)) != FC_OK) return rc;
-  return attention_ws_launch(ctx, st, g, tq, tk, tv, &tk0, &tv0, O, (uint32_t*)ws);
+  if (n0 > 0) {
+    if ((rc = make_tmap(ctx, &tk0, K0, g.d, n0, g.H_kv, g.d, (int64_t)n0 * g.d)) != FC_OK) return rc;
+    if ((rc = make_tmap(ctx, &tv0, V0, g.d, n0, g.H_kv, g.d, (int64_t)n0 * g.d)) != FC_OK) return rc;
+  }
+  if (g.n_seg > g.n_seg0) {
+    if ((rc = make_tmap(ctx, &tk, K, g.d, g.kv_rows, g.H_kv, g.k_rs, g.H_kv > 1 ? g.k_hs : g.k_rs * g.kv_rows)) != FC_OK) return rc;
+    if ((rc = make_tmap(ctx, &tv, V, g.d, g.kv_rows, g.H_kv, g.v_rs, g.H_kv > 1 ? g.v_hs : g.v_rs * g.kv_rows)) != FC_OK) return rc;
+  } else {  // no window: its maps are never followed
+    tk = n0 > 0 ? tk0 : tq;
+    tv = n0 > 0 ? tv0 : tq;
+  }
+  if (n0 == 0) tk0 = tk, tv0 = tv;
+  return attention_ws_launch(ctx, st, g, tq, tk, tv, &tk0, &tv0, split, O, (uint32_t*)ws);
 }
 
 }  // namespace fc

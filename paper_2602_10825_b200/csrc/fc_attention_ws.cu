@@ -87,7 +87,8 @@ struct WsSmem {
 };
 
 struct Item {
-  int h, hk, c, row0, n_vis;
+  int h, hk, c, row0, n_vis;  // logical keys [k_lo, n_vis)
+  int k_lo, part;             // kTwoStores: the part of the keys (0 and 0 otherwise)
   bool b_valid;  // tile B has at least one row of the chunk (false for the ragged last item of a chunk)
 };
 
@@ -149,8 +150,8 @@ __global__ void __launch_bounds__(kThreads, 1)
 attention_ws_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant__ CUtensorMap tmap_k,
                     const __grid_constant__ CUtensorMap tmap_v, const __grid_constant__ CUtensorMap tmap_k0,
                     const __grid_constant__ CUtensorMap tmap_v0, const __grid_constant__ fc::AttnGeom g,
-                    __nv_bfloat16* __restrict__ O, uint32_t* __restrict__ counter) {
-  constexpr bool kGather = kSource == kGatherMap;
+                    const __grid_constant__ fc::AttnSplit split, __nv_bfloat16* __restrict__ O, uint32_t* __restrict__ counter) {
+  constexpr bool kGather = kSource == kGatherMap, kTwo = kSource == kTwoStores;
   constexpr uint32_t kTileBytes = kBM * D * 2;
   constexpr int kAtoms = D / 64;
   constexpr uint32_t kAtomBytes = kBM * 128;
@@ -212,7 +213,7 @@ attention_ws_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
     int items = 0;
     for (int a = 0; a < n; ++a) {
       const int c = sh->act_chunk[a];
-      items += g.H_q * ((g.q_row_off[c + 1] - g.q_row_off[c] + 2 * kBM - 1) / (2 * kBM));
+      items += (kTwo ? split.n_splits : 1) * g.H_q * ((g.q_row_off[c + 1] - g.q_row_off[c] + 2 * kBM - 1) / (2 * kBM));
       sh->act_item_end[a] = items;
     }
     sh->n_act = n;
@@ -234,11 +235,18 @@ attention_ws_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
     int a = 0;
     while (a + 1 < n_act && item >= sh->act_item_end[a]) ++a;
     const int start = a > 0 ? sh->act_item_end[a - 1] : 0;
-    const int pairs = (sh->act_item_end[a] - start) / g.H_q;
+    const int pairs = (sh->act_item_end[a] - start) / (kTwo ? split.n_splits * g.H_q : g.H_q);
     it.c = sh->act_chunk[a];
     it.h = (item - start) / pairs;
     it.row0 = g.q_row_off[it.c] + ((item - start) % pairs) * 2 * kBM;
     it.n_vis = g.vis[it.c];
+    it.k_lo = it.part = 0;
+    if constexpr (kTwo) {  // the parts of all heads one after the other
+      it.part = it.h / g.H_q;
+      it.h %= g.H_q;
+      it.k_lo = it.part * split.part_keys;
+      if (it.part + 1 < split.n_splits) it.n_vis = min(it.n_vis, it.k_lo + split.part_keys);
+    }
     it.hk = it.h / g.group;
     it.b_valid = it.row0 + kBM < g.q_row_off[it.c + 1];
     return it;
@@ -254,11 +262,20 @@ attention_ws_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
     return item;
   };
 
+  // Tokens of segment s that the item sees (behind the `skip` first ones); none, or a negative number, for a segment before
+  // the item's keys (kTwoStores only) or behind them.
+  auto seg_tokens = [&](const Item& it, int s, int& skip) {
+    skip = kTwo ? max(it.k_lo - g.seg_log[s], 0) : 0;
+    return min(g.seg_log[s + 1], it.n_vis) - g.seg_log[s] - skip;
+  };
   auto count_tiles = [&](const Item& it) {
-    int n = 0;
+    int n = 0, skip;
     for (int s = 0; s < g.n_seg; ++s) {
-      const int seg_vis = min(g.seg_log[s + 1], it.n_vis) - g.seg_log[s];
-      if (seg_vis <= 0) break;
+      const int seg_vis = seg_tokens(it, s, skip);
+      if (seg_vis <= 0) {
+        if (kTwo) continue;
+        break;
+      }
       n += (seg_vis + kBN - 1) / kBN;
     }
     return n;
@@ -323,12 +340,16 @@ attention_ws_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
         }
       } else {
       for (int s = 0; s < g.n_seg; ++s) {
-        const int seg_vis = min(g.seg_log[s + 1], it.n_vis) - g.seg_log[s];
-        if (seg_vis <= 0) break;
+        int skip;
+        const int seg_vis = seg_tokens(it, s, skip);
+        if (seg_vis <= 0) {
+          if (kTwo) continue;
+          break;
+        }
         const CUtensorMap* map_k = kSource == kTwoStores && s < g.n_seg0 ? &tmap_k0 : &tmap_k;
         const CUtensorMap* map_v = kSource == kTwoStores && s < g.n_seg0 ? &tmap_v0 : &tmap_v;
         for (int j0 = 0; j0 < seg_vis; j0 += kBN, ++kv) {
-          const int st = kv % kStages, ph = (kv / kStages) & 1, prow = g.seg_phys[s] + j0;
+          const int st = kv % kStages, ph = (kv / kStages) & 1, prow = g.seg_phys[s] + skip + j0;
           warp_wait(smem_u32(&sh->k_empty[st]), ph ^ 1, abort);
           if (lane == 0) {
             mbar_expect_tx(smem_u32(&sh->k_full[st]), kTileBytes);
@@ -433,7 +454,9 @@ attention_ws_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
         umma_commit(b_kempty + 8 * st);
       }
       // the walk over the segments, to know which tiles are ragged (their V stage is patched before PV)
-      int seg = 0, seg_left = n_tiles > 0 ? min(g.seg_log[1], it.n_vis) - g.seg_log[0] : 0;
+      int seg = 0, skip, seg_left = n_tiles > 0 ? seg_tokens(it, 0, skip) : 0;
+      if (kTwo && n_tiles > 0)
+        while (seg_left <= 0) seg_left = seg_tokens(it, ++seg, skip);
       for (int j = 0; j < n_tiles; ++j, ++kv, ++uses) {
         const uint32_t st = kv & 1, ph = (kv >> 1) & 1;
         const uint32_t st2 = st ^ 1, ph2 = ((kv + 1) >> 1) & 1;  // the next key tile's stage
@@ -442,7 +465,7 @@ attention_ws_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
         seg_left -= kBN;
         if (seg_left <= 0 && more) {
           ++seg;
-          seg_left = min(g.seg_log[seg + 1], it.n_vis) - g.seg_log[seg];
+          seg_left = seg_tokens(it, seg, skip);
         }
         prep_pv(st, 0);
         if (more) prep_s(st2, 0);
@@ -489,8 +512,12 @@ attention_ws_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
       if (item < 0) break;
       const Item it = decode(item);
       for (int s = 0; s < g.n_seg; ++s) {
-        const int seg_vis = min(g.seg_log[s + 1], it.n_vis) - g.seg_log[s];
-        if (seg_vis <= 0) break;
+        int skip;
+        const int seg_vis = seg_tokens(it, s, skip);
+        if (seg_vis <= 0) {
+          if (kTwo) continue;
+          break;
+        }
         for (int j0 = 0; j0 < seg_vis; j0 += kBN, ++kv) {
           const int st = kv % kStages, ph = (kv / kStages) & 1;
           const int cols_valid = min(kBN, seg_vis - j0);
@@ -569,8 +596,12 @@ attention_ws_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
       float m = -INFINITY, l = 0.f;
       int j = 0;
       for (int s = 0; s < g.n_seg; ++s) {
-        const int seg_vis = min(g.seg_log[s + 1], it.n_vis) - g.seg_log[s];
-        if (seg_vis <= 0) break;
+        int skip;
+        const int seg_vis = seg_tokens(it, s, skip);
+        if (seg_vis <= 0) {
+          if (kTwo) continue;
+          break;
+        }
         for (int j0 = 0; j0 < seg_vis; j0 += kBN, ++kv, ++j, ++uses) {
           const int cols_valid = min(kBN, seg_vis - j0);
 #pragma unroll
@@ -628,6 +659,30 @@ attention_ws_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
       const int row = it.row0 + x * kBM + r_in;
       const bool row_ok = row < g.q_row_off[it.c + 1] &&
                           fc::bounds_ok(row >= 0 && row < g.q_row_off[g.W] && it.h >= 0 && it.h < g.H_q, g.status);
+      if constexpr (kTwo) {
+        if (split.n_splits > 1) {  // this part's sum, not divided by its weights; kv4_combine joins the parts
+          const int64_t vr = (int64_t)(row - g.q_row_off[0]) * g.group + it.h % g.group;
+          const int64_t at = (it.hk * split.n_vrows + vr) * split.n_splits + it.part;
+#pragma unroll
+          for (int q4 = 0; q4 < D / 32; ++q4) {
+            uint32_t r[32];
+            if (j > 0) {
+              tmem_ld32_wait(t_o + q4 * 32, r);
+            } else {
+#pragma unroll
+              for (int i = 0; i < 32; ++i) r[i] = 0;
+            }
+            if (row_ok) {
+#pragma unroll
+              for (int v = 0; v < 8; ++v)
+                *reinterpret_cast<uint4*>(split.o + at * D + q4 * 32 + v * 4) = make_uint4(r[4 * v], r[4 * v + 1], r[4 * v + 2], r[4 * v + 3]);
+            }
+          }
+          if (row_ok) split.ml[at] = make_float2(m, l);
+          tc_fence_before();
+          continue;
+        }
+      }
       const float inv = l > 0.f ? 1.f / l : 0.f;
       __nv_bfloat16* out = O + (int64_t)it.h * g.o_hs + (int64_t)row * g.o_rs;
 #pragma unroll
@@ -674,10 +729,10 @@ namespace fc {
 
 int attention_ws_launch(fc_ctx* ctx, cudaStream_t st, const AttnGeom& g, const CUtensorMap& tq,
                         const CUtensorMap& tk, const CUtensorMap& tv, const CUtensorMap* tk0, const CUtensorMap* tv0,
-                        void* O, uint32_t* counter) {
+                        const AttnSplit& split, void* O, uint32_t* counter) {
   int max_items = 0;
   for (int c = 0; c < g.W; ++c) max_items += (g.q_row_off[c + 1] - g.q_row_off[c] + 2 * kBM - 1) / (2 * kBM);
-  const int64_t items = (int64_t)max_items * g.H_q;
+  const int64_t items = (int64_t)max_items * g.H_q * (tk0 ? split.n_splits : 1);
   if (items == 0) return FC_OK;
   FC_CUDA_CHECK(cudaMemsetAsync(counter, 0, sizeof(uint32_t), st));
   const int grid = (int)std::min<int64_t>(items, (int64_t)ctx->sm_count);
@@ -686,7 +741,7 @@ int attention_ws_launch(fc_ctx* ctx, cudaStream_t st, const AttnGeom& g, const C
   const size_t smem = std::max<size_t>(need, 120 * 1024);
   auto launch = [&](auto kernel) -> int {
     FC_CUDA_CHECK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
-    kernel<<<grid, kThreads, smem, st>>>(tq, tk, tv, tk0 ? *tk0 : tk, tv0 ? *tv0 : tv, g, (__nv_bfloat16*)O, counter);
+    kernel<<<grid, kThreads, smem, st>>>(tq, tk, tv, tk0 ? *tk0 : tk, tv0 ? *tv0 : tv, g, split, (__nv_bfloat16*)O, counter);
     return FC_OK;
   };
   int rc;
