@@ -51,6 +51,13 @@ template <int D> struct Ring {
   static constexpr int kCodes = kStep * D / 2, kScales = kStep * D / 16;  // bytes of one tensor's step
   static constexpr int kBytes = 2 * (kCodes + kScales);
   static constexpr int kStages = 4;
+  // A window key is 2 D bytes a tensor: one buffer of 16 keys for K and one for V in the same place.  K of the next step is
+  // on its way while V of this one is worked on, and the other way round.
+  static constexpr int kWindow = kStep * D * 2;
+  static_assert(2 * kWindow <= kStages * kBytes, "the window's buffers fit the ring");
+  // Where 16-byte piece p of row r lies in its row, so that the eight lanes that are served together read different banks.
+  static __device__ __forceinline__ int k_piece(int r, int p) { return p ^ ((p >> 3) & 1) ^ ((r & 1) << 1); }
+  static __device__ __forceinline__ int v_piece(int r, int p) { return p ^ (((r >> 1) & 3) << 1) ^ ((p >> 1) & 1); }
 };
 
 template <int N> __device__ __forceinline__ void cp_async(uint32_t dst, const void* src) {
@@ -209,29 +216,61 @@ attention_kv4_rows_kernel(const __nv_bfloat16* __restrict__ Q, const __nv_bfloat
     k1 = (int)min((int64_t)k0 + g.window_part_keys, (int64_t)a.vis[c] - g.n_cache);
   }
 
-  // A step's copies: lane L brings 16 bytes of rows L/4 and L/4 + 8 of the codes, and the scales of a row of K or V.
-  constexpr int kLanesPerRow = D / 32, kRowsPerCopy = 32 / kLanesPerRow;
+  // A packed step's copies: lane L brings 16 bytes of rows L/4 and L/4 + 8 of the codes (D = 128), and the scales of a row of K
+  // or V.  The pointers stand at the warp's next step; positions behind the part's last key repeat it.
+  constexpr int kLanesPerRow = D / 32, kRowsPerCopy = 32 / kLanesPerRow, kAll = kStep * kWarps;
   const uint32_t ring = smem_u32(smem) + warp * R::kStages * R::kBytes;
+  const int kb0 = k0 + kStep * warp;
+  const uint8_t* codes_p = g.cache.k_codes + hk * g.cache.code_hs + (int64_t)(kb0 + lane / kLanesPerRow) * g.cache.code_rs + lane % kLanesPerRow * 16;
+  const uint16_t* scales_p = (lane < 16 ? g.cache.k_scales : g.cache.v_scales) + hk * g.cache.scale_hs + (int64_t)(kb0 + lane % 16) * g.cache.scale_rs;
+  const int64_t to_v = (int64_t)g.cache.v_codes - (int64_t)g.cache.k_codes;
+  const uint32_t codes_s = ring + lane * 16, scales_s = ring + 2 * R::kCodes + lane * (D / 16);
   auto copy = [&](int stage, int kb) {
-    const uint32_t dst = ring + stage * R::kBytes;
-    if (kb < k1) {
+    const uint32_t at = codes_s + stage * R::kBytes, at_s = scales_s + stage * R::kBytes;
+    if (kb + kStep <= k1) {
 #pragma unroll
       for (int i = 0; i < kStep / kRowsPerCopy; ++i) {
-        const int r = i * kRowsPerCopy + lane / kLanesPerRow;
-        const int64_t off = hk * g.cache.code_hs + (int64_t)min(kb + r, k1 - 1) * g.cache.code_rs + lane % kLanesPerRow * 16;
-        const uint32_t at = dst + r * (D / 2) + lane % kLanesPerRow * 16;
-        cp_async<16>(at, g.cache.k_codes + off);
-        cp_async<16>(at + R::kCodes, g.cache.v_codes + off);
+        cp_async<16>(at + i * 512, codes_p + i * kRowsPerCopy * g.cache.code_rs);
+        cp_async<16>(at + R::kCodes + i * 512, codes_p + to_v + i * kRowsPerCopy * g.cache.code_rs);
       }
-      const int64_t off = hk * g.cache.scale_hs + (int64_t)min(kb + lane % 16, k1 - 1) * g.cache.scale_rs;
-      cp_async<D / 16>(dst + 2 * R::kCodes + lane * (D / 16), (lane < 16 ? g.cache.k_scales : g.cache.v_scales) + off);
+      cp_async<D / 16>(at_s, scales_p);
+    } else if (kb < k1) {
+      const int last = k1 - 1 - kb;
+#pragma unroll
+      for (int i = 0; i < kStep / kRowsPerCopy; ++i) {
+        const int r = lane / kLanesPerRow;
+        const int64_t off = (int64_t)(min(r + i * kRowsPerCopy, last) - r) * g.cache.code_rs;
+        cp_async<16>(at + i * 512, codes_p + off);
+        cp_async<16>(at + R::kCodes + i * 512, codes_p + to_v + off);
+      }
+      cp_async<D / 16>(at_s, scales_p + (int64_t)(min(lane % 16, last) - lane % 16) * g.cache.scale_rs);
+    }
+    codes_p += kAll * g.cache.code_rs;
+    scales_p += kAll * g.cache.scale_rs;
+    cp_async_commit();
+  };
+  // A window step's copies of one tensor: the lanes look one row each up and pass it on.
+  auto copy_window = [&](const __nv_bfloat16* base, int64_t rs, uint32_t at, int kb, bool is_v) {
+    if (kb < k1) {
+      const uint32_t row = (uint32_t)fc::window_row(a, min(kb + lane % 16, k1 - 1));  // below 2^32
+      constexpr int kPieces = D / 8, kRowsAtOnce = 32 / kPieces;
+#pragma unroll
+      for (int i = 0; i < kStep / kRowsAtOnce; ++i) {
+        const int r = i * kRowsAtOnce + lane / kPieces, p = lane % kPieces;
+        const int64_t phys = __shfl_sync(0xffffffffu, row, r);
+        cp_async<16>(at + r * (2 * D) + 16 * (is_v ? R::v_piece(r, p) : R::k_piece(r, p)), base + phys * rs + 8 * p);
+      }
     }
     cp_async_commit();
   };
-  const int kb0 = k0 + kStep * warp;
+  const __nv_bfloat16* kw = K + hk * a.k_hs;
+  const __nv_bfloat16* vw = V + hk * a.v_hs;
   if (!window) {
 #pragma unroll
-    for (int i = 0; i < R::kStages - 1; ++i) copy(i, kb0 + i * kStep * kWarps);
+    for (int i = 0; i < R::kStages - 1; ++i) copy(i, kb0 + i * kAll);
+  } else {
+    copy_window(kw, a.k_rs, ring, kb0, false);
+    copy_window(vw, a.v_rs, ring + R::kWindow, kb0, true);
   }
   // everything up to here reads only what the host knows; the list is on the device
   if (part == 0 && hk == 0 && blockIdx.z == 0 && tid == 0) fc::report_bad_ids(a);
@@ -265,47 +304,55 @@ attention_kv4_rows_kernel(const __nv_bfloat16* __restrict__ Q, const __nv_bfloat
   }
   const float scale_log2 = a.scale * 1.4426950408889634f;
 
+  const uint8_t* buf = smem + warp * R::kStages * R::kBytes;
   if (!window) {
-    int stage = 0;
-    for (int kb = kb0; kb < k1; kb += kStep * kWarps) {
-      copy(stage == 0 ? R::kStages - 1 : stage - 1, kb + (R::kStages - 1) * kStep * kWarps);
+    int stage = 0, kb = kb0;
+    auto next = [&]() {  // the next step's data is there; another step's is sent for, into the place of the one before
+      copy((stage + R::kStages - 1) % R::kStages, kb + (R::kStages - 1) * kAll);
       cp_async_wait<R::kStages - 1>();
       __syncwarp();
-      const uint8_t* buf = smem + (warp * R::kStages + stage) * R::kBytes;
-      if (kb + kStep <= k1) packed_step<D, NT, false>(st, buf, qb, scale_log2, lane, kStep);
-      else packed_step<D, NT, true>(st, buf, qb, scale_log2, lane, k1 - kb);
+    };
+    for (; kb + kStep <= k1; kb += kAll) {
+      next();
+      packed_step<D, NT, false>(st, buf + stage * R::kBytes, qb, scale_log2, lane, kStep);
       __syncwarp();  // the stage has been read by every lane before it is filled again
-      stage = stage == R::kStages - 1 ? 0 : stage + 1;
+      stage = (stage + 1) % R::kStages;
+    }
+    if (kb < k1) {
+      next();
+      packed_step<D, NT, true>(st, buf + stage * R::kBytes, qb, scale_log2, lane, k1 - kb);
     }
     cp_async_wait<0>();
   } else {
-    const __nv_bfloat16* kp = K + hk * a.k_hs + q * kLaneDims;
-    const __nv_bfloat16* vp = V + hk * a.v_hs + n * kLaneCols;
-    for (int kb = k0 + kStep * warp; kb < k1; kb += kStep * kWarps) {
+    for (int kb = kb0; kb < k1; kb += kAll) {
+      cp_async_wait<1>();
+      __syncwarp();
       float s[NT][4] = {};
-      {
-        const __nv_bfloat16* r0 = kp + fc::window_row(a, min(kb + n, k1 - 1)) * a.k_rs;
-        const __nv_bfloat16* r1 = kp + fc::window_row(a, min(kb + 8 + n, k1 - 1)) * a.k_rs;
 #pragma unroll
-        for (int i = 0; i < kLaneDims / 8; ++i) {
-          const uint4 x = *reinterpret_cast<const uint4*>(r0 + 8 * i), y = *reinterpret_cast<const uint4*>(r1 + 8 * i);
+      for (int i = 0; i < kLaneDims / 8; ++i) {
+        const int p = q * (kLaneDims / 8) + i;
+        const uint4 x = *reinterpret_cast<const uint4*>(buf + n * (2 * D) + 16 * R::k_piece(n, p));
+        const uint4 y = *reinterpret_cast<const uint4*>(buf + (n + 8) * (2 * D) + 16 * R::k_piece(n, p));
 #pragma unroll
-          for (int t = 0; t < NT; ++t) {
-            mma(s[t], x.x, y.x, x.y, y.y, qb[t][4 * i], qb[t][4 * i + 1]);
-            mma(s[t], x.z, y.z, x.w, y.w, qb[t][4 * i + 2], qb[t][4 * i + 3]);
-          }
+        for (int t = 0; t < NT; ++t) {
+          mma(s[t], x.x, y.x, x.y, y.y, qb[t][4 * i], qb[t][4 * i + 1]);
+          mma(s[t], x.z, y.z, x.w, y.w, qb[t][4 * i + 2], qb[t][4 * i + 3]);
         }
       }
+      __syncwarp();
+      copy_window(kw, a.k_rs, ring, kb + kAll, false);
       uint32_t p0[NT], p1[NT];
       softmax_step<D, NT, true>(st, s, scale_log2, lane, k1 - kb, p0, p1);
-      const __nv_bfloat16* r[4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) r[i] = vp + fc::window_row(a, min(kb + 2 * q + (i & 1) + 8 * (i >> 1), k1 - 1)) * a.v_rs;
+      cp_async_wait<1>();
+      __syncwarp();
 #pragma unroll
       for (int w = 0; w < kLaneCols / 8; ++w) {
         uint4 x[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) x[i] = *reinterpret_cast<const uint4*>(r[i] + 8 * w);
+        for (int i = 0; i < 4; ++i) {
+          const int r = 2 * q + (i & 1) + 8 * (i >> 1);
+          x[i] = *reinterpret_cast<const uint4*>(buf + R::kWindow + r * (2 * D) + 16 * R::v_piece(r, n * (kLaneCols / 8) + w));
+        }
         const uint32_t* y[4] = {&x[0].x, &x[1].x, &x[2].x, &x[3].x};
 #pragma unroll
         for (int i = 0; i < 4; ++i)
@@ -314,7 +361,10 @@ attention_kv4_rows_kernel(const __nv_bfloat16* __restrict__ Q, const __nv_bfloat
             mma(st.o[t][4 * w + i], prmt(y[0][i], y[1][i], 0x5410), prmt(y[0][i], y[1][i], 0x7632), prmt(y[2][i], y[3][i], 0x5410),
                 prmt(y[2][i], y[3][i], 0x7632), p0[t], p1[t]);
       }
+      __syncwarp();
+      copy_window(vw, a.v_rs, ring + R::kWindow, kb + kAll, true);
     }
+    cp_async_wait<0>();
   }
 
   // join the four warps

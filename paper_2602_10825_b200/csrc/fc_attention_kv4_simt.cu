@@ -22,8 +22,11 @@ template <> __device__ __forceinline__ float4 load4<__nv_bfloat16>(const __nv_bf
   const uint2 w = *reinterpret_cast<const uint2*>(p);
   return make_float4(fc::bf16_lo(w.x), fc::bf16_hi(w.x), fc::bf16_lo(w.y), fc::bf16_hi(w.y));
 }
-__device__ __forceinline__ void store1(float* p, float x) { *p = x; }
-__device__ __forceinline__ void store1(__nv_bfloat16* p, float x) { *p = __float2bfloat16_rn(x); }
+__device__ __forceinline__ void store4(float* p, float4 x) { *reinterpret_cast<float4*>(p) = x; }
+__device__ __forceinline__ void store4(__nv_bfloat16* p, float4 x) {
+  const __nv_bfloat162 a = __floats2bfloat162_rn(x.x, x.y), b = __floats2bfloat162_rn(x.z, x.w);
+  *reinterpret_cast<uint2*>(p) = make_uint2(*reinterpret_cast<const uint32_t*>(&a), *reinterpret_cast<const uint32_t*>(&b));
+}
 
 // Eight elements of a packed row as fp32.
 __device__ __forceinline__ void unpack8(const uint8_t* codes, const uint16_t* scales, int w, float (&x)[8]) {
@@ -156,8 +159,7 @@ attention_kv4_simt_kernel(const T* __restrict__ Q, const T* __restrict__ K, cons
   T* out = O + (int64_t)h * a.o_hs + (int64_t)row * a.o_rs;
 #pragma unroll
   for (int i = 0; i < P; ++i)
-#pragma unroll
-    for (int e = 0; e < 4; ++e) store1(out + (i * 4 + t) * 4 + e, o[4 * i + e] * inv);
+    store4(out + (i * 4 + t) * 4, make_float4(o[4 * i] * inv, o[4 * i + 1] * inv, o[4 * i + 2] * inv, o[4 * i + 3] * inv));
   if (a.lse && t == 0) a.lse[(int64_t)h * a.lse_hs + row] = l > 0.f ? m + logf(l) : (l == l ? -INFINITY : l);
 }
 
@@ -231,11 +233,58 @@ kv4_combine_kernel(T* __restrict__ O, const __grid_constant__ fc::Kv4AttnGeom g)
     }
     const float inv = l > 0.f ? 1.f / l : (l == l ? 0.f : l);
     T* out = O + (int64_t)h * a.o_hs + (int64_t)row * a.o_rs + 4 * tid;
-    store1(out, o.x * inv);
-    store1(out + 1, o.y * inv);
-    store1(out + 2, o.z * inv);
-    store1(out + 3, o.w * inv);
+    store4(out, make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv));
     if (a.lse && tid == 0)
+      a.lse[(int64_t)h * a.lse_hs + row] =
+          l > 0.f ? (kLog2 ? (m + log2f(l)) * 0.6931471805599453f : m + logf(l)) : (l == l ? -INFINITY : l);
+  }
+}
+
+// The same with one warp per row and no barrier, for many rows of few parts (at most 32): lane p holds part p's maximum and sum.
+template <typename T, int D, bool kLog2>
+__global__ void __launch_bounds__(kCombineThreads)
+kv4_combine_warp_kernel(T* __restrict__ O, const __grid_constant__ fc::Kv4AttnGeom g) {
+  constexpr int kLanes = D / 4, kGroups = 32 / kLanes;
+  const fc::AttnGeom& a = g.a;
+  const int lane = threadIdx.x % 32, hk = blockIdx.y;
+  const int64_t vr = (int64_t)blockIdx.x * (kCombineThreads / 32) + threadIdx.x / 32;
+  if (vr >= g.n_vrows) return;
+  const int row = a.q_row_off[0] + (int)(vr / a.group), h = hk * a.group + (int)(vr % a.group);
+  int c = 0;
+  while (c + 1 < a.W && row >= a.q_row_off[c + 1]) ++c;
+  const bool on = fc::chunk_active(a, c);
+  fc::pdl_wait();
+  if (!on) return;
+  const int64_t at = (hk * g.n_vrows + vr) * g.n_splits;
+  auto power = [](float x) { return kLog2 ? exp2f(x) : expf(x); };
+  const float2 ml = lane < g.n_splits ? g.part_ml[at + lane] : make_float2(-INFINITY, 0.f);
+  float m = ml.x;
+#pragma unroll
+  for (int k = 16; k; k >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, k));
+  const float w = ml.y != 0.f ? power(ml.x - m) : 0.f;
+  float l = w == 0.f ? (ml.y == ml.y ? 0.f : ml.y) : w * ml.y;
+#pragma unroll
+  for (int k = 16; k; k >>= 1) l += __shfl_xor_sync(0xffffffffu, l, k);
+  const int grp = lane / kLanes, d4 = lane % kLanes;
+  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+  for (int p0 = 0; p0 < g.n_splits; p0 += kGroups) {
+    const int p = p0 + grp;
+    const float wp = __shfl_sync(0xffffffffu, w, p & 31);
+    if (p < g.n_splits) {
+      const float4 x = *reinterpret_cast<const float4*>(g.part_o + (at + p) * D + 4 * d4);
+      o.x = fmaf(wp, x.x, o.x); o.y = fmaf(wp, x.y, o.y); o.z = fmaf(wp, x.z, o.z); o.w = fmaf(wp, x.w, o.w);
+    }
+  }
+  if (kGroups == 2) {
+    o.x += __shfl_xor_sync(0xffffffffu, o.x, 16); o.y += __shfl_xor_sync(0xffffffffu, o.y, 16);
+    o.z += __shfl_xor_sync(0xffffffffu, o.z, 16); o.w += __shfl_xor_sync(0xffffffffu, o.w, 16);
+  }
+  if (lane < kLanes) {
+    const float inv = l > 0.f ? 1.f / l : (l == l ? 0.f : l);
+    T* out = O + (int64_t)h * a.o_hs + (int64_t)row * a.o_rs + 4 * d4;
+    store4(out, make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv));
+    if (a.lse && lane == 0)
       a.lse[(int64_t)h * a.lse_hs + row] =
           l > 0.f ? (kLog2 ? (m + log2f(l)) * 0.6931471805599453f : m + logf(l)) : (l == l ? -INFINITY : l);
   }
@@ -260,10 +309,15 @@ size_t kv4_simt_workspace(const fc_ctx* ctx, Kv4AttnGeom& g) {
 }
 
 int kv4_combine(cudaStream_t st, const Kv4AttnGeom& g, int dtype, void* O, bool log2_units) {
-  const dim3 grid((unsigned)g.n_vrows, (unsigned)g.a.H_kv);
+  // A block per row has all its loads in flight at once, a warp per row has no barriers: the first for a few rows, which
+  // leave the device empty anyway, the second for many.
+  const bool warps = g.n_splits <= 32 && g.n_vrows * g.a.H_kv >= 1024;
+  const int per = warps ? kCombineThreads / 32 : 1;
+  const dim3 grid((unsigned)((g.n_vrows + per - 1) / per), (unsigned)g.a.H_kv);
 #define FC_COMBINE(T, D)                                                                    \
   do {                                                                                      \
-    auto kernel = log2_units ? kv4_combine_kernel<T, D, true> : kv4_combine_kernel<T, D, false>; \
+    auto kernel = warps ? (log2_units ? kv4_combine_warp_kernel<T, D, true> : kv4_combine_warp_kernel<T, D, false>) \
+                        : (log2_units ? kv4_combine_kernel<T, D, true> : kv4_combine_kernel<T, D, false>);          \
     FC_CUDA_CHECK(launch_pdl(kernel, grid, dim3(kCombineThreads), 0, st, (T*)O, g));               \
   } while (0)
   if (dtype == FC_F32) { if (g.a.d == 128) FC_COMBINE(float, 128); else FC_COMBINE(float, 64); }
