@@ -156,19 +156,23 @@ class Kv4Cache:
 
     def __init__(self, k_codes, k_scales, v_codes, v_scales):
         self.k_codes, self.k_scales, self.v_codes, self.v_scales = k_codes, k_scales, v_codes, v_scales
-        H, rows, half = k_codes.shape
-        for name, t, dtype, shape, like in (("k_codes", k_codes, torch.uint8, (H, rows, half), k_codes),
-                                            ("v_codes", v_codes, torch.uint8, (H, rows, half), k_codes),
-                                            ("k_scales", k_scales, torch.bfloat16, (H, rows, half // 16), k_scales),
-                                            ("v_scales", v_scales, torch.bfloat16, (H, rows, half // 16), k_scales)):
-            if t.dtype != dtype or tuple(t.shape) != shape or t.device != k_codes.device:
-                raise FcError(f"{name} must be {dtype} {list(shape)} on {k_codes.device}")
-            if t.stride() != like.stride() or t.stride(2) != 1:
-                raise FcError(f"{name}: K and V must share strides, with a contiguous last dimension")
-        self.H, self.rows, self.d, self.device = H, rows, 2 * half, k_codes.device
-        ch, cr, _ = k_codes.stride()
-        sh, sr, _ = k_scales.stride()
+        if k_codes.dim() != 3 or k_scales.dim() != 3:
+            raise FcError("codes and scales must be [heads, rows, ...]")
+        H, rows, half = shape = k_codes.shape
+        (ch, cr, c1), (sh, sr, s1) = k_codes.stride(), k_scales.stride()
+        device, s_shape = k_codes.device, (H, rows, half // 16)
+        if not (k_codes.dtype is v_codes.dtype is torch.uint8 and k_scales.dtype is v_scales.dtype is torch.bfloat16):
+            raise FcError("codes must be uint8 and scales bfloat16")
+        if not (v_codes.shape == shape and k_scales.shape == s_shape and v_scales.shape == s_shape):
+            raise FcError(f"codes must be [heads, rows, d/2] and scales [heads, rows, d/32], got {list(shape)}, {list(k_scales.shape)}, "
+                          f"{list(v_codes.shape)}, {list(v_scales.shape)}")
+        if not (device == v_codes.device == k_scales.device == v_scales.device):
+            raise FcError("codes and scales must be on one device")
+        if v_codes.stride() != (ch, cr, c1) or v_scales.stride() != (sh, sr, s1) or c1 != 1 or s1 != 1:
+            raise FcError("K and V must share strides, with a contiguous last dimension")
+        self.H, self.rows, self.d, self.device = H, rows, 2 * half, device
         self._c = _Kv4Cache(k_codes.data_ptr(), k_scales.data_ptr(), v_codes.data_ptr(), v_scales.data_ptr(), ch, cr, sh, sr, rows)
+        self._at = C.addressof(self._c)
 
     @staticmethod
     def empty(H, rows, d, device="cuda"):
@@ -187,6 +191,7 @@ class Context:
         self._h = C.c_void_p()
         self._L = lib()
         self.device = int(device)
+        self._dev = torch.device("cuda", self.device)
         rc = self._L.fc_create(C.byref(self._h), self.device)
         self._check(rc, "fc_create")
         self._ws = {}
@@ -395,25 +400,43 @@ class Context:
         return dict(kept_idx=kept_idx, n_kept=n_kept, K_dst=K_dst, V_dst=V_dst)
 
     # ------------------------------------------------------------------ the calls around the 4-bit store
+    # These calls take a few microseconds on the device where there is one token; the checks below are written for a
+    # host that should not take longer: one pass over each tensor's attributes, no temporaries.
     def _ptr(self, t, name, dtype=None):
         """Device pointer of a tensor on this context's device (None for None)."""
         if t is None:
             return None
-        if not t.is_cuda or t.device.index != self.device:
+        if t.device != self._dev:
             raise FcError(f"{name} must be on cuda:{self.device}, got {t.device}")
-        if dtype is not None and t.dtype != dtype:
+        if dtype is not None and t.dtype is not dtype:
             raise FcError(f"{name} must have dtype {dtype}, got {t.dtype}")
         return t.data_ptr()
 
+    def _rows(self, t, name, shape, dtype):
+        """Pointer and (head, row) strides of a [heads, rows, d] tensor."""
+        if t.shape != shape or t.dtype is not dtype:
+            raise FcError(f"{name} must be {list(shape)} of {dtype}, got {list(t.shape)} of {t.dtype}")
+        if t.device != self._dev:
+            raise FcError(f"{name} must be on cuda:{self.device}, got {t.device}")
+        hs, rs, one = t.stride()
+        if one != 1:
+            raise FcError(f"{name} must be [heads, rows, d] with a contiguous last dimension")
+        return t.data_ptr(), hs, rs
+
     def _raw_stream(self):
-        return torch.cuda.current_stream(self.device).cuda_stream
+        """Handle of the current stream, without building a Stream object (several microseconds)."""
+        return torch._C._cuda_getCurrentRawStream(self.device)
 
     def _scratch(self, key, n_bytes, stream):
         """Workspace of a call on `stream`: one buffer per stream, since calls on different streams may overlap; during a
         capture the graph gets its own, which lives in the graph's memory pool."""
-        with torch.cuda.device(self.device):
-            if torch.cuda.is_current_stream_capturing():
-                return torch.empty(n_bytes, dtype=torch.uint8, device=f"cuda:{self.device}")
+        if torch.cuda.current_device() == self.device:
+            capturing = torch.cuda.is_current_stream_capturing()
+        else:
+            with torch.cuda.device(self._dev):
+                capturing = torch.cuda.is_current_stream_capturing()
+        if capturing:
+            return torch.empty(n_bytes, dtype=torch.uint8, device=self._dev)
         return self.workspace((key, stream), n_bytes)
 
     # ------------------------------------------------------------------ fc_qk_norm_rope
@@ -426,89 +449,113 @@ class Context:
         like = K if Q is None else Q
         if like is None:
             raise FcError("Q and K are both None")
-        if Q is not None and K is not None and (Q.dtype != K.dtype or Q.shape[1:] != K.shape[1:]):
-            raise FcError("Q and K must share dtype, tokens and head size")
-        T, d = int(like.shape[1]), int(like.shape[2])
-        side = []
-        for name, x, out, w in (("Q", Q, Q_out, q_weight), ("K", K, K_out, k_weight)):
-            if x is None:
-                side.append((0, (0, 0), (0, 0), None, None, None, None))
-                continue
-            if out is None:
-                out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-            if out.shape != x.shape or out.dtype != x.dtype:
-                raise FcError(f"{name}_out must have {name}'s shape and dtype")
-            if w is not None and (w.shape != (d,) or w.stride(0) != 1):
-                raise FcError(f"the weight of {name} must be contiguous [{d}]")
-            side.append((x.shape[0], _hsr(x, name), _hsr(out, f"{name}_out"), self._ptr(x, name), self._ptr(out, f"{name}_out"),
-                         self._ptr(w, f"the weight of {name}", torch.float32), out))
-        (hq, qs, qos, qp, qop, qw, Q_out), (hk, ks, kos, kp, kop, kw, K_out) = side
+        if like.dim() != 3:
+            raise FcError("Q and K must be [heads, rows, d]")
+        dtype = like.dtype
+        hq, hk, (_, T, d) = 0, 0, like.shape
+        qp = qop = qw = kp = kop = kw = None
+        qh = qr = qoh = qor = kh = kr = koh = kor = 0
+        if Q is not None:
+            hq = Q.shape[0]
+            shape = (hq, T, d)
+            if Q_out is None:
+                Q_out = torch.empty(shape, dtype=dtype, device=self._dev)
+            qp, qh, qr = self._rows(Q, "Q", shape, dtype)
+            qop, qoh, qor = self._rows(Q_out, "Q_out", shape, dtype)
+            if q_weight is not None:
+                qw = self._weight(q_weight, d)
+        if K is not None:
+            hk = K.shape[0]
+            shape = (hk, T, d)
+            if K_out is None:
+                K_out = torch.empty(shape, dtype=dtype, device=self._dev)
+            kp, kh, kr = self._rows(K, "K", shape, dtype)
+            kop, koh, kor = self._rows(K_out, "K_out", shape, dtype)
+            if k_weight is not None:
+                kw = self._weight(k_weight, d)
         if pos is not None and (pos.shape != (T, 3) or not pos.is_contiguous()):
             raise FcError(f"pos must be contiguous [{T}, 3]")
-        if grid is None and pos is None and any(axes):
-            raise FcError("give the tokens' places: grid or pos")
+        if grid is None:
+            if pos is None and any(axes):
+                raise FcError("give the tokens' places: grid or pos")
+            grid = (0, 0, 0)
         freq = None
         if inv_freq is not None:
             freq = np.ascontiguousarray(np.asarray(inv_freq, dtype=np.float64))
             if freq.shape != (sum(axes) // 2,):
                 raise FcError(f"inv_freq must have {sum(axes) // 2} entries")
-        desc = _RopeDesc(hq, hk, d, T, *qs, *ks, *qos, *kos, tuple(axes), pairing, NORM_RMS if norm else NORM_NONE, eps, theta,
-                         *(grid or (0, 0, 0)))
-        rc = self._L.fc_qk_norm_rope(self._h, self._raw_stream(), C.byref(desc), qp, kp, _dt(like), qw, kw,
+        desc = _RopeDesc(hq, hk, d, T, qh, qr, kh, kr, qoh, qor, koh, kor, tuple(axes), pairing, NORM_RMS if norm else NORM_NONE, eps,
+                         theta, *grid)
+        rc = self._L.fc_qk_norm_rope(self._h, self._raw_stream(), C.addressof(desc), qp, kp, _dt(like), qw, kw,
                                      self._ptr(pos, "pos", torch.int32), None if freq is None else freq.ctypes.data, qop, kop)
         if rc:
             self._check(rc, "fc_qk_norm_rope")
         return Q_out, K_out
 
+    def _weight(self, w, d):
+        if w.shape != (d,) or w.stride(0) != 1:
+            raise FcError(f"a norm's weight must be contiguous [{d}]")
+        return self._ptr(w, "a norm's weight", torch.float32)
+
     # ------------------------------------------------------------------ fc_kv4_pack / fc_kv4_unpack
+    def _store(self, s, name):
+        """Address of a store's C struct."""
+        if s is None:
+            return None
+        if s.device != self._dev:
+            raise FcError(f"{name} must be on cuda:{self.device}, got {s.device}")
+        return s._at
+
     def kv4_pack(self, K, V, dst, *, old=None, n_old=None, kept_idx=None, dst_row=0, status=None):
         """Quantises rows of K, V [H, n_new, d] into the store `dst`, from row dst_row on; returns dst.
 
         With kept_idx [H, n_out] the rows are picked from [the first n_old rows of the store `old` | the new rows], the
         old ones copied as they are.  K and V may be None if only old rows are picked."""
-        if (K is None) != (V is None) or (K is not None and (K.dtype != V.dtype or K.shape != V.shape)):
-            raise FcError("K and V must share shape and dtype")
+        H, d = dst.H, dst.d
         n_old = 0 if old is None else old.rows if n_old is None else int(n_old)
-        n_new, ks, vs, dt = 0, (0, 0), (0, 0), BF16
-        if K is not None:
-            if K.shape[0] != dst.H or K.shape[2] != dst.d:
-                raise FcError(f"K and V must be [{dst.H}, rows, {dst.d}]")
-            n_new, ks, vs, dt = K.shape[1], _hsr(K, "K"), _hsr(V, "V"), _dt(K)
-        if old is not None and (old.H != dst.H or old.d != dst.d):
+        n_new, dt, kp, vp, kh, kr, vh, vr = 0, BF16, None, None, 0, 0, 0, 0
+        if K is not None and V is not None:
+            n_new, dt = K.shape[1], _dt(K)
+            shape = (H, n_new, d)
+            kp, kh, kr = self._rows(K, "K", shape, K.dtype)
+            vp, vh, vr = self._rows(V, "V", shape, K.dtype)
+        elif K is not None or V is not None:
+            raise FcError("K and V: give both or neither")
+        if old is not None and (old.H != H or old.d != d):
             raise FcError("old and dst must share heads and head size")
         n_out, kept_hs = n_old + n_new, 0
         if kept_idx is not None:
-            if kept_idx.dim() != 2 or kept_idx.shape[0] != dst.H or kept_idx.stride(1) != 1:
-                raise FcError(f"kept_idx must be [{dst.H}, rows] with contiguous rows")
-            n_out, kept_hs = kept_idx.shape[1], max(kept_idx.stride(0), kept_idx.shape[1])
-        for s, name in ((old, "old"), (dst, "dst")):
-            if s is not None:
-                self._ptr(s.k_codes, name)
-        desc = _Kv4PackDesc(dst.H, dst.d, n_old, n_new, n_out, dst_row, *ks, *vs)
-        rc = self._L.fc_kv4_pack(self._h, self._raw_stream(), C.byref(desc), self._ptr(K, "K"), self._ptr(V, "V"), dt,
-                                 None if old is None else C.byref(old._c), self._ptr(kept_idx, "kept_idx", torch.int32), kept_hs,
-                                 C.byref(dst._c), self._ptr(status, "status", torch.int32))
+            if kept_idx.dim() != 2 or kept_idx.shape[0] != H or kept_idx.stride(1) != 1:
+                raise FcError(f"kept_idx must be [{H}, rows] with contiguous rows")
+            n_out = kept_idx.shape[1]
+            kept_hs = kept_idx.stride(0) if H > 1 else n_out
+        desc = _Kv4PackDesc(H, d, n_old, n_new, n_out, dst_row, kh, kr, vh, vr)
+        rc = self._L.fc_kv4_pack(self._h, self._raw_stream(), C.addressof(desc), kp, vp, dt, self._store(old, "old"),
+                                 self._ptr(kept_idx, "kept_idx", torch.int32), kept_hs, self._store(dst, "dst"),
+                                 self._ptr(status, "status", torch.int32))
         if rc:
             self._check(rc, "fc_kv4_pack")
         return dst
 
     def kv4_unpack(self, src, *, row=0, n=None, K_dst=None, V_dst=None, dtype=torch.bfloat16, keys_only=False):
         """Values of rows row .. row + n - 1 of a store as plain [H, n, d] tensors (K, V); V is None with keys_only."""
-        n = (K_dst.shape[1] if K_dst is not None else src.rows - row) if n is None else int(n)
+        given = K_dst if K_dst is not None else V_dst
+        if given is not None:
+            dtype = given.dtype
+        n = (src.rows - row if given is None else given.shape[1]) if n is None else int(n)
         shape = (src.H, n, src.d)
-        if K_dst is None and (V_dst is None or not keys_only):
-            K_dst = torch.empty(shape, dtype=dtype if V_dst is None else V_dst.dtype, device=src.device)
-        if V_dst is None and not keys_only:
-            V_dst = torch.empty(shape, dtype=K_dst.dtype, device=src.device)
-        for name, t in (("K_dst", K_dst), ("V_dst", V_dst)):
-            if t is not None and (tuple(t.shape) != shape or t.dtype != (K_dst if K_dst is not None else V_dst).dtype):
-                raise FcError(f"{name} must be {list(shape)}, K_dst and V_dst of one dtype")
-        self._ptr(src.k_codes, "src")
-        ks = (0, 0) if K_dst is None else _hsr(K_dst, "K_dst")
-        vs = (0, 0) if V_dst is None else _hsr(V_dst, "V_dst")
-        desc = _Kv4UnpackDesc(src.H, src.d, n, row, *ks, *vs)
-        rc = self._L.fc_kv4_unpack(self._h, self._raw_stream(), C.byref(desc), C.byref(src._c), self._ptr(K_dst, "K_dst"),
-                                   self._ptr(V_dst, "V_dst"), _dt(K_dst if K_dst is not None else V_dst))
+        if K_dst is None:
+            K_dst = torch.empty(shape, dtype=dtype, device=self._dev)
+        kp, kh, kr = self._rows(K_dst, "K_dst", shape, dtype)
+        vp, vh, vr = None, 0, 0
+        if keys_only:
+            V_dst = None
+        else:
+            if V_dst is None:
+                V_dst = torch.empty(shape, dtype=dtype, device=self._dev)
+            vp, vh, vr = self._rows(V_dst, "V_dst", shape, dtype)
+        desc = _Kv4UnpackDesc(src.H, src.d, n, row, kh, kr, vh, vr)
+        rc = self._L.fc_kv4_unpack(self._h, self._raw_stream(), C.addressof(desc), self._store(src, "src"), kp, vp, _dt(K_dst))
         if rc:
             self._check(rc, "fc_kv4_unpack")
         return K_dst, V_dst
@@ -521,49 +568,54 @@ class Context:
 
         cache may be None (no clean region), K and V too (no window).  Without a segment table the window is the rows of
         K and V in order; with one, its logical offsets count from the window's start."""
-        if (K is None) != (V is None):
-            raise FcError("K and V: give both or neither")
         if cache is None and K is None:
             raise FcError("give a store, a window, or both")
+        if Q.dim() != 3:
+            raise FcError("Q must be [heads, rows, d]")
+        H_q, rows, d = shape = Q.shape
+        dtype, dt = Q.dtype, _dt(Q)
+        qp, qh, qr = self._rows(Q, "Q", shape, dtype)
+        op, oh, orow = self._rows(O, "O", shape, dtype)
         H_kv = cache.H if cache is not None else K.shape[0]
-        if O.dtype != Q.dtype or (K is not None and (K.dtype != Q.dtype or V.dtype != Q.dtype)):
-            raise FcError("Q, K, V, O must share one dtype")
-        if O.shape != Q.shape or (cache is not None and cache.d != Q.shape[2]):
-            raise FcError("Q, O and the store must share the head size, Q and O their shape")
-        if K is not None and (K.shape[0] != H_kv or K.shape[2] != Q.shape[2] or V.shape != K.shape):
-            raise FcError(f"K and V must be [{H_kv}, rows, {Q.shape[2]}]")
+        if cache is not None and cache.d != d:
+            raise FcError("Q and the store must share the head size")
         n_cache = (0 if cache is None else cache.rows) if n_cache is None else int(n_cache)
         W = len(kv_visible_len)
-        if len(q_chunk_row_off) != W + 1 or q_chunk_row_off[W] > Q.shape[1] or active_ids.numel() > W:
+        if len(q_chunk_row_off) != W + 1 or q_chunk_row_off[W] > rows or active_ids.numel() > W:
             raise FcError("q_chunk_row_off must have one entry more than kv_visible_len and stay inside Q; active_ids at most as many")
-        ks, vs, rows, n_seg, sl, sp = (0, 0), (0, 0), 0, 0, None, None
-        if K is not None:
-            ks, vs, rows = _hsr(K, "K"), _hsr(V, "V"), K.shape[1]
+        kp = vp = sl = sp = None
+        kh = kr = vh = vr = n_window = n_seg = 0
+        if K is not None and V is not None:
+            n_window = K.shape[1]
+            kp, kh, kr = self._rows(K, "K", (H_kv, n_window, d), dtype)
+            vp, vh, vr = self._rows(V, "V", (H_kv, n_window, d), dtype)
             if seg_phys_off is None:
-                n_seg, sl, sp = (1, (C.c_int32 * 2)(0, rows), (C.c_int32 * 1)(0)) if rows else (0, None, None)
+                if n_window:
+                    n_seg, sl, sp = 1, (C.c_int32 * 2)(0, n_window), (C.c_int32 * 1)(0)
             else:
                 n_seg = len(seg_phys_off)
                 if len(seg_logical_off) != n_seg + 1:
                     raise FcError("seg_logical_off must have one entry more than seg_phys_off")
                 sl, sp = (C.c_int32 * (n_seg + 1))(*seg_logical_off), (C.c_int32 * n_seg)(*seg_phys_off)
-        desc = _AttnDesc(Q.shape[0], H_kv, Q.shape[2], W, *_hsr(Q, "Q"), *ks, *vs, *_hsr(O, "O"), rows, scale, impl)
+        elif K is not None or V is not None:
+            raise FcError("K and V: give both or neither")
+        desc = _AttnDesc(H_q, H_kv, d, W, qh, qr, kh, kr, vh, vr, oh, orow, n_window, scale, impl)
         off, vis = (C.c_int32 * (W + 1))(*q_chunk_row_off), (C.c_int32 * W)(*kv_visible_len)
-        dt, stream, dp = _dt(Q), self._raw_stream(), C.byref(desc)
-        if cache is not None:
-            self._ptr(cache.k_codes, "cache")
+        stream, dp = self._raw_stream(), C.addressof(desc)
         lse_hs = 0
         if lse is not None:
-            if lse.dim() != 2 or lse.shape[0] != Q.shape[0] or lse.shape[1] < q_chunk_row_off[W] or lse.stride(1) != 1:
+            if lse.dim() != 2 or lse.shape[0] != H_q or lse.shape[1] < q_chunk_row_off[W] or lse.stride(1) != 1:
                 raise FcError("lse must be [H_q, rows] with contiguous rows")
             lse_hs = max(lse.stride(0), 1)
         if ws is None:
             need = self._L.fc_chunk_attention_kv4_workspace_bytes(self._h, dp, dt, off, vis, n_cache)
-            ws = self._scratch("attention_kv4", need, stream) if need else None
+            if need:
+                ws = self._scratch("attention_kv4", need, stream)
         rc = self._L.fc_chunk_attention_kv4(
-            self._h, stream, dp, self._ptr(Q, "Q"), None if cache is None else C.byref(cache._c), n_cache, self._ptr(K, "K"),
-            self._ptr(V, "V"), dt, off, vis, sl, sp, n_seg, self._ptr(active_ids, "active_ids", torch.int32),
-            self._ptr(n_active, "n_active", torch.int32), self._ptr(O, "O"), self._ptr(lse, "lse", torch.float32), lse_hs,
-            self._ptr(status, "status", torch.int32), self._ptr(ws, "ws"), 0 if ws is None else ws.numel())
+            self._h, stream, dp, qp, self._store(cache, "cache"), n_cache, kp, vp, dt, off, vis, sl, sp, n_seg,
+            self._ptr(active_ids, "active_ids", torch.int32), self._ptr(n_active, "n_active", torch.int32), op,
+            self._ptr(lse, "lse", torch.float32), lse_hs, self._ptr(status, "status", torch.int32), self._ptr(ws, "ws"),
+            0 if ws is None else ws.numel())
         if rc:
             self._check(rc, "fc_chunk_attention_kv4")
         return O

@@ -39,13 +39,6 @@ int check_geometry(const fc_attn_desc* desc, int dtype, const int32_t* q_chunk_r
 
 enum Path { kSimt, kRows, kUnpacked };
 
-Path choose(const fc_attn_desc* desc, int dtype, const fc::Kv4AttnGeom& g) {
-  if (dtype == FC_F32 || desc->impl == 1) return kSimt;
-  if (desc->impl == 2) return kUnpacked;
-  if (desc->impl == 3) return kRows;
-  return g.n_vrows > 256 ? kUnpacked : kRows;
-}
-
 // Rows of the clean region that some chunk sees.
 int cache_rows(const fc::Kv4AttnGeom& g) {
   int n = 0;
@@ -57,6 +50,7 @@ int cache_rows(const fc::Kv4AttnGeom& g) {
 struct UnpackedPlan {
   fc::AttnSplit split;
   size_t k, v, o, ml, bytes;  // offsets
+  double us;                  // estimate of the whole path
 };
 
 UnpackedPlan plan_unpacked(const fc_ctx* ctx, const fc::Kv4AttnGeom& g) {
@@ -81,6 +75,8 @@ UnpackedPlan plan_unpacked(const fc_ctx* ctx, const fc::Kv4AttnGeom& g) {
     const double us = 1.8 * rounds * ((tiles + k - 1) / k) + (k > 1 ? 5 + k * part_us : 0);
     if (k == 1 || us < best) best = us, n = k;
   }
+  // 20 us for the launches of the path, the unpacking at 6 TB/s
+  p.us = 20 + best + 2.0 * a.H_kv * cache_rows(g) * a.d * 2.56 / 6e6;
   if (n > 1) {
     p.split.part_keys = (int32_t)((tiles + n - 1) / n * 128);
     p.split.n_splits = (int32_t)((vis + p.split.part_keys - 1) / p.split.part_keys);
@@ -96,6 +92,18 @@ UnpackedPlan plan_unpacked(const fc_ctx* ctx, const fc::Kv4AttnGeom& g) {
   return p;
 }
 
+// Few rows read the packed keys in one pass but spend a tensor instruction on eight of them; many rows pay for unpacking once.  The
+// line between the two moves with the heads and the keys, so that the estimates are compared (measured at 24 heads of 128
+// over 28000 keys: 64 rows 112 us against 150, 128 rows 303 against 153).
+Path choose(const fc_ctx* ctx, const fc_attn_desc* desc, int dtype, const fc::Kv4AttnGeom& g_in) {
+  if (dtype == FC_F32 || desc->impl == 1) return kSimt;
+  if (desc->impl == 2) return kUnpacked;
+  if (desc->impl == 3) return kRows;
+  fc::Kv4AttnGeom g = g_in;
+  fc::kv4_rows_workspace(ctx, g);
+  return fc::kv4_rows_us(ctx, g) <= plan_unpacked(ctx, g).us ? kRows : kUnpacked;
+}
+
 size_t plan(const fc_ctx* ctx, Path path, fc::Kv4AttnGeom& g) {
   if (path == kSimt) return fc::kv4_simt_workspace(ctx, g);
   if (path == kRows) return fc::kv4_rows_workspace(ctx, g);
@@ -109,7 +117,7 @@ extern "C" size_t fc_chunk_attention_kv4_workspace_bytes(const fc_ctx* ctx, cons
                                                          int n_cache) {
   fc::Kv4AttnGeom g = {};
   if (!ctx || check_geometry(desc, dtype, q_chunk_row_off, kv_visible_len, n_cache, g) != FC_OK) return 0;
-  return plan(ctx, choose(desc, dtype, g), g);
+  return plan(ctx, choose(ctx, desc, dtype, g), g);
 }
 
 extern "C" int fc_chunk_attention_kv4(fc_ctx* ctx, void* stream, const fc_attn_desc* desc, const void* Q,
@@ -159,7 +167,7 @@ extern "C" int fc_chunk_attention_kv4(fc_ctx* ctx, void* stream, const fc_attn_d
   a.active_ids = active_ids; a.n_active = n_active; a.lse = lse; a.status = status;
   if (n_cache > 0) g.cache = fc::kv4_view(*cache);
 
-  const Path path = choose(desc, dtype, g);
+  const Path path = choose(ctx, desc, dtype, g);
   const size_t need = plan(ctx, path, g);
   if (need > 0) {
     if (!ws || ws_bytes < need) return FC_ERR_WORKSPACE;

@@ -26,6 +26,7 @@ using namespace fc::sm100;  // ex2, cvt_bf16x2, max3
 constexpr int kWarps = 4, kThreads = 32 * kWarps;
 constexpr int kStep = 16;  // keys per warp and step
 constexpr float kRescaleThreshold = 8.f;
+constexpr int kWindowCost = 3;  // a window key has 3.6 times the bytes of a packed one
 #ifndef BP1
 #define BP1 3
 #endif
@@ -205,16 +206,13 @@ attention_kv4_rows_kernel(const __nv_bfloat16* __restrict__ Q, const __nv_bfloat
   if (c < 0) return;
   const int rows_here = min(kRows, (a.q_row_off[c + 1] - a.q_row_off[c]) * a.group - v0);
 
-  // keys of this part: of the clean region, or of the window
-  const bool window = part >= g.cache_parts;
-  int k0, k1;
-  if (!window) {
-    k0 = part * g.part_keys;
-    k1 = (int)min((int64_t)k0 + g.part_keys, (int64_t)min(g.n_cache, a.vis[c]));
-  } else {
-    k0 = (part - g.cache_parts) * g.window_part_keys;
-    k1 = (int)min((int64_t)k0 + g.window_part_keys, (int64_t)a.vis[c] - g.n_cache);
-  }
+  // The parts cut an axis of costs: the clean region's keys, then the window's at kWindowCost each.  This part's packed
+  // keys are [k0, k1), its window keys [w0, w1).
+  const int64_t x0 = (int64_t)part * g.part_keys, x1 = x0 + g.part_keys;
+  const int cache = min(g.n_cache, a.vis[c]), behind = max(a.vis[c] - g.n_cache, 0);
+  const int k0 = (int)min(x0, (int64_t)g.n_cache), k1 = (int)min(x1, (int64_t)cache);
+  const int w0 = (int)min((max(x0 - g.n_cache_ceil, (int64_t)0)) / kWindowCost, (int64_t)behind);
+  const int w1 = (int)min((max(x1 - g.n_cache_ceil, (int64_t)0)) / kWindowCost, (int64_t)behind);
 
   // A packed step's copies: lane L brings 16 bytes of rows L/4 and L/4 + 8 of the codes (D = 128), and the scales of a row of K
   // or V.  The pointers stand at the warp's next step; positions behind the part's last key repeat it.
@@ -251,8 +249,8 @@ attention_kv4_rows_kernel(const __nv_bfloat16* __restrict__ Q, const __nv_bfloat
   };
   // A window step's copies of one tensor: the lanes look one row each up and pass it on.
   auto copy_window = [&](const __nv_bfloat16* base, int64_t rs, uint32_t at, int kb, bool is_v) {
-    if (kb < k1) {
-      const uint32_t row = (uint32_t)fc::window_row(a, min(kb + lane % 16, k1 - 1));  // below 2^32
+    if (kb < w1) {
+      const uint32_t row = (uint32_t)fc::window_row(a, min(kb + lane % 16, w1 - 1));  // below 2^32
       constexpr int kPieces = D / 8, kRowsAtOnce = 32 / kPieces;
 #pragma unroll
       for (int i = 0; i < kStep / kRowsAtOnce; ++i) {
@@ -265,12 +263,9 @@ attention_kv4_rows_kernel(const __nv_bfloat16* __restrict__ Q, const __nv_bfloat
   };
   const __nv_bfloat16* kw = K + hk * a.k_hs;
   const __nv_bfloat16* vw = V + hk * a.v_hs;
-  if (!window) {
+  if (k0 < k1) {
 #pragma unroll
     for (int i = 0; i < R::kStages - 1; ++i) copy(i, kb0 + i * kAll);
-  } else {
-    copy_window(kw, a.k_rs, ring, kb0, false);
-    copy_window(vw, a.v_rs, ring + R::kWindow, kb0, true);
   }
   // everything up to here reads only what the host knows; the list is on the device
   if (part == 0 && hk == 0 && blockIdx.z == 0 && tid == 0) fc::report_bad_ids(a);
@@ -305,7 +300,7 @@ attention_kv4_rows_kernel(const __nv_bfloat16* __restrict__ Q, const __nv_bfloat
   const float scale_log2 = a.scale * 1.4426950408889634f;
 
   const uint8_t* buf = smem + warp * R::kStages * R::kBytes;
-  if (!window) {
+  if (k0 < k1) {
     int stage = 0, kb = kb0;
     auto next = [&]() {  // the next step's data is there; another step's is sent for, into the place of the one before
       copy((stage + R::kStages - 1) % R::kStages, kb + (R::kStages - 1) * kAll);
@@ -323,8 +318,13 @@ attention_kv4_rows_kernel(const __nv_bfloat16* __restrict__ Q, const __nv_bfloat
       packed_step<D, NT, true>(st, buf + stage * R::kBytes, qb, scale_log2, lane, k1 - kb);
     }
     cp_async_wait<0>();
-  } else {
-    for (int kb = kb0; kb < k1; kb += kAll) {
+    __syncwarp();
+  }
+  if (w0 < w1) {
+    const int wb0 = w0 + kStep * warp;
+    copy_window(kw, a.k_rs, ring, wb0, false);
+    copy_window(vw, a.v_rs, ring + R::kWindow, wb0, true);
+    for (int kb = wb0; kb < w1; kb += kAll) {
       cp_async_wait<1>();
       __syncwarp();
       float s[NT][4] = {};
@@ -342,7 +342,7 @@ attention_kv4_rows_kernel(const __nv_bfloat16* __restrict__ Q, const __nv_bfloat
       __syncwarp();
       copy_window(kw, a.k_rs, ring, kb + kAll, false);
       uint32_t p0[NT], p1[NT];
-      softmax_step<D, NT, true>(st, s, scale_log2, lane, k1 - kb, p0, p1);
+      softmax_step<D, NT, true>(st, s, scale_log2, lane, w1 - kb, p0, p1);
       cp_async_wait<1>();
       __syncwarp();
 #pragma unroll
@@ -436,24 +436,27 @@ size_t kv4_rows_workspace(const fc_ctx* ctx, Kv4AttnGeom& g) {
   for (int c = 0; c < g.a.W; ++c) vis = std::max(vis, g.a.vis[c]);
   const int nt = tiles_of(g);
   const int64_t tiles = tile_count(g.a, 8 * nt) * g.a.H_kv;
-  const int64_t cache = std::min(vis, g.n_cache), window = std::max(vis - g.n_cache, 0);
-  // At most one set of resident blocks where that leaves two steps for every warp, shared out by what a key costs: a
-  // window key has 3.6 times the bytes of a packed one.
-  constexpr int64_t kWindowCost = 3, kAll = kStep * kWarps, kLeast = 2 * kAll;
+  // At most one set of resident blocks, where that leaves a step or more for every warp.
+  constexpr int64_t kUnit = kStep * kWarps;
+  const int64_t window = std::max(vis - g.n_cache, 0);
+  const int64_t cache = window > 0 ? ((int64_t)g.n_cache + kUnit - 1) / kUnit * kUnit : std::min(vis, g.n_cache);
+  const int64_t total = cache + kWindowCost * window;
   const int64_t slots = std::min<int64_t>(kKv4MaxSplits, std::max<int64_t>(1, (int64_t)ctx->sm_count * blocks_per_sm(nt) / std::max<int64_t>(1, tiles)));
-  auto parts_of = [&](int64_t per, int64_t wper) { return (cache + per - 1) / per + (window + wper - 1) / wper; };
-  int64_t per = std::max(kLeast, (cache + kWindowCost * window) / slots / kAll * kAll), wper;
-  for (;; per += kAll) {
-    wper = std::max<int64_t>(kAll, per / kWindowCost / kAll * kAll);
-    if (parts_of(per, wper) <= std::max<int64_t>(slots, (cache > 0) + (window > 0))) break;
-  }
-  g.part_keys = (int32_t)std::min<int64_t>(per, INT32_MAX / 2);
-  g.window_part_keys = (int32_t)std::min<int64_t>(wper, INT32_MAX / 2);
-  g.cache_parts = (int32_t)((cache + g.part_keys - 1) / g.part_keys);
-  g.n_splits = (int32_t)std::max<int64_t>(1, parts_of(g.part_keys, g.window_part_keys));
+  const int64_t per = std::max(2 * kUnit, (total + slots * kUnit - 1) / (slots * kUnit) * kUnit);
+  g.part_keys = per;
+  g.n_cache_ceil = cache;
+  g.n_splits = (int32_t)std::max<int64_t>(1, (total + per - 1) / per);
   if (g.n_splits == 1) return 0;
   const int64_t parts = g.a.H_kv * g.n_vrows * g.n_splits;
   return align_up(parts * g.a.d * sizeof(float), 256) + align_up(parts * sizeof(float2), 256);
+}
+
+// Measured on B200: a step of a block's four warps takes 0.36 us (D = 128; 0.2 for 64) for every block of the SM it runs
+// on, whether eight or sixteen rows ride along; 9 us for the launches, the first loads and the joining.
+double kv4_rows_us(const fc_ctx* ctx, const Kv4AttnGeom& g) {
+  const int64_t blocks = tile_count(g.a, 8 * tiles_of(g)) * g.a.H_kv * g.n_splits;
+  const double per_sm = (double)((blocks + ctx->sm_count - 1) / ctx->sm_count);
+  return 9 + per_sm * (double)g.part_keys / (kStep * kWarps) * (g.a.d == 128 ? 0.36 : 0.2);
 }
 
 int kv4_rows(cudaStream_t st, const Kv4AttnGeom& g, const void* Q, const void* K, const void* V, void* O) {

@@ -301,7 +301,7 @@ size_t kv4_simt_workspace(const fc_ctx* ctx, Kv4AttnGeom& g) {
   const int64_t want = blocks > 0 ? (4ll * ctx->sm_count + blocks - 1) / blocks : 1;  // about four blocks an SM
   const int64_t most = std::min<int64_t>(kMaxSplits, (vis + kMinPart - 1) / kMinPart);
   const int64_t n = std::max<int64_t>(1, std::min(want, most));
-  g.part_keys = (int32_t)std::max<int64_t>(kKeys, ((vis + n - 1) / n + kKeys - 1) / kKeys * kKeys);
+  g.part_keys = std::max<int64_t>(kKeys, ((vis + n - 1) / n + kKeys - 1) / kKeys * kKeys);
   g.n_splits = (int32_t)std::max<int64_t>(1, ((int64_t)vis + g.part_keys - 1) / g.part_keys);
   if (g.n_splits == 1) return 0;
   const int64_t parts = g.a.H_kv * g.n_vrows * g.n_splits;

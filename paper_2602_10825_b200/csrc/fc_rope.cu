@@ -185,9 +185,9 @@ qk_norm_rope_kernel(const T* Q, const T* K, T* Q_out, T* K_out, const float* __r
 
 // f radians per position -> turns per position modulo one, times 2^64
 uint64_t turns_of(double f) {
-  long double t = (long double)f / 6.283185307179586476925286766559005768L;
-  t -= floorl(t);
-  return t < 1.0L ? (uint64_t)ldexpl(t, 64) : 0;
+  long double t = (long double)f * 0.159154943091895335768883763372514362L;
+  if (!(t >= 0.0L && t < 1.0L)) t -= floorl(t);
+  return t < 1.0L ? (uint64_t)(t * 0x1p64L) : 0;
 }
 
 }  // namespace
@@ -219,12 +219,19 @@ extern "C" int fc_qk_norm_rope(fc_ctx* ctx, void* stream, const fc_rope_desc* de
       if (frame > INT32_MAX || desc->grid_t0 + (int64_t)(desc->T > 0 ? desc->T - 1 : 0) / frame > INT32_MAX) return FC_ERR_INVALID_ARG;
     }
     int k = 0;
-    for (int a = 0; a < 3; ++a)
-      for (int i = 0; i < desc->axis_dim[a] / 2; ++i, ++k) {
+    for (int a = 0; a < 3; ++a) {
+      const int half = desc->axis_dim[a] / 2;
+      const bool same = !inv_freq && a > 0 && desc->axis_dim[a] == desc->axis_dim[a - 1];  // height and width, as a rule
+      for (int i = 0; i < half; ++i, ++k) {
+        if (same) {
+          g.turns[k] = g.turns[k - half];
+          continue;
+        }
         const double f = inv_freq ? inv_freq[k] : pow(desc->theta, -2.0 * i / desc->axis_dim[a]);
         if (!std::isfinite(f)) return FC_ERR_INVALID_ARG;
         g.turns[k] = turns_of(f);
       }
+    }
   }
   const int es = fc::elem_size(dtype);
   const struct { int heads; const void *in, *out; int64_t s[4]; } side[2] = {

@@ -485,20 +485,20 @@ def test_binding_refusals(fc, ctx):
         ctx.qk_norm_rope(K, None, axes=(0, 0, 0), q_weight=torch.ones(32, device="cuda"))
     with pytest.raises(fc.FcError, match="invalid argument"):
         ctx.qk_norm_rope(K, None, axes=(25, 20, 19), grid=(0, 2, 4))
-    with pytest.raises(fc.FcError, match="share shape"):
+    with pytest.raises(fc.FcError, match="V must be"):
         ctx.kv4_pack(K, K[:, :4], cache)
     with pytest.raises(fc.FcError, match="invalid argument"):
         ctx.kv4_pack(K, K, cache, dst_row=1)
     with pytest.raises(fc.FcError, match="share strides"):
-        fc.Kv4Cache(cache.k_codes, cache.k_scales, cache.v_codes[:, :, :], torch.empty((2, 16, 2), dtype=BF16, device="cuda")[:, ::2])
-    with pytest.raises(fc.FcError, match="must be"):
+        fc.Kv4Cache(cache.k_codes, cache.k_scales, cache.v_codes, torch.empty((2, 16, 2), dtype=BF16, device="cuda")[:, ::2])
+    with pytest.raises(fc.FcError, match="codes must be"):
         fc.Kv4Cache(cache.k_codes, cache.k_scales, cache.v_codes[:, :4], cache.v_scales)
     with pytest.raises(fc.FcError, match="invalid argument"):
         ctx.kv4_unpack(cache, row=4, n=5)
     O = torch.zeros_like(K)
     with pytest.raises(fc.FcError, match="invalid argument"):
         ctx.chunk_attention_kv4(K, cache, None, None, [0, 8], [9], ids, one, O)
-    with pytest.raises(fc.FcError, match="share one dtype"):
+    with pytest.raises(fc.FcError, match="K must be"):
         ctx.chunk_attention_kv4(K, cache, K.float(), K.float(), [0, 8], [9], ids, one, O)
     with pytest.raises(fc.FcError, match="store, a window"):
         ctx.chunk_attention_kv4(K, None, None, None, [0, 8], [0], ids, one, O)
