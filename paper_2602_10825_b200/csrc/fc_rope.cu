@@ -1,182 +1,229 @@
 // fc_qk_norm_rope: RMS norm of every head of queries and keys, and the rotation over (time, height, width), in one pass.
 //
-// A head's row is spread over 16-byte pieces, one per lane (16 lanes for a bf16 row of 128): each element is read and
-// written once and everything between is in registers.  A group of lanes owns a token and walks over some of its heads,
-// so that the token's cosines and sines, which all heads share, are computed once per group and not once per row.
+// Bound by HBM: every element is read and written once.  A head's row is spread over 16-byte pieces, one per lane (16 lanes for a
+// bf16 row of 128), and everything between the load and the store is in registers.  A group of lanes owns a token and walks
+// over some of its heads, four rows' loads in flight.  What it takes to stay under the copy rate is few instructions:
+//   - The cosines and sines of a token serve all its heads.  A block computes them once for its tokens, a pair a thread, and
+//     leaves them in shared memory; a group keeps its own in registers, multiplied by the norm's weights, so that the
+//     normed, weighted and rotated pair is (x0 cw0 - x1 sw1, x1 cw1 + x0 sw0) / rms.
+//   - Even and odd elements are held as pairs of fp32, so that squares, rotation and scaling are two-wide instructions.
+//   - With FC_ROPE_HALVES the partner of an element sits in another lane at an odd distance: the rows go through shared
+//     memory as they are, and the partners are read one by one.
 // Angles: a pair's frequency is held in turns as a 64-bit fixed-point fraction, so position x frequency is one wrapping
 // integer product whose overflow is exactly the reduction modulo a full turn; its top 32 bits go to sincospif.
 #include <climits>
 #include <cmath>
 
 #include "fc_common.cuh"
+#include "fc_tcgen05.cuh"
 
 namespace {
 
+using fc::sm100::add2;
+using fc::sm100::cvt_bf16x2;
+using fc::sm100::fma2;
+using fc::sm100::pack2;
+using fc::sm100::unpack2;
+
 constexpr int kThreads = 256;
-constexpr int kUnroll = 4;  // heads whose loads are in flight together
 
 struct RopeGeom {
-  int32_t H_q, H_kv, T, heads_per_item;
+  int32_t H_q, H_kv, T;
+  int32_t tokens, heads_per_group;  // tokens of a block; heads that a group of lanes walks over
   int64_t q_hs, q_rs, k_hs, k_rs, qo_hs, qo_rs, ko_hs, ko_rs;
   int32_t axis_dim[3];
   int32_t norm;
   float eps;
   int32_t t0, gh, gw;
-  int64_t n_items;
   uint64_t turns[64];  // per pair, in the order of the sections: turns per position, modulo one, times 2^64
 };
 
-template <typename T> struct Piece;  // 16 bytes of a row
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+  uint64_t d;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+  return d;
+}
+
+// 16 bytes of a row as even and odd elements, two of each to a register pair: e[i] = (x[4i], x[4i+2]), o[i] = (x[4i+1], x[4i+3]).
+template <typename T> struct Piece;
 template <> struct Piece<__nv_bfloat16> {
   static constexpr int N = 8;
-  static __device__ __forceinline__ void load(const void* p, float (&x)[N]) {
-    const uint4 v = *reinterpret_cast<const uint4*>(p);
-    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      x[2 * i] = fc::bf16_lo(w[i]);
-      x[2 * i + 1] = fc::bf16_hi(w[i]);
-    }
+  static __device__ __forceinline__ void split(const uint4& v, uint64_t (&e)[2], uint64_t (&o)[2]) {
+    e[0] = pack2(fc::bf16_lo(v.x), fc::bf16_lo(v.y));
+    o[0] = pack2(fc::bf16_hi(v.x), fc::bf16_hi(v.y));
+    e[1] = pack2(fc::bf16_lo(v.z), fc::bf16_lo(v.w));
+    o[1] = pack2(fc::bf16_hi(v.z), fc::bf16_hi(v.w));
   }
-  static __device__ __forceinline__ void store(void* p, const float (&x)[N]) {
-    uint4 v;
-    uint32_t* w = &v.x;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const __nv_bfloat162 b = __floats2bfloat162_rn(x[2 * i], x[2 * i + 1]);
-      w[i] = *reinterpret_cast<const uint32_t*>(&b);
-    }
-    *reinterpret_cast<uint4*>(p) = v;
+  static __device__ __forceinline__ uint4 join(const uint64_t (&e)[2], const uint64_t (&o)[2]) {
+    float a[4], b[4];
+    unpack2(e[0], a[0], a[1]);
+    unpack2(o[0], b[0], b[1]);
+    unpack2(e[1], a[2], a[3]);
+    unpack2(o[1], b[2], b[3]);
+    return make_uint4(cvt_bf16x2(a[0], b[0]), cvt_bf16x2(a[1], b[1]), cvt_bf16x2(a[2], b[2]), cvt_bf16x2(a[3], b[3]));
   }
 };
 template <> struct Piece<float> {
   static constexpr int N = 4;
-  static __device__ __forceinline__ void load(const void* p, float (&x)[N]) {
-    const float4 v = *reinterpret_cast<const float4*>(p);
-    x[0] = v.x; x[1] = v.y; x[2] = v.z; x[3] = v.w;
+  static __device__ __forceinline__ void split(const uint4& v, uint64_t (&e)[1], uint64_t (&o)[1]) {
+    e[0] = pack2(__uint_as_float(v.x), __uint_as_float(v.z));
+    o[0] = pack2(__uint_as_float(v.y), __uint_as_float(v.w));
   }
-  static __device__ __forceinline__ void store(void* p, const float (&x)[N]) {
-    *reinterpret_cast<float4*>(p) = make_float4(x[0], x[1], x[2], x[3]);
+  static __device__ __forceinline__ uint4 join(const uint64_t (&e)[1], const uint64_t (&o)[1]) {
+    float a[2], b[2];
+    unpack2(e[0], a[0], a[1]);
+    unpack2(o[0], b[0], b[1]);
+    return make_uint4(__float_as_uint(a[0]), __float_as_uint(b[0]), __float_as_uint(a[1]), __float_as_uint(b[1]));
   }
 };
 
-// Element e of a head: the pair it belongs to (-1: it does not turn), its partner and whether it is the pair's first.
-template <bool kHalves>
-__device__ __forceinline__ void place(const RopeGeom& g, int e, int& pair, int& axis, int& partner, bool& first) {
-  int start = 0, pair0 = 0;
-  pair = -1; axis = 0; partner = e; first = true;
+// FC_ROPE_HALVES: the pair element e of a head belongs to (-1: it does not turn), its partner and whether it is the first.
+__device__ __forceinline__ void place(const RopeGeom& g, int e, int& pair, int& partner, bool& first) {
+  int start = 0;
+  pair = -1; partner = e; first = true;
 #pragma unroll
   for (int a = 0; a < 3; ++a) {
     const int n = g.axis_dim[a], o = e - start;
     if (o >= 0 && o < n) {
-      axis = a;
-      if (kHalves) {
-        first = o < n / 2;
-        pair = pair0 + (first ? o : o - n / 2);
-        partner = first ? e + n / 2 : e - n / 2;
-      } else {
-        first = (o & 1) == 0;
-        pair = pair0 + o / 2;
-        partner = e ^ 1;
-      }
+      first = o < n / 2;
+      pair = start / 2 + (first ? o : o - n / 2);
+      partner = first ? e + n / 2 : e - n / 2;
     }
     start += n;
-    pair0 += n / 2;
   }
 }
 
 template <typename T, int D, bool kHalves>
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(kThreads, 4)
 qk_norm_rope_kernel(const T* Q, const T* K, T* Q_out, T* K_out, const float* __restrict__ q_weight,
                     const float* __restrict__ k_weight, const int32_t* __restrict__ pos, const __grid_constant__ RopeGeom g) {
   using P = Piece<T>;
-  constexpr int E = P::N, L = D / E;  // elements per lane, lanes per row
-  __shared__ uint64_t turns_s[64];
-  __shared__ float row_s[kHalves ? kThreads * E : 1];  // the normed row, where partners sit in other lanes
-  const int tid = threadIdx.x;
-  if (tid < 64) turns_s[tid] = g.turns[tid];
+  // Heads whose loads are in flight together (measured: a chunk of 4680 tokens of 48 bf16 heads takes 27.4 us with four, 28.5
+  // with three and 30 and more with two or with the next loads sent before the arithmetic; fp32 22.8 us with three, 24.8 with four).
+  constexpr int kUnroll = sizeof(T) == 4 ? 3 : 4;
+  constexpr int E = P::N, L = D / E, G = kThreads / L, V = E / 4;  // elements per lane, lanes per row, rows per block, pairs of pairs
+  __shared__ float2 cs_s[G * (D / 2)];                     // (cos, sin) of the block's tokens and pairs
+  __shared__ T row_s[kHalves ? kUnroll * kThreads * E : 1];  // the rows in flight, where partners sit in other lanes
+  const int tid = threadIdx.x, lane = tid % L, grp = tid / L;
+  const int first_token = blockIdx.x * g.tokens;
+
+  const int pairs = (g.axis_dim[0] + g.axis_dim[1] + g.axis_dim[2]) / 2;
+  for (int x = tid; x < g.tokens * (D / 2); x += kThreads) {
+    const int t = x / (D / 2), pair = x % (D / 2), n = min(first_token + t, g.T - 1);
+    if (pair >= pairs) {  // what does not turn, in the order of FC_ROPE_PAIRS
+      cs_s[x] = make_float2(1.f, 0.f);
+      continue;
+    }
+    const int axis = pair < g.axis_dim[0] / 2 ? 0 : pair < (g.axis_dim[0] + g.axis_dim[1]) / 2 ? 1 : 2;
+    int at;
+    if (pos) {
+      at = pos[3ll * n + axis];
+    } else {
+      const int frame = g.gh * g.gw;
+      at = axis == 0 ? g.t0 + n / frame : axis == 1 ? n % frame / g.gw : n % g.gw;
+    }
+    const uint64_t phase = (uint64_t)(int64_t)at * g.turns[pair] + 0x80000000ull;
+    float2 cs;
+    sincospif((float)(int32_t)(phase >> 32) * 0x1p-31f, &cs.y, &cs.x);
+    cs_s[x] = cs;
+  }
   __syncthreads();
 
-  const int lane = tid % L, grp = tid / L;
-  const int64_t item = (int64_t)blockIdx.x * (kThreads / L) + grp;
-  const bool live = item < g.n_items;
-  const int n = live ? (int)(item % g.T) : 0;
-  const int h0 = live ? (int)(item / g.T) * g.heads_per_item : 0;
-  const int h1 = live ? min(h0 + g.heads_per_item, g.H_q + g.H_kv) : 0;
+  const int t = grp % g.tokens, n = first_token + t;
+  const int h0 = (blockIdx.y * (G / g.tokens) + grp / g.tokens) * g.heads_per_group;
+  const int h1 = min(h0 + g.heads_per_group, g.H_q + g.H_kv);
+  if (n >= g.T || h0 >= h1) return;
+  const unsigned mask = L == 32 ? 0xffffffffu : ((1u << L) - 1u) << (tid & 31 & ~(L - 1));
 
-  int p[3];
-  if (pos) {
+  int partner[E], pair[E];  // FC_ROPE_HALVES only
+  uint32_t second = 0;      // the elements that are second in their pair
+  if (kHalves) {
 #pragma unroll
-    for (int a = 0; a < 3; ++a) p[a] = pos[3ll * n + a];
-  } else {
-    const int frame = g.gh * g.gw;
-    p[0] = g.t0 + n / frame;
-    p[1] = n % frame / g.gw;
-    p[2] = n % g.gw;
-  }
-  // out[i] = y[i] * c[i] + y[partner of i] * s[i]
-  float c[E], s[E];
-  int partner[E];
-#pragma unroll
-  for (int i = 0; i < E; ++i) {
-    int pair, axis;
-    bool first;
-    place<kHalves>(g, lane * E + i, pair, axis, partner[i], first);
-    c[i] = 1.f;
-    s[i] = 0.f;
-    if (!kHalves && (i & 1)) {  // the pair's angle is that of the element before
-      c[i] = c[i - 1];
-      s[i] = -s[i - 1];
-    } else if (pair >= 0) {
-      const int at = axis == 0 ? p[0] : axis == 1 ? p[1] : p[2];
-      const uint64_t phase = (uint64_t)(int64_t)at * turns_s[pair] + 0x80000000ull;
-      float sn;
-      sincospif((float)(int32_t)(phase >> 32) * 0x1p-31f, &sn, &c[i]);
-      s[i] = first ? -sn : sn;
+    for (int i = 0; i < E; ++i) {
+      bool first;
+      place(g, lane * E + i, pair[i], partner[i], first);
+      second |= first ? 0u : 1u << i;
     }
   }
 
   auto walk = [&](const T* src, T* dst, int64_t hs, int64_t rs, int64_t ohs, int64_t ors, const float* weight, int a, int b) {
-    float w[E];
+    // out[i] = x[i] c[i] + x[partner] s[i], with the weights of the elements it takes
+    uint64_t ce[V], co[V], se[V], so[V];
 #pragma unroll
-    for (int i = 0; i < E; ++i) w[i] = weight && g.norm ? weight[lane * E + i] : 1.f;
-    const T* in = src + (int64_t)n * rs + lane * E;
-    T* out = dst + (int64_t)n * ors + lane * E;
-    for (int h = a; h < b; h += kUnroll) {
-      float x[kUnroll][E];
+    for (int v = 0; v < V; ++v) {
+      float c[4], s[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int e = lane * E + 4 * v + i;
+        if (kHalves) {
+          const float2 cs = pair[4 * v + i] >= 0 ? cs_s[t * (D / 2) + pair[4 * v + i]] : make_float2(1.f, 0.f);
+          c[i] = cs.x;
+          s[i] = second >> (4 * v + i) & 1 ? cs.y : -cs.y;
+        } else {
+          const float2 cs = cs_s[t * (D / 2) + e / 2];
+          c[i] = cs.x;
+          s[i] = i & 1 ? cs.y : -cs.y;
+        }
+        if (weight && g.norm) {
+          c[i] *= weight[e];
+          s[i] *= weight[kHalves ? partner[4 * v + i] : e ^ 1];
+        }
+      }
+      ce[v] = pack2(c[0], c[2]);
+      co[v] = pack2(c[1], c[3]);
+      se[v] = pack2(s[0], s[2]);
+      so[v] = pack2(s[1], s[3]);
+    }
+    const T* in = src + (int64_t)n * rs + lane * E + a * hs;
+    T* out = dst + (int64_t)n * ors + lane * E + a * ohs;
+    for (int h = a; h < b; h += kUnroll, in += kUnroll * hs, out += kUnroll * ohs) {
+      uint4 raw[kUnroll];
 #pragma unroll
       for (int u = 0; u < kUnroll; ++u)
-        if (h + u < b) P::load(in + (int64_t)(h + u) * hs, x[u]);
+        if (h + u < b) raw[u] = *reinterpret_cast<const uint4*>(in + u * hs);
+      if (kHalves) {
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u)
+          if (h + u < b) *reinterpret_cast<uint4*>(&row_s[(u * G + grp) * D + lane * E]) = raw[u];
+        __syncwarp(mask);
+      }
 #pragma unroll
       for (int u = 0; u < kUnroll; ++u) {
         if (h + u >= b) break;
-        if (g.norm) {
-          float sum = 0.f;
+        uint64_t e[V], o[V], pe[V], po[V];
+        P::split(raw[u], e, o);
+        if (kHalves) {
+          const T* row = &row_s[(u * G + grp) * D];
 #pragma unroll
-          for (int i = 0; i < E; ++i) sum = fmaf(x[u][i], x[u][i], sum);
-          const unsigned mask = L == 32 ? 0xffffffffu : ((1u << L) - 1u) << (tid & 31 & ~(L - 1));
+          for (int v = 0; v < V; ++v) {
+            pe[v] = pack2(fc::to_float<T>(row[partner[4 * v]]), fc::to_float<T>(row[partner[4 * v + 2]]));
+            po[v] = pack2(fc::to_float<T>(row[partner[4 * v + 1]]), fc::to_float<T>(row[partner[4 * v + 3]]));
+          }
+        }
+        uint64_t r2 = pack2(1.f, 1.f);
+        if (g.norm) {
+          uint64_t sum2 = mul2(e[0], e[0]);
+          sum2 = fma2(o[0], o[0], sum2);
+#pragma unroll
+          for (int v = 1; v < V; ++v) sum2 = fma2(o[v], o[v], fma2(e[v], e[v], sum2));
+          float sum, other;
+          unpack2(sum2, sum, other);
+          sum += other;
 #pragma unroll
           for (int k = 1; k < L; k <<= 1) sum += __shfl_xor_sync(mask, sum, k);
-          const float r = 1.f / sqrtf(sum * (1.f / D) + g.eps);
-#pragma unroll
-          for (int i = 0; i < E; ++i) x[u][i] *= r * w[i];
+          const float r = rsqrtf(fmaf(sum, 1.f / D, g.eps));
+          r2 = pack2(r, r);
         }
-        float y[E];
-        if (kHalves) {
-          float* row = row_s + grp * D;
-          const unsigned mask = L == 32 ? 0xffffffffu : ((1u << L) - 1u) << (tid & 31 & ~(L - 1));
 #pragma unroll
-          for (int i = 0; i < E; ++i) row[lane * E + i] = x[u][i];
-          __syncwarp(mask);
-#pragma unroll
-          for (int i = 0; i < E; ++i) y[i] = fmaf(x[u][i], c[i], row[partner[i]] * s[i]);
-          __syncwarp(mask);
-        } else {
-#pragma unroll
-          for (int i = 0; i < E; ++i) y[i] = fmaf(x[u][i], c[i], x[u][i ^ 1] * s[i]);
+        for (int v = 0; v < V; ++v) {
+          const uint64_t y0 = fma2(e[v], ce[v], mul2(kHalves ? pe[v] : o[v], se[v]));
+          const uint64_t y1 = fma2(o[v], co[v], mul2(kHalves ? po[v] : e[v], so[v]));
+          e[v] = mul2(y0, r2);
+          o[v] = mul2(y1, r2);
         }
-        P::store(out + (int64_t)(h + u) * ohs, y);
+        *reinterpret_cast<uint4*>(out + u * ohs) = P::join(e, o);
       }
+      if (kHalves) __syncwarp(mask);
     }
   };
   if (h0 < g.H_q) walk(Q, Q_out, g.q_hs, g.q_rs, g.qo_hs, g.qo_rs, q_weight, h0, min(h1, g.H_q));
@@ -256,19 +303,26 @@ extern "C" int fc_qk_norm_rope(fc_ctx* ctx, void* stream, const fc_rope_desc* de
   g.t0 = grid_used ? desc->grid_t0 : 0;
   g.gh = grid_used ? desc->grid_h : 1;
   g.gw = grid_used ? desc->grid_w : 1;
-  // heads per item: as many as leave the device one full set of resident groups; a lone token gets a group per head
+  // A group of lanes takes as many heads as leave the device half a set of resident groups (more heads amortise the group's
+  // constants, fewer leave loads in flight); a lone token gets a group per head.  A block then takes as few tokens as its groups
+  // have use for.
   const int lanes = desc->d * es / 16, groups = kThreads / lanes;
-  const int64_t resident = (int64_t)ctx->sm_count * 2048 / lanes;
+  const int64_t resident = (int64_t)ctx->sm_count * 1024 / lanes;
   int64_t per = heads * desc->T / resident;
   per = per < 1 ? 1 : per > heads ? heads : per;
-  g.heads_per_item = (int32_t)per;
-  g.n_items = (heads + per - 1) / per * desc->T;
-  const int64_t blocks = (g.n_items + groups - 1) / groups;
-  if (blocks > INT32_MAX) return FC_ERR_UNSUPPORTED;
+  int parts = 1;  // of the heads, in a block
+  while (parts < groups && parts * per < heads) parts *= 2;
+  while (groups / parts > 1 && groups / parts / 2 >= desc->T) parts *= 2;
+  if (parts * per >= heads) per = (heads + parts - 1) / parts;  // the same number for every group
+  g.tokens = groups / parts;
+  g.heads_per_group = (int32_t)per;
+  const int64_t blocks = ((int64_t)desc->T + g.tokens - 1) / g.tokens, splits = (heads + parts * per - 1) / (parts * per);
+  if (splits > 65535) return FC_ERR_UNSUPPORTED;
+  const dim3 grid((unsigned)blocks, (unsigned)splits);
   FC_DEVICE_GUARD(ctx);
   cudaStream_t st = (cudaStream_t)stream;
 #define FC_ROPE_LAUNCH(T, D, HALVES)                                                                                  \
-  qk_norm_rope_kernel<T, D, HALVES><<<(unsigned)blocks, kThreads, 0, st>>>((const T*)Q, (const T*)K, (T*)Q_out, (T*)K_out, \
+  qk_norm_rope_kernel<T, D, HALVES><<<grid, kThreads, 0, st>>>((const T*)Q, (const T*)K, (T*)Q_out, (T*)K_out, \
                                                                            q_weight, k_weight, pos, g)
 #define FC_ROPE_PICK(T)                                                                                      \
   if (desc->d == 128) {                                                                                      \
