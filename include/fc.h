@@ -458,8 +458,9 @@ int fc_kv4_unpack(fc_ctx* ctx, void* stream, const fc_kv4_unpack_desc* desc, con
  * token get zeros (lse -inf).  There is no token map: a 4-bit store is compacted by fc_kv4_pack.
  *
  *   desc             as above; k_* and v_* strides and kv_rows describe the window.  impl: 0 auto; 1 force the
- *                    CUDA-core kernel (the path of fp32); bf16 only (FC_ERR_UNSUPPORTED): 2 unpack into the workspace and
- *                    run the tcgen05 kernel of fc_chunk_attention over [workspace | window]; 3 force the kernel for few rows.
+ *                    CUDA-core kernel; 2 (bf16 only) unpack into the workspace and run the tcgen05 kernel of
+ *                    fc_chunk_attention over [workspace | window]; 3 force the kernel for few rows, which reads the packed keys
+ *                    in one pass and is also the path of fp32.
  *   active_ids       as above; an id outside [0, W) sets FC_DEV_BAD_INDEX and is ignored.
  *   cache            HOST struct, rows >= n_cache; may be NULL if n_cache is 0.
  *   K, V             DEVICE [H_kv, kv_rows, d], the window; may be NULL if n_seg is 0 (no window).

@@ -17,7 +17,7 @@ int check_geometry(const fc_attn_desc* desc, int dtype, const int32_t* q_chunk_r
   if (desc->W > FC_MAX_CHUNKS || desc->H_kv > 65535) return FC_ERR_UNSUPPORTED;
   if (desc->impl < 0 || desc->impl > 3) return FC_ERR_INVALID_ARG;
   if (!(desc->scale >= 0.f)) return FC_ERR_INVALID_ARG;
-  if (desc->impl >= 2 && dtype != FC_BF16) return FC_ERR_UNSUPPORTED;
+  if (desc->impl == 2 && dtype != FC_BF16) return FC_ERR_UNSUPPORTED;
   fc::AttnGeom& a = g.a;
   a.H_q = desc->H_q; a.H_kv = desc->H_kv; a.d = desc->d; a.W = desc->W;
   a.group = desc->H_q / desc->H_kv;
@@ -32,6 +32,7 @@ int check_geometry(const fc_attn_desc* desc, int dtype, const int32_t* q_chunk_r
     a.vis[c] = kv_visible_len[c];
   }
   g.n_cache = n_cache;
+  g.f32 = dtype == FC_F32;
   g.n_vrows = (int64_t)(a.q_row_off[a.W] - a.q_row_off[0]) * a.group;
   if (g.n_vrows > INT32_MAX) return FC_ERR_UNSUPPORTED;
   return FC_OK;
@@ -96,9 +97,9 @@ UnpackedPlan plan_unpacked(const fc_ctx* ctx, const fc::Kv4AttnGeom& g) {
 // line between the two moves with the heads and the keys, so that the estimates are compared (measured at 24 heads of 128
 // over 28000 keys: 64 rows 112 us against 150, 128 rows 303 against 153).
 Path choose(const fc_ctx* ctx, const fc_attn_desc* desc, int dtype, const fc::Kv4AttnGeom& g_in) {
-  if (dtype == FC_F32 || desc->impl == 1) return kSimt;
+  if (desc->impl == 1) return kSimt;
   if (desc->impl == 2) return kUnpacked;
-  if (desc->impl == 3) return kRows;
+  if (desc->impl == 3 || dtype == FC_F32) return kRows;
   fc::Kv4AttnGeom g = g_in;
   fc::kv4_rows_workspace(ctx, g);
   return fc::kv4_rows_us(ctx, g) <= plan_unpacked(ctx, g).us ? kRows : kUnpacked;

@@ -15,6 +15,7 @@ struct Kv4AttnGeom {
   AttnGeom a;        // segments and store fields describe the window; vis counts cache and window together
   Kv4View cache;
   int32_t n_cache;
+  bool f32;             // type of Q, the window and O
   int32_t n_splits;  // parts the keys are cut into, at most kKv4MaxSplits
   int64_t part_keys;    // keys per part (few-row kernel: on its axis of costs)
   int64_t n_cache_ceil; // few-row kernel: where the window starts on that axis
@@ -68,7 +69,7 @@ inline int64_t tile_count(const AttnGeom& a, int rows_per_tile) {
 
 size_t kv4_simt_workspace(const fc_ctx* ctx, Kv4AttnGeom& g);  // also sets the split
 int kv4_simt(cudaStream_t st, const Kv4AttnGeom& g, const void* Q, const void* K, const void* V, int dtype, void* O);
-// bf16, few rows: tensor cores fed from registers
+// few rows, and fp32: tensor cores fed from registers
 size_t kv4_rows_workspace(const fc_ctx* ctx, Kv4AttnGeom& g);
 double kv4_rows_us(const fc_ctx* ctx, const Kv4AttnGeom& g);  // estimate, of a geometry that kv4_rows_workspace has seen
 int kv4_rows(cudaStream_t st, const Kv4AttnGeom& g, const void* Q, const void* K, const void* V, void* O);

@@ -1,18 +1,23 @@
-// Attention of few query rows over [4-bit clean region | window], bf16: one pass over the keys, cut into parts that a
-// second kernel joins.
+// Attention of few query rows over [4-bit clean region | window]: one pass over the keys, cut into parts that a second kernel
+// joins; also the path of fp32 tensors whatever their rows.
 //
 // Bound by the bytes of the clean region and, next to it, by the issue slots that unpacking takes: 4.5 bits an element leave an
-// SM about 46 elements per clock to unpack at the copy rate.  So nothing goes through shared memory: a warp loads the codes
-// of 16 keys straight into the registers of its tensor-core operands, and every element costs about 1.6 instructions.
+// SM about 46 elements per clock to unpack at the copy rate.  So a warp takes the codes of 16 keys from its own ring in shared
+// memory (cp.async, three steps ahead) straight into the registers of its tensor-core operands, at about 1.6 instructions an element.
 //   S^T = K Q^T   m16n8k16, keys as rows, up to 8 NT query rows as columns.  The order of the head's elements along the
 //                 contraction is free as long as K and Q agree: lane (key, q) takes elements [q D/4, (q+1) D/4) of its key, which
-//                 is one load and one scale.
+//                 is one access and one scale.
 //   O^T = V^T P^T dims as rows.  Again the order of the rows is free: lane (n, q) takes dims [n D/8, (n+1) D/8) of keys 2q,
 //                 2q+1, 2q+8, 2q+9; the codes of two keys are brought into one register before they are unpacked, so that
 //                 the pair along the contraction is a pair of 16-bit halves.
 // P^T goes from the accumulator layout of the first product to the operand layout of the second by movmatrix.
 // The maximum is lazy (it moves when a logit passes it by 2^8), so that the usual step has no shuffles and no rescaling.
 // The four warps of a block take 16-key steps in turn and join their sums through shared memory at the end.
+//
+// fp32.  A 24-bit number is exactly the sum of three bf16 numbers (its bits cut into three), and an unpacked key is
+// exactly one.  So Q K^T over the clean region is three products of bf16 numbers, each exact before it is added in fp32, and so
+// is P V; over an fp32 window the six products of parts that reach 2^-24 are taken.  The tensor core cuts, rather than
+// rounds, what it adds up; so the small parts have accumulators of their own, and O is added up outside, step by step.
 #include <algorithm>
 #include <cmath>
 
@@ -45,6 +50,17 @@ __device__ __forceinline__ uint32_t transpose8x8(uint32_t x) {
   asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
   return y;
 }
+// The three bf16 parts of fp32 numbers a, b as pairs (a low, b high): p[0] + p[1] + p[2] = (a, b) exactly.
+__device__ __forceinline__ void parts_of(float a, float b, uint32_t (&p)[3]) {
+#pragma unroll
+  for (int i = 0; i < 3; ++i) {
+    p[i] = __byte_perm(__float_as_uint(a), __float_as_uint(b), 0x7632);
+    a -= __uint_as_float(__float_as_uint(a) & 0xffff0000u);
+    b -= __uint_as_float(__float_as_uint(b) & 0xffff0000u);
+  }
+}
+template <typename T> constexpr int kParts = sizeof(T) == 4 ? 3 : 1;
+
 __device__ __forceinline__ uint32_t prmt(uint32_t a, uint32_t b, uint32_t sel) { return __byte_perm(a, b, sel); }
 
 // A warp's ring of 16-key steps in shared memory, filled by cp.async: the codes of K and V, then their scales.
@@ -52,13 +68,21 @@ template <int D> struct Ring {
   static constexpr int kCodes = kStep * D / 2, kScales = kStep * D / 16;  // bytes of one tensor's step
   static constexpr int kBytes = 2 * (kCodes + kScales);
   static constexpr int kStages = 4;
-  // A window key is 2 D bytes a tensor: one buffer of 16 keys for K and one for V in the same place.  K of the next step is
-  // on its way while V of this one is worked on, and the other way round.
-  static constexpr int kWindow = kStep * D * 2;
-  static_assert(2 * kWindow <= kStages * kBytes, "the window's buffers fit the ring");
+};
+
+// The window's keys in the place of the ring: 16 rows of K and 16 of V.  bf16 rows have a buffer each: K of the next step is on
+// its way while V of this one is worked on, and the other way round; fp32 rows take turns in one.
+template <typename T, int D> struct Window {
+  static constexpr int kRow = D * (int)sizeof(T), kBytes = kStep * kRow, kPieces = kRow / 16;
+  static constexpr bool kOne = 2 * kBytes > Ring<D>::kStages * Ring<D>::kBytes;
+  static_assert(kBytes <= Ring<D>::kStages * Ring<D>::kBytes, "the window's rows fit the ring");
   // Where 16-byte piece p of row r lies in its row, so that the eight lanes that are served together read different banks.
-  static __device__ __forceinline__ int k_piece(int r, int p) { return p ^ ((p >> 3) & 1) ^ ((r & 1) << 1); }
-  static __device__ __forceinline__ int v_piece(int r, int p) { return p ^ (((r >> 1) & 3) << 1) ^ ((p >> 1) & 1); }
+  static __device__ __forceinline__ int k_piece(int r, int p) {
+    return kPieces == 32 ? p ^ ((p >> 3) & 3) ^ ((r & 1) << 2) : p ^ ((p >> 3) & 1) ^ ((r & 1) << 1);
+  }
+  static __device__ __forceinline__ int v_piece(int r, int p) {
+    return kPieces == 32 ? p ^ ((r >> 1) & 3) : p ^ (((r >> 1) & 3) << 1) ^ ((p >> 1) & 1);
+  }
 };
 
 template <int N> __device__ __forceinline__ void cp_async(uint32_t dst, const void* src) {
@@ -90,9 +114,9 @@ template <int D, int NT> struct State {
 };
 
 // S^T -> P^T operands.  n_valid: keys of the step that exist (kTail only).
-template <int D, int NT, bool kTail>
+template <typename T, int D, int NT, bool kTail>
 __device__ __forceinline__ void softmax_step(State<D, NT>& st, float (&s)[NT][4], float scale_log2, int lane, int n_valid,
-                                             uint32_t (&p0)[NT], uint32_t (&p1)[NT]) {
+                                             uint32_t (&p0)[kParts<T>][NT], uint32_t (&p1)[kParts<T>][NT]) {
   bool move = false;
 #pragma unroll
   for (int t = 0; t < NT; ++t) {
@@ -133,22 +157,64 @@ __device__ __forceinline__ void softmax_step(State<D, NT>& st, float (&s)[NT][4]
     const float e2 = ex2(fmaf(s[t][2], scale_log2, -st.ref[t][0])), e3 = ex2(fmaf(s[t][3], scale_log2, -st.ref[t][1]));
     st.l[t][0] += e0 + e2;
     st.l[t][1] += e1 + e3;
-    p0[t] = transpose8x8(cvt_bf16x2(e0, e1));
-    p1[t] = transpose8x8(cvt_bf16x2(e2, e3));
+    if constexpr (kParts<T> == 1) {
+      p0[0][t] = transpose8x8(cvt_bf16x2(e0, e1));
+      p1[0][t] = transpose8x8(cvt_bf16x2(e2, e3));
+    } else {
+      uint32_t a[3], b[3];
+      parts_of(e0, e1, a);
+      parts_of(e2, e3, b);
+#pragma unroll
+      for (int i = 0; i < 3; ++i) {
+        p0[i][t] = transpose8x8(a[i]);
+        p1[i][t] = transpose8x8(b[i]);
+      }
+    }
+  }
+}
+
+// S^T += K Q^T over 16 elements of the head, K as NK parts of operand registers: s the largest products, rest the others.
+template <typename T, int D, int NT, int NK>
+__device__ __forceinline__ void logits(float (&s)[NT][4], float (&rest)[NT][4], const uint32_t (&k)[NK][4],
+                                       const uint32_t (&qb)[kParts<T>][NT][D / 8], int at) {
+#pragma unroll
+  for (int t = 0; t < NT; ++t) {
+#pragma unroll
+    for (int i = NK - 1; i >= 0; --i)
+#pragma unroll
+      for (int j = kParts<T> - 1; j >= 0; --j)
+        if (i + j < 3) mma(i + j == 0 ? s[t] : rest[t], k[i][0], k[i][1], k[i][2], k[i][3], qb[j][t][at], qb[j][t][at + 1]);
+  }
+}
+// O^T tile += V^T P^T, V as NV parts.
+template <typename T, int NT, int NV>
+__device__ __forceinline__ void weigh(float (&o)[4], const uint32_t (&v)[NV][4], const uint32_t (&p0)[kParts<T>][NT],
+                                      const uint32_t (&p1)[kParts<T>][NT], int t) {
+  if constexpr (kParts<T> == 1) {
+    mma(o, v[0][0], v[0][1], v[0][2], v[0][3], p0[0][t], p1[0][t]);
+  } else {
+    float x[4] = {};
+#pragma unroll
+    for (int w = 2; w >= 0; --w)  // the smallest products first
+#pragma unroll
+      for (int i = 0; i < NV; ++i)
+        if (w - i >= 0 && w - i < 3) mma(x, v[i][0], v[i][1], v[i][2], v[i][3], p0[w - i][t], p1[w - i][t]);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) o[i] += x[i];
   }
 }
 
 // One step over 16 packed keys, which lie at `buf`.
-template <int D, int NT, bool kTail>
-__device__ __forceinline__ void packed_step(State<D, NT>& st, const uint8_t* buf, const uint32_t (&qb)[NT][D / 8], float scale_log2,
-                                            int lane, int n_valid) {
+template <typename T, int D, int NT, bool kTail>
+__device__ __forceinline__ void packed_step(State<D, NT>& st, const uint8_t* buf, const uint32_t (&qb)[kParts<T>][NT][D / 8],
+                                            float scale_log2, int lane, int n_valid) {
   using R = Ring<D>;
   const int n = lane >> 2, q = lane & 3;
   const uint8_t* kc = buf + n * (D / 2) + q * (D / 8);
   const uint8_t* vc = buf + R::kCodes + 2 * q * (D / 2) + n * (D / 16);
   const uint16_t* ks = reinterpret_cast<const uint16_t*>(buf + 2 * R::kCodes) + n * (D / 32) + q * D / 128;
   const uint16_t* vs = reinterpret_cast<const uint16_t*>(buf + 2 * R::kCodes + R::kScales) + 2 * q * (D / 32) + n * D / 256;
-  float s[NT][4] = {};
+  float s[NT][4] = {}, rest[NT][4] = {};
   {
     uint32_t k0[D / 32], k1[D / 32];
     lds_words(kc, k0);
@@ -160,19 +226,23 @@ __device__ __forceinline__ void packed_step(State<D, NT>& st, const uint8_t* buf
       uint32_t x[4], y[4];
       fc::kv4_word(k0[w], s0, b0, x);
       fc::kv4_word(k1[w], s1, b1, y);
-#pragma unroll
-      for (int t = 0; t < NT; ++t) {
-        mma(s[t], x[0], y[0], x[1], y[1], qb[t][4 * w], qb[t][4 * w + 1]);
-        mma(s[t], x[2], y[2], x[3], y[3], qb[t][4 * w + 2], qb[t][4 * w + 3]);
-      }
+      const uint32_t lo[1][4] = {{x[0], y[0], x[1], y[1]}}, hi[1][4] = {{x[2], y[2], x[3], y[3]}};
+      logits<T, D>(s, rest, lo, qb, 4 * w);
+      logits<T, D>(s, rest, hi, qb, 4 * w + 2);
     }
   }
-  uint32_t v[4][D / 64], p0[NT], p1[NT];
+  if constexpr (kParts<T> > 1) {
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) s[t][i] += rest[t][i];
+  }
+  uint32_t v[4][D / 64], p0[kParts<T>][NT], p1[kParts<T>][NT];
 #pragma unroll
   for (int i = 0; i < 4; ++i) lds_words(vc + ((i & 1) + 8 * (i >> 1)) * (D / 2), v[i]);
   const uint32_t sl = vs[0] | ((uint32_t)vs[D / 32] << 16), sh = vs[8 * (D / 32)] | ((uint32_t)vs[9 * (D / 32)] << 16);
   const uint32_t bl = fc::kv4_bias2(sl), bh = fc::kv4_bias2(sh);
-  softmax_step<D, NT, kTail>(st, s, scale_log2, lane, n_valid, p0, p1);
+  softmax_step<T, D, NT, kTail>(st, s, scale_log2, lane, n_valid, p0, p1);
 #pragma unroll
   for (int w = 0; w < D / 64; ++w) {
     uint32_t el[4], ol[4], eh[4], oh[4];  // even and odd elements, low and high keys
@@ -181,28 +251,35 @@ __device__ __forceinline__ void packed_step(State<D, NT>& st, const uint8_t* buf
     fc::kv4_word(prmt(v[2][w], v[3][w], 0x5410), sh, bh, eh);
     fc::kv4_word(prmt(v[2][w], v[3][w], 0x7632), sh, bh, oh);
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t x[1][4] = {{el[i], ol[i], eh[i], oh[i]}};
 #pragma unroll
-      for (int t = 0; t < NT; ++t) mma(st.o[t][4 * w + i], el[i], ol[i], eh[i], oh[i], p0[t], p1[t]);
+      for (int t = 0; t < NT; ++t) weigh<T, NT>(st.o[t][4 * w + i], x, p0, p1, t);
+    }
   }
 }
 
-template <int D, int NT>
+__device__ __forceinline__ void store4(float* p, float4 x) { *reinterpret_cast<float4*>(p) = x; }
+__device__ __forceinline__ void store4(__nv_bfloat16* p, float4 x) {
+  *reinterpret_cast<uint2*>(p) = make_uint2(cvt_bf16x2(x.x, x.y), cvt_bf16x2(x.z, x.w));
+}
+
+template <typename T, int D, int NT>
 __global__ void __launch_bounds__(kThreads, blocks_per_sm(NT))
-attention_kv4_rows_kernel(const __nv_bfloat16* __restrict__ Q, const __nv_bfloat16* __restrict__ K,
-                          const __nv_bfloat16* __restrict__ V, __nv_bfloat16* __restrict__ O,
+attention_kv4_rows_kernel(const T* __restrict__ Q, const T* __restrict__ K, const T* __restrict__ V, T* __restrict__ O,
                           const __grid_constant__ fc::Kv4AttnGeom g) {
-  constexpr int kRows = 8 * NT, kLaneDims = D / 4, kLaneCols = D / 8;
+  constexpr int kRows = 8 * NT, kLaneDims = D / 4, kLaneCols = D / 8, kPer = 16 / (int)sizeof(T);
   using R = Ring<D>;
+  using Wn = Window<T, D>;
   // the rings, and after the last step, in their place, what the warps join
   __shared__ __align__(16) uint8_t smem[kWarps * (R::kStages * R::kBytes > kRows * (D + 4) * 4 ? R::kStages * R::kBytes : kRows * (D + 4) * 4)];
   __shared__ float2 ml_s[kWarps][kRows];
   fc::pdl_launch_dependents();  // the joining kernel may take its place; it waits for this grid to end
   const fc::AttnGeom& a = g.a;
   const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32, n = lane >> 2, q = lane & 3;
-  const int part = blockIdx.x, hk = blockIdx.y;
+  const int part = blockIdx.z, hk = blockIdx.y;
   int v0 = 0;
-  const int c = fc::tile_chunk<kRows>(a, blockIdx.z, v0);
+  const int c = fc::tile_chunk<kRows>(a, blockIdx.x, v0);
   if (c < 0) return;
   const int rows_here = min(kRows, (a.q_row_off[c + 1] - a.q_row_off[c]) * a.group - v0);
 
@@ -248,45 +325,53 @@ attention_kv4_rows_kernel(const __nv_bfloat16* __restrict__ Q, const __nv_bfloat
     cp_async_commit();
   };
   // A window step's copies of one tensor: the lanes look one row each up and pass it on.
-  auto copy_window = [&](const __nv_bfloat16* base, int64_t rs, uint32_t at, int kb, bool is_v) {
+  auto copy_window = [&](const T* base, int64_t rs, uint32_t at, int kb, bool is_v) {
     if (kb < w1) {
       const uint32_t row = (uint32_t)fc::window_row(a, min(kb + lane % 16, w1 - 1));  // below 2^32
-      constexpr int kPieces = D / 8, kRowsAtOnce = 32 / kPieces;
+      constexpr int kPieces = Wn::kPieces, kRowsAtOnce = 32 / kPieces;
 #pragma unroll
       for (int i = 0; i < kStep / kRowsAtOnce; ++i) {
         const int r = i * kRowsAtOnce + lane / kPieces, p = lane % kPieces;
         const int64_t phys = __shfl_sync(0xffffffffu, row, r);
-        cp_async<16>(at + r * (2 * D) + 16 * (is_v ? R::v_piece(r, p) : R::k_piece(r, p)), base + phys * rs + 8 * p);
+        cp_async<16>(at + r * Wn::kRow + 16 * (is_v ? Wn::v_piece(r, p) : Wn::k_piece(r, p)), base + phys * rs + kPer * p);
       }
     }
     cp_async_commit();
   };
-  const __nv_bfloat16* kw = K + hk * a.k_hs;
-  const __nv_bfloat16* vw = V + hk * a.v_hs;
+  const T* kw = K + hk * a.k_hs;
+  const T* vw = V + hk * a.v_hs;
   if (k0 < k1) {
 #pragma unroll
     for (int i = 0; i < R::kStages - 1; ++i) copy(i, kb0 + i * kAll);
   }
   // everything up to here reads only what the host knows; the list is on the device
-  if (part == 0 && hk == 0 && blockIdx.z == 0 && tid == 0) fc::report_bad_ids(a);
+  if (part == 0 && hk == 0 && blockIdx.x == 0 && tid == 0) fc::report_bad_ids(a);
   if (!fc::chunk_active(a, c)) {
     cp_async_wait<0>();
     return;
   }
 
-  uint32_t qb[NT][kLaneDims / 2];
+  uint32_t qb[kParts<T>][NT][kLaneDims / 2];
 #pragma unroll
   for (int t = 0; t < NT; ++t) {
     const int r = 8 * t + n;
 #pragma unroll
-    for (int i = 0; i < kLaneDims / 8; ++i) {
+    for (int i = 0; i < kLaneDims / kPer; ++i) {
       uint4 x = make_uint4(0u, 0u, 0u, 0u);
       if (r < rows_here) {
         const int v = v0 + r;
-        const __nv_bfloat16* src = Q + (int64_t)(hk * a.group + v % a.group) * a.q_hs + (int64_t)(a.q_row_off[c] + v / a.group) * a.q_rs;
-        x = *reinterpret_cast<const uint4*>(src + q * kLaneDims + 8 * i);
+        const T* src = Q + (int64_t)(hk * a.group + v % a.group) * a.q_hs + (int64_t)(a.q_row_off[c] + v / a.group) * a.q_rs;
+        x = *reinterpret_cast<const uint4*>(src + q * kLaneDims + kPer * i);
       }
-      qb[t][4 * i] = x.x; qb[t][4 * i + 1] = x.y; qb[t][4 * i + 2] = x.z; qb[t][4 * i + 3] = x.w;
+      if constexpr (kParts<T> == 1) {
+        qb[0][t][4 * i] = x.x; qb[0][t][4 * i + 1] = x.y; qb[0][t][4 * i + 2] = x.z; qb[0][t][4 * i + 3] = x.w;
+      } else {
+        uint32_t lo[3], hi[3];
+        parts_of(__uint_as_float(x.x), __uint_as_float(x.y), lo);
+        parts_of(__uint_as_float(x.z), __uint_as_float(x.w), hi);
+#pragma unroll
+        for (int j = 0; j < 3; ++j) qb[j][t][2 * i] = lo[j], qb[j][t][2 * i + 1] = hi[j];
+      }
     }
   }
   State<D, NT> st;
@@ -309,60 +394,93 @@ attention_kv4_rows_kernel(const __nv_bfloat16* __restrict__ Q, const __nv_bfloat
     };
     for (; kb + kStep <= k1; kb += kAll) {
       next();
-      packed_step<D, NT, false>(st, buf + stage * R::kBytes, qb, scale_log2, lane, kStep);
+      packed_step<T, D, NT, false>(st, buf + stage * R::kBytes, qb, scale_log2, lane, kStep);
       __syncwarp();  // the stage has been read by every lane before it is filled again
       stage = (stage + 1) % R::kStages;
     }
     if (kb < k1) {
       next();
-      packed_step<D, NT, true>(st, buf + stage * R::kBytes, qb, scale_log2, lane, k1 - kb);
+      packed_step<T, D, NT, true>(st, buf + stage * R::kBytes, qb, scale_log2, lane, k1 - kb);
     }
     cp_async_wait<0>();
     __syncwarp();
   }
   if (w0 < w1) {
     const int wb0 = w0 + kStep * warp;
+    const uint32_t v_at = Wn::kOne ? 0 : Wn::kBytes;
     copy_window(kw, a.k_rs, ring, wb0, false);
-    copy_window(vw, a.v_rs, ring + R::kWindow, wb0, true);
+    if (!Wn::kOne) copy_window(vw, a.v_rs, ring + v_at, wb0, true);
     for (int kb = wb0; kb < w1; kb += kAll) {
-      cp_async_wait<1>();
+      cp_async_wait<Wn::kOne ? 0 : 1>();
       __syncwarp();
-      float s[NT][4] = {};
+      float s[NT][4] = {}, rest[NT][4] = {};
 #pragma unroll
-      for (int i = 0; i < kLaneDims / 8; ++i) {
-        const int p = q * (kLaneDims / 8) + i;
-        const uint4 x = *reinterpret_cast<const uint4*>(buf + n * (2 * D) + 16 * R::k_piece(n, p));
-        const uint4 y = *reinterpret_cast<const uint4*>(buf + (n + 8) * (2 * D) + 16 * R::k_piece(n, p));
-#pragma unroll
-        for (int t = 0; t < NT; ++t) {
-          mma(s[t], x.x, y.x, x.y, y.y, qb[t][4 * i], qb[t][4 * i + 1]);
-          mma(s[t], x.z, y.z, x.w, y.w, qb[t][4 * i + 2], qb[t][4 * i + 3]);
+      for (int i = 0; i < kLaneDims / kPer; ++i) {
+        const int p = q * (kLaneDims / kPer) + i;
+        const uint4 x = *reinterpret_cast<const uint4*>(buf + n * Wn::kRow + 16 * Wn::k_piece(n, p));
+        const uint4 y = *reinterpret_cast<const uint4*>(buf + (n + 8) * Wn::kRow + 16 * Wn::k_piece(n, p));
+        if constexpr (kParts<T> == 1) {
+          const uint32_t lo[1][4] = {{x.x, y.x, x.y, y.y}}, hi[1][4] = {{x.z, y.z, x.w, y.w}};
+          logits<T, D>(s, rest, lo, qb, 4 * i);
+          logits<T, D>(s, rest, hi, qb, 4 * i + 2);
+        } else {
+          uint32_t xl[3], xh[3], yl[3], yh[3];
+          parts_of(__uint_as_float(x.x), __uint_as_float(x.y), xl);
+          parts_of(__uint_as_float(x.z), __uint_as_float(x.w), xh);
+          parts_of(__uint_as_float(y.x), __uint_as_float(y.y), yl);
+          parts_of(__uint_as_float(y.z), __uint_as_float(y.w), yh);
+          const uint32_t k[3][4] = {{xl[0], yl[0], xh[0], yh[0]}, {xl[1], yl[1], xh[1], yh[1]}, {xl[2], yl[2], xh[2], yh[2]}};
+          logits<T, D>(s, rest, k, qb, 2 * i);
         }
       }
+      if constexpr (kParts<T> > 1) {
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) s[t][i] += rest[t][i];
+      }
       __syncwarp();
-      copy_window(kw, a.k_rs, ring, kb + kAll, false);
-      uint32_t p0[NT], p1[NT];
-      softmax_step<D, NT, true>(st, s, scale_log2, lane, w1 - kb, p0, p1);
-      cp_async_wait<1>();
+      if (Wn::kOne) copy_window(vw, a.v_rs, ring, kb, true);
+      else copy_window(kw, a.k_rs, ring, kb + kAll, false);
+      uint32_t p0[kParts<T>][NT], p1[kParts<T>][NT];
+      softmax_step<T, D, NT, true>(st, s, scale_log2, lane, w1 - kb, p0, p1);
+      cp_async_wait<Wn::kOne ? 0 : 1>();
       __syncwarp();
 #pragma unroll
-      for (int w = 0; w < kLaneCols / 8; ++w) {
+      for (int w = 0; w < kLaneCols / kPer; ++w) {
         uint4 x[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const int r = 2 * q + (i & 1) + 8 * (i >> 1);
-          x[i] = *reinterpret_cast<const uint4*>(buf + R::kWindow + r * (2 * D) + 16 * R::v_piece(r, n * (kLaneCols / 8) + w));
+          x[i] = *reinterpret_cast<const uint4*>(buf + v_at + r * Wn::kRow + 16 * Wn::v_piece(r, n * (kLaneCols / kPer) + w));
         }
         const uint32_t* y[4] = {&x[0].x, &x[1].x, &x[2].x, &x[3].x};
+        if constexpr (kParts<T> == 1) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
+          for (int i = 0; i < 4; ++i) {
+            const uint32_t v[1][4] = {{prmt(y[0][i], y[1][i], 0x5410), prmt(y[0][i], y[1][i], 0x7632),
+                                       prmt(y[2][i], y[3][i], 0x5410), prmt(y[2][i], y[3][i], 0x7632)}};
 #pragma unroll
-          for (int t = 0; t < NT; ++t)
-            mma(st.o[t][4 * w + i], prmt(y[0][i], y[1][i], 0x5410), prmt(y[0][i], y[1][i], 0x7632), prmt(y[2][i], y[3][i], 0x5410),
-                prmt(y[2][i], y[3][i], 0x7632), p0[t], p1[t]);
+            for (int t = 0; t < NT; ++t) weigh<T, NT>(st.o[t][4 * w + i], v, p0, p1, t);
+          }
+        } else {
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {  // dims 2i and 2i + 1 of the four that were read
+            uint32_t e[4][3];
+            parts_of(__uint_as_float(y[0][2 * i]), __uint_as_float(y[1][2 * i]), e[0]);
+            parts_of(__uint_as_float(y[0][2 * i + 1]), __uint_as_float(y[1][2 * i + 1]), e[1]);
+            parts_of(__uint_as_float(y[2][2 * i]), __uint_as_float(y[3][2 * i]), e[2]);
+            parts_of(__uint_as_float(y[2][2 * i + 1]), __uint_as_float(y[3][2 * i + 1]), e[3]);
+            const uint32_t v[3][4] = {{e[0][0], e[1][0], e[2][0], e[3][0]}, {e[0][1], e[1][1], e[2][1], e[3][1]},
+                                      {e[0][2], e[1][2], e[2][2], e[3][2]}};
+#pragma unroll
+            for (int t = 0; t < NT; ++t) weigh<T, NT>(st.o[t][2 * w + i], v, p0, p1, t);
+          }
+        }
       }
       __syncwarp();
-      copy_window(vw, a.v_rs, ring + R::kWindow, kb + kAll, true);
+      if (Wn::kOne) copy_window(kw, a.k_rs, ring, kb + kAll, false);
+      else copy_window(vw, a.v_rs, ring + v_at, kb + kAll, true);
     }
     cp_async_wait<0>();
   }
@@ -413,15 +531,15 @@ attention_kv4_rows_kernel(const __nv_bfloat16* __restrict__ Q, const __nv_bfloat
       const float inv = l > 0.f ? 1.f / l : (l == l ? 0.f : l);
       const int h = hk * a.group + v % a.group;
       const int64_t rowg = a.q_row_off[c] + v / a.group;
-      *reinterpret_cast<uint2*>(O + h * a.o_hs + rowg * a.o_rs + d4) =
-          make_uint2(cvt_bf16x2(o.x * inv, o.y * inv), cvt_bf16x2(o.z * inv, o.w * inv));
+      store4(O + h * a.o_hs + rowg * a.o_rs + d4, make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv));
       if (a.lse && d4 == 0) a.lse[h * a.lse_hs + rowg] = l > 0.f ? (m + log2f(l)) * 0.6931471805599453f : (l == l ? -INFINITY : l);
     }
   }
 }
 
-// Rows per tile: eight where no chunk has more, else sixteen.
+// Rows per tile / 8: one where no chunk has more than eight rows, and for fp32 (whose Q takes three times the registers), else two.
 int tiles_of(const fc::Kv4AttnGeom& g) {
+  if (g.f32) return 1;
   for (int c = 0; c < g.a.W; ++c)
     if ((int64_t)(g.a.q_row_off[c + 1] - g.a.q_row_off[c]) * g.a.group > 8) return 2;
   return 1;
@@ -463,16 +581,16 @@ int kv4_rows(cudaStream_t st, const Kv4AttnGeom& g, const void* Q, const void* K
   const int nt = tiles_of(g);
   const int64_t tiles = tile_count(g.a, 8 * nt);
   if (tiles == 0) return FC_OK;
-  if (tiles > 65535) return FC_ERR_UNSUPPORTED;
-  const dim3 grid((unsigned)g.n_splits, (unsigned)g.a.H_kv, (unsigned)tiles);
-#define FC_KV4_ROWS(D, NT)                                                                                              \
-  attention_kv4_rows_kernel<D, NT><<<grid, kThreads, 0, st>>>((const __nv_bfloat16*)Q, (const __nv_bfloat16*)K,         \
-                                                              (const __nv_bfloat16*)V, (__nv_bfloat16*)O, g)
-  if (g.a.d == 128) { if (nt == 1) FC_KV4_ROWS(128, 1); else FC_KV4_ROWS(128, 2); }
-  else { if (nt == 1) FC_KV4_ROWS(64, 1); else FC_KV4_ROWS(64, 2); }
+  if (tiles > INT32_MAX) return FC_ERR_UNSUPPORTED;
+  const dim3 grid((unsigned)tiles, (unsigned)g.a.H_kv, (unsigned)g.n_splits);
+#define FC_KV4_ROWS(T, D, NT) \
+  attention_kv4_rows_kernel<T, D, NT><<<grid, kThreads, 0, st>>>((const T*)Q, (const T*)K, (const T*)V, (T*)O, g)
+  if (g.f32) { if (g.a.d == 128) FC_KV4_ROWS(float, 128, 1); else FC_KV4_ROWS(float, 64, 1); }
+  else if (g.a.d == 128) { if (nt == 1) FC_KV4_ROWS(__nv_bfloat16, 128, 1); else FC_KV4_ROWS(__nv_bfloat16, 128, 2); }
+  else { if (nt == 1) FC_KV4_ROWS(__nv_bfloat16, 64, 1); else FC_KV4_ROWS(__nv_bfloat16, 64, 2); }
 #undef FC_KV4_ROWS
   FC_LAUNCH_CHECK("attention_kv4_rows_kernel");
-  return g.n_splits > 1 ? kv4_combine(st, g, FC_BF16, O, true) : FC_OK;
+  return g.n_splits > 1 ? kv4_combine(st, g, g.f32 ? FC_F32 : FC_BF16, O, true) : FC_OK;
 }
 
 }  // namespace fc

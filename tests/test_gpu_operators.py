@@ -369,13 +369,13 @@ CASES = [
 
 
 @pytest.mark.parametrize("d", [64, 128])
-@pytest.mark.parametrize("dtype, impl", [(BF16, 0), (BF16, 1), (BF16, 2), (BF16, 3), (F32, 0)])
+@pytest.mark.parametrize("dtype, impl", [(BF16, 0), (BF16, 1), (BF16, 2), (BF16, 3), (F32, 0), (F32, 1)])
 @pytest.mark.parametrize("case", CASES, ids=lambda c: "-".join(map(str, c["lens"])) + f"@{c['n_cache']}")
 def test_attention(fc, ctx, case, dtype, impl, d):
     run_attention(fc, ctx, d=d, dtype=dtype, impl=impl, **case)
 
 
-@pytest.mark.parametrize("dtype, impl", [(BF16, 0), (BF16, 1), (BF16, 2), (BF16, 3), (F32, 0)])
+@pytest.mark.parametrize("dtype, impl", [(BF16, 0), (BF16, 1), (BF16, 2), (BF16, 3), (F32, 0), (F32, 1)])
 def test_attention_visible_lengths(fc, ctx, dtype, impl):
     # nothing visible, one token, inside the clean region, at its end, inside the window, at a tile's edge
     for cut in ([0, 1, 100], [128, 129, 300], [299, 301, 333], [0, 0, 0]):
@@ -384,7 +384,7 @@ def test_attention_visible_lengths(fc, ctx, dtype, impl):
     run_attention(fc, ctx, H_q=2, H_kv=2, d=64, lens=[2, 2], n_cache=9000, win=False, active=[0, 1], cut=[3, 9000], dtype=dtype, impl=impl)
 
 
-@pytest.mark.parametrize("dtype, impl", [(BF16, 0), (BF16, 1), (BF16, 2), (BF16, 3), (F32, 0)])
+@pytest.mark.parametrize("dtype, impl", [(BF16, 0), (BF16, 1), (BF16, 2), (BF16, 3), (F32, 0), (F32, 1)])
 def test_attention_large_logits_and_scale(fc, ctx, dtype, impl):
     # logits up to hundreds: one key takes nearly all the weight
     run_attention(fc, ctx, H_q=2, H_kv=1, d=64, lens=[40], n_cache=700, win=True, active=[0], sigma=4.0, dtype=dtype, impl=impl)

@@ -129,7 +129,7 @@ def attn(L, ctx, *, Q=P, K=P, V=P, O=P, dtype=b.BF16, cache=True, n_cache=100, o
 
 @pytest.mark.parametrize("kw, want", [
     (dict(dtype=2), UNSUPPORTED), (dict(d=80), UNSUPPORTED), (dict(H_q=3), INVALID), (dict(W=0), INVALID), (dict(W=65), UNSUPPORTED),
-    (dict(impl=-1), INVALID), (dict(impl=9), INVALID), (dict(impl=2, dtype=b.F32), UNSUPPORTED), (dict(impl=3, dtype=b.F32), UNSUPPORTED), (dict(scale=-1.0), INVALID), (dict(scale=float("nan")), INVALID),
+    (dict(impl=-1), INVALID), (dict(impl=9), INVALID), (dict(impl=2, dtype=b.F32), UNSUPPORTED), (dict(scale=-1.0), INVALID), (dict(scale=float("nan")), INVALID),
     (dict(off=(0, 5, 4)), INVALID), (dict(off=(-1, 5, 10)), INVALID), (dict(vis=(105, 111)), INVALID), (dict(vis=(-1, 110)), INVALID),
     (dict(n_cache=-1), INVALID), (dict(cache=None), INVALID), (dict(cache=store(rows=99)), INVALID), (dict(Q=None), INVALID),
     (dict(ids=None), INVALID), (dict(K=None), INVALID), (dict(Q=P + 8), MISALIGNED), (dict(q_hs=4), MISALIGNED), (dict(o_rs=64), INVALID),
