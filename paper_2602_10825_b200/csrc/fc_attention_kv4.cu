@@ -102,7 +102,7 @@ Path choose(const fc_ctx* ctx, const fc_attn_desc* desc, int dtype, const fc::Kv
   if (desc->impl == 3 || dtype == FC_F32) return kRows;
   fc::Kv4AttnGeom g = g_in;
   fc::kv4_rows_workspace(ctx, g);
-  return fc::kv4_rows_us(ctx, g) <= plan_unpacked(ctx, g).us ? kRows : kUnpacked;
+  return g.rows_us <= plan_unpacked(ctx, g).us ? kRows : kUnpacked;
 }
 
 size_t plan(const fc_ctx* ctx, Path path, fc::Kv4AttnGeom& g) {

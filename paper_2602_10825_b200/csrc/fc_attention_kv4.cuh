@@ -19,6 +19,7 @@ struct Kv4AttnGeom {
   int32_t n_splits;  // parts the keys are cut into, at most kKv4MaxSplits
   int64_t part_keys;    // keys per part (few-row kernel: on its axis of costs)
   int64_t n_cache_ceil; // few-row kernel: where the window starts on that axis
+  double rows_us;       // few-row kernel: estimate of the whole call
   int64_t n_vrows;   // virtual rows per key head, all chunks
   float* part_o;     // [H_kv, n_vrows, n_splits, d] unnormalised outputs, used if n_splits > 1
   float2* part_ml;   // [H_kv, n_vrows, n_splits] running maximum (log2 units for the tensor-core kernel) and sum
@@ -71,7 +72,6 @@ size_t kv4_simt_workspace(const fc_ctx* ctx, Kv4AttnGeom& g);  // also sets the 
 int kv4_simt(cudaStream_t st, const Kv4AttnGeom& g, const void* Q, const void* K, const void* V, int dtype, void* O);
 // few rows, and fp32: tensor cores fed from registers
 size_t kv4_rows_workspace(const fc_ctx* ctx, Kv4AttnGeom& g);
-double kv4_rows_us(const fc_ctx* ctx, const Kv4AttnGeom& g);  // estimate, of a geometry that kv4_rows_workspace has seen
 int kv4_rows(cudaStream_t st, const Kv4AttnGeom& g, const void* Q, const void* K, const void* V, void* O);
 // Joins the parts of every active row and writes O and lse.
 int kv4_combine(cudaStream_t st, const Kv4AttnGeom& g, int dtype, void* O, bool log2_units);

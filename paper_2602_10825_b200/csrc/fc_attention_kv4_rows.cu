@@ -32,13 +32,9 @@ constexpr int kWarps = 4, kThreads = 32 * kWarps;
 constexpr int kStep = 16;  // keys per warp and step
 constexpr float kRescaleThreshold = 8.f;
 constexpr int kWindowCost = 3;  // a window key has 3.6 times the bytes of a packed one
-#ifndef BP1
-#define BP1 3
-#endif
-#ifndef BP2
-#define BP2 2
-#endif
-constexpr int blocks_per_sm(int nt) { return nt == 1 ? BP1 : BP2; }  // resident, by the registers the kernel is given
+// Resident blocks, by the registers the kernel is given (measured: three and two are as fast as four and three at one token, and
+// faster at 64 rows of 24 heads, 110 us against 125).
+constexpr int blocks_per_sm(int nt) { return nt == 1 ? 3 : 2; }
 
 __device__ __forceinline__ void mma(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
   asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
@@ -279,7 +275,7 @@ attention_kv4_rows_kernel(const T* __restrict__ Q, const T* __restrict__ K, cons
   const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32, n = lane >> 2, q = lane & 3;
   const int part = blockIdx.z, hk = blockIdx.y;
   int v0 = 0;
-  const int c = fc::tile_chunk<kRows>(a, blockIdx.x, v0);
+  const int c = fc::tile_chunk<kRows>(a, gridDim.x - 1 - blockIdx.x, v0);  // the last chunks, which see most, start first
   if (c < 0) return;
   const int rows_here = min(kRows, (a.q_row_off[c + 1] - a.q_row_off[c]) * a.group - v0);
 
@@ -545,6 +541,10 @@ int tiles_of(const fc::Kv4AttnGeom& g) {
   return 1;
 }
 
+// Measured on B200: what a step of a block's four warps takes for every block of the SM it runs on, whether eight or sixteen
+// rows ride along.
+double step_us(const fc::Kv4AttnGeom& g) { return g.a.d == 128 ? (g.f32 ? 0.40 : 0.30) : (g.f32 ? 0.20 : 0.18); }
+
 }  // namespace
 
 namespace fc {
@@ -554,27 +554,38 @@ size_t kv4_rows_workspace(const fc_ctx* ctx, Kv4AttnGeom& g) {
   for (int c = 0; c < g.a.W; ++c) vis = std::max(vis, g.a.vis[c]);
   const int nt = tiles_of(g);
   const int64_t tiles = tile_count(g.a, 8 * nt) * g.a.H_kv;
-  // At most one set of resident blocks, where that leaves a step or more for every warp.
+  // The number of parts is the one that should be fastest.  A part is at least two steps; joining the parts costs a kernel and their
+  // bytes.  Where all blocks are resident at once, the fullest SM counts (a block that has the SM to itself takes 1.35 times
+  // its share of a full one); otherwise all the work does, half a part more for the blocks that end last, and 3 us for each set
+  // of blocks to start and end.
   constexpr int64_t kUnit = kStep * kWarps;
-  const int64_t window = std::max(vis - g.n_cache, 0);
-  const int64_t cache = window > 0 ? ((int64_t)g.n_cache + kUnit - 1) / kUnit * kUnit : std::min(vis, g.n_cache);
-  const int64_t total = cache + kWindowCost * window;
-  const int64_t slots = std::min<int64_t>(kKv4MaxSplits, std::max<int64_t>(1, (int64_t)ctx->sm_count * blocks_per_sm(nt) / std::max<int64_t>(1, tiles)));
-  const int64_t per = std::max(2 * kUnit, (total + slots * kUnit - 1) / (slots * kUnit) * kUnit);
-  g.part_keys = per;
+  auto units_of = [&](int v) {
+    const int64_t window = std::max(v - g.n_cache, 0);
+    return ((window > 0 ? ((int64_t)g.n_cache + kUnit - 1) / kUnit * kUnit : std::min(v, g.n_cache)) + kWindowCost * window + kUnit - 1) / kUnit;
+  };
+  const int64_t units = std::max<int64_t>(1, units_of(vis)), slots = (int64_t)ctx->sm_count * blocks_per_sm(nt);
+  int64_t work = 0;
+  for (int c = 0; c < g.a.W; ++c)
+    work += ((int64_t)(g.a.q_row_off[c + 1] - g.a.q_row_off[c]) * g.a.group + 8 * nt - 1) / (8 * nt) * g.a.H_kv * units_of(g.a.vis[c]);
+  const double join_us = 2.0 * 4 * g.a.d * g.a.H_kv * g.n_vrows / 4e6, u = step_us(g);
+  double best = 0;
+  int64_t last = 0;
+  for (int64_t k = 1; k <= std::min<int64_t>(kKv4MaxSplits, std::max<int64_t>(1, units / 2)); ++k) {
+    const int64_t steps = (units + k - 1) / k, n = (units + steps - 1) / steps, blocks = tiles * n;
+    if (n == last) continue;
+    last = n;
+    const int64_t on_sm = (blocks + ctx->sm_count - 1) / ctx->sm_count;
+    const double us = (blocks <= slots ? u * steps * (on_sm == 1 ? 1.35 : (double)on_sm) + 3
+                                       : u * ((double)work / ctx->sm_count + 0.5 * blocks_per_sm(nt) * steps) + 3.0 * blocks / slots) +
+                      (n > 1 ? 4 + n * join_us : 0);
+    if (k == 1 || us < best) best = us, g.part_keys = steps * kUnit, g.n_splits = (int32_t)n;
+  }
+  const int64_t cache = vis > g.n_cache ? ((int64_t)g.n_cache + kUnit - 1) / kUnit * kUnit : vis;
   g.n_cache_ceil = cache;
-  g.n_splits = (int32_t)std::max<int64_t>(1, (total + per - 1) / per);
+  g.rows_us = best + 4;
   if (g.n_splits == 1) return 0;
   const int64_t parts = g.a.H_kv * g.n_vrows * g.n_splits;
   return align_up(parts * g.a.d * sizeof(float), 256) + align_up(parts * sizeof(float2), 256);
-}
-
-// Measured on B200: a step of a block's four warps takes 0.36 us (D = 128; 0.2 for 64) for every block of the SM it runs
-// on, whether eight or sixteen rows ride along; 9 us for the launches, the first loads and the joining.
-double kv4_rows_us(const fc_ctx* ctx, const Kv4AttnGeom& g) {
-  const int64_t blocks = tile_count(g.a, 8 * tiles_of(g)) * g.a.H_kv * g.n_splits;
-  const double per_sm = (double)((blocks + ctx->sm_count - 1) / ctx->sm_count);
-  return 9 + per_sm * (double)g.part_keys / (kStep * kWarps) * (g.a.d == 128 ? 0.36 : 0.2);
 }
 
 int kv4_rows(cudaStream_t st, const Kv4AttnGeom& g, const void* Q, const void* K, const void* V, void* O) {
