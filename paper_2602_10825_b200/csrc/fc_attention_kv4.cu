@@ -93,22 +93,35 @@ UnpackedPlan plan_unpacked(const fc_ctx* ctx, const fc::Kv4AttnGeom& g) {
   return p;
 }
 
+// What a call does, with the workspace it takes and the split of the keys in g.
+//
 // Few rows read the packed keys in one pass but spend a tensor instruction on eight of them; many rows pay for unpacking once.  The
 // line between the two moves with the heads and the keys, so that the estimates are compared (measured at 24 heads of 128
-// over 28000 keys: 64 rows 112 us against 150, 128 rows 303 against 153).
-Path choose(const fc_ctx* ctx, const fc_attn_desc* desc, int dtype, const fc::Kv4AttnGeom& g_in) {
-  if (desc->impl == 1) return kSimt;
-  if (desc->impl == 2) return kUnpacked;
-  if (desc->impl == 3 || dtype == FC_F32) return kRows;
-  fc::Kv4AttnGeom g = g_in;
-  fc::kv4_rows_workspace(ctx, g);
-  return g.rows_us <= plan_unpacked(ctx, g).us ? kRows : kUnpacked;
-}
+// over 28000 keys: 64 rows 111 us against 151, 128 rows 212 against 154).
+struct Plan {
+  Path path;
+  UnpackedPlan unpacked;  // kUnpacked
+  size_t bytes;
+};
 
-size_t plan(const fc_ctx* ctx, Path path, fc::Kv4AttnGeom& g) {
-  if (path == kSimt) return fc::kv4_simt_workspace(ctx, g);
-  if (path == kRows) return fc::kv4_rows_workspace(ctx, g);
-  return plan_unpacked(ctx, g).bytes;
+Plan plan(const fc_ctx* ctx, const fc_attn_desc* desc, int dtype, fc::Kv4AttnGeom& g) {
+  Plan p = {};
+  if (desc->impl == 1) {
+    p.path = kSimt;
+    p.bytes = fc::kv4_simt_workspace(ctx, g);
+    return p;
+  }
+  if (desc->impl != 2) {
+    p.path = kRows;
+    p.bytes = fc::kv4_rows_workspace(ctx, g);
+    if (desc->impl == 3 || dtype == FC_F32) return p;
+  }
+  p.unpacked = plan_unpacked(ctx, g);
+  if (desc->impl == 2 || p.unpacked.us < g.rows_us) {
+    p.path = kUnpacked;
+    p.bytes = p.unpacked.bytes;
+  }
+  return p;
 }
 
 }  // namespace
@@ -118,7 +131,7 @@ extern "C" size_t fc_chunk_attention_kv4_workspace_bytes(const fc_ctx* ctx, cons
                                                          int n_cache) {
   fc::Kv4AttnGeom g = {};
   if (!ctx || check_geometry(desc, dtype, q_chunk_row_off, kv_visible_len, n_cache, g) != FC_OK) return 0;
-  return plan(ctx, choose(ctx, desc, dtype, g), g);
+  return plan(ctx, desc, dtype, g).bytes;
 }
 
 extern "C" int fc_chunk_attention_kv4(fc_ctx* ctx, void* stream, const fc_attn_desc* desc, const void* Q,
@@ -168,12 +181,12 @@ extern "C" int fc_chunk_attention_kv4(fc_ctx* ctx, void* stream, const fc_attn_d
   a.active_ids = active_ids; a.n_active = n_active; a.lse = lse; a.status = status;
   if (n_cache > 0) g.cache = fc::kv4_view(*cache);
 
-  const Path path = choose(ctx, desc, dtype, g);
-  const size_t need = plan(ctx, path, g);
+  Plan p = plan(ctx, desc, dtype, g);
+  const size_t need = p.bytes;
   if (need > 0) {
     if (!ws || ws_bytes < need) return FC_ERR_WORKSPACE;
     if (!fc::aligned16(ws)) return FC_ERR_MISALIGNED;
-    if (path != kUnpacked) {
+    if (p.path != kUnpacked) {
       const int64_t parts = a.H_kv * g.n_vrows * g.n_splits;
       g.part_o = (float*)ws;
       g.part_ml = (float2*)((char*)ws + fc::align_up(parts * a.d * sizeof(float), 256));
@@ -181,17 +194,17 @@ extern "C" int fc_chunk_attention_kv4(fc_ctx* ctx, void* stream, const fc_attn_d
   }
   FC_DEVICE_GUARD(ctx);
   cudaStream_t st = (cudaStream_t)stream;
-  if (path == kSimt) return fc::kv4_simt(st, g, Q, K, V, dtype, O);
-  if (path == kRows) return fc::kv4_rows(st, g, Q, K, V, O);
-  UnpackedPlan p = plan_unpacked(ctx, g);
+  if (p.path == kSimt) return fc::kv4_simt(st, g, Q, K, V, dtype, O);
+  if (p.path == kRows) return fc::kv4_rows(st, g, Q, K, V, O);
+  UnpackedPlan& u = p.unpacked;
   const int n0 = cache_rows(g);
   char* base = (char*)ws;
   const int64_t hs = (int64_t)n0 * a.d;
-  if (n0 > 0 && (rc = fc::kv4_unpack_launch(ctx, st, g.cache, a.H_kv, a.d, 0, n0, base + p.k, base + p.v, FC_BF16, hs, a.d, hs, a.d)) != FC_OK)
+  if (n0 > 0 && (rc = fc::kv4_unpack_launch(ctx, st, g.cache, a.H_kv, a.d, 0, n0, base + u.k, base + u.v, FC_BF16, hs, a.d, hs, a.d)) != FC_OK)
     return rc;
-  p.split.o = g.part_o = (float*)(base + p.o);
-  p.split.ml = g.part_ml = (float2*)(base + p.ml);
-  g.n_splits = p.split.n_splits;
-  if ((rc = fc::attention_tc_two(ctx, st, a, Q, base + p.k, base + p.v, n0, K, V, p.split, O, ws, ws_bytes)) != FC_OK) return rc;
-  return p.split.n_splits > 1 ? fc::kv4_combine(st, g, dtype, O, true) : FC_OK;
+  u.split.o = g.part_o = (float*)(base + u.o);
+  u.split.ml = g.part_ml = (float2*)(base + u.ml);
+  g.n_splits = u.split.n_splits;
+  if ((rc = fc::attention_tc_two(ctx, st, a, Q, base + u.k, base + u.v, n0, K, V, u.split, O, ws, ws_bytes)) != FC_OK) return rc;
+  return u.split.n_splits > 1 ? fc::kv4_combine(st, g, dtype, O, true) : FC_OK;
 }

@@ -55,7 +55,11 @@ __device__ __forceinline__ void parts_of(float a, float b, uint32_t (&p)[3]) {
     b -= __uint_as_float(__float_as_uint(b) & 0xffff0000u);
   }
 }
-template <typename T> constexpr int kParts = sizeof(T) == 4 ? 3 : 1;
+template <typename T> constexpr int kParts = sizeof(T) == 4 ? 3 : 1;  // of Q, and of a window's K and V
+// Of P.  bf16 rounds a weight by up to 2^-8, which is as much again as the output's own rounding: of up to eight rows, bound by
+// the unpacking, the rest of the weight is taken along (one token over 28080 keys: 32.5 us against 31.0, error 1.7e-3 against 2.4e-3);
+// of sixteen it would cost 20 to 25 %.
+template <typename T, int NT> constexpr int kWeightParts = sizeof(T) == 4 ? 3 : (NT == 1 ? 2 : 1);
 
 __device__ __forceinline__ uint32_t prmt(uint32_t a, uint32_t b, uint32_t sel) { return __byte_perm(a, b, sel); }
 
@@ -112,7 +116,8 @@ template <int D, int NT> struct State {
 // S^T -> P^T operands.  n_valid: keys of the step that exist (kTail only).
 template <typename T, int D, int NT, bool kTail>
 __device__ __forceinline__ void softmax_step(State<D, NT>& st, float (&s)[NT][4], float scale_log2, int lane, int n_valid,
-                                             uint32_t (&p0)[kParts<T>][NT], uint32_t (&p1)[kParts<T>][NT]) {
+                                             uint32_t (&p0)[kWeightParts<T, NT>][NT],
+                                             uint32_t (&p1)[kWeightParts<T, NT>][NT]) {
   bool move = false;
 #pragma unroll
   for (int t = 0; t < NT; ++t) {
@@ -154,8 +159,13 @@ __device__ __forceinline__ void softmax_step(State<D, NT>& st, float (&s)[NT][4]
     st.l[t][0] += e0 + e2;
     st.l[t][1] += e1 + e3;
     if constexpr (kParts<T> == 1) {
-      p0[0][t] = transpose8x8(cvt_bf16x2(e0, e1));
-      p1[0][t] = transpose8x8(cvt_bf16x2(e2, e3));
+      const uint32_t a = cvt_bf16x2(e0, e1), b = cvt_bf16x2(e2, e3);
+      p0[0][t] = transpose8x8(a);
+      p1[0][t] = transpose8x8(b);
+      if constexpr (kWeightParts<T, NT> == 2) {
+        p0[1][t] = transpose8x8(cvt_bf16x2(e0 - fc::bf16_lo(a), e1 - fc::bf16_hi(a)));
+        p1[1][t] = transpose8x8(cvt_bf16x2(e2 - fc::bf16_lo(b), e3 - fc::bf16_hi(b)));
+      }
     } else {
       uint32_t a[3], b[3];
       parts_of(e0, e1, a);
@@ -184,10 +194,11 @@ __device__ __forceinline__ void logits(float (&s)[NT][4], float (&rest)[NT][4], 
 }
 // O^T tile += V^T P^T, V as NV parts.
 template <typename T, int NT, int NV>
-__device__ __forceinline__ void weigh(float (&o)[4], const uint32_t (&v)[NV][4], const uint32_t (&p0)[kParts<T>][NT],
-                                      const uint32_t (&p1)[kParts<T>][NT], int t) {
+__device__ __forceinline__ void weigh(float (&o)[4], const uint32_t (&v)[NV][4], const uint32_t (&p0)[kWeightParts<T, NT>][NT],
+                                      const uint32_t (&p1)[kWeightParts<T, NT>][NT], int t) {
   if constexpr (kParts<T> == 1) {
-    mma(o, v[0][0], v[0][1], v[0][2], v[0][3], p0[0][t], p1[0][t]);
+#pragma unroll
+    for (int i = kWeightParts<T, NT> - 1; i >= 0; --i) mma(o, v[0][0], v[0][1], v[0][2], v[0][3], p0[i][t], p1[i][t]);
   } else {
     float x[4] = {};
 #pragma unroll
@@ -233,7 +244,7 @@ __device__ __forceinline__ void packed_step(State<D, NT>& st, const uint8_t* buf
 #pragma unroll
       for (int i = 0; i < 4; ++i) s[t][i] += rest[t][i];
   }
-  uint32_t v[4][D / 64], p0[kParts<T>][NT], p1[kParts<T>][NT];
+  uint32_t v[4][D / 64], p0[kWeightParts<T, NT>][NT], p1[kWeightParts<T, NT>][NT];
 #pragma unroll
   for (int i = 0; i < 4; ++i) lds_words(vc + ((i & 1) + 8 * (i >> 1)) * (D / 2), v[i]);
   const uint32_t sl = vs[0] | ((uint32_t)vs[D / 32] << 16), sh = vs[8 * (D / 32)] | ((uint32_t)vs[9 * (D / 32)] << 16);
@@ -438,7 +449,7 @@ attention_kv4_rows_kernel(const T* __restrict__ Q, const T* __restrict__ K, cons
       __syncwarp();
       if (Wn::kOne) copy_window(vw, a.v_rs, ring, kb, true);
       else copy_window(kw, a.k_rs, ring, kb + kAll, false);
-      uint32_t p0[kParts<T>][NT], p1[kParts<T>][NT];
+      uint32_t p0[kWeightParts<T, NT>][NT], p1[kWeightParts<T, NT>][NT];
       softmax_step<T, D, NT, true>(st, s, scale_log2, lane, w1 - kb, p0, p1);
       cp_async_wait<Wn::kOne ? 0 : 1>();
       __syncwarp();
@@ -573,6 +584,7 @@ size_t kv4_rows_workspace(const fc_ctx* ctx, Kv4AttnGeom& g) {
   for (int64_t k = 1; k <= std::min<int64_t>(kKv4MaxSplits, std::max<int64_t>(1, units / 2)); ++k) {
     const int64_t steps = (units + k - 1) / k, n = (units + steps - 1) / steps, blocks = tiles * n;
     if (n == last) continue;
+    if (k > 1 && blocks > 4 * slots) break;
     last = n;
     const int64_t on_sm = (blocks + ctx->sm_count - 1) / ctx->sm_count;
     const double us = (blocks <= slots ? u * steps * (on_sm == 1 ? 1.35 : (double)on_sm) + 3

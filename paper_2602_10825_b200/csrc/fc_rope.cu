@@ -231,8 +231,8 @@ qk_norm_rope_kernel(const T* Q, const T* K, T* Q_out, T* K_out, const float* __r
 }
 
 // f radians per position -> turns per position modulo one, times 2^64
-uint64_t turns_of(double f) {
-  long double t = (long double)f * 0.159154943091895335768883763372514362L;
+uint64_t turns_of(long double f) {
+  long double t = f * 0.159154943091895335768883763372514362L;
   if (!(t >= 0.0L && t < 1.0L)) t -= floorl(t);
   return t < 1.0L ? (uint64_t)(t * 0x1p64L) : 0;
 }
@@ -268,13 +268,11 @@ extern "C" int fc_qk_norm_rope(fc_ctx* ctx, void* stream, const fc_rope_desc* de
     int k = 0;
     for (int a = 0; a < 3; ++a) {
       const int half = desc->axis_dim[a] / 2;
-      const bool same = !inv_freq && a > 0 && desc->axis_dim[a] == desc->axis_dim[a - 1];  // height and width, as a rule
-      for (int i = 0; i < half; ++i, ++k) {
-        if (same) {
-          g.turns[k] = g.turns[k - half];
-          continue;
-        }
-        const double f = inv_freq ? inv_freq[k] : pow(desc->theta, -2.0 * i / desc->axis_dim[a]);
+      // theta^(-2i/n) as powers of one ratio: 64 bits of mantissa leave 58 after as many products
+      const long double ratio = inv_freq || half == 0 ? 0.0L : powl(desc->theta, -1.0L / half);
+      long double f = 1.0L;
+      for (int i = 0; i < half; ++i, ++k, f *= ratio) {
+        if (inv_freq) f = inv_freq[k];
         if (!std::isfinite(f)) return FC_ERR_INVALID_ARG;
         g.turns[k] = turns_of(f);
       }

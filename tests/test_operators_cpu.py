@@ -158,6 +158,17 @@ def test_attention_no_rows_and_workspace(L, ctx):
     assert attn(L, ctx, ws_bytes=need, **{**kw, "ws": P + 8}) == MISALIGNED
 
 
+def test_packed_descriptors_are_the_structures():
+    for fields, cls in ((b._ROPE_FIELDS, b._RopeDesc), (b._PACK_FIELDS, b._Kv4PackDesc), (b._UNPACK_FIELDS, b._Kv4UnpackDesc),
+                        (b._ATTN_FIELDS, b._AttnDesc)):
+        n = len(fields.unpack(bytes(fields.size)))
+        raw = fields.pack(*range(1, n + 1)).ljust(C.sizeof(cls), b"\0")
+        got = cls.from_buffer_copy(raw)
+        values = [getattr(got, name) for name, _ in cls._fields_]
+        flat = [x for v in values for x in (list(v) if hasattr(v, "__len__") else [v])]
+        assert flat == list(range(1, n + 1))
+
+
 # ------------------------------------------------------------------------------------ the plain forms themselves
 
 def test_plain_format_by_hand():
