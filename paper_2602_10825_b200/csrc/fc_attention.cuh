@@ -23,8 +23,11 @@ struct AttnGeom {
   uint32_t* status;
 };
 
-// Parts of the keys whose results another kernel joins (attention_tc_two only; n_splits 1: no parts).
+// attention_tc_two only: how the work is cut up.  Parts of the keys have their results joined by another kernel (n_splits 1: no
+// parts).
 struct AttnSplit {
+  int32_t pack = 1;     // query heads taken as rows of one tile: 1, or the group where it divides a tile's 128 rows
+  bool follows = false; // the stream's last kernel writes K0 / V0, clears the counter and lets this one start early
   int32_t n_splits = 1, part_keys = 0;  // part p: logical keys [p part_keys, (p + 1) part_keys), the last one to the end
   int64_t n_vrows = 0;
   float* o = nullptr;   // [H_kv, n_vrows, n_splits, d]: sums not divided by their weights
@@ -38,9 +41,11 @@ int attention_tc(fc_ctx* ctx, cudaStream_t st, const AttnGeom& g, const void* Q,
                  const void* V, void* O, void* ws, size_t ws_bytes);
 size_t attention_tc_workspace_bytes();
 // The same over two stores: logical tokens [0, n0) are the rows of K0 / V0 (dense [H_kv, n0, d]), the others are found
-// in K / V through the segment table, whose offsets count from n0.
+// in K / V through the segment table, whose offsets count from n0.  `before` is called once nothing but launches is left that
+// could fail; it launches the kernel that writes K0 / V0.
 int attention_tc_two(fc_ctx* ctx, cudaStream_t st, const AttnGeom& g, const void* Q, const void* K0, const void* V0, int n0,
-                     const void* K, const void* V, const AttnSplit& split, void* O, void* ws, size_t ws_bytes);
+                     const void* K, const void* V, const AttnSplit& split, void* O, void* ws, size_t ws_bytes,
+                     int (*before)(void*), void* arg);
 // warp-specialised kernel; tensor maps as built by attention_tc (tk0, tv0: those of the second store, or NULL),
 // `counter` = 4 bytes of workspace
 int attention_ws_launch(fc_ctx* ctx, cudaStream_t st, const AttnGeom& g, const CUtensorMap& tq,

@@ -57,16 +57,18 @@ struct UnpackedPlan {
 UnpackedPlan plan_unpacked(const fc_ctx* ctx, const fc::Kv4AttnGeom& g) {
   const fc::AttnGeom& a = g.a;
   UnpackedPlan p;
+  // grouped heads share their key tiles where whole groups fill a tile of 128 rows
+  if (128 % a.group == 0 && (int64_t)a.q_row_off[a.W] * a.group <= INT32_MAX) p.split.pack = a.group;
   int64_t pairs = 0;
   int vis = 0;
   for (int c = 0; c < a.W; ++c) {
-    pairs += (a.q_row_off[c + 1] - a.q_row_off[c] + 255) / 256;  // query rows of a work item
+    pairs += ((int64_t)(a.q_row_off[c + 1] - a.q_row_off[c]) * p.split.pack + 255) / 256;  // rows of a work item
     vis = std::max(vis, a.vis[c]);
   }
   // Work items are handed out one at a time to one block per SM, so that the time is (rounds) x (key tiles of an item); cutting
   // the keys fills the last round at the price of writing and reading the parts.  Measured: 1.8 us a key tile, the parts' bytes at
   // 4 TB/s and 5 us for the joining kernel.
-  const int64_t items = std::max<int64_t>(1, pairs * a.H_q);
+  const int64_t items = std::max<int64_t>(1, pairs * (a.H_q / p.split.pack));
   const int64_t tiles = (vis + 127) / 128;
   const double part_us = 2.0 * 4 * a.d * a.H_kv * g.n_vrows / 4e6;
   int64_t n = 1;
@@ -93,6 +95,12 @@ UnpackedPlan plan_unpacked(const fc_ctx* ctx, const fc::Kv4AttnGeom& g) {
   return p;
 }
 
+// Strides that a tensor map takes: not 0 where there is more than one head, below 2^40 bytes.  The few-row kernel takes any.
+bool maps_fit(const fc_attn_desc* d) {
+  auto fits = [](int heads, int64_t hs, int64_t rs) { return rs < (1ll << 38) && (heads == 1 || (hs > 0 && hs < (1ll << 31))); };
+  return fits(d->H_q, d->q_hs, d->q_rs) && fits(d->H_kv, d->k_hs, d->k_rs) && fits(d->H_kv, d->v_hs, d->v_rs);
+}
+
 // What a call does, with the workspace it takes and the split of the keys in g.
 //
 // Few rows read the packed keys in one pass but spend a tensor instruction on eight of them; many rows pay for unpacking once.  The
@@ -117,7 +125,7 @@ Plan plan(const fc_ctx* ctx, const fc_attn_desc* desc, int dtype, fc::Kv4AttnGeo
     if (desc->impl == 3 || dtype == FC_F32) return p;
   }
   p.unpacked = plan_unpacked(ctx, g);
-  if (desc->impl == 2 || p.unpacked.us < g.rows_us) {
+  if (desc->impl == 2 || (p.unpacked.us < g.rows_us && maps_fit(desc))) {
     p.path = kUnpacked;
     p.bytes = p.unpacked.bytes;
   }
@@ -199,12 +207,23 @@ extern "C" int fc_chunk_attention_kv4(fc_ctx* ctx, void* stream, const fc_attn_d
   UnpackedPlan& u = p.unpacked;
   const int n0 = cache_rows(g);
   char* base = (char*)ws;
-  const int64_t hs = (int64_t)n0 * a.d;
-  if (n0 > 0 && (rc = fc::kv4_unpack_launch(ctx, st, g.cache, a.H_kv, a.d, 0, n0, base + u.k, base + u.v, FC_BF16, hs, a.d, hs, a.d)) != FC_OK)
-    return rc;
+  struct Unpack {
+    cudaStream_t st;
+    const fc::Kv4AttnGeom* g;
+    int n0;
+    void *k, *v;
+    uint32_t* counter;
+  } unpack = {st, &g, n0, base + u.k, base + u.v, (uint32_t*)ws};
+  auto before = [](void* arg) -> int {
+    const Unpack& x = *(const Unpack*)arg;
+    const int64_t hs = (int64_t)x.n0 * x.g->a.d;
+    return fc::kv4_unpack_launch(x.st, x.g->cache, x.g->a.H_kv, x.g->a.d, 0, x.n0, x.k, x.v, FC_BF16, hs, x.g->a.d, hs, x.g->a.d, x.counter);
+  };
+  u.split.follows = n0 > 0;
   u.split.o = g.part_o = (float*)(base + u.o);
   u.split.ml = g.part_ml = (float2*)(base + u.ml);
   g.n_splits = u.split.n_splits;
-  if ((rc = fc::attention_tc_two(ctx, st, a, Q, base + u.k, base + u.v, n0, K, V, u.split, O, ws, ws_bytes)) != FC_OK) return rc;
+  if ((rc = fc::attention_tc_two(ctx, st, a, Q, base + u.k, base + u.v, n0, K, V, u.split, O, ws, ws_bytes, before, &unpack)) != FC_OK)
+    return rc;
   return u.split.n_splits > 1 ? fc::kv4_combine(st, g, dtype, O, true) : FC_OK;
 }

@@ -53,6 +53,27 @@ static int make_tmap_rows(fc_ctx* ctx, CUtensorMap* map, const void* base, int d
   return FC_OK;
 }
 
+// [groups of `pack` heads, rows, pack, d] view of a [heads, rows, d] bf16 tensor, box = 64 elements x pack heads x 128 / pack rows: a
+// tile of 128 rows in which the heads of a row follow one another.
+static int make_tmap_heads(fc_ctx* ctx, CUtensorMap* map, const void* base, int d, int pack, int64_t rows, int groups,
+                           int64_t head_stride, int64_t row_stride) {
+  const cuuint64_t dims[4] = {(cuuint64_t)d, (cuuint64_t)pack, (cuuint64_t)rows, (cuuint64_t)groups};
+  // the stride of an axis of one entry is never used, but has to be a valid one
+  const int64_t hs = pack * groups > 1 ? head_stride : row_stride;
+  const cuuint64_t strides[3] = {(cuuint64_t)hs * 2, (cuuint64_t)row_stride * 2, (cuuint64_t)(pack * hs) * 2};
+  const cuuint32_t box[4] = {64, (cuuint32_t)pack, (cuuint32_t)(kBM / pack), 1};
+  const cuuint32_t estr[4] = {1, 1, 1, 1};
+  CUresult r = ((EncodeTiledFn)ctx->encode_tiled)(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(base), dims,
+                                                  strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                                                  CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                                                  CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  if (r != CUDA_SUCCESS) {
+    fc::set_cuda_error(cudaErrorInvalidValue, "cuTensorMapEncodeTiled");
+    return FC_ERR_CUDA;
+  }
+  return FC_OK;
+}
+
 size_t attention_tc_workspace_bytes() { return 256; }
 
 bool attention_tc_supported(const AttnGeom& g, int dtype) {
@@ -118,7 +139,8 @@ int attention_tc(fc_ctx* ctx, cudaStream_t st, const AttnGeom& g_in, const void*
 }
 
 int attention_tc_two(fc_ctx* ctx, cudaStream_t st, const AttnGeom& g_in, const void* Q, const void* K0, const void* V0, int n0,
-                     const void* K, const void* V, const AttnSplit& split, void* O, void* ws, size_t ws_bytes) {
+                     const void* K, const void* V, const AttnSplit& split, void* O, void* ws, size_t ws_bytes,
+                     int (*before)(void*), void* arg) {
   if (!ws || ws_bytes < attention_tc_workspace_bytes()) return FC_ERR_WORKSPACE;
   if (!aligned16(ws)) return FC_ERR_MISALIGNED;
   AttnGeom g = g_in;
@@ -134,7 +156,7 @@ int attention_tc_two(fc_ctx* ctx, cudaStream_t st, const AttnGeom& g_in, const v
   if (q_rows == 0) return FC_OK;
   CUtensorMap tq, tk0, tv0, tk, tv;
   int rc;
-  if ((rc = make_tmap(ctx, &tq, Q, g.d, q_rows, g.H_q, g.q_rs, g.H_q > 1 ? g.q_hs : g.q_rs * q_rows)) != FC_OK) return rc;
+  if ((rc = make_tmap_heads(ctx, &tq, Q, g.d, split.pack, q_rows, g.H_q / split.pack, g.q_hs, g.q_rs)) != FC_OK) return rc;
   if (n0 > 0) {
     if ((rc = make_tmap(ctx, &tk0, K0, g.d, n0, g.H_kv, g.d, (int64_t)n0 * g.d)) != FC_OK) return rc;
     if ((rc = make_tmap(ctx, &tv0, V0, g.d, n0, g.H_kv, g.d, (int64_t)n0 * g.d)) != FC_OK) return rc;
@@ -147,6 +169,7 @@ int attention_tc_two(fc_ctx* ctx, cudaStream_t st, const AttnGeom& g_in, const v
     tv = n0 > 0 ? tv0 : tq;
   }
   if (n0 == 0) tk0 = tk, tv0 = tv;
+  if ((rc = before(arg)) != FC_OK) return rc;
   return attention_ws_launch(ctx, st, g, tq, tk, tv, &tk0, &tv0, split, O, (uint32_t*)ws);
 }
 

@@ -44,6 +44,8 @@
 // overwritten with zeros in shared memory by warp 11 before the PV instructions of that tile are issued, so that not
 // even a NaN or an infinity in such a row can reach an output (0 x inf would).
 // Every mbarrier wait is bounded (see mbar_wait_bounded); tensor memory is always released.
+#include <algorithm>
+#include <climits>
 #include <cmath>
 
 #include "fc_attention.cuh"
@@ -152,6 +154,9 @@ attention_ws_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
                     const __grid_constant__ CUtensorMap tmap_v0, const __grid_constant__ fc::AttnGeom g,
                     const __grid_constant__ fc::AttnSplit split, __nv_bfloat16* __restrict__ O, uint32_t* __restrict__ counter) {
   constexpr bool kGather = kSource == kGatherMap, kTwo = kSource == kTwoStores;
+  // kTwoStores takes the `pack` query heads of a key head as rows of the same tile (row v of a head group is head v % pack,
+  // query row v / pack), so that a key tile is read once for all of them; "head" below is the group then.
+  const int pk = kTwo ? split.pack : 1, n_heads = g.H_q / pk;
   constexpr uint32_t kTileBytes = kBM * D * 2;
   constexpr int kAtoms = D / 64;
   constexpr uint32_t kAtomBytes = kBM * 128;
@@ -213,7 +218,7 @@ attention_ws_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
     int items = 0;
     for (int a = 0; a < n; ++a) {
       const int c = sh->act_chunk[a];
-      items += (kTwo ? split.n_splits : 1) * g.H_q * ((g.q_row_off[c + 1] - g.q_row_off[c] + 2 * kBM - 1) / (2 * kBM));
+      items += (kTwo ? split.n_splits : 1) * n_heads * (((g.q_row_off[c + 1] - g.q_row_off[c]) * pk + 2 * kBM - 1) / (2 * kBM));
       sh->act_item_end[a] = items;
     }
     sh->n_act = n;
@@ -235,20 +240,20 @@ attention_ws_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
     int a = 0;
     while (a + 1 < n_act && item >= sh->act_item_end[a]) ++a;
     const int start = a > 0 ? sh->act_item_end[a - 1] : 0;
-    const int pairs = (sh->act_item_end[a] - start) / (kTwo ? split.n_splits * g.H_q : g.H_q);
+    const int pairs = (sh->act_item_end[a] - start) / (kTwo ? split.n_splits * n_heads : n_heads);
     it.c = sh->act_chunk[a];
     it.h = (item - start) / pairs;
-    it.row0 = g.q_row_off[it.c] + ((item - start) % pairs) * 2 * kBM;
+    it.row0 = g.q_row_off[it.c] * pk + ((item - start) % pairs) * 2 * kBM;
     it.n_vis = g.vis[it.c];
     it.k_lo = it.part = 0;
     if constexpr (kTwo) {  // the parts of all heads one after the other
-      it.part = it.h / g.H_q;
-      it.h %= g.H_q;
+      it.part = it.h / n_heads;
+      it.h %= n_heads;
       it.k_lo = it.part * split.part_keys;
       if (it.part + 1 < split.n_splits) it.n_vis = min(it.n_vis, it.k_lo + split.part_keys);
     }
-    it.hk = it.h / g.group;
-    it.b_valid = it.row0 + kBM < g.q_row_off[it.c + 1];
+    it.hk = pk > 1 ? it.h : it.h / g.group;
+    it.b_valid = it.row0 + kBM < g.q_row_off[it.c + 1] * pk;
     return it;
   };
   // consumer side of the item ring; -1 once the list is exhausted or the CTA has given up
@@ -289,7 +294,12 @@ attention_ws_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
     // ------------------------------------------------------------------ scheduler + TMA producer
     uint32_t kv = 0, it_n = 0;
     int next = 0;
-    if (lane == 0) next = (int)atomicAdd(counter, 1u);
+    // kTwoStores: the kernel before writes the first store and clears the counter.  Blocks that start while it still runs
+    // elsewhere are ahead of the others; so the first item of a block is its own, and only the others come off the counter.
+    if constexpr (kTwo) fc::pdl_wait();
+    auto take = [&]() { return kTwo ? (int)(gridDim.x + atomicAdd(counter, 1u)) : (int)atomicAdd(counter, 1u); };
+    if (kTwo) next = blockIdx.x;
+    else if (lane == 0) next = take();
     while (true) {
       int item = __shfl_sync(0xffffffffu, next, 0);
       if (item >= total_items) item = -1;
@@ -300,15 +310,17 @@ attention_ws_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
         mbar_arrive(smem_u32(&sh->it_full[slot]));
       }
       if (item < 0 || *abort) break;
-      if (lane == 0) next = (int)atomicAdd(counter, 1u);  // in flight while this item's tiles are loaded
+      if (lane == 0) next = take();  // in flight while this item's tiles are loaded
       const Item it = decode(item);
       warp_wait(smem_u32(&sh->q_empty), (it_n & 1) ^ 1, abort);
       if (lane == 0) {
         mbar_expect_tx(smem_u32(&sh->q_full), 2 * kTileBytes);
         for (int t = 0; t < 2; ++t)
-          for (int x = 0; x < kAtoms; ++x)
-            tma_load_3d(q_s + t * kTileBytes + x * kAtomBytes, &tmap_q, smem_u32(&sh->q_full), x * 64,
-                        it.row0 + t * kBM, it.h);
+          for (int x = 0; x < kAtoms; ++x) {
+            const uint32_t dst = q_s + t * kTileBytes + x * kAtomBytes;
+            if constexpr (kTwo) tma_load_4d(dst, &tmap_q, smem_u32(&sh->q_full), x * 64, 0, (it.row0 + t * kBM) / pk, it.h);
+            else tma_load_3d(dst, &tmap_q, smem_u32(&sh->q_full), x * 64, it.row0 + t * kBM, it.h);
+          }
       }
       if constexpr (kGather) {
         // One logical segment [0, n_vis) whose token j of head hk lives in physical row tok[j].  Lane L brings rows
@@ -656,12 +668,12 @@ attention_ws_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
       warp_wait(smem_u32(&sh->o_done[x]), items & 1, abort);
       ++items;
       tc_fence_after();
-      const int row = it.row0 + x * kBM + r_in;
-      const bool row_ok = row < g.q_row_off[it.c + 1] &&
-                          fc::bounds_ok(row >= 0 && row < g.q_row_off[g.W] && it.h >= 0 && it.h < g.H_q, g.status);
+      const int v = it.row0 + x * kBM + r_in, row = v / pk, head = pk > 1 ? it.h * pk + v % pk : it.h;
+      const bool row_ok = v < g.q_row_off[it.c + 1] * pk &&
+                          fc::bounds_ok(row >= 0 && row < g.q_row_off[g.W] && head >= 0 && head < g.H_q, g.status);
       if constexpr (kTwo) {
         if (split.n_splits > 1) {  // this part's sum, not divided by its weights; kv4_combine joins the parts
-          const int64_t vr = (int64_t)(row - g.q_row_off[0]) * g.group + it.h % g.group;
+          const int64_t vr = (int64_t)(row - g.q_row_off[0]) * g.group + head % g.group;
           const int64_t at = (it.hk * split.n_vrows + vr) * split.n_splits + it.part;
 #pragma unroll
           for (int q4 = 0; q4 < D / 32; ++q4) {
@@ -684,7 +696,7 @@ attention_ws_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
         }
       }
       const float inv = l > 0.f ? 1.f / l : 0.f;
-      __nv_bfloat16* out = O + (int64_t)it.h * g.o_hs + (int64_t)row * g.o_rs;
+      __nv_bfloat16* out = O + (int64_t)head * g.o_hs + (int64_t)row * g.o_rs;
 #pragma unroll
       for (int q4 = 0; q4 < D / 32; ++q4) {
         uint32_t r[32];
@@ -707,7 +719,7 @@ attention_ws_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
         }
       }
       if (g.lse && row_ok)
-        g.lse[(int64_t)it.h * g.lse_hs + row] = l > 0.f ? (m + log2f(l)) * 0.6931471805599453f : -INFINITY;
+        g.lse[(int64_t)head * g.lse_hs + row] = l > 0.f ? (m + log2f(l)) * 0.6931471805599453f : -INFINITY;
       tc_fence_before();  // O_x has been read before this warp's next p_ready arrival lets PV_x overwrite it
     }
   }
@@ -730,18 +742,24 @@ namespace fc {
 int attention_ws_launch(fc_ctx* ctx, cudaStream_t st, const AttnGeom& g, const CUtensorMap& tq,
                         const CUtensorMap& tk, const CUtensorMap& tv, const CUtensorMap* tk0, const CUtensorMap* tv0,
                         const AttnSplit& split, void* O, uint32_t* counter) {
-  int max_items = 0;
-  for (int c = 0; c < g.W; ++c) max_items += (g.q_row_off[c + 1] - g.q_row_off[c] + 2 * kBM - 1) / (2 * kBM);
-  const int64_t items = (int64_t)max_items * g.H_q * (tk0 ? split.n_splits : 1);
+  const int pk = tk0 ? split.pack : 1;
+  int64_t max_items = 0;
+  for (int c = 0; c < g.W; ++c) max_items += ((int64_t)(g.q_row_off[c + 1] - g.q_row_off[c]) * pk + 2 * kBM - 1) / (2 * kBM);
+  const int64_t items = max_items * (g.H_q / pk) * (tk0 ? split.n_splits : 1);
   if (items == 0) return FC_OK;
-  FC_CUDA_CHECK(cudaMemsetAsync(counter, 0, sizeof(uint32_t), st));
+  if (items > INT32_MAX) return FC_ERR_UNSUPPORTED;
+  if (!split.follows) FC_CUDA_CHECK(cudaMemsetAsync(counter, 0, sizeof(uint32_t), st));
   const int grid = (int)std::min<int64_t>(items, (int64_t)ctx->sm_count);
   // at least half of the shared memory, so that a second CTA (and its 512 columns) never joins the SM
   const size_t need = (2 + 2 * kStages) * (size_t)kBM * g.d * 2 + sizeof(WsSmem) + 1024;
   const size_t smem = std::max<size_t>(need, 120 * 1024);
   auto launch = [&](auto kernel) -> int {
     FC_CUDA_CHECK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
-    kernel<<<grid, kThreads, smem, st>>>(tq, tk, tv, tk0 ? *tk0 : tk, tv0 ? *tv0 : tv, g, split, (__nv_bfloat16*)O, counter);
+    if (split.follows)  // its setup overlaps the kernel before, which cleared the counter
+      FC_CUDA_CHECK(launch_pdl(kernel, dim3(grid), dim3(kThreads), smem, st, tq, tk, tv, tk0 ? *tk0 : tk, tv0 ? *tv0 : tv, g, split,
+                               (__nv_bfloat16*)O, counter));
+    else
+      kernel<<<grid, kThreads, smem, st>>>(tq, tk, tv, tk0 ? *tk0 : tk, tv0 ? *tv0 : tv, g, split, (__nv_bfloat16*)O, counter);
     return FC_OK;
   };
   int rc;

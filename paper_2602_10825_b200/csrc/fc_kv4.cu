@@ -235,6 +235,7 @@ struct UnpackGeom {
   int32_t n;
   int64_t row0, k_hs, k_rs, v_hs, v_rs;
   fc::Kv4View src;
+  uint32_t* clear;
 };
 
 __device__ __forceinline__ void store8(__nv_bfloat16* p, const uint32_t (&v)[4]) {
@@ -249,8 +250,10 @@ template <typename T, int D>
 __global__ void __launch_bounds__(kThreads)
 kv4_unpack_kernel(T* __restrict__ K, T* __restrict__ V, const __grid_constant__ UnpackGeom g) {
   constexpr int W = D / 8, R = kThreads / W;
+  fc::pdl_launch_dependents();
   const int w = threadIdx.x % W, h = blockIdx.y;
   const bool is_v = blockIdx.z != 0;
+  if (g.clear && threadIdx.x == 0 && blockIdx.x == 0 && h == 0 && !is_v) *g.clear = 0;
   T* dst = is_v ? V : K;
   if (!dst) return;
   const uint8_t* codes = is_v ? g.src.v_codes : g.src.k_codes;
@@ -288,11 +291,10 @@ int check_rows(const void* p, int d, int es, int64_t hs, int64_t rs) {
 
 namespace fc {
 
-int kv4_unpack_launch(fc_ctx* ctx, cudaStream_t st, const Kv4View& src, int H, int d, int64_t row0, int n, void* K_dst, void* V_dst,
-                      int dtype, int64_t k_hs, int64_t k_rs, int64_t v_hs, int64_t v_rs) {
-  (void)ctx;
+int kv4_unpack_launch(cudaStream_t st, const Kv4View& src, int H, int d, int64_t row0, int n, void* K_dst, void* V_dst, int dtype,
+                      int64_t k_hs, int64_t k_rs, int64_t v_hs, int64_t v_rs, uint32_t* clear) {
   if (n == 0 || (!K_dst && !V_dst)) return FC_OK;
-  UnpackGeom g = {n, row0, k_hs, k_rs, v_hs, v_rs, src};
+  UnpackGeom g = {n, row0, k_hs, k_rs, v_hs, v_rs, src, clear};
   const int rows = kRowsPerThread * kThreads / (d / 8);
   const dim3 grid((unsigned)((n + rows - 1) / rows), (unsigned)H, 2);
 #define FC_UNPACK(T, D) kv4_unpack_kernel<T, D><<<grid, kThreads, 0, st>>>((T*)K_dst, (T*)V_dst, g)
@@ -367,6 +369,6 @@ extern "C" int fc_kv4_unpack(fc_ctx* ctx, void* stream, const fc_kv4_unpack_desc
   if (K_dst && (rc = check_rows(K_dst, desc->d, es, desc->k_hs, desc->k_rs)) != FC_OK) return rc;
   if (V_dst && (rc = check_rows(V_dst, desc->d, es, desc->v_hs, desc->v_rs)) != FC_OK) return rc;
   FC_DEVICE_GUARD(ctx);
-  return fc::kv4_unpack_launch(ctx, (cudaStream_t)stream, fc::kv4_view(*src), desc->H, desc->d, desc->src_row, desc->n, K_dst,
-                               V_dst, dtype, desc->k_hs, desc->k_rs, desc->v_hs, desc->v_rs);
+  return fc::kv4_unpack_launch((cudaStream_t)stream, fc::kv4_view(*src), desc->H, desc->d, desc->src_row, desc->n, K_dst,
+                               V_dst, dtype, desc->k_hs, desc->k_rs, desc->v_hs, desc->v_rs, nullptr);
 }

@@ -68,8 +68,9 @@ __device__ __forceinline__ void kv4_word(uint32_t w, uint32_t s2, uint32_t b2, u
   out[3] = hfma2_bf16(kv4_pair16<3>(w), s2, b2);
 }
 
-// Unpacks rows [row0, row0 + n) of K and V into [H, n, d] tensors (fc_kv4.cu); either destination may be NULL.
-int kv4_unpack_launch(fc_ctx* ctx, cudaStream_t st, const Kv4View& src, int H, int d, int64_t row0, int n, void* K_dst, void* V_dst,
-                      int dtype, int64_t k_hs, int64_t k_rs, int64_t v_hs, int64_t v_rs);
+// Unpacks rows [row0, row0 + n) of K and V into [H, n, d] tensors (fc_kv4.cu); either destination may be NULL.  `clear`: a word that
+// is set to zero on the way, or NULL.  A kernel launched by launch_pdl behind it may start early.
+int kv4_unpack_launch(cudaStream_t st, const Kv4View& src, int H, int d, int64_t row0, int n, void* K_dst, void* V_dst, int dtype,
+                      int64_t k_hs, int64_t k_rs, int64_t v_hs, int64_t v_rs, uint32_t* clear);
 
 }  // namespace fc

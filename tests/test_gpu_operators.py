@@ -365,6 +365,9 @@ CASES = [
     dict(H_q=2, H_kv=2, lens=[300, 31, 200], n_cache=1000, win=True, active=[0, 2]),
     dict(H_q=2, H_kv=2, lens=[64, 64], n_cache=0, win=True, active=[0, 1]),
     dict(H_q=2, H_kv=2, lens=[20, 20, 20], n_cache=100, win=True, active=[]),
+    dict(H_q=8, H_kv=2, lens=[97, 130, 33], n_cache=1500, win=True, active=[0, 2]),
+    dict(H_q=6, H_kv=2, lens=[150, 10], n_cache=900, win=True, active=[0, 1]),
+    dict(H_q=16, H_kv=1, lens=[70], n_cache=2000, win=False, active=[0]),
 ]
 
 
