@@ -78,8 +78,8 @@ UnpackedPlan plan_unpacked(const fc_ctx* ctx, const fc::Kv4AttnGeom& g) {
     const double us = 1.8 * rounds * ((tiles + k - 1) / k) + (k > 1 ? 5 + k * part_us : 0);
     if (k == 1 || us < best) best = us, n = k;
   }
-  // 20 us for the launches of the path, the unpacking at 6 TB/s
-  p.us = 20 + best + 2.0 * a.H_kv * cache_rows(g) * a.d * 2.56 / 6e6;
+  // 8 us for the launches of the path, the unpacking at 6 TB/s
+  p.us = 8 + best + 2.0 * a.H_kv * cache_rows(g) * a.d * 2.56 / 6e6;
   if (n > 1) {
     p.split.part_keys = (int32_t)((tiles + n - 1) / n * 128);
     p.split.n_splits = (int32_t)((vis + p.split.part_keys - 1) / p.split.part_keys);
@@ -98,14 +98,15 @@ UnpackedPlan plan_unpacked(const fc_ctx* ctx, const fc::Kv4AttnGeom& g) {
 // Strides that a tensor map takes: not 0 where there is more than one head, below 2^40 bytes.  The few-row kernel takes any.
 bool maps_fit(const fc_attn_desc* d) {
   auto fits = [](int heads, int64_t hs, int64_t rs) { return rs < (1ll << 38) && (heads == 1 || (hs > 0 && hs < (1ll << 31))); };
-  return fits(d->H_q, d->q_hs, d->q_rs) && fits(d->H_kv, d->k_hs, d->k_rs) && fits(d->H_kv, d->v_hs, d->v_rs);
+  const bool window = d->kv_rows > 0;
+  return fits(d->H_q, d->q_hs, d->q_rs) && (!window || (fits(d->H_kv, d->k_hs, d->k_rs) && fits(d->H_kv, d->v_hs, d->v_rs)));
 }
 
 // What a call does, with the workspace it takes and the split of the keys in g.
 //
 // Few rows read the packed keys in one pass but spend a tensor instruction on eight of them; many rows pay for unpacking once.  The
 // line between the two moves with the heads and the keys, so that the estimates are compared (measured at 24 heads of 128
-// over 28000 keys: 64 rows 111 us against 151, 128 rows 212 against 154).
+// over 28000 keys: 64 rows 111 us against 147, 128 rows 212 against 150).
 struct Plan {
   Path path;
   UnpackedPlan unpacked;  // kUnpacked
@@ -189,6 +190,7 @@ extern "C" int fc_chunk_attention_kv4(fc_ctx* ctx, void* stream, const fc_attn_d
   a.active_ids = active_ids; a.n_active = n_active; a.lse = lse; a.status = status;
   if (n_cache > 0) g.cache = fc::kv4_view(*cache);
 
+  if (desc->impl == 2 && !maps_fit(desc)) return FC_ERR_UNSUPPORTED;
   Plan p = plan(ctx, desc, dtype, g);
   const size_t need = p.bytes;
   if (need > 0) {

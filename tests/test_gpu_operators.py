@@ -387,6 +387,26 @@ def test_attention_visible_lengths(fc, ctx, dtype, impl):
     run_attention(fc, ctx, H_q=2, H_kv=2, d=64, lens=[2, 2], n_cache=9000, win=False, active=[0, 1], cut=[3, 9000], dtype=dtype, impl=impl)
 
 
+@pytest.mark.parametrize("rows", [3, 700])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_attention_strides_and_broadcast_heads(fc, ctx, dtype, rows):
+    # tokens before heads, a slice of a wider row; and one q, one window for all heads (head stride 0), however many the rows
+    H, d, n_cache = 4, 64, 300
+    cache, Kc, Vc = packed_store(fc, ctx, H, n_cache, d, 3)
+    wide = rand((rows, 3 * H, d), 5, 1.0, dtype).transpose(0, 1)
+    out = torch.zeros((rows, 2, H, d), dtype=dtype, device="cuda")
+    flat = rand((rows, d), 6, 1.0, dtype)
+    for Q, K, V in ((wide[:H], wide[H:2 * H], wide[2 * H:]), (flat.expand(H, rows, d), flat.expand(H, rows, d), wide[2 * H:])):
+        O = out[:, 1].transpose(0, 1)
+        ctx.chunk_attention_kv4(Q, cache, K, V, [0, rows], [n_cache + rows], i32([0]), i32([1]), O)
+        want = pf.attention(f64(Q), np.concatenate([Kc, f64(K)], 1), np.concatenate([Vc, f64(V)], 1), [0, rows], [n_cache + rows], [0])
+        check_attention(O, None, *want, dtype, dtype == BF16, n_cache + rows, d)
+    assert (out[:, 0] == 0).all()
+    if dtype == BF16:
+        with pytest.raises(fc.FcError, match="unsupported"):
+            ctx.chunk_attention_kv4(flat.expand(H, rows, d), cache, None, None, [0, rows], [n_cache], i32([0]), i32([1]), O, impl=2)
+
+
 @pytest.mark.parametrize("dtype, impl", [(BF16, 0), (BF16, 1), (BF16, 2), (BF16, 3), (F32, 0), (F32, 1)])
 def test_attention_large_logits_and_scale(fc, ctx, dtype, impl):
     # logits up to hundreds: one key takes nearly all the weight
