@@ -1,6 +1,7 @@
 // fc_qk_norm_rope: RMS norm of every head of queries and keys, and the rotation over (time, height, width), in one pass.
 //
-// Bound by HBM: every element is read and written once.  A head's row is spread over 16-byte pieces, one per lane (16 lanes for a
+// Bound by HBM: every element is read and written once (4680 tokens of 48 bf16 heads of 128 in 25 us with the launch, 4.6 TB/s; a
+// plain copy of the same bytes takes 21).  A head's row is spread over 16-byte pieces, one per lane (16 lanes for a
 // bf16 row of 128), and everything between the load and the store is in registers.  A group of lanes owns a token and walks
 // over some of its heads, four rows' loads in flight.  What it takes to stay under the copy rate is few instructions:
 //   - The cosines and sines of a token serve all its heads.  A block computes them once for its tokens, a pair a thread, and
@@ -94,18 +95,35 @@ __device__ __forceinline__ void place(const RopeGeom& g, int e, int& pair, int& 
 }
 
 template <typename T, int D, bool kHalves>
-__global__ void __launch_bounds__(kThreads, 4)
+__global__ void __launch_bounds__(kThreads, kHalves && sizeof(T) == 2 ? 3 : 4)  // 80 registers where eight partners are looked up, else 64
 qk_norm_rope_kernel(const T* Q, const T* K, T* Q_out, T* K_out, const float* __restrict__ q_weight,
                     const float* __restrict__ k_weight, const int32_t* __restrict__ pos, const __grid_constant__ RopeGeom g) {
   using P = Piece<T>;
-  // Heads whose loads are in flight together (measured: a chunk of 4680 tokens of 48 bf16 heads takes 27.4 us with four, 28.5
-  // with three and 30 and more with two or with the next loads sent before the arithmetic; fp32 22.8 us with three, 24.8 with four).
+  // Heads whose loads are in flight together.  Measured at a chunk of 4680 tokens of 48 bf16 heads: 27.4 us with four, 28.5 with
+  // three, 30 and more with two or with the next rows sent for before the arithmetic; fp32, 18719 tokens of 8 heads of 64:
+  // 22.8 us with three, 24.8 with four.  Sending for the first rows before the angles brought these to 25.0 and 20.8.
   constexpr int kUnroll = sizeof(T) == 4 ? 3 : 4;
   constexpr int E = P::N, L = D / E, G = kThreads / L, V = E / 4;  // elements per lane, lanes per row, rows per block, pairs of pairs
   __shared__ float2 cs_s[G * (D / 2)];                     // (cos, sin) of the block's tokens and pairs
   __shared__ T row_s[kHalves ? kUnroll * kThreads * E : 1];  // the rows in flight, where partners sit in other lanes
   const int tid = threadIdx.x, lane = tid % L, grp = tid / L;
   const int first_token = blockIdx.x * g.tokens;
+
+  const int t = grp % g.tokens, n = first_token + t;
+  const int h0 = (blockIdx.y * (G / g.tokens) + grp / g.tokens) * g.heads_per_group;
+  const int h1 = min(h0 + g.heads_per_group, g.H_q + g.H_kv);
+  const bool idle = n >= g.T || h0 >= h1;
+  // the first rows are sent for before the angles are worked out
+  uint4 raw[kUnroll];
+  if (!idle) {
+    const bool q = h0 < g.H_q;
+    const T* in = (q ? Q + (int64_t)n * g.q_rs + h0 * g.q_hs : K + (int64_t)n * g.k_rs + (h0 - g.H_q) * g.k_hs) + lane * E;
+    const int rows = (q ? min(h1, g.H_q) : h1) - h0;
+    const int64_t hs = q ? g.q_hs : g.k_hs;
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u)
+      if (u < rows) raw[u] = *reinterpret_cast<const uint4*>(in + u * hs);
+  }
 
   const int pairs = (g.axis_dim[0] + g.axis_dim[1] + g.axis_dim[2]) / 2;
   for (int x = tid; x < g.tokens * (D / 2); x += kThreads) {
@@ -129,36 +147,28 @@ qk_norm_rope_kernel(const T* Q, const T* K, T* Q_out, T* K_out, const float* __r
   }
   __syncthreads();
 
-  const int t = grp % g.tokens, n = first_token + t;
-  const int h0 = (blockIdx.y * (G / g.tokens) + grp / g.tokens) * g.heads_per_group;
-  const int h1 = min(h0 + g.heads_per_group, g.H_q + g.H_kv);
-  if (n >= g.T || h0 >= h1) return;
+  if (idle) return;
   const unsigned mask = L == 32 ? 0xffffffffu : ((1u << L) - 1u) << (tid & 31 & ~(L - 1));
 
-  int partner[E], pair[E];  // FC_ROPE_HALVES only
-  uint32_t second = 0;      // the elements that are second in their pair
-  if (kHalves) {
-#pragma unroll
-    for (int i = 0; i < E; ++i) {
-      bool first;
-      place(g, lane * E + i, pair[i], partner[i], first);
-      second |= first ? 0u : 1u << i;
-    }
-  }
-
-  auto walk = [&](const T* src, T* dst, int64_t hs, int64_t rs, int64_t ohs, int64_t ors, const float* weight, int a, int b) {
+  auto walk = [&](const T* src, T* dst, int64_t hs, int64_t rs, int64_t ohs, int64_t ors, const float* weight, int a, int b, bool loaded) {
     // out[i] = x[i] c[i] + x[partner] s[i], with the weights of the elements it takes
     uint64_t ce[V], co[V], se[V], so[V];
+    int partner[kHalves ? E : 1];  // where an element's partner lies in the rows of row_s
 #pragma unroll
     for (int v = 0; v < V; ++v) {
       float c[4], s[4];
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const int e = lane * E + 4 * v + i;
+        int other = e ^ 1;
         if (kHalves) {
-          const float2 cs = pair[4 * v + i] >= 0 ? cs_s[t * (D / 2) + pair[4 * v + i]] : make_float2(1.f, 0.f);
+          int pair;
+          bool first;
+          place(g, e, pair, other, first);
+          partner[4 * v + i] = grp * D + other;
+          const float2 cs = pair >= 0 ? cs_s[t * (D / 2) + pair] : make_float2(1.f, 0.f);
           c[i] = cs.x;
-          s[i] = second >> (4 * v + i) & 1 ? cs.y : -cs.y;
+          s[i] = first ? -cs.y : cs.y;
         } else {
           const float2 cs = cs_s[t * (D / 2) + e / 2];
           c[i] = cs.x;
@@ -166,7 +176,7 @@ qk_norm_rope_kernel(const T* Q, const T* K, T* Q_out, T* K_out, const float* __r
         }
         if (weight && g.norm) {
           c[i] *= weight[e];
-          s[i] *= weight[kHalves ? partner[4 * v + i] : e ^ 1];
+          s[i] *= weight[other];
         }
       }
       ce[v] = pack2(c[0], c[2]);
@@ -177,10 +187,11 @@ qk_norm_rope_kernel(const T* Q, const T* K, T* Q_out, T* K_out, const float* __r
     const T* in = src + (int64_t)n * rs + lane * E + a * hs;
     T* out = dst + (int64_t)n * ors + lane * E + a * ohs;
     for (int h = a; h < b; h += kUnroll, in += kUnroll * hs, out += kUnroll * ohs) {
-      uint4 raw[kUnroll];
+      if (h > a || !loaded) {
 #pragma unroll
-      for (int u = 0; u < kUnroll; ++u)
-        if (h + u < b) raw[u] = *reinterpret_cast<const uint4*>(in + u * hs);
+        for (int u = 0; u < kUnroll; ++u)
+          if (h + u < b) raw[u] = *reinterpret_cast<const uint4*>(in + u * hs);
+      }
       if (kHalves) {
 #pragma unroll
         for (int u = 0; u < kUnroll; ++u)
@@ -193,7 +204,7 @@ qk_norm_rope_kernel(const T* Q, const T* K, T* Q_out, T* K_out, const float* __r
         uint64_t e[V], o[V], pe[V], po[V];
         P::split(raw[u], e, o);
         if (kHalves) {
-          const T* row = &row_s[(u * G + grp) * D];
+          const T* row = &row_s[u * G * D];
 #pragma unroll
           for (int v = 0; v < V; ++v) {
             pe[v] = pack2(fc::to_float<T>(row[partner[4 * v]]), fc::to_float<T>(row[partner[4 * v + 2]]));
@@ -226,8 +237,8 @@ qk_norm_rope_kernel(const T* Q, const T* K, T* Q_out, T* K_out, const float* __r
       if (kHalves) __syncwarp(mask);
     }
   };
-  if (h0 < g.H_q) walk(Q, Q_out, g.q_hs, g.q_rs, g.qo_hs, g.qo_rs, q_weight, h0, min(h1, g.H_q));
-  if (h1 > g.H_q) walk(K, K_out, g.k_hs, g.k_rs, g.ko_hs, g.ko_rs, k_weight, max(h0 - g.H_q, 0), h1 - g.H_q);
+  if (h0 < g.H_q) walk(Q, Q_out, g.q_hs, g.q_rs, g.qo_hs, g.qo_rs, q_weight, h0, min(h1, g.H_q), true);
+  if (h1 > g.H_q) walk(K, K_out, g.k_hs, g.k_rs, g.ko_hs, g.ko_rs, k_weight, max(h0 - g.H_q, 0), h1 - g.H_q, h0 >= g.H_q);
 }
 
 // f radians per position -> turns per position modulo one, times 2^64
