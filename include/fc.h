@@ -367,7 +367,7 @@ int fc_kv_select_compact_ex(fc_ctx* ctx, void* stream, const float* score, int n
  *   Q, Q_out         DEVICE [H_q, T, d], K, K_out DEVICE [H_kv, T, d]; `dtype` elements with the strides of the
  *                    descriptor (any order of heads and tokens, e.g. slices of a fused projection).  H_q or
  *                    H_kv may be 0 (its pointers are then ignored), T too.  An output may be its own input (same pointer
- *                    and strides); other overlap is not allowed.
+ *                    and strides); other overlap is not allowed, nor rows of an output that overlap one another.
  *   q_weight, k_weight  DEVICE [d] fp32 or NULL; ignored for FC_NORM_NONE.
  *   pos              DEVICE [T, 3] int32, contiguous, or NULL: token n then stands at
  *                    (grid_t0 + n / (grid_h grid_w), n / grid_w % grid_h, n % grid_w).
@@ -405,7 +405,7 @@ int fc_qk_norm_rope(fc_ctx* ctx, void* stream, const fc_rope_desc* desc, const v
  * attention over these values without another rounding.  In each little-endian 32-bit word of eight
  * elements, element 2i is at bits 4i of the low half and element 2i+1 at bits 4i of the high half (i = 0..3).
  * The pointers are DEVICE pointers inside a HOST struct; K and V share strides.  Code bases and strides are
- * multiples of 16 bytes, scale bases of 16 bytes, scale strides of d/32 elements. */
+ * multiples of 16 bytes, scale bases and strides of a row's scales (d/32 elements). */
 typedef struct {
   void *k_codes, *k_scales, *v_codes, *v_scales;
   int64_t code_hs, code_rs;   /* bytes: head, row (row >= d/2) */
@@ -466,6 +466,7 @@ int fc_kv4_unpack(fc_ctx* ctx, void* stream, const fc_kv4_unpack_desc* desc, con
  *   K, V             DEVICE [H_kv, kv_rows, d], the window; may be NULL if n_seg is 0 (no window).
  *   kv_visible_len   as above, at most 2^31 - 4097.
  *   n_seg            <= FC_MAX_SEGMENTS - 1.
+ * In fp32 an infinity in q or in a window row that is seen makes what it reaches NaN.
  * Deterministic.  Workspace: fc_chunk_attention_kv4_workspace_bytes() of the same arguments (0 for arguments
  * that the call refuses). */
 size_t fc_chunk_attention_kv4_workspace_bytes(const fc_ctx* ctx, const fc_attn_desc* desc, int dtype,

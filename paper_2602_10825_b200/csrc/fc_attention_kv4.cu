@@ -162,6 +162,7 @@ extern "C" int fc_chunk_attention_kv4(fc_ctx* ctx, void* stream, const fc_attn_d
     if (strides[i] < 0 || (strides[i] * es) % 16) return FC_ERR_MISALIGNED;
     if (i % 2 && strides[i] < desc->d) return FC_ERR_INVALID_ARG;
   }
+  if (desc->H_q > 1 && desc->o_hs < desc->d) return FC_ERR_INVALID_ARG;  // heads of O would overlap
   if (!fc::aligned16(Q) || !fc::aligned16(O)) return FC_ERR_MISALIGNED;
   if (n_cache > 0 && (rc = fc::kv4_check(cache, desc->d, n_cache)) != FC_OK) return rc;
   if (n_seg > FC_MAX_SEGMENTS - 1) return FC_ERR_UNSUPPORTED;

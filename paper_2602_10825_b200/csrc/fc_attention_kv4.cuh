@@ -25,12 +25,12 @@ struct Kv4AttnGeom {
   float2* part_ml;   // [H_kv, n_vrows, n_splits] running maximum (log2 units for the tensor-core kernel) and sum
 };
 
-// Whether chunk c is on the device-side list (at most 64 entries).
+// Whether chunk c is on the device-side list (at most 64 entries); called by whole warps.
 __device__ __forceinline__ bool chunk_active(const AttnGeom& a, int c) {
-  const int n = min(max(*a.n_active, 0), a.W);
-  for (int i = 0; i < n; ++i)
-    if (a.active_ids[i] == c) return true;
-  return false;
+  static_assert(FC_MAX_CHUNKS <= 64, "two entries a lane");
+  const int lane = threadIdx.x % 32, n = min(max(*a.n_active, 0), a.W);
+  const bool mine = (lane < n && a.active_ids[lane] == c) || (lane + 32 < n && a.active_ids[lane + 32] == c);
+  return __any_sync(0xffffffffu, mine);
 }
 
 // An id outside [0, W) is reported and otherwise ignored.

@@ -51,12 +51,15 @@ attention_kv4_simt_kernel(const T* __restrict__ Q, const T* __restrict__ K, cons
 
   const fc::AttnGeom& a = g.a;
   const int tid = threadIdx.x, hk = blockIdx.y, part = blockIdx.z;
-  if (tid == 0) {
+  if (tid < 32) {
     int v0 = 0;
     const int c = fc::tile_chunk<kRows>(a, blockIdx.x, v0);
-    sh_chunk = c >= 0 && fc::chunk_active(a, c) ? c : -1;
-    sh_v0 = v0;
-    if (blockIdx.x == 0 && hk == 0 && part == 0) fc::report_bad_ids(a);
+    const bool on = fc::chunk_active(a, c);
+    if (tid == 0) {
+      sh_chunk = c >= 0 && on ? c : -1;
+      sh_v0 = v0;
+      if (blockIdx.x == 0 && hk == 0 && part == 0) fc::report_bad_ids(a);
+    }
   }
   __syncthreads();
   const int c = sh_chunk;

@@ -329,6 +329,7 @@ extern "C" int fc_kv4_pack(fc_ctx* ctx, void* stream, const fc_kv4_pack_desc* de
   if (desc->n_old > 0 && (rc = fc::kv4_check(old, desc->d, desc->n_old)) != FC_OK) return rc;
   if (desc->dst_row > INT64_MAX - desc->n_out) return FC_ERR_INVALID_ARG;
   if ((rc = fc::kv4_check(dst, desc->d, desc->dst_row + desc->n_out)) != FC_OK) return rc;
+  if (desc->H > 1 && (dst->code_hs < desc->d / 2 || dst->scale_hs < desc->d / fc::kKv4Group)) return FC_ERR_INVALID_ARG;  // overlap
 
   PackGeom g = {};
   g.n_old = desc->n_old; g.n_new = desc->n_new; g.n_out = desc->n_out; g.dst_row = desc->dst_row;
@@ -368,6 +369,7 @@ extern "C" int fc_kv4_unpack(fc_ctx* ctx, void* stream, const fc_kv4_unpack_desc
   if ((rc = fc::kv4_check(src, desc->d, desc->src_row + desc->n)) != FC_OK) return rc;
   if (K_dst && (rc = check_rows(K_dst, desc->d, es, desc->k_hs, desc->k_rs)) != FC_OK) return rc;
   if (V_dst && (rc = check_rows(V_dst, desc->d, es, desc->v_hs, desc->v_rs)) != FC_OK) return rc;
+  if (desc->H > 1 && ((K_dst && desc->k_hs < desc->d) || (V_dst && desc->v_hs < desc->d))) return FC_ERR_INVALID_ARG;  // overlap
   FC_DEVICE_GUARD(ctx);
   return fc::kv4_unpack_launch((cudaStream_t)stream, fc::kv4_view(*src), desc->H, desc->d, desc->src_row, desc->n, K_dst,
                                V_dst, dtype, desc->k_hs, desc->k_rs, desc->v_hs, desc->v_rs, nullptr);

@@ -23,8 +23,8 @@ inline Kv4View kv4_view(const fc_kv4_cache& c) {
 inline int kv4_check(const fc_kv4_cache* c, int d, int64_t rows_needed) {
   if (!c || !c->k_codes || !c->k_scales || !c->v_codes || !c->v_scales) return FC_ERR_INVALID_ARG;
   if (c->rows < rows_needed) return FC_ERR_INVALID_ARG;
-  if (!aligned16(c->k_codes) || !aligned16(c->v_codes) || !aligned16(c->k_scales) || !aligned16(c->v_scales))
-    return FC_ERR_MISALIGNED;
+  if (!aligned16(c->k_codes) || !aligned16(c->v_codes)) return FC_ERR_MISALIGNED;
+  if (((uintptr_t)c->k_scales | (uintptr_t)c->v_scales) % (d / kKv4Group * 2)) return FC_ERR_MISALIGNED;
   if (c->code_hs < 0 || c->code_rs < 0 || c->code_hs % 16 || c->code_rs % 16) return FC_ERR_MISALIGNED;
   const int groups = d / kKv4Group;
   if (c->scale_hs < 0 || c->scale_rs < 0 || c->scale_hs % groups || c->scale_rs % groups) return FC_ERR_MISALIGNED;

@@ -105,7 +105,7 @@ qk_norm_rope_kernel(const T* Q, const T* K, T* Q_out, T* K_out, const float* __r
   constexpr int kUnroll = sizeof(T) == 4 ? 3 : 4;
   constexpr int E = P::N, L = D / E, G = kThreads / L, V = E / 4;  // elements per lane, lanes per row, rows per block, pairs of pairs
   __shared__ float2 cs_s[G * (D / 2)];                     // (cos, sin) of the block's tokens and pairs
-  __shared__ T row_s[kHalves ? kUnroll * kThreads * E : 1];  // the rows in flight, where partners sit in other lanes
+  __shared__ __align__(16) T row_s[kHalves ? kUnroll * kThreads * E : 1];  // the rows in flight, where partners sit in other lanes
   const int tid = threadIdx.x, lane = tid % L, grp = tid / L;
   const int first_token = blockIdx.x * g.tokens;
 
@@ -298,6 +298,7 @@ extern "C" int fc_qk_norm_rope(fc_ctx* ctx, void* stream, const fc_rope_desc* de
     if (!fc::aligned16(x.in) || !fc::aligned16(x.out)) return FC_ERR_MISALIGNED;
     for (int64_t s : x.s)
       if (s < 0 || (s * es) % 16) return FC_ERR_MISALIGNED;
+    if ((x.heads > 1 && x.s[2] < desc->d) || (desc->T > 1 && x.s[3] < desc->d)) return FC_ERR_INVALID_ARG;  // rows would overlap
   }
   const int64_t heads = (int64_t)desc->H_q + desc->H_kv;
   if (heads == 0 || desc->T == 0) return FC_OK;

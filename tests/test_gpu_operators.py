@@ -178,6 +178,27 @@ def test_pack_and_unpack(fc, ctx, H, n, d, dtype):
         assert (dst[:, 0] == 5).all() and (dst[:, n - 1:] == 5).all()
 
 
+@pytest.mark.parametrize("d", [64, 128])
+def test_slices_of_a_store(fc, ctx, d):
+    # a store seen from an odd row on, rows before heads: every call takes it
+    H, n, first = 3, 45, 7
+    t = [torch.zeros((n + 20, H, k), dtype=dt, device="cuda").transpose(0, 1) for k, dt in 2 * ((d // 2, torch.uint8), (d // 32, BF16))]
+    part = fc.Kv4Cache(*(x[:, first:first + n] for x in t))
+    K, V = rand((H, n, d), 1), rand((H, n, d), 2)
+    ctx.kv4_pack(K, V, part)
+    check_packed(part, K, V)
+    assert all((x[:, :first] == 0).all() and (x[:, first + n:] == 0).all() for x in t)
+    Ku, Vu = ctx.kv4_unpack(part, row=3, n=n - 3)
+    assert np.array_equal(f64(Ku), pf.quantise(f64(K))[2][:, 3:]) and np.array_equal(f64(Vu), pf.quantise(f64(V))[2][:, 3:])
+    again = ctx.kv4_pack(None, None, fc.Kv4Cache.empty(H, n, d), old=part)
+    assert same_store(again, part)
+    for rows in (2, 300):
+        Q = rand((H, rows, d), 3)
+        O = torch.zeros_like(Q)
+        ctx.chunk_attention_kv4(Q, part, None, None, [0, rows], [n], i32([0]), i32([1]), O)
+        check_attention(O, None, *pf.attention(f64(Q), pf.quantise(f64(K))[2], pf.quantise(f64(V))[2], [0, rows], [n], [0]), BF16, True, n, d)
+
+
 @pytest.mark.parametrize("dtype", [BF16, F32])
 def test_pack_ties_extremes_and_strides(fc, ctx, dtype):
     x = torch.zeros((2, 40, 64), dtype=F32)
@@ -424,6 +445,27 @@ def test_attention_nan_query_stays_in_its_row(fc, ctx, rows):
         ctx.chunk_attention_kv4(Q, cache, None, None, [0, rows], [400], i32([0]), i32([1]), O)
         bad = torch.isnan(O)
         assert bad[1, 1].all() and int(bad.sum()) == 64
+
+
+@pytest.mark.parametrize("dtype, impl", [(BF16, 1), (BF16, 2), (BF16, 3), (F32, 0)])
+def test_attention_many_chunks(fc, ctx, dtype, impl):
+    # as many chunks as there may be, most of them short; half active, one of them named twice
+    lens = [(7 * c) % 11 for c in range(64)]
+    ids = list(range(0, 64, 2))
+    cache, Kc, Vc = packed_store(fc, ctx, 2, 70, 64, 3)
+    off = [0] + list(np.cumsum(lens))
+    Q = rand((4, off[-1], 64), 4, 1.0, dtype)
+    K, V = rand((2, off[-1], 64), 5, 1.0, dtype), rand((2, off[-1], 64), 6, 1.0, dtype)
+    vis = [70 + o for o in off[1:]]
+    O = torch.full_like(Q, 9.0)
+    # the window in 63 pieces, one after the other
+    cuts = off[:63] + [off[-1]]
+    ctx.chunk_attention_kv4(Q, cache, K, V, off, vis, i32(ids + [ids[5]]), i32([len(ids) + 1]), O, impl=impl,
+                            seg_logical_off=cuts, seg_phys_off=cuts[:-1])
+    want = pf.attention(f64(Q), np.concatenate([Kc, f64(K)], 1), np.concatenate([Vc, f64(V)], 1), off, vis, ids)
+    rows = np.concatenate([np.arange(off[c], off[c + 1]) for c in ids]).astype(int)
+    check_attention(O, None, *want, dtype, dtype == BF16 and impl != 1, vis[-1], 64, rows)
+    assert (f64(O)[:, np.setdiff1d(np.arange(off[-1]), rows)] == 9).all()
 
 
 def test_attention_bad_ids_are_reported(fc, ctx):

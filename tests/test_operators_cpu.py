@@ -55,6 +55,7 @@ def rope(L, ctx, *, Q=P, K=P, Qo=P, Ko=P, dtype=b.BF16, wq=None, wk=None, pos=No
     (dict(theta=float("inf")), INVALID), (dict(grid_h=0), INVALID), (dict(grid_w=-3), INVALID),
     (dict(grid_h=1 << 20, grid_w=1 << 20), INVALID), (dict(grid_t0=2 ** 31 - 1, grid_h=1, grid_w=1), INVALID),
     (dict(freq=[float("nan")] * 64), INVALID), (dict(Q=P + 8), MISALIGNED), (dict(q_hs=4), MISALIGNED), (dict(ko_rs=-8), MISALIGNED),
+    (dict(qo_hs=64), INVALID), (dict(ko_rs=0), INVALID),
 ])
 def test_rope_refusals(L, ctx, kw, want):
     assert rope(L, ctx, **kw) == want
@@ -84,6 +85,7 @@ def pack(L, ctx, *, K=P, V=P, dtype=b.BF16, old=None, kept=None, kept_hs=0, dst=
     (dict(dst=None), INVALID), (dict(dst=store(rows=9)), INVALID), (dict(dst_row=91), INVALID), (dict(dst_row=2 ** 63 - 5), INVALID),
     (dict(dst=store(k_codes=P + 4)), MISALIGNED), (dict(dst=store(code_rs=72)), MISALIGNED), (dict(dst=store(code_rs=48)), INVALID),
     (dict(dst=store(scale_rs=6)), MISALIGNED), (dict(dst=store(scale_rs=0)), INVALID), (dict(dst=store(v_scales=None)), INVALID),
+    (dict(dst=store(k_scales=P + 4)), MISALIGNED), (dict(dst=store(code_hs=0)), INVALID), (dict(dst=store(scale_hs=0)), INVALID),
 ])
 def test_pack_refusals(L, ctx, kw, want):
     assert pack(L, ctx, **kw) == want
@@ -100,7 +102,7 @@ def unpack(L, ctx, *, K=P, V=P, dtype=b.BF16, src=True, **kw):
 @pytest.mark.parametrize("kw, want", [
     (dict(dtype=3), UNSUPPORTED), (dict(d=256), UNSUPPORTED), (dict(n=-1), INVALID), (dict(src_row=-1), INVALID),
     (dict(K=None, V=None), INVALID), (dict(src=None), INVALID), (dict(n=101), INVALID), (dict(src_row=91), INVALID),
-    (dict(k_rs=120), INVALID), (dict(v_rs=132), MISALIGNED), (dict(K=P + 1), MISALIGNED),
+    (dict(k_rs=120), INVALID), (dict(v_rs=132), MISALIGNED), (dict(K=P + 1), MISALIGNED), (dict(v_hs=0), INVALID),
 ])
 def test_unpack_refusals(L, ctx, kw, want):
     assert unpack(L, ctx, **kw) == want
@@ -135,7 +137,7 @@ def attn(L, ctx, *, Q=P, K=P, V=P, O=P, dtype=b.BF16, cache=True, n_cache=100, o
     (dict(ids=None), INVALID), (dict(K=None), INVALID), (dict(Q=P + 8), MISALIGNED), (dict(q_hs=4), MISALIGNED), (dict(o_rs=64), INVALID),
     (dict(k_rs=100), MISALIGNED), (dict(kv_rows=9), INVALID), (dict(seg=((1, 10), (0,))), INVALID), (dict(seg=((0, 10), (-1,))), INVALID),
     (dict(seg=(tuple(range(65)), tuple(range(64)))), UNSUPPORTED), (dict(seg=None), INVALID), (dict(lse=P, lse_hs=0), INVALID),
-    (dict(cache=store(k_codes=P + 8)), MISALIGNED),
+    (dict(cache=store(k_codes=P + 8)), MISALIGNED), (dict(o_hs=0), INVALID), (dict(impl=2, q_hs=0), UNSUPPORTED),
 ])
 def test_attention_refusals(L, ctx, kw, want):
     assert attn(L, ctx, **kw) == want
