@@ -566,8 +566,8 @@ size_t kv4_rows_workspace(const fc_ctx* ctx, Kv4AttnGeom& g) {
   const int nt = tiles_of(g);
   const int64_t tiles = tile_count(g.a, 8 * nt) * g.a.H_kv;
   // The number of parts is the one that should be fastest.  A part is at least two steps; joining the parts costs a kernel and their
-  // bytes.  Where all blocks are resident at once, the fullest SM counts (a block that has the SM to itself takes 1.35 times
-  // its share of a full one); otherwise all the work does, half a part more for the blocks that end last, and 3 us for each set
+  // bytes.  Where all blocks are resident at once, the fullest SM counts (one or two blocks on an SM take 1.35 or
+  // 1.08 times their share of a full one); otherwise all the work does, half a part more for the blocks that end last, and 3 us for each set
   // of blocks to start and end.
   constexpr int64_t kUnit = kStep * kWarps;
   auto units_of = [&](int v) {
@@ -587,7 +587,7 @@ size_t kv4_rows_workspace(const fc_ctx* ctx, Kv4AttnGeom& g) {
     if (k > 1 && blocks > 4 * slots) break;
     last = n;
     const int64_t on_sm = (blocks + ctx->sm_count - 1) / ctx->sm_count;
-    const double us = (blocks <= slots ? u * steps * (on_sm == 1 ? 1.35 : (double)on_sm) + 3
+    const double us = (blocks <= slots ? u * steps * (on_sm == 1 ? 1.35 : on_sm == 2 ? 2.15 : (double)on_sm) + 3
                                        : u * ((double)work / ctx->sm_count + 0.5 * blocks_per_sm(nt) * steps) + 3.0 * blocks / slots) +
                       (n > 1 ? 4 + n * join_us : 0);
     if (k == 1 || us < best) best = us, g.part_keys = steps * kUnit, g.n_splits = (int32_t)n;
