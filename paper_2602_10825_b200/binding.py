@@ -154,6 +154,7 @@ def _host_i32(x):
 # in their order): a third of the time of filling a ctypes structure.
 _ROPE_FIELDS, _PACK_FIELDS = struct.Struct("@4i8q3i2ifd3i"), struct.Struct("@5i5q")
 _UNPACK_FIELDS, _ATTN_FIELDS = struct.Struct("@3i5q"), struct.Struct("@4i9qfi")
+_CACHE_FIELDS = struct.Struct("@4P5q")
 
 
 def _int32(x):
@@ -169,23 +170,28 @@ class Kv4Cache:
 
     def __init__(self, k_codes, k_scales, v_codes, v_scales):
         self.k_codes, self.k_scales, self.v_codes, self.v_scales = k_codes, k_scales, v_codes, v_scales
-        if k_codes.dim() != 3 or k_scales.dim() != 3:
+        shape, s_shape, strides, s_strides = k_codes.shape, k_scales.shape, k_codes.stride(), k_scales.stride()
+        if len(shape) != 3 or len(s_shape) != 3:
             raise FcError("codes and scales must be [heads, rows, ...]")
-        H, rows, half = shape = k_codes.shape
-        (ch, cr, c1), (sh, sr, s1) = k_codes.stride(), k_scales.stride()
-        device, s_shape = k_codes.device, (H, rows, half // 16)
+        H, rows, half = shape
         if not (k_codes.dtype is v_codes.dtype is torch.uint8 and k_scales.dtype is v_scales.dtype is torch.bfloat16):
             raise FcError("codes must be uint8 and scales bfloat16")
-        if not (v_codes.shape == shape and k_scales.shape == s_shape and v_scales.shape == s_shape):
-            raise FcError(f"codes must be [heads, rows, d/2] and scales [heads, rows, d/32], got {list(shape)}, {list(k_scales.shape)}, "
+        if v_codes.shape != shape or v_scales.shape != s_shape or s_shape != (H, rows, half // 16):
+            raise FcError(f"codes must be [heads, rows, d/2] and scales [heads, rows, d/32], got {list(shape)}, {list(s_shape)}, "
                           f"{list(v_codes.shape)}, {list(v_scales.shape)}")
-        if not (device == v_codes.device == k_scales.device == v_scales.device):
+        device = k_codes.get_device()
+        if not (device == v_codes.get_device() == k_scales.get_device() == v_scales.get_device()):
             raise FcError("codes and scales must be on one device")
-        if v_codes.stride() != (ch, cr, c1) or v_scales.stride() != (sh, sr, s1) or c1 != 1 or s1 != 1:
+        ch, cr, c1 = strides
+        sh, sr, s1 = s_strides
+        if v_codes.stride() != strides or v_scales.stride() != s_strides or c1 != 1 or s1 != 1:
             raise FcError("K and V must share strides, with a contiguous last dimension")
-        self.H, self.rows, self.d, self.device = H, rows, 2 * half, device
-        self._c = _Kv4Cache(k_codes.data_ptr(), k_scales.data_ptr(), v_codes.data_ptr(), v_scales.data_ptr(), ch, cr, sh, sr, rows)
-        self._at = C.addressof(self._c)
+        self.H, self.rows, self.d, self._device = H, rows, 2 * half, device
+        self._c = _CACHE_FIELDS.pack(k_codes.data_ptr(), k_scales.data_ptr(), v_codes.data_ptr(), v_scales.data_ptr(), ch, cr, sh, sr, rows)
+
+    @property
+    def device(self):
+        return self.k_codes.device
 
     @staticmethod
     def empty(H, rows, d, device="cuda"):
@@ -419,7 +425,7 @@ class Context:
         """Device pointer of a tensor on this context's device (None for None)."""
         if t is None:
             return None
-        if t.device != self._dev:
+        if t.get_device() != self.device:
             raise FcError(f"{name} must be on cuda:{self.device}, got {t.device}")
         if dtype is not None and t.dtype is not dtype:
             raise FcError(f"{name} must have dtype {dtype}, got {t.dtype}")
@@ -429,7 +435,7 @@ class Context:
         """Pointer and (head, row) strides of a [heads, rows, d] tensor."""
         if t.shape != shape or t.dtype is not dtype:
             raise FcError(f"{name} must be {list(shape)} of {dtype}, got {list(t.shape)} of {t.dtype}")
-        if t.device != self._dev:
+        if t.get_device() != self.device:
             raise FcError(f"{name} must be on cuda:{self.device}, got {t.device}")
         hs, rs, one = t.stride()
         if one != 1:
@@ -514,12 +520,12 @@ class Context:
 
     # ------------------------------------------------------------------ fc_kv4_pack / fc_kv4_unpack
     def _store(self, s, name):
-        """Address of a store's C struct."""
+        """A store's C struct, as bytes that a call can take the address of."""
         if s is None:
             return None
-        if s.device != self._dev:
+        if s._device != self.device:
             raise FcError(f"{name} must be on cuda:{self.device}, got {s.device}")
-        return s._at
+        return s._c
 
     def kv4_pack(self, K, V, dst, *, old=None, n_old=None, kept_idx=None, dst_row=0, status=None):
         """Quantises rows of K, V [H, n_new, d] into the store `dst`, from row dst_row on; returns dst.

@@ -162,7 +162,7 @@ def test_attention_no_rows_and_workspace(L, ctx):
 
 def test_packed_descriptors_are_the_structures():
     for fields, cls in ((b._ROPE_FIELDS, b._RopeDesc), (b._PACK_FIELDS, b._Kv4PackDesc), (b._UNPACK_FIELDS, b._Kv4UnpackDesc),
-                        (b._ATTN_FIELDS, b._AttnDesc)):
+                        (b._ATTN_FIELDS, b._AttnDesc), (b._CACHE_FIELDS, b._Kv4Cache)):
         n = len(fields.unpack(bytes(fields.size)))
         raw = fields.pack(*range(1, n + 1)).ljust(C.sizeof(cls), b"\0")
         got = cls.from_buffer_copy(raw)
