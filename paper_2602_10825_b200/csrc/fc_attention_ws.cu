@@ -46,8 +46,8 @@
 // Two stores (fc_chunk_attention_kv4).  The first segments lie in a store of their own, the workspace that the clean region was
 // unpacked into; nothing is copied to bring it together with the window.  Three things follow from the fewer rows such calls may
 // have: the keys can be cut into parts (an item is then a part of the keys, its result goes to the workspace undivided, and
-// another kernel joins them: 256 rows of 24 heads over 28256 keys took 468 us in one part, 193 in six); grouped query heads are
-// rows of one tile (64 rows of 16 heads on 4: 102 us, with this 48); and the setup overlaps the kernel that unpacks (5 us a call).
+// another kernel joins them: 256 rows of 24 heads over 28256 keys took 468 us in one part and 164 now); grouped query heads are
+// rows of one tile (64 rows of 16 heads on 4: 102 us, with this 48); and the setup overlaps the kernel that unpacks (4 us a call).
 // Every mbarrier wait is bounded (see mbar_wait_bounded); tensor memory is always released.
 #include <algorithm>
 #include <climits>
