@@ -602,6 +602,8 @@ class Context:
             raise FcError("Q and the store must share the head size")
         n_cache = (0 if cache is None else cache.rows) if n_cache is None else int(n_cache)
         W = len(kv_visible_len)
+        if not active_ids.is_contiguous():
+            raise FcError("active_ids must be contiguous")
         if len(q_chunk_row_off) != W + 1 or q_chunk_row_off[W] > rows or active_ids.numel() > W:
             raise FcError("q_chunk_row_off must have one entry more than kv_visible_len and stay inside Q; active_ids at most as many")
         kp = vp = sl = sp = None

@@ -58,7 +58,7 @@ UnpackedPlan plan_unpacked(const fc_ctx* ctx, const fc::Kv4AttnGeom& g) {
   const fc::AttnGeom& a = g.a;
   UnpackedPlan p;
   // grouped heads share their key tiles where whole groups fill a tile of 128 rows
-  if (128 % a.group == 0 && (int64_t)a.q_row_off[a.W] * a.group <= INT32_MAX) p.split.pack = a.group;
+  if (128 % a.group == 0 && (int64_t)a.q_row_off[a.W] * a.group <= INT32_MAX - 4096) p.split.pack = a.group;
   int64_t pairs = 0;
   int vis = 0;
   for (int c = 0; c < a.W; ++c) {

@@ -7,7 +7,8 @@ Tolerances.  A rounding to bf16 is off by at most 2^-8 of the value, one to fp32
   packing    none: codes and scales are compared as bits.
   attention  fp32: a logit is off by at most (d + 4) 2^-24 |q||k| scale, a weight by twice that, and sums of n terms by
              n 2^-24, all relative to A = sum p |v|.  The tensor-core kernels round each weight to bf16 (2^-8 A) and take
-             exponentials good to 1e-4 (A again); then the output's rounding.
+             exponentials good to 1e-4 (A again); then the output's rounding.  The log of the weights' sum is off by the logit's
+             error, the sum's n 2^-24, the exponentials' 1e-4, and its own rounding and that of the logarithm (2^-22).
 """
 import math
 
@@ -277,6 +278,18 @@ def test_pack_append_and_compact(fc, ctx, dtype, d):
     assert same_store(ctx.kv4_pack(K[:, n_old:], V[:, n_old:], fc.Kv4Cache.empty(H, n_old + n_new, d), old=old), whole)
 
 
+def test_pack_within_one_store(fc, ctx):
+    # a store may be packed from its own rows as long as what is read and what is written lie apart
+    H, n, d = 2, 40, 64
+    K, V = rand((H, n, d), 1), rand((H, n, d), 2)
+    store = ctx.kv4_pack(K, V, fc.Kv4Cache.empty(H, 2 * n, d))
+    kept = torch.arange(n - 1, -1, -1).repeat(H, 1).int().cuda()
+    ctx.kv4_pack(None, None, store, old=store, n_old=n, kept_idx=kept, dst_row=n)
+    assert torch.equal(store.k_codes[:, n:].flip(1), store.k_codes[:, :n]) and torch.equal(store.v_scales[:, n:].flip(1), store.v_scales[:, :n])
+    with pytest.raises(fc.FcError, match="invalid argument"):
+        ctx.kv4_pack(None, None, store, old=store, n_old=n, kept_idx=kept, dst_row=n - 1)
+
+
 def test_pack_bad_index_leaves_the_row(fc, ctx):
     H, n, d = 2, 50, 128
     K, V = rand((H, n, d), 1), rand((H, n, d), 2)
@@ -329,7 +342,8 @@ def check_attention(O, lse, want, want_lse, A, size, dtype, tensor_cores, n, d, 
         got, w = f64(lse)[:, rows], want_lse[:, rows]
         assert np.array_equal(np.isneginf(got), np.isneginf(w))
         fine = np.isfinite(w)
-        assert (np.abs(got[fine] - w[fine]) <= rel * 0.1 + 1e-4 * tensor_cores + 1e-5 + 2.0 ** -23 * np.abs(w[fine])).all()
+        tol = ((d + 4) * size + n) * 2.0 ** -24 + 1e-4 * tensor_cores + 2.0 ** -22 * np.maximum(1.0, np.abs(w[fine]))
+        assert (np.abs(got[fine] - w[fine]) <= tol).all()
 
 
 def packed_store(fc, ctx, H, n, d, seed, sigma=1.0, extra=0):
@@ -567,6 +581,8 @@ def test_binding_refusals(fc, ctx):
         ctx.chunk_attention_kv4(K, cache, K.float(), K.float(), [0, 8], [9], ids, one, O)
     with pytest.raises(fc.FcError, match="store, a window"):
         ctx.chunk_attention_kv4(K, None, None, None, [0, 8], [0], ids, one, O)
+    with pytest.raises(fc.FcError, match="contiguous"):
+        ctx.chunk_attention_kv4(K, cache, None, None, [0, 4, 8], [8, 8], i32([0, 1, 1, 0])[::2], one, O)
     with pytest.raises(fc.FcError, match="inside Q"):
         ctx.chunk_attention_kv4(K, cache, None, None, [0, 9], [8], ids, one, O)
     with pytest.raises(fc.FcError, match="workspace"):
