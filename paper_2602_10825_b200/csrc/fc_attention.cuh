@@ -23,16 +23,35 @@ struct AttnGeom {
   uint32_t* status;
 };
 
-// attention_tc_two only: how the work is cut up.  Parts of the keys have their results joined by another kernel (n_splits 1: no
-// parts).
+// attention_tc_two only: how the work is cut up.
+//
+// Work items (a chunk's 256 rows of one head or group of heads) are handed out to one block per SM.  As many as fill whole rounds of
+// the blocks are worked through in one piece; the keys of the others, the shortest, are cut into parts, so that the last
+// round is full too.  How many there are is known on the device only (the active list is there), so the kernel decides and leaves
+// word for the one that joins the parts.
 struct AttnSplit {
   int32_t pack = 1;     // query heads taken as rows of one tile: 1, or the group where it divides a tile's 128 rows
   bool follows = false; // the stream's last kernel writes K0 / V0, clears the counter and lets this one start early
-  int32_t n_splits = 1, part_keys = 0;  // part p: logical keys [p part_keys, (p + 1) part_keys), the last one to the end
-  int64_t n_vrows = 0;
-  float* o = nullptr;   // [H_kv, n_vrows, n_splits, d]: sums not divided by their weights
-  float2* ml = nullptr; // [H_kv, n_vrows, n_splits]: reference (log2 units) and sum of the weights
+  int32_t slots = 0;    // room for parts; 0: every item in one piece
+  float* o = nullptr;   // [slots, 256, d]: sums not divided by their weights
+  float2* ml = nullptr; // [slots, 256]: reference (log2 units) and sum of the weights
+  int32_t* plan = nullptr; // [4 + 4 * blocks]: cut items, parts of each, -, -; then of each: chunk, head, first row, -
 };
+constexpr int kMaxParts = 32;
+
+// Parts for each of `rest` items of `tiles` key tiles on `blocks` blocks.  The unit is the time of a key tile, 1.8 us; the
+// joining kernel costs three of them, and the parts' bytes go at 4 TB/s.
+__host__ __device__ inline int split_parts(int rest, int blocks, int tiles, int d, int slots, float* cost) {
+  const float part = (float)rest * 256 * d * 8 / 7.2e6f;
+  int best_n = 1;
+  float best = (float)tiles * ((rest + blocks - 1) / blocks);
+  for (int n = 2; n <= kMaxParts && rest * n <= slots && n * 3 <= tiles; ++n) {
+    const float c = (float)((rest * n + blocks - 1) / blocks) * ((tiles + n - 1) / n) + 3.f + n * part;
+    if (c < best) best = c, best_n = n;
+  }
+  if (cost) *cost = best;
+  return best_n;
+}
 
 int attention_simt(cudaStream_t st, const AttnGeom& g, const void* Q, const void* K, const void* V,
                    int dtype, void* O);

@@ -47,11 +47,11 @@ int cache_rows(const fc::Kv4AttnGeom& g) {
   return std::min(n, g.n_cache);
 }
 
-// Workspace of the unpacked path: the tcgen05 kernel's own, K, V, and the parts where there are any.
+// Workspace of the unpacked path: the tcgen05 kernel's own, K, V, and room for parts of the keys.
 struct UnpackedPlan {
   fc::AttnSplit split;
-  size_t k, v, o, ml, bytes;  // offsets
-  double us;                  // estimate of the whole path
+  size_t k, v, plan, o, ml, bytes;  // offsets
+  double us;                        // estimate of the whole path
 };
 
 UnpackedPlan plan_unpacked(const fc_ctx* ctx, const fc::Kv4AttnGeom& g) {
@@ -59,38 +59,27 @@ UnpackedPlan plan_unpacked(const fc_ctx* ctx, const fc::Kv4AttnGeom& g) {
   UnpackedPlan p;
   // grouped heads share their key tiles where whole groups fill a tile of 128 rows
   if (128 % a.group == 0 && (int64_t)a.q_row_off[a.W] * a.group <= INT32_MAX - 4096) p.split.pack = a.group;
-  int64_t pairs = 0;
+  int64_t items = 0;
   int vis = 0;
   for (int c = 0; c < a.W; ++c) {
-    pairs += ((int64_t)(a.q_row_off[c + 1] - a.q_row_off[c]) * p.split.pack + 255) / 256;  // rows of a work item
+    items += ((int64_t)(a.q_row_off[c + 1] - a.q_row_off[c]) * p.split.pack + 255) / 256;  // rows of a work item
     vis = std::max(vis, a.vis[c]);
   }
-  // Work items are handed out one at a time to one block per SM, so that the time is (rounds) x (key tiles of an item); cutting
-  // the keys fills the last round at the price of writing and reading the parts.  Measured: 1.8 us a key tile, the parts' bytes at
-  // 4 TB/s and 5 us for the joining kernel.
-  const int64_t items = std::max<int64_t>(1, pairs * (a.H_q / p.split.pack));
-  const int64_t tiles = (vis + 127) / 128;
-  const double part_us = 2.0 * 4 * a.d * a.H_kv * g.n_vrows / 4e6;
-  int64_t n = 1;
-  double best = 0;
-  for (int64_t k = 1; k <= std::min<int64_t>(32, std::max<int64_t>(1, tiles / 4)); ++k) {
-    const int64_t rounds = (items * k + ctx->sm_count - 1) / ctx->sm_count;
-    const double us = 1.8 * rounds * ((tiles + k - 1) / k) + (k > 1 ? 5 + k * part_us : 0);
-    if (k == 1 || us < best) best = us, n = k;
-  }
-  // 8 us for the launches of the path, the unpacking at 6 TB/s
-  p.us = 8 + best + 2.0 * a.H_kv * cache_rows(g) * a.d * 2.56 / 6e6;
-  if (n > 1) {
-    p.split.part_keys = (int32_t)((tiles + n - 1) / n * 128);
-    p.split.n_splits = (int32_t)((vis + p.split.part_keys - 1) / p.split.part_keys);
-    p.split.n_vrows = g.n_vrows;
-  }
-  const size_t rows = (size_t)a.H_kv * cache_rows(g) * a.d * 2;
-  const size_t parts = p.split.n_splits > 1 ? (size_t)a.H_kv * g.n_vrows * p.split.n_splits : 0;
+  items *= a.H_q / p.split.pack;
+  // Room for three parts a block: the cut items fill one round or two and some.
+  const int tiles = (int)(((int64_t)vis + 127) / 128);
+  if (tiles >= 6) p.split.slots = (int32_t)std::min<int64_t>(3 * ctx->sm_count, items * fc::kMaxParts);
+  float last = 0.f;
+  const int rest = (int)(items % ctx->sm_count);
+  if (rest > 0) fc::split_parts(rest, ctx->sm_count, tiles, a.d, p.split.slots, &last);
+  // 8 us for the launches of the path, 1.8 us a key tile, the unpacking at 6 TB/s
+  p.us = 8 + 1.8 * ((double)(items / ctx->sm_count) * tiles + last) + 2.0 * a.H_kv * cache_rows(g) * a.d * 2.56 / 6e6;
+  const size_t rows = (size_t)a.H_kv * cache_rows(g) * a.d * 2, parts = (size_t)p.split.slots * 256;
   p.k = fc::attention_tc_workspace_bytes();
   p.v = p.k + fc::align_up(rows, 256);
-  p.o = p.v + fc::align_up(rows, 256);
-  p.ml = p.o + fc::align_up(parts * a.d * sizeof(float), 256);
+  p.plan = p.v + fc::align_up(rows, 256);
+  p.o = p.plan + fc::align_up((4 + 4 * (size_t)ctx->sm_count) * sizeof(int32_t), 256);
+  p.ml = p.o + parts * a.d * sizeof(float);
   p.bytes = p.ml + parts * sizeof(float2);
   return p;
 }
@@ -223,10 +212,8 @@ extern "C" int fc_chunk_attention_kv4(fc_ctx* ctx, void* stream, const fc_attn_d
     return fc::kv4_unpack_launch(x.st, x.g->cache, x.g->a.H_kv, x.g->a.d, 0, x.n0, x.k, x.v, FC_BF16, hs, x.g->a.d, hs, x.g->a.d, x.counter);
   };
   u.split.follows = n0 > 0;
-  u.split.o = g.part_o = (float*)(base + u.o);
-  u.split.ml = g.part_ml = (float2*)(base + u.ml);
-  g.n_splits = u.split.n_splits;
-  if ((rc = fc::attention_tc_two(ctx, st, a, Q, base + u.k, base + u.v, n0, K, V, u.split, O, ws, ws_bytes, before, &unpack)) != FC_OK)
-    return rc;
-  return u.split.n_splits > 1 ? fc::kv4_combine(st, g, dtype, O, true) : FC_OK;
+  u.split.o = (float*)(base + u.o);
+  u.split.ml = (float2*)(base + u.ml);
+  u.split.plan = (int32_t*)(base + u.plan);
+  return fc::attention_tc_two(ctx, st, a, Q, base + u.k, base + u.v, n0, K, V, u.split, O, ws, ws_bytes, before, &unpack);
 }

@@ -45,9 +45,9 @@
 // even a NaN or an infinity in such a row can reach an output (0 x inf would).
 // Two stores (fc_chunk_attention_kv4).  The first segments lie in a store of their own, the workspace that the clean region was
 // unpacked into; nothing is copied to bring it together with the window.  Three things follow from the fewer rows such calls may
-// have: the keys can be cut into parts (an item is then a part of the keys, its result goes to the workspace undivided, and
-// another kernel joins them: 256 rows of 24 heads over 28256 keys took 468 us in one part and 164 now); grouped query heads are
-// rows of one tile (64 rows of 16 heads on 4: 102 us, with this 48); and the setup overlaps the kernel that unpacks (4 us a call).
+// have.  The items that do not fill a round of the blocks have their keys cut into parts, and attention_join_kernel joins
+// their results (256 rows of 24 heads over 28256 keys: 468 us in one piece).  Grouped query heads are rows of one tile (64 rows of 16
+// heads on 4: half the time).  And the setup overlaps the kernel that unpacks (4 us a call).
 // Every mbarrier wait is bounded (see mbar_wait_bounded); tensor memory is always released.
 #include <algorithm>
 #include <climits>
@@ -60,6 +60,7 @@
 namespace {
 
 using namespace fc::sm100;
+using fc::kMaxParts;
 
 constexpr int kBM = 128, kBN = 128;
 constexpr int kHalf = kBN / 2;  // key columns per S accumulator
@@ -89,13 +90,14 @@ struct WsSmem {
   uint32_t tmem_base;
   uint32_t abort;
   int32_t n_act, total_items;
+  int32_t n_whole, n_rest, n_parts;     // kTwoStores: items in one piece, items cut into parts, parts of each
   int32_t act_chunk[FC_MAX_CHUNKS];     // active chunks, longest visible prefix first
   int32_t act_item_end[FC_MAX_CHUNKS];  // running item count over that list (all heads)
 };
 
 struct Item {
   int h, hk, c, row0, n_vis;  // logical keys [k_lo, n_vis)
-  int k_lo, part;             // kTwoStores: the part of the keys (0 and 0 otherwise)
+  int k_lo, part, slot;       // kTwoStores: the part of the keys, and where its result goes (-1: the item is in one piece)
   bool b_valid;  // tile B has at least one row of the chunk (false for the ragged last item of a chunk)
 };
 
@@ -223,11 +225,28 @@ attention_ws_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
     int items = 0;
     for (int a = 0; a < n; ++a) {
       const int c = sh->act_chunk[a];
-      items += (kTwo ? split.n_splits : 1) * n_heads * (((g.q_row_off[c + 1] - g.q_row_off[c]) * pk + 2 * kBM - 1) / (2 * kBM));
+      items += n_heads * (((g.q_row_off[c + 1] - g.q_row_off[c]) * pk + 2 * kBM - 1) / (2 * kBM));
       sh->act_item_end[a] = items;
     }
     sh->n_act = n;
     sh->total_items = items;
+    if constexpr (kTwo) {
+      const int blocks = gridDim.x, whole = split.slots > 0 ? items / blocks * blocks : items, rest = items - whole;
+      int parts = 1;
+      if (rest > 0) {
+        int a = 0;  // the chunk of the first item that could be cut: none behind it sees more
+        while (sh->act_item_end[a] <= whole) ++a;
+        parts = fc::split_parts(rest, blocks, (g.vis[sh->act_chunk[a]] + kBN - 1) / kBN, D, split.slots, nullptr);
+      }
+      sh->n_parts = parts;
+      sh->n_rest = parts > 1 ? rest : 0;
+      sh->n_whole = items - sh->n_rest;
+      sh->total_items = sh->n_whole + sh->n_rest * parts;
+      if (blockIdx.x == 0 && split.slots > 0) {
+        split.plan[0] = sh->n_rest;
+        split.plan[1] = parts;
+      }
+    }
   }
   if (warp == 0) {
     tmem_alloc(smem_u32(&sh->tmem_base), kTmemCols);
@@ -242,20 +261,31 @@ attention_ws_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
 
   auto decode = [&](int item) {
     Item it;
+    it.part = 0;
+    it.slot = -1;
+    if constexpr (kTwo) {
+      if (item >= sh->n_whole) {  // the first parts of all cut items, then their second ones, and so on
+        const int x = item - sh->n_whole;
+        it.part = x / sh->n_rest;
+        item = sh->n_whole + x % sh->n_rest;
+        it.slot = (item - sh->n_whole) * sh->n_parts + it.part;
+      }
+    }
     int a = 0;
     while (a + 1 < n_act && item >= sh->act_item_end[a]) ++a;
     const int start = a > 0 ? sh->act_item_end[a - 1] : 0;
-    const int pairs = (sh->act_item_end[a] - start) / (kTwo ? split.n_splits * n_heads : n_heads);
+    const int pairs = (sh->act_item_end[a] - start) / n_heads;
     it.c = sh->act_chunk[a];
     it.h = (item - start) / pairs;
     it.row0 = g.q_row_off[it.c] * pk + ((item - start) % pairs) * 2 * kBM;
     it.n_vis = g.vis[it.c];
-    it.k_lo = it.part = 0;
-    if constexpr (kTwo) {  // the parts of all heads one after the other
-      it.part = it.h / n_heads;
-      it.h %= n_heads;
-      it.k_lo = it.part * split.part_keys;
-      if (it.part + 1 < split.n_splits) it.n_vis = min(it.n_vis, it.k_lo + split.part_keys);
+    it.k_lo = 0;
+    if constexpr (kTwo) {
+      if (it.slot >= 0) {
+        const int keys = ((it.n_vis + sh->n_parts - 1) / sh->n_parts + kBN - 1) / kBN * kBN;
+        it.k_lo = min(it.part * keys, it.n_vis);
+        it.n_vis = min(it.n_vis, it.k_lo + keys);
+      }
     }
     it.hk = pk > 1 ? it.h : it.h / g.group;
     it.b_valid = it.row0 + kBM < g.q_row_off[it.c + 1] * pk;
@@ -677,9 +707,14 @@ attention_ws_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
       const bool row_ok = v < g.q_row_off[it.c + 1] * pk &&
                           fc::bounds_ok(row >= 0 && row < g.q_row_off[g.W] && head >= 0 && head < g.H_q, g.status);
       if constexpr (kTwo) {
-        if (split.n_splits > 1) {  // this part's sum, not divided by its weights; kv4_combine joins the parts
-          const int64_t vr = (int64_t)(row - g.q_row_off[0]) * g.group + head % g.group;
-          const int64_t at = (it.hk * split.n_vrows + vr) * split.n_splits + it.part;
+        if (it.slot >= 0) {  // this part's sum, not divided by its weights; another kernel joins the parts
+          const int64_t at = (int64_t)it.slot * (2 * kBM) + x * kBM + r_in;
+          if (it.part == 0 && x == 0 && r_in == 0) {
+            int32_t* entry = split.plan + 4 + it.slot / sh->n_parts * 4;
+            entry[0] = it.c;
+            entry[1] = it.h;
+            entry[2] = it.row0;
+          }
 #pragma unroll
           for (int q4 = 0; q4 < D / 32; ++q4) {
             uint32_t r[32];
@@ -740,6 +775,52 @@ attention_ws_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
   if (warp == 0) tmem_dealloc(tmem, kTmemCols);
 }
 
+// Joins the parts of the cut items, a warp a row: O = sum_p 2^(m_p - m) o_p / sum_p 2^(m_p - m) l_p.
+template <int D>
+__global__ void __launch_bounds__(256)
+attention_join_kernel(const __grid_constant__ fc::AttnGeom g, const __grid_constant__ fc::AttnSplit split,
+                      __nv_bfloat16* __restrict__ O) {
+  constexpr int kLanes = D / 4, kGroups = 32 / kLanes;  // lanes of a part's row, parts at once
+  const int lane = threadIdx.x % 32, item = blockIdx.x, r = blockIdx.y * 8 + threadIdx.x / 32;
+  fc::pdl_wait();
+  const int n = split.plan[1];
+  if (item >= split.plan[0]) return;
+  const int c = split.plan[4 + 4 * item], h = split.plan[5 + 4 * item], v = split.plan[6 + 4 * item] + r, pk = split.pack;
+  if (v >= g.q_row_off[c + 1] * pk) return;
+  const int row = v / pk, head = pk > 1 ? h * pk + v % pk : h;
+  const int64_t at = (int64_t)item * n * (2 * kBM) + r;  // of the first part; the others follow a tile pair apart
+  const float2 ml = lane < n ? split.ml[at + (int64_t)lane * (2 * kBM)] : make_float2(-INFINITY, 0.f);
+  float m = ml.x;
+#pragma unroll
+  for (int k = 16; k; k >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, k));
+  const float w = ml.y != 0.f ? exp2f(ml.x - m) : 0.f;  // a part that saw no token has the reference -inf
+  float l = w == 0.f ? (ml.y == ml.y ? 0.f : ml.y) : w * ml.y;
+#pragma unroll
+  for (int k = 16; k; k >>= 1) l += __shfl_xor_sync(0xffffffffu, l, k);
+  const int grp = lane / kLanes, d4 = lane % kLanes;
+  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 8
+  for (int p0 = 0; p0 < n; p0 += kGroups) {
+    const int p = p0 + grp;
+    const float wp = __shfl_sync(0xffffffffu, w, p & 31);
+    if (p < n) {
+      const float4 y = *reinterpret_cast<const float4*>(split.o + (at + (int64_t)p * (2 * kBM)) * D + 4 * d4);
+      o.x = fmaf(wp, y.x, o.x); o.y = fmaf(wp, y.y, o.y); o.z = fmaf(wp, y.z, o.z); o.w = fmaf(wp, y.w, o.w);
+    }
+  }
+  if (kGroups == 2) {
+    o.x += __shfl_xor_sync(0xffffffffu, o.x, 16); o.y += __shfl_xor_sync(0xffffffffu, o.y, 16);
+    o.z += __shfl_xor_sync(0xffffffffu, o.z, 16); o.w += __shfl_xor_sync(0xffffffffu, o.w, 16);
+  }
+  if (lane < kLanes) {
+    const float inv = l > 0.f ? 1.f / l : (l == l ? 0.f : l);
+    *reinterpret_cast<uint2*>(O + (int64_t)head * g.o_hs + (int64_t)row * g.o_rs + 4 * d4) =
+        make_uint2(cvt_bf16x2(o.x * inv, o.y * inv), cvt_bf16x2(o.z * inv, o.w * inv));
+    if (g.lse && lane == 0)
+      g.lse[(int64_t)head * g.lse_hs + row] = l > 0.f ? (m + log2f(l)) * 0.6931471805599453f : (l == l ? -INFINITY : l);
+  }
+}
+
 }  // namespace
 
 namespace fc {
@@ -750,11 +831,11 @@ int attention_ws_launch(fc_ctx* ctx, cudaStream_t st, const AttnGeom& g, const C
   const int pk = tk0 ? split.pack : 1;
   int64_t max_items = 0;
   for (int c = 0; c < g.W; ++c) max_items += ((int64_t)(g.q_row_off[c + 1] - g.q_row_off[c]) * pk + 2 * kBM - 1) / (2 * kBM);
-  const int64_t items = max_items * (g.H_q / pk) * (tk0 ? split.n_splits : 1);
+  const int64_t items = max_items * (g.H_q / pk);
   if (items == 0) return FC_OK;
-  if (items > INT32_MAX) return FC_ERR_UNSUPPORTED;
+  if (items > INT32_MAX / kMaxParts) return FC_ERR_UNSUPPORTED;
   if (!split.follows) FC_CUDA_CHECK(cudaMemsetAsync(counter, 0, sizeof(uint32_t), st));
-  const int grid = (int)std::min<int64_t>(items, (int64_t)ctx->sm_count);
+  const int grid = split.slots > 0 ? ctx->sm_count : (int)std::min<int64_t>(items, (int64_t)ctx->sm_count);
   // at least half of the shared memory, so that a second CTA (and its 512 columns) never joins the SM
   const size_t need = (2 + 2 * kStages) * (size_t)kBM * g.d * 2 + sizeof(WsSmem) + 1024;
   const size_t smem = std::max<size_t>(need, 120 * 1024);
@@ -773,6 +854,12 @@ int attention_ws_launch(fc_ctx* ctx, cudaStream_t st, const AttnGeom& g, const C
   else rc = g.d == 128 ? launch(attention_ws_kernel<128, kSegments>) : launch(attention_ws_kernel<64, kSegments>);
   if (rc != FC_OK) return rc;
   FC_LAUNCH_CHECK("attention_ws_kernel");
+  if (split.slots > 0) {
+    const dim3 rows((unsigned)std::min<int64_t>(items, grid), 2 * kBM / 8);
+    if (g.d == 128) FC_CUDA_CHECK(launch_pdl(attention_join_kernel<128>, rows, dim3(256), 0, st, g, split, (__nv_bfloat16*)O));
+    else FC_CUDA_CHECK(launch_pdl(attention_join_kernel<64>, rows, dim3(256), 0, st, g, split, (__nv_bfloat16*)O));
+    FC_LAUNCH_CHECK("attention_join_kernel");
+  }
   return FC_OK;
 }
 

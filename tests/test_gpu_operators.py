@@ -422,6 +422,16 @@ def test_attention_visible_lengths(fc, ctx, dtype, impl):
     run_attention(fc, ctx, H_q=2, H_kv=2, d=64, lens=[2, 2], n_cache=9000, win=False, active=[0, 1], cut=[3, 9000], dtype=dtype, impl=impl)
 
 
+@pytest.mark.parametrize("case", [
+    dict(H_q=40, H_kv=40, lens=[1000], n_cache=1500, win=True, active=[0]),           # 160 items: 12 are cut where 148 fill a round
+    dict(H_q=80, H_kv=20, lens=[520, 30], n_cache=1300, win=True, active=[0, 1]),      # 200: the cut ones belong to both chunks
+    dict(H_q=3, H_kv=3, lens=[2600, 2600], n_cache=900, win=True, active=[1]),         # 33: every item is cut
+    dict(H_q=20, H_kv=20, lens=[256 * 7, 256], n_cache=1100, win=False, active=[0, 1]),  # 160, whole tiles only
+], ids=lambda c: f"{c['H_q']}-{c['H_kv']}")
+def test_attention_items_cut_into_parts(fc, ctx, case):
+    run_attention(fc, ctx, d=64, dtype=BF16, impl=2, **case)
+
+
 @pytest.mark.parametrize("rows", [3, 700])
 @pytest.mark.parametrize("dtype", [BF16, F32])
 def test_attention_strides_and_broadcast_heads(fc, ctx, dtype, rows):
