@@ -783,13 +783,22 @@ attention_join_kernel(const __grid_constant__ fc::AttnGeom g, const __grid_const
   constexpr int kLanes = D / 4, kGroups = 32 / kLanes;  // lanes of a part's row, parts at once
   const int lane = threadIdx.x % 32, item = blockIdx.x, r = blockIdx.y * 8 + threadIdx.x / 32;
   fc::pdl_wait();
-  const int n = split.plan[1];
-  if (item >= split.plan[0]) return;
-  const int c = split.plan[4 + 4 * item], h = split.plan[5 + 4 * item], v = split.plan[6 + 4 * item] + r, pk = split.pack;
-  if (v >= g.q_row_off[c + 1] * pk) return;
+  const int32_t* entry = split.plan + 4 + 4 * item;  // in the array whether or not so many items were cut
+  const int cut = split.plan[0], n = split.plan[1], c = entry[0], h = entry[1], v = entry[2] + r, pk = split.pack;
+  if (item >= cut || v >= g.q_row_off[c + 1] * pk) return;
   const int row = v / pk, head = pk > 1 ? h * pk + v % pk : h;
   const int64_t at = (int64_t)item * n * (2 * kBM) + r;  // of the first part; the others follow a tile pair apart
+  const int grp = lane / kLanes, d4 = lane % kLanes;
+  const float* src = split.o + (at + (int64_t)grp * (2 * kBM)) * D + 4 * d4;
+  constexpr int kAhead = 8;  // accesses sent for before the weights are worked out, and at a time
   const float2 ml = lane < n ? split.ml[at + (int64_t)lane * (2 * kBM)] : make_float2(-INFINITY, 0.f);
+  float4 y[kAhead];
+  auto load = [&](int p0) {
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i)
+      if (p0 + i * kGroups + grp < n) y[i] = *reinterpret_cast<const float4*>(src + (int64_t)(p0 + i * kGroups) * (2 * kBM) * D);
+  };
+  load(0);
   float m = ml.x;
 #pragma unroll
   for (int k = 16; k; k >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, k));
@@ -797,15 +806,16 @@ attention_join_kernel(const __grid_constant__ fc::AttnGeom g, const __grid_const
   float l = w == 0.f ? (ml.y == ml.y ? 0.f : ml.y) : w * ml.y;
 #pragma unroll
   for (int k = 16; k; k >>= 1) l += __shfl_xor_sync(0xffffffffu, l, k);
-  const int grp = lane / kLanes, d4 = lane % kLanes;
   float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 8
-  for (int p0 = 0; p0 < n; p0 += kGroups) {
-    const int p = p0 + grp;
-    const float wp = __shfl_sync(0xffffffffu, w, p & 31);
-    if (p < n) {
-      const float4 y = *reinterpret_cast<const float4*>(split.o + (at + (int64_t)p * (2 * kBM)) * D + 4 * d4);
-      o.x = fmaf(wp, y.x, o.x); o.y = fmaf(wp, y.y, o.y); o.z = fmaf(wp, y.z, o.z); o.w = fmaf(wp, y.w, o.w);
+  for (int p0 = 0; p0 < n; p0 += kAhead * kGroups) {
+    if (p0 > 0) load(p0);
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+      const int p = p0 + i * kGroups + grp;
+      const float wp = __shfl_sync(0xffffffffu, w, p & 31);
+      if (p < n) {
+        o.x = fmaf(wp, y[i].x, o.x); o.y = fmaf(wp, y[i].y, o.y); o.z = fmaf(wp, y[i].z, o.z); o.w = fmaf(wp, y[i].w, o.w);
+      }
     }
   }
   if (kGroups == 2) {
