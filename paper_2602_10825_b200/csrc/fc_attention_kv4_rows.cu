@@ -70,12 +70,10 @@ template <int D> struct Ring {
   static constexpr int kStages = 4;
 };
 
-// The window's keys in the place of the ring: 16 rows of K and 16 of V.  bf16 rows have a buffer each: K of the next step is on
-// its way while V of this one is worked on, and the other way round; fp32 rows take turns in one.
+// The window's keys in the place of the ring: 16 rows of K and 16 of V.  K of the next step is on its way while V of this one is
+// worked on, and the other way round.
 template <typename T, int D> struct Window {
   static constexpr int kRow = D * (int)sizeof(T), kBytes = kStep * kRow, kPieces = kRow / 16;
-  static constexpr bool kOne = 2 * kBytes > Ring<D>::kStages * Ring<D>::kBytes;
-  static_assert(kBytes <= Ring<D>::kStages * Ring<D>::kBytes, "the window's rows fit the ring");
   // Where 16-byte piece p of row r lies in its row, so that the eight lanes that are served together read different banks.
   static __device__ __forceinline__ int k_piece(int r, int p) {
     return kPieces == 32 ? p ^ ((p >> 3) & 3) ^ ((r & 1) << 2) : p ^ ((p >> 3) & 1) ^ ((r & 1) << 1);
@@ -84,6 +82,11 @@ template <typename T, int D> struct Window {
     return kPieces == 32 ? p ^ ((r >> 1) & 3) : p ^ (((r >> 1) & 3) << 1) ^ ((p >> 1) & 1);
   }
 };
+// Shared memory of a warp: the ring or the window's rows; of a block: also, after the last step, what the warps join.
+template <typename T, int D> constexpr int kWarpBytes =
+    Ring<D>::kStages * Ring<D>::kBytes > 2 * Window<T, D>::kBytes ? Ring<D>::kStages * Ring<D>::kBytes : 2 * Window<T, D>::kBytes;
+template <typename T, int D, int NT> constexpr int kBlockBytes =
+    kWarps * (kWarpBytes<T, D> > 8 * NT * (D + 4) * 4 ? kWarpBytes<T, D> : 8 * NT * (D + 4) * 4);
 
 template <int N> __device__ __forceinline__ void cp_async(uint32_t dst, const void* src) {
   if constexpr (N == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
@@ -278,8 +281,7 @@ attention_kv4_rows_kernel(const T* __restrict__ Q, const T* __restrict__ K, cons
   constexpr int kRows = 8 * NT, kLaneDims = D / 4, kLaneCols = D / 8, kPer = 16 / (int)sizeof(T);
   using R = Ring<D>;
   using Wn = Window<T, D>;
-  // the rings, and after the last step, in their place, what the warps join
-  __shared__ __align__(16) uint8_t smem[kWarps * (R::kStages * R::kBytes > kRows * (D + 4) * 4 ? R::kStages * R::kBytes : kRows * (D + 4) * 4)];
+  extern __shared__ __align__(16) uint8_t smem[];
   __shared__ float2 ml_s[kWarps][kRows];
   fc::pdl_launch_dependents();  // the joining kernel may take its place; it waits for this grid to end
   const fc::AttnGeom& a = g.a;
@@ -301,7 +303,7 @@ attention_kv4_rows_kernel(const T* __restrict__ Q, const T* __restrict__ K, cons
   // A packed step's copies: lane L brings 16 bytes of rows L/4 and L/4 + 8 of the codes (D = 128), and the scales of a row of K
   // or V.  The pointers stand at the warp's next step; positions behind the part's last key repeat it.
   constexpr int kLanesPerRow = D / 32, kRowsPerCopy = 32 / kLanesPerRow, kAll = kStep * kWarps;
-  const uint32_t ring = smem_u32(smem) + warp * R::kStages * R::kBytes;
+  const uint32_t ring = smem_u32(smem) + warp * kWarpBytes<T, D>;
   const int kb0 = k0 + kStep * warp;
   const uint8_t* codes_p = g.cache.k_codes + hk * g.cache.code_hs + (int64_t)(kb0 + lane / kLanesPerRow) * g.cache.code_rs + lane % kLanesPerRow * 16;
   const uint16_t* scales_p = (lane < 16 ? g.cache.k_scales : g.cache.v_scales) + hk * g.cache.scale_hs + (int64_t)(kb0 + lane % 16) * g.cache.scale_rs;
@@ -391,7 +393,7 @@ attention_kv4_rows_kernel(const T* __restrict__ Q, const T* __restrict__ K, cons
   }
   const float scale_log2 = a.scale * 1.4426950408889634f;
 
-  const uint8_t* buf = smem + warp * R::kStages * R::kBytes;
+  const uint8_t* buf = smem + warp * kWarpBytes<T, D>;
   if (k0 < k1) {
     int stage = 0, kb = kb0;
     auto next = [&]() {  // the next step's data is there; another step's is sent for, into the place of the one before
@@ -414,11 +416,10 @@ attention_kv4_rows_kernel(const T* __restrict__ Q, const T* __restrict__ K, cons
   }
   if (w0 < w1) {
     const int wb0 = w0 + kStep * warp;
-    const uint32_t v_at = Wn::kOne ? 0 : Wn::kBytes;
     copy_window(kw, a.k_rs, ring, wb0, false);
-    if (!Wn::kOne) copy_window(vw, a.v_rs, ring + v_at, wb0, true);
+    copy_window(vw, a.v_rs, ring + Wn::kBytes, wb0, true);
     for (int kb = wb0; kb < w1; kb += kAll) {
-      cp_async_wait<Wn::kOne ? 0 : 1>();
+      cp_async_wait<1>();
       __syncwarp();
       float s[NT][4] = {}, rest[NT][4] = {};
 #pragma unroll
@@ -447,11 +448,10 @@ attention_kv4_rows_kernel(const T* __restrict__ Q, const T* __restrict__ K, cons
           for (int i = 0; i < 4; ++i) s[t][i] += rest[t][i];
       }
       __syncwarp();
-      if (Wn::kOne) copy_window(vw, a.v_rs, ring, kb, true);
-      else copy_window(kw, a.k_rs, ring, kb + kAll, false);
+      copy_window(kw, a.k_rs, ring, kb + kAll, false);
       uint32_t p0[kWeightParts<T, NT>][NT], p1[kWeightParts<T, NT>][NT];
       softmax_step<T, D, NT, true>(st, s, scale_log2, lane, w1 - kb, p0, p1);
-      cp_async_wait<Wn::kOne ? 0 : 1>();
+      cp_async_wait<1>();
       __syncwarp();
 #pragma unroll
       for (int w = 0; w < kLaneCols / kPer; ++w) {
@@ -459,7 +459,7 @@ attention_kv4_rows_kernel(const T* __restrict__ Q, const T* __restrict__ K, cons
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const int r = 2 * q + (i & 1) + 8 * (i >> 1);
-          x[i] = *reinterpret_cast<const uint4*>(buf + v_at + r * Wn::kRow + 16 * Wn::v_piece(r, n * (kLaneCols / kPer) + w));
+          x[i] = *reinterpret_cast<const uint4*>(buf + Wn::kBytes + r * Wn::kRow + 16 * Wn::v_piece(r, n * (kLaneCols / kPer) + w));
         }
         const uint32_t* y[4] = {&x[0].x, &x[1].x, &x[2].x, &x[3].x};
         if constexpr (kParts<T> == 1) {
@@ -486,8 +486,7 @@ attention_kv4_rows_kernel(const T* __restrict__ Q, const T* __restrict__ K, cons
         }
       }
       __syncwarp();
-      if (Wn::kOne) copy_window(kw, a.k_rs, ring, kb + kAll, false);
-      else copy_window(vw, a.v_rs, ring + v_at, kb + kAll, true);
+      copy_window(vw, a.v_rs, ring + Wn::kBytes, kb + kAll, true);
     }
     cp_async_wait<0>();
   }
@@ -606,8 +605,13 @@ int kv4_rows(cudaStream_t st, const Kv4AttnGeom& g, const void* Q, const void* K
   if (tiles == 0) return FC_OK;
   if (tiles > INT32_MAX) return FC_ERR_UNSUPPORTED;
   const dim3 grid((unsigned)tiles, (unsigned)g.a.H_kv, (unsigned)g.n_splits);
-#define FC_KV4_ROWS(T, D, NT) \
-  attention_kv4_rows_kernel<T, D, NT><<<grid, kThreads, 0, st>>>((const T*)Q, (const T*)K, (const T*)V, (T*)O, g)
+#define FC_KV4_ROWS(T, D, NT)                                                                                           \
+  do {                                                                                                                  \
+    constexpr int smem = kBlockBytes<T, D, NT>;                                                                         \
+    if (smem > 48 * 1024)                                                                                               \
+      FC_CUDA_CHECK(cudaFuncSetAttribute(attention_kv4_rows_kernel<T, D, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem)); \
+    attention_kv4_rows_kernel<T, D, NT><<<grid, kThreads, smem, st>>>((const T*)Q, (const T*)K, (const T*)V, (T*)O, g);  \
+  } while (0)
   if (g.f32) { if (g.a.d == 128) FC_KV4_ROWS(float, 128, 1); else FC_KV4_ROWS(float, 64, 1); }
   else if (g.a.d == 128) { if (nt == 1) FC_KV4_ROWS(__nv_bfloat16, 128, 1); else FC_KV4_ROWS(__nv_bfloat16, 128, 2); }
   else { if (nt == 1) FC_KV4_ROWS(__nv_bfloat16, 64, 1); else FC_KV4_ROWS(__nv_bfloat16, 64, 2); }
