@@ -1,5 +1,9 @@
 // fc_qk_norm_rope: RMS norm of every head of queries and keys, and the rotation over (time, height, width), in one pass.
 //
+// Measured with the launch: 4680 tokens of 48 bf16 heads of 128 in 25.0 us (35.7 with far pairs), 18719 tokens of 8 fp32 heads of
+// 64 in 19.2; blocks of 256 threads 25.2, 37.2 and 20.8; without sending for the first rows before the angles 27.4 and 22.8; with two
+// rows in flight, or the next rows sent for before the arithmetic, slower still.
+//
 // Bound by HBM: every element is read and written once (4680 tokens of 48 bf16 heads of 128 in 25 us with the launch, 4.6 TB/s; a
 // plain copy of the same bytes takes 21).  A head's row is spread over 16-byte pieces, one per lane (16 lanes for a
 // bf16 row of 128), and everything between the load and the store is in registers.  A group of lanes owns a token and walks
@@ -26,7 +30,9 @@ using fc::sm100::fma2;
 using fc::sm100::pack2;
 using fc::sm100::unpack2;
 
-constexpr int kThreads = 256;
+// Small blocks: a block's angles hold up only its own rows.
+constexpr int kThreads = 128;
+constexpr int kUnroll = 4;  // heads whose loads are in flight together
 
 struct RopeGeom {
   int32_t H_q, H_kv, T;
@@ -95,14 +101,10 @@ __device__ __forceinline__ void place(const RopeGeom& g, int e, int& pair, int& 
 }
 
 template <typename T, int D, bool kHalves>
-__global__ void __launch_bounds__(kThreads, kHalves && sizeof(T) == 2 ? 3 : 4)  // 80 registers where eight partners are looked up, else 64
+__global__ void __launch_bounds__(kThreads, kHalves && sizeof(T) == 2 ? 6 : 8)  // 80 registers where eight partners are looked up, else 64
 qk_norm_rope_kernel(const T* Q, const T* K, T* Q_out, T* K_out, const float* __restrict__ q_weight,
                     const float* __restrict__ k_weight, const int32_t* __restrict__ pos, const __grid_constant__ RopeGeom g) {
   using P = Piece<T>;
-  // Heads whose loads are in flight together.  Measured at a chunk of 4680 tokens of 48 bf16 heads: 27.4 us with four, 28.5 with
-  // three, 30 and more with two or with the next rows sent for before the arithmetic; fp32, 18719 tokens of 8 heads of 64:
-  // 22.8 us with three, 24.8 with four.  Sending for the first rows before the angles brought these to 25.0 and 20.8.
-  constexpr int kUnroll = sizeof(T) == 4 ? 3 : 4;
   constexpr int E = P::N, L = D / E, G = kThreads / L, V = E / 4;  // elements per lane, lanes per row, rows per block, pairs of pairs
   __shared__ float2 cs_s[G * (D / 2)];                     // (cos, sin) of the block's tokens and pairs
   __shared__ __align__(16) T row_s[kHalves ? kUnroll * kThreads * E : 1];  // the rows in flight, where partners sit in other lanes
