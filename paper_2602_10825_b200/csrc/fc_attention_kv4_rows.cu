@@ -116,11 +116,9 @@ template <int D, int NT> struct State {
   float l[NT][2], ref[NT][2], move_at[NT][2];
 };
 
-// S^T -> P^T operands.  n_valid: keys of the step that exist (kTail only).
-template <typename T, int D, int NT, bool kTail>
-__device__ __forceinline__ void softmax_step(State<D, NT>& st, float (&s)[NT][4], float scale_log2, int lane, int n_valid,
-                                             uint32_t (&p0)[kWeightParts<T, NT>][NT],
-                                             uint32_t (&p1)[kWeightParts<T, NT>][NT]) {
+// S^T -> P^T operands, in two halves: the maxima (n_valid: keys of the step that exist, kTail only), and the weights.
+template <int D, int NT, bool kTail>
+__device__ __forceinline__ void move_maximum(State<D, NT>& st, float (&s)[NT][4], float scale_log2, int lane, int n_valid) {
   bool move = false;
 #pragma unroll
   for (int t = 0; t < NT; ++t) {
@@ -155,6 +153,10 @@ __device__ __forceinline__ void softmax_step(State<D, NT>& st, float (&s)[NT][4]
         }
       }
   }
+}
+template <typename T, int D, int NT>
+__device__ __forceinline__ void weights(State<D, NT>& st, const float (&s)[NT][4], float scale_log2,
+                                        uint32_t (&p0)[kWeightParts<T, NT>][NT], uint32_t (&p1)[kWeightParts<T, NT>][NT]) {
 #pragma unroll
   for (int t = 0; t < NT; ++t) {
     const float e0 = ex2(fmaf(s[t][0], scale_log2, -st.ref[t][0])), e1 = ex2(fmaf(s[t][1], scale_log2, -st.ref[t][1]));
@@ -214,32 +216,29 @@ __device__ __forceinline__ void weigh(float (&o)[4], const uint32_t (&v)[NV][4],
   }
 }
 
-// One step over 16 packed keys, which lie at `buf`.
-template <typename T, int D, int NT, bool kTail>
-__device__ __forceinline__ void packed_step(State<D, NT>& st, const uint8_t* buf, const uint32_t (&qb)[kParts<T>][NT][D / 8],
-                                            float scale_log2, int lane, int n_valid) {
+// One step over 16 packed keys, which lie at `buf`, in two halves: S^T, and O^T += V^T P^T.
+template <typename T, int D, int NT>
+__device__ __forceinline__ void packed_logits(float (&s)[NT][4], const uint8_t* buf, const uint32_t (&qb)[kParts<T>][NT][D / 8], int lane) {
   using R = Ring<D>;
   const int n = lane >> 2, q = lane & 3;
   const uint8_t* kc = buf + n * (D / 2) + q * (D / 8);
-  const uint8_t* vc = buf + R::kCodes + 2 * q * (D / 2) + n * (D / 16);
   const uint16_t* ks = reinterpret_cast<const uint16_t*>(buf + 2 * R::kCodes) + n * (D / 32) + q * D / 128;
-  const uint16_t* vs = reinterpret_cast<const uint16_t*>(buf + 2 * R::kCodes + R::kScales) + 2 * q * (D / 32) + n * D / 256;
-  float s[NT][4] = {}, rest[NT][4] = {};
-  {
-    uint32_t k0[D / 32], k1[D / 32];
-    lds_words(kc, k0);
-    lds_words(kc + 8 * (D / 2), k1);
-    const uint32_t s0 = fc::kv4_scale2(ks[0]), s1 = fc::kv4_scale2(ks[8 * (D / 32)]);
-    const uint32_t b0 = fc::kv4_bias2(s0), b1 = fc::kv4_bias2(s1);
+  float rest[NT][4] = {};
+  uint32_t k0[D / 32], k1[D / 32];
+  lds_words(kc, k0);
+  lds_words(kc + 8 * (D / 2), k1);
+  const uint32_t s0 = fc::kv4_scale2(ks[0]), s1 = fc::kv4_scale2(ks[8 * (D / 32)]);
+  const uint32_t b0 = fc::kv4_bias2(s0), b1 = fc::kv4_bias2(s1);
 #pragma unroll
-    for (int w = 0; w < D / 32; ++w) {
-      uint32_t x[4], y[4];
-      fc::kv4_word(k0[w], s0, b0, x);
-      fc::kv4_word(k1[w], s1, b1, y);
-      const uint32_t lo[1][4] = {{x[0], y[0], x[1], y[1]}}, hi[1][4] = {{x[2], y[2], x[3], y[3]}};
-      logits<T, D>(s, rest, lo, qb, 4 * w);
-      logits<T, D>(s, rest, hi, qb, 4 * w + 2);
-    }
+  for (int t = 0; t < NT; ++t) s[t][0] = s[t][1] = s[t][2] = s[t][3] = 0.f;
+#pragma unroll
+  for (int w = 0; w < D / 32; ++w) {
+    uint32_t x[4], y[4];
+    fc::kv4_word(k0[w], s0, b0, x);
+    fc::kv4_word(k1[w], s1, b1, y);
+    const uint32_t lo[1][4] = {{x[0], y[0], x[1], y[1]}}, hi[1][4] = {{x[2], y[2], x[3], y[3]}};
+    logits<T, D>(s, rest, lo, qb, 4 * w);
+    logits<T, D>(s, rest, hi, qb, 4 * w + 2);
   }
   if constexpr (kParts<T> > 1) {
 #pragma unroll
@@ -247,12 +246,19 @@ __device__ __forceinline__ void packed_step(State<D, NT>& st, const uint8_t* buf
 #pragma unroll
       for (int i = 0; i < 4; ++i) s[t][i] += rest[t][i];
   }
+}
+template <typename T, int D, int NT>
+__device__ __forceinline__ void packed_weigh(State<D, NT>& st, const uint8_t* buf, const float (&s)[NT][4], float scale_log2, int lane) {
+  using R = Ring<D>;
+  const int n = lane >> 2, q = lane & 3;
+  const uint8_t* vc = buf + R::kCodes + 2 * q * (D / 2) + n * (D / 16);
+  const uint16_t* vs = reinterpret_cast<const uint16_t*>(buf + 2 * R::kCodes + R::kScales) + 2 * q * (D / 32) + n * D / 256;
   uint32_t v[4][D / 64], p0[kWeightParts<T, NT>][NT], p1[kWeightParts<T, NT>][NT];
 #pragma unroll
   for (int i = 0; i < 4; ++i) lds_words(vc + ((i & 1) + 8 * (i >> 1)) * (D / 2), v[i]);
   const uint32_t sl = vs[0] | ((uint32_t)vs[D / 32] << 16), sh = vs[8 * (D / 32)] | ((uint32_t)vs[9 * (D / 32)] << 16);
   const uint32_t bl = fc::kv4_bias2(sl), bh = fc::kv4_bias2(sh);
-  softmax_step<T, D, NT, kTail>(st, s, scale_log2, lane, n_valid, p0, p1);
+  weights<T, D, NT>(st, s, scale_log2, p0, p1);
 #pragma unroll
   for (int w = 0; w < D / 64; ++w) {
     uint32_t el[4], ol[4], eh[4], oh[4];  // even and odd elements, low and high keys
@@ -351,7 +357,7 @@ attention_kv4_rows_kernel(const T* __restrict__ Q, const T* __restrict__ K, cons
   const T* vw = V + hk * a.v_hs;
   if (k0 < k1) {
 #pragma unroll
-    for (int i = 0; i < R::kStages - 1; ++i) copy(i, kb0 + i * kAll);
+    for (int i = 0; i < R::kStages; ++i) copy(i, kb0 + i * kAll);
   }
   // everything up to here reads only what the host knows; the list is on the device
   if (part == 0 && hk == 0 && blockIdx.x == 0 && tid == 0) fc::report_bad_ids(a);
@@ -395,24 +401,45 @@ attention_kv4_rows_kernel(const T* __restrict__ Q, const T* __restrict__ K, cons
 
   const uint8_t* buf = smem + warp * kWarpBytes<T, D>;
   if (k0 < k1) {
+    // The products of one step with the keys come between the maxima of the step before and its weights, so that the two
+    // steps' chains of instructions fill each other's gaps.
     int stage = 0, kb = kb0;
-    auto next = [&]() {  // the next step's data is there; another step's is sent for, into the place of the one before
-      copy((stage + R::kStages - 1) % R::kStages, kb + (R::kStages - 1) * kAll);
+    float s[NT][4], s_next[NT][4];
+    auto at = [&](int step) { return buf + (stage + step) % R::kStages * R::kBytes; };
+    auto done = [&]() {  // the step's place has been read by every lane: another step is sent for
+      __syncwarp();
+      copy(stage, kb + R::kStages * kAll);
+      stage = (stage + 1) % R::kStages;
+      kb += kAll;
+    };
+    if (kb + kStep <= k1) {
       cp_async_wait<R::kStages - 1>();
       __syncwarp();
-    };
-    for (; kb + kStep <= k1; kb += kAll) {
-      next();
-      packed_step<T, D, NT, false>(st, buf + stage * R::kBytes, qb, scale_log2, lane, kStep);
-      __syncwarp();  // the stage has been read by every lane before it is filled again
-      stage = (stage + 1) % R::kStages;
-    }
-    if (kb < k1) {
-      next();
-      packed_step<T, D, NT, true>(st, buf + stage * R::kBytes, qb, scale_log2, lane, k1 - kb);
+      packed_logits<T, D, NT>(s, at(0), qb, lane);
+      for (; kb + kAll + kStep <= k1;) {
+        move_maximum<D, NT, false>(st, s, scale_log2, lane, kStep);
+        cp_async_wait<R::kStages - 2>();
+        __syncwarp();
+        packed_logits<T, D, NT>(s_next, at(1), qb, lane);
+        packed_weigh<T, D, NT>(st, at(0), s, scale_log2, lane);
+        done();
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) s[t][i] = s_next[t][i];
+      }
+      move_maximum<D, NT, false>(st, s, scale_log2, lane, kStep);
+      packed_weigh<T, D, NT>(st, at(0), s, scale_log2, lane);
+      done();
     }
     cp_async_wait<0>();
     __syncwarp();
+    if (kb < k1) {
+      packed_logits<T, D, NT>(s, at(0), qb, lane);
+      move_maximum<D, NT, true>(st, s, scale_log2, lane, k1 - kb);
+      packed_weigh<T, D, NT>(st, at(0), s, scale_log2, lane);
+      __syncwarp();
+    }
   }
   if (w0 < w1) {
     const int wb0 = w0 + kStep * warp;
@@ -450,7 +477,8 @@ attention_kv4_rows_kernel(const T* __restrict__ Q, const T* __restrict__ K, cons
       __syncwarp();
       copy_window(kw, a.k_rs, ring, kb + kAll, false);
       uint32_t p0[kWeightParts<T, NT>][NT], p1[kWeightParts<T, NT>][NT];
-      softmax_step<T, D, NT, true>(st, s, scale_log2, lane, w1 - kb, p0, p1);
+      move_maximum<D, NT, true>(st, s, scale_log2, lane, w1 - kb);
+      weights<T, D, NT>(st, s, scale_log2, p0, p1);
       cp_async_wait<1>();
       __syncwarp();
 #pragma unroll
