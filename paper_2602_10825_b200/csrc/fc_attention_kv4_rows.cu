@@ -359,13 +359,6 @@ attention_kv4_rows_kernel(const T* __restrict__ Q, const T* __restrict__ K, cons
 #pragma unroll
     for (int i = 0; i < R::kStages; ++i) copy(i, kb0 + i * kAll);
   }
-  // everything up to here reads only what the host knows; the list is on the device
-  if (part == 0 && hk == 0 && blockIdx.x == 0 && tid == 0) fc::report_bad_ids(a);
-  if (!fc::chunk_active(a, c)) {
-    cp_async_wait<0>();
-    return;
-  }
-
   uint32_t qb[kParts<T>][NT][kLaneDims / 2];
 #pragma unroll
   for (int t = 0; t < NT; ++t) {
@@ -389,6 +382,13 @@ attention_kv4_rows_kernel(const T* __restrict__ Q, const T* __restrict__ K, cons
       }
     }
   }
+  // everything up to here reads only what the host knows; the list is on the device
+  if (part == 0 && hk == 0 && blockIdx.x == 0 && tid == 0) fc::report_bad_ids(a);
+  if (!fc::chunk_active(a, c)) {
+    cp_async_wait<0>();
+    return;
+  }
+
   State<D, NT> st;
 #pragma unroll
   for (int t = 0; t < NT; ++t) {

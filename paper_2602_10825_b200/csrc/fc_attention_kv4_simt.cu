@@ -188,6 +188,14 @@ kv4_combine_kernel(T* __restrict__ O, const __grid_constant__ fc::Kv4AttnGeom g)
   const int64_t at = (hk * g.n_vrows + vr) * g.n_splits;
   auto power = [](float x) { return kLog2 ? exp2f(x) : expf(x); };
 
+  // the first parts are sent for before their weights are worked out
+  const int grp = tid / kLanes, d4 = tid % kLanes;
+  constexpr int kAhead = 4;
+  float4 y[kAhead];
+#pragma unroll
+  for (int i = 0; i < kAhead; ++i)
+    if (grp + i * kGroups < g.n_splits) y[i] = *reinterpret_cast<const float4*>(g.part_o + (at + grp + i * kGroups) * D + 4 * d4);
+
   float m = -INFINITY;
   float2 mine[(fc::kKv4MaxSplits + kCombineThreads - 1) / kCombineThreads];
 #pragma unroll
@@ -218,10 +226,15 @@ kv4_combine_kernel(T* __restrict__ O, const __grid_constant__ fc::Kv4AttnGeom g)
 #pragma unroll
   for (int w = 0; w < kWarps; ++w) l += l_s[w];
 
-  const int grp = tid / kLanes, d4 = tid % kLanes;
   float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+  for (int i = 0; i < kAhead; ++i)
+    if (grp + i * kGroups < g.n_splits) {
+      const float w = w_s[grp + i * kGroups];
+      o.x = fmaf(w, y[i].x, o.x); o.y = fmaf(w, y[i].y, o.y); o.z = fmaf(w, y[i].z, o.z); o.w = fmaf(w, y[i].w, o.w);
+    }
 #pragma unroll 4
-  for (int p = grp; p < g.n_splits; p += kGroups) {
+  for (int p = grp + kAhead * kGroups; p < g.n_splits; p += kGroups) {
     const float4 x = *reinterpret_cast<const float4*>(g.part_o + (at + p) * D + 4 * d4);
     const float w = w_s[p];
     o.x = fmaf(w, x.x, o.x); o.y = fmaf(w, x.y, o.y); o.z = fmaf(w, x.z, o.z); o.w = fmaf(w, x.w, o.w);
