@@ -785,7 +785,9 @@ attention_join_kernel(const __grid_constant__ fc::AttnGeom g, const __grid_const
   fc::pdl_wait();
   const int32_t* entry = split.plan + 4 + 4 * item;  // in the array whether or not so many items were cut
   const int cut = split.plan[0], n = split.plan[1], c = entry[0], h = entry[1], v = entry[2] + r, pk = split.pack;
-  if (item >= cut || v >= g.q_row_off[c + 1] * pk) return;
+  // A block of the kernel before that gave up on a wait may have left its items' entries unwritten: those name no row.
+  if (item >= cut || (uint32_t)c >= (uint32_t)g.W || (uint32_t)h >= (uint32_t)(g.H_q / pk) || entry[2] < g.q_row_off[c] * pk) return;
+  if (v >= g.q_row_off[c + 1] * pk) return;
   const int row = v / pk, head = pk > 1 ? h * pk + v % pk : h;
   const int64_t at = (int64_t)item * n * (2 * kBM) + r;  // of the first part; the others follow a tile pair apart
   const int grp = lane / kLanes, d4 = lane % kLanes;
