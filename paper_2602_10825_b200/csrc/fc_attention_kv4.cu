@@ -170,6 +170,7 @@ extern "C" int fc_chunk_attention_kv4(fc_ctx* ctx, void* stream, const fc_attn_d
     }
     window = seg_logical_off[n_seg];
   }
+  if (n_cache + window > INT32_MAX - 4096) return FC_ERR_UNSUPPORTED;  // logical offsets of the two stores together are 32-bit
   for (int c = 0; c < a.W; ++c)
     if (a.vis[c] > n_cache + window) return FC_ERR_INVALID_ARG;
   if (lse && lse_hs <= 0) return FC_ERR_INVALID_ARG;

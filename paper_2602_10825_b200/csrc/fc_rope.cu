@@ -1,11 +1,7 @@
 // fc_qk_norm_rope: RMS norm of every head of queries and keys, and the rotation over (time, height, width), in one pass.
 //
-// Measured with the launch: 4680 tokens of 48 bf16 heads of 128 in 25.0 us (35.7 with far pairs), 18719 tokens of 8 fp32 heads of
-// 64 in 19.2; blocks of 256 threads 25.2, 37.2 and 20.8; without sending for the first rows before the angles 27.4 and 22.8; with two
-// rows in flight, or the next rows sent for before the arithmetic, slower still.
-//
-// Bound by HBM: every element is read and written once (4680 tokens of 48 bf16 heads of 128 in 25 us with the launch, 4.6 TB/s; a
-// plain copy of the same bytes takes 21).  A head's row is spread over 16-byte pieces, one per lane (16 lanes for a
+// Bound by HBM: every element is read and written once (4680 tokens of 48 bf16 heads of 128 at 4.6 TB/s, launch included; a
+// plain copy of the same bytes takes 21 us).  A head's row is spread over 16-byte pieces, one per lane (16 lanes for a
 // bf16 row of 128), and everything between the load and the store is in registers.  A group of lanes owns a token and walks
 // over some of its heads, four rows' loads in flight.  What it takes to stay under the copy rate is few instructions:
 //   - The cosines and sines of a token serve all its heads.  A block computes them once for its tokens, a pair a thread, and
@@ -16,6 +12,10 @@
 //     memory as they are, and the partners are read one by one.
 // Angles: a pair's frequency is held in turns as a 64-bit fixed-point fraction, so position x frequency is one wrapping
 // integer product whose overflow is exactly the reduction modulo a full turn; its top 32 bits go to sincospif.
+//
+// Measured with the launch: 4680 tokens of 48 bf16 heads of 128 in 25.0 us (35.7 with far pairs), 18719 tokens of 8 fp32 heads of
+// 64 in 19.2; blocks of 256 threads 25.2, 37.2 and 20.8; without sending for the first rows before the angles 27.4 and 22.8; with two
+// rows in flight, or the next rows sent for before the arithmetic, slower still.
 #include <climits>
 #include <cmath>
 
