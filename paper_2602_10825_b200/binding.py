@@ -166,10 +166,13 @@ class Kv4Cache:
     """A 4-bit store of K and V rows (fc_kv4_cache): codes uint8 [H, rows, d/2] and scales bf16 [H, rows, d/32].
 
     Strided views (a slice of a larger store) are fine as long as K and V share strides and the last dimensions are
-    contiguous; the format is described in include/fc.h."""
+    contiguous; the format is described in include/fc.h.  The four tensors are fixed, and so is their memory (their contents are
+    not): build another store, which costs a microsecond or two, to use others."""
+
+    k_codes, k_scales, v_codes, v_scales = (property(lambda self, i=i: self._tensors[i]) for i in range(4))
 
     def __init__(self, k_codes, k_scales, v_codes, v_scales):
-        self.k_codes, self.k_scales, self.v_codes, self.v_scales = k_codes, k_scales, v_codes, v_scales
+        self._tensors = k_codes, k_scales, v_codes, v_scales
         shape, s_shape, strides, s_strides = k_codes.shape, k_scales.shape, k_codes.stride(), k_scales.stride()
         if len(shape) != 3 or len(s_shape) != 3:
             raise FcError("codes and scales must be [heads, rows, ...]")

@@ -143,6 +143,20 @@ def test_attention_refusals(L, ctx, kw, want):
     assert attn(L, ctx, **kw) == want
 
 
+def test_attention_refuses_offsets_that_pass_32_bits(L, ctx):
+    n = 2 ** 31 - 4097
+    assert attn(L, ctx, n_cache=n, cache=store(rows=n), ws=None) == UNSUPPORTED  # and ten tokens of a window behind them
+
+
+def test_a_store_keeps_its_tensors():
+    torch = pytest.importorskip("torch")
+    s = fc.Kv4Cache.empty(2, 5, 64, device="cpu")
+    assert s.k_codes.shape == (2, 5, 32) and s.v_scales.shape == (2, 5, 2) and (s.H, s.rows, s.d) == (2, 5, 64)
+    for name in ("k_codes", "k_scales", "v_codes", "v_scales"):
+        with pytest.raises(AttributeError):
+            setattr(s, name, torch.zeros_like(getattr(s, name)))
+
+
 def test_attention_no_rows_and_workspace(L, ctx):
     assert attn(L, ctx, off=(3, 3, 3), Q=None, O=None, ids=None, n_active=None) == 0
     desc = b._AttnDesc(H_q=4, H_kv=2, d=128, W=1)
