@@ -19,6 +19,7 @@ struct Kv4AttnGeom {
   int32_t n_splits;  // parts the keys are cut into, at most kKv4MaxSplits
   int64_t part_keys;    // keys per part (few-row kernel: on its axis of costs)
   int64_t n_cache_ceil; // few-row kernel: where the window starts on that axis
+  int32_t row_tiles;    // few-row kernel: rows of a tile / 8
   double rows_us;       // few-row kernel: estimate of the whole call
   int64_t n_vrows;   // virtual rows per key head, all chunks
   float* part_o;     // [H_kv, n_vrows, n_splits, d] unnormalised outputs, used if n_splits > 1

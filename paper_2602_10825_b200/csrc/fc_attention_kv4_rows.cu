@@ -571,17 +571,56 @@ attention_kv4_rows_kernel(const T* __restrict__ Q, const T* __restrict__ K, cons
   }
 }
 
-// Rows per tile / 8: one where no chunk has more than eight rows, and for fp32 (whose Q takes three times the registers), else two.
-int tiles_of(const fc::Kv4AttnGeom& g) {
-  if (g.f32) return 1;
-  for (int c = 0; c < g.a.W; ++c)
-    if ((int64_t)(g.a.q_row_off[c + 1] - g.a.q_row_off[c]) * g.a.group > 8) return 2;
-  return 1;
+// Measured on B200: what a step of a block's four warps takes for every block of the SM it runs on.  Sixteen bf16 rows take as long
+// as eight; in fp32 a second set of eight costs two thirds of the first (the keys are unpacked or cut into parts once).
+double step_us(const fc::Kv4AttnGeom& g, int nt) {
+  if (!g.f32) return g.a.d == 128 ? 0.30 : 0.18;
+  return (g.a.d == 128 ? 0.40 : 0.20) * (nt == 2 ? 1.65 : 1.0);
 }
 
-// Measured on B200: what a step of a block's four warps takes for every block of the SM it runs on, whether eight or sixteen
-// rows ride along.
-double step_us(const fc::Kv4AttnGeom& g) { return g.a.d == 128 ? (g.f32 ? 0.40 : 0.30) : (g.f32 ? 0.20 : 0.18); }
+// The split of the keys for tiles of 8 nt rows: the number of parts is the one that should be fastest.  A part is at least two
+// steps; joining the parts costs a kernel and their bytes.  Where all blocks are resident at once, the fullest SM counts (one or
+// two blocks on an SM take 1.35 or 1.08 times their share of a full one); otherwise all the work does, half a part more for the
+// blocks that end last (the chunk that sees least comes last), and 3 us for each set of blocks to start and end.  fp32 parts in several
+// sets take 4 us more, measured (100 rows of 8 heads on 2 over 1100 keys: one part 36 us, two 42, three 41).
+struct Split {
+  double us;
+  int64_t part_keys;
+  int32_t n;
+};
+constexpr int64_t kUnit = kStep * kWarps;
+
+Split split_of(const fc_ctx* ctx, const fc::Kv4AttnGeom& g, int nt, int vis) {
+  const int64_t tiles = fc::tile_count(g.a, 8 * nt) * g.a.H_kv;
+  auto units_of = [&](int v) {
+    const int64_t window = std::max(v - g.n_cache, 0);
+    return ((window > 0 ? ((int64_t)g.n_cache + kUnit - 1) / kUnit * kUnit : std::min(v, g.n_cache)) + kWindowCost * window + kUnit - 1) / kUnit;
+  };
+  const int64_t units = std::max<int64_t>(1, units_of(vis)), slots = (int64_t)ctx->sm_count * blocks_per_sm(nt);
+  int64_t work = 0, least = units;
+  for (int c = 0; c < g.a.W; ++c) {
+    const int64_t rows = (int64_t)(g.a.q_row_off[c + 1] - g.a.q_row_off[c]) * g.a.group;
+    if (rows == 0) continue;
+    least = std::min(least, units_of(g.a.vis[c]));
+    work += (rows + 8 * nt - 1) / (8 * nt) * g.a.H_kv * units_of(g.a.vis[c]);
+  }
+  const double join_us = 2.0 * 4 * g.a.d * g.a.H_kv * g.n_vrows / 4e6, u = step_us(g, nt);
+  Split best = {};
+  int64_t last = 0;
+  for (int64_t k = 1; k <= std::min<int64_t>(fc::kKv4MaxSplits, std::max<int64_t>(1, units / 2)); ++k) {
+    const int64_t steps = (units + k - 1) / k, n = (units + steps - 1) / steps, blocks = tiles * n;
+    if (n == last) continue;
+    if (k > 1 && blocks > 4 * slots) break;
+    last = n;
+    const int64_t on_sm = (blocks + ctx->sm_count - 1) / ctx->sm_count;
+    const double us = (blocks <= slots ? u * steps * (on_sm == 1 ? 1.35 : on_sm == 2 ? 2.15 : (double)on_sm) + 3
+                                       : u * ((double)work / ctx->sm_count + 0.5 * blocks_per_sm(nt) * std::min(steps, least)) + 3.0 * blocks / slots +
+                                             (n > 1 && g.f32 ? 4 : 0)) +
+                      (n > 1 ? 4 + n * join_us : 0);
+    if (k == 1 || us < best.us) best = {us, steps * kUnit, (int32_t)n};
+  }
+  return best;
+}
 
 }  // namespace
 
@@ -590,45 +629,29 @@ namespace fc {
 size_t kv4_rows_workspace(const fc_ctx* ctx, Kv4AttnGeom& g) {
   int vis = 0;
   for (int c = 0; c < g.a.W; ++c) vis = std::max(vis, g.a.vis[c]);
-  const int nt = tiles_of(g);
-  const int64_t tiles = tile_count(g.a, 8 * nt) * g.a.H_kv;
-  // The number of parts is the one that should be fastest.  A part is at least two steps; joining the parts costs a kernel and their
-  // bytes.  Where all blocks are resident at once, the fullest SM counts (one or two blocks on an SM take 1.35 or
-  // 1.08 times their share of a full one); otherwise all the work does, half a part more for the blocks that end last, and 3 us for each set
-  // of blocks to start and end.
-  constexpr int64_t kUnit = kStep * kWarps;
-  auto units_of = [&](int v) {
-    const int64_t window = std::max(v - g.n_cache, 0);
-    return ((window > 0 ? ((int64_t)g.n_cache + kUnit - 1) / kUnit * kUnit : std::min(v, g.n_cache)) + kWindowCost * window + kUnit - 1) / kUnit;
-  };
-  const int64_t units = std::max<int64_t>(1, units_of(vis)), slots = (int64_t)ctx->sm_count * blocks_per_sm(nt);
-  int64_t work = 0;
-  for (int c = 0; c < g.a.W; ++c)
-    work += ((int64_t)(g.a.q_row_off[c + 1] - g.a.q_row_off[c]) * g.a.group + 8 * nt - 1) / (8 * nt) * g.a.H_kv * units_of(g.a.vis[c]);
-  const double join_us = 2.0 * 4 * g.a.d * g.a.H_kv * g.n_vrows / 4e6, u = step_us(g);
-  double best = 0;
-  int64_t last = 0;
-  for (int64_t k = 1; k <= std::min<int64_t>(kKv4MaxSplits, std::max<int64_t>(1, units / 2)); ++k) {
-    const int64_t steps = (units + k - 1) / k, n = (units + steps - 1) / steps, blocks = tiles * n;
-    if (n == last) continue;
-    if (k > 1 && blocks > 4 * slots) break;
-    last = n;
-    const int64_t on_sm = (blocks + ctx->sm_count - 1) / ctx->sm_count;
-    const double us = (blocks <= slots ? u * steps * (on_sm == 1 ? 1.35 : on_sm == 2 ? 2.15 : (double)on_sm) + 3
-                                       : u * ((double)work / ctx->sm_count + 0.5 * blocks_per_sm(nt) * steps) + 3.0 * blocks / slots) +
-                      (n > 1 ? 4 + n * join_us : 0);
-    if (k == 1 || us < best) best = us, g.part_keys = steps * kUnit, g.n_splits = (int32_t)n;
+  // Sixteen rows to a tile where some chunk has more than eight.  In fp32 that leaves fewer blocks of fewer registers to spare; so
+  // it has to promise 5 % (three chunks of 300 rows of 8 heads of 128 over 4000 keys and the window: 242 us against 283 with eight;
+  // 160 rows of 2 heads of 64 over 1040 keys: 16.7 against 12.5).
+  bool many = false;
+  for (int c = 0; c < g.a.W; ++c) many |= (int64_t)(g.a.q_row_off[c + 1] - g.a.q_row_off[c]) * g.a.group > 8;
+  g.row_tiles = many && !g.f32 ? 2 : 1;
+  Split best = split_of(ctx, g, g.row_tiles, vis);
+  if (many && g.f32) {
+    const Split two = split_of(ctx, g, 2, vis);
+    if (two.us < 0.95 * best.us) best = two, g.row_tiles = 2;
   }
+  g.part_keys = best.part_keys;
+  g.n_splits = best.n;
   const int64_t cache = vis > g.n_cache ? ((int64_t)g.n_cache + kUnit - 1) / kUnit * kUnit : vis;
   g.n_cache_ceil = cache;
-  g.rows_us = best + 4;
+  g.rows_us = best.us + 4;
   if (g.n_splits == 1) return 0;
   const int64_t parts = g.a.H_kv * g.n_vrows * g.n_splits;
   return align_up(parts * g.a.d * sizeof(float), 256) + align_up(parts * sizeof(float2), 256);
 }
 
 int kv4_rows(cudaStream_t st, const Kv4AttnGeom& g, const void* Q, const void* K, const void* V, void* O) {
-  const int nt = tiles_of(g);
+  const int nt = g.row_tiles;
   const int64_t tiles = tile_count(g.a, 8 * nt);
   if (tiles == 0) return FC_OK;
   if (tiles > INT32_MAX) return FC_ERR_UNSUPPORTED;
@@ -640,9 +663,14 @@ int kv4_rows(cudaStream_t st, const Kv4AttnGeom& g, const void* Q, const void* K
       FC_CUDA_CHECK(cudaFuncSetAttribute(attention_kv4_rows_kernel<T, D, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem)); \
     attention_kv4_rows_kernel<T, D, NT><<<grid, kThreads, smem, st>>>((const T*)Q, (const T*)K, (const T*)V, (T*)O, g);  \
   } while (0)
-  if (g.f32) { if (g.a.d == 128) FC_KV4_ROWS(float, 128, 1); else FC_KV4_ROWS(float, 64, 1); }
-  else if (g.a.d == 128) { if (nt == 1) FC_KV4_ROWS(__nv_bfloat16, 128, 1); else FC_KV4_ROWS(__nv_bfloat16, 128, 2); }
-  else { if (nt == 1) FC_KV4_ROWS(__nv_bfloat16, 64, 1); else FC_KV4_ROWS(__nv_bfloat16, 64, 2); }
+#define FC_KV4_ROWS_PICK(T)                                                                        \
+  do {                                                                                             \
+    if (g.a.d == 128) { if (nt == 1) FC_KV4_ROWS(T, 128, 1); else FC_KV4_ROWS(T, 128, 2); }        \
+    else { if (nt == 1) FC_KV4_ROWS(T, 64, 1); else FC_KV4_ROWS(T, 64, 2); }                       \
+  } while (0)
+  if (g.f32) FC_KV4_ROWS_PICK(float);
+  else FC_KV4_ROWS_PICK(__nv_bfloat16);
+#undef FC_KV4_ROWS_PICK
 #undef FC_KV4_ROWS
   FC_LAUNCH_CHECK("attention_kv4_rows_kernel");
   return g.n_splits > 1 ? kv4_combine(st, g, g.f32 ? FC_F32 : FC_BF16, O, true) : FC_OK;

@@ -432,6 +432,19 @@ def test_attention_items_cut_into_parts(fc, ctx, case):
     run_attention(fc, ctx, d=64, dtype=BF16, impl=2, **case)
 
 
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("case", [
+    dict(H_q=12, H_kv=12, lens=[190, 251], n_cache=700, win=True, active=[0, 1]),
+    dict(H_q=16, H_kv=4, lens=[251, 3, 130], n_cache=777, win=True, active=[0, 2]),
+    dict(H_q=24, H_kv=24, lens=[257, 9, 120], n_cache=0, win=True, active=[0, 1, 2]),
+    dict(H_q=24, H_kv=24, lens=[257, 40, 250], n_cache=333, win=True, active=[0, 1, 2], cut=[1, 0, 880]),
+    dict(H_q=8, H_kv=8, lens=[300, 300, 300], n_cache=4001, win=True, active=[0, 2]),  # at d = 128 also in two parts
+], ids=lambda c: "-".join(map(str, c["lens"])) + f"@{c['n_cache']}")
+def test_attention_fp32_of_many_rows(fc, ctx, case, d):
+    # enough rows that sixteen, not eight, go into a tile
+    run_attention(fc, ctx, d=d, dtype=F32, **case)
+
+
 @pytest.mark.parametrize("rows", [3, 700])
 @pytest.mark.parametrize("dtype", [BF16, F32])
 def test_attention_strides_and_broadcast_heads(fc, ctx, dtype, rows):
