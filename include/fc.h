@@ -462,7 +462,7 @@ int fc_kv4_unpack(fc_ctx* ctx, void* stream, const fc_kv4_unpack_desc* desc, con
  *                    CUDA-core kernel; 2 (bf16 only) unpack into the workspace and run the tcgen05 kernel of
  *                    fc_chunk_attention over [workspace | window]; 3 force the kernel for few rows, which reads the packed keys
  *                    in one pass and is also the path of fp32.
- *   active_ids       as above; an id outside [0, W) sets FC_DEV_BAD_INDEX and is ignored.
+ *   active_ids       as above; an id outside [0, W) sets FC_DEV_BAD_INDEX and is ignored.  A chunk named again is one chunk.
  *   cache            HOST struct, rows >= n_cache; may be NULL if n_cache is 0.
  *   K, V             DEVICE [H_kv, kv_rows, d], the window; may be NULL if n_seg is 0 (no window).
  *   kv_visible_len   as above, at most 2^31 - 4097.

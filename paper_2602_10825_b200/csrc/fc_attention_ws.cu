@@ -209,12 +209,16 @@ attention_ws_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
     // active chunks sorted by visible length, longest first (insertion sort, at most 64 entries)
     const int n_in = min(max(*g.n_active, 0), g.W);
     int n = 0;
+    uint64_t seen = 0;  // a chunk named again is one chunk all the same: the host counts rows of work once
+    static_assert(FC_MAX_CHUNKS <= 64, "a bit a chunk");
     for (int a = 0; a < n_in; ++a) {
       const int c = g.active_ids[a];
       if (c < 0 || c >= g.W) {
         if (g.status) atomicOr(g.status, FC_DEV_BAD_INDEX);
         continue;
       }
+      if (seen >> c & 1) continue;
+      seen |= 1ull << c;
       int p = n++;
       while (p > 0 && g.vis[sh->act_chunk[p - 1]] < g.vis[c]) {
         sh->act_chunk[p] = sh->act_chunk[p - 1];

@@ -505,6 +505,16 @@ def test_attention_many_chunks(fc, ctx, dtype, impl):
     assert (f64(O)[:, np.setdiff1d(np.arange(off[-1]), rows)] == 9).all()
 
 
+@pytest.mark.parametrize("dtype, impl", [(BF16, 0), (BF16, 1), (BF16, 2), (BF16, 3), (F32, 0)])
+def test_attention_chunk_named_more_than_once(fc, ctx, dtype, impl):
+    # 40 work items of 256 rows, 50 if the chunk that is named twice counted twice; 32 key tiles, so that items are cut into parts
+    run_attention(fc, ctx, H_q=10, H_kv=10, d=64, lens=[512, 256, 1], n_cache=4096, win=False, active=[0, 0, 1], cut=[4096, 4000, 4000],
+                  dtype=dtype, impl=impl)
+    # the copies behind what they hide, and every entry the same
+    run_attention(fc, ctx, H_q=4, H_kv=2, d=64, lens=[300, 20, 40], n_cache=1000, win=True, active=[1, 2, 1], dtype=dtype, impl=impl)
+    run_attention(fc, ctx, H_q=4, H_kv=2, d=64, lens=[300, 20, 40], n_cache=1000, win=True, active=[2, 2, 2], dtype=dtype, impl=impl)
+
+
 def test_attention_bad_ids_are_reported(fc, ctx):
     for dtype, rows in ((BF16, 3), (BF16, 400), (F32, 3)):
         cache, Kc, Vc = packed_store(fc, ctx, 1, 90, 64, 3)
