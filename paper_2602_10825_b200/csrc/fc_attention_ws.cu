@@ -763,7 +763,8 @@ attention_ws_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
         }
       }
       if (g.lse && row_ok)
-        g.lse[(int64_t)head * g.lse_hs + row] = l > 0.f ? (m + log2f(l)) * 0.6931471805599453f : -INFINITY;
+        g.lse[(int64_t)head * g.lse_hs + row] =
+            l > 0.f ? (m + log2f(l)) * 0.6931471805599453f : (kTwo && l != l ? l : -INFINITY);  // -inf: the row saw no token
       tc_fence_before();  // O_x has been read before this warp's next p_ready arrival lets PV_x overwrite it
     }
   }

@@ -484,6 +484,19 @@ def test_attention_nan_query_stays_in_its_row(fc, ctx, rows):
         assert bad[1, 1].all() and int(bad.sum()) == 64
 
 
+@pytest.mark.parametrize("dtype, impl", [(BF16, 0), (BF16, 1), (BF16, 2), (BF16, 3), (F32, 0), (F32, 1)])
+@pytest.mark.parametrize("rows, n", [(2, 400), (200, 400), (200, 3000)])
+def test_attention_log_sum_of_a_nan_row(fc, ctx, rows, n, dtype, impl):
+    # -inf says that a row saw no token; a row whose logits are NaN saw some
+    cache, _, _ = packed_store(fc, ctx, 2, n, 64, 3)
+    Q = rand((2, rows, 64), 4, 1.0, dtype)
+    Q[1, 1, 3] = float("nan")
+    O, lse = torch.zeros_like(Q), torch.zeros((2, rows), device="cuda")
+    ctx.chunk_attention_kv4(Q, cache, None, None, [0, rows], [n], i32([0]), i32([1]), O, lse=lse, impl=impl)
+    bad = torch.isnan(lse)
+    assert bad[1, 1] and int(bad.sum()) == 1 and torch.isnan(O[1, 1]).all()
+
+
 @pytest.mark.parametrize("dtype, impl", [(BF16, 1), (BF16, 2), (BF16, 3), (F32, 0)])
 def test_attention_many_chunks(fc, ctx, dtype, impl):
     # as many chunks as there may be, most of them short; half active, one of them named twice
