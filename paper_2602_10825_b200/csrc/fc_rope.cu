@@ -100,7 +100,9 @@ __device__ __forceinline__ void place(const RopeGeom& g, int e, int& pair, int& 
   }
 }
 
-template <typename T, int D, bool kHalves>
+// kPass: the sections leave elements that pass through.  An instance of its own, since the others have no register to spare (4680 tokens of
+// 48 bf16 heads of 128 in a replayed graph: 19.7 us, where half the elements pass through 20.5).
+template <typename T, int D, bool kHalves, bool kPass>
 __global__ void __launch_bounds__(kThreads, kHalves && sizeof(T) == 2 ? 6 : 8)  // 80 registers where eight partners are looked up, else 64
 qk_norm_rope_kernel(const T* Q, const T* K, T* Q_out, T* K_out, const float* __restrict__ q_weight,
                     const float* __restrict__ k_weight, const int32_t* __restrict__ pos, const __grid_constant__ RopeGeom g) {
@@ -127,7 +129,7 @@ qk_norm_rope_kernel(const T* Q, const T* K, T* Q_out, T* K_out, const float* __r
       if (u < rows) raw[u] = *reinterpret_cast<const uint4*>(in + u * hs);
   }
 
-  const int pairs = (g.axis_dim[0] + g.axis_dim[1] + g.axis_dim[2]) / 2;
+  const int turning = g.axis_dim[0] + g.axis_dim[1] + g.axis_dim[2], pairs = turning / 2;
   for (int x = tid; x < g.tokens * (D / 2); x += kThreads) {
     const int t = x / (D / 2), pair = x % (D / 2), n = min(first_token + t, g.T - 1);
     if (pair >= pairs) {  // what does not turn, in the order of FC_ROPE_PAIRS
@@ -180,6 +182,7 @@ qk_norm_rope_kernel(const T* Q, const T* K, T* Q_out, T* K_out, const float* __r
           c[i] *= weight[e];
           s[i] *= weight[other];
         }
+        if (kPass && e >= turning) s[i] = -0.f;
       }
       ce[v] = pack2(c[0], c[2]);
       co[v] = pack2(c[1], c[3]);
@@ -229,8 +232,17 @@ qk_norm_rope_kernel(const T* Q, const T* K, T* Q_out, T* K_out, const float* __r
         }
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-          const uint64_t y0 = fma2(e[v], ce[v], mul2(kHalves ? pe[v] : o[v], se[v]));
-          const uint64_t y1 = fma2(o[v], co[v], mul2(kHalves ? po[v] : e[v], so[v]));
+          uint64_t p0 = kHalves ? pe[v] : o[v], p1 = kHalves ? po[v] : e[v];  // the partners
+          if (kPass) {  // what passes through gets a partner of 0 in place of a perhaps infinite one: 0 times -0 adds nothing, even to a -0
+            const bool k0 = lane * E + 4 * v < turning, k1 = lane * E + 4 * v + 2 < turning;
+            float a[4];
+            unpack2(p0, a[0], a[1]);
+            unpack2(p1, a[2], a[3]);
+            p0 = pack2(k0 ? a[0] : 0.f, k1 ? a[1] : 0.f);
+            p1 = pack2(k0 ? a[2] : 0.f, k1 ? a[3] : 0.f);
+          }
+          const uint64_t y0 = fma2(e[v], ce[v], mul2(p0, se[v]));
+          const uint64_t y1 = fma2(o[v], co[v], mul2(p1, so[v]));
           e[v] = mul2(y0, r2);
           o[v] = mul2(y1, r2);
         }
@@ -333,9 +345,11 @@ extern "C" int fc_qk_norm_rope(fc_ctx* ctx, void* stream, const fc_rope_desc* de
   const dim3 grid((unsigned)blocks, (unsigned)splits);
   FC_DEVICE_GUARD(ctx);
   cudaStream_t st = (cudaStream_t)stream;
-#define FC_ROPE_LAUNCH(T, D, HALVES)                                                                                  \
-  qk_norm_rope_kernel<T, D, HALVES><<<grid, kThreads, 0, st>>>((const T*)Q, (const T*)K, (T*)Q_out, (T*)K_out, \
-                                                                           q_weight, k_weight, pos, g)
+#define FC_ROPE_LAUNCH(T, D, HALVES)                                                                                     \
+  do {                                                                                                                   \
+    auto kernel = turning < D ? qk_norm_rope_kernel<T, D, HALVES, true> : qk_norm_rope_kernel<T, D, HALVES, false>;      \
+    kernel<<<grid, kThreads, 0, st>>>((const T*)Q, (const T*)K, (T*)Q_out, (T*)K_out, q_weight, k_weight, pos, g);       \
+  } while (0)
 #define FC_ROPE_PICK(T)                                                                                      \
   if (desc->d == 128) {                                                                                      \
     if (desc->pairing == FC_ROPE_HALVES) FC_ROPE_LAUNCH(T, 128, true); else FC_ROPE_LAUNCH(T, 128, false);   \

@@ -122,6 +122,38 @@ def test_rope_far_positions_and_back(fc, ctx, halves):
     assert np.abs(f64(X) - f64(K)).max() <= 4e-6 * size * 2
 
 
+@pytest.mark.parametrize("halves", [False, True])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("d, axes", [(128, (2, 6, 22)), (64, (24, 20, 18)), (128, (0, 32, 64)), (64, (0, 0, 0))])
+def test_rope_elements_behind_the_sections_pass_through(fc, ctx, d, axes, dtype, halves):
+    t, T = sum(axes), 9
+    X = rand((3, T, d), 7, 1.0, dtype)
+    g = torch.Generator().manual_seed(d)
+    odd = torch.tensor([math.inf, -math.inf, math.nan, -0.0, 0.0, 1e-39, -3e38])
+    hit = torch.rand((3, T, d - t), generator=g) < 0.5
+    X[..., t:] = torch.where(hit, odd[torch.randint(0, 7, hit.shape, generator=g)], X[..., t:].float().cpu()).to(dtype).cuda()
+    pos = torch.randint(-3000, 3000, (T, 3), generator=g).int()
+    kw = dict(axes=axes, pos=pos.cuda(), pairing=fc.ROPE_HALVES if halves else fc.ROPE_PAIRS)
+    bits = torch.int16 if dtype == BF16 else torch.int32
+    nan = torch.isnan(X)
+    Y = X.clone()
+    for out in (ctx.qk_norm_rope(X, None, norm=False, **kw)[0], ctx.qk_norm_rope(None, Y, norm=False, K_out=Y, **kw)[1]):
+        assert torch.equal(torch.isnan(out), nan)
+        same = out.contiguous().view(bits) == X.view(bits)
+        assert (same | nan)[..., t:].all()
+        check_turned(out[..., :t], X[..., :t], dtype, pos=pos.numpy(), axes=axes, halves=halves, norm=False)
+    # normed: an element that passes through has its own weight, not its neighbour's
+    X = rand((3, T, d), 8, 1.0, dtype)
+    X[..., t::3] = -0.0
+    w = rand((d,), 3, 0.3, F32) + 1
+    w[-1] = math.inf
+    out = ctx.qk_norm_rope(X, None, q_weight=w, **kw)[0]
+    want, size = pf.norm_rope(f64(X), pos.numpy(), axes, halves=halves, weight=np.append(f64(w)[:-1], 1.0))
+    assert (np.abs(f64(out) - want) <= HALF[dtype] * np.abs(want) + 2e-6 * size)[..., :-1].all()
+    assert (torch.isinf(out[..., -1]) | torch.isnan(out[..., -1])).all()
+    assert (torch.signbit(out) == torch.signbit(X))[..., t:-1].all()
+
+
 def test_norm_rope_many_tokens_in_place(fc, ctx):
     # more rows than resident groups, so that a group walks over several heads; q in place
     T, H = 5000, 24
