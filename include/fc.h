@@ -423,7 +423,8 @@ typedef struct {
  *
  *   K_src, V_src     DEVICE [H, n_new, d], `dtype` (may be NULL if n_new is 0).
  *   old              HOST struct or NULL (n_old 0); its rows >= n_old.  Its first n_old rows must not overlap the rows that are
- *                    written (`dst` itself with dst_row < n_old is refused).
+ *                    written: refused, by their addresses and strides (`dst` itself with dst_row < n_old; slices of one store that
+ *                    share rows; stores of different strides whose heads lie between one another's).
  *   kept_idx         DEVICE [H, >= n_out] int32 or NULL (n_out <= n_old + n_new then).  An index outside
  *                    [0, n_old + n_new) sets FC_DEV_BAD_INDEX; its output row is left as it was.
  * Rows outside the written range are not touched.  Needs no workspace. */

@@ -328,9 +328,9 @@ extern "C" int fc_kv4_pack(fc_ctx* ctx, void* stream, const fc_kv4_pack_desc* de
   }
   if (desc->n_old > 0 && (rc = fc::kv4_check(old, desc->d, desc->n_old)) != FC_OK) return rc;
   if (desc->dst_row > INT64_MAX - desc->n_out) return FC_ERR_INVALID_ARG;
-  if (desc->n_old > 0 && (old->k_codes == dst->k_codes || old->v_codes == dst->v_codes) && desc->dst_row < desc->n_old)
-    return FC_ERR_INVALID_ARG;  // rows would be read and written at once
   if ((rc = fc::kv4_check(dst, desc->d, desc->dst_row + desc->n_out)) != FC_OK) return rc;
+  if (desc->n_old > 0 && fc::kv4_meet(*old, 0, desc->n_old, *dst, desc->dst_row, desc->n_out, desc->H, desc->d))
+    return FC_ERR_INVALID_ARG;  // rows would be read and written at once
   if (desc->H > 1 && (dst->code_hs < desc->d / 2 || dst->scale_hs < desc->d / fc::kKv4Group)) return FC_ERR_INVALID_ARG;  // overlap
 
   PackGeom g = {};

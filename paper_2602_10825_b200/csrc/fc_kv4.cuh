@@ -32,6 +32,62 @@ inline int kv4_check(const fc_kv4_cache* c, int d, int64_t rows_needed) {
   return FC_OK;
 }
 
+// Rows r < n of heads h < H, `width` bytes each from base + h hs + r rs on.
+struct RowSet {
+  uintptr_t base;
+  int64_t hs, rs, width;  // bytes, not negative
+  int64_t n;
+  int32_t H;
+};
+
+// Whether two such sets, of the same number of heads, share a byte.  Exact where their strides are equal; otherwise whole heads
+// (equal head strides) or whole sets are taken for contiguous.
+inline bool rows_meet(RowSet a, RowSet b) {
+  using I = __int128;  // strides are the caller's: no sum of them overflows here
+  if (a.n <= 0 || b.n <= 0 || a.H <= 0) return false;
+  if (a.H == 1) a.hs = b.hs = 0;
+  if (a.n == 1) a.rs = b.rs;
+  if (b.n == 1) b.rs = a.rs;
+  const I off = (I)b.base - (I)a.base;  // of b's first row from a's
+  const I a_head = (I)(a.n - 1) * a.rs + a.width, b_head = (I)(b.n - 1) * b.rs + b.width;
+  const int64_t last = a.H - 1;
+  if (off >= last * (I)a.hs + a_head || off + last * (I)b.hs + b_head <= 0) return false;
+  if (a.hs != b.hs) return true;
+  for (int64_t dh = -last; dh <= last; ++dh) {
+    const I x = off + dh * (I)a.hs;  // of a head of b from a head of a
+    if (x >= a_head || x + b_head <= 0) continue;
+    if (a.rs != b.rs || a.rs == 0) return true;
+    // a row of b starts x + dr rs behind a row of a, -a.n < dr < b.n, and they meet if that is above -b.width and below a.width
+    const I rs = a.rs, least = -(I)b.width - x, most = (I)a.width - x;  // least < dr rs < most
+    I lo = least / rs, hi = most / rs;
+    while (lo * rs <= least) ++lo;
+    while (hi * rs >= most) --hi;
+    if (lo < -(I)(a.n - 1)) lo = -(I)(a.n - 1);
+    if (hi > b.n - 1) hi = b.n - 1;
+    if (lo <= hi) return true;
+  }
+  return false;
+}
+
+// Whether rows [a0, a0 + na) of one store and rows [b0, b0 + nb) of another share memory.
+inline bool kv4_meet(const fc_kv4_cache& a, int64_t a0, int64_t na, const fc_kv4_cache& b, int64_t b0, int64_t nb, int H, int d) {
+  auto sets = [&](const fc_kv4_cache& c, int64_t r0, int64_t n, RowSet (&out)[4]) {
+    const void* p[4] = {c.k_codes, c.v_codes, c.k_scales, c.v_scales};
+    for (int i = 0; i < 4; ++i) {
+      const bool codes = i < 2;
+      const int64_t hs = codes ? c.code_hs : 2 * c.scale_hs, rs = codes ? c.code_rs : 2 * c.scale_rs;
+      out[i] = {(uintptr_t)p[i] + (uintptr_t)r0 * (uintptr_t)rs, hs, rs, codes ? d / 2 : d / kKv4Group * 2, n, H};
+    }
+  };
+  RowSet x[4], y[4];
+  sets(a, a0, na, x);
+  sets(b, b0, nb, y);
+  for (const RowSet& s : x)
+    for (const RowSet& t : y)
+      if (rows_meet(s, t)) return true;
+  return false;
+}
+
 __device__ __forceinline__ uint32_t hfma2_bf16(uint32_t a, uint32_t b, uint32_t c) {
   uint32_t d;
   asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(d) : "r"(a), "r"(b), "r"(c));

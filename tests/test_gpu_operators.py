@@ -322,6 +322,31 @@ def test_pack_within_one_store(fc, ctx):
         ctx.kv4_pack(None, None, store, old=store, n_old=n, kept_idx=kept, dst_row=n - 1)
 
 
+@pytest.mark.parametrize("layout", ["heads", "rows", "scales in the rows"])
+def test_pack_between_slices_that_lie_apart(fc, ctx, layout):
+    H, n, d = 3, 40, 128
+    if layout == "scales in the rows":  # 64 bytes of codes, then 8 of scales, 8 unused
+        bufs = [torch.zeros((H, 2 * n + 3, 80), dtype=torch.uint8, device="cuda") for _ in range(2)]
+        t = [x for b in bufs for x in (b[..., :64], b.view(BF16)[..., 32:36])]
+    else:
+        shapes = 2 * (((H, 2 * n + 3, d // 2), torch.uint8), ((H, 2 * n + 3, d // 32), BF16))
+        t = [torch.zeros(s if layout == "heads" else (s[1], s[0], s[2]), dtype=dt, device="cuda") for s, dt in shapes]
+        t = t if layout == "heads" else [x.transpose(0, 1) for x in t]
+    part = lambda a, b: fc.Kv4Cache(*(x[:, a:b] for x in t))  # noqa: E731
+    K, V = rand((H, n, d), 1), rand((H, n, d), 2)
+    for a, to in ((0, n), (n, 0), (3, n + 3)):
+        for x in t:
+            x.zero_()
+        old = ctx.kv4_pack(K, V, part(a, a + n))
+        check_packed(old, K, V)
+        got = ctx.kv4_pack(None, None, part(to, to + n), old=old)
+        check_packed(got, K, V)
+        check_packed(old, K, V)
+        with pytest.raises(fc.FcError, match="invalid argument"):
+            ctx.kv4_pack(None, None, part(a + 1, a + 1 + n), old=old)
+        check_packed(old, K, V)
+
+
 def test_pack_bad_index_leaves_the_row(fc, ctx):
     H, n, d = 2, 50, 128
     K, V = rand((H, n, d), 1), rand((H, n, d), 2)

@@ -91,6 +91,37 @@ def test_pack_refusals(L, ctx, kw, want):
     assert pack(L, ctx, **kw) == want
 
 
+def slice_of(row, rows_first=False, base=P, **kw):
+    """Rows from `row` on of a store of two heads of 200 rows of 128, heads before rows or rows before heads."""
+    c, s = ((64, 128), (4, 8)) if rows_first else ((64 * 200, 64), (4 * 200, 4))
+    at = lambda n, rs: base + n * 0x10_0000 + row * rs  # noqa: E731
+    f = dict(k_codes=at(0, c[1]), v_codes=at(1, c[1]), k_scales=at(2, 2 * s[1]), v_scales=at(3, 2 * s[1]), code_hs=c[0], code_rs=c[1],
+             scale_hs=s[0], scale_rs=s[1], rows=200 - row)
+    f.update(kw)
+    return b._Kv4Cache(**f)
+
+
+@pytest.mark.parametrize("rows_first", [False, True])
+@pytest.mark.parametrize("old, dst, dst_row", [(0, 0, 39), (0, 8, 0), (8, 0, 0), (8, 0, 47), (0, 30, 9), (100, 61, 0), (3, 3, 0)])
+def test_pack_refuses_slices_that_share_rows(L, ctx, old, dst, dst_row, rows_first):
+    kw = dict(n_old=40, n_new=0, n_out=40, K=None, V=None)
+    # the slices overlap by at least one row in every case
+    assert old < dst + dst_row + 40 and dst + dst_row < old + 40
+    assert pack(L, ctx, old=slice_of(old, rows_first), dst=slice_of(dst, rows_first), dst_row=dst_row, **kw) == INVALID
+
+
+def test_pack_refuses_stores_that_share_some_memory(L, ctx):
+    kw = dict(n_old=40, n_new=0, n_out=40, K=None, V=None)
+    far = slice_of(0, base=P + 0x100_0000)
+    old = slice_of(0)
+    for own in ("k_codes", "v_codes", "k_scales", "v_scales"):  # one tensor of the two stores is the same, or K of one is V of the other
+        for other in ("k" + own[1:], "v" + own[1:]):
+            shared = {**{n: getattr(far, n) for n in ("k_codes", "v_codes", "k_scales", "v_scales")}, own: getattr(old, other)}
+            assert pack(L, ctx, old=old, dst=slice_of(0, **shared), **kw) == INVALID
+    # heads of one store between the heads of another, with other strides
+    assert pack(L, ctx, old=old, dst=slice_of(100, code_hs=64 * 150, rows=100), **kw) == INVALID
+
+
 def unpack(L, ctx, *, K=P, V=P, dtype=b.BF16, src=True, **kw):
     f = dict(H=2, d=128, n=10, src_row=0, k_hs=1280, k_rs=128, v_hs=1280, v_rs=128)
     f.update(kw)
