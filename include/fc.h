@@ -468,7 +468,8 @@ int fc_kv4_unpack(fc_ctx* ctx, void* stream, const fc_kv4_unpack_desc* desc, con
  *   K, V             DEVICE [H_kv, kv_rows, d], the window; may be NULL if n_seg is 0 (no window).
  *   kv_visible_len   as above, at most 2^31 - 4097.
  *   n_seg            <= FC_MAX_SEGMENTS - 1.  n_cache and the window's tokens together are at most 2^31 - 4097.
- * An infinity in a row of V that is seen makes what it reaches infinite or NaN; in fp32 one in q, K or V makes it NaN.
+ * An infinity in a row of V that is seen makes what it reaches infinite or NaN; in fp32 one in q, K or V makes it NaN, and a
+ * magnitude that rounds to a bf16 infinity (2^128 - 2^119 and above) counts as one.
  * Deterministic.  Workspace: fc_chunk_attention_kv4_workspace_bytes() of the same arguments (0 for arguments
  * that the call refuses). */
 size_t fc_chunk_attention_kv4_workspace_bytes(const fc_ctx* ctx, const fc_attn_desc* desc, int dtype,

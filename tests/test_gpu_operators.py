@@ -502,6 +502,31 @@ def test_attention_fp32_of_many_rows(fc, ctx, case, d):
     run_attention(fc, ctx, d=d, dtype=F32, **case)
 
 
+@pytest.mark.parametrize("d", [64, 128])
+def test_attention_fp32_window_products(fc, ctx, d):
+    """The six products that are taken of an fp32 weight w and a value v of the window miss at most 2^-24 |w v|: rounding to eight
+    bits leaves at most 2^-8 of a number and then 2^-17, so that each of the two products of second and third parts is below 2^-25.
+
+    Every row sees two keys: one of weight 1 and value 0, and one of weight w = (1 + x) / 2 whose values are 1 and numbers with
+    large lower parts.  Its output is w v / (1 + w), and its ratio to the one where v is 1 is v.  In units of 2^-24 of it that is off by the
+    missing products (1), what the tensor core cuts off the sum and off its smaller addend (2 each; the sums before the last are
+    2^-7 of it), and the rounding of the product with the reciprocal (1, in both); w itself is the sum of its parts exactly."""
+    g = torch.Generator().manual_seed(d)
+    rows = 400
+    x = torch.rand(rows, generator=g, dtype=torch.float64) * 2.0 ** -7
+    Q, K, V = torch.zeros((1, rows, d)), torch.zeros((1, 2, d)), torch.zeros((1, 2, d))
+    Q[0, :, 0] = torch.log((1 + x) / 2).float()
+    K[0, 1, 0] = 1.0
+    V[0, 1] = 1 + torch.randint(0, 2 ** 16, (d,), generator=g).float() * 2.0 ** -23
+    V[0, 1, 0] = 1.0
+    Q, K, V = (t.cuda() for t in (Q, K, V))
+    O = torch.zeros_like(Q)
+    ctx.chunk_attention_kv4(Q, None, K, V, [0, rows], [2], i32([0]), i32([1]), O, scale=1.0, n_cache=0)
+    v = f64(V)[0, 1]
+    units = (f64(O)[0] / f64(O)[0, :, :1] / v - 1) * 2.0 ** 24
+    assert np.abs(units).max() <= 7, (units.min(), units.max())
+
+
 @pytest.mark.parametrize("rows", [3, 700])
 @pytest.mark.parametrize("dtype", [BF16, F32])
 def test_attention_strides_and_broadcast_heads(fc, ctx, dtype, rows):
