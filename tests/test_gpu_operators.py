@@ -5,7 +5,8 @@ Tolerances.  A rounding to bf16 is off by at most 2^-8 of the value, one to fp32
              (a chain of 8 and a tree of 4 or 5 sums, a square root, a division, two products) at most 10 units, the
              two products and the sum 3: below 2e-6 of the size of the pair, plus the output's rounding.
   packing    none: codes and scales are compared as bits.
-  attention  fp32: a logit is off by at most (d + 4) 2^-24 |q||k| scale, a weight by twice that, and sums of n terms by
+  attention  fp32: a logit is off by at most (d + 4) 2^-24 |q||k| scale (the products of parts that are left out over a window are 1 of the
+             4: below 2^-24 of each product), a weight by twice that, and sums of n terms by
              n 2^-24, all relative to A = sum p |v|.  The tensor-core kernels round each weight to bf16 (2^-8 A) and take
              exponentials good to 1e-4 (A again); then the output's rounding.  The log of the weights' sum is off by the logit's
              error, the sum's n 2^-24, the exponentials' 1e-4, and its own rounding and that of the logarithm (2^-22).
@@ -175,6 +176,17 @@ def test_norm_rope_zero_row_and_nonfinite(fc, ctx):
     assert torch.isnan(out[0, 2, 4:6]).all() or torch.isnan(out[0, 2, 5])  # inf / inf
 
 
+def test_norm_of_a_row_with_an_infinity(fc, ctx):
+    # the infinite element is inf / inf, which its pair takes on; every other element is x / inf
+    Q = rand((1, 3, 64), 1, 1.0, F32)
+    Q[0, 2, 5] = float("inf")
+    for halves, pair in ((fc.ROPE_PAIRS, [4, 5]), (fc.ROPE_HALVES, [5, 17])):
+        out = ctx.qk_norm_rope(Q, None, axes=(24, 20, 20), grid=(0, 1, 3), pairing=halves)[0]
+        nan = torch.isnan(out)
+        assert nan[0, 2].nonzero().flatten().tolist() == pair and int(nan.sum()) == 2
+        assert (out[0, 2][~nan[0, 2]] == 0).all()
+
+
 # ------------------------------------------------------------------------------------ fc_kv4_pack / fc_kv4_unpack
 
 def check_packed(cache, K, V, rows=slice(None)):
@@ -209,6 +221,17 @@ def test_pack_and_unpack(fc, ctx, H, n, d, dtype):
         Ku, none = ctx.kv4_unpack(cache, row=1, n=n - 2, K_dst=dst[:, 1:n - 1], keys_only=True)
         assert none is None and np.array_equal(f64(Ku), pf.quantise(f64(K))[2][:, 1:n - 1])
         assert (dst[:, 0] == 5).all() and (dst[:, n - 1:] == 5).all()
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("H, n, d", [(2, 33, 128), (3, 257, 64)])
+def test_packing_again_gives_the_same_store(fc, ctx, H, n, d, dtype):
+    # rounding a scale up to five bits adds less than a sixteenth, so a group's largest code is 7 and 7 s / 7 is s again
+    K, V = rand((H, n, d), n, 1.0, F32), rand((H, n, d), n + 1, 0.01, F32)
+    V *= torch.exp2(torch.randint(-60, 60, (H, n, 1), generator=torch.Generator().manual_seed(3)).float()).cuda()
+    K[0, 3], V[1, 5, :32] = 0.0, 0.0
+    cache = ctx.kv4_pack(K, V, fc.Kv4Cache.empty(H, n, d))
+    assert same_store(ctx.kv4_pack(*ctx.kv4_unpack(cache, dtype=dtype), fc.Kv4Cache.empty(H, n, d)), cache)
 
 
 @pytest.mark.parametrize("d", [64, 128])
