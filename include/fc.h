@@ -352,16 +352,19 @@ int fc_kv_select_compact_ex(fc_ctx* ctx, void* stream, const float* score, int n
  * fc_qk_norm_rope — RMS norms of queries and keys for each head and the position rotation over
  * several axes, in one pass.
  *
- * Not in the paper, whose method starts from given Q and K; the models it runs on make them this way.
- * For every token n and head, with x the head's d elements (fp32 throughout, one rounding to `dtype`):
+ * Not in the paper, whose method starts from given Q and K.  The norm is of each head's row; a model that norms a projection's whole row
+ * does that before the call and takes FC_NORM_NONE.
+ * For every token n and head, with x the head's d elements (fp32 throughout, one rounding to `dtype`; a row whose sum of squares
+ * leaves the range of fp32 has no meaningful norm):
  *     y = x * w / sqrt(mean(x^2) + eps)                      norm = FC_NORM_RMS; w = 1 where the weight is NULL
  *     y = x                                                  norm = FC_NORM_NONE
  * The first axis_dim[0] elements turn with the token's position on axis 0 (time), the next axis_dim[1]
- * with axis 1 (height), the next axis_dim[2] with axis 2 (width); elements behind them pass through.
+ * with axis 1 (height), the next axis_dim[2] with axis 2 (width); elements behind them pass through: y as it is, infinities and
+ * signs of zero too.
  * Pair i of a section of n elements is (2i, 2i+1) (FC_ROPE_PAIRS) or (i, i + n/2) (FC_ROPE_HALVES):
  *     (y0, y1) <- (y0 cos a - y1 sin a, y0 sin a + y1 cos a),   a = position * theta^(-2i/n)
- * The angle is reduced in 64-bit fixed point, so that it is as exact at position 2^31 as at 1.  Negative
- * positions turn back: the rotation by -p undoes the rotation by p, and the rotation of an already
+ * The angle is reduced in 64-bit fixed point, so that it is as exact at position 2^31 as at 1, and rounded to fp32 after that (off by
+ * 2^-24 of itself, which is at most half a turn).  Negative positions turn back: the rotation by -p undoes the rotation by p, and the rotation of an already
  * rotated key by (new - old) position moves it there.
  *
  *   Q, Q_out         DEVICE [H_q, T, d], K, K_out DEVICE [H_kv, T, d]; `dtype` elements with the strides of the
@@ -404,6 +407,7 @@ int fc_qk_norm_rope(fc_ctx* ctx, void* stream, const fc_rope_desc* desc, const v
  * A value has at most eight significant bits: it is exactly a bf16 number, so attention over the store is
  * attention over these values without another rounding.  In each little-endian 32-bit word of eight
  * elements, element 2i is at bits 4i of the low half and element 2i+1 at bits 4i of the high half (i = 0..3).
+ * Rows that the calls below write may not overlap one another, nor what the same call reads.
  * The pointers are DEVICE pointers inside a HOST struct; K and V share strides.  Code bases and strides are
  * multiples of 16 bytes, scale bases and strides of a row's scales (d/32 elements). */
 typedef struct {
@@ -468,6 +472,9 @@ int fc_kv4_unpack(fc_ctx* ctx, void* stream, const fc_kv4_unpack_desc* desc, con
  *   K, V             DEVICE [H_kv, kv_rows, d], the window; may be NULL if n_seg is 0 (no window).
  *   kv_visible_len   as above, at most 2^31 - 4097.
  *   n_seg            <= FC_MAX_SEGMENTS - 1.  n_cache and the window's tokens together are at most 2^31 - 4097.
+ * Logits, maxima, sums and outputs are kept in fp32.  Softmax weights too for fp32 tensors and with impl 1; otherwise they are rounded to bf16
+ * on their way to V, as in fc_chunk_attention (each by 2^-8 at most, which adds about as much to the output's error as its
+ * own rounding), with what the rounding leaves taken along (2^-17) where no chunk has more than eight rows times heads of a group.
  * An infinity in a row of V that is seen makes what it reaches infinite or NaN; in fp32 one in q, K or V makes it NaN, and a
  * magnitude that rounds to a bf16 infinity (2^128 - 2^119 and above) counts as one.
  * Deterministic.  Workspace: fc_chunk_attention_kv4_workspace_bytes() of the same arguments (0 for arguments

@@ -94,8 +94,11 @@ bool maps_fit(const fc_attn_desc* d) {
 // What a call does, with the workspace it takes and the split of the keys in g.
 //
 // Few rows read the packed keys in one pass but spend a tensor instruction on eight of them; many rows pay for unpacking once.  The
-// line between the two moves with the heads and the keys, so that the estimates are compared (measured at 24 heads of 128
-// over 28000 keys: 64 rows 111 us against 147, 128 rows 212 against 150).
+// line between the two moves with the heads and the keys, so that the estimates are compared.  Measured, row kernel against
+// unpacking: 24 heads of 128 over 28000 keys, 64 rows 111 us and 140, 128 rows 223 and 142; over 1500 keys, 64 rows 17 and 20, 256 rows 44
+// and 27; 16 heads on 4 over 28000 keys, 16 rows 26 and 37, 64 rows 86 and 45; 8 heads of 64 over 6000 keys, 128 rows 16 and
+// 20, 256 rows 25 and 23.  Of 72 such sizes the estimates took the slower one by more than 8 % once (16 heads on 4, 32 rows, 28000
+// keys: 43.4 against 38.5).
 struct Plan {
   Path path;
   UnpackedPlan unpacked;  // kUnpacked

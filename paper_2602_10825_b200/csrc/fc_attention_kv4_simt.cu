@@ -1,5 +1,6 @@
-// Attention over [4-bit clean region | window] on CUDA cores with fp32 arithmetic throughout: the path of fp32 tensors, and
-// a second opinion for the tensor-core kernels.
+// Attention over [4-bit clean region | window] on CUDA cores with fp32 arithmetic throughout, softmax weights included: a second opinion
+// for the tensor-core kernels, taken where impl = 1 asks for it.  The joining kernels at the end of the file serve the row kernel
+// (fc_attention_kv4_rows.cu) as well.
 //
 // A block of 128 threads owns 32 virtual rows of one active chunk and one key head, and one part of the keys; four threads
 // share a row, each holding every fourth 4-element piece of q and of the output.  Tiles of 32 keys are staged in shared

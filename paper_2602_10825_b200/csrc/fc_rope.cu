@@ -1,6 +1,6 @@
 // fc_qk_norm_rope: RMS norm of every head of queries and keys, and the rotation over (time, height, width), in one pass.
 //
-// Bound by HBM: every element is read and written once (4680 tokens of 48 bf16 heads of 128 at 4.6 TB/s, launch included; a
+// Bound by HBM: every element is read and written once (4680 tokens of 48 bf16 heads of 128 at 4.7 TB/s, launch included; a
 // plain copy of the same bytes takes 21 us).  A head's row is spread over 16-byte pieces, one per lane (16 lanes for a
 // bf16 row of 128), and everything between the load and the store is in registers.  A group of lanes owns a token and walks
 // over some of its heads, four rows' loads in flight.  What it takes to stay under the copy rate is few instructions:
@@ -11,11 +11,14 @@
 //   - With FC_ROPE_HALVES the partner of an element sits in another lane at an odd distance: the rows go through shared
 //     memory as they are, and the partners are read one by one.
 // Angles: a pair's frequency is held in turns as a 64-bit fixed-point fraction, so position x frequency is one wrapping
-// integer product whose overflow is exactly the reduction modulo a full turn; its top 32 bits go to sincospif.
+// integer product whose overflow is exactly the reduction modulo a full turn; its top 32 bits, rounded to an fp32 number, go to
+// sincospif (2^-24 of the angle, as much as the fp32 products behind it are off by).
 //
-// Measured with the launch: 4680 tokens of 48 bf16 heads of 128 in 25.0 us (35.7 with far pairs), 18719 tokens of 8 fp32 heads of
-// 64 in 19.2; blocks of 256 threads 25.2, 37.2 and 20.8; without sending for the first rows before the angles 27.4 and 22.8; with two
-// rows in flight, or the next rows sent for before the arithmetic, slower still.
+// Measured, one call among others with the launch: 4680 tokens of 48 bf16 heads of 128 in 24.6 us, 18719 tokens of 8 fp32 heads of 64 with
+// far pairs in 18.4.  In replayed graphs the first takes 21.0 us, with far pairs 31.7, which is the cost of reading each
+// partner by itself, two bytes at a time, from shared memory (fp32: 38.6 and 40.3).  When the sizes were chosen: blocks of 128 threads
+// 25.0 us (35.7 with far pairs, fp32 heads of 64 19.2), of 256 threads 25.2, 37.2 and 20.8; without sending for the first rows before
+// the angles 27.4 and 22.8; with two rows in flight, or the next rows sent for before the arithmetic, slower still.
 #include <climits>
 #include <cmath>
 
