@@ -288,10 +288,10 @@ extern "C" int fc_qk_norm_rope(fc_ctx* ctx, void* stream, const fc_rope_desc* de
   RopeGeom g = {};
   if (turning > 0) {
     if (!inv_freq && !(desc->theta > 0.0 && std::isfinite(desc->theta))) return FC_ERR_INVALID_ARG;
-    if (!pos) {
+    if (!pos && desc->T > 0) {  // no tokens, no places: their array may well be NULL
       if (desc->grid_h <= 0 || desc->grid_w <= 0) return FC_ERR_INVALID_ARG;
       const int64_t frame = (int64_t)desc->grid_h * desc->grid_w;
-      if (frame > INT32_MAX || desc->grid_t0 + (int64_t)(desc->T > 0 ? desc->T - 1 : 0) / frame > INT32_MAX) return FC_ERR_INVALID_ARG;
+      if (frame > INT32_MAX || desc->grid_t0 + (int64_t)(desc->T - 1) / frame > INT32_MAX) return FC_ERR_INVALID_ARG;
     }
     int k = 0;
     for (int a = 0; a < 3; ++a) {

@@ -66,6 +66,11 @@ def test_rope_nothing_to_do(L, ctx):
     assert rope(L, ctx, H_q=0, H_kv=0, Q=None, K=None, Qo=None, Ko=None) == 0
 
 
+def test_rope_of_no_tokens_asks_for_no_places(L, ctx):
+    # an empty tensor of places has the address 0
+    assert rope(L, ctx, T=0, pos=None, grid_h=0, grid_w=0) == 0
+
+
 # ------------------------------------------------------------------------------------ fc_kv4_pack / unpack
 
 def pack(L, ctx, *, K=P, V=P, dtype=b.BF16, old=None, kept=None, kept_hs=0, dst=True, **kw):
