@@ -633,6 +633,26 @@ def test_attention_chunk_named_more_than_once(fc, ctx, dtype, impl):
     run_attention(fc, ctx, H_q=4, H_kv=2, d=64, lens=[300, 20, 40], n_cache=1000, win=True, active=[2, 2, 2], dtype=dtype, impl=impl)
 
 
+@pytest.mark.parametrize("dtype, impl", [(BF16, 0), (BF16, 1), (BF16, 2), (BF16, 3), (F32, 0)])
+@pytest.mark.parametrize("lens, n_cache", [([1], 3000), ([3, 9], 700), ([300, 130], 1500), ([40, 0, 17], 0)])
+def test_attention_rows_before_and_behind_the_chunks_stay(fc, ctx, lens, n_cache, dtype, impl):
+    # the chunks are rows 5 .. of Q and O, with NaN queries around them
+    H_q, H_kv, d, first, behind = 4, 2, 64, 5, 300
+    off = [first] + [first + int(x) for x in np.cumsum(lens)]
+    rows = off[-1] + behind
+    cache, Kc, Vc = packed_store(fc, ctx, H_kv, n_cache, d, 3) if n_cache else (None, np.zeros((H_kv, 0, d)), np.zeros((H_kv, 0, d)))
+    Q, K, V = rand((H_q, rows, d), 4, 1.0, dtype), rand((H_kv, 90, d), 5, 1.0, dtype), rand((H_kv, 90, d), 6, 1.0, dtype)
+    Q[:, :first], Q[:, off[-1]:] = float("nan"), float("nan")
+    O, lse = torch.full_like(Q, 9.0), torch.full((H_q, rows), 9.0, device="cuda")
+    vis = [n_cache + 90 - c for c in range(len(lens))]
+    ids = list(range(len(lens)))
+    ctx.chunk_attention_kv4(Q, cache, K, V, off, vis, i32(ids), i32([len(ids)]), O, lse=lse, impl=impl)
+    want = pf.attention(f64(Q), np.concatenate([Kc, f64(K)], 1), np.concatenate([Vc, f64(V)], 1), off, vis, ids)
+    check_attention(O, lse, *want, dtype, dtype == BF16 and impl != 1, vis[0], d, slice(first, off[-1]))
+    for t in (O, lse):
+        assert (t[:, :first] == 9).all() and (t[:, off[-1]:] == 9).all()
+
+
 def test_attention_bad_ids_are_reported(fc, ctx):
     for dtype, rows in ((BF16, 3), (BF16, 400), (F32, 3)):
         cache, Kc, Vc = packed_store(fc, ctx, 1, 90, 64, 3)
