@@ -474,7 +474,8 @@ int fc_kv4_unpack(fc_ctx* ctx, void* stream, const fc_kv4_unpack_desc* desc, con
  *   n_seg            <= FC_MAX_SEGMENTS - 1.  n_cache and the window's tokens together are at most 2^31 - 4097.
  * Logits, maxima, sums and outputs are kept in fp32.  Softmax weights too for fp32 tensors and with impl 1; otherwise they are rounded to bf16
  * on their way to V, as in fc_chunk_attention (each by 2^-8 at most, which adds about as much to the output's error as its
- * own rounding), with what the rounding leaves taken along (2^-17) where no chunk has more than eight rows times heads of a group.
+ * own rounding).  The kernel for few rows (impl 3, or chosen by 0) takes along what the rounding leaves (2^-17 then) where no chunk has more
+ * than eight rows times heads of a group.
  * An infinity in a row of V that is seen makes what it reaches infinite or NaN; in fp32 one in q, K or V makes it NaN, and a
  * magnitude that rounds to a bf16 infinity (2^128 - 2^119 and above) counts as one.
  * Deterministic.  Workspace: fc_chunk_attention_kv4_workspace_bytes() of the same arguments (0 for arguments

@@ -1,6 +1,8 @@
 // The 4-bit row format (see fc.h): helpers shared by the kernels that write it, read it and attend over it.
 #pragma once
 
+#include <algorithm>
+
 #include "fc_common.cuh"
 
 namespace fc {
@@ -51,20 +53,20 @@ inline bool rows_meet(RowSet a, RowSet b) {
   const I off = (I)b.base - (I)a.base;  // of b's first row from a's
   const I a_head = (I)(a.n - 1) * a.rs + a.width, b_head = (I)(b.n - 1) * b.rs + b.width;
   const int64_t last = a.H - 1;
+  constexpr I kAll = (I)1 << 62;  // no memory is that large: below, 64 bits do
+  if (a_head > kAll || b_head > kAll || last * (I)a.hs > kAll || last * (I)b.hs > kAll) return true;
   if (off >= last * (I)a.hs + a_head || off + last * (I)b.hs + b_head <= 0) return false;
   if (a.hs != b.hs) return true;
   for (int64_t dh = -last; dh <= last; ++dh) {
-    const I x = off + dh * (I)a.hs;  // of a head of b from a head of a
-    if (x >= a_head || x + b_head <= 0) continue;
+    const I far = off + dh * (I)a.hs;  // of a head of b from a head of a
+    if (far >= a_head || far + b_head <= 0) continue;
     if (a.rs != b.rs || a.rs == 0) return true;
     // a row of b starts x + dr rs behind a row of a, -a.n < dr < b.n, and they meet if that is above -b.width and below a.width
-    const I rs = a.rs, least = -(I)b.width - x, most = (I)a.width - x;  // least < dr rs < most
-    I lo = least / rs, hi = most / rs;
+    const int64_t x = (int64_t)far, rs = a.rs, least = -b.width - x, most = a.width - x;  // least < dr rs < most
+    int64_t lo = least / rs, hi = most / rs;
     while (lo * rs <= least) ++lo;
     while (hi * rs >= most) --hi;
-    if (lo < -(I)(a.n - 1)) lo = -(I)(a.n - 1);
-    if (hi > b.n - 1) hi = b.n - 1;
-    if (lo <= hi) return true;
+    if (std::max(lo, 1 - a.n) <= std::min(hi, b.n - 1)) return true;
   }
   return false;
 }
