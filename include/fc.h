@@ -25,6 +25,17 @@
  *   fc_kv4_unpack           rows of a 4-bit store as plain rows (what fc_kv_score reads)
  *   fc_chunk_attention_kv4  fc_chunk_attention over [4-bit clean region | window]
  *
+ * And, for generations that roll on and branch, a clean region in pages of 8-bit rows:
+ *
+ *   fc_kv8_append           rows of several sequences into their pages
+ *   fc_kv8_unpack           tokens of the pages as plain rows
+ *   fc_pages_take, _drop    pages for sequences that grow; pages that sequences let go of
+ *   fc_pages_fork           a sequence that begins as another one did, sharing its pages
+ *   fc_pages_compact        the used pages moved to the front of their pool
+ *   fc_chunk_attention_kv8  fc_chunk_attention over [tokens in pages | window], with a sliding window and first tokens
+ *                           that stay visible
+ *   fc_chunk_attention_span the same over plain rows alone
+ *
  * Conventions
  *   - Plain C types only.  Every pointer argument says whether it is a HOST or a
  *     DEVICE pointer.  The caller owns every buffer, including the workspace,
@@ -81,7 +92,8 @@ enum {
   FC_DEV_TIMEOUT = 1u,   /* a bounded in-kernel wait expired; the affected outputs are invalid */
   FC_DEV_NAN_SCORE = 2u, /* a NaN score was ranked as -inf by the selection */
   FC_DEV_BAD_INDEX = 4u, /* an index read from device memory was out of range and was skipped */
-  FC_DEV_NONFINITE = 8u  /* an infinity or a NaN was packed into a 4-bit store (its group of elements reads as NaN) */
+  FC_DEV_NONFINITE = 8u, /* an infinity or a NaN was packed: a 4-bit store's group of elements reads as NaN, an 8-bit store's element */
+  FC_DEV_NO_PAGES = 16u  /* fewer pages were free than a call asked for; the entries left over hold -1 */
 };
 
 enum { FC_MAX_CHUNKS = 64, FC_MAX_SEGMENTS = 64 };
@@ -487,6 +499,153 @@ int fc_chunk_attention_kv4(fc_ctx* ctx, void* stream, const fc_attn_desc* desc, 
                            const int32_t* kv_visible_len, const int32_t* seg_logical_off, const int32_t* seg_phys_off,
                            int n_seg, const int32_t* active_ids, const int32_t* n_active, void* O, float* lse,
                            int64_t lse_hs, uint32_t* status, void* ws, size_t ws_bytes);
+
+/* ------------------------------------------------------------------------------------------
+ * The paged 8-bit store.
+ *
+ * A pool of n_pages pages holds K and V of any number of sequences.  A page is `page` tokens (16, 32, 64 or 128) of all heads;
+ * token j of a sequence is row j % page of page table[j / page], where `table` is the sequence's row of a DEVICE
+ * int32 array [sequences, entries] (row stride table_cs elements).  An entry of -1 is no page (never given, or dropped).
+ * A block, one page of one head, is `page` rows of d E4M3 codes (a sign, four bits of exponent with bias 7, three of mantissa; no
+ * infinities; +-448 the largest), one row behind the other, with a scale s for K and one for V:
+ *     s = the least number with four significant bits whose 448-fold is not below max|x|, clamped to [2^-117, 2^119]; 0 if all
+ *         are 0 (elements that are not finite are left out)
+ *     code = x / s rounded to the nearest code, ties to even, +-448 at most; NaN if x is not finite (FC_DEV_NONFINITE)
+ *     value = code * s
+ * A value has at most eight significant bits: it is exactly a bf16 number.
+ * The pointers are DEVICE pointers inside a HOST struct; K and V share strides.  Blocks must not overlap. */
+typedef struct {
+  void *k_codes, *v_codes;        /* bytes, 16-byte aligned */
+  float *k_scales, *v_scales;
+  int64_t code_ps, code_hs;       /* bytes, multiples of 16: page, head */
+  int64_t scale_ps, scale_hs;     /* elements */
+  int32_t n_pages, page;
+} fc_kv8_pool;
+
+/* fc_kv8_append — rows row_off[c] .. row_off[c+1] - 1 of K_src / V_src become tokens pos[c], pos[c] + 1, ... of sequence c.
+ *
+ * Where pos[c] falls inside a page, the block's scale becomes the larger of its own and the new rows', and where it grows the rows before
+ * pos[c] are rounded again: code' = code * s / s' rounded as above.  Rows of that block from pos[c] on are what a rewound
+ * sequence leaves behind: they are written over, or left as they are, and count for nothing but the scale.  A page
+ * whose first row is written starts with a scale of its own.
+ *
+ *   K_src, V_src     DEVICE [H, rows, d], `dtype`.
+ *   row_off          HOST [W+1], non-decreasing; pos HOST [W]; W <= FC_MAX_CHUNKS.  pos[c] + rows <= 2^31 - 4097.
+ *   table            DEVICE [W, table_cs] (table_cs covers every entry that is used where W > 1: rows of the table do not overlap).
+ *   ref              DEVICE [n_pages] int32 or NULL: how many entries name each page (see below).  With it, a page that more
+ *                    than one entry names is left as it is (FC_DEV_BAD_INDEX): fork a sequence before it is written to.
+ * An entry outside [0, n_pages) sets FC_DEV_BAD_INDEX and its rows are dropped.  Two sequences of a call may not name the same
+ * page where they write.  Needs no workspace. */
+typedef struct {
+  int32_t H, d, W;                /* d in {64, 128} */
+  int64_t k_hs, k_rs, v_hs, v_rs; /* element strides of K_src, V_src (fc_kv8_unpack: of K_dst, V_dst) */
+} fc_kv8_rows;
+
+int fc_kv8_append(fc_ctx* ctx, void* stream, const fc_kv8_rows* desc, const void* K_src, const void* V_src, int dtype,
+                  const int32_t* row_off, const int32_t* pos, const fc_kv8_pool* pool, const int32_t* table,
+                  int64_t table_cs, const int32_t* ref, uint32_t* status);
+
+/* fc_kv8_unpack — tokens first[c], first[c] + 1, ... of sequence c as rows row_off[c] .. row_off[c+1] - 1 of K_dst / V_dst.
+ *   K_dst, V_dst     DEVICE [H, rows, d], `dtype` (exact in both); either may be NULL (the score needs the keys only).
+ *   table            as above; table_cs may be 0 (several ranges of one sequence).
+ * Rows of an entry outside [0, n_pages) are zeros, and FC_DEV_BAD_INDEX is set.  Needs no workspace. */
+int fc_kv8_unpack(fc_ctx* ctx, void* stream, const fc_kv8_rows* desc, const fc_kv8_pool* pool, const int32_t* table,
+                  int64_t table_cs, const int32_t* first, const int32_t* row_off, void* K_dst, void* V_dst, int dtype,
+                  uint32_t* status);
+
+/* ------------------------------------------------------------------------------------------
+ * The pages of a pool.
+ *
+ *   ref              DEVICE [n_pages] int32, 16-byte aligned: how many table entries name each page; 0: the page is free.
+ *   table            DEVICE [sequences, table_cs] int32, as above.
+ * The caller sets `ref` to 0 and `table` to -1 once; the calls keep the two in step.  All of them are deterministic, and none asks the
+ * host: pages are found on the device.  Calls that work on the same counts belong on one stream.
+ *
+ * fc_pages_take — entries first[c] .. last[c] - 1 of sequence c get pages of their own.  Sequence by sequence and entry by
+ * entry, each takes the free page of the lowest number.  Where none is left, entries get -1 and FC_DEV_NO_PAGES is set.
+ * What the entries held before is forgotten, not dropped.
+ *
+ * fc_pages_drop — entries first[c] .. last[c] - 1 of sequence c let go of their pages and become -1.  A page that nobody
+ * names any more is free; its content stays until somebody takes it.  An entry of -1 is passed over; one that names no
+ * page of the pool, or a free one, sets FC_DEV_BAD_INDEX.
+ *
+ *   first, last      HOST [W], 0 <= first <= last; W <= FC_MAX_CHUNKS.  Rows of the table may not overlap (W > 1: table_cs >= every last). */
+int fc_pages_take(fc_ctx* ctx, void* stream, int32_t* ref, int n_pages, int32_t* table, int64_t table_cs, int W,
+                  const int32_t* first, const int32_t* last, uint32_t* status);
+int fc_pages_drop(fc_ctx* ctx, void* stream, int32_t* ref, int n_pages, int32_t* table, int64_t table_cs, int W,
+                  const int32_t* first, const int32_t* last, uint32_t* status);
+
+/* fc_pages_fork — sequence dst[i] begins as the first tokens[i] tokens of sequence src[i].  Pages that these fill are shared; the
+ * last one, if they fill it in part, is copied into a page of its own (taken as above, fork by fork), so that both
+ * sequences may go on.  Entries that are -1 (dropped) stay -1.  dst's entries behind these are left as they are, and what it named before is
+ * forgotten: drop it first.
+ *   src, dst         HOST [n], rows of the table: 0 <= . < n_seq; no dst twice, and none among the src.
+ *   tokens           HOST [n], >= 0; ceil(tokens / page) <= table_cs.  n <= FC_MAX_CHUNKS.
+ * Where no page is left for a copy, the entry gets -1 and FC_DEV_NO_PAGES is set.  An entry of src that names no page of the pool
+ * sets FC_DEV_BAD_INDEX and becomes -1.  H, d as for fc_kv8_append.  Workspace: fc_pages_workspace_bytes(n_pages).
+ *
+ * fc_pages_compact — the n used pages of the pool become pages 0 .. n - 1: those with numbers from n on, in ascending order, move into
+ * the free ones below n, in ascending order; counts go with them, and entries 0 .. entries - 1 of all n_seq rows
+ * of the table are rewritten.  What the pages hold that are free afterwards is left as it is.
+ *   n_used           DEVICE [1] int32 out or NULL: n.
+ * Tables that are not among those rows would point at the wrong pages.  An entry that names no page, or a free one from n on, sets
+ * FC_DEV_BAD_INDEX and is left.  Workspace: fc_pages_workspace_bytes(n_pages). */
+size_t fc_pages_workspace_bytes(int n_pages);
+int fc_pages_fork(fc_ctx* ctx, void* stream, const fc_kv8_pool* pool, int H, int d, int32_t* ref, int32_t* table,
+                  int64_t table_cs, int n_seq, int n, const int32_t* src, const int32_t* dst, const int32_t* tokens,
+                  uint32_t* status, void* ws, size_t ws_bytes);
+int fc_pages_compact(fc_ctx* ctx, void* stream, const fc_kv8_pool* pool, int H, int d, int32_t* ref, int32_t* table,
+                     int64_t table_cs, int n_seq, int entries, int32_t* n_used, uint32_t* status, void* ws,
+                     size_t ws_bytes);
+
+/* ------------------------------------------------------------------------------------------
+ * fc_chunk_attention_kv8 — fc_chunk_attention over a paged 8-bit clean region and a plain window, each chunk with a sliding window
+ * and first tokens that stay visible.
+ *
+ * The logical tokens of chunk c are the first cache_len[c] tokens of its sequence, in pages, followed by the plain tokens
+ * window_first[c], window_first[c] + 1, ... of K / V (in the order of the segment table).  Its rows see
+ *     j < kv_visible_len[c]   and   (j < n_sink   or   j >= kv_begin[c])
+ * and O and lse are the softmax over those tokens, as in fc_chunk_attention; rows that see none get zeros (lse -inf).  The chunks of a
+ * generation share a row of the table (table_cs 0) and see one another's plain tokens; sequences of a batch have rows of their own,
+ * and window_first points each at its own plain tokens.
+ *
+ *   desc             as for fc_chunk_attention; k_*, v_* and kv_rows describe the plain tokens.  impl: 0 auto; 2 (bf16
+ *                    only) unpack what is seen into the workspace and run the tcgen05 kernel; 3 the kernel for few rows, which
+ *                    reads the pages in place and is also the path of fp32.
+ *   pool, table      as above; both may be NULL if every cache_len is 0.
+ *   cache_len        HOST [W] or NULL (all 0).  kv_visible_len HOST [W]; kv_begin HOST [W] or NULL (all 0: no sliding window); window_first
+ *                    HOST [W] or NULL (all 0).  Tokens that no chunk sees need no page.
+ *   K, V, seg_*      as in fc_chunk_attention_kv4: the plain tokens; n_seg 0 if there are none.
+ * Everything else is as in fc_chunk_attention_kv4: the active list, grouped heads, rows of inactive chunks, how weights are rounded (fp32: not; the
+ * tcgen05 kernel: to bf16; few rows: to fp16 over the pages, in units of a 2^-15th of the largest so far or less, and to bf16 over plain rows,
+ * the rest taken along where no chunk has more than eight rows times heads of a group).  What lies in tokens that a chunk does not see
+ * never reaches its rows, whatever it is.  A NaN in a token that is seen makes what it reaches NaN, and so does an infinity in Q.
+ * An entry outside [0, n_pages) that is needed sets FC_DEV_BAD_INDEX; K and V of its tokens count as zeros.
+ * Deterministic.  Workspace: fc_chunk_attention_kv8_workspace_bytes() of the same arguments (0 for arguments that the call
+ * refuses). */
+size_t fc_chunk_attention_kv8_workspace_bytes(const fc_ctx* ctx, const fc_attn_desc* desc, int dtype, int page, int64_t table_cs,
+                                              const int32_t* cache_len, const int32_t* q_chunk_row_off,
+                                              const int32_t* kv_visible_len, int n_sink, const int32_t* kv_begin,
+                                              const int32_t* window_first, const int32_t* seg_logical_off, int n_seg);
+int fc_chunk_attention_kv8(fc_ctx* ctx, void* stream, const fc_attn_desc* desc, const void* Q, const fc_kv8_pool* pool,
+                           const int32_t* table, int64_t table_cs, const int32_t* cache_len, const void* K, const void* V,
+                           int dtype, const int32_t* q_chunk_row_off, const int32_t* kv_visible_len, int n_sink,
+                           const int32_t* kv_begin, const int32_t* window_first, const int32_t* seg_logical_off,
+                           const int32_t* seg_phys_off, int n_seg, const int32_t* active_ids, const int32_t* n_active,
+                           void* O, float* lse, int64_t lse_hs, uint32_t* status, void* ws, size_t ws_bytes);
+
+/* fc_chunk_attention_span — the same over plain rows alone: fc_chunk_attention in which chunk c sees tokens
+ *     j < kv_visible_len[c]   and   (j < n_sink   or   j >= kv_begin[c])
+ * of the segment table, from single tokens, whose keys are shared out among all SMs, to whole chunks.  Arguments, types and impl as above.
+ * Workspace: fc_chunk_attention_span_workspace_bytes() of the same arguments. */
+size_t fc_chunk_attention_span_workspace_bytes(const fc_ctx* ctx, const fc_attn_desc* desc, int dtype,
+                                               const int32_t* q_chunk_row_off, const int32_t* kv_visible_len, int n_sink,
+                                               const int32_t* kv_begin, const int32_t* seg_logical_off, int n_seg);
+int fc_chunk_attention_span(fc_ctx* ctx, void* stream, const fc_attn_desc* desc, const void* Q, const void* K, const void* V,
+                            int dtype, const int32_t* q_chunk_row_off, const int32_t* kv_visible_len, int n_sink,
+                            const int32_t* kv_begin, const int32_t* seg_logical_off, const int32_t* seg_phys_off, int n_seg,
+                            const int32_t* active_ids, const int32_t* n_active, void* O, float* lse, int64_t lse_hs,
+                            uint32_t* status, void* ws, size_t ws_bytes);
 
 #ifdef __cplusplus
 }

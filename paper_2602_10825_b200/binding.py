@@ -22,7 +22,8 @@ RED_MEANKEY, RED_TILED, RED_TILED_MAX = 0, 1, 2
 NORM_NONE, NORM_RMS = 0, 1
 ROPE_PAIRS, ROPE_HALVES = 0, 1
 KV4_GROUP = 32  # elements of a packed row that share a scale
-STATUS_BITS = {"timeout": 1, "nan_score": 2, "bad_index": 4, "nonfinite": 8}
+KV8_PAGES = (16, 32, 64, 128)  # tokens that a page of the 8-bit store may hold
+STATUS_BITS = {"timeout": 1, "nan_score": 2, "bad_index": 4, "nonfinite": 8, "no_pages": 16}
 
 
 class FcError(RuntimeError):
@@ -71,6 +72,17 @@ class _Kv4UnpackDesc(C.Structure):
                 ("k_rs", C.c_int64), ("v_hs", C.c_int64), ("v_rs", C.c_int64)]
 
 
+class _Kv8Pool(C.Structure):
+    _fields_ = [("k_codes", C.c_void_p), ("v_codes", C.c_void_p), ("k_scales", C.c_void_p), ("v_scales", C.c_void_p),
+                ("code_ps", C.c_int64), ("code_hs", C.c_int64), ("scale_ps", C.c_int64), ("scale_hs", C.c_int64),
+                ("n_pages", C.c_int32), ("page", C.c_int32)]
+
+
+class _Kv8Rows(C.Structure):
+    _fields_ = [("H", C.c_int32), ("d", C.c_int32), ("W", C.c_int32), ("k_hs", C.c_int64), ("k_rs", C.c_int64),
+                ("v_hs", C.c_int64), ("v_rs", C.c_int64)]
+
+
 class _CompactStrides(C.Structure):
     _fields_ = [("src_hs", C.c_int64), ("src_rs", C.c_int64), ("dst_hs", C.c_int64), ("dst_rs", C.c_int64)]
 
@@ -94,7 +106,8 @@ def lib():
         L.fc_last_cuda_error.restype = C.c_char_p
         for name in ("fc_chunk_decide_static_max_bytes", "fc_chunk_decide_workspace_bytes", "fc_chunk_attention_workspace_bytes",
                      "fc_kv_score_workspace_bytes", "fc_kv_select_compact_workspace_bytes",
-                     "fc_kv_select_compact_ex_workspace_bytes", "fc_chunk_attention_kv4_workspace_bytes"):
+                     "fc_kv_select_compact_ex_workspace_bytes", "fc_chunk_attention_kv4_workspace_bytes",
+                     "fc_pages_workspace_bytes", "fc_chunk_attention_kv8_workspace_bytes", "fc_chunk_attention_span_workspace_bytes"):
             getattr(L, name).restype = C.c_size_t
         L.fc_chunk_decide_workspace_bytes.argtypes = [C.c_int64, C.c_int]
         p, i32, i64 = C.c_void_p, C.c_int, C.c_int64
@@ -103,6 +116,15 @@ def lib():
         L.fc_kv4_unpack.argtypes = [p, p, p, p, p, p, i32]
         L.fc_chunk_attention_kv4_workspace_bytes.argtypes = [p, p, i32, p, p, i32]
         L.fc_chunk_attention_kv4.argtypes = [p, p, p, p, p, i32, p, p, i32, p, p, p, p, i32, p, p, p, p, i64, p, p, C.c_size_t]
+        L.fc_kv8_append.argtypes = [p, p, p, p, p, i32, p, p, p, p, i64, p, p]
+        L.fc_kv8_unpack.argtypes = [p, p, p, p, p, i64, p, p, p, p, i32, p]
+        L.fc_pages_take.argtypes = L.fc_pages_drop.argtypes = [p, p, p, i32, p, i64, i32, p, p, p]
+        L.fc_pages_fork.argtypes = [p, p, p, i32, i32, p, p, i64, i32, i32, p, p, p, p, p, C.c_size_t]
+        L.fc_pages_compact.argtypes = [p, p, p, i32, i32, p, p, i64, i32, i32, p, p, p, C.c_size_t]
+        L.fc_chunk_attention_kv8_workspace_bytes.argtypes = [p, p, i32, i32, i64, p, p, p, i32, p, p, p, i32]
+        L.fc_chunk_attention_kv8.argtypes = [p, p, p, p, p, p, i64, p, p, p, i32, p, p, i32, p, p, p, p, i32, p, p, p, p, i64, p, p, C.c_size_t]
+        L.fc_chunk_attention_span_workspace_bytes.argtypes = [p, p, i32, p, p, i32, p, p, i32]
+        L.fc_chunk_attention_span.argtypes = [p, p, p, p, p, p, i32, p, p, i32, p, p, p, i32, p, p, p, p, i64, p, p, C.c_size_t]
         _lib = L
     return _lib
 
@@ -160,6 +182,7 @@ def _packer(cls):
 # The descriptors of the calls around the 4-bit store.
 _ROPE_FIELDS, _PACK_FIELDS, _UNPACK_FIELDS = _packer(_RopeDesc), _packer(_Kv4PackDesc), _packer(_Kv4UnpackDesc)
 _ATTN_FIELDS, _CACHE_FIELDS = _packer(_AttnDesc), _packer(_Kv4Cache)
+_POOL_FIELDS, _KV8_ROWS_FIELDS = _packer(_Kv8Pool), _packer(_Kv8Rows)
 
 
 def _int32(x):
@@ -209,6 +232,54 @@ class Kv4Cache:
         codes = [torch.empty((H, rows, d // 2), dtype=torch.uint8, device=device) for _ in range(2)]
         scales = [torch.empty((H, rows, d // KV4_GROUP), dtype=torch.bfloat16, device=device) for _ in range(2)]
         return Kv4Cache(codes[0], scales[0], codes[1], scales[1])
+
+
+class Kv8Pool:
+    """A pool of pages of 8-bit K and V rows (fc_kv8_pool): codes uint8 (or float8_e4m3fn) [pages, H, page, d] and scales fp32 [pages, H].
+
+    page is 16, 32, 64 or 128 tokens.  Strided views are fine as long as K and V share strides and a block, one page of one head, is
+    contiguous; the format is described in include/fc.h.  The four tensors are fixed, and so is their memory."""
+
+    k_codes, k_scales, v_codes, v_scales = (property(lambda self, i=i: self._tensors[i]) for i in range(4))
+
+    def __init__(self, k_codes, k_scales, v_codes, v_scales):
+        self._tensors = k_codes, k_scales, v_codes, v_scales
+        shape, s_shape, strides, s_strides = k_codes.shape, k_scales.shape, k_codes.stride(), k_scales.stride()
+        if len(shape) != 4:
+            raise FcError("codes must be [pages, heads, page, d]")
+        n, H, page, d = shape
+        if k_codes.dtype not in (torch.uint8, torch.float8_e4m3fn) or v_codes.dtype is not k_codes.dtype \
+                or not (k_scales.dtype is v_scales.dtype is torch.float32):
+            raise FcError("codes must be uint8 or float8_e4m3fn, and scales float32")
+        if v_codes.shape != shape or s_shape != (n, H) or v_scales.shape != s_shape:
+            raise FcError(f"codes must be [pages, heads, page, d] and scales [pages, heads], got {list(shape)}, {list(s_shape)}, "
+                          f"{list(v_codes.shape)}, {list(v_scales.shape)}")
+        device = k_codes.get_device()
+        if not (device == v_codes.get_device() == k_scales.get_device() == v_scales.get_device()):
+            raise FcError("codes and scales must be on one device")
+        if v_codes.stride() != strides or v_scales.stride() != s_strides or strides[3] != 1 or strides[2] != d:
+            raise FcError("K and V must share strides, and a block (one page of one head) must be contiguous")
+        self.n_pages, self.H, self.page, self.d, self._device = n, H, page, d, device
+        self._c = _POOL_FIELDS.pack(k_codes.data_ptr(), v_codes.data_ptr(), k_scales.data_ptr(), v_scales.data_ptr(),
+                                    strides[0], strides[1], s_strides[0], s_strides[1], n, page)
+
+    @property
+    def device(self):
+        return self.k_codes.device
+
+    @staticmethod
+    def empty(n_pages, H, page, d, device="cuda"):
+        """An uninitialised pool."""
+        if page not in KV8_PAGES:
+            raise FcError(f"page must be one of {KV8_PAGES}")
+        codes = [torch.empty((n_pages, H, page, d), dtype=torch.uint8, device=device) for _ in range(2)]
+        scales = [torch.empty((n_pages, H), dtype=torch.float32, device=device) for _ in range(2)]
+        return Kv8Pool(codes[0], scales[0], codes[1], scales[1])
+
+    def tables(self, n_seq, entries):
+        """(ref, table) of a pool that nobody uses yet: counts [n_pages], all 0, and rows of entries, all -1."""
+        return (torch.zeros(self.n_pages, dtype=torch.int32, device=self.device),
+                torch.full((n_seq, entries), -1, dtype=torch.int32, device=self.device))
 
 
 class Context:
@@ -648,4 +719,219 @@ class Context:
             0 if ws is None else ws.numel())
         if rc:
             self._check(rc, "fc_chunk_attention_kv4")
+        return O
+
+    # ------------------------------------------------------------------ the paged 8-bit store
+    def _table(self, table, name="table"):
+        """Pointer and row stride of an int32 table [sequences, entries]."""
+        if table.dim() != 2 or (table.shape[1] > 1 and table.stride(1) != 1):
+            raise FcError(f"{name} must be [sequences, entries] with contiguous rows")
+        return self._ptr(table, name, torch.int32), table.stride(0)
+
+    def _counts(self, ref, n_pages):
+        if ref.dim() != 1 or ref.shape[0] != n_pages or (n_pages > 1 and ref.stride(0) != 1):
+            raise FcError(f"ref must be contiguous [{n_pages}]")
+        return self._ptr(ref, "ref", torch.int32)
+
+    def _in_table(self, pool, table, ends):
+        """Every sequence's tokens have entries: sequence c ends behind token ends[c]."""
+        if table.shape[0] < len(ends):
+            raise FcError(f"table must have a row for each of the {len(ends)} sequences")
+        if len(ends) and max(ends) > table.shape[1] * pool.page:
+            raise FcError(f"table has entries for {table.shape[1] * pool.page} tokens, {max(ends)} are used")
+
+    def kv8_append(self, K, V, pool, table, pos, row_off=None, *, ref=None, status=None):
+        """Rows row_off[c] .. row_off[c+1] - 1 of K, V [H, rows, d] become tokens pos[c], ... of sequence c; returns the pool.
+
+        table [sequences, entries] names the pages of each sequence.  Without row_off there is one sequence, which gets all rows.  With
+        ref, pages that several entries name are not written to (status bit bad_index)."""
+        rows = K.shape[1]
+        shape = (pool.H, rows, pool.d)
+        kp, kh, kr = self._rows(K, "K", shape, K.dtype)
+        vp, vh, vr = self._rows(V, "V", shape, K.dtype)
+        row_off = (0, rows) if row_off is None else row_off
+        W = len(pos)
+        if len(row_off) != W + 1 or row_off[W] > rows:
+            raise FcError("row_off must have one entry more than pos and stay inside K")
+        self._in_table(pool, table, [p + b - a for p, a, b in zip(pos, row_off, row_off[1:])])
+        tp, cs = self._table(table)
+        desc = _KV8_ROWS_FIELDS.pack(pool.H, pool.d, W, kh, kr, vh, vr)
+        rc = self._L.fc_kv8_append(self._h, self._raw_stream(), desc, kp, vp, _dt(K), _int32(row_off), _int32(pos), self._store(pool, "pool"),
+                                   tp, cs, None if ref is None else self._counts(ref, pool.n_pages), self._ptr(status, "status", torch.int32))
+        if rc:
+            self._check(rc, "fc_kv8_append")
+        return pool
+
+    def kv8_unpack(self, pool, table, first, row_off, *, K_dst=None, V_dst=None, dtype=torch.bfloat16, keys_only=False, status=None):
+        """Values of tokens first[c], ... of sequence c as rows row_off[c] .. row_off[c+1] - 1 of (K, V) [H, rows, d]; V is None with
+        keys_only.  A table of one row serves any number of ranges."""
+        given = K_dst if K_dst is not None else V_dst
+        if given is not None:
+            dtype = given.dtype
+        W = len(first)
+        if len(row_off) != W + 1:
+            raise FcError("row_off must have one entry more than first")
+        rows = row_off[W] if given is None else given.shape[1]
+        if row_off[W] > rows:
+            raise FcError("row_off must stay inside the destination")
+        shape = (pool.H, rows, pool.d)
+        if K_dst is None:
+            K_dst = torch.empty(shape, dtype=dtype, device=self._dev)
+        kp, kh, kr = self._rows(K_dst, "K_dst", shape, dtype)
+        vp, vh, vr = None, 0, 0
+        if keys_only:
+            V_dst = None
+        else:
+            if V_dst is None:
+                V_dst = torch.empty(shape, dtype=dtype, device=self._dev)
+            vp, vh, vr = self._rows(V_dst, "V_dst", shape, dtype)
+        ends = [f + b - a for f, a, b in zip(first, row_off, row_off[1:])]
+        shared = table.shape[0] == 1
+        self._in_table(pool, table, [max(ends)] if shared and ends else ends)
+        tp, cs = self._table(table)
+        desc = _KV8_ROWS_FIELDS.pack(pool.H, pool.d, W, kh, kr, vh, vr)
+        rc = self._L.fc_kv8_unpack(self._h, self._raw_stream(), desc, self._store(pool, "pool"), tp, 0 if shared else cs, _int32(first),
+                                   _int32(row_off), kp, vp, _dt(K_dst), self._ptr(status, "status", torch.int32))
+        if rc:
+            self._check(rc, "fc_kv8_unpack")
+        return K_dst, V_dst
+
+    # ------------------------------------------------------------------ the pages of a pool
+    def _pages(self, call, name, ref, table, first, last, status):
+        W = len(first)
+        if len(last) != W or W > table.shape[0] or (W and max(last) > table.shape[1]):
+            raise FcError("first and last must have one entry a sequence and stay inside the table")
+        tp, cs = self._table(table)
+        rc = call(self._h, self._raw_stream(), self._counts(ref, ref.shape[0]), ref.shape[0], tp, cs, W, _int32(first), _int32(last),
+                  self._ptr(status, "status", torch.int32))
+        if rc:
+            self._check(rc, name)
+        return table
+
+    def pages_take(self, ref, table, first, last, *, status=None):
+        """Entries first[c] .. last[c] - 1 of sequence c get pages of their own, free ones of the lowest numbers; returns the table."""
+        return self._pages(self._L.fc_pages_take, "fc_pages_take", ref, table, first, last, status)
+
+    def pages_drop(self, ref, table, first, last, *, status=None):
+        """Entries first[c] .. last[c] - 1 of sequence c let go of their pages and become -1; returns the table."""
+        return self._pages(self._L.fc_pages_drop, "fc_pages_drop", ref, table, first, last, status)
+
+    def pages_fork(self, pool, ref, table, src, dst, tokens, *, status=None, ws=None):
+        """Sequence dst[i] begins as the first tokens[i] tokens of sequence src[i]: full pages are shared, a partly filled last one is
+        copied; returns the table."""
+        n = len(src)
+        if len(dst) != n or len(tokens) != n:
+            raise FcError("src, dst and tokens must have one entry a fork")
+        if n and max(tokens) > table.shape[1] * pool.page:
+            raise FcError(f"table has entries for {table.shape[1] * pool.page} tokens, {max(tokens)} are asked for")
+        tp, cs = self._table(table)
+        stream = self._raw_stream()
+        if ws is None:
+            ws = self._scratch("pages", self._L.fc_pages_workspace_bytes(pool.n_pages), stream)
+        rc = self._L.fc_pages_fork(self._h, stream, self._store(pool, "pool"), pool.H, pool.d, self._counts(ref, pool.n_pages), tp,
+                                   cs if table.shape[0] > 1 else table.shape[1], table.shape[0], n, _int32(src), _int32(dst), _int32(tokens),
+                                   self._ptr(status, "status", torch.int32), self._ptr(ws, "ws"), ws.numel())
+        if rc:
+            self._check(rc, "fc_pages_fork")
+        return table
+
+    def pages_compact(self, pool, ref, table, *, n_used=None, status=None, ws=None):
+        """Moves the used pages of the pool to its front and rewrites the counts and the table, which must be all of it; returns the table."""
+        tp, cs = self._table(table)
+        stream = self._raw_stream()
+        if ws is None:
+            ws = self._scratch("pages", self._L.fc_pages_workspace_bytes(pool.n_pages), stream)
+        rc = self._L.fc_pages_compact(self._h, stream, self._store(pool, "pool"), pool.H, pool.d, self._counts(ref, pool.n_pages), tp, cs,
+                                      table.shape[0], table.shape[1], self._ptr(n_used, "n_used", torch.int32),
+                                      self._ptr(status, "status", torch.int32), self._ptr(ws, "ws"), ws.numel())
+        if rc:
+            self._check(rc, "fc_pages_compact")
+        return table
+
+    # ------------------------------------------------------------------ fc_chunk_attention_kv8 / fc_chunk_attention_span
+    def chunk_attention_kv8(self, Q, pool, table, cache_len, K, V, q_chunk_row_off, kv_visible_len, active_ids, n_active, O, *, n_sink=0,
+                            kv_begin=None, window_first=None, seg_logical_off=None, seg_phys_off=None, lse=None, scale=0.0, impl=0,
+                            status=None, ws=None):
+        """fc_chunk_attention over [the first cache_len[c] tokens of chunk c in pages | plain tokens K, V from window_first[c] on]; a chunk
+        sees its tokens j < kv_visible_len[c] with j < n_sink or j >= kv_begin[c].
+
+        table [W, entries] has a row for each chunk, or one that all share.  K and V may be None (everything is in pages).  Without a
+        segment table the plain tokens are the rows of K and V in order."""
+        W = len(kv_visible_len)
+        if len(cache_len) != W:
+            raise FcError("cache_len and kv_visible_len must have one entry a chunk")
+        if table.shape[0] not in (1, W) or max(cache_len, default=0) > table.shape[1] * pool.page:
+            raise FcError("table must have one row, or one for each chunk, with entries for cache_len tokens")
+        tp, cs = self._table(table)
+        paged = (self._store(pool, "pool"), tp, cs if table.shape[0] > 1 else 0, _int32(cache_len), pool)
+        return self._span("kv8", Q, paged, K, V, q_chunk_row_off, kv_visible_len, n_sink, kv_begin, window_first, seg_logical_off,
+                          seg_phys_off, active_ids, n_active, O, lse, scale, impl, status, ws)
+
+    def chunk_attention_span(self, Q, K, V, q_chunk_row_off, kv_visible_len, seg_logical_off, seg_phys_off, active_ids, n_active, O, *,
+                             n_sink=0, kv_begin=None, lse=None, scale=0.0, impl=0, status=None, ws=None):
+        """fc_chunk_attention in which chunk c sees its tokens j < kv_visible_len[c] with j < n_sink or j >= kv_begin[c]."""
+        return self._span("span", Q, None, K, V, q_chunk_row_off, kv_visible_len, n_sink, kv_begin, None, seg_logical_off, seg_phys_off,
+                          active_ids, n_active, O, lse, scale, impl, status, ws)
+
+    def _span(self, kind, Q, paged, K, V, q_chunk_row_off, kv_visible_len, n_sink, kv_begin, window_first, seg_logical_off, seg_phys_off,
+              active_ids, n_active, O, lse, scale, impl, status, ws):
+        if Q.dim() != 3:
+            raise FcError("Q must be [heads, rows, d]")
+        H_q, rows, d = shape = Q.shape
+        dtype, dt = Q.dtype, _dt(Q)
+        qp, qh, qr = self._rows(Q, "Q", shape, dtype)
+        op, oh, orow = self._rows(O, "O", shape, dtype)
+        if paged is None and K is None:
+            raise FcError("K and V are None")
+        H_kv = paged[4].H if paged else K.shape[0]
+        if paged and paged[4].d != d:
+            raise FcError("Q and the pool must share the head size")
+        W = len(kv_visible_len)
+        if not active_ids.is_contiguous():
+            raise FcError("active_ids must be contiguous")
+        if len(q_chunk_row_off) != W + 1 or q_chunk_row_off[W] > rows or active_ids.numel() > W:
+            raise FcError("q_chunk_row_off must have one entry more than kv_visible_len and stay inside Q; active_ids at most as many")
+        for name, x in (("kv_begin", kv_begin), ("window_first", window_first)):
+            if x is not None and len(x) != W:
+                raise FcError(f"{name} must have one entry a chunk")
+        kp = vp = sl = sp = None
+        kh = kr = vh = vr = n_plain = n_seg = 0
+        if K is not None and V is not None:
+            n_plain = K.shape[1]
+            kp, kh, kr = self._rows(K, "K", (H_kv, n_plain, d), dtype)
+            vp, vh, vr = self._rows(V, "V", (H_kv, n_plain, d), dtype)
+            if seg_phys_off is None:
+                if n_plain:
+                    n_seg, sl, sp = 1, _int32((0, n_plain)), _int32((0,))
+            else:
+                n_seg = len(seg_phys_off)
+                if len(seg_logical_off) != n_seg + 1:
+                    raise FcError("seg_logical_off must have one entry more than seg_phys_off")
+                sl, sp = _int32(seg_logical_off), _int32(seg_phys_off)
+        elif K is not None or V is not None:
+            raise FcError("K and V: give both or neither")
+        dp = _ATTN_FIELDS.pack(H_q, H_kv, d, W, qh, qr, kh, kr, vh, vr, oh, orow, n_plain, scale, impl)
+        off, vis, stream = _int32(q_chunk_row_off), _int32(kv_visible_len), self._raw_stream()
+        begin = None if kv_begin is None else _int32(kv_begin)
+        first = None if window_first is None else _int32(window_first)
+        lse_hs = 0
+        if lse is not None:
+            if lse.dim() != 2 or lse.shape[0] != H_q or lse.shape[1] < q_chunk_row_off[W] or lse.stride(1) != 1:
+                raise FcError("lse must be [H_q, rows] with contiguous rows")
+            lse_hs = max(lse.stride(0), 1)
+        L, h = self._L, self._h
+        if ws is None:
+            need = (L.fc_chunk_attention_kv8_workspace_bytes(h, dp, dt, paged[4].page, paged[2], paged[3], off, vis, n_sink, begin, first, sl, n_seg)
+                    if paged else L.fc_chunk_attention_span_workspace_bytes(h, dp, dt, off, vis, n_sink, begin, sl, n_seg))
+            if need:
+                ws = self._scratch("attention_span", need, stream)
+        tail = (self._ptr(active_ids, "active_ids", torch.int32), self._ptr(n_active, "n_active", torch.int32), op,
+                self._ptr(lse, "lse", torch.float32), lse_hs, self._ptr(status, "status", torch.int32), self._ptr(ws, "ws"),
+                0 if ws is None else ws.numel())
+        if paged:
+            rc = L.fc_chunk_attention_kv8(h, stream, dp, qp, *paged[:4], kp, vp, dt, off, vis, n_sink, begin, first, sl, sp, n_seg, *tail)
+        else:
+            rc = L.fc_chunk_attention_span(h, stream, dp, qp, kp, vp, dt, off, vis, n_sink, begin, sl, sp, n_seg, *tail)
+        if rc:
+            self._check(rc, f"fc_chunk_attention_{kind}")
         return O

@@ -25,11 +25,11 @@
 #include <cmath>
 
 #include "fc_attention_kv4.cuh"
-#include "fc_tcgen05.cuh"
+#include "fc_mma_sync.cuh"
 
 namespace {
 
-using namespace fc::sm100;  // ex2, cvt_bf16x2, max3
+using namespace fc::sm100;  // mma and its operands, ex2, cvt_bf16x2, max3
 
 constexpr int kWarps = 4, kThreads = 32 * kWarps;
 constexpr int kStep = 16;  // keys per warp and step
@@ -39,34 +39,11 @@ constexpr int kWindowCost = 3;  // a window key has 3.6 times the bytes of a pac
 // faster at 64 rows of 24 heads over 28064 keys, 110 us against 125 before a step's products were moved up).
 constexpr int blocks_per_sm(int nt) { return nt == 1 ? 3 : 2; }
 
-__device__ __forceinline__ void mma(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
-  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
-               : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-               : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
-}
-__device__ __forceinline__ uint32_t transpose8x8(uint32_t x) {
-  uint32_t y;
-  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
-  return y;
-}
-// The three bf16 parts of fp32 numbers a, b as pairs (a low, b high): p[0] + p[1] + p[2] = (a, b) exactly.  The first two are rounded, not
-// cut: what is left of a number is then at most 2^-8 and 2^-17 of it, and the third part, seven bits at most, is exact.
-__device__ __forceinline__ void parts_of(float a, float b, uint32_t (&p)[3]) {
-#pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    p[i] = cvt_bf16x2(a, b);
-    a -= fc::bf16_lo(p[i]);
-    b -= fc::bf16_hi(p[i]);
-  }
-  p[2] = __byte_perm(__float_as_uint(a), __float_as_uint(b), 0x7632);
-}
 template <typename T> constexpr int kParts = sizeof(T) == 4 ? 3 : 1;  // of Q, and of a window's K and V
 // Of P.  bf16 rounds a weight by up to 2^-8, which is as much again as the output's own rounding: of up to eight rows, bound by
 // the unpacking, the rest of the weight is taken along (one token over 28080 keys: 32.5 us against 31.0, error 1.7e-3 against 2.4e-3);
 // of sixteen it would cost 20 to 25 %.
 template <typename T, int NT> constexpr int kWeightParts = sizeof(T) == 4 ? 3 : (NT == 1 ? 2 : 1);
-
-__device__ __forceinline__ uint32_t prmt(uint32_t a, uint32_t b, uint32_t sel) { return __byte_perm(a, b, sel); }
 
 // A warp's ring of 16-key steps in shared memory, filled by cp.async: the codes of K and V, then their scales.
 template <int D> struct Ring {
@@ -278,11 +255,6 @@ __device__ __forceinline__ void packed_weigh(State<D, NT>& st, const uint8_t* bu
       for (int t = 0; t < NT; ++t) weigh<T, NT>(st.o[t][4 * w + i], x, p0, p1, t);
     }
   }
-}
-
-__device__ __forceinline__ void store4(float* p, float4 x) { *reinterpret_cast<float4*>(p) = x; }
-__device__ __forceinline__ void store4(__nv_bfloat16* p, float4 x) {
-  *reinterpret_cast<uint2*>(p) = make_uint2(cvt_bf16x2(x.x, x.y), cvt_bf16x2(x.z, x.w));
 }
 
 template <typename T, int D, int NT>

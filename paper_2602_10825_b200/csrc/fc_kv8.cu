@@ -1,0 +1,375 @@
+// fc_kv8_append and fc_kv8_unpack: rows into and out of the paged 8-bit store.
+//
+// Both are bound by HBM: appending moves es + 1 bytes an element, unpacking 1 + es.
+//   append   a block of threads owns one block of the store (page and head; K or V), whose rows it holds in registers between the
+//            one read, the maximum that gives the scale, and the one write.  Rows that were there before are read only
+//            where the scale grows.
+//   unpack   eight codes a thread and access, several rows' loads in flight.
+//
+// Codes are the nearest ones to the true quotient, whatever the type.  A tie between two codes is a number t of at most five
+// significant bits, and a scale s has four.
+//   bf16 rows, and codes that are rounded again (8 significant bits: x is either t s or at least 2^-9 of it away): x (1/s) is off by
+//               2^-22 at most, so that it is rounded to 12 bits first, which puts a tie where it belongs and crosses none.
+//   fp32 rows   the rounded quotient is on the right side of a tie, or on it where x = t s: x is at least half an ulp of t, times s, away from
+//               t s otherwise, and more than half an ulp of the quotient.
+#include <algorithm>
+#include <climits>
+
+#include "fc_kv8.cuh"
+#include "fc_tcgen05.cuh"
+
+namespace {
+
+using fc::sm100::cvt_bf16x2;
+using fc::sm100::fma2;
+using fc::sm100::pack2;
+using fc::sm100::unpack2;
+
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+  uint64_t d;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+  return d;
+}
+// a in the low byte
+__device__ __forceinline__ uint32_t cvt_e4m3x2(float a, float b) {
+  uint16_t d;
+  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(d) : "f"(b), "f"(a));
+  return d;
+}
+
+// Eight elements as they lie in memory.
+template <typename T> struct Eight;
+template <> struct Eight<__nv_bfloat16> { uint4 w; };
+template <> struct Eight<float> { float4 a, b; };
+__device__ __forceinline__ void load8(const __nv_bfloat16* p, Eight<__nv_bfloat16>& x) { x.w = fc::ld_stream16(p); }
+__device__ __forceinline__ void load8(const float* p, Eight<float>& x) {
+  x.a = *reinterpret_cast<const float4*>(p);
+  x.b = *reinterpret_cast<const float4*>(p + 4);
+}
+__device__ __forceinline__ void get8(const Eight<__nv_bfloat16>& x, float (&v)[8]) {
+  const uint32_t w[4] = {x.w.x, x.w.y, x.w.z, x.w.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) v[2 * i] = fc::bf16_lo(w[i]), v[2 * i + 1] = fc::bf16_hi(w[i]);
+}
+__device__ __forceinline__ void get8(const Eight<float>& x, float (&v)[8]) {
+  v[0] = x.a.x; v[1] = x.a.y; v[2] = x.a.z; v[3] = x.a.w;
+  v[4] = x.b.x; v[5] = x.b.y; v[6] = x.b.z; v[7] = x.b.w;
+}
+
+// Bits of the largest finite magnitude; `bad` if an element is not finite.
+template <typename T>
+__device__ __forceinline__ uint32_t largest(const Eight<T>& x, bool& bad) {
+  float v[8];
+  get8(x, v);
+  uint32_t m = 0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const uint32_t a = __float_as_uint(v[i]) & 0x7fffffffu;
+    bad |= a >= 0x7f800000u;
+    m = max(m, a >= 0x7f800000u ? 0u : a);
+  }
+  return m;
+}
+
+// The least number of four significant bits whose 448-fold is not below a (bits of a finite magnitude): an upper bound of the
+// quotient cut to four bits is it, or the one before.  448 times a number of four bits is exact.
+__device__ __forceinline__ float scale_of(uint32_t a) {
+  if (a == 0) return 0.f;
+  const float x = fmaxf(__uint_as_float(a), 0x1.cp-109f);  // 448 2^-117
+  const uint32_t low = __float_as_uint(__fmul_ru(x, 0x1.24924ap-9f)) & ~0xfffffu;  // 1/448, rounded up
+  return fminf(__uint_as_float(448.f * __uint_as_float(low) >= x ? low : low + 0x100000u), 0x1p119f);
+}
+
+// Pairs of x / s: r = 1 / s, rounded.  See the head of the file for why this meets every tie.
+__device__ __forceinline__ uint32_t codes2_short(float x0, float x1, uint64_t r2) {
+  const uint64_t q = mul2(pack2(x0, x1), r2);
+  const uint64_t t = mul2(q, pack2(4097.f, 4097.f));
+  const uint64_t rest = fma2(q, pack2(-1.f, -1.f), t);      // t - q
+  const uint64_t cut = fma2(rest, pack2(-1.f, -1.f), t);    // q in 12 bits; NaN for an infinity
+  float a, b;
+  unpack2(cut, a, b);
+  return cvt_e4m3x2(a, b);
+}
+__device__ __forceinline__ uint2 codes8(const Eight<__nv_bfloat16>& x, float, float r) {
+  float v[8];
+  get8(x, v);
+  const uint64_t r2 = pack2(r, r);
+  return make_uint2(codes2_short(v[0], v[1], r2) | codes2_short(v[2], v[3], r2) << 16,
+                    codes2_short(v[4], v[5], r2) | codes2_short(v[6], v[7], r2) << 16);
+}
+__device__ __forceinline__ uint2 codes8(const Eight<float>& x, float s, float) {
+  float v[8];
+  get8(x, v);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) v[i] = fmaf(v[i], 0.f, s > 0.f ? __fdiv_rn(v[i], s) : v[i]);  // an infinity becomes a NaN
+  return make_uint2(cvt_e4m3x2(v[0], v[1]) | cvt_e4m3x2(v[2], v[3]) << 16, cvt_e4m3x2(v[4], v[5]) | cvt_e4m3x2(v[6], v[7]) << 16);
+}
+// Eight codes of scale s_old as codes of a larger scale.
+__device__ __forceinline__ uint2 again8(uint2 c, float s_old, float r) {
+  const uint64_t r2 = pack2(r, r);
+  auto four = [&](uint32_t w) {
+    const uint32_t lo = fc::e4m3_lo2(w), hi = fc::e4m3_hi2(w);
+    return codes2_short(fc::half_lo(lo) * s_old, fc::half_hi(lo) * s_old, r2) |
+           codes2_short(fc::half_lo(hi) * s_old, fc::half_hi(hi) * s_old, r2) << 16;
+  };
+  return make_uint2(four(c.x), four(c.y));
+}
+
+struct AppendGeom {
+  int32_t W;
+  int32_t block_end[FC_MAX_CHUNKS];  // running count of the pages that sequences write to
+  int32_t row_off[FC_MAX_CHUNKS + 1], pos[FC_MAX_CHUNKS];
+  int64_t k_hs, k_rs, v_hs, v_rs, table_cs;
+  fc::Kv8View pool;
+  const int32_t *table, *ref;
+};
+
+// kThreads threads hold kVec vectors of eight elements each: a block of page x d elements.
+template <typename T, int D, int kThreads, int kVec>
+__global__ void __launch_bounds__(kThreads)
+kv8_append_kernel(const T* __restrict__ K, const T* __restrict__ V, const __grid_constant__ AppendGeom g, uint32_t* __restrict__ status) {
+  constexpr int kRowVecs = D / 8;
+  __shared__ uint32_t largest_s[kThreads / 32];
+  const int tid = threadIdx.x, h = blockIdx.y;
+  const bool is_v = blockIdx.z != 0;
+  int c = 0;
+  while (c + 1 < g.W && (int)blockIdx.x >= g.block_end[c]) ++c;
+  const int entry = g.pos[c] / (1 << g.pool.page_log2) + (int)blockIdx.x - (c > 0 ? g.block_end[c - 1] : 0);
+  const int page_id = g.table[c * g.table_cs + entry];
+  if (page_id < 0 || page_id >= g.pool.n_pages || (g.ref && g.ref[page_id] != 1)) {
+    if (tid == 0 && status) atomicOr(status, (uint32_t)FC_DEV_BAD_INDEX);
+    return;
+  }
+  // rows lo .. hi - 1 of the block are new; row r of it is row src0 + r of the source
+  const int64_t token0 = (int64_t)entry << g.pool.page_log2, src0 = g.row_off[c] + token0 - g.pos[c];
+  const int page = 1 << g.pool.page_log2;
+  const int lo = (int)max(g.pos[c] - token0, (int64_t)0);
+  const int hi = (int)min((int64_t)page, g.pos[c] + (int64_t)(g.row_off[c + 1] - g.row_off[c]) - token0);
+  const T* src = (is_v ? V + h * g.v_hs : K + h * g.k_hs);
+  const int64_t rs = is_v ? g.v_rs : g.k_rs;
+  uint8_t* codes = (is_v ? g.pool.v_codes : g.pool.k_codes) + page_id * g.pool.code_ps + h * g.pool.code_hs;
+  float* scale_p = (is_v ? g.pool.v_scales : g.pool.k_scales) + page_id * g.pool.scale_ps + h * g.pool.scale_hs;
+
+  Eight<T> x[kVec];
+  bool bad = false;
+  uint32_t a = 0;
+#pragma unroll
+  for (int i = 0; i < kVec; ++i) {
+    const int vec = tid + i * kThreads, row = vec / kRowVecs;
+    if (row >= lo && row < hi) load8(src + (src0 + row) * rs + vec % kRowVecs * 8, x[i]);
+  }
+  const float s_old = lo > 0 ? *scale_p : 0.f;
+#pragma unroll
+  for (int i = 0; i < kVec; ++i) {
+    const int row = (tid + i * kThreads) / kRowVecs;
+    if (row >= lo && row < hi) a = max(a, largest(x[i], bad));
+  }
+  a = __reduce_max_sync(0xffffffffu, a);
+  if (tid % 32 == 0) largest_s[tid / 32] = a;
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < kThreads / 32; ++i) a = max(a, largest_s[i]);
+  const float s = fmaxf(scale_of(a), s_old), r = s > 0.f ? __frcp_rn(s) : 0.f;
+#pragma unroll
+  for (int i = 0; i < kVec; ++i) {
+    const int vec = tid + i * kThreads, row = vec / kRowVecs;
+    uint2* at = reinterpret_cast<uint2*>(codes + vec * 8);
+    if (row >= lo && row < hi) *at = codes8(x[i], s, r);
+    else if (row < lo && s > s_old) *at = again8(*at, s_old, r);
+  }
+  if (tid == 0 && (lo == 0 || s > s_old)) *scale_p = s;  // every thread has read the old one before the barrier
+  if (bad && status) atomicOr(status, (uint32_t)FC_DEV_NONFINITE);
+}
+
+struct UnpackGeom {
+  fc::Kv8Jobs jobs;
+  int64_t k_hs, k_rs, v_hs, v_rs, table_cs;
+  fc::Kv8View src;
+  const int32_t* table;
+  uint32_t *status, *clear;
+};
+
+constexpr int kUnpackThreads = 256;
+constexpr int kUnpackRows = 4;  // rows whose loads are in flight together
+
+__device__ __forceinline__ void store8(__nv_bfloat16* p, const float (&v)[8]) {
+  *reinterpret_cast<uint4*>(p) = make_uint4(cvt_bf16x2(v[0], v[1]), cvt_bf16x2(v[2], v[3]), cvt_bf16x2(v[4], v[5]), cvt_bf16x2(v[6], v[7]));
+}
+__device__ __forceinline__ void store8(float* p, const float (&v)[8]) {
+  *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
+  *reinterpret_cast<float4*>(p + 4) = make_float4(v[4], v[5], v[6], v[7]);
+}
+
+template <typename T, int D>
+__global__ void __launch_bounds__(kUnpackThreads)
+kv8_unpack_kernel(T* __restrict__ K, T* __restrict__ V, const __grid_constant__ UnpackGeom g) {
+  constexpr int kRowVecs = D / 8, R = kUnpackThreads / kRowVecs;
+  fc::pdl_launch_dependents();
+  const int w = threadIdx.x % kRowVecs, h = blockIdx.y;
+  const bool is_v = blockIdx.z & 1;
+  if (g.clear && threadIdx.x == 0 && blockIdx.x == 0 && h == 0 && blockIdx.z == 0) *g.clear = 0;
+  T* dst = is_v ? V : K;
+  if (!dst) return;
+  const fc::Kv8Job job = g.jobs.job[blockIdx.z >> 1];
+  const int64_t r0 = (int64_t)blockIdx.x * kUnpackRows * R + threadIdx.x / kRowVecs;
+  if (r0 >= job.n) return;
+  const uint8_t* codes = (is_v ? g.src.v_codes : g.src.k_codes) + h * g.src.code_hs;
+  const float* scales = (is_v ? g.src.v_scales : g.src.k_scales) + h * g.src.scale_hs;
+  const int64_t hs = is_v ? g.v_hs : g.k_hs, rs = is_v ? g.v_rs : g.k_rs;
+  const int32_t* table = g.table + job.seq * g.table_cs;
+  int32_t page_id[kUnpackRows];
+  uint2 word[kUnpackRows];
+  float scale[kUnpackRows];
+#pragma unroll
+  for (int u = 0; u < kUnpackRows; ++u) {
+    const int64_t r = r0 + u * R;
+    page_id[u] = r < job.n ? __ldg(table + ((job.first + r) >> g.src.page_log2)) : -1;
+  }
+  bool bad = false;
+#pragma unroll
+  for (int u = 0; u < kUnpackRows; ++u) {
+    const int64_t r = r0 + u * R;
+    word[u] = make_uint2(0u, 0u);
+    scale[u] = 0.f;
+    if (r >= job.n) continue;
+    if (page_id[u] >= 0 && page_id[u] < g.src.n_pages) {
+      const int in_page = (int)((job.first + r) & ((1 << g.src.page_log2) - 1));
+      word[u] = __ldg(reinterpret_cast<const uint2*>(codes + page_id[u] * g.src.code_ps + in_page * D + 8 * w));
+      scale[u] = __ldg(scales + page_id[u] * g.src.scale_ps);
+    } else {
+      bad = true;
+    }
+  }
+#pragma unroll
+  for (int u = 0; u < kUnpackRows; ++u) {
+    const int64_t r = r0 + u * R;
+    if (r >= job.n) continue;
+    const uint32_t p[4] = {fc::e4m3_lo2(word[u].x), fc::e4m3_hi2(word[u].x), fc::e4m3_lo2(word[u].y), fc::e4m3_hi2(word[u].y)};
+    float v[8];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[2 * i] = fc::half_lo(p[i]) * scale[u], v[2 * i + 1] = fc::half_hi(p[i]) * scale[u];
+    store8(dst + h * hs + (job.dst_row + r) * rs + 8 * w, v);
+  }
+  if (bad && g.status) atomicOr(g.status, (uint32_t)FC_DEV_BAD_INDEX);
+}
+
+int check_rows(const void* p, int d, int es, int64_t hs, int64_t rs) {
+  if (!fc::aligned16(p)) return FC_ERR_MISALIGNED;
+  if (hs < 0 || rs < 0 || (hs * es) % 16 || (rs * es) % 16) return FC_ERR_MISALIGNED;
+  return rs < d ? FC_ERR_INVALID_ARG : FC_OK;
+}
+
+// What append and unpack ask of their common arguments: `at` is the first token of each sequence's rows.
+int check_common(const fc_kv8_rows* desc, int dtype, const int32_t* row_off, const int32_t* at) {
+  if (dtype != FC_BF16 && dtype != FC_F32) return FC_ERR_UNSUPPORTED;
+  if (desc->d != 64 && desc->d != 128) return FC_ERR_UNSUPPORTED;
+  if (desc->H <= 0 || desc->W <= 0 || !row_off || !at) return FC_ERR_INVALID_ARG;
+  if (desc->H > 65535 || desc->W > FC_MAX_CHUNKS) return FC_ERR_UNSUPPORTED;
+  for (int c = 0; c < desc->W; ++c) {
+    if (row_off[c] < 0 || row_off[c + 1] < row_off[c] || at[c] < 0) return FC_ERR_INVALID_ARG;
+    if ((int64_t)at[c] + (row_off[c + 1] - row_off[c]) > INT32_MAX - 4096) return FC_ERR_UNSUPPORTED;
+  }
+  return FC_OK;
+}
+
+}  // namespace
+
+namespace fc {
+
+int kv8_unpack_launch(cudaStream_t st, const Kv8View& src, int H, int d, const int32_t* table, int64_t table_cs, const Kv8Jobs& jobs,
+                      void* K_dst, void* V_dst, int dtype, int64_t k_hs, int64_t k_rs, int64_t v_hs, int64_t v_rs,
+                      uint32_t* status, uint32_t* clear) {
+  int n = 0;
+  for (int i = 0; i < jobs.n; ++i) n = std::max(n, jobs.job[i].n);
+  if (n == 0 || (!K_dst && !V_dst)) return FC_OK;
+  UnpackGeom g = {jobs, k_hs, k_rs, v_hs, v_rs, table_cs, src, table, status, clear};
+  const int rows = kUnpackRows * kUnpackThreads / (d / 8);
+  const dim3 grid((unsigned)((n + (int64_t)rows - 1) / rows), (unsigned)H, 2u * jobs.n);
+#define FC_UNPACK(T, D) kv8_unpack_kernel<T, D><<<grid, kUnpackThreads, 0, st>>>((T*)K_dst, (T*)V_dst, g)
+  if (dtype == FC_F32) { if (d == 128) FC_UNPACK(float, 128); else FC_UNPACK(float, 64); }
+  else { if (d == 128) FC_UNPACK(__nv_bfloat16, 128); else FC_UNPACK(__nv_bfloat16, 64); }
+#undef FC_UNPACK
+  FC_LAUNCH_CHECK("kv8_unpack_kernel");
+  return FC_OK;
+}
+
+}  // namespace fc
+
+extern "C" int fc_kv8_append(fc_ctx* ctx, void* stream, const fc_kv8_rows* desc, const void* K_src, const void* V_src, int dtype,
+                             const int32_t* row_off, const int32_t* pos, const fc_kv8_pool* pool, const int32_t* table,
+                             int64_t table_cs, const int32_t* ref, uint32_t* status) {
+  if (!ctx || !desc) return FC_ERR_INVALID_ARG;
+  int rc = check_common(desc, dtype, row_off, pos);
+  if (rc != FC_OK) return rc;
+  if (row_off[desc->W] == row_off[0]) return FC_OK;
+  if (!K_src || !V_src || !table || table_cs < 0) return FC_ERR_INVALID_ARG;
+  const int es = fc::elem_size(dtype);
+  if ((rc = check_rows(K_src, desc->d, es, desc->k_hs, desc->k_rs)) != FC_OK) return rc;
+  if ((rc = check_rows(V_src, desc->d, es, desc->v_hs, desc->v_rs)) != FC_OK) return rc;
+  if ((rc = fc::kv8_check(pool, desc->H, desc->d)) != FC_OK) return rc;
+  AppendGeom g = {};
+  g.W = desc->W;
+  g.pool = fc::kv8_view(*pool);
+  int64_t blocks = 0;
+  for (int c = 0; c < g.W; ++c) {
+    const int64_t n = row_off[c + 1] - row_off[c], end = ((int64_t)pos[c] + n + pool->page - 1) / pool->page;
+    if (n > 0) {
+      if (g.W > 1 && table_cs < end) return FC_ERR_INVALID_ARG;  // rows of the table would overlap
+      blocks += end - pos[c] / pool->page;
+    }
+    if (blocks > INT32_MAX) return FC_ERR_UNSUPPORTED;
+    g.block_end[c] = (int32_t)blocks;
+    g.row_off[c] = row_off[c];
+    g.pos[c] = pos[c];
+  }
+  g.row_off[g.W] = row_off[g.W];
+  g.k_hs = desc->k_hs; g.k_rs = desc->k_rs; g.v_hs = desc->v_hs; g.v_rs = desc->v_rs;
+  g.table = table; g.table_cs = table_cs; g.ref = ref;
+  FC_DEVICE_GUARD(ctx);
+  cudaStream_t st = (cudaStream_t)stream;
+  const dim3 grid((unsigned)blocks, (unsigned)desc->H, 2);
+#define FC_APPEND(T, D, THREADS, VEC) kv8_append_kernel<T, D, THREADS, VEC><<<grid, THREADS, 0, st>>>((const T*)K_src, (const T*)V_src, g, status)
+#define FC_APPEND_PICK(T)                                                                                                        \
+  do {                                                                                                                           \
+    if (desc->d == 128) switch (pool->page) {                                                                                    \
+      case 16: FC_APPEND(T, 128, 256, 1); break;                                                                                 \
+      case 32: FC_APPEND(T, 128, 256, 2); break;                                                                                 \
+      case 64: FC_APPEND(T, 128, 256, 4); break;                                                                                 \
+      default: FC_APPEND(T, 128, 256, 8);                                                                                        \
+    } else switch (pool->page) {                                                                                                 \
+      case 16: FC_APPEND(T, 64, 128, 1); break;                                                                                  \
+      case 32: FC_APPEND(T, 64, 256, 1); break;                                                                                  \
+      case 64: FC_APPEND(T, 64, 256, 2); break;                                                                                  \
+      default: FC_APPEND(T, 64, 256, 4);                                                                                         \
+    }                                                                                                                            \
+  } while (0)
+  if (dtype == FC_F32) FC_APPEND_PICK(float);
+  else FC_APPEND_PICK(__nv_bfloat16);
+#undef FC_APPEND_PICK
+#undef FC_APPEND
+  FC_LAUNCH_CHECK("kv8_append_kernel");
+  return FC_OK;
+}
+
+extern "C" int fc_kv8_unpack(fc_ctx* ctx, void* stream, const fc_kv8_rows* desc, const fc_kv8_pool* pool, const int32_t* table,
+                             int64_t table_cs, const int32_t* first, const int32_t* row_off, void* K_dst, void* V_dst, int dtype,
+                             uint32_t* status) {
+  if (!ctx || !desc) return FC_ERR_INVALID_ARG;
+  int rc = check_common(desc, dtype, row_off, first);
+  if (rc != FC_OK) return rc;
+  if (row_off[desc->W] == row_off[0]) return FC_OK;
+  if ((!K_dst && !V_dst) || !table || table_cs < 0) return FC_ERR_INVALID_ARG;
+  const int es = fc::elem_size(dtype);
+  if (K_dst && (rc = check_rows(K_dst, desc->d, es, desc->k_hs, desc->k_rs)) != FC_OK) return rc;
+  if (V_dst && (rc = check_rows(V_dst, desc->d, es, desc->v_hs, desc->v_rs)) != FC_OK) return rc;
+  const int64_t rows = row_off[desc->W];
+  if (K_dst && !fc::grid_disjoint(desc->H, desc->k_hs, rows, desc->k_rs, desc->d)) return FC_ERR_INVALID_ARG;  // rows overlap
+  if (V_dst && !fc::grid_disjoint(desc->H, desc->v_hs, rows, desc->v_rs, desc->d)) return FC_ERR_INVALID_ARG;
+  if ((rc = fc::kv8_check(pool, desc->H, desc->d)) != FC_OK) return rc;
+  fc::Kv8Jobs jobs = {};
+  for (int c = 0; c < desc->W; ++c)
+    if (row_off[c + 1] > row_off[c]) jobs.job[jobs.n++] = {c, first[c], row_off[c + 1] - row_off[c], row_off[c]};
+  FC_DEVICE_GUARD(ctx);
+  return fc::kv8_unpack_launch((cudaStream_t)stream, fc::kv8_view(*pool), desc->H, desc->d, table, table_cs, jobs, K_dst, V_dst,
+                               dtype, desc->k_hs, desc->k_rs, desc->v_hs, desc->v_rs, status, nullptr);
+}

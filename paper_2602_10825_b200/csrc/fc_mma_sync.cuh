@@ -1,0 +1,44 @@
+// What the kernels share that feed mma.sync from registers.
+#pragma once
+
+#include "fc_common.cuh"
+#include "fc_tcgen05.cuh"
+
+namespace fc {
+namespace sm100 {
+
+__device__ __forceinline__ void mma(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+               : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+               : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+               : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+               : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t transpose8x8(uint32_t x) {
+  uint32_t y;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+  return y;
+}
+// The three bf16 parts of fp32 numbers a, b as pairs (a low, b high): p[0] + p[1] + p[2] = (a, b) exactly.  The first two are rounded, not
+// cut: what is left of a number is then at most 2^-8 and 2^-17 of it, and the third part, seven bits at most, is exact.
+__device__ __forceinline__ void parts_of(float a, float b, uint32_t (&p)[3]) {
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    p[i] = cvt_bf16x2(a, b);
+    a -= fc::bf16_lo(p[i]);
+    b -= fc::bf16_hi(p[i]);
+  }
+  p[2] = __byte_perm(__float_as_uint(a), __float_as_uint(b), 0x7632);
+}
+__device__ __forceinline__ uint32_t prmt(uint32_t a, uint32_t b, uint32_t sel) { return __byte_perm(a, b, sel); }
+
+__device__ __forceinline__ void store4(float* p, float4 x) { *reinterpret_cast<float4*>(p) = x; }
+__device__ __forceinline__ void store4(__nv_bfloat16* p, float4 x) {
+  *reinterpret_cast<uint2*>(p) = make_uint2(cvt_bf16x2(x.x, x.y), cvt_bf16x2(x.z, x.w));
+}
+
+}  // namespace sm100
+}  // namespace fc
