@@ -39,6 +39,12 @@ struct AttnSplit {
 };
 constexpr int kMaxParts = 32;
 
+// What each chunk sees where that is more than a prefix: rows [lo[i][c], hi[i][c]) of the first store (i = 0, 1), and tokens of
+// the segment table (i = 2, 3), in this order.
+struct AttnSpans {
+  int32_t lo[4][FC_MAX_CHUNKS], hi[4][FC_MAX_CHUNKS];
+};
+
 // Parts for each of `rest` items of `tiles` key tiles on `blocks` blocks.  The unit is the time of a key tile, 1.8 us; the
 // joining kernel costs three of them, and the parts' bytes go at 4 TB/s.
 __host__ __device__ inline int split_parts(int rest, int blocks, int tiles, int d, int slots, float* cost) {
@@ -60,16 +66,17 @@ int attention_tc(fc_ctx* ctx, cudaStream_t st, const AttnGeom& g, const void* Q,
                  const void* V, void* O, void* ws, size_t ws_bytes);
 size_t attention_tc_workspace_bytes();
 // The same over two stores: logical tokens [0, n0) are the rows of K0 / V0 (dense [H_kv, n0, d]), the others are found
-// in K / V through the segment table, whose offsets count from n0.  `before` is called once nothing but launches is left that
+// in K / V through the segment table, whose offsets count from n0.  With `spans` these say what each chunk sees, g.vis counts the keys of
+// a chunk, and the segment table's offsets count from 0.  `before` is called once nothing but launches is left that
 // could fail; it launches the kernel that writes K0 / V0.
 int attention_tc_two(fc_ctx* ctx, cudaStream_t st, const AttnGeom& g, const void* Q, const void* K0, const void* V0, int n0,
                      const void* K, const void* V, const AttnSplit& split, void* O, void* ws, size_t ws_bytes,
-                     int (*before)(void*), void* arg);
+                     int (*before)(void*), void* arg, const AttnSpans* spans = nullptr);
 // warp-specialised kernel; tensor maps as built by attention_tc (tk0, tv0: those of the second store, or NULL),
 // `counter` = 4 bytes of workspace
 int attention_ws_launch(fc_ctx* ctx, cudaStream_t st, const AttnGeom& g, const CUtensorMap& tq,
                         const CUtensorMap& tk, const CUtensorMap& tv, const CUtensorMap* tk0, const CUtensorMap* tv0,
-                        const AttnSplit& split, void* O, uint32_t* counter);
+                        const AttnSplit& split, const AttnSpans* spans, void* O, uint32_t* counter);
 bool attention_tc_supported(const AttnGeom& g, int dtype);
 // Tensor map of a [heads, rows, d] bf16 tensor: box = 64 elements (128 bytes) x `box_rows` rows x 1 head, 128-byte
 // swizzle; rows past `rows` read as zero.

@@ -82,15 +82,104 @@ bool sees_rows(const fc::SpanGeom& g) {
   return false;
 }
 
+// The tcgen05 path: what is seen of the pages is unpacked into the workspace first, [H_kv, rows, d] of K and of V, and the tokens'
+// spans become rows of that.
+struct TilePlan {
+  fc::AttnSplit split;
+  fc::AttnSpans spans;
+  fc::Kv8Jobs jobs;
+  int32_t vis[FC_MAX_CHUNKS];  // keys that each chunk sees
+  int rows;                    // of the workspace, per head
+  size_t k, v, plan, o, ml, bytes;  // offsets
+  double us;                        // estimate of the whole path
+};
+
+// False if there are more rows to unpack than a tensor map's place can name.
+bool plan_tiles(const fc_ctx* ctx, const fc::SpanGeom& g, TilePlan& p) {
+  // the tokens to unpack: of the shared sequence those that some chunk sees, else each chunk's own
+  const bool shared = g.table_cs == 0;
+  for (int c = 0; c < g.W; ++c) {
+    for (int i = 0; i < 4; ++i) p.spans.lo[i][c] = g.lo[i][c], p.spans.hi[i][c] = g.hi[i][c];
+    p.vis[c] = 0;
+    for (int i = 0; i < 4; ++i) p.vis[c] += g.hi[i][c] - g.lo[i][c];
+  }
+  p.rows = 0;
+  p.jobs.n = 0;
+  for (int c0 = 0; c0 < g.W; c0 += shared ? g.W : 1) {
+    const int c1 = shared ? g.W : c0 + 1;
+    int first = 0, from = INT32_MAX, to = 0;  // tokens [0, first) and [from, to)
+    for (int c = c0; c < c1; ++c) {
+      if (fc::span_rows(g, c) == 0) continue;
+      first = std::max(first, g.hi[0][c]);
+      if (g.hi[1][c] > g.lo[1][c]) from = std::min(from, g.lo[1][c]), to = std::max(to, g.hi[1][c]);
+    }
+    if (from <= first) first = std::max(first, to), from = to = 0;
+    else if (to == 0) from = 0;
+    const int at_first = p.rows, at_from = p.rows + first - from;  // row of token 0, and of token 0 counted from the second range
+    if (first > 0) p.jobs.job[p.jobs.n++] = {shared ? 0 : c0, 0, first, p.rows};
+    if (to > from) p.jobs.job[p.jobs.n++] = {shared ? 0 : c0, from, to - from, p.rows + first};
+    for (int c = c0; c < c1; ++c)
+      for (int i = 0; i < 2; ++i) {
+        const int move = to > from && g.lo[i][c] >= from ? at_from : at_first;
+        p.spans.lo[i][c] += move;
+        p.spans.hi[i][c] += move;
+      }
+    if ((int64_t)p.rows + first + (to - from) > INT32_MAX - 4096) return false;
+    p.rows += first + to - from;
+  }
+  // grouped heads share their key tiles where whole groups fill a tile of 128 rows
+  p.split = fc::AttnSplit();
+  if (128 % g.group == 0 && (int64_t)g.q_row_off[g.W] * g.group <= INT32_MAX - 4096) p.split.pack = g.group;
+  int64_t items = 0, tiles = 0;  // work items of 256 rows, and the key tiles that they take together
+  int most = 0;
+  for (int c = 0; c < g.W; ++c) {
+    const int64_t n = ((int64_t)(g.q_row_off[c + 1] - g.q_row_off[c]) * p.split.pack + 255) / 256;
+    items += n;
+    tiles += n * ((p.vis[c] + 127) / 128);
+    if (n > 0) most = std::max(most, p.vis[c]);
+  }
+  items *= g.H_q / p.split.pack;
+  tiles *= g.H_q / p.split.pack;
+  const int most_tiles = (most + 127) / 128;
+  if (most_tiles >= 6) p.split.slots = (int32_t)std::min<int64_t>(3 * ctx->sm_count, items * fc::kMaxParts);
+  float last = 0.f;
+  const int rest = (int)(items % ctx->sm_count);
+  if (rest > 0) fc::split_parts(rest, ctx->sm_count, most_tiles, g.d, p.split.slots, &last);
+  // 8 us for the launches of the path, 1.8 us a key tile, the unpacking at 5 TB/s
+  const double whole = items > 0 ? (double)tiles / items : 0;
+  p.us = 8 + 1.8 * ((double)(items / ctx->sm_count) * whole + last) + 2.0 * g.H_kv * p.rows * g.d * 3 / 5e6;
+  const size_t bytes = (size_t)g.H_kv * p.rows * g.d * 2, parts = (size_t)p.split.slots * 256;
+  p.k = fc::attention_tc_workspace_bytes();
+  p.v = p.k + fc::align_up(bytes, 256);
+  p.plan = p.v + fc::align_up(bytes, 256);
+  p.o = p.plan + fc::align_up((4 + 4 * (size_t)ctx->sm_count) * sizeof(int32_t), 256);
+  p.ml = p.o + parts * g.d * sizeof(float);
+  p.bytes = p.ml + parts * sizeof(float2);
+  return true;
+}
+
+// Strides of Q that a tensor map takes.  The kernel for few rows takes any.
+bool maps_fit(const fc_attn_desc* d) { return d->q_rs < (1ll << 38) && (d->H_q == 1 || (d->q_hs > 0 && d->q_hs < (1ll << 31))); }
+
+// What a call does, with the workspace it takes and the split of the keys in g.
 struct Plan {
   bool tiles;  // the tcgen05 kernel
+  TilePlan t;
   size_t bytes;
 };
-Plan plan(const fc_ctx* ctx, const fc_attn_desc* desc, fc::SpanGeom& g) {
-  (void)desc;
-  Plan p = {};
-  p.bytes = fc::span_rows_workspace(ctx, g);
-  return p;
+int plan(const fc_ctx* ctx, const fc_attn_desc* desc, fc::SpanGeom& g, Plan& p) {
+  p.tiles = false;
+  if (desc->impl != 2) {
+    p.bytes = fc::span_rows_workspace(ctx, g);
+    if (desc->impl == 3 || g.f32) return FC_OK;
+  }
+  const bool fits = maps_fit(desc) && plan_tiles(ctx, g, p.t);
+  if (!fits && desc->impl == 2) return FC_ERR_UNSUPPORTED;
+  if (fits && (desc->impl == 2 || p.t.us < g.rows_us)) {
+    p.tiles = true;
+    p.bytes = p.t.bytes;
+  }
+  return FC_OK;
 }
 
 int attend(fc_ctx* ctx, void* stream, const fc_attn_desc* desc, const void* Q, const fc_kv8_pool* pool, const int32_t* table,
@@ -137,19 +226,51 @@ int attend(fc_ctx* ctx, void* stream, const fc_attn_desc* desc, const void* Q, c
   g.lse_hs = lse_hs;
   g.active_ids = active_ids; g.n_active = n_active; g.lse = lse; g.status = status;
 
-  const Plan p = plan(ctx, desc, g);
+  Plan p;
+  if ((rc = plan(ctx, desc, g, p)) != FC_OK) return rc;
   if (p.bytes > 0) {
     if (!ws || ws_bytes < p.bytes) return FC_ERR_WORKSPACE;
     if (!fc::aligned16(ws)) return FC_ERR_MISALIGNED;
   }
   FC_DEVICE_GUARD(ctx);
   cudaStream_t st = (cudaStream_t)stream;
-  if (p.bytes > 0) {
-    const size_t r = (size_t)g.H_kv * g.block_end[g.W - 1] * 8 * g.row_tiles;
-    g.part_o = (float*)ws;
-    g.part_ml = (float2*)((char*)ws + fc::align_up(r * g.d * sizeof(float), 256));
+  char* base = (char*)ws;
+  if (!p.tiles) {
+    if (p.bytes > 0) {
+      const size_t r = (size_t)g.H_kv * g.block_end[g.W - 1] * 8 * g.row_tiles;
+      g.part_o = (float*)ws;
+      g.part_ml = (float2*)(base + fc::align_up(r * g.d * sizeof(float), 256));
+    }
+    return fc::span_rows_launch(ctx, st, g, Q, K, V, O);
   }
-  return fc::span_rows_launch(ctx, st, g, Q, K, V, O);
+  TilePlan& t = p.t;
+  fc::AttnGeom a = {};
+  a.H_q = g.H_q; a.H_kv = g.H_kv; a.d = g.d; a.W = g.W; a.group = g.group; a.n_seg = rows ? g.n_seg : 0;
+  a.q_hs = g.q_hs; a.q_rs = g.q_rs; a.k_hs = g.k_hs; a.k_rs = g.k_rs; a.v_hs = g.v_hs; a.v_rs = g.v_rs; a.o_hs = g.o_hs; a.o_rs = g.o_rs;
+  a.kv_rows = g.kv_rows; a.lse_hs = g.lse_hs; a.scale = g.scale;
+  std::copy(g.q_row_off, g.q_row_off + g.W + 1, a.q_row_off);
+  std::copy(t.vis, t.vis + g.W, a.vis);
+  std::copy(g.seg_log, g.seg_log + g.n_seg + 1, a.seg_log);
+  std::copy(g.seg_phys, g.seg_phys + g.n_seg, a.seg_phys);
+  a.active_ids = active_ids; a.n_active = n_active; a.lse = lse; a.status = status;
+  struct Unpack {
+    cudaStream_t st;
+    const fc::SpanGeom* g;
+    const TilePlan* t;
+    void *k, *v;
+    uint32_t* counter;
+  } unpack = {st, &g, &t, base + t.k, base + t.v, (uint32_t*)ws};
+  auto before = [](void* arg) -> int {
+    const Unpack& x = *(const Unpack*)arg;
+    const int64_t hs = (int64_t)x.t->rows * x.g->d;
+    return fc::kv8_unpack_launch(x.st, x.g->pool, x.g->H_kv, x.g->d, x.g->table, x.g->table_cs, x.t->jobs, x.k, x.v, FC_BF16, hs, x.g->d, hs,
+                                 x.g->d, x.g->status, x.counter);
+  };
+  t.split.follows = t.rows > 0;
+  t.split.o = (float*)(base + t.o);
+  t.split.ml = (float2*)(base + t.ml);
+  t.split.plan = (int32_t*)(base + t.plan);
+  return fc::attention_tc_two(ctx, st, a, Q, base + t.k, base + t.v, t.rows, K, V, t.split, O, ws, ws_bytes, before, &unpack, &t.spans);
 }
 
 size_t workspace(const fc_ctx* ctx, const fc_attn_desc* desc, int dtype, int page, int64_t table_cs, const int32_t* q_chunk_row_off,
@@ -157,7 +278,8 @@ size_t workspace(const fc_ctx* ctx, const fc_attn_desc* desc, int dtype, int pag
   fc::SpanGeom g = {};
   if (!ctx || check_geometry(desc, dtype, page, table_cs, q_chunk_row_off, visible, seg_logical_off, n_seg, g) != FC_OK) return 0;
   if (g.q_row_off[g.W] == g.q_row_off[0]) return 0;
-  return plan(ctx, desc, g).bytes;
+  Plan p;
+  return plan(ctx, desc, g, p) == FC_OK ? p.bytes : 0;
 }
 
 }  // namespace

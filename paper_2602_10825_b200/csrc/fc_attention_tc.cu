@@ -135,23 +135,27 @@ int attention_tc(fc_ctx* ctx, cudaStream_t st, const AttnGeom& g_in, const void*
     if ((rc = make_tmap(ctx, &tk, K, g.d, g.kv_rows, g.H_kv, g.k_rs, g.H_kv > 1 ? g.k_hs : g.k_rs * g.kv_rows)) != FC_OK) return rc;
     if ((rc = make_tmap(ctx, &tv, V, g.d, g.kv_rows, g.H_kv, g.v_rs, g.H_kv > 1 ? g.v_hs : g.v_rs * g.kv_rows)) != FC_OK) return rc;
   }
-  return attention_ws_launch(ctx, st, g, tq, tk, tv, nullptr, nullptr, AttnSplit(), O, (uint32_t*)ws);
+  return attention_ws_launch(ctx, st, g, tq, tk, tv, nullptr, nullptr, AttnSplit(), nullptr, O, (uint32_t*)ws);
 }
 
 int attention_tc_two(fc_ctx* ctx, cudaStream_t st, const AttnGeom& g_in, const void* Q, const void* K0, const void* V0, int n0,
                      const void* K, const void* V, const AttnSplit& split, void* O, void* ws, size_t ws_bytes,
-                     int (*before)(void*), void* arg) {
+                     int (*before)(void*), void* arg, const AttnSpans* spans) {
   if (!ws || ws_bytes < attention_tc_workspace_bytes()) return FC_ERR_WORKSPACE;
   if (!aligned16(ws)) return FC_ERR_MISALIGNED;
   AttnGeom g = g_in;
   g.n_seg = g.n_seg0 = 0;
-  if (n0 > 0) {
-    g.seg_log[0] = 0;
-    g.seg_log[1] = n0;
-    g.seg_phys[0] = 0;
-    g.n_seg = g.n_seg0 = 1;
+  if (spans) {
+    g.n_seg = merge_segments(g_in, g, 0, 0);
+  } else {
+    if (n0 > 0) {
+      g.seg_log[0] = 0;
+      g.seg_log[1] = n0;
+      g.seg_phys[0] = 0;
+      g.n_seg = g.n_seg0 = 1;
+    }
+    g.n_seg = merge_segments(g_in, g, g.n_seg, n0);
   }
-  g.n_seg = merge_segments(g_in, g, g.n_seg, n0);
   const int64_t q_rows = g.q_row_off[g.W];
   if (q_rows == 0) return FC_OK;
   CUtensorMap tq, tk0, tv0, tk, tv;
@@ -170,7 +174,7 @@ int attention_tc_two(fc_ctx* ctx, cudaStream_t st, const AttnGeom& g_in, const v
   }
   if (n0 == 0) tk0 = tk, tv0 = tv;
   if ((rc = before(arg)) != FC_OK) return rc;
-  return attention_ws_launch(ctx, st, g, tq, tk, tv, &tk0, &tv0, split, O, (uint32_t*)ws);
+  return attention_ws_launch(ctx, st, g, tq, tk, tv, &tk0, &tv0, split, spans, O, (uint32_t*)ws);
 }
 
 }  // namespace fc

@@ -43,7 +43,7 @@
 // every exponential on the special-function unit, and masked columns are forced to 0); the V rows themselves are
 // overwritten with zeros in shared memory by warp 11 before the PV instructions of that tile are issued, so that not
 // even a NaN or an infinity in such a row can reach an output (0 x inf would).
-// Two stores (fc_chunk_attention_kv4).  The first segments lie in a store of their own, the workspace that the clean region was
+// Two stores (fc_chunk_attention_kv4, and with ranges of its own for each chunk fc_chunk_attention_kv8).  The first segments lie in a store of their own, the workspace that the clean region was
 // unpacked into; nothing is copied to bring it together with the window.  Three things follow from the fewer rows such calls may
 // have.  The items that do not fill a round of the blocks have their keys cut into parts, and attention_join_kernel joins
 // their results (256 rows of 24 heads over 28256 keys: 468 us in one piece).  Grouped query heads are rows of one tile (64 rows of 16
@@ -90,14 +90,14 @@ struct WsSmem {
   uint32_t tmem_base;
   uint32_t abort;
   int32_t n_act, total_items;
-  int32_t n_whole, n_rest, n_parts;     // kTwoStores: items in one piece, items cut into parts, parts of each
+  int32_t n_whole, n_rest, n_parts;     // two stores: items in one piece, items cut into parts, parts of each
   int32_t act_chunk[FC_MAX_CHUNKS];     // active chunks, longest visible prefix first
   int32_t act_item_end[FC_MAX_CHUNKS];  // running item count over that list (all heads)
 };
 
 struct Item {
   int h, hk, c, row0, n_vis;  // logical keys [k_lo, n_vis)
-  int k_lo, part, slot;       // kTwoStores: the part of the keys, and where its result goes (-1: the item is in one piece)
+  int k_lo, part, slot;       // two stores: the part of the keys, and where its result goes (-1: the item is in one piece)
   bool b_valid;  // tile B has at least one row of the chunk (false for the ragged last item of a chunk)
 };
 
@@ -152,16 +152,29 @@ __device__ __forceinline__ void warp_wait(uint32_t bar, uint32_t parity, volatil
 //   kGatherMap  the per-head token map g.tok_index (tmap_k / tmap_v are then 2-D maps over all rows of all heads, box one
 //               row high)
 //   kTwoStores  the segment table; the first g.n_seg0 segments lie in a store of their own (tmap_k0 / tmap_v0)
-enum Source { kSegments, kGatherMap, kTwoStores };
+//   kSpans      as kTwoStores, but what a chunk sees are up to two ranges of rows of the first store and two ranges of
+//               the segment table (fc::AttnSpans); g.vis counts its keys
+enum Source { kSegments, kGatherMap, kTwoStores, kSpans };
+
+struct NoSpans {};
+template <Source kSource> struct SpansOf { using type = NoSpans; };
+template <> struct SpansOf<kSpans> { using type = fc::AttnSpans; };
+
+// Where a role stands in the runs of an item, the pieces of its keys that lie together in a store: the next one, and (kSpans) the
+// chunk's keys before it.
+struct Runs {
+  int next = 0, keys = 0;
+};
 
 template <int D, Source kSource>
 __global__ void __launch_bounds__(kThreads, 1)
 attention_ws_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant__ CUtensorMap tmap_k,
                     const __grid_constant__ CUtensorMap tmap_v, const __grid_constant__ CUtensorMap tmap_k0,
                     const __grid_constant__ CUtensorMap tmap_v0, const __grid_constant__ fc::AttnGeom g,
-                    const __grid_constant__ fc::AttnSplit split, __nv_bfloat16* __restrict__ O, uint32_t* __restrict__ counter) {
-  constexpr bool kGather = kSource == kGatherMap, kTwo = kSource == kTwoStores;
-  // kTwoStores takes the `pack` query heads of a key head as rows of the same tile (row v of a head group is head v % pack,
+                    const __grid_constant__ fc::AttnSplit split, __nv_bfloat16* __restrict__ O, uint32_t* __restrict__ counter,
+                    const __grid_constant__ typename SpansOf<kSource>::type spans) {
+  constexpr bool kGather = kSource == kGatherMap, kTwo = kSource == kTwoStores || kSource == kSpans;
+  // Two stores: the kernel takes the `pack` query heads of a key head as rows of the same tile (row v of a head group is head v % pack,
   // query row v / pack), so that a key tile is read once for all of them; "head" below is the group then.
   const int pk = kTwo ? split.pack : 1, n_heads = g.H_q / pk;
   constexpr uint32_t kTileBytes = kBM * D * 2;
@@ -202,7 +215,7 @@ attention_ws_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
     tma_prefetch_desc(&tmap_q);
     tma_prefetch_desc(&tmap_k);
     tma_prefetch_desc(&tmap_v);
-    if (kSource == kTwoStores) {
+    if (kTwo) {
       tma_prefetch_desc(&tmap_k0);
       tma_prefetch_desc(&tmap_v0);
     }
@@ -306,22 +319,53 @@ attention_ws_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
     return item;
   };
 
-  // Tokens of segment s that the item sees (behind the `skip` first ones); none, or a negative number, for a segment before
-  // the item's keys (kTwoStores only) or behind them.
-  auto seg_tokens = [&](const Item& it, int s, int& skip) {
-    skip = kTwo ? max(it.k_lo - g.seg_log[s], 0) : 0;
-    return min(g.seg_log[s + 1], it.n_vis) - g.seg_log[s] - skip;
+  // The item's next run: how many tokens it has (0: there is none), its first physical row, and whether it lies in the first of two
+  // stores.  A part of an item's keys (kTwo) may begin and end inside a run.
+  auto next_run = [&](const Item& it, Runs& w, int& prow, bool& first_store) {
+    if constexpr (kSource == kSpans) {
+      const int n = 2 + 2 * g.n_seg;
+      while (w.next < n) {
+        const int r = w.next++;
+        int lo, hi, phys;
+        if (r < 2) {
+          lo = phys = spans.lo[r][it.c];
+          hi = spans.hi[r][it.c];
+        } else {
+          const int i = r < 2 + g.n_seg ? 2 : 3, s = r - 2 - (i - 2) * g.n_seg;
+          lo = max(spans.lo[i][it.c], g.seg_log[s]);
+          hi = min(spans.hi[i][it.c], g.seg_log[s + 1]);
+          phys = g.seg_phys[s] + lo - g.seg_log[s];
+        }
+        if (hi <= lo) continue;
+        const int skip = max(it.k_lo - w.keys, 0), tokens = min(hi - lo, it.n_vis - w.keys) - skip;
+        w.keys += hi - lo;
+        if (tokens <= 0) continue;
+        prow = phys + skip;
+        first_store = r < 2;
+        return tokens;
+      }
+    } else if constexpr (kTwo) {
+      while (w.next < g.n_seg) {
+        const int s = w.next++, skip = max(it.k_lo - g.seg_log[s], 0);
+        const int tokens = min(g.seg_log[s + 1], it.n_vis) - g.seg_log[s] - skip;
+        if (tokens <= 0) continue;  // before the item's keys, or behind them
+        prow = g.seg_phys[s] + skip;
+        first_store = s < g.n_seg0;
+        return tokens;
+      }
+    } else if (w.next < g.n_seg) {
+      const int s = w.next++;
+      prow = g.seg_phys[s];
+      first_store = false;
+      return min(g.seg_log[s + 1], it.n_vis) - g.seg_log[s];
+    }
+    return 0;
   };
   auto count_tiles = [&](const Item& it) {
-    int n = 0, skip;
-    for (int s = 0; s < g.n_seg; ++s) {
-      const int seg_vis = seg_tokens(it, s, skip);
-      if (seg_vis <= 0) {
-        if (kTwo) continue;
-        break;
-      }
-      n += (seg_vis + kBN - 1) / kBN;
-    }
+    Runs w;
+    int n = 0, prow, tokens;
+    bool first_store;
+    while ((tokens = next_run(it, w, prow, first_store)) > 0) n += (tokens + kBN - 1) / kBN;
     return n;
   };
 
@@ -333,7 +377,7 @@ attention_ws_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
     // ------------------------------------------------------------------ scheduler + TMA producer
     uint32_t kv = 0, it_n = 0;
     int next = 0;
-    // kTwoStores: the kernel before writes the first store and clears the counter.  Blocks that start while it still runs
+    // Two stores: the kernel before writes the first one and clears the counter.  Blocks that start while it still runs
     // elsewhere are ahead of the others; so the first item of a block is its own, and only the others come off the counter.
     if constexpr (kTwo) fc::pdl_wait();
     auto take = [&]() { return kTwo ? (int)(gridDim.x + atomicAdd(counter, 1u)) : (int)atomicAdd(counter, 1u); };
@@ -390,17 +434,14 @@ attention_ws_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
           __syncwarp();  // (the V rows of the tile are gathered by warp 11: two warps issue the copies)
         }
       } else {
-      for (int s = 0; s < g.n_seg; ++s) {
-        int skip;
-        const int seg_vis = seg_tokens(it, s, skip);
-        if (seg_vis <= 0) {
-          if (kTwo) continue;
-          break;
-        }
-        const CUtensorMap* map_k = kSource == kTwoStores && s < g.n_seg0 ? &tmap_k0 : &tmap_k;
-        const CUtensorMap* map_v = kSource == kTwoStores && s < g.n_seg0 ? &tmap_v0 : &tmap_v;
-        for (int j0 = 0; j0 < seg_vis; j0 += kBN, ++kv) {
-          const int st = kv % kStages, ph = (kv / kStages) & 1, prow = g.seg_phys[s] + skip + j0;
+      Runs w;
+      int tokens, prow0;
+      bool first_store;
+      while ((tokens = next_run(it, w, prow0, first_store)) > 0) {
+        const CUtensorMap* map_k = kTwo && first_store ? &tmap_k0 : &tmap_k;
+        const CUtensorMap* map_v = kTwo && first_store ? &tmap_v0 : &tmap_v;
+        for (int j0 = 0; j0 < tokens; j0 += kBN, ++kv) {
+          const int st = kv % kStages, ph = (kv / kStages) & 1, prow = prow0 + j0;
           warp_wait(smem_u32(&sh->k_empty[st]), ph ^ 1, abort);
           if (lane == 0) {
             mbar_expect_tx(smem_u32(&sh->k_full[st]), kTileBytes);
@@ -504,20 +545,18 @@ attention_ws_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
         umma_commit(b_sfull + 8);
         umma_commit(b_kempty + 8 * st);
       }
-      // the walk over the segments, to know which tiles are ragged (their V stage is patched before PV)
-      int seg = 0, skip, seg_left = n_tiles > 0 ? seg_tokens(it, 0, skip) : 0;
-      if (kTwo && n_tiles > 0)
-        while (seg_left <= 0) seg_left = seg_tokens(it, ++seg, skip);
+      // the walk over the runs, to know which tiles are ragged (their V stage is patched before PV)
+      Runs w;
+      int prow;
+      bool first_store;
+      int left = next_run(it, w, prow, first_store);
       for (int j = 0; j < n_tiles; ++j, ++kv, ++uses) {
         const uint32_t st = kv & 1, ph = (kv >> 1) & 1;
         const uint32_t st2 = st ^ 1, ph2 = ((kv + 1) >> 1) & 1;  // the next key tile's stage
         const bool more = j + 1 < n_tiles;
-        const bool ragged = seg_left < kBN;
-        seg_left -= kBN;
-        if (seg_left <= 0 && more) {
-          ++seg;
-          seg_left = seg_tokens(it, seg, skip);
-        }
+        const bool ragged = left < kBN;
+        left -= kBN;
+        if (left <= 0 && more) left = next_run(it, w, prow, first_store);
         prep_pv(st, 0);
         if (more) prep_s(st2, 0);
         mbar_wait_bounded(b_vfull + 8 * st, ph, abort);
@@ -562,16 +601,13 @@ attention_ws_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
       const int item = next_item(it_n);
       if (item < 0) break;
       const Item it = decode(item);
-      for (int s = 0; s < g.n_seg; ++s) {
-        int skip;
-        const int seg_vis = seg_tokens(it, s, skip);
-        if (seg_vis <= 0) {
-          if (kTwo) continue;
-          break;
-        }
-        for (int j0 = 0; j0 < seg_vis; j0 += kBN, ++kv) {
+      Runs w;
+      int tokens, prow;
+      bool first_store;
+      while ((tokens = next_run(it, w, prow, first_store)) > 0) {
+        for (int j0 = 0; j0 < tokens; j0 += kBN, ++kv) {
           const int st = kv % kStages, ph = (kv / kStages) & 1;
-          const int cols_valid = min(kBN, seg_vis - j0);
+          const int cols_valid = min(kBN, tokens - j0);
           if constexpr (kGather) {
             // token map: this warp also brings the tile's V rows (lane L rows 4L .. 4L+3, as the copy warp does for K)
             const int32_t* tok = g.tok_index + (int64_t)it.hk * g.tok_hs;
@@ -646,15 +682,12 @@ attention_ws_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
       }
       float m = -INFINITY, l = 0.f;
       int j = 0;
-      for (int s = 0; s < g.n_seg; ++s) {
-        int skip;
-        const int seg_vis = seg_tokens(it, s, skip);
-        if (seg_vis <= 0) {
-          if (kTwo) continue;
-          break;
-        }
-        for (int j0 = 0; j0 < seg_vis; j0 += kBN, ++kv, ++j, ++uses) {
-          const int cols_valid = min(kBN, seg_vis - j0);
+      Runs w;
+      int tokens, prow;
+      bool first_store;
+      while ((tokens = next_run(it, w, prow, first_store)) > 0) {
+        for (int j0 = 0; j0 < tokens; j0 += kBN, ++kv, ++j, ++uses) {
+          const int cols_valid = min(kBN, tokens - j0);
 #pragma unroll
           for (int u = 0; u < 2; ++u, ++sub) {
             const int mine_valid = min(max(cols_valid - u * kHalf, 0), kHalf);
@@ -844,7 +877,7 @@ namespace fc {
 
 int attention_ws_launch(fc_ctx* ctx, cudaStream_t st, const AttnGeom& g, const CUtensorMap& tq,
                         const CUtensorMap& tk, const CUtensorMap& tv, const CUtensorMap* tk0, const CUtensorMap* tv0,
-                        const AttnSplit& split, void* O, uint32_t* counter) {
+                        const AttnSplit& split, const AttnSpans* spans, void* O, uint32_t* counter) {
   const int pk = tk0 ? split.pack : 1;
   int64_t max_items = 0;
   for (int c = 0; c < g.W; ++c) max_items += ((int64_t)(g.q_row_off[c + 1] - g.q_row_off[c]) * pk + 2 * kBM - 1) / (2 * kBM);
@@ -856,19 +889,21 @@ int attention_ws_launch(fc_ctx* ctx, cudaStream_t st, const AttnGeom& g, const C
   // at least half of the shared memory, so that a second CTA (and its 512 columns) never joins the SM
   const size_t need = (2 + 2 * kStages) * (size_t)kBM * g.d * 2 + sizeof(WsSmem) + 1024;
   const size_t smem = std::max<size_t>(need, 120 * 1024);
-  auto launch = [&](auto kernel) -> int {
+  auto launch = [&](auto kernel, auto extra) -> int {
     FC_CUDA_CHECK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
     if (split.follows)  // its setup overlaps the kernel before, which cleared the counter
       FC_CUDA_CHECK(launch_pdl(kernel, dim3(grid), dim3(kThreads), smem, st, tq, tk, tv, tk0 ? *tk0 : tk, tv0 ? *tv0 : tv, g, split,
-                               (__nv_bfloat16*)O, counter));
+                               (__nv_bfloat16*)O, counter, extra));
     else
-      kernel<<<grid, kThreads, smem, st>>>(tq, tk, tv, tk0 ? *tk0 : tk, tv0 ? *tv0 : tv, g, split, (__nv_bfloat16*)O, counter);
+      kernel<<<grid, kThreads, smem, st>>>(tq, tk, tv, tk0 ? *tk0 : tk, tv0 ? *tv0 : tv, g, split, (__nv_bfloat16*)O, counter, extra);
     return FC_OK;
   };
+  const NoSpans none;
   int rc;
-  if (g.tok_index) rc = g.d == 128 ? launch(attention_ws_kernel<128, kGatherMap>) : launch(attention_ws_kernel<64, kGatherMap>);
-  else if (tk0) rc = g.d == 128 ? launch(attention_ws_kernel<128, kTwoStores>) : launch(attention_ws_kernel<64, kTwoStores>);
-  else rc = g.d == 128 ? launch(attention_ws_kernel<128, kSegments>) : launch(attention_ws_kernel<64, kSegments>);
+  if (g.tok_index) rc = g.d == 128 ? launch(attention_ws_kernel<128, kGatherMap>, none) : launch(attention_ws_kernel<64, kGatherMap>, none);
+  else if (spans) rc = g.d == 128 ? launch(attention_ws_kernel<128, kSpans>, *spans) : launch(attention_ws_kernel<64, kSpans>, *spans);
+  else if (tk0) rc = g.d == 128 ? launch(attention_ws_kernel<128, kTwoStores>, none) : launch(attention_ws_kernel<64, kTwoStores>, none);
+  else rc = g.d == 128 ? launch(attention_ws_kernel<128, kSegments>, none) : launch(attention_ws_kernel<64, kSegments>, none);
   if (rc != FC_OK) return rc;
   FC_LAUNCH_CHECK("attention_ws_kernel");
   if (split.slots > 0) {
