@@ -27,6 +27,7 @@ struct SpanGeom {
   // Kernel for few rows: the keys of chunk c are cut into parts[c] parts of part_units[c] units of cost; blocks are numbered
   // chunk by chunk, tile by tile, part by part.
   int32_t row_tiles;                 // rows of a tile / 8
+  int32_t cluster;                   // the parts of a tile are as many, one thread block cluster, and join themselves; 0: a second kernel joins
   int32_t parts[FC_MAX_CHUNKS], part_units[FC_MAX_CHUNKS], block_end[FC_MAX_CHUNKS];
   float* part_o;                     // [H_kv, blocks, rows of a tile, d] sums not divided by their weights
   float2* part_ml;                   // [H_kv, blocks, rows of a tile]: reference (log2 units) and sum of the weights

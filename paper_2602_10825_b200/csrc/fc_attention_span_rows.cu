@@ -34,10 +34,11 @@ using namespace fc::sm100;
 constexpr int kWarps = 4, kThreads = 32 * kWarps;
 constexpr int kStep = 16;            // keys per warp and step
 constexpr int kRing = 16 * 1024;     // bytes of a warp's two rings
+constexpr int kMaxCluster = 16;      // blocks of a cluster
 constexpr float kSlack = 8.f;        // log2 units by which a logit may pass the maximum before that moves
 constexpr float kLift = 7.f;         // weights are 2^kLift at the maximum
 constexpr int blocks_per_sm(int nt) { return nt == 1 ? 3 : 2; }
-template <typename T> constexpr int kPlainCost = (int)sizeof(T);  // cost of a step over plain rows, in steps over pages: its bytes
+template <typename T> constexpr int kPlainCost = sizeof(T) == 4 ? 3 : 2;  // cost of a step over plain rows, in steps over pages
 
 template <typename T> constexpr int kParts = sizeof(T) == 4 ? 3 : 1;       // bf16 parts of Q, K and V over plain rows
 template <typename T> constexpr int kHalves = sizeof(T) == 4 ? 2 : 1;      // fp16 parts of Q and of the weights over pages
@@ -115,9 +116,40 @@ __device__ __forceinline__ void weigh_logits(State<D, NT>& st, float (&s)[NT][4]
   }
 }
 
-// The page, and the scales of K and V, of 32 steps of a warp, one a lane.
-struct Steps {
-  int page;
+__device__ __forceinline__ void cluster_barrier() {
+  asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+// Shared memory of block `rank` of the cluster, at this block's address `at`.
+__device__ __forceinline__ uint32_t at_rank(uint32_t at, int rank) {
+  uint32_t a;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(at), "r"(rank));
+  return a;
+}
+__device__ __forceinline__ float2 cluster_load2(uint32_t at, int rank) {
+  float2 x;
+  asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(x.x), "=f"(x.y) : "r"(at_rank(at, rank)) : "memory");
+  return x;
+}
+__device__ __forceinline__ float4 cluster_load4(uint32_t at, int rank) {
+  float4 x;
+  asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(x.x), "=f"(x.y), "=f"(x.z), "=f"(x.w) : "r"(at_rank(at, rank)) : "memory");
+  return x;
+}
+
+// Four elements of virtual row v of chunk c: a sum of weights times values, its reference and the sum of the weights.
+template <typename T>
+__device__ __forceinline__ void write_row(T* O, const fc::SpanGeom& g, int c, int hk, int v, int d4, float4 o, float ref, float l) {
+  const float inv = l > 0.f ? 1.f / l : (l == l ? 0.f : l);
+  const int h = hk * g.group + v % g.group;
+  const int64_t row = g.q_row_off[c] + v / g.group;
+  store4(O + h * g.o_hs + row * g.o_rs + d4, make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv));
+  if (g.lse && d4 == 0) g.lse[h * g.lse_hs + row] = l > 0.f ? (ref + log2f(l)) * 0.6931471805599453f : (l == l ? -INFINITY : l);
+}
+
+// What a lane knows of one of the next 32 steps of its warp over pages: the page (-1: none), the first of its rows, which of the sixteen are
+// seen, and the scales of K and V.
+struct PagedStep {
+  int page, row, lo, hi;
   float ks, vs;
 };
 
@@ -151,7 +183,7 @@ attention_span_rows_kernel(const __grid_constant__ CUtensorMap map_k8, const __g
   constexpr int kRows = 8 * NT;
   using R = Ring<T, D>;
   extern __shared__ uint8_t smem_raw[];
-  __shared__ uint64_t bars[kWarps][2][2][kBars];  // warp; pages or plain rows; K or V; stage
+  __shared__ uint64_t bars[kWarps][2][2][kBars];  // warp; pages (K and V) or plain rows; K or V; stage
   __shared__ float2 ml_s[kWarps][kRows];
   __shared__ uint32_t abort_s;
   fc::pdl_launch_dependents();  // the joining kernel may take its place; it waits for this grid to end
@@ -164,12 +196,17 @@ attention_span_rows_kernel(const __grid_constant__ CUtensorMap map_k8, const __g
   const int rows_here = min(kRows, (g.q_row_off[c + 1] - g.q_row_off[c]) * g.group - v0);
 
   uint8_t* smem = (uint8_t*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
-  const uint8_t* ring_k = smem + warp * kRing;
-  const uint8_t* ring_v = ring_k + kRing / 2;
+  const uint32_t ring_s = smem_u32(smem) + warp * kRing;
   volatile uint32_t* abort = &abort_s;
   auto bar = [&](int plain, int v, int stage) { return smem_u32(&bars[warp][plain][v][stage]); };
   if (lane < 4 * kBars) mbar_init(smem_u32(&bars[warp][0][0][0] + lane), 1);
-  if (tid == 0) abort_s = 0;
+  if (tid == 0) {
+    abort_s = 0;
+    tma_prefetch_desc(&map_k8);
+    tma_prefetch_desc(&map_v8);
+    tma_prefetch_desc(&map_k);
+    tma_prefetch_desc(&map_v);
+  }
   mbar_fence_init();
   __syncthreads();
 
@@ -200,59 +237,56 @@ attention_span_rows_kernel(const __grid_constant__ CUtensorMap map_k8, const __g
     return Q + (int64_t)(hk * g.group + v % g.group) * g.q_hs + (int64_t)(g.q_row_off[c] + v / g.group) * g.q_rs;
   };
 
-  const bool active = fc::span_chunk_active(g, c);  // nothing is on its way yet
   if (hk == 0 && blockIdx.x == 0 && warp == 0) {
     const int n_ids = min(max(*g.n_active, 0), g.W);
     for (int i = lane; i < n_ids; i += 32)
       if ((g.active_ids[i] < 0 || g.active_ids[i] >= g.W) && g.status) atomicOr(g.status, (uint32_t)FC_DEV_BAD_INDEX);
   }
-  if (!active) return;
 
   // ------------------------------------------------------------------ pages
   const int m = max(0, (p1 - p0 - warp + kWarps - 1) / kWarps);  // this warp's steps: p0 + warp, + kWarps, ...
-  if (m > 0) {
-    constexpr int kStages = R::kPagedStages;
-    const int32_t* table = g.table + c * g.table_cs;
-    auto token_of = [&](int i, int& lo, int& hi) {  // first token of the warp's step i; tokens lo .. hi - 1 of the sixteen are seen
+  constexpr int kPagedStages = R::kPagedStages;
+  bool bad = false;  // an entry that names no page
+  auto look_up = [&](int i) {
+    PagedStep x = {-1, 0, 0, kStep, 0.f, 0.f};
+    if (i < m) {
       const int s = p0 + warp + i * kWarps, k = s < n_first ? 0 : 1;
       const int tok = (g.lo[k][c] / kStep + (k ? s - n_first : s)) * kStep;
-      lo = max(g.lo[k][c] - tok, 0);
-      hi = min(g.hi[k][c] - tok, kStep);
-      return tok;
-    };
-    auto load_steps = [&](int i0) {
-      Steps x = {-1, 0.f, 0.f};
-      if (i0 + lane < m) {
-        int lo, hi;
-        x.page = __ldg(table + (token_of(i0 + lane, lo, hi) >> log2));
-        if (x.page >= 0 && x.page < g.pool.n_pages) {
-          x.ks = __ldg(g.pool.k_scales + x.page * g.pool.scale_ps + hk * g.pool.scale_hs);
-          x.vs = __ldg(g.pool.v_scales + x.page * g.pool.scale_ps + hk * g.pool.scale_hs);
-        } else {
-          x.page = -1;
-          if (g.status) atomicOr(g.status, (uint32_t)FC_DEV_BAD_INDEX);
-        }
+      x.row = tok & ((1 << log2) - 1);
+      x.lo = max(g.lo[k][c] - tok, 0);
+      x.hi = min(g.hi[k][c] - tok, kStep);
+      x.page = __ldg(g.table + c * g.table_cs + (tok >> log2));
+      if (x.page >= 0 && x.page < g.pool.n_pages) {
+        x.ks = __ldg(g.pool.k_scales + x.page * g.pool.scale_ps + hk * g.pool.scale_hs);
+        x.vs = __ldg(g.pool.v_scales + x.page * g.pool.scale_ps + hk * g.pool.scale_hs);
+      } else {
+        x.page = -1;
+        bad = true;
       }
-      return x;
-    };
-    Steps cur = load_steps(0), next = load_steps(32);
-    auto send = [&](int i, int i_now, int v) {  // K or V of the warp's step i, while it works on step i_now
-      const int page = __shfl_sync(0xffffffffu, i / 32 == i_now / 32 ? cur.page : next.page, i & 31);
-      if (i >= m || lane != 0) return;
-      const int stage = i % kStages;
-      if (page < 0) {  // nothing to bring: its keys are zeros
-        mbar_arrive(bar(0, v, stage));
-        return;
-      }
-      int lo, hi;
-      const int tok = token_of(i, lo, hi);
-      mbar_expect_tx(bar(0, v, stage), R::kPaged);
-      tma_load_4d(smem_u32(v ? ring_v : ring_k) + stage * R::kPaged, v ? &map_v8 : &map_k8, bar(0, v, stage), 0, tok & ((1 << log2) - 1), hk, page);
-    };
-    for (int i = 0; i < kStages; ++i) {
-      send(i, 0, 0);
-      send(i, 0, 1);
     }
+    return x;
+  };
+  // Lane L looks up steps L, 32 + L, ..., and sends for them when their turn comes.
+  PagedStep cur = look_up(lane), next = look_up(32 + lane);
+  const uint32_t bar_s = bar(0, 0, 0);
+  auto send_paged = [&](const PagedStep& x, int stage) {
+    const uint32_t b = bar_s + 8 * stage, dst = ring_s + stage * (2 * R::kPaged);
+    if (x.page < 0) {  // nothing to bring: its keys are zeros
+      mbar_arrive(b);
+    } else {
+      mbar_expect_tx(b, 2 * R::kPaged);
+      tma_load_4d(dst, &map_k8, b, 0, x.row, hk, x.page);
+      tma_load_4d(dst + R::kPaged, &map_v8, b, 0, x.row, hk, x.page);
+    }
+  };
+  if (lane < min(m, kPagedStages)) send_paged(cur, lane);
+  // everything up to here asks only what the host knows; the list is on the device
+  if (!fc::span_chunk_active(g, c)) {
+    for (int i = 0; i < min(m, kPagedStages); ++i) mbar_wait_bounded(bar_s + 8 * i, 0, abort);  // what was sent for lands before its memory is given back
+    return;
+  }
+  if (m > 0) {
+    constexpr int kStages = kPagedStages;
     // Q as fp16 parts of rows brought to 2^14, and what undoes that
     uint32_t qb[kHalves<T>][NT][D / 8];
     float qs[NT][2];
@@ -298,44 +332,34 @@ attention_span_rows_kernel(const __grid_constant__ CUtensorMap map_k8, const __g
     // where this lane reads: 32 (D = 128) or 16 bytes of keys n and n + 8; eight bytes of keys 2q, 2q+1, 2q+8, 2q+9.  A row is
     // 128 or 64 bytes, its 16-byte pieces exchanged by bits 7.. of the address.
     const int ka = D == 128 ? n * 128 + (((2 * q) ^ (n & 7)) << 4) : n * 64 + ((q ^ ((n >> 1) & 3)) << 4);
-    auto v_at = [&](int r, int j) {  // dims 64 j + 8 n of row r
-      return D == 128 ? r * 128 + (((4 * j + (n >> 1)) ^ (r & 7)) << 4) + 8 * (n & 1) : r * 64 + (((n >> 1) ^ ((r >> 1) & 3)) << 4) + 8 * (n & 1);
+    // (rows r and r + 8 are 8 D bytes apart)
+    auto v_at = [&](int r) {  // dims 8 n of row r; 64 + 8 n is 64 bytes from there, by exchange
+      return D == 128 ? r * 128 + (((n >> 1) ^ (r & 7)) << 4) + 8 * (n & 1) : r * 64 + (((n >> 1) ^ ((r >> 1) & 3)) << 4) + 8 * (n & 1);
     };
-    int va[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) va[i] = v_at(2 * q + (i & 1) + 8 * (i >> 1), 0);
+    const uint32_t k_at = ring_s + ka, va[2] = {ring_s + R::kPaged + v_at(2 * q), ring_s + R::kPaged + v_at(2 * q + 1)};
 
-    auto step = [&](int i, auto masked) {
+    auto step = [&](uint32_t off, float ks, float vs, int lo, int hi, bool no_page, auto masked) {
       constexpr bool kMask = decltype(masked)::value;
-      const int stage = i % kStages, parity = (i / kStages) & 1;
-      const float ks = __shfl_sync(0xffffffffu, cur.ks, i & 31), vs = __shfl_sync(0xffffffffu, cur.vs, i & 31);
-      int lo = 0, hi = kStep;
-      bool no_page = false;
-      if (kMask) {
-        token_of(i, lo, hi);
-        no_page = __shfl_sync(0xffffffffu, cur.page, i & 31) < 0;
-      }
-      mbar_wait_bounded(bar(0, 0, stage), parity, abort);
-      __syncwarp();
-      const uint8_t* kp = ring_k + stage * R::kPaged;
       uint32_t k0[D / 16], k1[D / 16];
 #pragma unroll
       for (int h = 0; h < D / 64; ++h) {
-        const uint4 a = *reinterpret_cast<const uint4*>(kp + (ka ^ (h << 4)));
-        const uint4 b = *reinterpret_cast<const uint4*>(kp + 8 * D + (ka ^ (h << 4)));
+        const uint32_t at = (k_at ^ (h << 4)) + off;
+        const uint4 a = lds16(at), b = lds16(at + 8 * D);
         k0[4 * h] = a.x; k0[4 * h + 1] = a.y; k0[4 * h + 2] = a.z; k0[4 * h + 3] = a.w;
         k1[4 * h] = b.x; k1[4 * h + 1] = b.y; k1[4 * h + 2] = b.z; k1[4 * h + 3] = b.w;
       }
-      __syncwarp();
-      send(i + kStages, i, 0);
-      float s[NT][4] = {}, rest[NT][4] = {};
+      float s[NT][4], rest[NT][4];
 #pragma unroll
       for (int w = 0; w < D / 16; ++w) {
         const uint32_t a0 = fc::e4m3_lo2(k0[w]), a1 = fc::e4m3_lo2(k1[w]), a2 = fc::e4m3_hi2(k0[w]), a3 = fc::e4m3_hi2(k1[w]);
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
-          mma_f16(s[t], a0, a1, a2, a3, qb[0][t][2 * w], qb[0][t][2 * w + 1]);
-          if constexpr (kHalves<T> == 2) mma_f16(rest[t], a0, a1, a2, a3, qb[1][t][2 * w], qb[1][t][2 * w + 1]);
+          auto add = [&](float (&d)[4], const uint32_t (&b)[D / 8]) {
+            if (w == 0) mma_f16_first(d, a0, a1, a2, a3, b[0], b[1]);
+            else mma_f16(d, a0, a1, a2, a3, b[2 * w], b[2 * w + 1]);
+          };
+          add(s[t], qb[0][t]);
+          if constexpr (kHalves<T> == 2) add(rest[t], qb[1][t]);
         }
       }
 #pragma unroll
@@ -357,22 +381,17 @@ attention_span_rows_kernel(const __grid_constant__ CUtensorMap map_k8, const __g
           pa[1][t][1] = transpose8x8(cvt_f16x2(s[t][2] - fc::half_lo(b), s[t][3] - fc::half_hi(b)));
         }
       }
-      mbar_wait_bounded(bar(0, 1, stage), parity, abort);
-      __syncwarp();
-      const uint8_t* vp = ring_v + stage * R::kPaged;
       uint2 v[D / 64][4];
 #pragma unroll
       for (int j = 0; j < D / 64; ++j)
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-          v[j][k] = *reinterpret_cast<const uint2*>(vp + (va[k] ^ (j << 6)));
+          v[j][k] = lds8((va[k & 1] ^ (j << 6)) + off + (k >> 1) * (8 * D));
           if (kMask) {
             const int key = 2 * q + (k & 1) + 8 * (k >> 1);
             if (no_page || key < lo || key >= hi) v[j][k] = make_uint2(0u, 0u);  // whatever it is: 0 x NaN is NaN
           }
         }
-      __syncwarp();
-      send(i + kStages, i, 1);
 #pragma unroll
       for (int j = 0; j < D / 64; ++j)
 #pragma unroll
@@ -384,25 +403,38 @@ attention_span_rows_kernel(const __grid_constant__ CUtensorMap map_k8, const __g
             const uint32_t a0 = fc::e4m3_lo2(ab), a1 = fc::e4m3_hi2(ab), a2 = fc::e4m3_lo2(cd), a3 = fc::e4m3_hi2(cd);
 #pragma unroll
             for (int t = 0; t < NT; ++t) {
-              float x[4] = {};
-#pragma unroll
-              for (int w = kHalves<T> - 1; w >= 0; --w) mma_f16(x, a0, a1, a2, a3, pa[w][t][0], pa[w][t][1]);
+              float x[4];
+              mma_f16_first(x, a0, a1, a2, a3, pa[kHalves<T> - 1][t][0], pa[kHalves<T> - 1][t][1]);
+              if constexpr (kHalves<T> == 2) mma_f16(x, a0, a1, a2, a3, pa[0][t][0], pa[0][t][1]);
 #pragma unroll
               for (int e = 0; e < 4; ++e) st.o[t][4 * j + 2 * h + k][e] = fmaf(vs, x[e], st.o[t][4 * j + 2 * h + k][e]);
             }
           }
         }
     };
+    int stage = 0;
+    uint32_t parity = 0;
     for (int i = 0; i < m; ++i) {
-      if (i > 0 && i % 32 == 0) {
+      const int at = i & 31;
+      if (at == 0 && i > 0) {
         cur = next;
-        next = load_steps(i + 32);
+        next = look_up(i + 32 + lane);
       }
-      int lo, hi;
-      token_of(i, lo, hi);
-      const bool whole = lo == 0 && hi == kStep && __shfl_sync(0xffffffffu, cur.page, i & 31) >= 0;
-      if (whole) step(i, std::false_type());
-      else step(i, std::true_type());
+      const float ks = __shfl_sync(0xffffffffu, cur.ks, at), vs = __shfl_sync(0xffffffffu, cur.vs, at);
+      const bool part = __shfl_sync(0xffffffffu, cur.page < 0 || cur.hi - cur.lo < kStep, at);
+      mbar_wait_bounded(bar_s + 8 * stage, parity, abort);
+      __syncwarp();
+      const uint32_t off = stage * (2 * R::kPaged);
+      if (!part) {
+        step(off, ks, vs, 0, kStep, false, std::false_type());
+      } else {
+        const int lo = __shfl_sync(0xffffffffu, cur.lo, at), hi = __shfl_sync(0xffffffffu, cur.hi, at), page = __shfl_sync(0xffffffffu, cur.page, at);
+        step(off, ks, vs, lo, hi, page < 0, std::true_type());
+      }
+      __syncwarp();  // the step's place has been read by every lane: another step is sent for
+      const int ahead = (at + kStages) & 31;
+      if (lane == ahead && i + kStages < m) send_paged(at + kStages < 32 ? cur : next, stage);
+      if (++stage == kStages) stage = 0, parity ^= 1;
     }
   }
 
@@ -422,7 +454,7 @@ attention_span_rows_kernel(const __grid_constant__ CUtensorMap map_k8, const __g
       mbar_expect_tx(bar(1, v, stage), R::kPlain);
 #pragma unroll
       for (int a = 0; a < R::kAtoms; ++a)
-        tma_load_3d(smem_u32(v ? ring_v : ring_k) + stage * R::kPlain + a * (kStep * 128), v ? &map_v : &map_k, bar(1, v, stage), a * (128 / (int)sizeof(T)), row, hk);
+        tma_load_3d(ring_s + (v ? kRing / 2 : 0) + stage * R::kPlain + a * (kStep * 128), v ? &map_v : &map_k, bar(1, v, stage), a * (128 / (int)sizeof(T)), row, hk);
     };
     for (int i = 0; i < kStages; ++i) {
       send(i, ahead_k, 0);
@@ -457,7 +489,7 @@ attention_span_rows_kernel(const __grid_constant__ CUtensorMap map_k8, const __g
       const int hi = min(kStep, now.len - (sidx - now.first) * kStep), stage = i % kStages, parity = (i / kStages) & 1;
       mbar_wait_bounded(bar(1, 0, stage), parity, abort);
       __syncwarp();
-      const uint8_t* kp = ring_k + stage * R::kPlain;
+      const uint32_t kp = ring_s + stage * R::kPlain;
       float s[NT][4] = {}, rest[NT][4] = {};
       auto products = [&](const auto& k, int at) {  // K as NK parts of operand registers; `at`: first register of Q
         constexpr int NK = kParts<T>;
@@ -474,7 +506,7 @@ attention_span_rows_kernel(const __grid_constant__ CUtensorMap map_k8, const __g
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
           const int at = a * (kStep * 128) + n * 128 + (((2 * q + h) ^ (n & 7)) << 4);
-          const uint4 x = *reinterpret_cast<const uint4*>(kp + at), y = *reinterpret_cast<const uint4*>(kp + at + 8 * 128);
+          const uint4 x = lds16(kp + at), y = lds16(kp + at + 8 * 128);
           if constexpr (kParts<T> == 1) {
             const uint32_t lo[1][4] = {{x.x, y.x, x.y, y.y}}, hi4[1][4] = {{x.z, y.z, x.w, y.w}};
             products(lo, 8 * a + 4 * h);
@@ -518,10 +550,10 @@ attention_span_rows_kernel(const __grid_constant__ CUtensorMap map_k8, const __g
       }
       mbar_wait_bounded(bar(1, 1, stage), parity, abort);
       __syncwarp();
-      const uint8_t* vp = ring_v + stage * R::kPlain;
+      const uint32_t vp = ring_s + kRing / 2 + stage * R::kPlain;
       auto piece = [&](int k, int a, int p) {  // 16-byte piece p of atom a of the lane's k-th key; zeros behind the run's end
         const int r = 2 * q + (k & 1) + 8 * (k >> 1);
-        uint4 x = *reinterpret_cast<const uint4*>(vp + a * (kStep * 128) + r * 128 + ((p ^ (r & 7)) << 4));
+        uint4 x = lds16(vp + a * (kStep * 128) + r * 128 + ((p ^ (r & 7)) << 4));
         if (r >= hi) x = make_uint4(0u, 0u, 0u, 0u);
         return x;
       };
@@ -574,6 +606,8 @@ attention_span_rows_kernel(const __grid_constant__ CUtensorMap map_k8, const __g
     }
   }
 
+  if (bad && g.status) atomicOr(g.status, (uint32_t)FC_DEV_BAD_INDEX);
+
   // ------------------------------------------------------------------ join the four warps
   if (*abort) {  // something never arrived: copies still in flight get time to land before their memory is used again
     for (int i = 0; i < 2000; ++i) __nanosleep(1000);
@@ -600,6 +634,8 @@ attention_span_rows_kernel(const __grid_constant__ CUtensorMap map_k8, const __g
         }
     }
   __syncthreads();
+  auto block_o = reinterpret_cast<float(*)[D + 4]>(smem + sizeof(float) * kWarps * kRows * (D + 4));
+  auto block_ml = reinterpret_cast<float2*>(block_o + kRows);
   for (int x = tid; x < rows_here * (D / 4); x += kThreads) {
     const int row = x / (D / 4), d4 = x % (D / 4) * 4;
     float mx = -INFINITY, l = 0.f;
@@ -615,19 +651,46 @@ attention_span_rows_kernel(const __grid_constant__ CUtensorMap map_k8, const __g
       l = fmaf(f, ml.y, l);
       o.x = fmaf(f, y.x, o.x); o.y = fmaf(f, y.y, o.y); o.z = fmaf(f, y.z, o.z); o.w = fmaf(f, y.w, o.w);
     }
-    const int v = v0 + row;
-    if (n_parts > 1) {
+    if (n_parts == 1) {
+      write_row<T>(O, g, c, hk, v0 + row, d4, o, mx, l);
+    } else if (g.cluster) {
+      *reinterpret_cast<float4*>(&block_o[row][d4]) = o;
+      if (d4 == 0) block_ml[row] = make_float2(mx, l);
+    } else {
       const int64_t at = ((int64_t)hk * gridDim.x + blockIdx.x) * kRows + row;
       *reinterpret_cast<float4*>(g.part_o + at * D + d4) = o;
       if (d4 == 0) g.part_ml[at] = make_float2(mx, l);
-    } else {
-      const float inv = l > 0.f ? 1.f / l : (l == l ? 0.f : l);
-      const int h = hk * g.group + v % g.group;
-      const int64_t row_g = g.q_row_off[c] + v / g.group;
-      store4(O + h * g.o_hs + row_g * g.o_rs + d4, make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv));
-      if (g.lse && d4 == 0) g.lse[h * g.lse_hs + row_g] = l > 0.f ? (mx + log2f(l)) * 0.6931471805599453f : (l == l ? -INFINITY : l);
     }
   }
+  if (n_parts == 1 || !g.cluster) return;
+  // the parts of the tile are the blocks of this cluster: each joins a share of the rows' pieces
+  cluster_barrier();
+  for (int x = part * kThreads + tid; x < rows_here * (D / 4); x += n_parts * kThreads) {
+    const int row = x / (D / 4), d4 = x % (D / 4) * 4;
+    const uint32_t at_o = smem_u32(&block_o[row][d4]), at_ml = smem_u32(&block_ml[row]);
+    float2 ml[kMaxCluster];
+    float4 y[kMaxCluster];
+    float mx = -INFINITY, l = 0.f;
+#pragma unroll
+    for (int p = 0; p < kMaxCluster; ++p)
+      if (p < n_parts) {
+        ml[p] = cluster_load2(at_ml, p);
+        y[p] = cluster_load4(at_o, p);
+      }
+#pragma unroll
+    for (int p = 0; p < kMaxCluster; ++p)
+      if (p < n_parts) mx = fmaxf(mx, ml[p].x);
+    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+    for (int p = 0; p < kMaxCluster; ++p) {
+      if (p >= n_parts || !(ml[p].y != 0.f)) continue;
+      const float f = ex2(ml[p].x - mx);
+      l = fmaf(f, ml[p].y, l);
+      o.x = fmaf(f, y[p].x, o.x); o.y = fmaf(f, y[p].y, o.y); o.z = fmaf(f, y[p].z, o.z); o.w = fmaf(f, y[p].w, o.w);
+    }
+    write_row<T>(O, g, c, hk, v0 + row, d4, o, mx, l);
+  }
+  cluster_barrier();  // the others have read this block's memory
 }
 
 // Joins the parts of a tile's rows, a block a row; its four warps take the parts in turn.
@@ -689,11 +752,7 @@ attention_span_join_kernel(T* __restrict__ O, const __grid_constant__ fc::SpanGe
     o.x += y.x; o.y += y.y; o.z += y.z; o.w += y.w;
     l += l_s[i];
   }
-  const float inv = l > 0.f ? 1.f / l : (l == l ? 0.f : l);
-  const int h = hk * g.group + v % g.group;
-  const int64_t row_g = g.q_row_off[c] + v / g.group;
-  store4(O + h * g.o_hs + row_g * g.o_rs + 4 * d4, make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv));
-  if (g.lse && d4 == 0) g.lse[h * g.lse_hs + row_g] = l > 0.f ? (m + log2f(l)) * 0.6931471805599453f : (l == l ? -INFINITY : l);
+  write_row<T>(O, g, c, hk, v, 4 * d4, o, m, l);
 }
 
 constexpr int kMaxParts = 256;
@@ -710,44 +769,90 @@ int64_t units_of(const fc::SpanGeom& g, int c) {
   return steps(0) + steps(1) + plain * (g.f32 ? kPlainCost<float> : kPlainCost<__nv_bfloat16>);
 }
 
-// Parts for tiles of 8 nt rows: as many as should be fastest.
-double split(const fc_ctx* ctx, fc::SpanGeom& g, int nt) {
-  int64_t units[FC_MAX_CHUNKS], most = 1;
+// Measured on B200, in microseconds a unit of cost (a step over pages of a block's four warps, divided by four): of a block alone on its SM,
+// of one of two, and of an SM whose blocks keep it busy (D = 128: the bandwidth).  Steps over plain rows come to 0.7 to 1.3 of this a unit.
+struct UnitUs {
+  double alone, two, full;
+};
+UnitUs unit_us(const fc::SpanGeom& g, int nt) {
+  static const UnitUs t[2][2][2] = {{{{0.115, 0.149, 0.057}, {0.122, 0.163, 0.081}}, {{0.156, 0.184, 0.099}, {0.177, 0.230, 0.115}}},
+                                    {{{0.122, 0.160, 0.063}, {0.152, 0.207, 0.104}}, {{0.186, 0.224, 0.098}, {0.228, 0.300, 0.150}}}};
+  return t[g.f32][g.d == 128][nt - 1];
+}
+
+// How a call's keys are cut for tiles of 8 nt rows.
+//   in clusters   every tile's keys into the same number of parts, at most 16, whose blocks are a cluster and join themselves
+//   by size       every chunk's into parts of at most `size` units, which a second kernel joins (3.5 us and its bytes): where a few tiles see many keys,
+//                 or some chunks far more than others
+// of which the fastest is taken, by the times above; a call takes 4.4 us besides.  Clusters cannot fill a group of SMs to its last place, which
+// leaves about a tenth (more than eight blocks: a fifth) of the device's places free.  Of 60 calls at random, of 5 to 60 us, the choice was 3 %
+// above the best of sixteen cuts in the median and within 20 % for nine in ten; 68 % in one, of six chunks of which the device left five out.
+struct Cut {
+  double us;
+  int32_t cluster;
+  int64_t size;
+};
+Cut cut_of(const fc_ctx* ctx, const fc::SpanGeom& g, int nt, const int64_t* units) {
+  const UnitUs u = unit_us(g, nt);
+  const double sm = ctx->sm_count, places = sm * blocks_per_sm(nt);
+  int64_t tiles[FC_MAX_CHUNKS], all = 0, most = 1;
+  double work = 0;
   for (int c = 0; c < g.W; ++c) {
-    units[c] = fc::span_rows(g, c) > 0 ? std::max<int64_t>(1, units_of(g, c)) : 0;
-    most = std::max(most, units[c]);
+    tiles[c] = (fc::span_rows(g, c) + 8 * nt - 1) / (8 * nt) * g.H_kv;
+    all += tiles[c];
+    work += (double)tiles[c] * units[c];
+    if (tiles[c]) most = std::max(most, units[c]);
   }
-  const double unit_us = (g.d == 128 ? 0.095 : 0.06) * (g.f32 ? 1.6 : 1.0) * (nt == 2 ? 1.3 : 1.0);  // of a full SM
-  const int64_t slots = (int64_t)ctx->sm_count * blocks_per_sm(nt);
-  double best = 0;
-  int64_t best_size = 0, last = 0;
-  for (int64_t k = 1; k <= std::min<int64_t>(kMaxParts, std::max<int64_t>(1, most / 8)); ++k) {
-    const int64_t size = ((most + k - 1) / k + kWarps - 1) / kWarps * kWarps;
-    if (size == last) continue;
-    last = size;
-    int64_t blocks = 0, work = 0, parts_rows = 0;
+  auto time_of = [&](double blocks, double size, double room) {
+    size = std::ceil(size / kWarps) * kWarps;
+    if (blocks <= room) return size * std::max(blocks <= sm ? u.alone : blocks <= 1.75 * sm ? u.two : 1.25 * u.two, u.full * blocks / sm);
+    return u.full * work / sm + 0.7 * size * u.alone + 3.5 * blocks / room;  // a set of blocks takes 3.5 us to start and end
+  };
+  Cut best = {0, 1, 0};
+  for (int n = 1; n <= kMaxCluster && (n == 1 || most >= kWarps * n); ++n) {
+    const double room = n == 1 ? places : (n <= 8 ? 0.9 : nt == 1 ? 0.82 : 0.78) * places;
+    const double us = 4.4 + (n > 1 ? 0.5 + 0.1 * n : 0) + time_of((double)all * n, (double)((most + n - 1) / n), room);
+    if (n == 1 || us < best.us) best = {us, n, 0};
+  }
+  for (int64_t n = 2; n <= kMaxParts && most >= 2 * kWarps * n; n += (n + 7) / 8) {
+    const int64_t size = (most + n - 1) / n;
+    double blocks = 0, rows = 0;
     for (int c = 0; c < g.W; ++c) {
-      const int64_t tiles = (fc::span_rows(g, c) + 8 * nt - 1) / (8 * nt) * g.H_kv, parts = units[c] ? (units[c] + size - 1) / size : 0;
-      blocks += tiles * parts;
-      work += tiles * units[c];
-      if (parts > 1) parts_rows += tiles * parts * 8 * nt;
+      const double parts = (double)((units[c] + size - 1) / size);
+      blocks += tiles[c] * parts;
+      if (parts > 1) rows += tiles[c] * parts * 8 * nt;
     }
-    if (k > 1 && blocks > 6 * slots) break;
-    const int64_t on_sm = std::min<int64_t>((blocks + ctx->sm_count - 1) / ctx->sm_count, blocks_per_sm(nt));
-    const double alone = unit_us * size * std::max(1.4, (double)on_sm);  // a block alone on an SM is bound by its chains of instructions
-    const double all = unit_us * (double)work / ctx->sm_count + (blocks > slots ? 0.5 * unit_us * std::min<int64_t>(size, most) : 0);
-    const double us = std::max(alone, all) + 3 + 1.5 * ((blocks + slots - 1) / slots - 1) + (parts_rows ? 3.5 + 2.0 * 4 * g.d * parts_rows / 4e6 : 0);
-    if (k == 1 || us < best) best = us, best_size = size;
-  }
-  int64_t blocks = 0;
-  for (int c = 0; c < g.W; ++c) {
-    g.parts[c] = units[c] ? (int32_t)((units[c] + best_size - 1) / best_size) : 1;
-    // an even cut, in whole rounds of the warps
-    g.part_units[c] = units[c] ? (int32_t)(((units[c] + g.parts[c] - 1) / g.parts[c] + kWarps - 1) / kWarps * kWarps) : 1;
-    blocks += (fc::span_rows(g, c) + 8 * nt - 1) / (8 * nt) * g.parts[c];
-    g.block_end[c] = (int32_t)std::min<int64_t>(blocks, INT32_MAX);
+    const double us = 4.4 + 3.5 + 2.0 * 4 * g.d * rows / 4e6 + time_of(blocks, (double)size, places);
+    if (us < best.us) best = {us, 0, size};
   }
   return best;
+}
+
+double split(const fc_ctx* ctx, fc::SpanGeom& g) {
+  int64_t units[FC_MAX_CHUNKS];
+  bool many = false;
+  for (int c = 0; c < g.W; ++c) {
+    units[c] = std::max<int64_t>(1, units_of(g, c));
+    many |= fc::span_rows(g, c) > 8;
+  }
+  // sixteen rows to a tile where some chunk has more than eight, unless twice the tiles are faster
+  int nt = 1;
+  Cut cut = cut_of(ctx, g, 1, units);
+  if (many) {
+    const Cut two = cut_of(ctx, g, 2, units);
+    if (two.us + 0.7 < cut.us) cut = two, nt = 2;
+  }
+  g.row_tiles = nt;
+  g.cluster = cut.cluster;
+  int64_t blocks = 0;
+  for (int c = 0; c < g.W; ++c) {
+    const int64_t parts = cut.cluster ? cut.cluster : (units[c] + cut.size - 1) / cut.size;
+    g.parts[c] = (int32_t)parts;
+    g.part_units[c] = (int32_t)(((units[c] + parts - 1) / parts + kWarps - 1) / kWarps * kWarps);  // whole rounds of the warps
+    blocks += (fc::span_rows(g, c) + 8 * nt - 1) / (8 * nt) * parts;
+    g.block_end[c] = (int32_t)std::min<int64_t>(blocks, INT32_MAX);
+  }
+  return cut.us;
 }
 
 typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
@@ -787,13 +892,10 @@ int map_rows(fc_ctx* ctx, CUtensorMap* map, const void* base, const fc::SpanGeom
 namespace fc {
 
 size_t span_rows_workspace(const fc_ctx* ctx, SpanGeom& g) {
-  bool many = false;
-  for (int c = 0; c < g.W; ++c) many |= span_rows(g, c) > 8;
-  g.row_tiles = many ? 2 : 1;
-  g.rows_us = split(ctx, g, g.row_tiles) + 2;
+  g.rows_us = split(ctx, g);
   bool joined = false;
   for (int c = 0; c < g.W; ++c) joined |= g.parts[c] > 1;
-  if (!joined) return 0;
+  if (!joined || g.cluster) return 0;
   const size_t rows = (size_t)g.H_kv * g.block_end[g.W - 1] * 8 * g.row_tiles;
   return align_up(rows * g.d * sizeof(float), 256) + align_up(rows * sizeof(float2), 256);
 }
@@ -817,11 +919,23 @@ int span_rows_launch(fc_ctx* ctx, cudaStream_t st, const SpanGeom& g, const void
   if (plain && ((rc = map_rows(ctx, &k, K, g, g.k_hs, g.k_rs)) != FC_OK || (rc = map_rows(ctx, &v, V, g, g.v_hs, g.v_rs)) != FC_OK)) return rc;
   const dim3 grid((unsigned)blocks, (unsigned)g.H_kv);
   constexpr int smem = kWarps * kRing + 1024;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = st;
+  cudaLaunchAttribute attr;
+  attr.id = cudaLaunchAttributeClusterDimension;
+  attr.val.clusterDim.x = (unsigned)std::max(g.cluster, 1);
+  attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+  cfg.attrs = &attr;
+  cfg.numAttrs = g.cluster > 1 ? 1 : 0;
 #define FC_SPAN_ROWS(T, D, NT)                                                                                                        \
   do {                                                                                                                                \
-    static_assert(kWarps * 8 * NT * (D + 4) * 4 <= kWarps * kRing, "the joined rows take the rings' place");                          \
+    static_assert((kWarps + 1) * 8 * NT * (D + 4) * 4 + 8 * NT * 8 <= kWarps * kRing, "what is joined takes the rings' place");       \
     FC_CUDA_CHECK(cudaFuncSetAttribute(attention_span_rows_kernel<T, D, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));     \
-    attention_span_rows_kernel<T, D, NT><<<grid, kThreads, smem, st>>>(k8, v8, k, v, (const T*)Q, (T*)O, g);                          \
+    if (g.cluster > 8) FC_CUDA_CHECK(cudaFuncSetAttribute(attention_span_rows_kernel<T, D, NT>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1)); \
+    FC_CUDA_CHECK(cudaLaunchKernelEx(&cfg, attention_span_rows_kernel<T, D, NT>, k8, v8, k, v, (const T*)Q, (T*)O, g));                \
   } while (0)
 #define FC_SPAN_ROWS_PICK(T)                                                                       \
   do {                                                                                             \
@@ -833,7 +947,7 @@ int span_rows_launch(fc_ctx* ctx, cudaStream_t st, const SpanGeom& g, const void
 #undef FC_SPAN_ROWS_PICK
 #undef FC_SPAN_ROWS
   FC_LAUNCH_CHECK("attention_span_rows_kernel");
-  if (!joined) return FC_OK;
+  if (!joined || g.cluster) return FC_OK;
   const dim3 join((unsigned)rows, (unsigned)g.H_kv);
   cudaError_t e;
   if (g.f32) e = g.d == 128 ? launch_pdl(attention_span_join_kernel<float, 128>, join, dim3(128), 0, st, (float*)O, g, blocks)
