@@ -920,18 +920,20 @@ class Context:
                 raise FcError("lse must be [H_q, rows] with contiguous rows")
             lse_hs = max(lse.stride(0), 1)
         L, h = self._L, self._h
-        if ws is None:
+        ids, n = self._ptr(active_ids, "active_ids", torch.int32), self._ptr(n_active, "n_active", torch.int32)
+        lse_p, status = self._ptr(lse, "lse", torch.float32), self._ptr(status, "status", torch.int32)
+
+        def call(ws):
+            tail = (ids, n, op, lse_p, lse_hs, status, self._ptr(ws, "ws"), 0 if ws is None else ws.numel())
+            if paged:
+                return L.fc_chunk_attention_kv8(h, stream, dp, qp, *paged[:4], kp, vp, dt, off, vis, n_sink, begin, first, sl, sp, n_seg, *tail)
+            return L.fc_chunk_attention_span(h, stream, dp, qp, kp, vp, dt, off, vis, n_sink, begin, sl, sp, n_seg, *tail)
+
+        rc = call(ws)
+        if rc == -4 and ws is None:  # few rows mostly need no workspace, and a call that is refused has launched nothing
             need = (L.fc_chunk_attention_kv8_workspace_bytes(h, dp, dt, paged[4].page, paged[2], paged[3], off, vis, n_sink, begin, first, sl, n_seg)
                     if paged else L.fc_chunk_attention_span_workspace_bytes(h, dp, dt, off, vis, n_sink, begin, sl, n_seg))
-            if need:
-                ws = self._scratch("attention_span", need, stream)
-        tail = (self._ptr(active_ids, "active_ids", torch.int32), self._ptr(n_active, "n_active", torch.int32), op,
-                self._ptr(lse, "lse", torch.float32), lse_hs, self._ptr(status, "status", torch.int32), self._ptr(ws, "ws"),
-                0 if ws is None else ws.numel())
-        if paged:
-            rc = L.fc_chunk_attention_kv8(h, stream, dp, qp, *paged[:4], kp, vp, dt, off, vis, n_sink, begin, first, sl, sp, n_seg, *tail)
-        else:
-            rc = L.fc_chunk_attention_span(h, stream, dp, qp, kp, vp, dt, off, vis, n_sink, begin, sl, sp, n_seg, *tail)
+            rc = call(self._scratch("attention_span", need, stream))
         if rc:
             self._check(rc, f"fc_chunk_attention_{kind}")
         return O

@@ -269,17 +269,17 @@ attention_span_rows_kernel(const __grid_constant__ CUtensorMap map_k8, const __g
   // Lane L looks up steps L, 32 + L, ..., and sends for them when their turn comes.
   PagedStep cur = look_up(lane), next = look_up(32 + lane);
   const uint32_t bar_s = bar(0, 0, 0);
-  auto send_paged = [&](const PagedStep& x, int stage) {
+  auto send_paged = [&](int page, int row, int stage) {
     const uint32_t b = bar_s + 8 * stage, dst = ring_s + stage * (2 * R::kPaged);
-    if (x.page < 0) {  // nothing to bring: its keys are zeros
+    if (page < 0) {  // nothing to bring: its keys are zeros
       mbar_arrive(b);
     } else {
       mbar_expect_tx(b, 2 * R::kPaged);
-      tma_load_4d(dst, &map_k8, b, 0, x.row, hk, x.page);
-      tma_load_4d(dst + R::kPaged, &map_v8, b, 0, x.row, hk, x.page);
+      tma_load_4d(dst, &map_k8, b, 0, row, hk, page);
+      tma_load_4d(dst + R::kPaged, &map_v8, b, 0, row, hk, page);
     }
   };
-  if (lane < min(m, kPagedStages)) send_paged(cur, lane);
+  if (lane < min(m, kPagedStages)) send_paged(cur.page, cur.row, lane);
   // everything up to here asks only what the host knows; the list is on the device
   if (!fc::span_chunk_active(g, c)) {
     for (int i = 0; i < min(m, kPagedStages); ++i) mbar_wait_bounded(bar_s + 8 * i, 0, abort);  // what was sent for lands before its memory is given back
@@ -338,8 +338,8 @@ attention_span_rows_kernel(const __grid_constant__ CUtensorMap map_k8, const __g
     };
     const uint32_t k_at = ring_s + ka, va[2] = {ring_s + R::kPaged + v_at(2 * q), ring_s + R::kPaged + v_at(2 * q + 1)};
 
-    auto step = [&](uint32_t off, float ks, float vs, int lo, int hi, bool no_page, auto masked) {
-      constexpr bool kMask = decltype(masked)::value;
+    // A step in two halves: the products of the keys at `off` of the ring with Q, and what follows from them.
+    auto products = [&](uint32_t off, float (&s)[NT][4], float (&rest)[NT][4]) {
       uint32_t k0[D / 16], k1[D / 16];
 #pragma unroll
       for (int h = 0; h < D / 64; ++h) {
@@ -348,7 +348,6 @@ attention_span_rows_kernel(const __grid_constant__ CUtensorMap map_k8, const __g
         k0[4 * h] = a.x; k0[4 * h + 1] = a.y; k0[4 * h + 2] = a.z; k0[4 * h + 3] = a.w;
         k1[4 * h] = b.x; k1[4 * h + 1] = b.y; k1[4 * h + 2] = b.z; k1[4 * h + 3] = b.w;
       }
-      float s[NT][4], rest[NT][4];
 #pragma unroll
       for (int w = 0; w < D / 16; ++w) {
         const uint32_t a0 = fc::e4m3_lo2(k0[w]), a1 = fc::e4m3_lo2(k1[w]), a2 = fc::e4m3_hi2(k0[w]), a3 = fc::e4m3_hi2(k1[w]);
@@ -362,6 +361,9 @@ attention_span_rows_kernel(const __grid_constant__ CUtensorMap map_k8, const __g
           if constexpr (kHalves<T> == 2) add(rest[t], qb[1][t]);
         }
       }
+    };
+    auto finish = [&](uint32_t off, float (&s)[NT][4], const float (&rest)[NT][4], float ks, float vs, int lo, int hi, bool no_page, auto masked) {
+      constexpr bool kMask = decltype(masked)::value;
 #pragma unroll
       for (int t = 0; t < NT; ++t)
 #pragma unroll
@@ -412,8 +414,14 @@ attention_span_rows_kernel(const __grid_constant__ CUtensorMap map_k8, const __g
           }
         }
     };
+    // The products of one step are worked out before the other half of the step before, so that the two steps' chains of
+    // instructions fill each other's gaps.  (Behind the last step they are of whatever the ring holds, and not used.)
     int stage = 0;
     uint32_t parity = 0;
+    float s[NT][4], rest[NT][4], s_next[NT][4], rest_next[NT][4];
+    mbar_wait_bounded(bar_s, 0, abort);
+    __syncwarp();
+    products(0, s, rest);
     for (int i = 0; i < m; ++i) {
       const int at = i & 31;
       if (at == 0 && i > 0) {
@@ -422,19 +430,31 @@ attention_span_rows_kernel(const __grid_constant__ CUtensorMap map_k8, const __g
       }
       const float ks = __shfl_sync(0xffffffffu, cur.ks, at), vs = __shfl_sync(0xffffffffu, cur.vs, at);
       const bool part = __shfl_sync(0xffffffffu, cur.page < 0 || cur.hi - cur.lo < kStep, at);
-      mbar_wait_bounded(bar_s + 8 * stage, parity, abort);
+      const int stage1 = stage + 1 == kStages ? 0 : stage + 1;
+      const uint32_t parity1 = stage1 == 0 ? parity ^ 1 : parity;
+      const uint32_t off = stage * (2 * R::kPaged), off1 = stage1 * (2 * R::kPaged);
+      if (i + 1 < m) mbar_wait_bounded(bar_s + 8 * stage1, parity1, abort);
       __syncwarp();
-      const uint32_t off = stage * (2 * R::kPaged);
       if (!part) {
-        step(off, ks, vs, 0, kStep, false, std::false_type());
+        products(off1, s_next, rest_next);
+        finish(off, s, rest, ks, vs, 0, kStep, false, std::false_type());
       } else {
         const int lo = __shfl_sync(0xffffffffu, cur.lo, at), hi = __shfl_sync(0xffffffffu, cur.hi, at), page = __shfl_sync(0xffffffffu, cur.page, at);
-        step(off, ks, vs, lo, hi, page < 0, std::true_type());
+        products(off1, s_next, rest_next);
+        finish(off, s, rest, ks, vs, lo, hi, page < 0, std::true_type());
       }
+#pragma unroll
+      for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          s[t][k] = s_next[t][k];
+          if constexpr (kHalves<T> == 2) rest[t][k] = rest_next[t][k];
+        }
       __syncwarp();  // the step's place has been read by every lane: another step is sent for
       const int ahead = (at + kStages) & 31;
-      if (lane == ahead && i + kStages < m) send_paged(at + kStages < 32 ? cur : next, stage);
-      if (++stage == kStages) stage = 0, parity ^= 1;
+      if (lane == ahead && i + kStages < m) send_paged(at + kStages < 32 ? cur.page : next.page, at + kStages < 32 ? cur.row : next.row, stage);
+      stage = stage1;
+      parity = parity1;
     }
   }
 
@@ -775,8 +795,8 @@ struct UnitUs {
   double alone, two, full;
 };
 UnitUs unit_us(const fc::SpanGeom& g, int nt) {
-  static const UnitUs t[2][2][2] = {{{{0.115, 0.149, 0.057}, {0.122, 0.163, 0.081}}, {{0.156, 0.184, 0.099}, {0.177, 0.230, 0.115}}},
-                                    {{{0.122, 0.160, 0.063}, {0.152, 0.207, 0.104}}, {{0.186, 0.224, 0.098}, {0.228, 0.300, 0.150}}}};
+  static const UnitUs t[2][2][2] = {{{{0.115, 0.149, 0.057}, {0.122, 0.163, 0.081}}, {{0.150, 0.195, 0.095}, {0.183, 0.230, 0.115}}},
+                                    {{{0.122, 0.160, 0.063}, {0.152, 0.207, 0.104}}, {{0.200, 0.238, 0.088}, {0.224, 0.300, 0.150}}}};
   return t[g.f32][g.d == 128][nt - 1];
 }
 

@@ -4,14 +4,14 @@
 //   append   a block of threads owns one block of the store (page and head; K or V), whose rows it holds in registers between the
 //            one read, the maximum that gives the scale, and the one write.  Rows that were there before are read only
 //            where the scale grows.
-//   unpack   eight codes a thread and access, several rows' loads in flight.
+//   unpack   a 16-byte store a thread and access, several rows' loads in flight.
 //
 // Codes are the nearest ones to the true quotient, whatever the type.  A tie between two codes is a number t of at most five
 // significant bits, and a scale s has four.
-//   bf16 rows, and codes that are rounded again (8 significant bits: x is either t s or at least 2^-9 of it away): x (1/s) is off by
-//               2^-22 at most, so that it is rounded to 12 bits first, which puts a tie where it belongs and crosses none.
-//   fp32 rows   the rounded quotient is on the right side of a tie, or on it where x = t s: x is at least half an ulp of t, times s, away from
-//               t s otherwise, and more than half an ulp of the quotient.
+//   bf16 rows   (8 significant bits: x is either t s or at least 2^-9 of it away) x (1/s) is off by 2^-23 at most, so that it is
+//               rounded to fp16 first, which puts a tie where it belongs and crosses none.
+//   fp32 rows, and codes that are rounded again: the rounded quotient is on the right side of a tie, or on it where x = t s: x is otherwise
+//               away from t s by so much that the quotient is more than half an ulp from t.
 #include <algorithm>
 #include <climits>
 
@@ -21,7 +21,6 @@
 namespace {
 
 using fc::sm100::cvt_bf16x2;
-using fc::sm100::fma2;
 using fc::sm100::pack2;
 using fc::sm100::unpack2;
 
@@ -56,16 +55,34 @@ __device__ __forceinline__ void get8(const Eight<float>& x, float (&v)[8]) {
   v[4] = x.b.x; v[5] = x.b.y; v[6] = x.b.z; v[7] = x.b.w;
 }
 
-// Bits of the largest finite magnitude; `bad` if an element is not finite.
+__device__ __forceinline__ uint32_t max2_nan(uint32_t a, uint32_t b) {  // bf16 pairs; a NaN is the largest
+  uint32_t d;
+  asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+  return d;
+}
+// Bits of the largest magnitude; at or above those of infinity if an element is not finite.
+__device__ __forceinline__ uint32_t largest(const Eight<__nv_bfloat16>& x) {
+  constexpr uint32_t kAbs = 0x7fff7fffu;
+  const uint32_t m = max2_nan(max2_nan(x.w.x & kAbs, x.w.y & kAbs), max2_nan(x.w.z & kAbs, x.w.w & kAbs));
+  return max(m << 16, m & 0xffff0000u);
+}
+__device__ __forceinline__ uint32_t largest(const Eight<float>& x) {
+  float v[8];
+  get8(x, v);
+  uint32_t m = 0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) m = max(m, __float_as_uint(v[i]) & 0x7fffffffu);  // as integers
+  return m;
+}
+// The same of the finite elements alone.
 template <typename T>
-__device__ __forceinline__ uint32_t largest(const Eight<T>& x, bool& bad) {
+__device__ __noinline__ uint32_t largest_finite(const Eight<T> x) {
   float v[8];
   get8(x, v);
   uint32_t m = 0;
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
     const uint32_t a = __float_as_uint(v[i]) & 0x7fffffffu;
-    bad |= a >= 0x7f800000u;
     m = max(m, a >= 0x7f800000u ? 0u : a);
   }
   return m;
@@ -80,43 +97,56 @@ __device__ __forceinline__ float scale_of(uint32_t a) {
   return fminf(__uint_as_float(448.f * __uint_as_float(low) >= x ? low : low + 0x100000u), 0x1p119f);
 }
 
-// Pairs of x / s: r = 1 / s, rounded.  See the head of the file for why this meets every tie.
+// Two codes of x / s: r = 1 / s, rounded.  See the head of the file for why this meets every tie.  An infinity would be cut to 448.
 __device__ __forceinline__ uint32_t codes2_short(float x0, float x1, uint64_t r2) {
-  const uint64_t q = mul2(pack2(x0, x1), r2);
-  const uint64_t t = mul2(q, pack2(4097.f, 4097.f));
-  const uint64_t rest = fma2(q, pack2(-1.f, -1.f), t);      // t - q
-  const uint64_t cut = fma2(rest, pack2(-1.f, -1.f), t);    // q in 12 bits; NaN for an infinity
   float a, b;
-  unpack2(cut, a, b);
-  return cvt_e4m3x2(a, b);
+  unpack2(mul2(pack2(x0, x1), r2), a, b);
+  uint32_t h;
+  uint16_t d;
+  asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(h) : "f"(b), "f"(a));
+  asm("cvt.rn.satfinite.e4m3x2.f16x2 %0, %1;" : "=h"(d) : "r"(h));
+  return d;
 }
-__device__ __forceinline__ uint2 codes8(const Eight<__nv_bfloat16>& x, float, float r) {
+__device__ __forceinline__ uint2 codes8_finite(const Eight<__nv_bfloat16>& x, float, float r) {
   float v[8];
   get8(x, v);
   const uint64_t r2 = pack2(r, r);
-  return make_uint2(codes2_short(v[0], v[1], r2) | codes2_short(v[2], v[3], r2) << 16,
-                    codes2_short(v[4], v[5], r2) | codes2_short(v[6], v[7], r2) << 16);
+  return make_uint2(__byte_perm(codes2_short(v[0], v[1], r2), codes2_short(v[2], v[3], r2), 0x5410),
+                    __byte_perm(codes2_short(v[4], v[5], r2), codes2_short(v[6], v[7], r2), 0x5410));
 }
-__device__ __forceinline__ uint2 codes8(const Eight<float>& x, float s, float) {
+template <bool kFinite>
+__device__ __forceinline__ uint2 codes8_of(const float (&x)[8], float s) {
   float v[8];
-  get8(x, v);
 #pragma unroll
-  for (int i = 0; i < 8; ++i) v[i] = fmaf(v[i], 0.f, s > 0.f ? __fdiv_rn(v[i], s) : v[i]);  // an infinity becomes a NaN
+  for (int i = 0; i < 8; ++i) {
+    v[i] = s > 0.f ? __fdiv_rn(x[i], s) : x[i];
+    if (!kFinite) v[i] = fmaf(x[i], 0.f, v[i]);  // an infinity becomes a NaN
+  }
   return make_uint2(cvt_e4m3x2(v[0], v[1]) | cvt_e4m3x2(v[2], v[3]) << 16, cvt_e4m3x2(v[4], v[5]) | cvt_e4m3x2(v[6], v[7]) << 16);
 }
-// Eight codes of scale s_old as codes of a larger scale.
-__device__ __forceinline__ uint2 again8(uint2 c, float s_old, float r) {
-  const uint64_t r2 = pack2(r, r);
-  auto four = [&](uint32_t w) {
-    const uint32_t lo = fc::e4m3_lo2(w), hi = fc::e4m3_hi2(w);
-    return codes2_short(fc::half_lo(lo) * s_old, fc::half_hi(lo) * s_old, r2) |
-           codes2_short(fc::half_lo(hi) * s_old, fc::half_hi(hi) * s_old, r2) << 16;
-  };
-  return make_uint2(four(c.x), four(c.y));
+__device__ __forceinline__ uint2 codes8_finite(const Eight<float>& x, float s, float) {
+  float v[8];
+  get8(x, v);
+  return codes8_of<true>(v, s);
+}
+// Any elements, as quotients: what the two above give for finite ones.
+template <typename T>
+__device__ __noinline__ uint2 codes8_any(const Eight<T> x, float s) {
+  float v[8];
+  get8(x, v);
+  return codes8_of<false>(v, s);
+}
+// Eight codes of scale s_old as codes of a larger scale s.
+__device__ __noinline__ uint2 again8(uint2 c, float s_old, float s) {
+  const uint32_t h[4] = {fc::e4m3_lo2(c.x), fc::e4m3_hi2(c.x), fc::e4m3_lo2(c.y), fc::e4m3_hi2(c.y)};
+  float v[8];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) v[2 * i] = fc::half_lo(h[i]) * s_old, v[2 * i + 1] = fc::half_hi(h[i]) * s_old;  // eight bits: exact
+  return codes8_of<true>(v, s);  // a NaN stays one
 }
 
 struct AppendGeom {
-  int32_t W;
+  int32_t W, H;
   int32_t block_end[FC_MAX_CHUNKS];  // running count of the pages that sequences write to
   int32_t row_off[FC_MAX_CHUNKS + 1], pos[FC_MAX_CHUNKS];
   int64_t k_hs, k_rs, v_hs, v_rs, table_cs;
@@ -124,22 +154,22 @@ struct AppendGeom {
   const int32_t *table, *ref;
 };
 
-// kThreads threads hold kVec vectors of eight elements each: a block of page x d elements.
-template <typename T, int D, int kThreads, int kVec>
-__global__ void __launch_bounds__(kThreads)
+constexpr int kAppendThreads = 256;
+
+// A group of kGroup threads owns a block of page x d elements, kVec vectors of eight elements a thread; the groups of a block of threads own
+// neighbouring heads' ones.
+template <typename T, int D, int kGroup, int kVec>
+__global__ void __launch_bounds__(kAppendThreads)
 kv8_append_kernel(const T* __restrict__ K, const T* __restrict__ V, const __grid_constant__ AppendGeom g, uint32_t* __restrict__ status) {
-  constexpr int kRowVecs = D / 8;
-  __shared__ uint32_t largest_s[kThreads / 32];
-  const int tid = threadIdx.x, h = blockIdx.y;
+  constexpr int kRowVecs = D / 8, kGroups = kAppendThreads / kGroup;
+  __shared__ uint32_t largest_s[kAppendThreads / 32];
+  const int group = threadIdx.x / kGroup, tid = threadIdx.x % kGroup, h = blockIdx.y * kGroups + group;
   const bool is_v = blockIdx.z != 0;
   int c = 0;
   while (c + 1 < g.W && (int)blockIdx.x >= g.block_end[c]) ++c;
   const int entry = g.pos[c] / (1 << g.pool.page_log2) + (int)blockIdx.x - (c > 0 ? g.block_end[c - 1] : 0);
   const int page_id = g.table[c * g.table_cs + entry];
-  if (page_id < 0 || page_id >= g.pool.n_pages || (g.ref && g.ref[page_id] != 1)) {
-    if (tid == 0 && status) atomicOr(status, (uint32_t)FC_DEV_BAD_INDEX);
-    return;
-  }
+  if (h >= g.H) return;  // a whole group
   // rows lo .. hi - 1 of the block are new; row r of it is row src0 + r of the source
   const int64_t token0 = (int64_t)entry << g.pool.page_log2, src0 = g.row_off[c] + token0 - g.pos[c];
   const int page = 1 << g.pool.page_log2;
@@ -147,37 +177,52 @@ kv8_append_kernel(const T* __restrict__ K, const T* __restrict__ V, const __grid
   const int hi = (int)min((int64_t)page, g.pos[c] + (int64_t)(g.row_off[c + 1] - g.row_off[c]) - token0);
   const T* src = (is_v ? V + h * g.v_hs : K + h * g.k_hs);
   const int64_t rs = is_v ? g.v_rs : g.k_rs;
-  uint8_t* codes = (is_v ? g.pool.v_codes : g.pool.k_codes) + page_id * g.pool.code_ps + h * g.pool.code_hs;
-  float* scale_p = (is_v ? g.pool.v_scales : g.pool.k_scales) + page_id * g.pool.scale_ps + h * g.pool.scale_hs;
-
   Eight<T> x[kVec];
   bool bad = false;
   uint32_t a = 0;
 #pragma unroll
   for (int i = 0; i < kVec; ++i) {
-    const int vec = tid + i * kThreads, row = vec / kRowVecs;
+    const int vec = tid + i * kGroup, row = vec / kRowVecs;
     if (row >= lo && row < hi) load8(src + (src0 + row) * rs + vec % kRowVecs * 8, x[i]);
   }
+  // the rows are on their way whether or not there is a page for them
+  if (page_id < 0 || page_id >= g.pool.n_pages || (g.ref && g.ref[page_id] != 1)) {
+    if (threadIdx.x == 0 && status) atomicOr(status, (uint32_t)FC_DEV_BAD_INDEX);
+    return;
+  }
+  uint8_t* codes = (is_v ? g.pool.v_codes : g.pool.k_codes) + page_id * g.pool.code_ps + h * g.pool.code_hs;
+  float* scale_p = (is_v ? g.pool.v_scales : g.pool.k_scales) + page_id * g.pool.scale_ps + h * g.pool.scale_hs;
   const float s_old = lo > 0 ? *scale_p : 0.f;
 #pragma unroll
   for (int i = 0; i < kVec; ++i) {
-    const int row = (tid + i * kThreads) / kRowVecs;
-    if (row >= lo && row < hi) a = max(a, largest(x[i], bad));
+    const int row = (tid + i * kGroup) / kRowVecs;
+    if (row >= lo && row < hi) a = max(a, largest(x[i]));
+  }
+  if (a >= 0x7f800000u) {
+    bad = true;
+    a = 0;
+#pragma unroll
+    for (int i = 0; i < kVec; ++i) {
+      const int row = (tid + i * kGroup) / kRowVecs;
+      if (row >= lo && row < hi) a = max(a, largest_finite<T>(x[i]));
+    }
   }
   a = __reduce_max_sync(0xffffffffu, a);
-  if (tid % 32 == 0) largest_s[tid / 32] = a;
-  __syncthreads();
+  if constexpr (kGroup > 32) {
+    if (tid % 32 == 0) largest_s[threadIdx.x / 32] = a;
+    asm volatile("bar.sync %0, %1;" ::"r"(1 + group), "n"(kGroup) : "memory");
 #pragma unroll
-  for (int i = 0; i < kThreads / 32; ++i) a = max(a, largest_s[i]);
+    for (int i = 0; i < kGroup / 32; ++i) a = max(a, largest_s[group * (kGroup / 32) + i]);
+  }
   const float s = fmaxf(scale_of(a), s_old), r = s > 0.f ? __frcp_rn(s) : 0.f;
 #pragma unroll
   for (int i = 0; i < kVec; ++i) {
-    const int vec = tid + i * kThreads, row = vec / kRowVecs;
+    const int vec = tid + i * kGroup, row = vec / kRowVecs;
     uint2* at = reinterpret_cast<uint2*>(codes + vec * 8);
-    if (row >= lo && row < hi) *at = codes8(x[i], s, r);
-    else if (row < lo && s > s_old) *at = again8(*at, s_old, r);
+    if (row >= lo && row < hi) *at = bad ? codes8_any<T>(x[i], s) : codes8_finite(x[i], s, r);
+    else if (row < lo && s > s_old) *at = again8(*at, s_old, s);
   }
-  if (tid == 0 && (lo == 0 || s > s_old)) *scale_p = s;  // every thread has read the old one before the barrier
+  if (tid == 0 && (lo == 0 || s > s_old)) *scale_p = s;  // every thread of the group has read the old one
   if (bad && status) atomicOr(status, (uint32_t)FC_DEV_NONFINITE);
 }
 
@@ -192,18 +237,27 @@ struct UnpackGeom {
 constexpr int kUnpackThreads = 256;
 constexpr int kUnpackRows = 4;  // rows whose loads are in flight together
 
-__device__ __forceinline__ void store8(__nv_bfloat16* p, const float (&v)[8]) {
-  *reinterpret_cast<uint4*>(p) = make_uint4(cvt_bf16x2(v[0], v[1]), cvt_bf16x2(v[2], v[3]), cvt_bf16x2(v[4], v[5]), cvt_bf16x2(v[6], v[7]));
+// The codes of a 16-byte store, and their values.
+__device__ __forceinline__ void store_values(__nv_bfloat16* p, uint2 c, float s) {
+  const uint32_t h[4] = {fc::e4m3_lo2(c.x), fc::e4m3_hi2(c.x), fc::e4m3_lo2(c.y), fc::e4m3_hi2(c.y)};
+  uint32_t w[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) w[i] = cvt_bf16x2(fc::half_lo(h[i]) * s, fc::half_hi(h[i]) * s);
+  *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
 }
-__device__ __forceinline__ void store8(float* p, const float (&v)[8]) {
-  *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
-  *reinterpret_cast<float4*>(p + 4) = make_float4(v[4], v[5], v[6], v[7]);
+__device__ __forceinline__ void store_values(float* p, uint32_t c, float s) {
+  const uint32_t a = fc::e4m3_lo2(c), b = fc::e4m3_hi2(c);
+  *reinterpret_cast<float4*>(p) = make_float4(fc::half_lo(a) * s, fc::half_hi(a) * s, fc::half_lo(b) * s, fc::half_hi(b) * s);
 }
+template <typename T> struct Codes;
+template <> struct Codes<__nv_bfloat16> { using type = uint2; };
+template <> struct Codes<float> { using type = uint32_t; };
 
 template <typename T, int D>
 __global__ void __launch_bounds__(kUnpackThreads)
 kv8_unpack_kernel(T* __restrict__ K, T* __restrict__ V, const __grid_constant__ UnpackGeom g) {
-  constexpr int kRowVecs = D / 8, R = kUnpackThreads / kRowVecs;
+  using C = typename Codes<T>::type;
+  constexpr int kVec = sizeof(C), kRowVecs = D / kVec, R = kUnpackThreads / kRowVecs;
   fc::pdl_launch_dependents();
   const int w = threadIdx.x % kRowVecs, h = blockIdx.y;
   const bool is_v = blockIdx.z & 1;
@@ -218,7 +272,7 @@ kv8_unpack_kernel(T* __restrict__ K, T* __restrict__ V, const __grid_constant__ 
   const int64_t hs = is_v ? g.v_hs : g.k_hs, rs = is_v ? g.v_rs : g.k_rs;
   const int32_t* table = g.table + job.seq * g.table_cs;
   int32_t page_id[kUnpackRows];
-  uint2 word[kUnpackRows];
+  C word[kUnpackRows];
   float scale[kUnpackRows];
 #pragma unroll
   for (int u = 0; u < kUnpackRows; ++u) {
@@ -229,12 +283,12 @@ kv8_unpack_kernel(T* __restrict__ K, T* __restrict__ V, const __grid_constant__ 
 #pragma unroll
   for (int u = 0; u < kUnpackRows; ++u) {
     const int64_t r = r0 + u * R;
-    word[u] = make_uint2(0u, 0u);
+    word[u] = C{};
     scale[u] = 0.f;
     if (r >= job.n) continue;
     if (page_id[u] >= 0 && page_id[u] < g.src.n_pages) {
       const int in_page = (int)((job.first + r) & ((1 << g.src.page_log2) - 1));
-      word[u] = __ldg(reinterpret_cast<const uint2*>(codes + page_id[u] * g.src.code_ps + in_page * D + 8 * w));
+      word[u] = __ldg(reinterpret_cast<const C*>(codes + page_id[u] * g.src.code_ps + in_page * D + kVec * w));
       scale[u] = __ldg(scales + page_id[u] * g.src.scale_ps);
     } else {
       bad = true;
@@ -243,12 +297,7 @@ kv8_unpack_kernel(T* __restrict__ K, T* __restrict__ V, const __grid_constant__ 
 #pragma unroll
   for (int u = 0; u < kUnpackRows; ++u) {
     const int64_t r = r0 + u * R;
-    if (r >= job.n) continue;
-    const uint32_t p[4] = {fc::e4m3_lo2(word[u].x), fc::e4m3_hi2(word[u].x), fc::e4m3_lo2(word[u].y), fc::e4m3_hi2(word[u].y)};
-    float v[8];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) v[2 * i] = fc::half_lo(p[i]) * scale[u], v[2 * i + 1] = fc::half_hi(p[i]) * scale[u];
-    store8(dst + h * hs + (job.dst_row + r) * rs + 8 * w, v);
+    if (r < job.n) store_values(dst + h * hs + (job.dst_row + r) * rs + kVec * w, word[u], scale[u]);
   }
   if (bad && g.status) atomicOr(g.status, (uint32_t)FC_DEV_BAD_INDEX);
 }
@@ -283,7 +332,7 @@ int kv8_unpack_launch(cudaStream_t st, const Kv8View& src, int H, int d, const i
   for (int i = 0; i < jobs.n; ++i) n = std::max(n, jobs.job[i].n);
   if (n == 0 || (!K_dst && !V_dst)) return FC_OK;
   UnpackGeom g = {jobs, k_hs, k_rs, v_hs, v_rs, table_cs, src, table, status, clear};
-  const int rows = kUnpackRows * kUnpackThreads / (d / 8);
+  const int rows = kUnpackRows * kUnpackThreads / (d / (dtype == FC_F32 ? 4 : 8));
   const dim3 grid((unsigned)((n + (int64_t)rows - 1) / rows), (unsigned)H, 2u * jobs.n);
 #define FC_UNPACK(T, D) kv8_unpack_kernel<T, D><<<grid, kUnpackThreads, 0, st>>>((T*)K_dst, (T*)V_dst, g)
   if (dtype == FC_F32) { if (d == 128) FC_UNPACK(float, 128); else FC_UNPACK(float, 64); }
@@ -309,6 +358,7 @@ extern "C" int fc_kv8_append(fc_ctx* ctx, void* stream, const fc_kv8_rows* desc,
   if ((rc = fc::kv8_check(pool, desc->H, desc->d)) != FC_OK) return rc;
   AppendGeom g = {};
   g.W = desc->W;
+  g.H = desc->H;
   g.pool = fc::kv8_view(*pool);
   int64_t blocks = 0;
   for (int c = 0; c < g.W; ++c) {
@@ -327,19 +377,20 @@ extern "C" int fc_kv8_append(fc_ctx* ctx, void* stream, const fc_kv8_rows* desc,
   g.table = table; g.table_cs = table_cs; g.ref = ref;
   FC_DEVICE_GUARD(ctx);
   cudaStream_t st = (cudaStream_t)stream;
-  const dim3 grid((unsigned)blocks, (unsigned)desc->H, 2);
-#define FC_APPEND(T, D, THREADS, VEC) kv8_append_kernel<T, D, THREADS, VEC><<<grid, THREADS, 0, st>>>((const T*)K_src, (const T*)V_src, g, status)
+#define FC_APPEND(T, D, GROUP, VEC)                                                                                              \
+  kv8_append_kernel<T, D, GROUP, VEC><<<dim3((unsigned)blocks, (unsigned)((desc->H + kAppendThreads / GROUP - 1) / (kAppendThreads / GROUP)), 2), \
+                                        kAppendThreads, 0, st>>>((const T*)K_src, (const T*)V_src, g, status)
 #define FC_APPEND_PICK(T)                                                                                                        \
   do {                                                                                                                           \
     if (desc->d == 128) switch (pool->page) {                                                                                    \
-      case 16: FC_APPEND(T, 128, 256, 1); break;                                                                                 \
-      case 32: FC_APPEND(T, 128, 256, 2); break;                                                                                 \
+      case 16: FC_APPEND(T, 128, 64, 4); break;                                                                                  \
+      case 32: FC_APPEND(T, 128, 128, 4); break;                                                                                 \
       case 64: FC_APPEND(T, 128, 256, 4); break;                                                                                 \
       default: FC_APPEND(T, 128, 256, 8);                                                                                        \
     } else switch (pool->page) {                                                                                                 \
-      case 16: FC_APPEND(T, 64, 128, 1); break;                                                                                  \
-      case 32: FC_APPEND(T, 64, 256, 1); break;                                                                                  \
-      case 64: FC_APPEND(T, 64, 256, 2); break;                                                                                  \
+      case 16: FC_APPEND(T, 64, 32, 4); break;                                                                                   \
+      case 32: FC_APPEND(T, 64, 64, 4); break;                                                                                   \
+      case 64: FC_APPEND(T, 64, 128, 4); break;                                                                                  \
       default: FC_APPEND(T, 64, 256, 4);                                                                                         \
     }                                                                                                                            \
   } while (0)
