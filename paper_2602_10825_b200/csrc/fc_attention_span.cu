@@ -145,9 +145,9 @@ bool plan_tiles(const fc_ctx* ctx, const fc::SpanGeom& g, TilePlan& p) {
   float last = 0.f;
   const int rest = (int)(items % ctx->sm_count);
   if (rest > 0) fc::split_parts(rest, ctx->sm_count, most_tiles, g.d, p.split.slots, &last);
-  // 8 us for the launches of the path, 1.8 us a key tile, the unpacking at 5 TB/s
+  // 9 us for the launches of the path, 1.8 us a key tile, the unpacking at 6.4 TB/s
   const double whole = items > 0 ? (double)tiles / items : 0;
-  p.us = 8 + 1.8 * ((double)(items / ctx->sm_count) * whole + last) + 2.0 * g.H_kv * p.rows * g.d * 3 / 5e6;
+  p.us = 9 + 1.8 * ((double)(items / ctx->sm_count) * whole + last) + 2.0 * g.H_kv * p.rows * g.d * 3 / 6.4e6;
   const size_t bytes = (size_t)g.H_kv * p.rows * g.d * 2, parts = (size_t)p.split.slots * 256;
   p.k = fc::attention_tc_workspace_bytes();
   p.v = p.k + fc::align_up(bytes, 256);

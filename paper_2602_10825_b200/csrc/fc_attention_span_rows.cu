@@ -35,6 +35,7 @@ constexpr int kWarps = 4, kThreads = 32 * kWarps;
 constexpr int kStep = 16;            // keys per warp and step
 constexpr int kRing = 16 * 1024;     // bytes of a warp's two rings
 constexpr int kMaxCluster = 16;      // blocks of a cluster
+constexpr int kSmem = kWarps * kRing + 1024;  // of a block, the rings on a 1024-byte boundary
 constexpr float kSlack = 8.f;        // log2 units by which a logit may pass the maximum before that moves
 constexpr float kLift = 7.f;         // weights are 2^kLift at the maximum
 constexpr int blocks_per_sm(int nt) { return nt == 1 ? 3 : 2; }
@@ -777,8 +778,12 @@ attention_span_join_kernel(T* __restrict__ O, const __grid_constant__ fc::SpanGe
 
 constexpr int kMaxParts = 256;
 
-// Units of cost of a chunk's keys (see the kernel).
-int64_t units_of(const fc::SpanGeom& g, int c) {
+// Units of cost of a chunk's keys (see the kernel), over pages and over plain rows.
+struct Units {
+  int64_t paged, plain;
+  int64_t all() const { return std::max<int64_t>(1, paged + plain); }
+};
+Units units_of(const fc::SpanGeom& g, int c) {
   auto steps = [&](int i) { return g.hi[i][c] > g.lo[i][c] ? (g.hi[i][c] + kStep - 1) / kStep - g.lo[i][c] / kStep : 0; };
   int64_t plain = 0;
   for (int i = 2; i < 4; ++i)
@@ -786,73 +791,80 @@ int64_t units_of(const fc::SpanGeom& g, int c) {
       const int n = std::min(g.hi[i][c], g.seg_log[s + 1]) - std::max(g.lo[i][c], g.seg_log[s]);
       if (n > 0) plain += (n + kStep - 1) / kStep;
     }
-  return steps(0) + steps(1) + plain * (g.f32 ? kPlainCost<float> : kPlainCost<__nv_bfloat16>);
+  return {steps(0) + steps(1), plain * (g.f32 ? kPlainCost<float> : kPlainCost<__nv_bfloat16>)};
 }
 
-// Measured on B200, in microseconds a unit of cost (a step over pages of a block's four warps, divided by four): of a block alone on its SM,
-// of one of two, and of an SM whose blocks keep it busy (D = 128: the bandwidth).  Steps over plain rows come to 0.7 to 1.3 of this a unit.
+// Measured on B200, in microseconds a unit of cost (a step of one of a block's four warps, divided by four and, over plain rows, by kPlainCost): of a
+// block alone on its SM, of one of two, and of an SM whose blocks keep it busy (D = 128: the bandwidth).
 struct UnitUs {
   double alone, two, full;
 };
-UnitUs unit_us(const fc::SpanGeom& g, int nt) {
-  static const UnitUs t[2][2][2] = {{{{0.115, 0.149, 0.057}, {0.122, 0.163, 0.081}}, {{0.150, 0.195, 0.095}, {0.183, 0.230, 0.115}}},
-                                    {{{0.122, 0.160, 0.063}, {0.152, 0.207, 0.104}}, {{0.200, 0.238, 0.088}, {0.224, 0.300, 0.150}}}};
-  return t[g.f32][g.d == 128][nt - 1];
+UnitUs unit_us(const fc::SpanGeom& g, int nt, double plain) {  // plain: their share of all units
+  static const UnitUs t[2][2][2][2] = {{{{{0.115, 0.149, 0.057}, {0.088, 0.099, 0.052}}, {{0.122, 0.163, 0.081}, {0.092, 0.103, 0.051}}},
+                                        {{{0.150, 0.195, 0.095}, {0.109, 0.184, 0.095}}, {{0.183, 0.230, 0.115}, {0.111, 0.188, 0.094}}}},
+                                       {{{{0.122, 0.160, 0.063}, {0.100, 0.126, 0.063}}, {{0.152, 0.207, 0.104}, {0.113, 0.145, 0.072}}},
+                                        {{{0.200, 0.238, 0.088}, {0.178, 0.237, 0.122}}, {{0.224, 0.300, 0.150}, {0.210, 0.275, 0.138}}}}};
+  const UnitUs &a = t[g.f32][g.d == 128][nt - 1][0], &b = t[g.f32][g.d == 128][nt - 1][1];
+  return {a.alone + plain * (b.alone - a.alone), a.two + plain * (b.two - a.two), a.full + plain * (b.full - a.full)};
 }
 
 // How a call's keys are cut for tiles of 8 nt rows.
 //   in clusters   every tile's keys into the same number of parts, at most 16, whose blocks are a cluster and join themselves
 //   by size       every chunk's into parts of at most `size` units, which a second kernel joins (3.5 us and its bytes): where a few tiles see many keys,
 //                 or some chunks far more than others
-// of which the fastest is taken, by the times above; a call takes 4.4 us besides.  Clusters cannot fill a group of SMs to its last place, which
-// leaves about a tenth (more than eight blocks: a fifth) of the device's places free.  Of 60 calls at random, of 5 to 60 us, the choice was 3 %
-// above the best of sixteen cuts in the median and within 20 % for nine in ten; 68 % in one, of six chunks of which the device left five out.
+// of which the fastest is taken, by the times above; a call takes 4.4 us besides.
+// Of 60 calls at random, of 5 to 60 us, the choice was 3 % above the best of sixteen cuts in the median and within 12 % for nine in ten; 63 % in one, of six
+// chunks of which the device left five out, which the host does not know.
 struct Cut {
   double us;
   int32_t cluster;
   int64_t size;
 };
-Cut cut_of(const fc_ctx* ctx, const fc::SpanGeom& g, int nt, const int64_t* units) {
-  const UnitUs u = unit_us(g, nt);
+Cut cut_of(const fc_ctx* ctx, const fc::SpanGeom& g, int nt, const Units* units) {
   const double sm = ctx->sm_count, places = sm * blocks_per_sm(nt);
   int64_t tiles[FC_MAX_CHUNKS], all = 0, most = 1;
-  double work = 0;
+  double work = 0, plain = 0;
   for (int c = 0; c < g.W; ++c) {
     tiles[c] = (fc::span_rows(g, c) + 8 * nt - 1) / (8 * nt) * g.H_kv;
     all += tiles[c];
-    work += (double)tiles[c] * units[c];
-    if (tiles[c]) most = std::max(most, units[c]);
+    work += (double)tiles[c] * units[c].all();
+    plain += (double)tiles[c] * units[c].plain;
+    if (tiles[c]) most = std::max(most, units[c].all());
   }
-  auto time_of = [&](double blocks, double size, double room) {
+  const UnitUs u = unit_us(g, nt, work > 0 ? plain / work : 0);
+  // Clusters lie unevenly: some SMs hold three blocks before every one holds two.
+  auto time_of = [&](double blocks, double size, double room, bool clusters) {
     size = std::ceil(size / kWarps) * kWarps;
-    if (blocks <= room) return size * std::max(blocks <= sm ? u.alone : blocks <= 1.75 * sm ? u.two : 1.25 * u.two, u.full * blocks / sm);
+    const double lone = blocks <= sm ? u.alone : blocks <= (clusters ? 1.75 : 2.0) * sm || nt == 2 ? u.two : 1.25 * u.two;
+    if (blocks <= room) return size * std::max(lone, u.full * blocks / sm);
     return u.full * work / sm + 0.7 * size * u.alone + 3.5 * blocks / room;  // a set of blocks takes 3.5 us to start and end
   };
   Cut best = {0, 1, 0};
   for (int n = 1; n <= kMaxCluster && (n == 1 || most >= kWarps * n); ++n) {
-    const double room = n == 1 ? places : (n <= 8 ? 0.9 : nt == 1 ? 0.82 : 0.78) * places;
-    const double us = 4.4 + (n > 1 ? 0.5 + 0.1 * n : 0) + time_of((double)all * n, (double)((most + n - 1) / n), room);
+    const int held = ctx->span_clusters[g.f32][g.d == 128][nt - 1][n];
+    const double room = n == 1 ? places : held > 0 ? (double)held * n : 0.75 * places;
+    const double us = 4.4 + (n > 1 ? 0.5 + 0.1 * n : 0) + time_of((double)all * n, (double)((most + n - 1) / n), room, n > 1);
     if (n == 1 || us < best.us) best = {us, n, 0};
   }
   for (int64_t n = 2; n <= kMaxParts && most >= 2 * kWarps * n; n += (n + 7) / 8) {
     const int64_t size = (most + n - 1) / n;
     double blocks = 0, rows = 0;
     for (int c = 0; c < g.W; ++c) {
-      const double parts = (double)((units[c] + size - 1) / size);
+      const double parts = (double)((units[c].all() + size - 1) / size);
       blocks += tiles[c] * parts;
       if (parts > 1) rows += tiles[c] * parts * 8 * nt;
     }
-    const double us = 4.4 + 3.5 + 2.0 * 4 * g.d * rows / 4e6 + time_of(blocks, (double)size, places);
+    const double us = 4.4 + 3.5 + 2.0 * 4 * g.d * rows / 4e6 + time_of(blocks, (double)size, places, false);
     if (us < best.us) best = {us, 0, size};
   }
   return best;
 }
 
 double split(const fc_ctx* ctx, fc::SpanGeom& g) {
-  int64_t units[FC_MAX_CHUNKS];
+  Units units[FC_MAX_CHUNKS];
   bool many = false;
   for (int c = 0; c < g.W; ++c) {
-    units[c] = std::max<int64_t>(1, units_of(g, c));
+    units[c] = units_of(g, c);
     many |= fc::span_rows(g, c) > 8;
   }
   // sixteen rows to a tile where some chunk has more than eight, unless twice the tiles are faster
@@ -866,9 +878,9 @@ double split(const fc_ctx* ctx, fc::SpanGeom& g) {
   g.cluster = cut.cluster;
   int64_t blocks = 0;
   for (int c = 0; c < g.W; ++c) {
-    const int64_t parts = cut.cluster ? cut.cluster : (units[c] + cut.size - 1) / cut.size;
+    const int64_t n = units[c].all(), parts = cut.cluster ? cut.cluster : (n + cut.size - 1) / cut.size;
     g.parts[c] = (int32_t)parts;
-    g.part_units[c] = (int32_t)(((units[c] + parts - 1) / parts + kWarps - 1) / kWarps * kWarps);  // whole rounds of the warps
+    g.part_units[c] = (int32_t)(((n + parts - 1) / parts + kWarps - 1) / kWarps * kWarps);  // whole rounds of the warps
     blocks += (fc::span_rows(g, c) + 8 * nt - 1) / (8 * nt) * parts;
     g.block_end[c] = (int32_t)std::min<int64_t>(blocks, INT32_MAX);
   }
@@ -907,9 +919,50 @@ int map_rows(fc_ctx* ctx, CUtensorMap* map, const void* base, const fc::SpanGeom
   return encode(ctx, map, g.f32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, base, dims, strides, box, CU_TENSOR_MAP_SWIZZLE_128B);
 }
 
+
+// Clusters of n blocks that the device holds at once.
+template <typename T, int D, int NT>
+void ask_clusters(int16_t (&held)[kMaxCluster + 1]) {
+  auto kernel = attention_span_rows_kernel<T, D, NT>;
+  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem) != cudaSuccess ||
+      cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess)
+    return;
+  for (int n = 2; n <= kMaxCluster; ++n) {
+    cudaLaunchAttribute attr;
+    attr.id = cudaLaunchAttributeClusterDimension;
+    attr.val.clusterDim.x = (unsigned)n;
+    attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)n);
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = kSmem;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    int count = 0;
+    if (cudaOccupancyMaxActiveClusters(&count, kernel, &cfg) == cudaSuccess) held[n] = (int16_t)std::min(count, 30000);
+  }
+}
+
 }  // namespace
 
 namespace fc {
+
+void span_rows_setup(fc_ctx* ctx) {
+  auto& h = ctx->span_clusters;
+  for (auto& a : h)
+    for (auto& b : a)
+      for (auto& c : b)
+        for (int16_t& x : c) x = 0;
+  ask_clusters<__nv_bfloat16, 64, 1>(h[0][0][0]);
+  ask_clusters<__nv_bfloat16, 64, 2>(h[0][0][1]);
+  ask_clusters<__nv_bfloat16, 128, 1>(h[0][1][0]);
+  ask_clusters<__nv_bfloat16, 128, 2>(h[0][1][1]);
+  ask_clusters<float, 64, 1>(h[1][0][0]);
+  ask_clusters<float, 64, 2>(h[1][0][1]);
+  ask_clusters<float, 128, 1>(h[1][1][0]);
+  ask_clusters<float, 128, 2>(h[1][1][1]);
+  cudaGetLastError();  // a question that was refused is no error of a call
+}
 
 size_t span_rows_workspace(const fc_ctx* ctx, SpanGeom& g) {
   g.rows_us = split(ctx, g);
@@ -938,7 +991,7 @@ int span_rows_launch(fc_ctx* ctx, cudaStream_t st, const SpanGeom& g, const void
   if (paged && ((rc = map_pages(ctx, &k8, g.pool.k_codes, g)) != FC_OK || (rc = map_pages(ctx, &v8, g.pool.v_codes, g)) != FC_OK)) return rc;
   if (plain && ((rc = map_rows(ctx, &k, K, g, g.k_hs, g.k_rs)) != FC_OK || (rc = map_rows(ctx, &v, V, g, g.v_hs, g.v_rs)) != FC_OK)) return rc;
   const dim3 grid((unsigned)blocks, (unsigned)g.H_kv);
-  constexpr int smem = kWarps * kRing + 1024;
+  constexpr int smem = kSmem;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = grid;
   cfg.blockDim = dim3(kThreads);

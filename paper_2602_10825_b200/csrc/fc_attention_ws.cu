@@ -160,12 +160,6 @@ struct NoSpans {};
 template <Source kSource> struct SpansOf { using type = NoSpans; };
 template <> struct SpansOf<kSpans> { using type = fc::AttnSpans; };
 
-// Where a role stands in the runs of an item, the pieces of its keys that lie together in a store: the next one, and (kSpans) the
-// chunk's keys before it.
-struct Runs {
-  int next = 0, keys = 0;
-};
-
 template <int D, Source kSource>
 __global__ void __launch_bounds__(kThreads, 1)
 attention_ws_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant__ CUtensorMap tmap_k,
@@ -319,53 +313,55 @@ attention_ws_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
     return item;
   };
 
-  // The item's next run: how many tokens it has (0: there is none), its first physical row, and whether it lies in the first of two
-  // stores.  A part of an item's keys (kTwo) may begin and end inside a run.
-  auto next_run = [&](const Item& it, Runs& w, int& prow, bool& first_store) {
+  // An item's keys come in runs, pieces that lie together in a store: the segments, or (kSpans) the two ranges of the first store and
+  // what each of the other two shares with each segment.
+  auto n_runs = [&]() { return kSource == kSpans ? 2 + 2 * g.n_seg : g.n_seg; };
+  // kSpans: the range of run s, and the physical row of its first token
+  auto span_run = [&](const Item& it, int s, int& lo, int& hi) {
     if constexpr (kSource == kSpans) {
-      const int n = 2 + 2 * g.n_seg;
-      while (w.next < n) {
-        const int r = w.next++;
-        int lo, hi, phys;
-        if (r < 2) {
-          lo = phys = spans.lo[r][it.c];
-          hi = spans.hi[r][it.c];
-        } else {
-          const int i = r < 2 + g.n_seg ? 2 : 3, s = r - 2 - (i - 2) * g.n_seg;
-          lo = max(spans.lo[i][it.c], g.seg_log[s]);
-          hi = min(spans.hi[i][it.c], g.seg_log[s + 1]);
-          phys = g.seg_phys[s] + lo - g.seg_log[s];
-        }
-        if (hi <= lo) continue;
-        const int skip = max(it.k_lo - w.keys, 0), tokens = min(hi - lo, it.n_vis - w.keys) - skip;
-        w.keys += hi - lo;
-        if (tokens <= 0) continue;
-        prow = phys + skip;
-        first_store = r < 2;
-        return tokens;
+      if (s < 2) {
+        lo = spans.lo[s][it.c];
+        hi = spans.hi[s][it.c];
+        return lo;
       }
-    } else if constexpr (kTwo) {
-      while (w.next < g.n_seg) {
-        const int s = w.next++, skip = max(it.k_lo - g.seg_log[s], 0);
-        const int tokens = min(g.seg_log[s + 1], it.n_vis) - g.seg_log[s] - skip;
-        if (tokens <= 0) continue;  // before the item's keys, or behind them
-        prow = g.seg_phys[s] + skip;
-        first_store = s < g.n_seg0;
-        return tokens;
-      }
-    } else if (w.next < g.n_seg) {
-      const int s = w.next++;
-      prow = g.seg_phys[s];
-      first_store = false;
-      return min(g.seg_log[s + 1], it.n_vis) - g.seg_log[s];
+      const int i = s < 2 + g.n_seg ? 2 : 3, seg = s - 2 - (i - 2) * g.n_seg;
+      lo = max(spans.lo[i][it.c], g.seg_log[seg]);
+      hi = min(spans.hi[i][it.c], g.seg_log[seg + 1]);
+      return g.seg_phys[seg] + lo - g.seg_log[seg];
+    } else {
+      return 0;
     }
-    return 0;
+  };
+  // Tokens of run s that the item sees (behind the `skip` first ones); none, or a negative number, for a run before
+  // the item's keys (kTwo only) or behind them.  `keys`: the chunk's keys before the run (kSpans; the runs are asked for in turn).
+  auto seg_tokens = [&](const Item& it, int s, int& skip, int& keys) {
+    if constexpr (kSource == kSpans) {
+      int lo, hi;
+      span_run(it, s, lo, hi);
+      if (hi <= lo) return 0;
+      skip = max(it.k_lo - keys, 0);
+      const int tokens = min(hi - lo, it.n_vis - keys) - skip;
+      keys += hi - lo;
+      return tokens;
+    } else {
+      skip = kTwo ? max(it.k_lo - g.seg_log[s], 0) : 0;
+      return min(g.seg_log[s + 1], it.n_vis) - g.seg_log[s] - skip;
+    }
+  };
+  auto first_row = [&](const Item& it, int s) {
+    int lo, hi;
+    return kSource == kSpans ? span_run(it, s, lo, hi) : g.seg_phys[s];
   };
   auto count_tiles = [&](const Item& it) {
-    Runs w;
-    int n = 0, prow, tokens;
-    bool first_store;
-    while ((tokens = next_run(it, w, prow, first_store)) > 0) n += (tokens + kBN - 1) / kBN;
+    int n = 0, skip, keys = 0;
+    for (int s = 0; s < n_runs(); ++s) {
+      const int seg_vis = seg_tokens(it, s, skip, keys);
+      if (seg_vis <= 0) {
+        if (kTwo) continue;
+        break;
+      }
+      n += (seg_vis + kBN - 1) / kBN;
+    }
     return n;
   };
 
@@ -434,14 +430,19 @@ attention_ws_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
           __syncwarp();  // (the V rows of the tile are gathered by warp 11: two warps issue the copies)
         }
       } else {
-      Runs w;
-      int tokens, prow0;
-      bool first_store;
-      while ((tokens = next_run(it, w, prow0, first_store)) > 0) {
-        const CUtensorMap* map_k = kTwo && first_store ? &tmap_k0 : &tmap_k;
-        const CUtensorMap* map_v = kTwo && first_store ? &tmap_v0 : &tmap_v;
-        for (int j0 = 0; j0 < tokens; j0 += kBN, ++kv) {
-          const int st = kv % kStages, ph = (kv / kStages) & 1, prow = prow0 + j0;
+      int keys = 0;
+      for (int s = 0; s < n_runs(); ++s) {
+        int skip;
+        const int seg_vis = seg_tokens(it, s, skip, keys);
+        if (seg_vis <= 0) {
+          if (kTwo) continue;
+          break;
+        }
+        const bool in_first = kTwo && s < (kSource == kSpans ? 2 : g.n_seg0);
+        const CUtensorMap* map_k = in_first ? &tmap_k0 : &tmap_k;
+        const CUtensorMap* map_v = in_first ? &tmap_v0 : &tmap_v;
+        for (int j0 = 0; j0 < seg_vis; j0 += kBN, ++kv) {
+          const int st = kv % kStages, ph = (kv / kStages) & 1, prow = first_row(it, s) + skip + j0;
           warp_wait(smem_u32(&sh->k_empty[st]), ph ^ 1, abort);
           if (lane == 0) {
             mbar_expect_tx(smem_u32(&sh->k_full[st]), kTileBytes);
@@ -546,17 +547,21 @@ attention_ws_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
         umma_commit(b_kempty + 8 * st);
       }
       // the walk over the runs, to know which tiles are ragged (their V stage is patched before PV)
-      Runs w;
-      int prow;
-      bool first_store;
-      int left = next_run(it, w, prow, first_store);
+      int seg = 0, skip, keys = 0, seg_left = n_tiles > 0 ? seg_tokens(it, 0, skip, keys) : 0;
+      if (kTwo && n_tiles > 0)
+        while (seg_left <= 0) seg_left = seg_tokens(it, ++seg, skip, keys);
       for (int j = 0; j < n_tiles; ++j, ++kv, ++uses) {
         const uint32_t st = kv & 1, ph = (kv >> 1) & 1;
         const uint32_t st2 = st ^ 1, ph2 = ((kv + 1) >> 1) & 1;  // the next key tile's stage
         const bool more = j + 1 < n_tiles;
-        const bool ragged = left < kBN;
-        left -= kBN;
-        if (left <= 0 && more) left = next_run(it, w, prow, first_store);
+        const bool ragged = seg_left < kBN;
+        seg_left -= kBN;
+        if (seg_left <= 0 && more) {
+          ++seg;
+          seg_left = seg_tokens(it, seg, skip, keys);
+          if (kSource == kSpans)
+            while (seg_left <= 0) seg_left = seg_tokens(it, ++seg, skip, keys);
+        }
         prep_pv(st, 0);
         if (more) prep_s(st2, 0);
         mbar_wait_bounded(b_vfull + 8 * st, ph, abort);
@@ -601,13 +606,17 @@ attention_ws_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
       const int item = next_item(it_n);
       if (item < 0) break;
       const Item it = decode(item);
-      Runs w;
-      int tokens, prow;
-      bool first_store;
-      while ((tokens = next_run(it, w, prow, first_store)) > 0) {
-        for (int j0 = 0; j0 < tokens; j0 += kBN, ++kv) {
+      int keys = 0;
+      for (int s = 0; s < n_runs(); ++s) {
+        int skip;
+        const int seg_vis = seg_tokens(it, s, skip, keys);
+        if (seg_vis <= 0) {
+          if (kTwo) continue;
+          break;
+        }
+        for (int j0 = 0; j0 < seg_vis; j0 += kBN, ++kv) {
           const int st = kv % kStages, ph = (kv / kStages) & 1;
-          const int cols_valid = min(kBN, tokens - j0);
+          const int cols_valid = min(kBN, seg_vis - j0);
           if constexpr (kGather) {
             // token map: this warp also brings the tile's V rows (lane L rows 4L .. 4L+3, as the copy warp does for K)
             const int32_t* tok = g.tok_index + (int64_t)it.hk * g.tok_hs;
@@ -682,12 +691,16 @@ attention_ws_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
       }
       float m = -INFINITY, l = 0.f;
       int j = 0;
-      Runs w;
-      int tokens, prow;
-      bool first_store;
-      while ((tokens = next_run(it, w, prow, first_store)) > 0) {
-        for (int j0 = 0; j0 < tokens; j0 += kBN, ++kv, ++j, ++uses) {
-          const int cols_valid = min(kBN, tokens - j0);
+      int keys = 0;
+      for (int s = 0; s < n_runs(); ++s) {
+        int skip;
+        const int seg_vis = seg_tokens(it, s, skip, keys);
+        if (seg_vis <= 0) {
+          if (kTwo) continue;
+          break;
+        }
+        for (int j0 = 0; j0 < seg_vis; j0 += kBN, ++kv, ++j, ++uses) {
+          const int cols_valid = min(kBN, seg_vis - j0);
 #pragma unroll
           for (int u = 0; u < 2; ++u, ++sub) {
             const int mine_valid = min(max(cols_valid - u * kHalf, 0), kHalf);

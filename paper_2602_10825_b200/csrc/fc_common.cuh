@@ -12,12 +12,16 @@ struct fc_ctx {
   int sm_count;
   int smem_optin;       // max dynamic shared memory per block (opt-in), bytes
   void* encode_tiled;   // cuTensorMapEncodeTiled, resolved through the runtime
+  // thread block clusters of n blocks of the few-row kernel over spans that the device holds at once (fc_attention_span_rows.cu):
+  // [fp32][d = 128][sixteen rows to a tile][n]; 0 if that could not be asked
+  int16_t span_clusters[2][2][2][17];
 };
 
 namespace fc {
 
 void set_cuda_error(cudaError_t e, const char* where);
 void decide_static_setup(int device);  // fc_decide.cu: address of the built-in scratch of fc_chunk_decide_static
+void span_rows_setup(fc_ctx* ctx);     // fc_attention_span_rows.cu: ctx->span_clusters
 
 inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 inline size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }

@@ -54,6 +54,7 @@ extern "C" int fc_create(fc_ctx** out, int device) {
     return FC_ERR_CUDA;
   }
   fc::decide_static_setup(device);
+  fc::span_rows_setup(ctx);
   *out = ctx;
   return FC_OK;
 }

@@ -26,7 +26,7 @@ def L():
 @pytest.fixture(scope="module")
 def ctx():
     # fc_ctx: device, SM count, shared memory limit, driver entry point
-    buf = C.create_string_buffer(struct.pack("iii4xP", 0, 148, 232448, 0), 64)
+    buf = C.create_string_buffer(struct.pack("iii4xP", 0, 148, 232448, 0), 512)
     return C.cast(buf, C.c_void_p), buf
 
 
