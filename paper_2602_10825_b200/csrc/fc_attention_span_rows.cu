@@ -143,6 +143,7 @@ __device__ __forceinline__ void write_row(T* O, const fc::SpanGeom& g, int c, in
   const float inv = l > 0.f ? 1.f / l : (l == l ? 0.f : l);
   const int h = hk * g.group + v % g.group;
   const int64_t row = g.q_row_off[c] + v / g.group;
+  if (!fc::bounds_ok(row >= 0 && row < g.q_row_off[g.W] && h >= 0 && h < g.H_q, g.status)) return;
   store4(O + h * g.o_hs + row * g.o_rs + d4, make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv));
   if (g.lse && d4 == 0) g.lse[h * g.lse_hs + row] = l > 0.f ? (ref + log2f(l)) * 0.6931471805599453f : (l == l ? -INFINITY : l);
 }

@@ -228,7 +228,7 @@ kv8_append_kernel(const T* __restrict__ K, const T* __restrict__ V, const __grid
 
 struct UnpackGeom {
   fc::Kv8Jobs jobs;
-  int64_t k_hs, k_rs, v_hs, v_rs, table_cs;
+  int64_t k_hs, k_rs, v_hs, v_rs, table_cs, rows;  // rows of a head of the destination
   fc::Kv8View src;
   const int32_t* table;
   uint32_t *status, *clear;
@@ -297,7 +297,7 @@ kv8_unpack_kernel(T* __restrict__ K, T* __restrict__ V, const __grid_constant__ 
 #pragma unroll
   for (int u = 0; u < kUnpackRows; ++u) {
     const int64_t r = r0 + u * R;
-    if (r < job.n) store_values(dst + h * hs + (job.dst_row + r) * rs + kVec * w, word[u], scale[u]);
+    if (r < job.n && fc::bounds_ok(job.dst_row + r < g.rows && w < kRowVecs, g.status)) store_values(dst + h * hs + (job.dst_row + r) * rs + kVec * w, word[u], scale[u]);
   }
   if (bad && g.status) atomicOr(g.status, (uint32_t)FC_DEV_BAD_INDEX);
 }
@@ -331,7 +331,9 @@ int kv8_unpack_launch(cudaStream_t st, const Kv8View& src, int H, int d, const i
   int n = 0;
   for (int i = 0; i < jobs.n; ++i) n = std::max(n, jobs.job[i].n);
   if (n == 0 || (!K_dst && !V_dst)) return FC_OK;
-  UnpackGeom g = {jobs, k_hs, k_rs, v_hs, v_rs, table_cs, src, table, status, clear};
+  int64_t end = 0;
+  for (int i = 0; i < jobs.n; ++i) end = std::max<int64_t>(end, (int64_t)jobs.job[i].dst_row + jobs.job[i].n);
+  UnpackGeom g = {jobs, k_hs, k_rs, v_hs, v_rs, table_cs, end, src, table, status, clear};
   const int rows = kUnpackRows * kUnpackThreads / (d / (dtype == FC_F32 ? 4 : 8));
   const dim3 grid((unsigned)((n + (int64_t)rows - 1) / rows), (unsigned)H, 2u * jobs.n);
 #define FC_UNPACK(T, D) kv8_unpack_kernel<T, D><<<grid, kUnpackThreads, 0, st>>>((T*)K_dst, (T*)V_dst, g)

@@ -5,6 +5,8 @@
 
 namespace fc {
 
+constexpr int kMaxPages = INT32_MAX - 8192;  // counters of pages run past the end by a tile
+
 // A pool as a kernel sees it (K and V share strides).
 struct Kv8View {
   uint8_t *k_codes, *v_codes;
@@ -33,6 +35,7 @@ inline bool grid_disjoint(int64_t n, int64_t a, int64_t m, int64_t b, int64_t wi
 inline int kv8_check(const fc_kv8_pool* p, int H, int d) {
   if (!p || !p->k_codes || !p->v_codes || !p->k_scales || !p->v_scales) return FC_ERR_INVALID_ARG;
   if (p->n_pages <= 0) return FC_ERR_INVALID_ARG;
+  if (p->n_pages > kMaxPages) return FC_ERR_UNSUPPORTED;
   if (page_log2(p->page) < 0) return FC_ERR_UNSUPPORTED;
   if (!aligned16(p->k_codes) || !aligned16(p->v_codes) || ((uintptr_t)p->k_scales | (uintptr_t)p->v_scales) % 4) return FC_ERR_MISALIGNED;
   if (p->code_ps < 0 || p->code_hs < 0 || p->code_ps % 16 || p->code_hs % 16) return FC_ERR_MISALIGNED;

@@ -257,6 +257,7 @@ pages_copy_kernel(const __grid_constant__ CopyGeom g, uint32_t* __restrict__ sta
     const int64_t rest = u >> 1;
     const int h = (int)(rest % g.H);
     const int2 m = g.copies.pair[rest / g.H];
+    if (!fc::bounds_ok((uint32_t)m.x < (uint32_t)g.pool.n_pages && (uint32_t)m.y < (uint32_t)g.pool.n_pages, status)) continue;
     uint8_t* base = (is_v ? g.pool.v_codes : g.pool.k_codes) + h * g.pool.code_hs;
     const uint8_t* from = base + m.x * g.pool.code_ps;
     uint8_t* to = base + m.y * g.pool.code_ps;
@@ -292,7 +293,7 @@ pages_copy_kernel(const __grid_constant__ CopyGeom g, uint32_t* __restrict__ sta
 int ranges_of(const int32_t* ref, int n_pages, const int32_t* table, int64_t table_cs, int W, const int32_t* first, const int32_t* last,
               Ranges& r) {
   if (!first || !last || n_pages <= 0 || W <= 0 || table_cs < 0) return FC_ERR_INVALID_ARG;
-  if (W > FC_MAX_CHUNKS) return FC_ERR_UNSUPPORTED;
+  if (W > FC_MAX_CHUNKS || n_pages > fc::kMaxPages) return FC_ERR_UNSUPPORTED;
   int64_t n = 0;
   for (int c = 0; c < W; ++c) {
     if (first[c] < 0 || last[c] < first[c]) return FC_ERR_INVALID_ARG;
@@ -318,6 +319,7 @@ int check_pool(const fc_kv8_pool* pool, int H, int d) {
 int launch_copies(fc_ctx* ctx, cudaStream_t st, const CopyGeom& g, int64_t most, uint32_t* status) {
   const int64_t units = std::max<int64_t>(most * g.H * 2, g.n_seq > 0 ? 1 : 0);
   const int grid = (int)std::min<int64_t>(units, 8ll * ctx->sm_count);
+  if (grid == 0) return FC_OK;
   FC_CUDA_CHECK(fc::launch_pdl(pages_copy_kernel, dim3(grid), dim3(kCopyThreads), 0, st, g, status));
   FC_LAUNCH_CHECK("pages_copy_kernel");
   return FC_OK;

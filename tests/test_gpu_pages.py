@@ -713,6 +713,28 @@ def test_pages_and_append_are_captured(fc, ctx):
         assert torch.equal(ref, want[0]) and torch.equal(table, want[1])
 
 
+@pytest.mark.parametrize("dtype, impl", IMPLS)
+def test_attention_over_nothing(fc, ctx, dtype, impl):
+    # no pages, no plain rows, nothing seen: zeros, and a log-sum of nothing
+    H, d, rows = 3, 64, 7
+    Q, O, lse = rand((H, rows, d), 1, 1.0, dtype), torch.full((H, rows, d), 9.0, dtype=dtype, device="cuda"), torch.zeros((H, rows), device="cuda")
+    args = ([0, rows], [0])
+    ctx.chunk_attention_kv8(Q, fc.Kv8Pool.empty(1, H, 16, d), i32([[-1]]), [0], None, None, *args, i32([0]), i32([1]), O, lse=lse, impl=impl)
+    assert (O == 0).all() and (lse == -math.inf).all()
+    O.fill_(9.0)
+    K = torch.full((H, 5, d), math.nan, dtype=dtype, device="cuda")
+    ctx.chunk_attention_span(Q, K, K, *args, [0, 5], [0], i32([0]), i32([1]), O, n_sink=3, lse=lse, impl=impl)
+    assert (O == 0).all() and (lse == -math.inf).all()
+
+
+def test_compact_without_tables(fc, ctx):
+    for n in (1, 2, 5):
+        pool, ref = filled_pool(fc, n, 1, 16, 64, 1), i32([0] * (n - 1) + [3])
+        codes, n_used = pool.k_codes.clone(), status_word()
+        ctx.pages_compact(pool, ref, torch.zeros((0, 4), dtype=torch.int32, device="cuda"), n_used=n_used)
+        assert ref.tolist() == [3] + [0] * (n - 1) and int(n_used) == 1 and torch.equal(pool.k_codes[0], codes[n - 1])
+
+
 def test_binding_refusals(fc, ctx):
     H, d, page = 2, 64, 16
     pool = filled_pool(fc, 4, H, page, d, 1)

@@ -45,7 +45,7 @@ def pool(**kw):
 
 
 POOL_REFUSALS = [
-    (dict(k_codes=None), INVALID), (dict(v_scales=None), INVALID), (dict(n_pages=0), INVALID), (dict(page=48), UNSUPPORTED), (dict(page=8), UNSUPPORTED),
+    (dict(k_codes=None), INVALID), (dict(v_scales=None), INVALID), (dict(n_pages=0), INVALID), (dict(n_pages=2 ** 31 - 8000), UNSUPPORTED), (dict(page=48), UNSUPPORTED), (dict(page=8), UNSUPPORTED),
     (dict(k_codes=P + 8), MISALIGNED), (dict(k_scales=P + 2), MISALIGNED), (dict(code_hs=64 * 128 + 8), MISALIGNED), (dict(code_ps=-16), MISALIGNED),
     (dict(scale_hs=-1), INVALID), (dict(code_hs=64 * 128 - 16), INVALID), (dict(code_ps=3 * 64 * 128), INVALID), (dict(scale_ps=3), INVALID),
     (dict(scale_hs=0), INVALID), (dict(code_ps=1 << 41), UNSUPPORTED),
@@ -107,7 +107,7 @@ def ranges(L, ctx, name, *, ref=P, n_pages=100, table=P, cs=9, W=2, first=(0, 3)
 
 @pytest.mark.parametrize("name", ["fc_pages_take", "fc_pages_drop"])
 @pytest.mark.parametrize("kw, want", [
-    (dict(ref=None), INVALID), (dict(table=None), INVALID), (dict(n_pages=0), INVALID), (dict(W=0), INVALID), (dict(W=65), UNSUPPORTED),
+    (dict(ref=None), INVALID), (dict(table=None), INVALID), (dict(n_pages=0), INVALID), (dict(n_pages=2 ** 31 - 8000), UNSUPPORTED), (dict(W=0), INVALID), (dict(W=65), UNSUPPORTED),
     (dict(first=(-1, 0)), INVALID), (dict(first=(3, 3)), INVALID), (dict(last=(2, 10)), INVALID), (dict(cs=-1), INVALID), (dict(first=None), INVALID),
     (dict(last=None), INVALID), (dict(ref=P + 4), MISALIGNED),
     (dict(W=1, first=(0,), last=(2 ** 31 - 1,)), UNSUPPORTED),
