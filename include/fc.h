@@ -616,10 +616,12 @@ int fc_pages_compact(fc_ctx* ctx, void* stream, const fc_kv8_pool* pool, int H, 
  *   cache_len        HOST [W] or NULL (all 0).  kv_visible_len HOST [W]; kv_begin HOST [W] or NULL (all 0: no sliding window); window_first
  *                    HOST [W] or NULL (all 0).  Tokens that no chunk sees need no page.
  *   K, V, seg_*      as in fc_chunk_attention_kv4: the plain tokens; n_seg 0 if there are none.
- * Everything else is as in fc_chunk_attention_kv4: the active list, grouped heads, rows of inactive chunks, how weights are rounded (fp32: not; the
- * tcgen05 kernel: to bf16; few rows: to fp16 over the pages, in units of a 2^-15th of the largest so far or less, and to bf16 over plain rows,
- * the rest taken along where no chunk has more than eight rows times heads of a group).  What lies in tokens that a chunk does not see
- * never reaches its rows, whatever it is.  A NaN in a token that is seen makes what it reaches NaN, and so does an infinity in Q.
+ * Everything else is as in fc_chunk_attention_kv4: the active list, grouped heads, rows of inactive chunks.  Logits, maxima, sums and outputs are kept
+ * in fp32.  Softmax weights are rounded on their way to V: for fp32 tensors by 2^-22 at most; by the tcgen05 kernel to bf16; by the
+ * kernel for few rows to fp16 over pages (2^-11 of a weight, or 2^-32 of the row's largest so far where that is more) and to bf16 over
+ * plain rows, where what that leaves is taken along if no tile has more than eight rows times heads of a group.
+ * What lies in tokens that a chunk does not see never reaches its rows, whatever it is.  A NaN in a token that is seen makes what it reaches NaN, and so
+ * does an infinity in Q.  Head strides of K and V are not 0 where there are several heads.
  * An entry outside [0, n_pages) that is needed sets FC_DEV_BAD_INDEX; K and V of its tokens count as zeros.
  * Deterministic.  Workspace: fc_chunk_attention_kv8_workspace_bytes() of the same arguments (0 for arguments that the call
  * refuses). */

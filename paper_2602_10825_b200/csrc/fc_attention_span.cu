@@ -145,9 +145,9 @@ bool plan_tiles(const fc_ctx* ctx, const fc::SpanGeom& g, TilePlan& p) {
   float last = 0.f;
   const int rest = (int)(items % ctx->sm_count);
   if (rest > 0) fc::split_parts(rest, ctx->sm_count, most_tiles, g.d, p.split.slots, &last);
-  // 9 us for the launches of the path, 1.8 us a key tile, the unpacking at 6.4 TB/s
+  // 12 us for the launches of the path, 1.8 us a key tile, the unpacking at 6.4 TB/s
   const double whole = items > 0 ? (double)tiles / items : 0;
-  p.us = 9 + 1.8 * ((double)(items / ctx->sm_count) * whole + last) + 2.0 * g.H_kv * p.rows * g.d * 3 / 6.4e6;
+  p.us = 12 + 1.8 * ((double)(items / ctx->sm_count) * whole + last) + 2.0 * g.H_kv * p.rows * g.d * 3 / 6.4e6;
   const size_t bytes = (size_t)g.H_kv * p.rows * g.d * 2, parts = (size_t)p.split.slots * 256;
   p.k = fc::attention_tc_workspace_bytes();
   p.v = p.k + fc::align_up(bytes, 256);
@@ -220,6 +220,7 @@ int attend(fc_ctx* ctx, void* stream, const fc_attn_desc* desc, const void* Q, c
     }
   }
   if (lse && lse_hs <= 0) return FC_ERR_INVALID_ARG;
+  if (!rows) g.n_seg = 0;
   g.q_hs = desc->q_hs; g.q_rs = desc->q_rs; g.k_hs = desc->k_hs; g.k_rs = desc->k_rs;
   g.v_hs = desc->v_hs; g.v_rs = desc->v_rs; g.o_hs = desc->o_hs; g.o_rs = desc->o_rs;
   g.kv_rows = std::min<int64_t>(desc->kv_rows, INT32_MAX);

@@ -1,8 +1,8 @@
 // Attention of few query rows over [8-bit pages | plain rows], each chunk over its first tokens and its sliding window: one pass over the
 // keys, cut into parts that a second kernel joins; also the path of fp32 tensors whatever their rows.
 //
-// Bound by the bytes of the keys.  A warp takes 16 keys at a step from its own rings in shared memory, one for K and one for V, which the copy
-// engine fills (a box of 16 rows is one instruction of one lane, and lies swizzled so that the reads below meet no bank twice),
+// Bound by the bytes of the keys.  A warp takes 32 keys at a step (16 over plain rows) from its own ring in shared memory, which the copy
+// engine fills (a box of the step's rows is one instruction of one lane, and lies swizzled so that the reads below meet no bank twice),
 // and feeds them to mma.sync from registers:
 //   S^T = K Q^T   m16n8k16, keys as rows, up to 8 NT query rows as columns.  The order of the head's elements along the
 //                 contraction is free as long as K and Q agree: lane (n, q) takes, of keys n and n + 8, the bytes 32 q .. 32 q + 31 of
@@ -14,8 +14,11 @@
 // Pages.  A code is exactly an fp16 number, and one instruction makes two; so the products are of fp16.  Q, which is a
 // bf16 number of any size, is brought into fp16 by a power of two of its row that puts the row's largest element at 2^14: all of its bits are
 // kept down to 2^-29 of that.  The keys' scale goes into the logits, the values' scale multiplies a step's sum before it is
-// added to O, which is in fp32 (two fp32 instructions a step and tile of 16 dims).  Weights are taken 2^7 times larger than
-// their reference asks for, so that fp16's smallest step, 2^-24, is 2^-31 of the largest weight.
+// added to O, which is in fp32.  Weights are taken 2^7 times larger than their reference asks for, so that fp16's smallest step,
+// 2^-24, is 2^-31 of the largest weight.  A step is about 215 instructions for each 16 keys of one to eight rows, which is what a block alone on
+// its SM is bound by (0.45 us for its four warps' 64 keys; with 16 keys a step, and a barrier, a look-up, a vote and a copy for each, 0.62); from
+// one and a half blocks an SM on it is the bandwidth: one token over 28080 tokens of 24 heads 34.0 us, the same without the arithmetic 32, the
+// bytes' own time 26.3.
 // Plain rows go through the products of their own type (bf16, or for fp32 the six largest products of three bf16 parts each).
 // fp32 over pages: two fp16 parts of Q, and of the weights, leave out 2^-23 of a number at most.
 // The maximum is lazy (it moves when a logit passes it by 2^8), so that the usual step has no shuffles and no rescaling.
@@ -32,14 +35,17 @@ namespace {
 using namespace fc::sm100;
 
 constexpr int kWarps = 4, kThreads = 32 * kWarps;
-constexpr int kStep = 16;            // keys per warp and step
+constexpr int kStep = 16;            // keys per warp and step over plain rows, and of a matrix instruction
+constexpr int kPagedStep = 32;       // over pages
+constexpr int kTable = 64 * 32;      // bytes of what a warp knows of its next steps over pages
 constexpr int kRing = 16 * 1024;     // bytes of a warp's two rings
 constexpr int kMaxCluster = 16;      // blocks of a cluster
-constexpr int kSmem = kWarps * kRing + 1024;  // of a block, the rings on a 1024-byte boundary
+constexpr int kSmem = kWarps * (kRing + kTable) + 1024;  // of a block, the rings on a 1024-byte boundary
 constexpr float kSlack = 8.f;        // log2 units by which a logit may pass the maximum before that moves
 constexpr float kLift = 7.f;         // weights are 2^kLift at the maximum
 constexpr int blocks_per_sm(int nt) { return nt == 1 ? 3 : 2; }
-template <typename T> constexpr int kPlainCost = sizeof(T) == 4 ? 3 : 2;  // cost of a step over plain rows, in steps over pages
+constexpr int kPagedCost = 2;        // cost of a step over pages, and over plain rows
+template <typename T> constexpr int kPlainCost = sizeof(T) == 4 ? 3 : 2;
 
 template <typename T> constexpr int kParts = sizeof(T) == 4 ? 3 : 1;       // bf16 parts of Q, K and V over plain rows
 template <typename T> constexpr int kHalves = sizeof(T) == 4 ? 2 : 1;      // fp16 parts of Q and of the weights over pages
@@ -47,7 +53,7 @@ template <typename T> constexpr int kHalves = sizeof(T) == 4 ? 2 : 1;      // fp
 template <typename T, int NT> constexpr int kWeightParts = sizeof(T) == 4 ? 3 : (NT == 1 ? 2 : 1);
 
 template <typename T, int D> struct Ring {
-  static constexpr int kPaged = kStep * D, kPlain = kStep * D * (int)sizeof(T);  // bytes of one tensor's step
+  static constexpr int kPaged = kPagedStep * D, kPlain = kStep * D * (int)sizeof(T);  // bytes of one tensor's step
   static constexpr int kPagedStages = kRing / 2 / kPaged, kPlainStages = kRing / 2 / kPlain;
   static constexpr int kAtoms = D * (int)sizeof(T) / 128;  // boxes of 128 bytes x 16 rows of a plain step
   static_assert(kPlainStages >= 1 && kPagedStages <= 8, "stages");
@@ -69,28 +75,37 @@ template <int D, int NT> struct State {
   float l[NT][2], ref[NT][2], move_at[NT][2];
 };
 
-// Logits (log2 units) to weights, in place.  kMask: keys lo .. hi - 1 of the step count.
-template <int D, int NT, bool kMask>
-__device__ __forceinline__ void weigh_logits(State<D, NT>& st, float (&s)[NT][4], int lane, int lo, int hi) {
+// Logits (log2 units) of N times 16 keys to weights, in place.  kMask: keys lo .. hi - 1 of them count.
+template <int D, int NT, bool kMask, int N>
+__device__ __forceinline__ void weigh_logits(State<D, NT>& st, float (&s)[N][NT][4], int lane, int lo, int hi) {
   bool move = false;
 #pragma unroll
   for (int t = 0; t < NT; ++t) {
     if (kMask) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int key = (lane >> 2) + (i >= 2 ? 8 : 0);
-        if (key < lo || key >= hi) s[t][i] = -INFINITY;
-      }
+      for (int k = 0; k < N; ++k)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int key = 16 * k + (lane >> 2) + (i >= 2 ? 8 : 0);
+          if (key < lo || key >= hi) s[k][t][i] = -INFINITY;
+        }
     }
-    move |= fmaxf(s[t][0], s[t][2]) > st.move_at[t][0];
-    move |= fmaxf(s[t][1], s[t][3]) > st.move_at[t][1];
+#pragma unroll
+    for (int r = 0; r < 2; ++r) {
+      float x = fmaxf(s[0][t][r], s[0][t][2 + r]);
+#pragma unroll
+      for (int k = 1; k < N; ++k) x = max3(x, s[k][t][r], s[k][t][2 + r]);
+      move |= x > st.move_at[t][r];
+    }
   }
   if (__any_sync(0xffffffffu, move)) {
 #pragma unroll
     for (int t = 0; t < NT; ++t)
 #pragma unroll
       for (int r = 0; r < 2; ++r) {
-        float x = fmaxf(s[t][r], s[t][2 + r]);
+        float x = fmaxf(s[0][t][r], s[0][t][2 + r]);
+#pragma unroll
+        for (int k = 1; k < N; ++k) x = max3(x, s[k][t][r], s[k][t][2 + r]);
         x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 4));
         x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 8));
         x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 16));
@@ -109,12 +124,14 @@ __device__ __forceinline__ void weigh_logits(State<D, NT>& st, float (&s)[NT][4]
       }
   }
 #pragma unroll
-  for (int t = 0; t < NT; ++t) {
+  for (int t = 0; t < NT; ++t)
 #pragma unroll
-    for (int i = 0; i < 4; ++i) s[t][i] = ex2(s[t][i] - st.ref[t][i & 1]);
-    st.l[t][0] += s[t][0] + s[t][2];
-    st.l[t][1] += s[t][1] + s[t][3];
-  }
+    for (int k = 0; k < N; ++k) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) s[k][t][i] = ex2(s[k][t][i] - st.ref[t][i & 1]);
+      st.l[t][0] += s[k][t][0] + s[k][t][2];
+      st.l[t][1] += s[k][t][1] + s[k][t][3];
+    }
 }
 
 __device__ __forceinline__ void cluster_barrier() {
@@ -148,12 +165,14 @@ __device__ __forceinline__ void write_row(T* O, const fc::SpanGeom& g, int c, in
   if (g.lse && d4 == 0) g.lse[h * g.lse_hs + row] = l > 0.f ? (ref + log2f(l)) * 0.6931471805599453f : (l == l ? -INFINITY : l);
 }
 
-// What a lane knows of one of the next 32 steps of its warp over pages: the page (-1: none), the first of its rows, which of the sixteen are
-// seen, and the scales of K and V.
-struct PagedStep {
-  int page, row, lo, hi;
-  float ks, vs;
+// What a warp knows of one of its next steps over pages: the pages of its two halves (the same one, but for pages of 16 tokens; -1: none is needed, or
+// the entry names none); the first of its rows, and which of the 32 are seen, as row | lo << 8 | hi << 16, negative unless all are and
+// one page has them; and the scales of K and V of the halves.
+struct __align__(16) PagedStep {
+  int page[2], place, pad;
+  float ks[2], vs[2];
 };
+static_assert(sizeof(PagedStep) * 64 == kTable, "two groups of 32 steps");
 
 // The steps over plain rows, numbered run by run: a run is what a span and a segment share.
 struct Walk {
@@ -204,22 +223,27 @@ attention_span_rows_kernel(const __grid_constant__ CUtensorMap map_k8, const __g
   if (lane < 4 * kBars) mbar_init(smem_u32(&bars[warp][0][0][0] + lane), 1);
   if (tid == 0) {
     abort_s = 0;
-    tma_prefetch_desc(&map_k8);
-    tma_prefetch_desc(&map_v8);
-    tma_prefetch_desc(&map_k);
-    tma_prefetch_desc(&map_v);
+    if (g.pool.n_pages > 0) {
+      tma_prefetch_desc(&map_k8);
+      tma_prefetch_desc(&map_v8);
+    }
+    if (g.n_seg > 0) {
+      tma_prefetch_desc(&map_k);
+      tma_prefetch_desc(&map_v);
+    }
   }
   mbar_fence_init();
   __syncthreads();
 
-  // This part's steps: the axis has a unit for each step over pages, then kPlainCost for each over plain rows.
+  // This part's steps: the axis has kPagedCost units for each step over pages, then kPlainCost for each over plain rows.
   const int log2 = g.pool.page_log2;
-  auto steps_of = [&](int i) { return g.hi[i][c] > g.lo[i][c] ? (g.hi[i][c] + kStep - 1) / kStep - g.lo[i][c] / kStep : 0; };
+  auto steps_of = [&](int i) { return g.hi[i][c] > g.lo[i][c] ? (g.hi[i][c] + kPagedStep - 1) / kPagedStep - g.lo[i][c] / kPagedStep : 0; };
   const int n_first = steps_of(0), n_paged = n_first + steps_of(1);
   const int64_t x0 = (int64_t)part * g.part_units[c], x1 = x0 + g.part_units[c];
-  const int p0 = (int)min(x0, (int64_t)n_paged), p1 = (int)min(x1, (int64_t)n_paged);
+  auto paged_at = [&](int64_t x) { return (int)min((x + kPagedCost - 1) / kPagedCost, (int64_t)n_paged); };
+  const int p0 = paged_at(x0), p1 = paged_at(x1);
   const bool last_part = part == n_parts - 1;  // takes what there is
-  auto plain_at = [&](int64_t x) { return (int)(max(x - n_paged, (int64_t)0) + kPlainCost<T> - 1) / kPlainCost<T>; };
+  auto plain_at = [&](int64_t x) { return (int)((max(x - (int64_t)kPagedCost * n_paged, (int64_t)0) + kPlainCost<T> - 1) / kPlainCost<T>); };
   const int w0 = plain_at(x0), w1 = last_part ? INT_MAX - 64 : plain_at(x1);
 
   State<D, NT> st;
@@ -249,39 +273,73 @@ attention_span_rows_kernel(const __grid_constant__ CUtensorMap map_k8, const __g
   const int m = max(0, (p1 - p0 - warp + kWarps - 1) / kWarps);  // this warp's steps: p0 + warp, + kWarps, ...
   constexpr int kPagedStages = R::kPagedStages;
   bool bad = false;  // an entry that names no page
-  auto look_up = [&](int i) {
-    PagedStep x = {-1, 0, 0, kStep, 0.f, 0.f};
+  auto look_up = [&](int i) {  // all but the scales
+    PagedStep x = {{-1, -1}, kPagedStep << 16, 0, {0.f, 0.f}, {0.f, 0.f}};
     if (i < m) {
       const int s = p0 + warp + i * kWarps, k = s < n_first ? 0 : 1;
-      const int tok = (g.lo[k][c] / kStep + (k ? s - n_first : s)) * kStep;
-      x.row = tok & ((1 << log2) - 1);
-      x.lo = max(g.lo[k][c] - tok, 0);
-      x.hi = min(g.hi[k][c] - tok, kStep);
-      x.page = __ldg(g.table + c * g.table_cs + (tok >> log2));
-      if (x.page >= 0 && x.page < g.pool.n_pages) {
-        x.ks = __ldg(g.pool.k_scales + x.page * g.pool.scale_ps + hk * g.pool.scale_hs);
-        x.vs = __ldg(g.pool.v_scales + x.page * g.pool.scale_ps + hk * g.pool.scale_hs);
-      } else {
-        x.page = -1;
-        bad = true;
+      const int tok = (g.lo[k][c] / kPagedStep + (k ? s - n_first : s)) * kPagedStep;
+      const int lo = max(g.lo[k][c] - tok, 0), hi = min(g.hi[k][c] - tok, kPagedStep);
+      bool part = lo > 0 || hi < kPagedStep || log2 == 4;
+      const int32_t* entry = g.table + c * g.table_cs + (tok >> log2);
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        if (e == 1 && log2 > 4) {
+          x.page[1] = x.page[0];
+        } else if (log2 > 4 || (lo < 16 * (e + 1) && hi > 16 * e)) {
+          x.page[e] = __ldg(entry + e);
+          if (x.page[e] < 0 || x.page[e] >= g.pool.n_pages) {
+            x.page[e] = -1;
+            bad = part = true;
+          }
+        }
       }
+      x.place = (tok & ((1 << log2) - 1)) | lo << 8 | hi << 16 | (part ? INT_MIN : 0);
     }
     return x;
   };
-  // Lane L looks up steps L, 32 + L, ..., and sends for them when their turn comes.
-  PagedStep cur = look_up(lane), next = look_up(32 + lane);
+  auto look_up_scales = [&](PagedStep& x) {
+#pragma unroll
+    for (int e = 0; e < 2; ++e)
+      if (x.page[e] >= 0) {
+        x.ks[e] = __ldg(g.pool.k_scales + x.page[e] * g.pool.scale_ps + hk * g.pool.scale_hs);
+        x.vs[e] = __ldg(g.pool.v_scales + x.page[e] * g.pool.scale_ps + hk * g.pool.scale_hs);
+      }
+  };
   const uint32_t bar_s = bar(0, 0, 0);
-  auto send_paged = [&](int page, int row, int stage) {
+  auto send_paged = [&](int page0, int page1, int row, int stage) {
     const uint32_t b = bar_s + 8 * stage, dst = ring_s + stage * (2 * R::kPaged);
-    if (page < 0) {  // nothing to bring: its keys are zeros
+    if (page0 < 0 && page1 < 0) {  // nothing to bring
       mbar_arrive(b);
-    } else {
+    } else if (log2 > 4) {
       mbar_expect_tx(b, 2 * R::kPaged);
-      tma_load_4d(dst, &map_k8, b, 0, row, hk, page);
-      tma_load_4d(dst + R::kPaged, &map_v8, b, 0, row, hk, page);
+      tma_load_4d(dst, &map_k8, b, 0, row, hk, page0);
+      tma_load_4d(dst + R::kPaged, &map_v8, b, 0, row, hk, page0);
+    } else {
+      mbar_expect_tx(b, (page0 >= 0 && page1 >= 0 ? 2 : 1) * R::kPaged);
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const int page = e ? page1 : page0;
+        if (page < 0) continue;
+        tma_load_4d(dst + e * (16 * D), &map_k8, b, 0, 0, hk, page);
+        tma_load_4d(dst + R::kPaged + e * (16 * D), &map_v8, b, 0, 0, hk, page);
+      }
     }
   };
-  if (lane < min(m, kPagedStages)) send_paged(cur.page, cur.row, lane);
+  // Lane L looks up steps L, 32 + L, ...: two groups of 32 are in the table.  The first steps are sent for before the scales are here.
+  PagedStep* const table = reinterpret_cast<PagedStep*>(smem + kWarps * kRing + warp * kTable);
+  const uint32_t table_s = smem_u32(table);
+  if (m > 0) {
+    PagedStep x = look_up(lane);
+    if (lane < min(m, kPagedStages)) send_paged(x.page[0], x.page[1], x.place & 255, lane);
+    look_up_scales(x);
+    table[lane] = x;
+    if (m > 32) {
+      x = look_up(32 + lane);
+      look_up_scales(x);
+      table[32 + lane] = x;
+    }
+    __syncwarp();
+  }
   // everything up to here asks only what the host knows; the list is on the device
   if (!fc::span_chunk_active(g, c)) {
     for (int i = 0; i < min(m, kPagedStages); ++i) mbar_wait_bounded(bar_s + 8 * i, 0, abort);  // what was sent for lands before its memory is given back
@@ -340,123 +398,134 @@ attention_span_rows_kernel(const __grid_constant__ CUtensorMap map_k8, const __g
     };
     const uint32_t k_at = ring_s + ka, va[2] = {ring_s + R::kPaged + v_at(2 * q), ring_s + R::kPaged + v_at(2 * q + 1)};
 
-    // A step in two halves: the products of the keys at `off` of the ring with Q, and what follows from them.
-    auto products = [&](uint32_t off, float (&s)[NT][4], float (&rest)[NT][4]) {
-      uint32_t k0[D / 16], k1[D / 16];
+    // A step: the products of its keys with Q, the weights, and O.  kPart: keys lo .. hi - 1 count, and the halves have pages and scales of
+    // their own.
+    auto step = [&](uint32_t off, float4 scales, int lo, int hi, bool none0, bool none1, auto parted) {
+      constexpr bool kPart = decltype(parted)::value;
+      float s[2][NT][4];
 #pragma unroll
-      for (int h = 0; h < D / 64; ++h) {
-        const uint32_t at = (k_at ^ (h << 4)) + off;
-        const uint4 a = lds16(at), b = lds16(at + 8 * D);
-        k0[4 * h] = a.x; k0[4 * h + 1] = a.y; k0[4 * h + 2] = a.z; k0[4 * h + 3] = a.w;
-        k1[4 * h] = b.x; k1[4 * h + 1] = b.y; k1[4 * h + 2] = b.z; k1[4 * h + 3] = b.w;
+      for (int e = 0; e < 2; ++e) {
+        uint32_t k0[D / 16], k1[D / 16];
+#pragma unroll
+        for (int h = 0; h < D / 64; ++h) {
+          const uint32_t at = (k_at ^ (h << 4)) + off + e * (16 * D);
+          const uint4 a = lds16(at), b = lds16(at + 8 * D);
+          k0[4 * h] = a.x; k0[4 * h + 1] = a.y; k0[4 * h + 2] = a.z; k0[4 * h + 3] = a.w;
+          k1[4 * h] = b.x; k1[4 * h + 1] = b.y; k1[4 * h + 2] = b.z; k1[4 * h + 3] = b.w;
+        }
+        float rest[NT][4];
+#pragma unroll
+        for (int w = 0; w < D / 16; ++w) {
+          const uint32_t a0 = fc::e4m3_lo2(k0[w]), a1 = fc::e4m3_lo2(k1[w]), a2 = fc::e4m3_hi2(k0[w]), a3 = fc::e4m3_hi2(k1[w]);
+#pragma unroll
+          for (int t = 0; t < NT; ++t) {
+            auto add = [&](float (&d)[4], const uint32_t (&b)[D / 8]) {
+              if (w == 0) mma_f16_first(d, a0, a1, a2, a3, b[0], b[1]);
+              else mma_f16(d, a0, a1, a2, a3, b[2 * w], b[2 * w + 1]);
+            };
+            add(s[e][t], qb[0][t]);
+            if constexpr (kHalves<T> == 2) add(rest[t], qb[1][t]);
+          }
+        }
+        const float ks = kPart && e == 1 ? scales.y : scales.x;
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            s[e][t][k] = (kHalves<T> == 2 ? s[e][t][k] + rest[t][k] : s[e][t][k]) * (qs[t][k & 1] * ks);
+            if (kPart && (e ? none1 : none0)) s[e][t][k] = 0.f;
+          }
       }
+      weigh_logits<D, NT, kPart, 2>(st, s, lane, lo, hi);
+      uint32_t pa[2][kHalves<T>][NT][2];
 #pragma unroll
-      for (int w = 0; w < D / 16; ++w) {
-        const uint32_t a0 = fc::e4m3_lo2(k0[w]), a1 = fc::e4m3_lo2(k1[w]), a2 = fc::e4m3_hi2(k0[w]), a3 = fc::e4m3_hi2(k1[w]);
+      for (int e = 0; e < 2; ++e)
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
-          auto add = [&](float (&d)[4], const uint32_t (&b)[D / 8]) {
-            if (w == 0) mma_f16_first(d, a0, a1, a2, a3, b[0], b[1]);
-            else mma_f16(d, a0, a1, a2, a3, b[2 * w], b[2 * w + 1]);
-          };
-          add(s[t], qb[0][t]);
-          if constexpr (kHalves<T> == 2) add(rest[t], qb[1][t]);
-        }
-      }
-    };
-    auto finish = [&](uint32_t off, float (&s)[NT][4], const float (&rest)[NT][4], float ks, float vs, int lo, int hi, bool no_page, auto masked) {
-      constexpr bool kMask = decltype(masked)::value;
-#pragma unroll
-      for (int t = 0; t < NT; ++t)
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          s[t][k] = (kHalves<T> == 2 ? s[t][k] + rest[t][k] : s[t][k]) * (qs[t][k & 1] * ks);
-          if (kMask && no_page) s[t][k] = 0.f;
-        }
-      weigh_logits<D, NT, kMask>(st, s, lane, lo, hi);
-      uint32_t pa[kHalves<T>][NT][2];
-#pragma unroll
-      for (int t = 0; t < NT; ++t) {
-        const uint32_t a = cvt_f16x2(s[t][0], s[t][1]), b = cvt_f16x2(s[t][2], s[t][3]);
-        pa[0][t][0] = transpose8x8(a);
-        pa[0][t][1] = transpose8x8(b);
-        if constexpr (kHalves<T> == 2) {
-          pa[1][t][0] = transpose8x8(cvt_f16x2(s[t][0] - fc::half_lo(a), s[t][1] - fc::half_hi(a)));
-          pa[1][t][1] = transpose8x8(cvt_f16x2(s[t][2] - fc::half_lo(b), s[t][3] - fc::half_hi(b)));
-        }
-      }
-      uint2 v[D / 64][4];
-#pragma unroll
-      for (int j = 0; j < D / 64; ++j)
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          v[j][k] = lds8((va[k & 1] ^ (j << 6)) + off + (k >> 1) * (8 * D));
-          if (kMask) {
-            const int key = 2 * q + (k & 1) + 8 * (k >> 1);
-            if (no_page || key < lo || key >= hi) v[j][k] = make_uint2(0u, 0u);  // whatever it is: 0 x NaN is NaN
+          const uint32_t a = cvt_f16x2(s[e][t][0], s[e][t][1]), b = cvt_f16x2(s[e][t][2], s[e][t][3]);
+          pa[e][0][t][0] = transpose8x8(a);
+          pa[e][0][t][1] = transpose8x8(b);
+          if constexpr (kHalves<T> == 2) {
+            pa[e][1][t][0] = transpose8x8(cvt_f16x2(s[e][t][0] - fc::half_lo(a), s[e][t][1] - fc::half_hi(a)));
+            pa[e][1][t][1] = transpose8x8(cvt_f16x2(s[e][t][2] - fc::half_lo(b), s[e][t][3] - fc::half_hi(b)));
           }
         }
 #pragma unroll
-      for (int j = 0; j < D / 64; ++j)
+      for (int j = 0; j < D / 64; ++j) {
+        uint2 v[2][4];
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const uint32_t y[4] = {h ? v[j][0].y : v[j][0].x, h ? v[j][1].y : v[j][1].x, h ? v[j][2].y : v[j][2].x, h ? v[j][3].y : v[j][3].x};
+        for (int e = 0; e < 2; ++e)
 #pragma unroll
-          for (int k = 0; k < 2; ++k) {  // dims 2 k and 2 k + 1 of the four that were read
-            const uint32_t ab = prmt(y[0], y[1], k ? 0x7362 : 0x5140), cd = prmt(y[2], y[3], k ? 0x7362 : 0x5140);
-            const uint32_t a0 = fc::e4m3_lo2(ab), a1 = fc::e4m3_hi2(ab), a2 = fc::e4m3_lo2(cd), a3 = fc::e4m3_hi2(cd);
-#pragma unroll
-            for (int t = 0; t < NT; ++t) {
-              float x[4];
-              mma_f16_first(x, a0, a1, a2, a3, pa[kHalves<T> - 1][t][0], pa[kHalves<T> - 1][t][1]);
-              if constexpr (kHalves<T> == 2) mma_f16(x, a0, a1, a2, a3, pa[0][t][0], pa[0][t][1]);
-#pragma unroll
-              for (int e = 0; e < 4; ++e) st.o[t][4 * j + 2 * h + k][e] = fmaf(vs, x[e], st.o[t][4 * j + 2 * h + k][e]);
+          for (int k = 0; k < 4; ++k) {
+            v[e][k] = lds8((va[k & 1] ^ (j << 6)) + off + e * (16 * D) + (k >> 1) * (8 * D));
+            if (kPart) {
+              const int key = 16 * e + 2 * q + (k & 1) + 8 * (k >> 1);
+              if ((e ? none1 : none0) || key < lo || key >= hi) v[e][k] = make_uint2(0u, 0u);  // whatever it is: 0 x NaN is NaN
             }
           }
-        }
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int k = 0; k < 2; ++k) {  // dims 2 k and 2 k + 1 of the four that were read
+            uint32_t a[2][4];
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+              const uint32_t y[4] = {h ? v[e][0].y : v[e][0].x, h ? v[e][1].y : v[e][1].x, h ? v[e][2].y : v[e][2].x, h ? v[e][3].y : v[e][3].x};
+              const uint32_t ab = prmt(y[0], y[1], k ? 0x7362 : 0x5140), cd = prmt(y[2], y[3], k ? 0x7362 : 0x5140);
+              a[e][0] = fc::e4m3_lo2(ab); a[e][1] = fc::e4m3_hi2(ab); a[e][2] = fc::e4m3_lo2(cd); a[e][3] = fc::e4m3_hi2(cd);
+            }
+#pragma unroll
+            for (int t = 0; t < NT; ++t) {
+              float(&o)[4] = st.o[t][4 * j + 2 * h + k];
+              float x[4];
+#pragma unroll
+              for (int e = 0; e < 2; ++e) {
+#pragma unroll
+                for (int w = kHalves<T> - 1; w >= 0; --w) {
+                  if (w == kHalves<T> - 1 && (kPart || e == 0)) mma_f16_first(x, a[e][0], a[e][1], a[e][2], a[e][3], pa[e][w][t][0], pa[e][w][t][1]);
+                  else mma_f16(x, a[e][0], a[e][1], a[e][2], a[e][3], pa[e][w][t][0], pa[e][w][t][1]);
+                }
+                if (kPart || e == 1) {
+                  const float vs = kPart && e == 0 ? scales.z : scales.w;
+#pragma unroll
+                  for (int i = 0; i < 4; ++i) o[i] = fmaf(vs, x[i], o[i]);
+                }
+              }
+            }
+          }
+      }
     };
-    // The products of one step are worked out before the other half of the step before, so that the two steps' chains of
-    // instructions fill each other's gaps.  (Behind the last step they are of whatever the ring holds, and not used.)
     int stage = 0;
     uint32_t parity = 0;
-    float s[NT][4], rest[NT][4], s_next[NT][4], rest_next[NT][4];
-    mbar_wait_bounded(bar_s, 0, abort);
-    __syncwarp();
-    products(0, s, rest);
+    PagedStep pending;
     for (int i = 0; i < m; ++i) {
-      const int at = i & 31;
-      if (at == 0 && i > 0) {
-        cur = next;
-        next = look_up(i + 32 + lane);
-      }
-      const float ks = __shfl_sync(0xffffffffu, cur.ks, at), vs = __shfl_sync(0xffffffffu, cur.vs, at);
-      const bool part = __shfl_sync(0xffffffffu, cur.page < 0 || cur.hi - cur.lo < kStep, at);
-      const int stage1 = stage + 1 == kStages ? 0 : stage + 1;
-      const uint32_t parity1 = stage1 == 0 ? parity ^ 1 : parity;
-      const uint32_t off = stage * (2 * R::kPaged), off1 = stage1 * (2 * R::kPaged);
-      if (i + 1 < m) mbar_wait_bounded(bar_s + 8 * stage1, parity1, abort);
-      __syncwarp();
-      if (!part) {
-        products(off1, s_next, rest_next);
-        finish(off, s, rest, ks, vs, 0, kStep, false, std::false_type());
-      } else {
-        const int lo = __shfl_sync(0xffffffffu, cur.lo, at), hi = __shfl_sync(0xffffffffu, cur.hi, at), page = __shfl_sync(0xffffffffu, cur.page, at);
-        products(off1, s_next, rest_next);
-        finish(off, s, rest, ks, vs, lo, hi, page < 0, std::true_type());
-      }
-#pragma unroll
-      for (int t = 0; t < NT; ++t)
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          s[t][k] = s_next[t][k];
-          if constexpr (kHalves<T> == 2) rest[t][k] = rest_next[t][k];
+      if (i >= 32 && (i & 15) == 0) {  // the group after this one: looked up as this one begins, in the table halfway through it
+        if ((i & 16) == 0) {
+          pending = look_up(i + 32 + lane);
+          look_up_scales(pending);
+        } else {
+          table[((i & ~31) + 32 + lane) & 63] = pending;
         }
+        __syncwarp();
+      }
+      const uint32_t entry = table_s + (i & 63) * (int)sizeof(PagedStep), off = stage * (2 * R::kPaged);
+      const uint4 sc = lds16(entry + 16);
+      const float4 scales = make_float4(__uint_as_float(sc.x), __uint_as_float(sc.y), __uint_as_float(sc.z), __uint_as_float(sc.w));
+      const int place = (int)lds4(entry + 8);
+      mbar_wait_bounded(bar_s + 8 * stage, parity, abort);
+      __syncwarp();
+      if (place >= 0) {
+        step(off, scales, 0, kPagedStep, false, false, std::false_type());
+      } else {
+        const uint2 pages = lds8(entry);
+        step(off, scales, place >> 8 & 255, place >> 16 & 255, (int)pages.x < 0, (int)pages.y < 0, std::true_type());
+      }
       __syncwarp();  // the step's place has been read by every lane: another step is sent for
-      const int ahead = (at + kStages) & 31;
-      if (lane == ahead && i + kStages < m) send_paged(at + kStages < 32 ? cur.page : next.page, at + kStages < 32 ? cur.row : next.row, stage);
-      stage = stage1;
-      parity = parity1;
+      if (i + kStages < m && elected()) {
+        const uint4 x = lds16(table_s + ((i + kStages) & 63) * (int)sizeof(PagedStep));
+        send_paged((int)x.x, (int)x.y, (int)x.z & 255, stage);
+      }
+      if (++stage == kStages) stage = 0, parity ^= 1;
     }
   }
 
@@ -512,7 +581,8 @@ attention_span_rows_kernel(const __grid_constant__ CUtensorMap map_k8, const __g
       mbar_wait_bounded(bar(1, 0, stage), parity, abort);
       __syncwarp();
       const uint32_t kp = ring_s + stage * R::kPlain;
-      float s[NT][4] = {}, rest[NT][4] = {};
+      float s1[1][NT][4] = {}, rest[NT][4] = {};
+      auto& s = s1[0];
       auto products = [&](const auto& k, int at) {  // K as NK parts of operand registers; `at`: first register of Q
         constexpr int NK = kParts<T>;
 #pragma unroll
@@ -549,8 +619,8 @@ attention_span_rows_kernel(const __grid_constant__ CUtensorMap map_k8, const __g
       for (int t = 0; t < NT; ++t)
 #pragma unroll
         for (int k = 0; k < 4; ++k) s[t][k] = (kParts<T> > 1 ? s[t][k] + rest[t][k] : s[t][k]) * scale_log2;
-      if (hi == kStep) weigh_logits<D, NT, false>(st, s, lane, 0, kStep);
-      else weigh_logits<D, NT, true>(st, s, lane, 0, hi);
+      if (hi == kStep) weigh_logits<D, NT, false, 1>(st, s1, lane, 0, kStep);
+      else weigh_logits<D, NT, true, 1>(st, s1, lane, 0, hi);
       uint32_t pa[kWeightParts<T, NT>][NT][2];
 #pragma unroll
       for (int t = 0; t < NT; ++t) {
@@ -785,26 +855,26 @@ struct Units {
   int64_t all() const { return std::max<int64_t>(1, paged + plain); }
 };
 Units units_of(const fc::SpanGeom& g, int c) {
-  auto steps = [&](int i) { return g.hi[i][c] > g.lo[i][c] ? (g.hi[i][c] + kStep - 1) / kStep - g.lo[i][c] / kStep : 0; };
+  auto steps = [&](int i) { return g.hi[i][c] > g.lo[i][c] ? (g.hi[i][c] + kPagedStep - 1) / kPagedStep - g.lo[i][c] / kPagedStep : 0; };
   int64_t plain = 0;
   for (int i = 2; i < 4; ++i)
     for (int s = 0; s < g.n_seg; ++s) {
       const int n = std::min(g.hi[i][c], g.seg_log[s + 1]) - std::max(g.lo[i][c], g.seg_log[s]);
       if (n > 0) plain += (n + kStep - 1) / kStep;
     }
-  return {steps(0) + steps(1), plain * (g.f32 ? kPlainCost<float> : kPlainCost<__nv_bfloat16>)};
+  return {(int64_t)kPagedCost * (steps(0) + steps(1)), plain * (g.f32 ? kPlainCost<float> : kPlainCost<__nv_bfloat16>)};
 }
 
-// Measured on B200, in microseconds a unit of cost (a step of one of a block's four warps, divided by four and, over plain rows, by kPlainCost): of a
+// Measured on B200, in microseconds a unit of cost (a step of a block's four warps, divided by four and by kPagedCost or kPlainCost): of a
 // block alone on its SM, of one of two, and of an SM whose blocks keep it busy (D = 128: the bandwidth).
 struct UnitUs {
   double alone, two, full;
 };
 UnitUs unit_us(const fc::SpanGeom& g, int nt, double plain) {  // plain: their share of all units
-  static const UnitUs t[2][2][2][2] = {{{{{0.115, 0.149, 0.057}, {0.088, 0.099, 0.052}}, {{0.122, 0.163, 0.081}, {0.092, 0.103, 0.051}}},
-                                        {{{0.150, 0.195, 0.095}, {0.109, 0.184, 0.095}}, {{0.183, 0.230, 0.115}, {0.111, 0.188, 0.094}}}},
-                                       {{{{0.122, 0.160, 0.063}, {0.100, 0.126, 0.063}}, {{0.152, 0.207, 0.104}, {0.113, 0.145, 0.072}}},
-                                        {{{0.200, 0.238, 0.088}, {0.178, 0.237, 0.122}}, {{0.224, 0.300, 0.150}, {0.210, 0.275, 0.138}}}}};
+  static const UnitUs t[2][2][2][2] = {{{{{0.066, 0.098, 0.057}, {0.088, 0.099, 0.052}}, {{0.086, 0.123, 0.062}, {0.092, 0.103, 0.051}}},
+                                        {{{0.112, 0.135, 0.100}, {0.109, 0.184, 0.095}}, {{0.124, 0.160, 0.100}, {0.111, 0.188, 0.094}}}},
+                                       {{{{0.079, 0.116, 0.052}, {0.100, 0.126, 0.063}}, {{0.103, 0.160, 0.080}, {0.113, 0.145, 0.072}}},
+                                        {{{0.140, 0.199, 0.095}, {0.178, 0.237, 0.122}}, {{0.166, 0.230, 0.115}, {0.210, 0.275, 0.138}}}}};
   const UnitUs &a = t[g.f32][g.d == 128][nt - 1][0], &b = t[g.f32][g.d == 128][nt - 1][1];
   return {a.alone + plain * (b.alone - a.alone), a.two + plain * (b.two - a.two), a.full + plain * (b.full - a.full)};
 }
@@ -813,9 +883,9 @@ UnitUs unit_us(const fc::SpanGeom& g, int nt, double plain) {  // plain: their s
 //   in clusters   every tile's keys into the same number of parts, at most 16, whose blocks are a cluster and join themselves
 //   by size       every chunk's into parts of at most `size` units, which a second kernel joins (3.5 us and its bytes): where a few tiles see many keys,
 //                 or some chunks far more than others
-// of which the fastest is taken, by the times above; a call takes 4.4 us besides.
-// Of 60 calls at random, of 5 to 60 us, the choice was 3 % above the best of sixteen cuts in the median and within 12 % for nine in ten; 63 % in one, of six
-// chunks of which the device left five out, which the host does not know.
+// of which the fastest is taken, by the times above; a call takes 4.8 us besides.
+// Of 60 calls at random, of 5 to 60 us, the choice was as fast as the best of sixteen cuts in the median, within 10 % for nine in ten, and at most 15 %
+// above it; chunks that the device leaves out, which the host does not know, can cost more (63 % where it left out five of six).
 struct Cut {
   double us;
   int32_t cluster;
@@ -835,7 +905,7 @@ Cut cut_of(const fc_ctx* ctx, const fc::SpanGeom& g, int nt, const Units* units)
   const UnitUs u = unit_us(g, nt, work > 0 ? plain / work : 0);
   // Clusters lie unevenly: some SMs hold three blocks before every one holds two.
   auto time_of = [&](double blocks, double size, double room, bool clusters) {
-    size = std::ceil(size / kWarps) * kWarps;
+    size = std::ceil(size / (kWarps * kPagedCost)) * (kWarps * kPagedCost);
     const double lone = blocks <= sm ? u.alone : blocks <= (clusters ? 1.75 : 2.0) * sm || nt == 2 ? u.two : 1.25 * u.two;
     if (blocks <= room) return size * std::max(lone, u.full * blocks / sm);
     return u.full * work / sm + 0.7 * size * u.alone + 3.5 * blocks / room;  // a set of blocks takes 3.5 us to start and end
@@ -844,7 +914,7 @@ Cut cut_of(const fc_ctx* ctx, const fc::SpanGeom& g, int nt, const Units* units)
   for (int n = 1; n <= kMaxCluster && (n == 1 || most >= kWarps * n); ++n) {
     const int held = ctx->span_clusters[g.f32][g.d == 128][nt - 1][n];
     const double room = n == 1 ? places : held > 0 ? (double)held * n : 0.75 * places;
-    const double us = 4.4 + (n > 1 ? 0.5 + 0.1 * n : 0) + time_of((double)all * n, (double)((most + n - 1) / n), room, n > 1);
+    const double us = 4.8 + (n > 1 ? 0.5 + 0.1 * n : 0) + time_of((double)all * n, (double)((most + n - 1) / n), room, n > 1);
     if (n == 1 || us < best.us) best = {us, n, 0};
   }
   for (int64_t n = 2; n <= kMaxParts && most >= 2 * kWarps * n; n += (n + 7) / 8) {
@@ -855,7 +925,7 @@ Cut cut_of(const fc_ctx* ctx, const fc::SpanGeom& g, int nt, const Units* units)
       blocks += tiles[c] * parts;
       if (parts > 1) rows += tiles[c] * parts * 8 * nt;
     }
-    const double us = 4.4 + 3.5 + 2.0 * 4 * g.d * rows / 4e6 + time_of(blocks, (double)size, places, false);
+    const double us = 4.8 + 3.5 + 2.0 * 4 * g.d * rows / 4e6 + time_of(blocks, (double)size, places, false);
     if (us < best.us) best = {us, 0, size};
   }
   return best;
@@ -881,7 +951,8 @@ double split(const fc_ctx* ctx, fc::SpanGeom& g) {
   for (int c = 0; c < g.W; ++c) {
     const int64_t n = units[c].all(), parts = cut.cluster ? cut.cluster : (n + cut.size - 1) / cut.size;
     g.parts[c] = (int32_t)parts;
-    g.part_units[c] = (int32_t)(((n + parts - 1) / parts + kWarps - 1) / kWarps * kWarps);  // whole rounds of the warps
+    constexpr int kRound = kWarps * kPagedCost;
+    g.part_units[c] = (int32_t)(((n + parts - 1) / parts + kRound - 1) / kRound * kRound);  // whole rounds of the warps
     blocks += (fc::span_rows(g, c) + 8 * nt - 1) / (8 * nt) * parts;
     g.block_end[c] = (int32_t)std::min<int64_t>(blocks, INT32_MAX);
   }
@@ -902,13 +973,13 @@ int encode(fc_ctx* ctx, CUtensorMap* map, CUtensorMapDataType type, int rank, co
   }
   return FC_OK;
 }
-// Pages of codes: a box is 16 rows of a block.
+// Pages of codes: a box is 32 rows of a block, or all 16.
 int map_pages(fc_ctx* ctx, CUtensorMap* map, const void* base, const fc::SpanGeom& g) {
   const int page = 1 << g.pool.page_log2;
   const int64_t block = (int64_t)page * g.d;  // the stride of an axis of one entry is never used, but has to be a valid one
   const cuuint64_t dims[4] = {(cuuint64_t)g.d, (cuuint64_t)page, (cuuint64_t)g.H_kv, (cuuint64_t)g.pool.n_pages};
   const cuuint64_t strides[3] = {(cuuint64_t)g.d, (cuuint64_t)(g.H_kv > 1 ? g.pool.code_hs : block), (cuuint64_t)(g.pool.n_pages > 1 ? g.pool.code_ps : block)};
-  const cuuint32_t box[4] = {(cuuint32_t)g.d, kStep, 1, 1};
+  const cuuint32_t box[4] = {(cuuint32_t)g.d, (cuuint32_t)std::min(page, kPagedStep), 1, 1};
   return encode(ctx, map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 4, base, dims, strides, box, g.d == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B);
 }
 // Plain rows: a box is 128 bytes of 16 rows.
