@@ -517,8 +517,8 @@ int fc_chunk_attention_kv4(fc_ctx* ctx, void* stream, const fc_attn_desc* desc, 
 typedef struct {
   void *k_codes, *v_codes;        /* bytes, 16-byte aligned */
   float *k_scales, *v_scales;
-  int64_t code_ps, code_hs;       /* bytes, multiples of 16: page, head */
-  int64_t scale_ps, scale_hs;     /* elements */
+  int64_t code_ps, code_hs;       /* bytes, multiples of 16 below 2^36: page, head */
+  int64_t scale_ps, scale_hs;     /* elements, below 2^31 */
   int32_t n_pages, page;
 } fc_kv8_pool;
 

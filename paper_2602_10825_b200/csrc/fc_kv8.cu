@@ -10,8 +10,10 @@
 // significant bits, and a scale s has four.
 //   bf16 rows   (8 significant bits: x is either t s or at least 2^-9 of it away) x (1/s) is off by 2^-23 at most, so that it is
 //               rounded to fp16 first, which puts a tie where it belongs and crosses none.
-//   fp32 rows, and codes that are rounded again: the rounded quotient is on the right side of a tie, or on it where x = t s: x is otherwise
-//               away from t s by so much that the quotient is more than half an ulp from t.
+//   fp32 rows   q = x (1/s) and one correction, q + (x - q s)(1/s), whose remainder is exact: t itself where x = t s, since what is left of q's
+//               error is 2^-46 of it; otherwise x is an ulp or more from t s, and the quotient 0.53 ulp or more from t, so that
+//               it stays on its side.  The remainder has to be a normal number: below a scale of 2^-90 the quotient is divided.
+//   codes that are rounded again: divided.
 #include <algorithm>
 #include <climits>
 
@@ -124,12 +126,18 @@ __device__ __forceinline__ uint2 codes8_of(const float (&x)[8], float s) {
   }
   return make_uint2(cvt_e4m3x2(v[0], v[1]) | cvt_e4m3x2(v[2], v[3]) << 16, cvt_e4m3x2(v[4], v[5]) | cvt_e4m3x2(v[6], v[7]) << 16);
 }
-__device__ __forceinline__ uint2 codes8_finite(const Eight<float>& x, float s, float) {
+// s at least 2^-90, so that nothing below is too small for a remainder.
+__device__ __forceinline__ uint2 codes8_finite(const Eight<float>& x, float s, float r) {
   float v[8];
   get8(x, v);
-  return codes8_of<true>(v, s);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const float q = v[i] * r;
+    v[i] = copysignf(fmaf(fmaf(-q, s, v[i]), r, q), v[i]);  // a zero keeps its sign
+  }
+  return make_uint2(cvt_e4m3x2(v[0], v[1]) | cvt_e4m3x2(v[2], v[3]) << 16, cvt_e4m3x2(v[4], v[5]) | cvt_e4m3x2(v[6], v[7]) << 16);
 }
-// Any elements, as quotients: what the two above give for finite ones.
+// Any elements and scales, as quotients: what the two above give where they may be used.
 template <typename T>
 __device__ __noinline__ uint2 codes8_any(const Eight<T> x, float s) {
   float v[8];
@@ -175,27 +183,33 @@ kv8_append_kernel(const T* __restrict__ K, const T* __restrict__ V, const __grid
   const int page = 1 << g.pool.page_log2;
   const int lo = (int)max(g.pos[c] - token0, (int64_t)0);
   const int hi = (int)min((int64_t)page, g.pos[c] + (int64_t)(g.row_off[c + 1] - g.row_off[c]) - token0);
-  const T* src = (is_v ? V + h * g.v_hs : K + h * g.k_hs);
+  // the thread's first row, and from one of its rows to the next
+  constexpr int kRowsApart = kGroup / kRowVecs;
+  static_assert(kGroup % kRowVecs == 0, "a thread keeps its columns");
   const int64_t rs = is_v ? g.v_rs : g.k_rs;
+  const int row0 = tid / kRowVecs;
+  const T* src = (is_v ? V + h * g.v_hs : K + h * g.k_hs) + (src0 + row0) * rs + tid % kRowVecs * 8;
   Eight<T> x[kVec];
   bool bad = false;
   uint32_t a = 0;
+  const int64_t step = kRowsApart * rs;
 #pragma unroll
   for (int i = 0; i < kVec; ++i) {
-    const int vec = tid + i * kGroup, row = vec / kRowVecs;
-    if (row >= lo && row < hi) load8(src + (src0 + row) * rs + vec % kRowVecs * 8, x[i]);
+    const int row = row0 + i * kRowsApart;
+    if (row >= lo && row < hi) load8(src, x[i]);
+    src += step;
   }
   // the rows are on their way whether or not there is a page for them
   if (page_id < 0 || page_id >= g.pool.n_pages || (g.ref && g.ref[page_id] != 1)) {
     if (threadIdx.x == 0 && status) atomicOr(status, (uint32_t)FC_DEV_BAD_INDEX);
     return;
   }
-  uint8_t* codes = (is_v ? g.pool.v_codes : g.pool.k_codes) + page_id * g.pool.code_ps + h * g.pool.code_hs;
-  float* scale_p = (is_v ? g.pool.v_scales : g.pool.k_scales) + page_id * g.pool.scale_ps + h * g.pool.scale_hs;
+  uint8_t* codes = fc::kv8_block(is_v ? g.pool.v_codes : g.pool.k_codes, g.pool, page_id, h);
+  float* scale_p = fc::kv8_scale(is_v ? g.pool.v_scales : g.pool.k_scales, g.pool, page_id, h);
   const float s_old = lo > 0 ? *scale_p : 0.f;
 #pragma unroll
   for (int i = 0; i < kVec; ++i) {
-    const int row = (tid + i * kGroup) / kRowVecs;
+    const int row = row0 + i * kRowsApart;
     if (row >= lo && row < hi) a = max(a, largest(x[i]));
   }
   if (a >= 0x7f800000u) {
@@ -203,7 +217,7 @@ kv8_append_kernel(const T* __restrict__ K, const T* __restrict__ V, const __grid
     a = 0;
 #pragma unroll
     for (int i = 0; i < kVec; ++i) {
-      const int row = (tid + i * kGroup) / kRowVecs;
+      const int row = row0 + i * kRowsApart;
       if (row >= lo && row < hi) a = max(a, largest_finite<T>(x[i]));
     }
   }
@@ -215,11 +229,12 @@ kv8_append_kernel(const T* __restrict__ K, const T* __restrict__ V, const __grid
     for (int i = 0; i < kGroup / 32; ++i) a = max(a, largest_s[group * (kGroup / 32) + i]);
   }
   const float s = fmaxf(scale_of(a), s_old), r = s > 0.f ? __frcp_rn(s) : 0.f;
+  const bool slow = bad || (sizeof(T) == 4 && s < 0x1p-90f);
 #pragma unroll
   for (int i = 0; i < kVec; ++i) {
-    const int vec = tid + i * kGroup, row = vec / kRowVecs;
-    uint2* at = reinterpret_cast<uint2*>(codes + vec * 8);
-    if (row >= lo && row < hi) *at = bad ? codes8_any<T>(x[i], s) : codes8_finite(x[i], s, r);
+    const int row = row0 + i * kRowsApart;
+    uint2* at = reinterpret_cast<uint2*>(codes) + tid + i * kGroup;
+    if (row >= lo && row < hi) *at = slow ? codes8_any<T>(x[i], s) : codes8_finite(x[i], s, r);
     else if (row < lo && s > s_old) *at = again8(*at, s_old, s);
   }
   if (tid == 0 && (lo == 0 || s > s_old)) *scale_p = s;  // every thread of the group has read the old one
@@ -265,39 +280,37 @@ kv8_unpack_kernel(T* __restrict__ K, T* __restrict__ V, const __grid_constant__ 
   T* dst = is_v ? V : K;
   if (!dst) return;
   const fc::Kv8Job job = g.jobs.job[blockIdx.z >> 1];
-  const int64_t r0 = (int64_t)blockIdx.x * kUnpackRows * R + threadIdx.x / kRowVecs;
+  const int r0 = blockIdx.x * (kUnpackRows * R) + threadIdx.x / kRowVecs;  // below 2^31, as the tokens are
   if (r0 >= job.n) return;
-  const uint8_t* codes = (is_v ? g.src.v_codes : g.src.k_codes) + h * g.src.code_hs;
-  const float* scales = (is_v ? g.src.v_scales : g.src.k_scales) + h * g.src.scale_hs;
-  const int64_t hs = is_v ? g.v_hs : g.k_hs, rs = is_v ? g.v_rs : g.k_rs;
+  uint8_t* codes = fc::kv8_block(is_v ? g.src.v_codes : g.src.k_codes, g.src, 0, h);
+  float* scales = fc::kv8_scale(is_v ? g.src.v_scales : g.src.k_scales, g.src, 0, h);
+  const int64_t rs = is_v ? g.v_rs : g.k_rs;
   const int32_t* table = g.table + job.seq * g.table_cs;
   int32_t page_id[kUnpackRows];
   C word[kUnpackRows];
   float scale[kUnpackRows];
 #pragma unroll
-  for (int u = 0; u < kUnpackRows; ++u) {
-    const int64_t r = r0 + u * R;
-    page_id[u] = r < job.n ? __ldg(table + ((job.first + r) >> g.src.page_log2)) : -1;
-  }
+  for (int u = 0; u < kUnpackRows; ++u) page_id[u] = r0 + u * R < job.n ? __ldg(table + ((job.first + r0 + u * R) >> g.src.page_log2)) : -1;
   bool bad = false;
 #pragma unroll
   for (int u = 0; u < kUnpackRows; ++u) {
-    const int64_t r = r0 + u * R;
     word[u] = C{};
     scale[u] = 0.f;
-    if (r >= job.n) continue;
-    if (page_id[u] >= 0 && page_id[u] < g.src.n_pages) {
-      const int in_page = (int)((job.first + r) & ((1 << g.src.page_log2) - 1));
-      word[u] = __ldg(reinterpret_cast<const C*>(codes + page_id[u] * g.src.code_ps + in_page * D + kVec * w));
-      scale[u] = __ldg(scales + page_id[u] * g.src.scale_ps);
-    } else {
-      bad = true;
+    const bool there = (uint32_t)page_id[u] < (uint32_t)g.src.n_pages;
+    if (there) {
+      const int in_page = (job.first + r0 + u * R) & ((1 << g.src.page_log2) - 1);
+      word[u] = __ldg(reinterpret_cast<const C*>(fc::kv8_block(codes, g.src, page_id[u], 0)) + in_page * kRowVecs + w);
+      scale[u] = __ldg(fc::kv8_scale(scales, g.src, page_id[u], 0));
     }
+    bad |= !there && r0 + u * R < job.n;
   }
+  T* out = dst + h * (is_v ? g.v_hs : g.k_hs) + (job.dst_row + r0) * rs + kVec * w;
+  const int64_t step = R * rs;
 #pragma unroll
   for (int u = 0; u < kUnpackRows; ++u) {
-    const int64_t r = r0 + u * R;
-    if (r < job.n && fc::bounds_ok(job.dst_row + r < g.rows && w < kRowVecs, g.status)) store_values(dst + h * hs + (job.dst_row + r) * rs + kVec * w, word[u], scale[u]);
+    const int r = r0 + u * R;
+    if (r < job.n && fc::bounds_ok(job.dst_row + r < g.rows, g.status)) store_values(out, word[u], scale[u]);
+    out += step;
   }
   if (bad && g.status) atomicOr(g.status, (uint32_t)FC_DEV_BAD_INDEX);
 }

@@ -40,10 +40,20 @@ inline int kv8_check(const fc_kv8_pool* p, int H, int d) {
   if (!aligned16(p->k_codes) || !aligned16(p->v_codes) || ((uintptr_t)p->k_scales | (uintptr_t)p->v_scales) % 4) return FC_ERR_MISALIGNED;
   if (p->code_ps < 0 || p->code_hs < 0 || p->code_ps % 16 || p->code_hs % 16) return FC_ERR_MISALIGNED;
   if (p->scale_ps < 0 || p->scale_hs < 0) return FC_ERR_INVALID_ARG;
-  if (p->code_ps >= (1ll << 40) || p->code_hs >= (1ll << 40)) return FC_ERR_UNSUPPORTED;  // what a tensor map takes
+  // what 32 bits hold in units of 16 bytes, and of a scale
+  if (p->code_ps >= (1ll << 36) || p->code_hs >= (1ll << 36) || p->scale_ps > INT32_MAX || p->scale_hs > INT32_MAX) return FC_ERR_UNSUPPORTED;
   if (!grid_disjoint(p->n_pages, p->code_ps, H, p->code_hs, (int64_t)p->page * d)) return FC_ERR_INVALID_ARG;
   if (!grid_disjoint(p->n_pages, p->scale_ps, H, p->scale_hs, 1)) return FC_ERR_INVALID_ARG;
   return FC_OK;
+}
+
+// First byte of a block, and its scale: one multiplication each.
+__device__ __forceinline__ uint8_t* kv8_block(uint8_t* codes, const Kv8View& p, int page, int h) {
+  return reinterpret_cast<uint8_t*>(reinterpret_cast<uint4*>(codes) + (uint64_t)(uint32_t)page * (uint32_t)(p.code_ps >> 4) +
+                                    (uint64_t)(uint32_t)h * (uint32_t)(p.code_hs >> 4));
+}
+__device__ __forceinline__ float* kv8_scale(float* scales, const Kv8View& p, int page, int h) {
+  return scales + (uint64_t)(uint32_t)page * (uint32_t)p.scale_ps + (uint64_t)(uint32_t)h * (uint32_t)p.scale_hs;
 }
 
 // Two codes (the low 16 bits) as two fp16 numbers: exact.

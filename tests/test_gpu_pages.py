@@ -190,6 +190,21 @@ def test_append_fp32_next_to_ties(fc, ctx):
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("size", [2.0 ** -124, 2.0 ** -108, 2.0 ** -90, 2.0 ** -81, 1.0, 2.0 ** 100])
+def test_append_rows_of_any_size(fc, ctx, size, dtype):
+    # zeros of both signs among them, and next to the scale below which fp32 rows are divided
+    H, d, page, n = 9, 64, 32, 32
+    K = (rand((H, n, d), 1, 1.0, F32) * torch.linspace(0.5, 2.1, H, device="cuda")[:, None, None] * size).to(dtype)
+    K[:, :, :2] = torch.tensor([0.0, -0.0], device="cuda")
+    pool, t = filled_pool(fc, 1, H, page, d, 1), np.asarray([[0]])
+    want = numpy_pool(pool)
+    ctx.kv8_append(K, -K, pool, i32(t), [0])
+    want.append(f64(K), 0, t[0], 0)
+    want.append(-f64(K), 1, t[0], 0)
+    same_pool(pool, want)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
 def test_append_nonfinite_elements(fc, ctx, dtype):
     H, d, page, n = 2, 64, 32, 20
     K, V = rand((H, n, d), 1, 1.0, dtype), rand((H, n, d), 2, 1.0, dtype)

@@ -48,7 +48,7 @@ POOL_REFUSALS = [
     (dict(k_codes=None), INVALID), (dict(v_scales=None), INVALID), (dict(n_pages=0), INVALID), (dict(n_pages=2 ** 31 - 8000), UNSUPPORTED), (dict(page=48), UNSUPPORTED), (dict(page=8), UNSUPPORTED),
     (dict(k_codes=P + 8), MISALIGNED), (dict(k_scales=P + 2), MISALIGNED), (dict(code_hs=64 * 128 + 8), MISALIGNED), (dict(code_ps=-16), MISALIGNED),
     (dict(scale_hs=-1), INVALID), (dict(code_hs=64 * 128 - 16), INVALID), (dict(code_ps=3 * 64 * 128), INVALID), (dict(scale_ps=3), INVALID),
-    (dict(scale_hs=0), INVALID), (dict(code_ps=1 << 41), UNSUPPORTED),
+    (dict(scale_hs=0), INVALID), (dict(code_ps=1 << 36), UNSUPPORTED), (dict(scale_ps=1 << 31), UNSUPPORTED),
 ]
 
 
