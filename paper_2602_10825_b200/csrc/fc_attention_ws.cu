@@ -93,6 +93,8 @@ struct WsSmem {
   int32_t n_whole, n_rest, n_parts;     // two stores: items in one piece, items cut into parts, parts of each
   int32_t act_chunk[FC_MAX_CHUNKS];     // active chunks, longest visible prefix first
   int32_t act_item_end[FC_MAX_CHUNKS];  // running item count over that list (all heads)
+  // kSpans: the items that have rows in tile A only, one a head of the chunks that leave such a rest, come behind all others
+  int32_t tail_item_end[FC_MAX_CHUNKS];
 };
 
 struct Item {
@@ -236,8 +238,16 @@ attention_ws_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
     int items = 0;
     for (int a = 0; a < n; ++a) {
       const int c = sh->act_chunk[a];
-      items += n_heads * (((g.q_row_off[c + 1] - g.q_row_off[c]) * pk + 2 * kBM - 1) / (2 * kBM));
+      // (a rest of at most 128 rows counts below)
+      items += n_heads * (((g.q_row_off[c + 1] - g.q_row_off[c]) * pk + (kSource == kSpans ? kBM : 2 * kBM) - 1) / (2 * kBM));
       sh->act_item_end[a] = items;
+    }
+    if constexpr (kSource == kSpans) {
+      for (int a = 0; a < n; ++a) {
+        const int c = sh->act_chunk[a], rest = (g.q_row_off[c + 1] - g.q_row_off[c]) * pk % (2 * kBM);
+        if (rest > 0 && rest <= kBM) items += n_heads;
+        sh->tail_item_end[a] = items;
+      }
     }
     sh->n_act = n;
     sh->total_items = items;
@@ -245,8 +255,13 @@ attention_ws_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
       const int blocks = gridDim.x, whole = split.slots > 0 ? items / blocks * blocks : items, rest = items - whole;
       int parts = 1;
       if (rest > 0) {
-        int a = 0;  // the chunk of the first item that could be cut: none behind it sees more
-        while (sh->act_item_end[a] <= whole) ++a;
+        int a = 0;  // the chunk of the first item that could be cut: none behind it sees more (kSpans: of its kind)
+        if constexpr (kSource == kSpans) {
+          if (whole >= sh->act_item_end[n - 1]) while (sh->tail_item_end[a] <= whole) ++a;
+          else while (sh->act_item_end[a] <= whole) ++a;
+        } else {
+          while (sh->act_item_end[a] <= whole) ++a;
+        }
         parts = fc::split_parts(rest, blocks, (g.vis[sh->act_chunk[a]] + kBN - 1) / kBN, D, split.slots, nullptr);
       }
       sh->n_parts = parts;
@@ -283,12 +298,28 @@ attention_ws_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
       }
     }
     int a = 0;
-    while (a + 1 < n_act && item >= sh->act_item_end[a]) ++a;
-    const int start = a > 0 ? sh->act_item_end[a - 1] : 0;
-    const int pairs = (sh->act_item_end[a] - start) / n_heads;
-    it.c = sh->act_chunk[a];
-    it.h = (item - start) / pairs;
-    it.row0 = g.q_row_off[it.c] * pk + ((item - start) % pairs) * 2 * kBM;
+    if constexpr (kSource == kSpans) {
+      const int n_pairs = sh->act_item_end[n_act - 1];
+      if (item >= n_pairs) {
+        while (a + 1 < n_act && item >= sh->tail_item_end[a]) ++a;
+        it.c = sh->act_chunk[a];
+        it.h = item - (a > 0 ? sh->tail_item_end[a - 1] : n_pairs);
+        it.row0 = g.q_row_off[it.c] * pk + (g.q_row_off[it.c + 1] - g.q_row_off[it.c]) * pk / (2 * kBM) * (2 * kBM);
+      } else {
+        while (a + 1 < n_act && item >= sh->act_item_end[a]) ++a;
+        const int start = a > 0 ? sh->act_item_end[a - 1] : 0, pairs = (sh->act_item_end[a] - start) / n_heads;
+        it.c = sh->act_chunk[a];
+        it.h = (item - start) / pairs;
+        it.row0 = g.q_row_off[it.c] * pk + ((item - start) % pairs) * 2 * kBM;
+      }
+    } else {
+      while (a + 1 < n_act && item >= sh->act_item_end[a]) ++a;
+      const int start = a > 0 ? sh->act_item_end[a - 1] : 0;
+      const int pairs = (sh->act_item_end[a] - start) / n_heads;
+      it.c = sh->act_chunk[a];
+      it.h = (item - start) / pairs;
+      it.row0 = g.q_row_off[it.c] * pk + ((item - start) % pairs) * 2 * kBM;
+    }
     it.n_vis = g.vis[it.c];
     it.k_lo = 0;
     if constexpr (kTwo) {
