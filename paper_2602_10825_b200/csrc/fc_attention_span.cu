@@ -97,6 +97,7 @@ struct TilePlan {
 // False if there are more rows to unpack than a tensor map's place can name.
 bool plan_tiles(const fc_ctx* ctx, const fc::SpanGeom& g, TilePlan& p) {
   // the tokens to unpack: of the shared sequence those that some chunk sees, else each chunk's own
+  p.jobs = {};
   const bool shared = g.table_cs == 0;
   for (int c = 0; c < g.W; ++c) {
     for (int i = 0; i < 4; ++i) p.spans.lo[i][c] = g.lo[i][c], p.spans.hi[i][c] = g.hi[i][c];
@@ -104,28 +105,47 @@ bool plan_tiles(const fc_ctx* ctx, const fc::SpanGeom& g, TilePlan& p) {
     for (int i = 0; i < 4; ++i) p.vis[c] += g.hi[i][c] - g.lo[i][c];
   }
   p.rows = 0;
-  p.jobs.n = 0;
+  p.jobs.W = g.W;
   for (int c0 = 0; c0 < g.W; c0 += shared ? g.W : 1) {
     const int c1 = shared ? g.W : c0 + 1;
-    int first = 0, from = INT32_MAX, to = 0;  // tokens [0, first) and [from, to)
-    for (int c = c0; c < c1; ++c) {
-      if (fc::span_rows(g, c) == 0) continue;
-      first = std::max(first, g.hi[0][c]);
-      if (g.hi[1][c] > g.lo[1][c]) from = std::min(from, g.lo[1][c]), to = std::max(to, g.hi[1][c]);
+    // what is seen, in order; pieces that meet become one job
+    struct Piece {
+      int32_t lo, hi;
+      uint64_t who;
+    } piece[2 * FC_MAX_CHUNKS];
+    int n = 0;
+    for (int c = c0; c < c1; ++c)
+      for (int i = 0; i < 2; ++i)
+        if (g.hi[i][c] > g.lo[i][c] && fc::span_rows(g, c) > 0) piece[n++] = {g.lo[i][c], g.hi[i][c], 1ull << c};
+    std::sort(piece, piece + n, [](const Piece& a, const Piece& b) { return a.lo < b.lo; });
+    const int first_job = p.jobs.n;
+    for (int k = 0; k < n; ++k) {
+      fc::Kv8Job* last = p.jobs.n > first_job ? &p.jobs.job[p.jobs.n - 1] : nullptr;
+      if (last && piece[k].lo <= last->first + last->n) {
+        last->n = std::max(last->n, piece[k].hi - last->first);
+        p.jobs.needed[p.jobs.n - 1] |= piece[k].who;
+      } else {
+        p.jobs.needed[p.jobs.n] = piece[k].who;
+        p.jobs.job[p.jobs.n++] = {shared ? 0 : c0, piece[k].lo, piece[k].hi - piece[k].lo, 0};
+      }
     }
-    if (from <= first) first = std::max(first, to), from = to = 0;
-    else if (to == 0) from = 0;
-    const int at_first = p.rows, at_from = p.rows + first - from;  // row of token 0, and of token 0 counted from the second range
-    if (first > 0) p.jobs.job[p.jobs.n++] = {shared ? 0 : c0, 0, first, p.rows};
-    if (to > from) p.jobs.job[p.jobs.n++] = {shared ? 0 : c0, from, to - from, p.rows + first};
+    for (int j = first_job; j < p.jobs.n; ++j) {
+      fc::Kv8Job& job = p.jobs.job[j];
+      if ((int64_t)p.rows + job.n > INT32_MAX - 4096) return false;
+      job.dst_row = p.rows;
+      p.rows += job.n;
+    }
     for (int c = c0; c < c1; ++c)
       for (int i = 0; i < 2; ++i) {
-        const int move = to > from && g.lo[i][c] >= from ? at_from : at_first;
-        p.spans.lo[i][c] += move;
-        p.spans.hi[i][c] += move;
+        if (g.hi[i][c] <= g.lo[i][c] || fc::span_rows(g, c) == 0) {
+          p.spans.lo[i][c] = p.spans.hi[i][c] = 0;
+          continue;
+        }
+        int j = first_job;
+        while (g.hi[i][c] > p.jobs.job[j].first + p.jobs.job[j].n) ++j;
+        p.spans.lo[i][c] += p.jobs.job[j].dst_row - p.jobs.job[j].first;
+        p.spans.hi[i][c] += p.jobs.job[j].dst_row - p.jobs.job[j].first;
       }
-    if ((int64_t)p.rows + first + (to - from) > INT32_MAX - 4096) return false;
-    p.rows += first + to - from;
   }
   // grouped heads share their key tiles where whole groups fill a tile of 128 rows
   p.split = fc::AttnSplit();
@@ -267,6 +287,8 @@ int attend(fc_ctx* ctx, void* stream, const fc_attn_desc* desc, const void* Q, c
     return fc::kv8_unpack_launch(x.st, x.g->pool, x.g->H_kv, x.g->d, x.g->table, x.g->table_cs, x.t->jobs, x.k, x.v, FC_BF16, hs, x.g->d, hs,
                                  x.g->d, x.g->status, x.counter);
   };
+  t.jobs.active_ids = active_ids;
+  t.jobs.n_active = n_active;
   t.split.follows = t.rows > 0;
   t.split.o = (float*)(base + t.o);
   t.split.ml = (float2*)(base + t.ml);

@@ -912,7 +912,9 @@ Cut cut_of(const fc_ctx* ctx, const fc::SpanGeom& g, int nt, const Units* units)
   };
   Cut best = {0, 1, 0};
   for (int n = 1; n <= kMaxCluster && (n == 1 || most >= kWarps * n); ++n) {
-    const int held = ctx->span_clusters[g.f32][g.d == 128][nt - 1][n];
+    const int16_t* clusters = ctx->span_clusters[g.f32][g.d == 128][nt - 1];
+    const int held = clusters[n];
+    if (n > 1 && held == 0 && (n > 8 || clusters[2] > 0)) break;  // not a size that the device takes
     const double room = n == 1 ? places : held > 0 ? (double)held * n : 0.75 * places;
     const double us = 4.8 + (n > 1 ? 0.5 + 0.1 * n : 0) + time_of((double)all * n, (double)((most + n - 1) / n), room, n > 1);
     if (n == 1 || us < best.us) best = {us, n, 0};

@@ -280,6 +280,16 @@ kv8_unpack_kernel(T* __restrict__ K, T* __restrict__ V, const __grid_constant__ 
   T* dst = is_v ? V : K;
   if (!dst) return;
   const fc::Kv8Job job = g.jobs.job[blockIdx.z >> 1];
+  if (g.jobs.active_ids) {
+    const int lane = threadIdx.x % 32, n = min(max(*g.jobs.n_active, 0), g.jobs.W);
+    uint64_t mine = 0;
+    for (int i = lane; i < n; i += 32) {
+      const int c = g.jobs.active_ids[i];
+      if (c >= 0 && c < g.jobs.W) mine |= 1ull << c;
+    }
+    const uint32_t lo = __reduce_or_sync(0xffffffffu, (uint32_t)mine), hi = __reduce_or_sync(0xffffffffu, (uint32_t)(mine >> 32));
+    if (!(((uint64_t)hi << 32 | lo) & g.jobs.needed[blockIdx.z >> 1])) return;
+  }
   const int r0 = blockIdx.x * (kUnpackRows * R) + threadIdx.x / kRowVecs;  // below 2^31, as the tokens are
   if (r0 >= job.n) return;
   uint8_t* codes = fc::kv8_block(is_v ? g.src.v_codes : g.src.k_codes, g.src, 0, h);

@@ -83,7 +83,12 @@ constexpr int kKv8Jobs = 2 * FC_MAX_CHUNKS;
 struct Kv8Jobs {
   int32_t n;
   Kv8Job job[kKv8Jobs];
+  // With a list of active chunks (DEVICE, as in fc_chunk_attention), only the jobs are done that one of them needs: bit c of needed[j].
+  const int32_t *active_ids, *n_active;
+  int32_t W;
+  uint64_t needed[kKv8Jobs];
 };
+static_assert(FC_MAX_CHUNKS <= 64, "a bit a chunk");
 
 // Unpacks jobs into [H, rows, d] tensors (fc_kv8.cu); either destination may be NULL.  `clear`: a word that is set to zero on the
 // way, or NULL.  A kernel launched by launch_pdl behind it may start early.

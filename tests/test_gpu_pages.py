@@ -650,6 +650,28 @@ def test_attention_over_entries_that_are_no_page(fc, ctx, dtype, impl):
     assert int(status) == 0
 
 
+@pytest.mark.parametrize("dtype, impl", IMPLS)
+def test_attention_minds_only_entries_that_active_chunks_see(fc, ctx, dtype, impl):
+    # a shared sequence of which nobody sees the middle; a batch in which a finished sequence has let go of its pages
+    H, d, page, n = 2, 64, 16, 160
+    pool, status = filled_pool(fc, 10, H, page, d, 1), status_word()
+    where = numpy_pool(pool)
+    Q = rand((H, 12, d), 2, 1.0, dtype)
+    O = torch.zeros_like(Q)
+    t = [0, 1, 2, 3, -1, 77, 6, 7, 8, 9]
+    kw = dict(n_sink=5, kv_begin=[20, 100], impl=impl, status=status)
+    ctx.chunk_attention_kv8(Q, pool, i32([t]), [64, n], None, None, [0, 6, 12], [64, n], i32([0, 1]), i32([2]), O, **kw)
+    assert int(status) == 0
+    kv = [tuple(where.rows(w, t, pg.seen_tokens(v, 5, b)) for w in (0, 1)) for v, b in ((64, 20), (n, 100))]
+    check(O, None, f64(Q), kv, [0, 6, 12], [0, 1], d ** -0.5, dtype, impl)
+    O.fill_(9.0)
+    tables_ = i32([t[:4], [-1] * 4, t[6:]])
+    ctx.chunk_attention_kv8(Q, pool, tables_, [64] * 3, None, None, [0, 4, 8, 12], [64] * 3, i32([2, 0]), i32([2]), O, impl=impl, status=status)
+    assert int(status) == 0
+    kv = [tuple(where.rows(w, r, range(64)) for w in (0, 1)) if r[0] >= 0 else None for r in tables_.tolist()]
+    check(O, None, f64(Q), kv, [0, 4, 8, 12], [0, 2], d ** -0.5, dtype, impl, 9.0)
+
+
 @pytest.mark.parametrize("rows", [3, 300])
 @pytest.mark.parametrize("dtype", [BF16, F32])
 def test_attention_strides(fc, ctx, dtype, rows):
