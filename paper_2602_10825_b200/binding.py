@@ -724,9 +724,10 @@ class Context:
     # ------------------------------------------------------------------ the paged 8-bit store
     def _table(self, table, name="table"):
         """Pointer and row stride of an int32 table [sequences, entries]."""
-        if table.dim() != 2 or (table.shape[1] > 1 and table.stride(1) != 1):
+        strides = table.stride()
+        if len(strides) != 2 or (strides[1] != 1 and table.shape[1] > 1):
             raise FcError(f"{name} must be [sequences, entries] with contiguous rows")
-        return self._ptr(table, name, torch.int32), table.stride(0)
+        return self._ptr(table, name, torch.int32), strides[0]
 
     def _counts(self, ref, n_pages):
         if ref.dim() != 1 or ref.shape[0] != n_pages or (n_pages > 1 and ref.stride(0) != 1):
@@ -756,7 +757,10 @@ class Context:
         self._in_table(pool, table, [p + b - a for p, a, b in zip(pos, row_off, row_off[1:])])
         tp, cs = self._table(table)
         desc = _KV8_ROWS_FIELDS.pack(pool.H, pool.d, W, kh, kr, vh, vr)
-        rc = self._L.fc_kv8_append(self._h, self._raw_stream(), desc, kp, vp, _dt(K), _int32(row_off), _int32(pos), self._store(pool, "pool"),
+        ints = array("i", row_off)
+        ints.extend(pos)
+        at = ints.buffer_info()[0]
+        rc = self._L.fc_kv8_append(self._h, self._raw_stream(), desc, kp, vp, _dt(K), at, at + 4 * (W + 1), self._store(pool, "pool"),
                                    tp, cs, None if ref is None else self._counts(ref, pool.n_pages), self._ptr(status, "status", torch.int32))
         if rc:
             self._check(rc, "fc_kv8_append")
@@ -790,8 +794,11 @@ class Context:
         self._in_table(pool, table, [max(ends)] if shared and ends else ends)
         tp, cs = self._table(table)
         desc = _KV8_ROWS_FIELDS.pack(pool.H, pool.d, W, kh, kr, vh, vr)
-        rc = self._L.fc_kv8_unpack(self._h, self._raw_stream(), desc, self._store(pool, "pool"), tp, 0 if shared else cs, _int32(first),
-                                   _int32(row_off), kp, vp, _dt(K_dst), self._ptr(status, "status", torch.int32))
+        ints = array("i", row_off)
+        ints.extend(first)
+        at = ints.buffer_info()[0]
+        rc = self._L.fc_kv8_unpack(self._h, self._raw_stream(), desc, self._store(pool, "pool"), tp, 0 if shared else cs, at + 4 * (W + 1),
+                                   at, kp, vp, _dt(K_dst), self._ptr(status, "status", torch.int32))
         if rc:
             self._check(rc, "fc_kv8_unpack")
         return K_dst, V_dst
@@ -802,7 +809,11 @@ class Context:
         if len(last) != W or W > table.shape[0] or (W and max(last) > table.shape[1]):
             raise FcError("first and last must have one entry a sequence and stay inside the table")
         tp, cs = self._table(table)
-        rc = call(self._h, self._raw_stream(), self._counts(ref, ref.shape[0]), ref.shape[0], tp, cs, W, _int32(first), _int32(last),
+        n_pages = ref.shape[0]
+        ints = array("i", first)
+        ints.extend(last)
+        at = ints.buffer_info()[0]
+        rc = call(self._h, self._raw_stream(), self._counts(ref, n_pages), n_pages, tp, cs, W, at, at + 4 * W,
                   self._ptr(status, "status", torch.int32))
         if rc:
             self._check(rc, name)
@@ -825,11 +836,15 @@ class Context:
         if n and max(tokens) > table.shape[1] * pool.page:
             raise FcError(f"table has entries for {table.shape[1] * pool.page} tokens, {max(tokens)} are asked for")
         tp, cs = self._table(table)
+        ints = array("i", src)
+        ints.extend(dst)
+        ints.extend(tokens)
+        at = ints.buffer_info()[0]
         stream = self._raw_stream()
         if ws is None:
             ws = self._scratch("pages", self._L.fc_pages_workspace_bytes(pool.n_pages), stream)
         rc = self._L.fc_pages_fork(self._h, stream, self._store(pool, "pool"), pool.H, pool.d, self._counts(ref, pool.n_pages), tp,
-                                   cs if table.shape[0] > 1 else table.shape[1], table.shape[0], n, _int32(src), _int32(dst), _int32(tokens),
+                                   cs if table.shape[0] > 1 else table.shape[1], table.shape[0], n, at, at + 4 * n, at + 8 * n,
                                    self._ptr(status, "status", torch.int32), self._ptr(ws, "ws"), ws.numel())
         if rc:
             self._check(rc, "fc_pages_fork")
@@ -857,15 +872,11 @@ class Context:
 
         table [W, entries] has a row for each chunk, or one that all share.  K and V may be None (everything is in pages).  Without a
         segment table the plain tokens are the rows of K and V in order."""
-        W = len(kv_visible_len)
-        if len(cache_len) != W:
-            raise FcError("cache_len and kv_visible_len must have one entry a chunk")
-        if table.shape[0] not in (1, W) or max(cache_len, default=0) > table.shape[1] * pool.page:
+        if table.shape[0] not in (1, len(kv_visible_len)) or max(cache_len, default=0) > table.shape[1] * pool.page:
             raise FcError("table must have one row, or one for each chunk, with entries for cache_len tokens")
         tp, cs = self._table(table)
-        paged = (self._store(pool, "pool"), tp, cs if table.shape[0] > 1 else 0, _int32(cache_len), pool)
-        return self._span("kv8", Q, paged, K, V, q_chunk_row_off, kv_visible_len, n_sink, kv_begin, window_first, seg_logical_off,
-                          seg_phys_off, active_ids, n_active, O, lse, scale, impl, status, ws)
+        return self._span("kv8", Q, (pool, tp, cs if table.shape[0] > 1 else 0, cache_len), K, V, q_chunk_row_off, kv_visible_len, n_sink,
+                          kv_begin, window_first, seg_logical_off, seg_phys_off, active_ids, n_active, O, lse, scale, impl, status, ws)
 
     def chunk_attention_span(self, Q, K, V, q_chunk_row_off, kv_visible_len, seg_logical_off, seg_phys_off, active_ids, n_active, O, *,
                              n_sink=0, kv_begin=None, lse=None, scale=0.0, impl=0, status=None, ws=None):
@@ -878,60 +889,85 @@ class Context:
         if Q.dim() != 3:
             raise FcError("Q must be [heads, rows, d]")
         H_q, rows, d = shape = Q.shape
-        dtype, dt = Q.dtype, _dt(Q)
+        dtype = Q.dtype
+        dt = _dt(Q)
         qp, qh, qr = self._rows(Q, "Q", shape, dtype)
         op, oh, orow = self._rows(O, "O", shape, dtype)
-        if paged is None and K is None:
+        if paged:
+            pool, tp, cs, cache_len = paged
+            H_kv = pool.H
+            if pool.d != d:
+                raise FcError("Q and the pool must share the head size")
+        elif K is None:
             raise FcError("K and V are None")
-        H_kv = paged[4].H if paged else K.shape[0]
-        if paged and paged[4].d != d:
-            raise FcError("Q and the pool must share the head size")
+        else:
+            H_kv = K.shape[0]
         W = len(kv_visible_len)
         if not active_ids.is_contiguous():
             raise FcError("active_ids must be contiguous")
         if len(q_chunk_row_off) != W + 1 or q_chunk_row_off[W] > rows or active_ids.numel() > W:
             raise FcError("q_chunk_row_off must have one entry more than kv_visible_len and stay inside Q; active_ids at most as many")
-        for name, x in (("kv_begin", kv_begin), ("window_first", window_first)):
-            if x is not None and len(x) != W:
-                raise FcError(f"{name} must have one entry a chunk")
-        kp = vp = sl = sp = None
+        # all host arrays one behind the other in a buffer, whose address the call takes
+        ints = array("i", q_chunk_row_off)
+        ints.extend(kv_visible_len)
+        begin = first = cache = sl = sp = None
+        for name, x in (("cache_len", cache_len if paged else None), ("kv_begin", kv_begin), ("window_first", window_first)):
+            if x is not None:
+                if len(x) != W:
+                    raise FcError(f"{name} must have one entry a chunk")
+                ints.extend(x)
+        kp = vp = None
         kh = kr = vh = vr = n_plain = n_seg = 0
         if K is not None and V is not None:
             n_plain = K.shape[1]
-            kp, kh, kr = self._rows(K, "K", (H_kv, n_plain, d), dtype)
-            vp, vh, vr = self._rows(V, "V", (H_kv, n_plain, d), dtype)
+            kv_shape = (H_kv, n_plain, d)
+            kp, kh, kr = self._rows(K, "K", kv_shape, dtype)
+            vp, vh, vr = self._rows(V, "V", kv_shape, dtype)
             if seg_phys_off is None:
                 if n_plain:
-                    n_seg, sl, sp = 1, _int32((0, n_plain)), _int32((0,))
+                    n_seg = 1
+                    ints.extend((0, n_plain, 0))
             else:
                 n_seg = len(seg_phys_off)
                 if len(seg_logical_off) != n_seg + 1:
                     raise FcError("seg_logical_off must have one entry more than seg_phys_off")
-                sl, sp = _int32(seg_logical_off), _int32(seg_phys_off)
+                ints.extend(seg_logical_off)
+                ints.extend(seg_phys_off)
         elif K is not None or V is not None:
             raise FcError("K and V: give both or neither")
+        off = ints.buffer_info()[0]
+        vis = off + 4 * (W + 1)
+        at = vis + 4 * W
+        if paged:
+            cache, at = at, at + 4 * W
+        if kv_begin is not None:
+            begin, at = at, at + 4 * W
+        if window_first is not None:
+            first, at = at, at + 4 * W
+        if n_seg:
+            sl, sp = at, at + 4 * (n_seg + 1)
         dp = _ATTN_FIELDS.pack(H_q, H_kv, d, W, qh, qr, kh, kr, vh, vr, oh, orow, n_plain, scale, impl)
-        off, vis, stream = _int32(q_chunk_row_off), _int32(kv_visible_len), self._raw_stream()
-        begin = None if kv_begin is None else _int32(kv_begin)
-        first = None if window_first is None else _int32(window_first)
-        lse_hs = 0
+        stream = self._raw_stream()
+        lse_p, lse_hs = None, 0
         if lse is not None:
             if lse.dim() != 2 or lse.shape[0] != H_q or lse.shape[1] < q_chunk_row_off[W] or lse.stride(1) != 1:
                 raise FcError("lse must be [H_q, rows] with contiguous rows")
-            lse_hs = max(lse.stride(0), 1)
+            lse_p, lse_hs = self._ptr(lse, "lse", torch.float32), max(lse.stride(0), 1)
         L, h = self._L, self._h
         ids, n = self._ptr(active_ids, "active_ids", torch.int32), self._ptr(n_active, "n_active", torch.int32)
-        lse_p, status = self._ptr(lse, "lse", torch.float32), self._ptr(status, "status", torch.int32)
+        status = self._ptr(status, "status", torch.int32)
 
         def call(ws):
-            tail = (ids, n, op, lse_p, lse_hs, status, self._ptr(ws, "ws"), 0 if ws is None else ws.numel())
+            wp, size = (None, 0) if ws is None else (self._ptr(ws, "ws"), ws.numel())
             if paged:
-                return L.fc_chunk_attention_kv8(h, stream, dp, qp, *paged[:4], kp, vp, dt, off, vis, n_sink, begin, first, sl, sp, n_seg, *tail)
-            return L.fc_chunk_attention_span(h, stream, dp, qp, kp, vp, dt, off, vis, n_sink, begin, sl, sp, n_seg, *tail)
+                return L.fc_chunk_attention_kv8(h, stream, dp, qp, self._store(pool, "pool"), tp, cs, cache, kp, vp, dt, off, vis, n_sink, begin,
+                                                first, sl, sp, n_seg, ids, n, op, lse_p, lse_hs, status, wp, size)
+            return L.fc_chunk_attention_span(h, stream, dp, qp, kp, vp, dt, off, vis, n_sink, begin, sl, sp, n_seg, ids, n, op, lse_p, lse_hs,
+                                             status, wp, size)
 
         rc = call(ws)
         if rc == -4 and ws is None:  # few rows mostly need no workspace, and a call that is refused has launched nothing
-            need = (L.fc_chunk_attention_kv8_workspace_bytes(h, dp, dt, paged[4].page, paged[2], paged[3], off, vis, n_sink, begin, first, sl, n_seg)
+            need = (L.fc_chunk_attention_kv8_workspace_bytes(h, dp, dt, pool.page, cs, cache, off, vis, n_sink, begin, first, sl, n_seg)
                     if paged else L.fc_chunk_attention_span_workspace_bytes(h, dp, dt, off, vis, n_sink, begin, sl, n_seg))
             rc = call(self._scratch("attention_span", need, stream))
         if rc:

@@ -94,6 +94,8 @@ struct TilePlan {
   double us;                        // estimate of the whole path
 };
 
+constexpr double kTilesUs = 12;  // what the path takes besides its work, measured
+
 // False if there are more rows to unpack than a tensor map's place can name.
 bool plan_tiles(const fc_ctx* ctx, const fc::SpanGeom& g, TilePlan& p) {
   // the tokens to unpack: of the shared sequence those that some chunk sees, else each chunk's own
@@ -165,9 +167,9 @@ bool plan_tiles(const fc_ctx* ctx, const fc::SpanGeom& g, TilePlan& p) {
   float last = 0.f;
   const int rest = (int)(items % ctx->sm_count);
   if (rest > 0) fc::split_parts(rest, ctx->sm_count, most_tiles, g.d, p.split.slots, &last);
-  // 12 us for the launches of the path, 1.8 us a key tile, the unpacking at 6.4 TB/s
+  // the launches of the path, 1.8 us a key tile, the unpacking at 6.4 TB/s
   const double whole = items > 0 ? (double)tiles / items : 0;
-  p.us = 12 + 1.8 * ((double)(items / ctx->sm_count) * whole + last) + 2.0 * g.H_kv * p.rows * g.d * 3 / 6.4e6;
+  p.us = kTilesUs + 1.8 * ((double)(items / ctx->sm_count) * whole + last) + 2.0 * g.H_kv * p.rows * g.d * 3 / 6.4e6;
   const size_t bytes = (size_t)g.H_kv * p.rows * g.d * 2, parts = (size_t)p.split.slots * 256;
   p.k = fc::attention_tc_workspace_bytes();
   p.v = p.k + fc::align_up(bytes, 256);
@@ -191,7 +193,7 @@ int plan(const fc_ctx* ctx, const fc_attn_desc* desc, fc::SpanGeom& g, Plan& p) 
   p.tiles = false;
   if (desc->impl != 2) {
     p.bytes = fc::span_rows_workspace(ctx, g);
-    if (desc->impl == 3 || g.f32) return FC_OK;
+    if (desc->impl == 3 || g.f32 || g.rows_us <= kTilesUs) return FC_OK;
   }
   const bool fits = maps_fit(desc) && plan_tiles(ctx, g, p.t);
   if (!fits && desc->impl == 2) return FC_ERR_UNSUPPORTED;

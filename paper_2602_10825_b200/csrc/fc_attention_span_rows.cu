@@ -1066,11 +1066,10 @@ int span_rows_launch(fc_ctx* ctx, cudaStream_t st, const SpanGeom& g, const void
   if (paged && ((rc = map_pages(ctx, &k8, g.pool.k_codes, g)) != FC_OK || (rc = map_pages(ctx, &v8, g.pool.v_codes, g)) != FC_OK)) return rc;
   if (plain && ((rc = map_rows(ctx, &k, K, g, g.k_hs, g.k_rs)) != FC_OK || (rc = map_rows(ctx, &v, V, g, g.v_hs, g.v_rs)) != FC_OK)) return rc;
   const dim3 grid((unsigned)blocks, (unsigned)g.H_kv);
-  constexpr int smem = kSmem;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = grid;
   cfg.blockDim = dim3(kThreads);
-  cfg.dynamicSmemBytes = smem;
+  cfg.dynamicSmemBytes = kSmem;  // which span_rows_setup allowed, and clusters of up to sixteen
   cfg.stream = st;
   cudaLaunchAttribute attr;
   attr.id = cudaLaunchAttributeClusterDimension;
@@ -1081,8 +1080,6 @@ int span_rows_launch(fc_ctx* ctx, cudaStream_t st, const SpanGeom& g, const void
 #define FC_SPAN_ROWS(T, D, NT)                                                                                                        \
   do {                                                                                                                                \
     static_assert((kWarps + 1) * 8 * NT * (D + 4) * 4 + 8 * NT * 8 <= kWarps * kRing, "what is joined takes the rings' place");       \
-    FC_CUDA_CHECK(cudaFuncSetAttribute(attention_span_rows_kernel<T, D, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));     \
-    if (g.cluster > 8) FC_CUDA_CHECK(cudaFuncSetAttribute(attention_span_rows_kernel<T, D, NT>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1)); \
     FC_CUDA_CHECK(cudaLaunchKernelEx(&cfg, attention_span_rows_kernel<T, D, NT>, k8, v8, k, v, (const T*)Q, (T*)O, g));                \
   } while (0)
 #define FC_SPAN_ROWS_PICK(T)                                                                       \
