@@ -650,6 +650,50 @@ def test_attention_over_entries_that_are_no_page(fc, ctx, dtype, impl):
     assert int(status) == 0
 
 
+@pytest.mark.parametrize("dtype, page", [(BF16, 16), (BF16, 128), (F32, 32)])
+def test_attention_of_very_many_heads(fc, ctx, dtype, page):
+    # more blocks than the device holds, each with more steps than its warps know of at a time
+    H, d, n = 470, 64, 9001
+    g = torch.Generator(device="cuda").manual_seed(1)
+    n_pages = -(-n // page)
+    codes = [torch.randint(0, 120, (n_pages, H, page, d), dtype=torch.uint8, device="cuda", generator=g) for _ in range(2)]
+    codes = [c | torch.randint(0, 2, c.shape, dtype=torch.uint8, device="cuda", generator=g) << 7 for c in codes]
+    scales = [(torch.rand((n_pages, H), device="cuda", generator=g) + 0.5) * s for s in (0.004, 0.01)]
+    pool, t = fc.Kv8Pool(codes[0], scales[0], codes[1], scales[1]), tables(n_pages, [n_pages], n_pages, 1)
+    Q = rand((H, 3, d), 2, 0.3, dtype)
+    O, lse, status = torch.zeros_like(Q), torch.zeros((H, 3), device="cuda"), status_word()
+    ctx.chunk_attention_kv8(Q, pool, i32(t), [n], None, None, [0, 3], [n], i32([0]), i32([1]), O, n_sink=40, kv_begin=[77], lse=lse, impl=3, status=status)
+    assert int(status) == 0
+    seen = np.asarray(pg.seen_tokens(n, 40, 77))
+    at, row = torch.from_numpy(t[0][seen // page]).cuda(), torch.from_numpy(seen % page).cuda()
+    for h in (0, 1, 233, 469):
+        kv = [(pg.code_values(c[at, h, row].cpu().numpy()) * f64(z[at, h])[:, None])[None] for c, z in zip(codes, scales)]
+        check(O[h:h + 1], lse[h:h + 1], f64(Q[h:h + 1]), [kv], [0, 3], [0], d ** -0.5, dtype, 3)
+
+
+@pytest.mark.parametrize("dtype, impl", IMPLS)
+def test_attention_of_a_span_over_many_segments(fc, ctx, dtype, impl):
+    # 62 segments in any order, some empty, some a row long, some that follow one another; what lies between them is NaN
+    rng, H, d = np.random.default_rng(5), 2, 128
+    lens = rng.integers(0, 40, 62)
+    lens[[3, 9, 10]] = 0, 1, 1
+    order, at, phys = rng.permutation(62), 1, np.zeros(62, int)
+    for s in order:
+        phys[s], at = at, at + lens[s] + int(rng.integers(0, 3))
+    log = np.concatenate([[0], np.cumsum(lens)])
+    row = np.concatenate([np.arange(n) + p for n, p in zip(lens, phys)]).astype(int)
+    K, V = (torch.full((H, at + 5, d), math.nan, dtype=dtype, device="cuda") for _ in range(2))
+    K[:, row], V[:, row] = rand((H, len(row), d), 1, 1.0, dtype), rand((H, len(row), d), 2, 1.0, dtype)
+    n = len(row)
+    off, vis, begin = [0, 3, 143, 148], [n, n - 100, n // 2], [n - 300, 201, 90]
+    Q, O = rand((H, 148, d), 3, 1.0, dtype), torch.zeros((H, 148, d), dtype=dtype, device="cuda")
+    status = status_word()
+    ctx.chunk_attention_span(Q, K, V, off, vis, log.tolist(), phys.tolist(), i32([0, 1, 2]), i32([3]), O, n_sink=70, kv_begin=begin, impl=impl, status=status)
+    assert int(status) == 0
+    kv = [tuple(f64(x)[:, row[pg.seen_tokens(v, 70, b)]] for x in (K, V)) for v, b in zip(vis, begin)]
+    check(O, None, f64(Q), kv, off, [0, 1, 2], d ** -0.5, dtype, impl)
+
+
 @pytest.mark.parametrize("dtype, impl", IMPLS)
 def test_attention_minds_only_entries_that_active_chunks_see(fc, ctx, dtype, impl):
     # a shared sequence of which nobody sees the middle; a batch in which a finished sequence has let go of its pages
