@@ -110,32 +110,27 @@ bool plan_tiles(const fc_ctx* ctx, const fc::SpanGeom& g, TilePlan& p) {
   p.jobs.W = g.W;
   for (int c0 = 0; c0 < g.W; c0 += shared ? g.W : 1) {
     const int c1 = shared ? g.W : c0 + 1;
-    // what is seen, in order; pieces that meet become one job
-    struct Piece {
-      int32_t lo, hi;
-      uint64_t who;
-    } piece[2 * FC_MAX_CHUNKS];
+    // What is seen, in order, cut wherever the set of chunks that see it changes: a job is brought only if one of its chunks is active, and
+    // entries that nobody needs are nobody's concern.  Jobs that meet lie next to each other, so that a chunk's range stays one.
+    struct End {
+      int32_t at;
+      uint64_t who;  // begins or ends to see
+    } end[4 * FC_MAX_CHUNKS];
     int n = 0;
     for (int c = c0; c < c1; ++c)
       for (int i = 0; i < 2; ++i)
-        if (g.hi[i][c] > g.lo[i][c] && fc::span_rows(g, c) > 0) piece[n++] = {g.lo[i][c], g.hi[i][c], 1ull << c};
-    std::sort(piece, piece + n, [](const Piece& a, const Piece& b) { return a.lo < b.lo; });
+        if (g.hi[i][c] > g.lo[i][c] && fc::span_rows(g, c) > 0) end[n++] = {g.lo[i][c], 1ull << c}, end[n++] = {g.hi[i][c], 1ull << c};
+    std::sort(end, end + n, [](const End& a, const End& b) { return a.at < b.at; });
     const int first_job = p.jobs.n;
-    for (int k = 0; k < n; ++k) {
-      fc::Kv8Job* last = p.jobs.n > first_job ? &p.jobs.job[p.jobs.n - 1] : nullptr;
-      if (last && piece[k].lo <= last->first + last->n) {
-        last->n = std::max(last->n, piece[k].hi - last->first);
-        p.jobs.needed[p.jobs.n - 1] |= piece[k].who;
-      } else {
-        p.jobs.needed[p.jobs.n] = piece[k].who;
-        p.jobs.job[p.jobs.n++] = {shared ? 0 : c0, piece[k].lo, piece[k].hi - piece[k].lo, 0};
-      }
-    }
-    for (int j = first_job; j < p.jobs.n; ++j) {
-      fc::Kv8Job& job = p.jobs.job[j];
-      if ((int64_t)p.rows + job.n > INT32_MAX - 4096) return false;
-      job.dst_row = p.rows;
-      p.rows += job.n;
+    uint64_t who = 0;
+    for (int k = 0; k + 1 < n; ++k) {
+      who ^= end[k].who;
+      const int64_t len = (int64_t)end[k + 1].at - end[k].at;
+      if (who == 0 || len == 0) continue;
+      if (p.rows + len > INT32_MAX - 4096) return false;
+      p.jobs.needed[p.jobs.n] = who;
+      p.jobs.job[p.jobs.n++] = {shared ? 0 : c0, end[k].at, (int32_t)len, p.rows};
+      p.rows += (int)len;
     }
     for (int c = c0; c < c1; ++c)
       for (int i = 0; i < 2; ++i) {
@@ -143,10 +138,10 @@ bool plan_tiles(const fc_ctx* ctx, const fc::SpanGeom& g, TilePlan& p) {
           p.spans.lo[i][c] = p.spans.hi[i][c] = 0;
           continue;
         }
-        int j = first_job;
-        while (g.hi[i][c] > p.jobs.job[j].first + p.jobs.job[j].n) ++j;
-        p.spans.lo[i][c] += p.jobs.job[j].dst_row - p.jobs.job[j].first;
-        p.spans.hi[i][c] += p.jobs.job[j].dst_row - p.jobs.job[j].first;
+        const fc::Kv8Job* job = std::upper_bound(p.jobs.job + first_job, p.jobs.job + p.jobs.n, g.lo[i][c],
+                                                 [](int32_t token, const fc::Kv8Job& x) { return token < x.first; }) - 1;
+        p.spans.lo[i][c] += job->dst_row - job->first;
+        p.spans.hi[i][c] += job->dst_row - job->first;
       }
   }
   // grouped heads share their key tiles where whole groups fill a tile of 128 rows

@@ -243,6 +243,7 @@ kv8_append_kernel(const T* __restrict__ K, const T* __restrict__ V, const __grid
 
 struct UnpackGeom {
   fc::Kv8Jobs jobs;
+  int32_t block_end[fc::kKv8Jobs];  // running count of the jobs' blocks, so that a short one beside a long one has no empty blocks
   int64_t k_hs, k_rs, v_hs, v_rs, table_cs, rows;  // rows of a head of the destination
   fc::Kv8View src;
   const int32_t* table;
@@ -275,11 +276,17 @@ kv8_unpack_kernel(T* __restrict__ K, T* __restrict__ V, const __grid_constant__ 
   constexpr int kVec = sizeof(C), kRowVecs = D / kVec, R = kUnpackThreads / kRowVecs;
   fc::pdl_launch_dependents();
   const int w = threadIdx.x % kRowVecs, h = blockIdx.y;
-  const bool is_v = blockIdx.z & 1;
+  const bool is_v = blockIdx.z != 0;
   if (g.clear && threadIdx.x == 0 && blockIdx.x == 0 && h == 0 && blockIdx.z == 0) *g.clear = 0;
   T* dst = is_v ? V : K;
   if (!dst) return;
-  const fc::Kv8Job job = g.jobs.job[blockIdx.z >> 1];
+  int j = 0;  // the first job whose end is behind this block
+  for (int end = g.jobs.n - 1; j < end;) {
+    const int mid = (j + end) / 2;
+    if (g.block_end[mid] > (int)blockIdx.x) end = mid;
+    else j = mid + 1;
+  }
+  const fc::Kv8Job job = g.jobs.job[j];
   if (g.jobs.active_ids) {
     const int lane = threadIdx.x % 32, n = min(max(*g.jobs.n_active, 0), g.jobs.W);
     uint64_t mine = 0;
@@ -288,9 +295,9 @@ kv8_unpack_kernel(T* __restrict__ K, T* __restrict__ V, const __grid_constant__ 
       if (c >= 0 && c < g.jobs.W) mine |= 1ull << c;
     }
     const uint32_t lo = __reduce_or_sync(0xffffffffu, (uint32_t)mine), hi = __reduce_or_sync(0xffffffffu, (uint32_t)(mine >> 32));
-    if (!(((uint64_t)hi << 32 | lo) & g.jobs.needed[blockIdx.z >> 1])) return;
+    if (!(((uint64_t)hi << 32 | lo) & g.jobs.needed[j])) return;
   }
-  const int r0 = blockIdx.x * (kUnpackRows * R) + threadIdx.x / kRowVecs;  // below 2^31, as the tokens are
+  const int r0 = ((int)blockIdx.x - (j > 0 ? g.block_end[j - 1] : 0)) * (kUnpackRows * R) + threadIdx.x / kRowVecs;  // below 2^31, as the tokens are
   if (r0 >= job.n) return;
   uint8_t* codes = fc::kv8_block(is_v ? g.src.v_codes : g.src.k_codes, g.src, 0, h);
   float* scales = fc::kv8_scale(is_v ? g.src.v_scales : g.src.k_scales, g.src, 0, h);
@@ -351,14 +358,13 @@ namespace fc {
 int kv8_unpack_launch(cudaStream_t st, const Kv8View& src, int H, int d, const int32_t* table, int64_t table_cs, const Kv8Jobs& jobs,
                       void* K_dst, void* V_dst, int dtype, int64_t k_hs, int64_t k_rs, int64_t v_hs, int64_t v_rs,
                       uint32_t* status, uint32_t* clear) {
-  int n = 0;
-  for (int i = 0; i < jobs.n; ++i) n = std::max(n, jobs.job[i].n);
-  if (n == 0 || (!K_dst && !V_dst)) return FC_OK;
-  int64_t end = 0;
+  int64_t end = 0, blocks = 0;
   for (int i = 0; i < jobs.n; ++i) end = std::max<int64_t>(end, (int64_t)jobs.job[i].dst_row + jobs.job[i].n);
-  UnpackGeom g = {jobs, k_hs, k_rs, v_hs, v_rs, table_cs, end, src, table, status, clear};
+  UnpackGeom g = {jobs, {}, k_hs, k_rs, v_hs, v_rs, table_cs, end, src, table, status, clear};
   const int rows = kUnpackRows * kUnpackThreads / (d / (dtype == FC_F32 ? 4 : 8));
-  const dim3 grid((unsigned)((n + (int64_t)rows - 1) / rows), (unsigned)H, 2u * jobs.n);
+  for (int i = 0; i < jobs.n; ++i) g.block_end[i] = (int32_t)(blocks += ((int64_t)jobs.job[i].n + rows - 1) / rows);
+  if (blocks == 0 || (!K_dst && !V_dst)) return FC_OK;
+  const dim3 grid((unsigned)blocks, (unsigned)H, 2);
 #define FC_UNPACK(T, D) kv8_unpack_kernel<T, D><<<grid, kUnpackThreads, 0, st>>>((T*)K_dst, (T*)V_dst, g)
   if (dtype == FC_F32) { if (d == 128) FC_UNPACK(float, 128); else FC_UNPACK(float, 64); }
   else { if (d == 128) FC_UNPACK(__nv_bfloat16, 128); else FC_UNPACK(__nv_bfloat16, 64); }

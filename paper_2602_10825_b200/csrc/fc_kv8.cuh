@@ -79,7 +79,7 @@ __device__ __forceinline__ float half_hi(uint32_t w) {
 struct Kv8Job {
   int32_t seq, first, n, dst_row;
 };
-constexpr int kKv8Jobs = 2 * FC_MAX_CHUNKS;
+constexpr int kKv8Jobs = 3 * FC_MAX_CHUNKS;  // what lies between the ends of as many windows, and of as many ranges from token 0 on
 struct Kv8Jobs {
   int32_t n;
   Kv8Job job[kKv8Jobs];

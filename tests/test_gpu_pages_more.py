@@ -1,0 +1,72 @@
+"""Calls around the paged 8-bit store that tests/test_gpu_pages.py does not make, against the same plain forms in 64 bits (page_forms.py);
+tolerances are derived as at its head, and where a test says so."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import page_forms as pg
+from test_gpu_pages import (BF16, F32, HALF, IMPLS, check, ctx, f64, fc, filled_pool, i32, numpy_pool, rand, same_pages, same_pool,  # noqa: F401
+                            status_word, tables)
+
+pytestmark = pytest.mark.gpu
+
+
+# ------------------------------------------------------------------------------------ entries that nobody needs
+
+@pytest.mark.parametrize("dtype, impl", IMPLS)
+@pytest.mark.parametrize("vis, begin, sink, active", [
+    ([160, 160], [20, 100], 0, [1]),                    # windows that overlap
+    ([100, 160], [20, 100], 0, [1]),                    # that meet
+    ([160, 150, 140], [10, 70, 133], 5, [1]),           # one inside the other, and first tokens that all see
+    ([90, 150, 160], [40, 60, 100], 70, [0]),           # first tokens that reach into the others' windows
+    ([33, 160, 64, 160], [0, 50, 31, 90], 3, [2, 0]),
+])
+def test_attention_over_a_shared_sequence_minds_what_active_chunks_see(fc, ctx, vis, begin, sink, active, dtype, impl):
+    # the pages that only inactive chunks see have been let go of: nobody asks for them, nothing is reported
+    H, d, page, n, W = 2, 64, 16, 160, len(vis)
+    pool, status = filled_pool(fc, 10, H, page, d, 1), status_word()
+    where = numpy_pool(pool)
+    live = {j // page for c in active for j in pg.seen_tokens(vis[c], sink, begin[c])}
+    t = [e if e in live else (-1, 77)[e % 2] for e in range(10)]
+    assert any(j // page not in live for c in range(W) for j in pg.seen_tokens(vis[c], sink, begin[c]))
+    off = [3 * c for c in range(W + 1)]
+    Q = rand((H, off[-1], d), 2, 1.0, dtype)
+    O = torch.full_like(Q, 9.0)
+    ids, count = i32(active + [-1] * (W - len(active))), i32([len(active)])
+    args = (None, None, off, vis, ids, count, O)
+    ctx.chunk_attention_kv8(Q, pool, i32([t]), [n] * W, *args, n_sink=sink, kv_begin=begin, impl=impl, status=status)
+    assert int(status) == 0
+    kv = [tuple(where.rows(w, t, pg.seen_tokens(vis[c], sink, begin[c])) for w in (0, 1)) if c in active else None for c in range(W)]
+    check(O, None, f64(Q), kv, off, active, d ** -0.5, dtype, impl, 9.0)
+    # one that an active chunk does see is reported
+    t[pg.seen_tokens(vis[active[0]], sink, begin[active[0]])[-1] // page] = -1
+    ctx.chunk_attention_kv8(Q, pool, i32([t]), [n] * W, *args, n_sink=sink, kv_begin=begin, impl=impl, status=status)
+    assert int(status) == fc.STATUS_BITS["bad_index"]
+
+
+@pytest.mark.parametrize("page", [16, 128])
+@pytest.mark.parametrize("dtype, impl", IMPLS)
+def test_attention_of_many_chunks_over_a_shared_sequence(fc, ctx, dtype, impl, page):
+    # 64 windows, each beginning and ending at a token of its own: as many pieces as there can be; some meet, some are inside others
+    H, d, n, W, sink = 2, 64, 2000, 64, 9
+    rng = np.random.default_rng(3)
+    begin = rng.permutation(1800)[:W].tolist()
+    vis = [min(n, b + int(k)) for b, k in zip(begin, rng.integers(1, 500, W))]
+    vis[7], begin[9], vis[11] = begin[8], vis[10], 5  # meeting; ending among the first tokens
+    active = sorted(rng.permutation(W)[:20].tolist())
+    n_pages = -(-n // page)
+    pool, status = filled_pool(fc, n_pages, H, page, d, 1), status_word()
+    where = numpy_pool(pool)
+    seen = [pg.seen_tokens(vis[c], sink, begin[c]) for c in range(W)]
+    live = {j // page for c in active for j in seen[c]}
+    t = [p if e in live else -1 for e, p in enumerate(tables(n_pages, [n_pages], n_pages, 4)[0])]
+    off = [2 * c for c in range(W + 1)]
+    Q = rand((H, off[-1], d), 2, 1.0, dtype)
+    O = torch.full_like(Q, 9.0)
+    ctx.chunk_attention_kv8(Q, pool, i32([t]), [n] * W, None, None, off, vis, i32(active), i32([len(active)]), O, n_sink=sink, kv_begin=begin, impl=impl,
+                            status=status)
+    assert int(status) == 0
+    kv = [tuple(where.rows(w, t, seen[c]) for w in (0, 1)) if c in active else None for c in range(W)]
+    check(O, None, f64(Q), kv, off, active, d ** -0.5, dtype, impl, 9.0)
