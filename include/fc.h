@@ -620,6 +620,8 @@ int fc_pages_compact(fc_ctx* ctx, void* stream, const fc_kv8_pool* pool, int H, 
  * in fp32.  Softmax weights are rounded on their way to V: for fp32 tensors by 2^-22 at most; by the tcgen05 kernel to bf16; by the
  * kernel for few rows to fp16 over pages (2^-11 of a weight, or 2^-32 of the row's largest so far where that is more) and to bf16 over
  * plain rows, where what that leaves is taken along if no tile has more than eight rows times heads of a group.
+ * Before they are divided by their sum, weights are at most 1 in the kernel for few rows and at most 2^8 in the tcgen05 kernel; the sum of
+ * weights times values has to stay below 2^128, which it does where the tokens that are seen, times the largest |value|, times that bound do.
  * What lies in tokens that a chunk does not see never reaches its rows, whatever it is.  A NaN in a token that is seen makes what it reaches NaN, and so
  * does an infinity in Q.  Head strides of K and V are not 0 where there are several heads.
  * An entry outside [0, n_pages) that is needed sets FC_DEV_BAD_INDEX; K and V of its tokens count as zeros.

@@ -15,7 +15,7 @@
 // bf16 number of any size, is brought into fp16 by a power of two of its row that puts the row's largest element at 2^14: all of its bits are
 // kept down to 2^-29 of that.  The keys' scale goes into the logits, the values' scale multiplies a step's sum before it is
 // added to O, which is in fp32.  Weights are taken 2^7 times larger than their reference asks for, so that fp16's smallest step,
-// 2^-24, is 2^-31 of the largest weight.  A step is about 215 instructions for each 16 keys of one to eight rows, which is what a block alone on
+// 2^-24, is 2^-31 of the largest weight; the values' scale, or over plain rows the weight, makes up for it.  A step is about 215 instructions for each 16 keys of one to eight rows, which is what a block alone on
 // its SM is bound by (0.45 us for its four warps' 64 keys; with 16 keys a step, and a barrier, a look-up, a vote and a copy for each, 0.62); from
 // one and a half blocks an SM on it is the bandwidth: one token over 28080 tokens of 24 heads 34.0 us, the same without the arithmetic 32, the
 // bytes' own time 26.3.
@@ -43,6 +43,7 @@ constexpr int kMaxCluster = 16;      // blocks of a cluster
 constexpr int kSmem = kWarps * (kRing + kTable) + 1024;  // of a block, the rings on a 1024-byte boundary
 constexpr float kSlack = 8.f;        // log2 units by which a logit may pass the maximum before that moves
 constexpr float kLift = 7.f;         // weights are 2^kLift at the maximum
+constexpr float kUnit = 32768.f;     // 2^(kLift + kSlack), the most that a weight can be: O is kept divided by it, so that it passes fp32's range no sooner than weights of 1 would
 constexpr int blocks_per_sm(int nt) { return nt == 1 ? 3 : 2; }
 constexpr int kPagedCost = 2;        // cost of a step over pages, and over plain rows
 template <typename T> constexpr int kPlainCost = sizeof(T) == 4 ? 3 : 2;
@@ -67,7 +68,7 @@ __device__ __forceinline__ uint32_t cvt_f16x2(float lo, float hi) {
 }
 __device__ __forceinline__ float pow2(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }  // -126 <= e <= 127
 
-// What a warp carries along its keys: O^T, this lane's share of the sums, and per row the reference of its exponents (log2
+// What a warp carries along its keys: O^T over kUnit, this lane's share of the sums, and per row the reference of its exponents (log2
 // units) and the logit above which it moves.  A row that has met no finite logit yet has move_at = -inf and the reference 0:
 // weights of -inf are 0 then, and a NaN stays one.
 template <int D, int NT> struct State {
@@ -154,10 +155,10 @@ __device__ __forceinline__ float4 cluster_load4(uint32_t at, int rank) {
   return x;
 }
 
-// Four elements of virtual row v of chunk c: a sum of weights times values, its reference and the sum of the weights.
+// Four elements of virtual row v of chunk c: a sum of weights times values over kUnit, its reference and the sum of the weights.
 template <typename T>
 __device__ __forceinline__ void write_row(T* O, const fc::SpanGeom& g, int c, int hk, int v, int d4, float4 o, float ref, float l) {
-  const float inv = l > 0.f ? 1.f / l : (l == l ? 0.f : l);
+  const float inv = l > 0.f ? kUnit / l : (l == l ? 0.f : l);
   const int h = hk * g.group + v % g.group;
   const int64_t row = g.q_row_off[c] + v / g.group;
   if (!fc::bounds_ok(row >= 0 && row < g.q_row_off[g.W] && h >= 0 && h < g.H_q, g.status)) return;
@@ -170,7 +171,7 @@ __device__ __forceinline__ void write_row(T* O, const fc::SpanGeom& g, int c, in
 // one page has them; and the scales of K and V of the halves.
 struct __align__(16) PagedStep {
   int page[2], place, pad;
-  float ks[2], vs[2];
+  float ks[2], vs[2];  // vs / kUnit
 };
 static_assert(sizeof(PagedStep) * 64 == kTable, "two groups of 32 steps");
 
@@ -302,7 +303,7 @@ attention_span_rows_kernel(const __grid_constant__ CUtensorMap map_k8, const __g
     for (int e = 0; e < 2; ++e)
       if (x.page[e] >= 0) {
         x.ks[e] = __ldg(g.pool.k_scales + x.page[e] * g.pool.scale_ps + hk * g.pool.scale_hs);
-        x.vs[e] = __ldg(g.pool.v_scales + x.page[e] * g.pool.scale_ps + hk * g.pool.scale_hs);
+        x.vs[e] = __ldg(g.pool.v_scales + x.page[e] * g.pool.scale_ps + hk * g.pool.scale_hs) * (1.f / kUnit);  // exact, below the normal numbers too
       }
   };
   const uint32_t bar_s = bar(0, 0, 0);
@@ -621,6 +622,10 @@ attention_span_rows_kernel(const __grid_constant__ CUtensorMap map_k8, const __g
         for (int k = 0; k < 4; ++k) s[t][k] = (kParts<T> > 1 ? s[t][k] + rest[t][k] : s[t][k]) * scale_log2;
       if (hi == kStep) weigh_logits<D, NT, false, 1>(st, s1, lane, 0, kStep);
       else weigh_logits<D, NT, true, 1>(st, s1, lane, 0, hi);
+#pragma unroll
+      for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) s[t][k] *= 1.f / kUnit;
       uint32_t pa[kWeightParts<T, NT>][NT][2];
 #pragma unroll
       for (int t = 0; t < NT; ++t) {

@@ -70,3 +70,42 @@ def test_attention_of_many_chunks_over_a_shared_sequence(fc, ctx, dtype, impl, p
     assert int(status) == 0
     kv = [tuple(where.rows(w, t, seen[c]) for w in (0, 1)) if c in active else None for c in range(W)]
     check(O, None, f64(Q), kv, off, active, d ** -0.5, dtype, impl, 9.0)
+
+
+# ------------------------------------------------------------------------------------ numbers of any size
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("size", [-90, 0, 100, 114, 121])
+@pytest.mark.parametrize("n, plain, rows", [(100, 0, 3), (60, 40, 11), (0, 100, 3), (0, 100, 11), (1, 0, 1), (0, 1, 1)])
+def test_attention_values_of_any_size(fc, ctx, n, plain, rows, size, dtype, d):
+    # values of up to 2^121 (of a single token: up to the largest that there are), a sum of whose number times their size stays below 2^128
+    H, page, up = 2, 32, 127 if n + plain == 1 and size == 121 else size
+    pool, t = filled_pool(fc, 4, H, page, d, 1), [2, 0, 3, 1]
+    pool.v_codes[pool.v_codes.bitwise_and(0x7f) > 0x78] = 0xf8  # magnitudes up to 256
+    pool.v_scales[:] = 2.0 ** (up - 8)
+    K, V = rand((H, plain, d), 3, 1.0, dtype), (rand((H, plain, d), 4, 1.0, F32).clamp(-4, 4) / 4 * 1.99 * 2.0 ** (up - 1)).to(dtype)
+    where = numpy_pool(pool)
+    kv = [np.concatenate([where.rows(w, t, range(n)), f64(y)], 1) for w, y in ((0, K), (1, V))]
+    assert np.abs(kv[1]).max() * (n + plain) < 2.0 ** 128
+    Q = rand((H, rows, d), 2, 2.0, dtype)
+    O, lse = torch.zeros_like(Q), torch.zeros((H, rows), device="cuda")
+    ctx.chunk_attention_kv8(Q, pool, i32([t]), [n], *((K, V) if plain else (None, None)), [0, rows], [n + plain], i32([0]), i32([1]), O, lse=lse, impl=3)
+    unit = 2.0 ** -up  # an exact change of scale, so that the tolerances mean what they say
+    check(O.double() * unit, lse, f64(Q), [(kv[0], kv[1] * unit)], [0, rows], [0], d ** -0.5, dtype, 3)
+
+
+@pytest.mark.parametrize("parts", [1, 40])
+def test_attention_values_of_any_size_in_parts(fc, ctx, parts):
+    # the same through the joins: of a cluster's blocks, and of chunks of very different lengths
+    H, d, page, n = 1, 64, 128, 128 * 20 * parts
+    pool = filled_pool(fc, 20 * parts, H, page, d, 1)
+    pool.v_codes.bitwise_and_(0x7f).clamp_(max=0x78)  # of one sign, so that the sums grow
+    pool.v_scales[:] = 2.0 ** (110 - 8)  # times the tokens: below 2^128
+    t = list(range(20 * parts))
+    for dtype in (BF16, F32):
+        Q, off, vis = rand((H, 9, d), 2, 0.01, dtype), [0, 1, 9], [n, 100]  # weights that are nearly the same
+        O = torch.zeros_like(Q)
+        ctx.chunk_attention_kv8(Q, pool, i32([t]), vis, None, None, off, vis, i32([0, 1]), i32([2]), O, impl=3)
+        kv = [tuple(numpy_pool(pool).rows(w, t, range(v)) * (1.0, 2.0 ** -110)[w] for w in (0, 1)) for v in vis]
+        check(O.double() * 2.0 ** -110, None, f64(Q), kv, off, [0, 1], d ** -0.5, dtype, 3)
