@@ -617,7 +617,8 @@ int fc_pages_compact(fc_ctx* ctx, void* stream, const fc_kv8_pool* pool, int H, 
  *                    HOST [W] or NULL (all 0).  Tokens that no chunk sees need no page.
  *   K, V, seg_*      as in fc_chunk_attention_kv4: the plain tokens; n_seg 0 if there are none.
  * Everything else is as in fc_chunk_attention_kv4: the active list, grouped heads, rows of inactive chunks.  Logits, maxima, sums and outputs are kept
- * in fp32.  Softmax weights are rounded on their way to V: for fp32 tensors by 2^-22 at most; by the tcgen05 kernel to bf16; by the
+ * in fp32.  Softmax weights are rounded on their way to V: for fp32 tensors by 2^-22 at most (over pages by 2^-43 of the row's largest so far
+ * where that is more); by the tcgen05 kernel to bf16; by the
  * kernel for few rows to fp16 over pages (2^-11 of a weight, or 2^-32 of the row's largest so far where that is more) and to bf16 over
  * plain rows, where what that leaves is taken along if no tile has more than eight rows times heads of a group.
  * Before they are divided by their sum, weights are at most 1 in the kernel for few rows and at most 2^8 in the tcgen05 kernel; the sum of

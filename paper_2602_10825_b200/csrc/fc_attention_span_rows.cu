@@ -20,7 +20,8 @@
 // one and a half blocks an SM on it is the bandwidth: one token over 28080 tokens of 24 heads 34.0 us, the same without the arithmetic 32, the
 // bytes' own time 26.3.
 // Plain rows go through the products of their own type (bf16, or for fp32 the six largest products of three bf16 parts each).
-// fp32 over pages: two fp16 parts of Q, and of the weights, leave out 2^-23 of a number at most.
+// fp32 over pages: two fp16 parts of Q, and of the weights, leave out at most 2^-23 of a number, or, where that is more, 2^-39 of the row's largest
+// element of Q and 2^-43 of its largest weight.
 // The maximum is lazy (it moves when a logit passes it by 2^8), so that the usual step has no shuffles and no rescaling.
 #include <algorithm>
 #include <climits>
@@ -50,6 +51,7 @@ template <typename T> constexpr int kPlainCost = sizeof(T) == 4 ? 3 : 2;
 
 template <typename T> constexpr int kParts = sizeof(T) == 4 ? 3 : 1;       // bf16 parts of Q, K and V over plain rows
 template <typename T> constexpr int kHalves = sizeof(T) == 4 ? 2 : 1;      // fp16 parts of Q and of the weights over pages
+constexpr float kRest = 2048.f;      // the weights' second part is taken 2^11 times larger: as large as the first at most, and fp16's smallest step is 2^-35 then
 // Weights over plain rows: bf16 rounds one by up to 2^-8, as much again as the output's own rounding; for up to eight rows the rest is taken along.
 template <typename T, int NT> constexpr int kWeightParts = sizeof(T) == 4 ? 3 : (NT == 1 ? 2 : 1);
 
@@ -447,8 +449,8 @@ attention_span_rows_kernel(const __grid_constant__ CUtensorMap map_k8, const __g
           pa[e][0][t][0] = transpose8x8(a);
           pa[e][0][t][1] = transpose8x8(b);
           if constexpr (kHalves<T> == 2) {
-            pa[e][1][t][0] = transpose8x8(cvt_f16x2(s[e][t][0] - fc::half_lo(a), s[e][t][1] - fc::half_hi(a)));
-            pa[e][1][t][1] = transpose8x8(cvt_f16x2(s[e][t][2] - fc::half_lo(b), s[e][t][3] - fc::half_hi(b)));
+            pa[e][1][t][0] = transpose8x8(cvt_f16x2((s[e][t][0] - fc::half_lo(a)) * kRest, (s[e][t][1] - fc::half_hi(a)) * kRest));
+            pa[e][1][t][1] = transpose8x8(cvt_f16x2((s[e][t][2] - fc::half_lo(b)) * kRest, (s[e][t][3] - fc::half_hi(b)) * kRest));
           }
         }
 #pragma unroll
@@ -478,18 +480,18 @@ attention_span_rows_kernel(const __grid_constant__ CUtensorMap map_k8, const __g
 #pragma unroll
             for (int t = 0; t < NT; ++t) {
               float(&o)[4] = st.o[t][4 * j + 2 * h + k];
-              float x[4];
 #pragma unroll
-              for (int e = 0; e < 2; ++e) {
+              for (int w = kHalves<T> - 1; w >= 0; --w) {
+                float x[4];
 #pragma unroll
-                for (int w = kHalves<T> - 1; w >= 0; --w) {
-                  if (w == kHalves<T> - 1 && (kPart || e == 0)) mma_f16_first(x, a[e][0], a[e][1], a[e][2], a[e][3], pa[e][w][t][0], pa[e][w][t][1]);
+                for (int e = 0; e < 2; ++e) {
+                  if (kPart || e == 0) mma_f16_first(x, a[e][0], a[e][1], a[e][2], a[e][3], pa[e][w][t][0], pa[e][w][t][1]);
                   else mma_f16(x, a[e][0], a[e][1], a[e][2], a[e][3], pa[e][w][t][0], pa[e][w][t][1]);
-                }
-                if (kPart || e == 1) {
-                  const float vs = kPart && e == 0 ? scales.z : scales.w;
+                  if (kPart || e == 1) {
+                    const float vs = (kPart && e == 0 ? scales.z : scales.w) * (w == 1 ? 1.f / kRest : 1.f);
 #pragma unroll
-                  for (int i = 0; i < 4; ++i) o[i] = fmaf(vs, x[i], o[i]);
+                    for (int i = 0; i < 4; ++i) o[i] = fmaf(vs, x[i], o[i]);
+                  }
                 }
               }
             }

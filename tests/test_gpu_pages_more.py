@@ -109,3 +109,28 @@ def test_attention_values_of_any_size_in_parts(fc, ctx, parts):
         ctx.chunk_attention_kv8(Q, pool, i32([t]), vis, None, None, off, vis, i32([0, 1]), i32([2]), O, impl=3)
         kv = [tuple(numpy_pool(pool).rows(w, t, range(v)) * (1.0, 2.0 ** -110)[w] for w in (0, 1)) for v in vis]
         check(O.double() * 2.0 ** -110, None, f64(Q), kv, off, [0, 1], d ** -0.5, dtype, 3)
+
+
+@pytest.mark.parametrize("d, page", [(64, 32), (128, 16), (128, 128)])
+@pytest.mark.parametrize("rows", [1, 8, 13])
+def test_attention_small_weights_of_fp32_rows(fc, ctx, rows, d, page):
+    # in every 32 keys one of weight 1, whose value is 0, beside 31 of weight e^-L: the output is what the small weights carry
+    n = 32 * 40
+    pool = fc.Kv8Pool.empty(n // page, 1, page, d)
+    for c in (pool.k_codes, pool.v_codes):
+        c.fill_(0)
+    pool.k_scales.fill_(1.0), pool.v_scales.fill_(1.0)
+    token = torch.arange(n, device="cuda").view(n // page, 1, page)
+    pool.k_codes[..., 0][token % 32 == 5] = 0x38            # 1
+    pool.v_codes[..., : d][token % 32 != 5] = 0x3c          # 1.5
+    L = torch.linspace(11, 18, rows, dtype=F32) if rows > 1 else torch.tensor([17.3])
+    Q, O = torch.zeros((1, rows, d), dtype=F32, device="cuda"), torch.zeros((1, rows, d), dtype=F32, device="cuda")
+    Q[0, :, 0] = L.cuda()
+    ctx.chunk_attention_kv8(Q, pool, i32([list(range(n // page))]), [n], None, None, [0, rows], [n], i32([0]), i32([1]), O, scale=1.0)
+    L = L.double().numpy()[:, None]
+    e = 31 * np.exp(-L)
+    want = 1.5 * e / (1 + e)
+    # The logit is one product: Q's parts leave out 2^-23 of it, and four roundings 2^-24 each; all in the exponent.  The exponential and a weight's
+    # parts 2^-22 each, the sums n 2^-24, and a weight that is small for fp16's parts 2^-43 of the largest.
+    rel = L * (2.0 ** -23 + 4 * 2.0 ** -24) + 2 * 2.0 ** -22 + n * 2.0 ** -24 + 2.0 ** -24
+    assert (np.abs(f64(O)[0] - want) <= rel * want + 1.5 * 31 * 2.0 ** -43).all()
