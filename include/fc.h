@@ -582,7 +582,8 @@ int fc_pages_drop(fc_ctx* ctx, void* stream, int32_t* ref, int n_pages, int32_t*
  *   src, dst         HOST [n], rows of the table: 0 <= . < n_seq; no dst twice, and none among the src.
  *   tokens           HOST [n], >= 0; ceil(tokens / page) <= table_cs.  n <= FC_MAX_CHUNKS.
  * Where no page is left for a copy, the entry gets -1 and FC_DEV_NO_PAGES is set.  An entry of src that names no page of the pool
- * sets FC_DEV_BAD_INDEX and becomes -1.  H, d as for fc_kv8_append.  Workspace: fc_pages_workspace_bytes(n_pages).
+ * sets FC_DEV_BAD_INDEX and becomes -1.  So does one that names a free page; filled in part it becomes a page of dst's own into which
+ * nothing is copied.  H, d as for fc_kv8_append.  Workspace: fc_pages_workspace_bytes(n_pages).
  *
  * fc_pages_compact — the n used pages of the pool become pages 0 .. n - 1: those with numbers from n on, in ascending order, move into
  * the free ones below n, in ascending order; counts go with them, and entries 0 .. entries - 1 of all n_seq rows

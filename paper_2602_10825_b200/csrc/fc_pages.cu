@@ -109,8 +109,8 @@ pages_drop_kernel(int32_t* __restrict__ ref, int n_pages, int32_t* __restrict__ 
   if (bad && status) atomicOr(status, (uint32_t)FC_DEV_BAD_INDEX);
 }
 
-// What the copying kernel finds in the workspace: the number of copies, the number of used pages, then pairs (from, to), and, for
-// compact, the new place of each page.
+// What the copying kernel finds in the workspace: the number of copies, the number of used pages, then pairs (from, to; from -1: none),
+// and, for compact, the new place of each page.
 struct Copies {
   int32_t* n;     // [2]
   int2* pair;
@@ -135,39 +135,57 @@ struct Forks {
 __global__ void __launch_bounds__(kThreads)
 pages_fork_kernel(int32_t* __restrict__ ref, int n_pages, int32_t* __restrict__ table, const __grid_constant__ Forks f, Copies copies,
                   uint32_t* __restrict__ status) {
-  __shared__ int32_t part_s[FC_MAX_CHUNKS], from_s[FC_MAX_CHUNKS], n_part;  // forks that copy a page, and from which
+  __shared__ int32_t look_s[FC_MAX_CHUNKS], part_s[FC_MAX_CHUNKS], from_s[FC_MAX_CHUNKS], n_part;  // forks that copy a page, and from which
+  constexpr int32_t kNoCopy = -2;
   fc::pdl_launch_dependents();
   const int tid = threadIdx.x, lane = tid % 32, warp = tid / 32;
   bool bad = false;
+  // A page that is free is not counted, so that every fork finds it free.
+  constexpr int kAtOnce = 4;
   for (int i = warp; i < f.n; i += kThreads / 32) {
     const int32_t* src = table + f.src[i] * f.table_cs;
     int32_t* dst = table + f.dst[i] * f.table_cs;
     const int full = f.tokens[i] / f.page;
-    for (int e = lane; e < full; e += 32) {
-      int p = src[e];
-      if (p < -1 || p >= n_pages) {
-        bad = true;
-        p = -1;
+    for (int e0 = lane; e0 < full; e0 += 32 * kAtOnce) {
+      int p[kAtOnce];
+      bool named[kAtOnce];
+#pragma unroll
+      for (int k = 0; k < kAtOnce; ++k) p[k] = e0 + 32 * k < full ? src[e0 + 32 * k] : -1;
+#pragma unroll
+      for (int k = 0; k < kAtOnce; ++k) named[k] = p[k] >= 0 && p[k] < n_pages && __ldcg(ref + p[k]) != 0;
+#pragma unroll
+      for (int k = 0; k < kAtOnce; ++k) {
+        if (e0 + 32 * k < full) dst[e0 + 32 * k] = named[k] ? p[k] : -1;
+        if (named[k]) atomicAdd(ref + p[k], 1);
+        bad |= !named[k] && p[k] != -1;
       }
-      dst[e] = p;
-      if (p >= 0) atomicAdd(ref + p, 1);
     }
+  }
+  if (tid < f.n) {  // the page that fork `tid` fills in part
+    int from = kNoCopy;
+    if (f.tokens[tid] % f.page != 0) {
+      const int e = f.tokens[tid] / f.page, p = table[f.src[tid] * f.table_cs + e];
+      if (p >= 0 && p < n_pages) {
+        from = p;
+        if (__ldcg(ref + p) == 0) {  // a page of its own all the same, into which nothing is copied
+          bad = true;
+          from = -1;
+        }
+      } else {
+        table[f.dst[tid] * f.table_cs + e] = -1;
+        bad |= p != -1;
+      }
+    }
+    look_s[tid] = from;
   }
   __threadfence_block();
   __syncthreads();
   if (tid == 0) {
     int n = 0;
     for (int i = 0; i < f.n; ++i) {
-      if (f.tokens[i] % f.page == 0) continue;
-      const int e = f.tokens[i] / f.page;
-      const int p = table[f.src[i] * f.table_cs + e];
-      if (p >= 0 && p < n_pages) {
-        part_s[n] = i;
-        from_s[n++] = p;
-      } else {
-        table[f.dst[i] * f.table_cs + e] = -1;
-        bad |= p != -1;
-      }
+      if (look_s[i] == kNoCopy) continue;
+      part_s[n] = i;
+      from_s[n++] = look_s[i];
     }
     n_part = n;
   }
@@ -257,6 +275,7 @@ pages_copy_kernel(const __grid_constant__ CopyGeom g, uint32_t* __restrict__ sta
     const int64_t rest = u >> 1;
     const int h = (int)(rest % g.H);
     const int2 m = g.copies.pair[rest / g.H];
+    if (m.x < 0) continue;  // nothing to copy
     if (!fc::bounds_ok((uint32_t)m.x < (uint32_t)g.pool.n_pages && (uint32_t)m.y < (uint32_t)g.pool.n_pages, status)) continue;
     uint8_t* base = (is_v ? g.pool.v_codes : g.pool.k_codes) + h * g.pool.code_hs;
     const uint8_t* from = base + m.x * g.pool.code_ps;

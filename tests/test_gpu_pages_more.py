@@ -134,3 +134,27 @@ def test_attention_small_weights_of_fp32_rows(fc, ctx, rows, d, page):
     # parts 2^-22 each, the sums n 2^-24, and a weight that is small for fp16's parts 2^-43 of the largest.
     rel = L * (2.0 ** -23 + 4 * 2.0 ** -24) + 2 * 2.0 ** -22 + n * 2.0 ** -24 + 2.0 ** -24
     assert (np.abs(f64(O)[0] - want) <= rel * want + 1.5 * 31 * 2.0 ** -43).all()
+
+
+# ------------------------------------------------------------------------------------ pages
+
+def test_fork_reports_free_pages(fc, ctx):
+    # as drop and compact do.  A free page is nobody's: it is not shared, and nothing is copied out of it
+    H, d, page, bad = 2, 64, 16, fc.STATUS_BITS["bad_index"]
+    pool, status = filled_pool(fc, 7, H, page, d, 1), status_word()
+    codes = pool.k_codes.clone()
+    ref, table = i32([1, 0, 1, 0, 0, 1, 1]), i32([[0, 1, 2, 5], [-1] * 4, [0, 2, 6, 3], [-1] * 4, [-1] * 4])
+    ctx.pages_fork(pool, ref, table, [0, 0], [1, 3], [48, 40], status=status)  # entry 1 names page 1, which is free
+    # the second fork fills entry 2 in part: page 2 is copied into the lowest free one
+    assert int(status) == bad
+    assert table.tolist() == [[0, 1, 2, 5], [0, -1, 2, -1], [0, 2, 6, 3], [0, -1, 1, -1], [-1] * 4]
+    assert ref.tolist() == [3, 1, 2, 0, 0, 1, 1]
+    codes[1] = codes[2]
+    assert torch.equal(pool.k_codes, codes)
+    status.zero_()
+    ctx.pages_fork(pool, ref, table, [2], [4], [50], status=status)  # entry 3 names page 3, free, and is filled in part
+    assert int(status) == bad and torch.equal(pool.k_codes, codes)
+    assert table[4].tolist() == [0, 2, 6, 3] and ref.tolist() == [4, 1, 3, 1, 0, 1, 2]
+    status.zero_()
+    ctx.pages_fork(pool, ref, table, [0], [4], [16], status=status)
+    assert int(status) == 0
