@@ -532,8 +532,9 @@ typedef struct {
  *   K_src, V_src     DEVICE [H, rows, d], `dtype`.
  *   row_off          HOST [W+1], non-decreasing; pos HOST [W]; W <= FC_MAX_CHUNKS.  pos[c] + rows <= 2^31 - 4097.
  *   table            DEVICE [W, table_cs] (table_cs covers every entry that is used where W > 1: rows of the table do not overlap).
- *   ref              DEVICE [n_pages] int32 or NULL: how many entries name each page (see below).  With it, a page that more
- *                    than one entry names is left as it is (FC_DEV_BAD_INDEX): fork a sequence before it is written to.
+ *   ref              DEVICE [n_pages] int32 or NULL: how many entries name each page (see below).  With it, only pages with a
+ *                    count of 1 are written to.  One that more entries name, or that is free, is left as it is
+ *                    (FC_DEV_BAD_INDEX): fork a sequence, or take its pages, before it is written to.
  * An entry outside [0, n_pages) sets FC_DEV_BAD_INDEX and its rows are dropped.  Two sequences of a call may not name the same
  * page where they write.  Needs no workspace. */
 typedef struct {

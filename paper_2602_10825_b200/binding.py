@@ -745,7 +745,7 @@ class Context:
         """Rows row_off[c] .. row_off[c+1] - 1 of K, V [H, rows, d] become tokens pos[c], ... of sequence c; returns the pool.
 
         table [sequences, entries] names the pages of each sequence.  Without row_off there is one sequence, which gets all rows.  With
-        ref, pages that several entries name are not written to (status bit bad_index)."""
+        ref, only pages that one entry names are written to, none that are shared or free (status bit bad_index)."""
         rows = K.shape[1]
         shape = (pool.H, rows, pool.d)
         kp, kh, kr = self._rows(K, "K", shape, K.dtype)

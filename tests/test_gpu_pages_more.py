@@ -158,3 +158,16 @@ def test_fork_reports_free_pages(fc, ctx):
     status.zero_()
     ctx.pages_fork(pool, ref, table, [0], [4], [16], status=status)
     assert int(status) == 0
+
+
+def test_append_writes_only_to_pages_with_one_holder(fc, ctx):
+    H, d, page = 2, 64, 16
+    K = rand((H, 40, d), 1)
+    pool, status = filled_pool(fc, 4, H, page, d, 1), status_word()
+    want = numpy_pool(pool)
+    ctx.kv8_append(K, K, pool, i32([[0, 1, 2]]), [0], ref=i32([1, 0, 1, 1]), status=status)  # page 1 is free
+    for a, b, p in ((0, 16, 0), (32, 40, 2)):
+        for which in (0, 1):
+            want.append(f64(K)[:, a:b], which, [p], 0)
+    same_pool(pool, want)
+    assert int(status) == fc.STATUS_BITS["bad_index"]
