@@ -1,5 +1,7 @@
 // Attention of few query rows over [8-bit pages | plain rows], each chunk over its first tokens and its sliding window: one pass over the
-// keys, cut into parts that a second kernel joins; also the path of fp32 tensors whatever their rows.
+// keys, cut into parts; also the path of fp32 tensors whatever their rows.  Up to sixteen parts of a tile of rows are the blocks of a thread block
+// cluster, which join through its shared memory; a second kernel joins them where a few tiles see many keys, or some chunks far more than
+// others, so that the chunks are cut into different numbers of parts.
 //
 // Bound by the bytes of the keys.  A warp takes 32 keys at a step (16 over plain rows) from its own ring in shared memory, which the copy
 // engine fills (a box of the step's rows is one instruction of one lane, and lies swizzled so that the reads below meet no bank twice),
