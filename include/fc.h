@@ -626,7 +626,9 @@ int fc_pages_compact(fc_ctx* ctx, void* stream, const fc_kv8_pool* pool, int H, 
  * Before they are divided by their sum, weights are at most 1 in the kernel for few rows and at most 2^8 in the tcgen05 kernel; the sum of
  * weights times values has to stay below 2^128, which it does where the tokens that are seen, times the largest |value|, times that bound do.
  * What lies in tokens that a chunk does not see never reaches its rows, whatever it is.  A NaN in a token that is seen makes what it reaches NaN, and so
- * does an infinity in Q.  Head strides of K and V are not 0 where there are several heads.
+ * does an infinity in Q.  One in a plain token's K or V that is seen makes what it reaches infinite or NaN, or leaves the token out where its logit is -inf;
+ * in fp32 it makes it NaN, and a magnitude in Q, K or V over plain tokens that rounds to a bf16 infinity (2^128 - 2^119 and above) counts as one.  A row
+ * all of whose logits are -inf is NaN.  Head strides of K and V are not 0 where there are several heads.
  * An entry outside [0, n_pages) that is needed sets FC_DEV_BAD_INDEX; K and V of its tokens count as zeros.
  * Deterministic.  Workspace: fc_chunk_attention_kv8_workspace_bytes() of the same arguments (0 for arguments that the call
  * refuses). */

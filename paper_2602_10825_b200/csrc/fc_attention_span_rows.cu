@@ -159,15 +159,23 @@ __device__ __forceinline__ float4 cluster_load4(uint32_t at, int rank) {
   return x;
 }
 
+// What a row gets whose weights are all 0: nothing was seen (0, and a log-sum of -inf), or, in a chunk that sees tokens, every logit was -inf (NaN).
+__device__ __forceinline__ float without_weights(const fc::SpanGeom& g, int c) {
+  bool sees = false;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) sees |= g.hi[i][c] > g.lo[i][c];
+  return sees ? __uint_as_float(0x7fc00000u) : 0.f;
+}
+
 // Four elements of virtual row v of chunk c: a sum of weights times values over kUnit, its reference and the sum of the weights.
 template <typename T>
-__device__ __forceinline__ void write_row(T* O, const fc::SpanGeom& g, int c, int hk, int v, int d4, float4 o, float ref, float l) {
-  const float inv = l > 0.f ? kUnit / l : (l == l ? 0.f : l);
+__device__ __forceinline__ void write_row(T* O, const fc::SpanGeom& g, int c, int hk, int v, int d4, float4 o, float ref, float l, float none) {
+  const float inv = l > 0.f ? kUnit / l : (l == l ? none : l);
   const int h = hk * g.group + v % g.group;
   const int64_t row = g.q_row_off[c] + v / g.group;
   if (!fc::bounds_ok(row >= 0 && row < g.q_row_off[g.W] && h >= 0 && h < g.H_q, g.status)) return;
   store4(O + h * g.o_hs + row * g.o_rs + d4, make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv));
-  if (g.lse && d4 == 0) g.lse[h * g.lse_hs + row] = l > 0.f ? (ref + log2f(l)) * 0.6931471805599453f : (l == l ? -INFINITY : l);
+  if (g.lse && d4 == 0) g.lse[h * g.lse_hs + row] = l > 0.f ? (ref + log2f(l)) * 0.6931471805599453f : (l == l && none == 0.f ? -INFINITY : inv);
 }
 
 // What a warp knows of one of its next steps over pages: the pages of its two halves (the same one, but for pages of 16 tokens; -1: none is needed, or
@@ -735,6 +743,7 @@ attention_span_rows_kernel(const __grid_constant__ CUtensorMap map_k8, const __g
         }
     }
   __syncthreads();
+  const float none = without_weights(g, c);
   auto block_o = reinterpret_cast<float(*)[D + 4]>(smem + sizeof(float) * kWarps * kRows * (D + 4));
   auto block_ml = reinterpret_cast<float2*>(block_o + kRows);
   for (int x = tid; x < rows_here * (D / 4); x += kThreads) {
@@ -753,7 +762,7 @@ attention_span_rows_kernel(const __grid_constant__ CUtensorMap map_k8, const __g
       o.x = fmaf(f, y.x, o.x); o.y = fmaf(f, y.y, o.y); o.z = fmaf(f, y.z, o.z); o.w = fmaf(f, y.w, o.w);
     }
     if (n_parts == 1) {
-      write_row<T>(O, g, c, hk, v0 + row, d4, o, mx, l);
+      write_row<T>(O, g, c, hk, v0 + row, d4, o, mx, l, none);
     } else if (g.cluster) {
       *reinterpret_cast<float4*>(&block_o[row][d4]) = o;
       if (d4 == 0) block_ml[row] = make_float2(mx, l);
@@ -789,7 +798,7 @@ attention_span_rows_kernel(const __grid_constant__ CUtensorMap map_k8, const __g
       l = fmaf(f, ml[p].y, l);
       o.x = fmaf(f, y[p].x, o.x); o.y = fmaf(f, y[p].y, o.y); o.z = fmaf(f, y[p].z, o.z); o.w = fmaf(f, y[p].w, o.w);
     }
-    write_row<T>(O, g, c, hk, v0 + row, d4, o, mx, l);
+    write_row<T>(O, g, c, hk, v0 + row, d4, o, mx, l, none);
   }
   cluster_barrier();  // the others have read this block's memory
 }
@@ -853,7 +862,7 @@ attention_span_join_kernel(T* __restrict__ O, const __grid_constant__ fc::SpanGe
     o.x += y.x; o.y += y.y; o.z += y.z; o.w += y.w;
     l += l_s[i];
   }
-  write_row<T>(O, g, c, hk, v, 4 * d4, o, m, l);
+  write_row<T>(O, g, c, hk, v, 4 * d4, o, m, l, without_weights(g, c));
 }
 
 constexpr int kMaxParts = 256;

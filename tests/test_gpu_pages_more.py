@@ -171,3 +171,59 @@ def test_append_writes_only_to_pages_with_one_holder(fc, ctx):
             want.append(f64(K)[:, a:b], which, [p], 0)
     same_pool(pool, want)
     assert int(status) == fc.STATUS_BITS["bad_index"]
+
+
+@pytest.mark.parametrize("rows", [1, 11, 140])
+@pytest.mark.parametrize("dtype, impl", IMPLS)
+def test_attention_infinities(fc, ctx, dtype, impl, rows):
+    # one in Q: NaN, of either sign.  One in K or V: what it reaches is infinite or NaN, or a token's logit is -inf and the others are left;
+    # nothing else differs, and what is not seen has no effect
+    H, d, n = 2, 64, 50
+    Q, K, V = rand((H, rows, d), 1, 1.0, dtype), rand((H, n, d), 2, 1.0, dtype), rand((H, n, d), 3, 1.0, dtype)
+    K[:, :, 0] = K[:, :, 0].abs() + 0.25
+    out = {}
+    for which in ("none", "q", "minus q", "k", "v", "unseen"):
+        q, k, v = Q.clone(), K.clone(), V.clone()
+        if which == "q":
+            q[0, 0, 0] = math.inf
+        elif which == "minus q":
+            q[0, 0, 0] = -math.inf
+        elif which == "k":
+            k[0, 20, 3] = math.inf
+        elif which == "v":
+            v[0, 20, 3] = -math.inf
+        elif which == "unseen":
+            k[0, 8, 3], v[1, 9, 3] = math.inf, -math.inf
+        O, lse = torch.full_like(Q, 9.0), torch.full((H, rows), 5.0, device="cuda")
+        ctx.chunk_attention_span(q, k, v, [0, rows], [n], [0, n], [0], i32([0]), i32([1]), O, n_sink=5, kv_begin=[13], lse=lse, impl=impl)
+        out[which] = O, lse
+    O, lse = out["none"]
+    assert torch.isfinite(O).all() and torch.isfinite(lse).all()
+    assert torch.equal(out["unseen"][0], O) and torch.equal(out["unseen"][1], lse)
+    for which in ("q", "minus q"):
+        got, got_lse = out[which]
+        assert torch.equal(got[1], O[1]) and torch.equal(got[0, 1:], O[0, 1:]) and torch.equal(got_lse[1], lse[1])
+        assert torch.isnan(got[0, 0]).all() and torch.isnan(got_lse[0, 0])
+    got = out["k"][0]  # logits of +inf or -inf: nothing else is seen, or the token is not
+    assert torch.equal(got[1], O[1])
+    per_row = torch.isnan(got[0]).all(1) | torch.isfinite(got[0]).all(1)
+    assert per_row.all() and (dtype == BF16 or torch.isnan(got[0]).all())
+    got = out["v"][0]
+    keep = torch.arange(d, device="cuda") != 3
+    assert torch.equal(got[1], O[1]) and torch.equal(got[0][:, keep], O[0][:, keep])
+    assert (torch.isnan(got[0, :, 3]) | (got[0, :, 3] == -math.inf)).all()
+
+
+@pytest.mark.parametrize("dtype, impl", IMPLS)
+def test_attention_infinities_in_queries_over_pages(fc, ctx, dtype, impl):
+    H, d, page, n, rows = 1, 64, 16, 40, 4
+    pool, t = filled_pool(fc, 3, H, page, d, 1), i32([[0, 1, 2]])
+    pool.k_codes[..., 0] = pool.k_codes[..., 0].bitwise_and(0x7f).clamp(min=8)  # positive
+    Q = rand((H, rows, d), 1, 1.0, dtype)
+    want, want_lse = torch.zeros_like(Q), torch.zeros((H, rows), device="cuda")
+    got, got_lse = torch.zeros_like(Q), torch.zeros((H, rows), device="cuda")
+    args = (pool, t, [n], None, None, [0, rows], [n], i32([0]), i32([1]))
+    ctx.chunk_attention_kv8(Q, *args, want, lse=want_lse, impl=impl)
+    Q[0, 1, 0], Q[0, 2, 0] = math.inf, -math.inf
+    ctx.chunk_attention_kv8(Q, *args, got, lse=got_lse, impl=impl)
+    assert torch.equal(got[0, ::3], want[0, ::3]) and torch.isnan(got[0, 1:3]).all() and torch.isnan(got_lse[0, 1:3]).all()
