@@ -281,7 +281,7 @@ int attend(fc_ctx* ctx, void* stream, const fc_attn_desc* desc, const void* Q, c
   auto before = [](void* arg) -> int {
     const Unpack& x = *(const Unpack*)arg;
     const int64_t hs = (int64_t)x.t->rows * x.g->d;
-    return fc::kv8_unpack_launch(x.st, x.g->pool, x.g->H_kv, x.g->d, x.g->table, x.g->table_cs, x.t->jobs, x.k, x.v, FC_BF16, hs, x.g->d, hs,
+    return fc::kv8_unpack_launch(x.st, x.g->pool, x.g->H_kv, x.g->d, x.g->table, x.g->table_cs, x.t->jobs, x.k, x.v, x.t->rows, FC_BF16, hs, x.g->d, hs,
                                  x.g->d, x.g->status, x.counter);
   };
   t.jobs.active_ids = active_ids;

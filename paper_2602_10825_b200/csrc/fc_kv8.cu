@@ -234,6 +234,7 @@ kv8_append_kernel(const T* __restrict__ K, const T* __restrict__ V, const __grid
   for (int i = 0; i < kVec; ++i) {
     const int row = row0 + i * kRowsApart;
     uint2* at = reinterpret_cast<uint2*>(codes) + tid + i * kGroup;
+    if (row < hi && !fc::bounds_ok(row < page && tid + i * kGroup < page * kRowVecs, status)) continue;
     if (row >= lo && row < hi) *at = slow ? codes8_any<T>(x[i], s) : codes8_finite(x[i], s, r);
     else if (row < lo && s > s_old) *at = again8(*at, s_old, s);
   }
@@ -356,11 +357,10 @@ int check_common(const fc_kv8_rows* desc, int dtype, const int32_t* row_off, con
 namespace fc {
 
 int kv8_unpack_launch(cudaStream_t st, const Kv8View& src, int H, int d, const int32_t* table, int64_t table_cs, const Kv8Jobs& jobs,
-                      void* K_dst, void* V_dst, int dtype, int64_t k_hs, int64_t k_rs, int64_t v_hs, int64_t v_rs,
+                      void* K_dst, void* V_dst, int64_t dst_rows, int dtype, int64_t k_hs, int64_t k_rs, int64_t v_hs, int64_t v_rs,
                       uint32_t* status, uint32_t* clear) {
-  int64_t end = 0, blocks = 0;
-  for (int i = 0; i < jobs.n; ++i) end = std::max<int64_t>(end, (int64_t)jobs.job[i].dst_row + jobs.job[i].n);
-  UnpackGeom g = {jobs, {}, k_hs, k_rs, v_hs, v_rs, table_cs, end, src, table, status, clear};
+  int64_t blocks = 0;
+  UnpackGeom g = {jobs, {}, k_hs, k_rs, v_hs, v_rs, table_cs, dst_rows, src, table, status, clear};
   const int rows = kUnpackRows * kUnpackThreads / (d / (dtype == FC_F32 ? 4 : 8));
   for (int i = 0; i < jobs.n; ++i) g.block_end[i] = (int32_t)(blocks += ((int64_t)jobs.job[i].n + rows - 1) / rows);
   if (blocks == 0 || (!K_dst && !V_dst)) return FC_OK;
@@ -453,5 +453,5 @@ extern "C" int fc_kv8_unpack(fc_ctx* ctx, void* stream, const fc_kv8_rows* desc,
     if (row_off[c + 1] > row_off[c]) jobs.job[jobs.n++] = {c, first[c], row_off[c + 1] - row_off[c], row_off[c]};
   FC_DEVICE_GUARD(ctx);
   return fc::kv8_unpack_launch((cudaStream_t)stream, fc::kv8_view(*pool), desc->H, desc->d, table, table_cs, jobs, K_dst, V_dst,
-                               dtype, desc->k_hs, desc->k_rs, desc->v_hs, desc->v_rs, status, nullptr);
+                               rows, dtype, desc->k_hs, desc->k_rs, desc->v_hs, desc->v_rs, status, nullptr);
 }

@@ -90,10 +90,10 @@ struct Kv8Jobs {
 };
 static_assert(FC_MAX_CHUNKS <= 64, "a bit a chunk");
 
-// Unpacks jobs into [H, rows, d] tensors (fc_kv8.cu); either destination may be NULL.  `clear`: a word that is set to zero on the
+// Unpacks jobs into [H, dst_rows, d] tensors (fc_kv8.cu); either destination may be NULL.  `clear`: a word that is set to zero on the
 // way, or NULL.  A kernel launched by launch_pdl behind it may start early.
 int kv8_unpack_launch(cudaStream_t st, const Kv8View& src, int H, int d, const int32_t* table, int64_t table_cs, const Kv8Jobs& jobs,
-                      void* K_dst, void* V_dst, int dtype, int64_t k_hs, int64_t k_rs, int64_t v_hs, int64_t v_rs,
+                      void* K_dst, void* V_dst, int64_t dst_rows, int dtype, int64_t k_hs, int64_t k_rs, int64_t v_hs, int64_t v_rs,
                       uint32_t* status, uint32_t* clear);
 
 }  // namespace fc

@@ -227,3 +227,17 @@ def test_attention_infinities_in_queries_over_pages(fc, ctx, dtype, impl):
     Q[0, 1, 0], Q[0, 2, 0] = math.inf, -math.inf
     ctx.chunk_attention_kv8(Q, *args, got, lse=got_lse, impl=impl)
     assert torch.equal(got[0, ::3], want[0, ::3]) and torch.isnan(got[0, 1:3]).all() and torch.isnan(got_lse[0, 1:3]).all()
+
+
+def test_on_the_bounds_checking_build(fc):
+    # the calls of this file whose stores are guarded there; every test counts its status
+    import os
+    import subprocess
+    import sys
+    from paper_2602_10825_b200 import build as fc_build
+    fc_build.build(debug_bounds=True)
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    run = subprocess.run([sys.executable, "-m", "pytest", "-x", "-q", "-p", "no:cacheprovider", "tests/test_gpu_pages_more.py", "-m", "gpu", "-k",
+                          "shared_sequence or free_pages or one_holder or captured"],
+                         cwd=root, env={**os.environ, "FC_LIB": "debug"}, capture_output=True, text=True, timeout=600)
+    assert run.returncode == 0, run.stdout[-3000:] + run.stderr[-2000:]
