@@ -241,3 +241,41 @@ def test_on_the_bounds_checking_build(fc):
                           "shared_sequence or free_pages or one_holder or captured"],
                          cwd=root, env={**os.environ, "FC_LIB": "debug"}, capture_output=True, text=True, timeout=600)
     assert run.returncode == 0, run.stdout[-3000:] + run.stderr[-2000:]
+
+
+def test_pages_and_append_captured_move_the_same_bytes(fc, ctx):
+    # the pool, the counts and the table are put back before each replay: all that a turn writes is the replay's own
+    H, d, page = 2, 64, 16
+    pool = filled_pool(fc, 20, H, page, d, 1)
+    ref, table = pool.tables(3, 8)
+    K, V, status = rand((H, 20, d), 1), rand((H, 20, d), 2), status_word()
+    ctx.pages_take(ref, table, [0, 0, 0], [3, 0, 3])
+    ctx.pages_drop(ref, table, [0, 0, 0], [0, 0, 1])  # a hole for the compaction
+    state = [pool.k_codes, pool.k_scales, pool.v_codes, pool.v_scales, ref, table, status]
+    start = [x.clone() for x in state]
+
+    def turn():
+        ctx.pages_fork(pool, ref, table, [0], [1], [37], status=status)
+        ctx.kv8_append(K, V, pool, table[1:2], [37], ref=ref, status=status)  # its rows from 48 on have no page: reported
+        ctx.pages_take(ref, table, [3, 4, 3], [4, 5, 3], status=status)
+        ctx.pages_drop(ref, table, [0, 0, 1], [1, 0, 3], status=status)
+        ctx.pages_compact(pool, ref, table, status=status)
+    turn()
+    torch.cuda.synchronize()
+    want = [x.clone() for x in state]
+    assert int(status) == fc.STATUS_BITS["bad_index"]
+    assert not torch.equal(want[0], start[0]) and not torch.equal(want[3], start[3])
+    graph = torch.cuda.CUDAGraph()
+    for x, y in zip(state, start):
+        x.copy_(y)
+    with torch.cuda.graph(graph):
+        turn()
+    torch.cuda.synchronize()
+    assert all(torch.equal(x, y) for x, y in zip(state, start))  # a capture runs nothing
+    for _ in range(3):
+        for x, y in zip(state, start):
+            x.copy_(y)
+        graph.replay()
+        torch.cuda.synchronize()
+        for i, (x, y) in enumerate(zip(state, want)):
+            assert torch.equal(x, y), f"tensor {i}"
