@@ -233,8 +233,8 @@ pages_compact_kernel(int32_t* __restrict__ ref, int n_pages, Copies copies, int3
       if (p + i < used) {
         if (c[i] == 0) copies.pair[hole++].y = p + i;
       } else {
-        copies.place[p + i] = c[i] != 0 ? mover : -1;
         if (c[i] != 0) copies.pair[mover++].x = p + i;
+        else copies.place[p + i] = -1;
       }
     }
     holes += (int)(total & 0xffffu);
