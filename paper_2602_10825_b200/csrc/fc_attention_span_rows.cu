@@ -937,7 +937,7 @@ Cut cut_of(const fc_ctx* ctx, const fc::SpanGeom& g, int nt, const Units* units)
     const double us = 4.8 + (n > 1 ? 0.5 + 0.1 * n : 0) + time_of((double)all * n, (double)((most + n - 1) / n), room, n > 1);
     if (n == 1 || us < best.us) best = {us, n, 0};
   }
-  if ((double)all * kMaxCluster >= places && work >= 0.5 * (double)most * all) return best;  // nothing that clusters do not reach
+  if (0.95 * best.us <= 4.8 + 3.5 + u.full * work / sm) return best;  // no cut by size is below that
   for (int64_t n = 2; n <= kMaxParts && most >= 2 * kWarps * n; n += (n + 7) / 8) {
     const int64_t size = (most + n - 1) / n;
     double blocks = 0, rows = 0;
