@@ -1,7 +1,7 @@
 // Attention of few query rows over [8-bit pages | plain rows], each chunk over its first tokens and its sliding window: one pass over the
 // keys, cut into parts; also the path of fp32 tensors whatever their rows.  Up to sixteen parts of a tile of rows are the blocks of a thread block
-// cluster, which join through its shared memory; a second kernel joins them where a few tiles see many keys, or some chunks far more than
-// others, so that the chunks are cut into different numbers of parts.
+// cluster, which join through its shared memory; a second kernel joins them where that is faster: a few tiles that see many keys, chunks that
+// see far more than others, clusters that would leave much of the device empty.
 //
 // Bound by the bytes of the keys.  A warp takes 32 keys at a step (16 over plain rows) from its own ring in shared memory, which the copy
 // engine fills (a box of the step's rows is one instruction of one lane, and lies swizzled so that the reads below meet no bank twice),
@@ -160,7 +160,7 @@ __device__ __forceinline__ float4 cluster_load4(uint32_t at, int rank) {
 }
 
 // What a row gets whose weights are all 0: nothing was seen (0, and a log-sum of -inf), or, in a chunk that sees tokens, every logit was -inf (NaN).
-__device__ __forceinline__ float without_weights(const fc::SpanGeom& g, int c) {
+__device__ __noinline__ float without_weights(const fc::SpanGeom& g, int c) {
   bool sees = false;
 #pragma unroll
   for (int i = 0; i < 4; ++i) sees |= g.hi[i][c] > g.lo[i][c];
@@ -169,13 +169,13 @@ __device__ __forceinline__ float without_weights(const fc::SpanGeom& g, int c) {
 
 // Four elements of virtual row v of chunk c: a sum of weights times values over kUnit, its reference and the sum of the weights.
 template <typename T>
-__device__ __forceinline__ void write_row(T* O, const fc::SpanGeom& g, int c, int hk, int v, int d4, float4 o, float ref, float l, float none) {
-  const float inv = l > 0.f ? kUnit / l : (l == l ? none : l);
+__device__ __forceinline__ void write_row(T* O, const fc::SpanGeom& g, int c, int hk, int v, int d4, float4 o, float ref, float l) {
+  const float inv = l > 0.f ? kUnit / l : (l == l ? without_weights(g, c) : l);
   const int h = hk * g.group + v % g.group;
   const int64_t row = g.q_row_off[c] + v / g.group;
   if (!fc::bounds_ok(row >= 0 && row < g.q_row_off[g.W] && h >= 0 && h < g.H_q, g.status)) return;
   store4(O + h * g.o_hs + row * g.o_rs + d4, make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv));
-  if (g.lse && d4 == 0) g.lse[h * g.lse_hs + row] = l > 0.f ? (ref + log2f(l)) * 0.6931471805599453f : (l == l && none == 0.f ? -INFINITY : inv);
+  if (g.lse && d4 == 0) g.lse[h * g.lse_hs + row] = l > 0.f ? (ref + log2f(l)) * 0.6931471805599453f : (inv == 0.f ? -INFINITY : inv);
 }
 
 // What a warp knows of one of its next steps over pages: the pages of its two halves (the same one, but for pages of 16 tokens; -1: none is needed, or
@@ -743,7 +743,6 @@ attention_span_rows_kernel(const __grid_constant__ CUtensorMap map_k8, const __g
         }
     }
   __syncthreads();
-  const float none = without_weights(g, c);
   auto block_o = reinterpret_cast<float(*)[D + 4]>(smem + sizeof(float) * kWarps * kRows * (D + 4));
   auto block_ml = reinterpret_cast<float2*>(block_o + kRows);
   for (int x = tid; x < rows_here * (D / 4); x += kThreads) {
@@ -762,7 +761,7 @@ attention_span_rows_kernel(const __grid_constant__ CUtensorMap map_k8, const __g
       o.x = fmaf(f, y.x, o.x); o.y = fmaf(f, y.y, o.y); o.z = fmaf(f, y.z, o.z); o.w = fmaf(f, y.w, o.w);
     }
     if (n_parts == 1) {
-      write_row<T>(O, g, c, hk, v0 + row, d4, o, mx, l, none);
+      write_row<T>(O, g, c, hk, v0 + row, d4, o, mx, l);
     } else if (g.cluster) {
       *reinterpret_cast<float4*>(&block_o[row][d4]) = o;
       if (d4 == 0) block_ml[row] = make_float2(mx, l);
@@ -798,7 +797,7 @@ attention_span_rows_kernel(const __grid_constant__ CUtensorMap map_k8, const __g
       l = fmaf(f, ml[p].y, l);
       o.x = fmaf(f, y[p].x, o.x); o.y = fmaf(f, y[p].y, o.y); o.z = fmaf(f, y[p].z, o.z); o.w = fmaf(f, y[p].w, o.w);
     }
-    write_row<T>(O, g, c, hk, v0 + row, d4, o, mx, l, none);
+    write_row<T>(O, g, c, hk, v0 + row, d4, o, mx, l);
   }
   cluster_barrier();  // the others have read this block's memory
 }
@@ -862,7 +861,7 @@ attention_span_join_kernel(T* __restrict__ O, const __grid_constant__ fc::SpanGe
     o.x += y.x; o.y += y.y; o.z += y.z; o.w += y.w;
     l += l_s[i];
   }
-  write_row<T>(O, g, c, hk, v, 4 * d4, o, m, l, without_weights(g, c));
+  write_row<T>(O, g, c, hk, v, 4 * d4, o, m, l);
 }
 
 constexpr int kMaxParts = 256;
@@ -900,10 +899,11 @@ UnitUs unit_us(const fc::SpanGeom& g, int nt, double plain) {  // plain: their s
 // How a call's keys are cut for tiles of 8 nt rows.
 //   in clusters   every tile's keys into the same number of parts, at most 16, whose blocks are a cluster and join themselves
 //   by size       every chunk's into parts of at most `size` units, which a second kernel joins (3.5 us and its bytes): where a few tiles see many keys,
-//                 or some chunks far more than others
+//                 some chunks far more than others, or the clusters that fit leave much of the device empty (64 rows of 24 heads over 28000 tokens in
+//                 pages: 100 us in three parts, 140 in clusters of two)
 // of which the fastest is taken, by the times above; a call takes 4.8 us besides.
-// Of 60 calls at random, of 5 to 60 us, the choice was as fast as the best of sixteen cuts in the median, within 10 % for nine in ten, and at most 15 %
-// above it; chunks that the device leaves out, which the host does not know, can cost more (63 % where it left out five of six).
+// Of 60 calls at random, of 5 to 60 us, the choice was within 1 % of the best of 32 cuts in the median, within 10 % for five in six, and at most 25 %
+// above it; chunks that the device leaves out, which the host does not know, can cost more (41 and 63 % were seen where it left out five of six).
 struct Cut {
   double us;
   int32_t cluster;
