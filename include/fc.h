@@ -616,7 +616,7 @@ int fc_pages_compact(fc_ctx* ctx, void* stream, const fc_kv8_pool* pool, int H, 
  *                    reads the pages in place and is also the path of fp32.
  *   pool, table      as above; both may be NULL if every cache_len is 0.
  *   cache_len        HOST [W] or NULL (all 0).  kv_visible_len HOST [W]; kv_begin HOST [W] or NULL (all 0: no sliding window); window_first
- *                    HOST [W] or NULL (all 0).  Tokens that no chunk sees need no page.
+ *                    HOST [W] or NULL (all 0).  Tokens that no active chunk sees need no page.
  *   K, V, seg_*      as in fc_chunk_attention_kv4: the plain tokens; n_seg 0 if there are none.
  * Everything else is as in fc_chunk_attention_kv4: the active list, grouped heads, rows of inactive chunks.  Logits, maxima, sums and outputs are kept
  * in fp32.  Softmax weights are rounded on their way to V: for fp32 tensors by 2^-22 at most (over pages by 2^-43 of the row's largest so far
@@ -629,7 +629,7 @@ int fc_pages_compact(fc_ctx* ctx, void* stream, const fc_kv8_pool* pool, int H, 
  * does an infinity in Q.  One in a plain token's K or V that is seen makes what it reaches infinite or NaN, or leaves the token out where its logit is -inf;
  * in fp32 it makes it NaN, and a magnitude in Q, K or V over plain tokens that rounds to a bf16 infinity (2^128 - 2^119 and above) counts as one.  A row
  * all of whose logits are -inf is NaN.  Head strides of K and V are not 0 where there are several heads.
- * An entry outside [0, n_pages) that is needed sets FC_DEV_BAD_INDEX; K and V of its tokens count as zeros.
+ * An entry outside [0, n_pages) of whose tokens an active chunk sees one sets FC_DEV_BAD_INDEX; K and V of its tokens count as zeros.
  * Deterministic.  Workspace: fc_chunk_attention_kv8_workspace_bytes() of the same arguments (0 for arguments that the call
  * refuses). */
 size_t fc_chunk_attention_kv8_workspace_bytes(const fc_ctx* ctx, const fc_attn_desc* desc, int dtype, int page, int64_t table_cs,
